@@ -417,6 +417,116 @@ typedef enum {
 } cmpq_kernel;
 cmpq_status cmpq_kernel_resources(cmpq_kernel k, int* registers, int* static_smem_bytes);
 
+/* ---- serving in 8 bits: linear layers ----------------------------------------------------------
+ * (No counterpart in the paper, which quantizes weights only: these calls hold a served layer's
+ * activations, and the cache below its keys and values, in 8-bit integers.)
+ *
+ * cmpq_quantize_tokens: codes and scale of every row t of X [n][ldx >= d] of `dt`:
+ *   scale[t] = max_j |x_tj| * fl(1/127)      codes[t][j] = clamp(rint(x_tj * fl(1/scale[t])), -127, 127)
+ * every step one fp32 operation, ties to even; scale and codes are 0 where the row's largest magnitude is
+ * below 2^-120.  codes: [n][ldc] int8, ldc >= d a multiple of 16, base 16-byte aligned; the bytes from d
+ * up to the next multiple of 16 are set to 0.  The same call on a [d_out][d_in] weight gives the weight codes
+ * and channel scales that the products below take.  n may be 0. */
+cmpq_status cmpq_quantize_tokens(const void* X, cmpq_dtype dt, int64_t n, int64_t d, int64_t ldx, int8_t* codes,
+                                 int64_t ldc, float* scale, int32_t* nonfinite, void* stream);
+
+/* cmpq_matmul_i8: y[t][o] = fl16(fl(fl((float)(sum_j xc[t][j] * wc[o][j]) * xs[t]) * w_scale[o]) + bias[o])
+ * with the sum exact in int32 (d_in <= CMPQ_MAX_D_IN_I8).  xc [n][ldxc], wc [d_out][ldwc]: int8, bases
+ * 16-byte aligned, leading dimensions multiples of 16 (what lies between d_in and the leading dimension does
+ * not matter); bias [d_out] of `dt` or NULL; y [n][ldy >= d_out] of `dt`.  d_out <= CMPQ_MAX_D_IN.
+ * cmpq_linear_i8: both steps in one call, X [n][ldx] of `dt` as in cmpq_quantize_tokens.
+ * ws: cmpq_linear_i8_ws_bytes(n, d_in, d_out) for either call (0 for arguments out of range; n may be 0, then
+ * nothing is done).  Large products run on tensor maps made from the arguments inside the call. */
+#define CMPQ_MAX_D_IN_I8 131072
+size_t cmpq_linear_i8_ws_bytes(int64_t n, int64_t d_in, int64_t d_out);
+cmpq_status cmpq_matmul_i8(const int8_t* xc, int64_t ldxc, const float* xs, const int8_t* wc, int64_t ldwc,
+                           const float* w_scale, const void* bias, cmpq_dtype dt, int64_t n, int64_t d_in,
+                           int64_t d_out, void* y, int64_t ldy, void* ws, size_t ws_bytes, void* stream);
+cmpq_status cmpq_linear_i8(const void* X, cmpq_dtype dt, int64_t n, int64_t d_in, int64_t ldx, const int8_t* wc,
+                           int64_t ldwc, const float* w_scale, const void* bias, int64_t d_out, void* y, int64_t ldy,
+                           int32_t* nonfinite, void* ws, size_t ws_bytes, void* stream);
+
+/* ---- serving in 8 bits: paged cache of keys and values -----------------------------------------
+ * A cache is n_pages pages of page_tokens tokens.  Codes are [n_pages][n_kv_heads][page_tokens][head_dim]
+ * int8 in [-127, 127], 16-byte aligned; scales [n_pages][n_kv_heads] fp32: one per page and head, for keys
+ * and for values, either 0 or in [2^-60, 2^60]; a value is code * scale.
+ * head_dim 64, 128 or 256; page_tokens 16, 32, 64 or 128 (else CMPQ_ERR_UNSUPPORTED).
+ *
+ * A batch names the sequences of a call: sequence s holds lens[s] tokens AFTER the call, of which the
+ * tok_off[s+1] - tok_off[s] last ones are the call's (rows tok_off[s].. of its token arrays; tok_off[0] = 0,
+ * not decreasing, tok_off[n_seq] <= n_tok; a sequence may have none; rows past tok_off[n_seq] are left
+ * alone).  Token p of sequence s lies in page table[s][p / page_tokens], entries past the last token are
+ * never read.  tok_off, lens and table are device arrays; n_seq <= 65536, n_tok < 2^31.
+ *
+ * `word` (optional device int32, zeroed by the caller): the calls OR into it bit 0 when a key or value
+ * that they quantize is a NaN or an infinity (rotated keys count), and bit 2 when a length is negative or above max_len, a
+ * count of new tokens is above max_new or above the sequence's length (append and read), or a table entry
+ * is no page: such tokens and pages are left out, nothing out of range is read or written, and the outputs of
+ * that sequence are unspecified.  cmpq_check_cache waits for the stream and answers CMPQ_OK,
+ * CMPQ_ERR_NONFINITE (bit 0) or CMPQ_ERR_INVALID_ARG (bit 2). */
+typedef struct {
+    int8_t* k_codes;
+    float* k_scale;
+    int8_t* v_codes;
+    float* v_scale;
+    int64_t n_pages;
+    int32_t n_kv_heads;
+    int32_t head_dim;
+    int32_t page_tokens;
+} cmpq_cache;
+
+typedef struct {
+    const int32_t* tok_off; /* [n_seq + 1] */
+    const int32_t* lens;    /* [n_seq] */
+    const int32_t* table;   /* [n_seq][ld_table] */
+    int64_t ld_table;
+    int64_t n_seq;
+    int64_t n_tok;
+} cmpq_batch;
+
+cmpq_status cmpq_check_cache(const int32_t* word, void* stream);
+
+/* cmpq_cache_append: rotates the new keys by their positions and writes them and the new values into their
+ * pages.  k, v: [n_tok][ldk / ldv >= n_kv_heads * head_dim] of `dt`, the heads of a token next to each other.
+ * Rotation of the first rot_dim entries of a head (even, 0 for none): entry pair (a, b) = (i, i + rot_dim/2),
+ * or (2i, 2i+1) with `interleaved`, becomes (a c - b s, b c + a s) with c, s = cos/sin[position][i], fp32
+ * arrays [n_pos][rot_dim/2]; every step one fp32 operation.  A token at a position >= n_pos is bit 2 of `word`.
+ * Per page and head, with S the scale that stands there when the page holds earlier tokens of the sequence,
+ * else 0:
+ *   S' = max(S, clamp(fl(max |new values of the page| * fl(1/127)), 2^-60, 2^60))
+ *   new codes      clamp(rint(fl(x * fl(1/S'))), -127, 127)
+ *   earlier codes  rint(fl(c * fl(S * fl(1/S')))) when S' > S, unchanged otherwise
+ * q (optional): [n_tok][ldq >= n_heads * head_dim] queries of the same tokens, rotated likewise, rounded to
+ * `dt` and written to q_out [n_tok][ldqo]; q_out may be q itself.  Pages of different sequences of one call
+ * must not be the same page where one of them is written. */
+cmpq_status cmpq_cache_append(const cmpq_cache* cache, const cmpq_batch* batch, const void* k, int64_t ldk,
+                              const void* v, int64_t ldv, cmpq_dtype dt, const float* cos, const float* sin,
+                              int64_t n_pos, int32_t rot_dim, int32_t interleaved, const void* q, int64_t ldq,
+                              int32_t n_heads, void* q_out, int64_t ldqo, int32_t* word, void* stream);
+
+/* cmpq_cache_read: the keys and values of the batch's tokens (as the cache holds them: rotated, quantized) as
+ * 16-bit values, k_out, v_out [n_tok][ldo >= n_kv_heads * head_dim], fl16(code * scale). */
+cmpq_status cmpq_cache_read(const cmpq_cache* cache, const cmpq_batch* batch, cmpq_dtype dt, void* k_out, void* v_out,
+                            int64_t ldo, int32_t* word, void* stream);
+
+/* cmpq_cache_attention: for query row t (position p, head h, its key-value head h / (n_heads / n_kv_heads))
+ *   out[t][h] = sum_j softmax_j(scale * q[t][h] . k_j) v_j    over the visible tokens j of its sequence:
+ * j <= p, and j > p - window when window > 0; with causal = 0 all lens[s] tokens (window must be 0 then).
+ * A row that sees no token (a position below 0, a sequence of length 0) is 0.  lse (optional, fp32
+ * [n_tok][n_heads]) receives the natural logarithm of the softmax's sum, -infinity for such a row.
+ * q [n_tok][ldq], out [n_tok][ldo] of `dt`, heads next to each other; queries finite.
+ * max_new >= every count of new tokens and max_len >= every length are the caller's bounds (they choose the
+ * kernel and size the work space).  Probabilities and sums in fp32, products on the tensor cores in fp16 with
+ * fp32 accumulation: codes are exact there, a query row is scaled by a power of two into fp16's range, and
+ * probabilities are rounded to fp16.
+ * ws: cmpq_cache_attention_ws_bytes(n_seq, n_tok, max_new, max_len, n_heads, n_kv_heads, head_dim). */
+size_t cmpq_cache_attention_ws_bytes(int64_t n_seq, int64_t n_tok, int64_t max_new, int64_t max_len, int32_t n_heads,
+                                     int32_t n_kv_heads, int32_t head_dim);
+cmpq_status cmpq_cache_attention(const cmpq_cache* cache, const cmpq_batch* batch, const void* q, int64_t ldq,
+                                 cmpq_dtype dt, int32_t n_heads, int64_t max_new, int64_t max_len, float scale,
+                                 int32_t causal, int64_t window, void* out, int64_t ldo, float* lse, int32_t* word,
+                                 void* ws, size_t ws_bytes, void* stream);
+
 /* ---- host helpers (pure functions, no GPU work) ----------------------------------------------- */
 size_t cmpq_workspace_bytes(cmpq_op op, int64_t d_in, int64_t d_out);
 /* Algorithm 1 in rank form: how many channels get 2 and 4 bits. */

@@ -5,4 +5,4 @@ calls for one layer, `inputs` generates seeded synthetic layers, `build` compile
 Nothing is loaded at import time; the first call into `binding` loads libcmpq.so and raises if
 it has not been built.
 """
-__all__ = ["binding", "pipeline", "inputs", "build"]
+__all__ = ["binding", "pipeline", "serving", "inputs", "build"]

@@ -30,7 +30,25 @@ EXPORTS = (
     "cmpq_sweep_cache_bytes", "cmpq_sweep_begin", "cmpq_sweep_budget", "cmpq_sweep_budget_pack",
     "cmpq_quantize_layer_packed", "cmpq_protect_quantize_pack", "cmpq_check_finite",
     "cmpq_matvec_f16lut", "cmpq_lut_bytes", "cmpq_store_lut", "cmpq_load_lut", "cmpq_table_bits_per_weight",
+    "cmpq_quantize_tokens", "cmpq_matmul_i8", "cmpq_linear_i8", "cmpq_linear_i8_ws_bytes", "cmpq_check_cache",
+    "cmpq_cache_append", "cmpq_cache_read", "cmpq_cache_attention", "cmpq_cache_attention_ws_bytes",
 )
+
+MAX_D_IN_I8 = 131072
+
+
+class Cache(ctypes.Structure):
+    """cmpq_cache"""
+    _fields_ = [("k_codes", ctypes.c_void_p), ("k_scale", ctypes.c_void_p), ("v_codes", ctypes.c_void_p),
+                ("v_scale", ctypes.c_void_p), ("n_pages", ctypes.c_int64), ("n_kv_heads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("page_tokens", ctypes.c_int32)]
+
+
+class Batch(ctypes.Structure):
+    """cmpq_batch"""
+    _fields_ = [("tok_off", ctypes.c_void_p), ("lens", ctypes.c_void_p), ("table", ctypes.c_void_p),
+                ("ld_table", ctypes.c_int64), ("n_seq", ctypes.c_int64), ("n_tok", ctypes.c_int64)]
+
 
 _LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libcmpq.so")
 _lib = None
@@ -124,6 +142,24 @@ def lib():
         L.cmpq_alu_probe.restype = ci
         L.cmpq_kernel_resources.argtypes = [ci, ctypes.POINTER(ci), ctypes.POINTER(ci)]
         L.cmpq_kernel_resources.restype = ci
+        i32, f32 = ctypes.c_int32, ctypes.c_float
+        cache, batch = ctypes.POINTER(Cache), ctypes.POINTER(Batch)
+        L.cmpq_quantize_tokens.argtypes = [vp, ci, i64, i64, i64, vp, i64, vp, vp, vp]
+        L.cmpq_matmul_i8.argtypes = [vp, i64, vp, vp, i64, vp, vp, ci, i64, i64, i64, vp, i64, vp, sz, vp]
+        L.cmpq_linear_i8.argtypes = [vp, ci, i64, i64, i64, vp, i64, vp, vp, i64, vp, i64, vp, vp, sz, vp]
+        L.cmpq_linear_i8_ws_bytes.argtypes = [i64, i64, i64]
+        L.cmpq_check_cache.argtypes = [vp, vp]
+        L.cmpq_cache_append.argtypes = [cache, batch, vp, i64, vp, i64, ci, vp, vp, i64, i32, i32, vp, i64, i32, vp,
+                                        i64, vp, vp]
+        L.cmpq_cache_read.argtypes = [cache, batch, ci, vp, vp, i64, vp, vp]
+        L.cmpq_cache_attention.argtypes = [cache, batch, vp, i64, ci, i32, i64, i64, f32, i32, i64, vp, i64, vp, vp,
+                                           vp, sz, vp]
+        L.cmpq_cache_attention_ws_bytes.argtypes = [i64, i64, i64, i64, i32, i32, i32]
+        for name in ("cmpq_quantize_tokens", "cmpq_matmul_i8", "cmpq_linear_i8", "cmpq_check_cache", "cmpq_cache_append",
+                     "cmpq_cache_read", "cmpq_cache_attention"):
+            getattr(L, name).restype = ci
+        L.cmpq_linear_i8_ws_bytes.restype = sz
+        L.cmpq_cache_attention_ws_bytes.restype = sz
         L.cmpq_status_string.argtypes = [ci]
         L.cmpq_status_string.restype = ctypes.c_char_p
         _lib = L
@@ -417,3 +453,84 @@ def cmpq_transpose16(src, dst):
     dtype_code(src)
     _check(lib().cmpq_transpose16(_ptr(src), rows, cols, src.stride(0), _ptr(dst), dst.stride(0), _stream()),
            "cmpq_transpose16")
+
+
+# ---- serving in 8 bits -----------------------------------------------------------------------------------------
+
+def _rows(t, width, name):
+    """Leading dimension of a 2-D or 3-D tensor whose rows of `width` elements are contiguous."""
+    inner = t.stride(-1) == 1 and (t.dim() == 2 or t.shape[1] == 1 or t.stride(1) == t.shape[2])
+    if not inner or (t.shape[0] and t[0].numel() != width):
+        raise ValueError("%s needs contiguous rows of %d elements, got shape %s, strides %s"
+                         % (name, width, tuple(t.shape), tuple(t.stride())))
+    return t.stride(0) if t.shape[0] > 1 else width
+
+
+def cmpq_linear_i8_ws_bytes(n, d_in, d_out):
+    return int(lib().cmpq_linear_i8_ws_bytes(n, d_in, d_out))
+
+
+def cmpq_quantize_tokens(X, codes, scale, nonfinite=None):
+    """codes (int8 [n][d], rows on 16 bytes) and scale (fp32 [n]) of every row of X (fp16/bf16 [n][d])."""
+    n, d = X.shape
+    _check(lib().cmpq_quantize_tokens(_ptr(X), dtype_code(X), n, d, _rows(X, d, "X"), _ptr(codes),
+                                      codes.stride(0) if n else (d + 15) // 16 * 16, _ptr(scale), _ptr(nonfinite),
+                                      _stream()), "cmpq_quantize_tokens")
+
+
+def cmpq_matmul_i8(xc, xs, wc, w_scale, bias, y, ws):
+    """y [n][d_out] (fp16/bf16) = xc [n][d_in] times wc [d_out][d_in] (int8), scaled by xs and w_scale, plus bias."""
+    n, d_in = xc.shape
+    _check(lib().cmpq_matmul_i8(_ptr(xc), xc.stride(0) if n else (d_in + 15) // 16 * 16, _ptr(xs), _ptr(wc), wc.stride(0),
+                                _ptr(w_scale), _ptr(bias), dtype_code(y), n, d_in, wc.shape[0], _ptr(y),
+                                _rows(y, wc.shape[0], "y"), _ptr(ws), ws.numel(), _stream()), "cmpq_matmul_i8")
+
+
+def cmpq_linear_i8(X, wc, w_scale, bias, y, ws, nonfinite=None):
+    """y = the 8-bit linear layer (wc, w_scale, bias) of X (fp16/bf16 [n][d_in])."""
+    n, d_in = X.shape
+    _check(lib().cmpq_linear_i8(_ptr(X), dtype_code(X), n, d_in, _rows(X, d_in, "X"), _ptr(wc), wc.stride(0),
+                                _ptr(w_scale), _ptr(bias), wc.shape[0], _ptr(y), _rows(y, wc.shape[0], "y"),
+                                _ptr(nonfinite), _ptr(ws), ws.numel(), _stream()), "cmpq_linear_i8")
+
+
+def cmpq_check_cache(word):
+    """Waits for the current stream; raises CmpqError when a cache call reported something in `word`."""
+    _check(lib().cmpq_check_cache(_ptr(word), _stream()), "cmpq_check_cache")
+
+
+def cmpq_cache_append(cache, batch, k, v, cos=None, sin=None, interleaved=False, q=None, q_out=None, word=None):
+    """cache, batch: Cache and Batch structures.  k, v: [n_tok][n_kv][d]; q, q_out: [n_tok][n_heads][d] or None;
+    cos, sin: fp32 [n_pos][rot_dim / 2] or None."""
+    row = cache.n_kv_heads * cache.head_dim
+    heads = q.shape[1] if q is not None else 0
+    qrow = heads * cache.head_dim
+    _check(lib().cmpq_cache_append(cache, batch, _ptr(k), _rows(k, row, "k"), _ptr(v), _rows(v, row, "v"), dtype_code(k),
+                                   _ptr(cos), _ptr(sin), 0 if cos is None else cos.shape[0],
+                                   0 if cos is None else 2 * cos.shape[1], int(interleaved), _ptr(q),
+                                   0 if q is None else _rows(q, qrow, "q"), heads, _ptr(q_out),
+                                   0 if q is None else _rows(q_out, qrow, "q_out"), _ptr(word), _stream()),
+           "cmpq_cache_append")
+
+
+def cmpq_cache_read(cache, batch, k_out, v_out, word=None):
+    """k_out, v_out: [n_tok][n_kv][d] fp16/bf16 with one row stride."""
+    row = cache.n_kv_heads * cache.head_dim
+    ld = _rows(k_out, row, "k_out")
+    if _rows(v_out, row, "v_out") != ld or v_out.dtype != k_out.dtype:
+        raise ValueError("k_out and v_out need one row stride and dtype")
+    _check(lib().cmpq_cache_read(cache, batch, dtype_code(k_out), _ptr(k_out), _ptr(v_out), ld, _ptr(word), _stream()),
+           "cmpq_cache_read")
+
+
+def cmpq_cache_attention_ws_bytes(n_seq, n_tok, max_new, max_len, n_heads, n_kv_heads, head_dim):
+    return int(lib().cmpq_cache_attention_ws_bytes(n_seq, n_tok, max_new, max_len, n_heads, n_kv_heads, head_dim))
+
+
+def cmpq_cache_attention(cache, batch, q, max_new, max_len, scale, causal, window, out, lse, ws, word=None):
+    """q, out: [n_tok][n_heads][d] fp16/bf16; lse: fp32 [n_tok][n_heads] or None."""
+    heads = q.shape[1]
+    row = heads * cache.head_dim
+    _check(lib().cmpq_cache_attention(cache, batch, _ptr(q), _rows(q, row, "q"), dtype_code(q), heads, max_new, max_len,
+                                      scale, int(causal), window, _ptr(out), _rows(out, row, "out"), _ptr(lse),
+                                      _ptr(word), _ptr(ws), ws.numel(), _stream()), "cmpq_cache_attention")
