@@ -1,5 +1,8 @@
 // 8-bit linear layers: quantization of tokens and the integer product with scales per token and channel.
+#include <algorithm>
+
 #include "cache.cuh"
+#include "tc5.cuh"
 
 namespace cmpq {
 
@@ -37,6 +40,7 @@ template <int DT>
 __global__ void __launch_bounds__(kQtThreads)
 quantize_tokens_kernel(const uint16_t* __restrict__ X, int64_t d, int64_t ldx, int wide, int8_t* __restrict__ codes,
                        int64_t ldc, float* __restrict__ scale, int32_t* __restrict__ nonfinite) {
+    tc5::dependents_may_start();
     const uint16_t* row = X + blockIdx.x * ldx;
     int8_t* out = codes + blockIdx.x * ldc;
     const int t = threadIdx.x;
@@ -75,50 +79,357 @@ quantize_tokens_kernel(const uint16_t* __restrict__ X, int64_t d, int64_t ldx, i
         *reinterpret_cast<uint2*>(out + 8 * g) = group_codes<DT>(load8(row + 8 * g, d - 8 * g, wide), inv);
 }
 
-// Plain tiled product on the integer dot-product instruction: 64 x 64 outputs a block, 64 bytes of the sum at a
-// time.
+// ---- the product --------------------------------------------------------------------------------------------
+//
+// Both kernels compute the transposed product: 128 weight rows (output channels) are the rows of the accumulator, a
+// TMEM lane each, and the tokens its columns.  A thread of the epilogue then owns one channel (its scale and bias are
+// registers) and a warp's store is 32 neighbouring channels of one token, so y is written in whole 64-byte runs
+// without a detour, for any token count and row stride.  Weight and token codes are both K-major as they lie in
+// memory; 128 bytes of the sum are one swizzled TMA box and four instructions of K = 32.
+
+struct ProductArgs {
+    const float *xs, *ws;
+    const uint16_t* bias;
+    uint16_t* y;
+    int64_t ldy;
+    int n, d_out;
+    int kblocks;    // 128-byte blocks of the sum
+    int per;        // split kernel: blocks per CTA of a cluster
+    int n_tiles;    // token tiles
+    int m_tiles;    // channel tiles
+    int stages;     // split kernel
+    int32_t* failed;
+};
+
 template <int DT>
-__global__ void __launch_bounds__(256)
-matmul_i8_kernel(const int8_t* __restrict__ xc, int64_t ldxc, const float* __restrict__ xs,
-                 const int8_t* __restrict__ wc, int64_t ldwc, const float* __restrict__ ws,
-                 const uint16_t* __restrict__ bias, int64_t n, int64_t d_in, int64_t d_out, uint16_t* __restrict__ y,
-                 int64_t ldy) {
-    __shared__ int a[64][17], b[64][17];
-    const int64_t t0 = (int64_t)blockIdx.y * 64, o0 = (int64_t)blockIdx.x * 64;
-    const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-    int acc[4][4] = {};
-    for (int64_t k = 0; k < d_in; k += 64) {
-        for (int i = threadIdx.x; i < 64 * 16; i += 256) {
-            const int r = i >> 4, w = i & 15;
-            const int64_t j = k + 4 * w;
-            int va = 0, vb = 0;
-            if (j < d_in) {
-                const int keep = d_in - j >= 4 ? -1 : (1 << (8 * (int)(d_in - j))) - 1;
-                if (t0 + r < n) va = *reinterpret_cast<const int*>(xc + (t0 + r) * ldxc + j) & keep;
-                if (o0 + r < d_out) vb = *reinterpret_cast<const int*>(wc + (o0 + r) * ldwc + j) & keep;
+__device__ __forceinline__ uint16_t scaled(int acc, float xs, float ws, float bias, bool has_bias) {
+    float v = (float)acc * xs * ws;
+    if (has_bias) v += bias;
+    return round16<DT>(v);
+}
+
+constexpr int kMmThreads = 192;  // a warp for the loads, one for the products, four for the epilogue
+constexpr int kMmMaxStages = 8;
+
+// Few tokens: the weights are read once and their bytes are the time.  A cluster of up to eight CTAs splits the sum
+// of one tile, so that there are enough CTAs to keep every SM's loads in flight; the int32 parts are joined through
+// distributed shared memory (integers: the order does not matter), CTA r finishing the tokens r, r + S, ...  Launched
+// behind the quantization of its tokens, it fetches its first weights before that has ended.
+template <int DT, int BN>
+__global__ void __launch_bounds__(kMmThreads)
+matmul_i8_split_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__ CUtensorMap xmap,
+                       const __grid_constant__ ProductArgs A, const int splits) {
+    extern __shared__ uint8_t raw[];
+    uint8_t* smem = raw + ((1024u - (tc5::smem_addr(raw) & 1023u)) & 1023u);
+    __shared__ uint64_t full[kMmMaxStages], empty[kMmMaxStages], done;
+    __shared__ uint32_t tmem_at;
+    __shared__ int failed;
+    constexpr int kStage = (128 + BN) * 128, kCols = BN < 32 ? 32 : BN;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int rank = splits > 1 ? (int)tc5::cluster_rank() : 0;
+    const int tile = blockIdx.x / splits, nt = tile % A.n_tiles, mt = tile / A.n_tiles;
+    const int k0 = rank * A.per, k1 = min(A.kblocks, k0 + A.per), count = k1 - k0;
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < A.stages; ++i) tc5::mbar_init(full + i, 1), tc5::mbar_init(empty + i, 1);
+        tc5::mbar_init(&done, 1);
+        failed = 0;
+        tc5::mbar_init_fence();
+    }
+    if (warp == 1) tc5::tmem_alloc<1>(&tmem_at, kCols);
+    tc5::fence_before_sync();
+    __syncthreads();
+    tc5::fence_after_sync();
+    const uint32_t tmem = tmem_at;
+    if (warp == 0) {
+        if (tc5::elect_one()) {
+            const int first = min(count, A.stages);
+            for (int i = 0; i < first; ++i) {
+                tc5::mbar_expect_tx(full + i, kStage);
+                tc5::tma_load_2d(smem + i * kStage, &wmap, full + i, (k0 + i) * 128, mt * 128);
             }
-            a[r][w] = va;
-            b[r][w] = vb;
+            tc5::wait_for_previous();
+            for (int i = 0; i < first; ++i)
+                tc5::tma_load_2d(smem + i * kStage + 128 * 128, &xmap, full + i, (k0 + i) * 128, nt * BN);
+            int slot = 0, phase = 0;
+            for (int i = first; i < count; ++i) {
+                if (!tc5::mbar_wait(empty + slot, phase, &failed)) break;
+                tc5::mbar_expect_tx(full + slot, kStage);
+                tc5::tma_load_2d(smem + slot * kStage, &wmap, full + slot, (k0 + i) * 128, mt * 128);
+                tc5::tma_load_2d(smem + slot * kStage + 128 * 128, &xmap, full + slot, (k0 + i) * 128, nt * BN);
+                if (++slot == A.stages) slot = 0, phase ^= 1;
+            }
         }
-        __syncthreads();
+    } else if (warp == 1) {
+        if (tc5::elect_one()) {
+            int slot = 0, phase = 0;
+            for (int i = 0; i < count; ++i) {
+                if (!tc5::mbar_wait(full + slot, phase, &failed)) break;
+                tc5::fence_after_sync();
+                const uint32_t at = tc5::smem_addr(smem + slot * kStage);
+                const uint64_t a = tc5::desc_k_sw128(at), b = tc5::desc_k_sw128(at + 128 * 128);
 #pragma unroll
-        for (int w = 0; w < 16; ++w)
+                for (int k = 0; k < 4; ++k)
+                    tc5::mma_i8<1>(tmem, a + 2 * k, b + 2 * k, tc5::idesc_i8(128, BN), (i | k) != 0);
+                tc5::mma_commit(empty + slot);
+                if (++slot == A.stages) slot = 0, phase ^= 1;
+            }
+            tc5::mma_commit(&done);
+        }
+    } else {
+        tc5::wait_for_previous();  // the tokens' scales
+        tc5::mbar_wait(&done, 0, &failed);
+        tc5::fence_after_sync();
+        const int quad = warp & 3, row = quad * 32 + lane;
+        const int64_t o = (int64_t)mt * 128 + row;
+        const bool real = o < A.d_out;
+        const float ws = real ? __ldg(A.ws + o) : 0.0f, bias = real && A.bias ? widen16<DT>(A.bias[o]) : 0.0f;
+        const int t0 = nt * BN, left = min(BN, A.n - t0);
+        int* part = reinterpret_cast<int*>(smem);  // [token][128]: the loads into it have all been consumed
+        for (int c = 0; c < left; c += 16) {
+            uint32_t r[16];
+            tc5::tmem_ld16(tmem + ((uint32_t)quad << 21) + c, r);
+            tc5::tmem_ld_wait();
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) acc[i][j] = __dp4a(a[ty + 16 * i][w], b[tx + 16 * j][w], acc[i][j]);
+            for (int j = 0; j < 16; ++j) {
+                if (c + j >= left) break;
+                if (splits > 1) {
+                    part[(c + j) * 128 + row] = (int)r[j];
+                } else if (real) {
+                    const int64_t t = t0 + c + j;
+                    A.y[t * A.ldy + o] = scaled<DT>((int)r[j], A.xs[t], ws, bias, A.bias != nullptr);
+                }
+            }
+        }
+        tc5::fence_before_sync();
+        if (splits > 1) {
+            tc5::cluster_sync();
+            const uint32_t at = tc5::smem_addr(part);
+            for (int j = rank; j < left; j += splits) {
+                int acc = 0;
+                for (int s = 0; s < splits; ++s) acc += tc5::ld_cluster_s32(at + 4u * (j * 128 + row), s);
+                const int64_t t = t0 + j;
+                if (real) A.y[t * A.ldy + o] = scaled<DT>(acc, A.xs[t], ws, bias, A.bias != nullptr);
+            }
+            tc5::cluster_sync();
+        }
+    }
+    if (splits > 1 && warp < 2) {
+        __syncwarp();
+        tc5::cluster_sync();
+        tc5::cluster_sync();
+    }
+    __syncthreads();
+    if (failed) {  // the loads that were asked for have to land before the shared memory is given back
+        if (threadIdx.x == 0) {
+            const long long start = clock64();
+            while (clock64() - start < (1ll << 21)) __nanosleep(1000);
+            atomicExch(A.failed, 1);
+        }
         __syncthreads();
     }
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int64_t t = t0 + ty + 16 * i, o = o0 + tx + 16 * j;
-            if (t >= n || o >= d_out) continue;
-            float v = (float)acc[i][j] * xs[t] * ws[o];
-            if (bias) v += widen16<DT>(bias[o]);
-            y[t * ldy + o] = round16<DT>(v);
+    if (warp == 1) tc5::tmem_free<1>(tmem, kCols);
+}
+
+constexpr int kPairStages = 6, kPairStageBytes = 2 * 128 * 128;
+constexpr size_t kPairSmem = kPairStages * kPairStageBytes + 1024;
+
+// Many tokens: pairs of CTAs stay on their SMs and walk over tiles of 256 channels x 256 tokens (cta_group::2).  A CTA
+// loads its 128 channels and half of the tokens, so each byte that an SM reads feeds 512 products; six stages of 32 KB.  Two accumulators
+// of 256 columns alternate, the epilogue of one tile runs under the products of the next.  Token tiles go fastest: the
+// pairs at work share a few weight tiles and the token codes stay in L2.
+template <int DT>
+__global__ void __launch_bounds__(kMmThreads, 1)
+matmul_i8_pair_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__ CUtensorMap xmap,
+                      const __grid_constant__ ProductArgs A) {
+    extern __shared__ uint8_t raw[];
+    uint8_t* smem = raw + ((1024u - (tc5::smem_addr(raw) & 1023u)) & 1023u);
+    __shared__ uint64_t full[kPairStages], empty[kPairStages], acc_full[2], acc_empty[2];
+    __shared__ uint32_t tmem_at;
+    __shared__ int failed;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int rank = (int)tc5::cluster_rank();
+    const int tiles = A.n_tiles * A.m_tiles, first = blockIdx.x >> 1, step = gridDim.x >> 1;
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < kPairStages; ++i) tc5::mbar_init(full + i, 1), tc5::mbar_init(empty + i, 1);
+        for (int i = 0; i < 2; ++i) tc5::mbar_init(acc_full + i, 1), tc5::mbar_init(acc_empty + i, 8);
+        failed = 0;
+        tc5::mbar_init_fence();
+    }
+    if (warp == 1) tc5::tmem_alloc<2>(&tmem_at, 512);
+    tc5::fence_before_sync();
+    __syncthreads();
+    tc5::cluster_sync();
+    tc5::fence_after_sync();
+    const uint32_t tmem = tmem_at;
+    tc5::wait_for_previous();
+    if (warp == 0) {
+        if (tc5::elect_one()) {
+            int slot = 0, phase = 1;  // a new barrier counts as empty
+            bool ok = true;
+            for (int tile = first; ok && tile < tiles; tile += step) {
+                const int nt = tile % A.n_tiles, mt = tile / A.n_tiles;
+                for (int k = 0; k < A.kblocks; ++k) {
+                    if (!(ok = tc5::mbar_wait(empty + slot, phase, &failed))) break;
+                    if (rank == 0) tc5::mbar_expect_tx(full + slot, 2 * kPairStageBytes);
+                    uint8_t* at = smem + slot * kPairStageBytes;
+                    tc5::tma_load_2d_pair(at, &wmap, full + slot, k * 128, mt * 256 + rank * 128);
+                    tc5::tma_load_2d_pair(at + 128 * 128, &xmap, full + slot, k * 128, nt * 256 + rank * 128);
+                    if (++slot == kPairStages) slot = 0, phase ^= 1;
+                }
+            }
         }
+    } else if (warp == 1) {
+        if (rank == 0 && tc5::elect_one()) {
+            int slot = 0, phase = 0, acc = 0, acc_phase = 1;
+            bool ok = true;
+            for (int tile = first; ok && tile < tiles; tile += step) {
+                if (!tc5::mbar_wait(acc_empty + acc, acc_phase, &failed)) break;
+                tc5::fence_after_sync();
+                for (int k = 0; k < A.kblocks; ++k) {
+                    if (!(ok = tc5::mbar_wait(full + slot, phase, &failed))) break;
+                    tc5::fence_after_sync();
+                    const uint32_t at = tc5::smem_addr(smem + slot * kPairStageBytes);
+                    const uint64_t a = tc5::desc_k_sw128(at), b = tc5::desc_k_sw128(at + 128 * 128);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        tc5::mma_i8<2>(tmem + acc * 256, a + 2 * j, b + 2 * j, tc5::idesc_i8(256, 256), (k | j) != 0);
+                    tc5::mma_commit_pair(empty + slot);
+                    if (++slot == kPairStages) slot = 0, phase ^= 1;
+                }
+                tc5::mma_commit_pair(acc_full + acc);
+                acc ^= 1;
+                if (acc == 0) acc_phase ^= 1;
+            }
+        }
+    } else {
+        const int quad = warp & 3;
+        int acc = 0, phase = 0;
+        for (int tile = first; tile < tiles; tile += step) {
+            const int nt = tile % A.n_tiles, mt = tile / A.n_tiles;
+            const int64_t o = (int64_t)mt * 256 + rank * 128 + quad * 32 + lane;
+            const bool real = o < A.d_out;
+            const float ws = real ? __ldg(A.ws + o) : 0.0f, bias = real && A.bias ? widen16<DT>(A.bias[o]) : 0.0f;
+            const int t0 = nt * 256, left = min(256, A.n - t0);
+            if (!tc5::mbar_wait(acc_full + acc, phase, &failed)) break;
+            tc5::fence_after_sync();
+            const uint32_t at = tmem + ((uint32_t)quad << 21) + acc * 256;
+            for (int c = 0; c < left; c += 16) {
+                uint32_t r[16];
+                tc5::tmem_ld16(at + c, r);
+                tc5::tmem_ld_wait();
+                uint16_t* y = A.y + (int64_t)(t0 + c) * A.ldy + o;
+#pragma unroll
+                for (int j = 0; j < 16; ++j) {
+                    if (c + j < left && real)
+                        y[j * A.ldy] = scaled<DT>((int)r[j], __ldg(A.xs + t0 + c + j), ws, bias, A.bias != nullptr);
+                }
+            }
+            tc5::fence_before_sync();
+            __syncwarp();
+            if (lane == 0) tc5::mbar_arrive_remote(acc_empty + acc, 0);
+            acc ^= 1;
+            if (acc == 0) phase ^= 1;
+        }
+    }
+    __syncwarp();
+    __syncthreads();
+    if (failed) {
+        if (threadIdx.x == 0) {
+            const long long start = clock64();
+            while (clock64() - start < (1ll << 21)) __nanosleep(1000);
+            atomicExch(A.failed, 1);
+        }
+        __syncthreads();
+    }
+    tc5::cluster_sync();  // the pair's products and loads have ended on both sides
+    if (warp == 1) tc5::tmem_free<2>(tmem, 512);
+}
+
+bool make_byte_map(CUtensorMap* map, const void* base, int64_t rows, int64_t cols, int64_t ld, int box_rows) {
+    using Encode = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
+                                const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+    static const Encode encode = [] {
+        void* f = nullptr;
+        cudaDriverEntryPointQueryResult found;
+        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &f, cudaEnableDefault, &found) != cudaSuccess ||
+            found != cudaDriverEntryPointSuccess)
+            f = nullptr;
+        return reinterpret_cast<Encode>(f);
+    }();
+    if (!encode) return false;
+    const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)ld};
+    const cuuint32_t box[2] = {128, (cuuint32_t)box_rows}, steps[2] = {1, 1};
+    return encode(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(base), dims, strides, box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                  CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// A launch with clusters of `cluster` CTAs; `behind`: it may start before the kernel in front of it has ended.
+template <class Kernel, class... Args>
+static cmpq_status launch_cluster(Kernel kern, unsigned grid, int threads, size_t smem, int cluster, bool behind, cudaStream_t st,
+                                  const Args&... args) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(grid);
+    cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[2];
+    unsigned n = 0;
+    if (cluster > 1) {
+        attr[n].id = cudaLaunchAttributeClusterDimension;
+        attr[n].val.clusterDim.x = cluster, attr[n].val.clusterDim.y = 1, attr[n].val.clusterDim.z = 1;
+        ++n;
+    }
+    if (behind) {
+        attr[n].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        attr[n].val.programmaticStreamSerializationAllowed = 1;
+        ++n;
+    }
+    cfg.attrs = attr;
+    cfg.numAttrs = n;
+    return cudaLaunchKernelEx(&cfg, kern, args...) == cudaSuccess ? launch_status() : CMPQ_ERR_CUDA;
+}
+
+constexpr size_t kSplitSmem = 100 << 10;  // two CTAs share an SM
+
+template <int DT, int BN>
+static cmpq_status launch_split(const CUtensorMap& wmap, const CUtensorMap& xmap, ProductArgs a, bool behind, cudaStream_t st) {
+    constexpr int kStage = (128 + BN) * 128;
+    const int64_t tiles = (int64_t)a.m_tiles * a.n_tiles;
+    // enough CTAs for two per SM, at least two blocks of the sum each
+    const int want = (int)std::max<int64_t>(1, std::min<int64_t>(8, (2 * sm_count() + tiles - 1) / tiles));
+    a.per = std::max((a.kblocks + want - 1) / want, std::min(2, a.kblocks));
+    const int splits = (a.kblocks + a.per - 1) / a.per;
+    a.stages = std::min({(int)((kSplitSmem - 1024) / kStage), kMmMaxStages, std::max(a.per, 2)});
+    const size_t smem = (size_t)std::max(a.stages * kStage, 128 * BN * 4) + 1024;
+    static bool raised[64];
+    if (!raise_smem_limit_once(matmul_i8_split_kernel<DT, BN>, kSplitSmem, raised)) return CMPQ_ERR_CUDA;
+    if (tiles * splits > INT32_MAX) return CMPQ_ERR_UNSUPPORTED;
+    return launch_cluster(matmul_i8_split_kernel<DT, BN>, (unsigned)(tiles * splits), kMmThreads, smem, splits, behind, st, wmap, xmap, a, splits);
+}
+
+template <int DT>
+static cmpq_status launch_product(const int8_t* xc, int64_t ldxc, const int8_t* wc, int64_t ldwc, int64_t d_in, ProductArgs a, bool behind,
+                                  cudaStream_t st) {
+    a.kblocks = (int)((d_in + 127) / 128);
+    const int64_t pairs = (int64_t)((a.d_out + 255) / 256) * ((a.n + 255) / 256);
+    CUtensorMap wmap, xmap;
+    const bool pair = a.n > 128 && pairs * 4 >= sm_count();
+    const int bn = pair ? 128 : a.n <= 16 ? 16 : a.n <= 32 ? 32 : a.n <= 64 ? 64 : 128;
+    if (!make_byte_map(&wmap, wc, a.d_out, d_in, ldwc, 128) || !make_byte_map(&xmap, xc, a.n, d_in, ldxc, bn)) return CMPQ_ERR_CUDA;
+    if (pair) {
+        a.n_tiles = (a.n + 255) / 256, a.m_tiles = (a.d_out + 255) / 256;
+        static bool raised[64];
+        if (!raise_smem_limit_once(matmul_i8_pair_kernel<DT>, kPairSmem, raised)) return CMPQ_ERR_CUDA;
+        return launch_cluster(matmul_i8_pair_kernel<DT>, 2 * (unsigned)std::min<int64_t>(pairs, sm_count() / 2), kMmThreads, kPairSmem, 2, behind, st,
+                              wmap, xmap, a);
+    }
+    a.n_tiles = (a.n + bn - 1) / bn, a.m_tiles = (a.d_out + 127) / 128;
+    switch (bn) {
+        case 16: return launch_split<DT, 16>(wmap, xmap, a, behind, st);
+        case 32: return launch_split<DT, 32>(wmap, xmap, a, behind, st);
+        case 64: return launch_split<DT, 64>(wmap, xmap, a, behind, st);
+        default: return launch_split<DT, 128>(wmap, xmap, a, behind, st);
+    }
 }
 
 size_t linear_i8_codes_bytes(int64_t n, int64_t d_in) { return round_up((size_t)n * round_up(d_in, 16), 256); }
@@ -153,6 +464,21 @@ extern "C" cmpq_status cmpq_quantize_tokens(const void* X, cmpq_dtype dt, int64_
     return launch_status();
 }
 
+// The caller has checked everything.  The last 256 bytes of the work space take the mark of a kernel that gave up.
+static cmpq_status product(const int8_t* xc, int64_t ldxc, const float* xs, const int8_t* wc, int64_t ldwc, const float* w_scale, const void* bias,
+                           cmpq_dtype dt, int64_t n, int64_t d_in, int64_t d_out, void* y, int64_t ldy, void* ws, bool behind, void* stream) {
+    ProductArgs a = {};
+    a.xs = xs, a.ws = w_scale;
+    a.bias = static_cast<const uint16_t*>(bias);
+    a.y = static_cast<uint16_t*>(y);
+    a.ldy = ldy;
+    a.n = (int)n, a.d_out = (int)d_out;
+    a.failed = reinterpret_cast<int32_t*>(static_cast<char*>(ws) + cmpq_linear_i8_ws_bytes(n, d_in, d_out) - 256);
+    auto st = static_cast<cudaStream_t>(stream);
+    return dt == CMPQ_BF16 ? launch_product<CMPQ_BF16>(xc, ldxc, wc, ldwc, d_in, a, behind, st)
+                           : launch_product<CMPQ_F16>(xc, ldxc, wc, ldwc, d_in, a, behind, st);
+}
+
 extern "C" cmpq_status cmpq_matmul_i8(const int8_t* xc, int64_t ldxc, const float* xs, const int8_t* wc, int64_t ldwc,
                                       const float* w_scale, const void* bias, cmpq_dtype dt, int64_t n, int64_t d_in,
                                       int64_t d_out, void* y, int64_t ldy, void* ws, size_t ws_bytes, void* stream) {
@@ -163,15 +489,7 @@ extern "C" cmpq_status cmpq_matmul_i8(const int8_t* xc, int64_t ldxc, const floa
         !aligned_to(w_scale, 4) || !aligned_to(y, 2) || !aligned_to(bias, 2))
         return CMPQ_ERR_INVALID_ARG;
     if (!ws || !aligned_to(ws, 256) || ws_bytes < cmpq_linear_i8_ws_bytes(n, d_in, d_out)) return CMPQ_ERR_WORKSPACE;
-    const dim3 grid((unsigned)((d_out + 63) / 64), (unsigned)((n + 63) / 64));
-    auto st = static_cast<cudaStream_t>(stream);
-    const auto* b = static_cast<const uint16_t*>(bias);
-    auto* out = static_cast<uint16_t*>(y);
-    if (dt == CMPQ_BF16)
-        matmul_i8_kernel<CMPQ_BF16><<<grid, 256, 0, st>>>(xc, ldxc, xs, wc, ldwc, w_scale, b, n, d_in, d_out, out, ldy);
-    else
-        matmul_i8_kernel<CMPQ_F16><<<grid, 256, 0, st>>>(xc, ldxc, xs, wc, ldwc, w_scale, b, n, d_in, d_out, out, ldy);
-    return launch_status();
+    return product(xc, ldxc, xs, wc, ldwc, w_scale, bias, dt, n, d_in, d_out, y, ldy, ws, false, stream);
 }
 
 extern "C" cmpq_status cmpq_linear_i8(const void* X, cmpq_dtype dt, int64_t n, int64_t d_in, int64_t ldx,
@@ -190,5 +508,6 @@ extern "C" cmpq_status cmpq_linear_i8(const void* X, cmpq_dtype dt, int64_t n, i
     const int64_t ldc = (int64_t)round_up(d_in, 16);
     cmpq_status st = cmpq_quantize_tokens(X, dt, n, d_in, ldx, codes, ldc, scale, nonfinite, stream);
     if (st != CMPQ_OK) return st;
-    return cmpq_matmul_i8(codes, ldc, scale, wc, ldwc, w_scale, bias, dt, n, d_in, d_out, y, ldy, ws, ws_bytes, stream);
+    // the quantization lets the product start early; it was itself started after everything before it, the weights too
+    return product(codes, ldc, scale, wc, ldwc, w_scale, bias, dt, n, d_in, d_out, y, ldy, ws, true, stream);
 }
