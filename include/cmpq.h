@@ -462,8 +462,9 @@ cmpq_status cmpq_linear_i8(const void* X, cmpq_dtype dt, int64_t n, int64_t d_in
  * that they quantize is a NaN or an infinity (rotated keys count), and bit 2 when a length is negative or above max_len, a
  * count of new tokens is above max_new or above the sequence's length (append and read), or a table entry
  * is no page: such tokens and pages are left out, nothing out of range is read or written, and the outputs of
- * that sequence are unspecified.  cmpq_check_cache waits for the stream and answers CMPQ_OK,
- * CMPQ_ERR_NONFINITE (bit 0) or CMPQ_ERR_INVALID_ARG (bit 2). */
+ * that sequence are unspecified.  Bit 3: a kernel gave up waiting for its own copies
+ * (about a second; never seen).  cmpq_check_cache waits for the stream and answers CMPQ_OK, CMPQ_ERR_NONFINITE (bit 0),
+ * CMPQ_ERR_INVALID_ARG (bit 2) or CMPQ_ERR_INTERNAL (bit 3). */
 typedef struct {
     int8_t* k_codes;
     float* k_scale;

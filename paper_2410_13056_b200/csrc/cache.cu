@@ -254,7 +254,7 @@ extern "C" cmpq_status cmpq_check_cache(const int32_t* word, void* stream) {
     auto st = static_cast<cudaStream_t>(stream);
     if (cudaMemcpyAsync(&host, word, sizeof(host), cudaMemcpyDeviceToHost, st) != cudaSuccess) return CMPQ_ERR_CUDA;
     if (cudaStreamSynchronize(st) != cudaSuccess) return CMPQ_ERR_CUDA;
-    return host & kWordTable ? CMPQ_ERR_INVALID_ARG : host ? CMPQ_ERR_NONFINITE : CMPQ_OK;
+    return host & kWordInternal ? CMPQ_ERR_INTERNAL : host & kWordTable ? CMPQ_ERR_INVALID_ARG : host ? CMPQ_ERR_NONFINITE : CMPQ_OK;
 }
 
 extern "C" cmpq_status cmpq_cache_append(const cmpq_cache* cache, const cmpq_batch* batch, const void* k, int64_t ldk,

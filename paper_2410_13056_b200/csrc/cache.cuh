@@ -7,7 +7,7 @@
 
 namespace cmpq {
 
-constexpr int kWordNonfinite = 1, kWordTable = 4;  // bits of the device word
+constexpr int kWordNonfinite = 1, kWordTable = 4, kWordInternal = 8;  // bits of the device word
 constexpr float kScaleLo = 0x1p-60f, kScaleHi = 0x1p60f;
 
 template <int DT>

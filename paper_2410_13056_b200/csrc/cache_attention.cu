@@ -1,5 +1,12 @@
 // Attention over the paged 8-bit cache.
+//
+// out = softmax(scale q K^T) V with K = S_k[page] c, V = S_v[page] c, c int8.  The codes are exact in fp16, so both
+// products run on the tensor cores in fp16 with fp32 accumulation, a page's scale being one factor of its scores (keys)
+// or of its weights (values); a query row is scaled by a power of two into fp16's range first.
+#include <algorithm>
+
 #include "cache.cuh"
+#include "tc5.cuh"
 
 namespace cmpq {
 
@@ -10,71 +17,575 @@ struct AttnArgs {
     uint16_t* out;
     float* lse;
     int64_t ldq, ldo, max_new, max_len, window;
-    float scale;
+    float scale;  // times log2(e): scores are kept in powers of two
     int n_heads, causal;
+    int wide_q, wide_o;
     int32_t* word;
+    float* parts;  // partial results of the workers, see there
+    int workers;
 };
 
-// One warp per query row and head: the lanes share the head's entries, one key after the other.
-template <int DT, int D>
-__global__ void __launch_bounds__(128)
-attention_row_kernel(const __grid_constant__ AttnArgs A) {
-    const int lane = threadIdx.x & 31, P = A.c.page_tokens, H = A.c.n_kv_heads;
-    const int32_t* off = A.b.tok_off;
-    const int64_t t = blockIdx.x;
-    const int s = block_count(A.b.n_seq, [&](int64_t i) { return off[i] <= t; });
-    if (s >= A.b.n_seq) return;
-    const int64_t len = A.b.lens[s], pos = len - off[s + 1] + t;
-    if (len < 0 || len > A.max_len || off[s + 1] - off[s] > A.max_new) {
-        if (threadIdx.x == 0 && A.word) atomicOr(A.word, kWordTable);
-        return;
+constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
+
+__device__ __forceinline__ float ex2(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+// ---- few query rows: warps share out the cache -------------------------------------------------------------------
+//
+// The time is that of reading the cache once, so the keys are split over all warps of the GPU.  The rows of a sequence
+// and key-value head (its new tokens times the query heads of the group) are taken R = 8 NT at a time; such a unit is a
+// run of tiles of 32 tokens.  All units' tiles, one behind the other, are dealt to the workers (warps) in equal
+// contiguous runs: sequences of any lengths balance, and a worker meets few unit borders.  A unit inside one worker's
+// run is finished there; the parts of one that is cut go to the work space and are joined by a second kernel in the
+// order of the workers (no atomics: the same bytes every time).
+constexpr int kTile = 32;
+
+template <int D, int NT>
+struct Rows {
+    static constexpr int kR = 8 * NT;
+    static constexpr int kWarps = 4;
+    static constexpr int kTileBytes = kTile * D;                            // keys; as many for the values
+    static constexpr int kStages = D == 64 ? 6 : D == 128 ? 3 : 2;
+    static constexpr int kSmem = kWarps * kStages * 2 * kTileBytes + 1024;  // 97 KB (D 64, 128) or 129 KB
+    static constexpr int kPerSm = D == 256 ? 1 : 2;
+    static constexpr int kPart = kR * (D + 2);                              // floats of a partial result
+};
+
+struct SeqPlan {
+    int64_t first, n, len;  // row of the first query, queries, cached tokens
+    int tile0, tiles, blocks;
+    bool bad;
+};
+
+// What a sequence needs: its tiles per unit (one at least, so that rows without a key are written too) and its row
+// blocks.  `count` of its tiles is tiles * blocks * heads, 0 for a sequence without queries or with bad lengths.
+__device__ __forceinline__ SeqPlan seq_plan(const AttnArgs& A, int64_t s, int rows) {
+    SeqPlan p;
+    p.first = A.b.tok_off[s];
+    p.n = A.b.tok_off[s + 1] - p.first;
+    p.len = A.b.lens[s];
+    p.bad = p.len < 0 || p.len > A.max_len || p.n < 0 || p.n > A.max_new || p.first < 0 || p.first + p.n > A.b.n_tok;
+    const int64_t lo = A.window > 0 ? max((int64_t)0, p.len - p.n - A.window + 1) : 0;
+    p.tile0 = (int)(lo / kTile);
+    p.tiles = max(1, (int)((p.len + kTile - 1) / kTile) - p.tile0);
+    const int g = A.n_heads / A.c.n_kv_heads;
+    p.blocks = p.bad ? 0 : (int)((p.n * g + rows - 1) / rows);
+    return p;
+}
+__device__ __forceinline__ int64_t seq_tiles(const AttnArgs& A, const SeqPlan& p) {
+    return (int64_t)p.tiles * p.blocks * A.c.n_kv_heads;
+}
+
+// Inclusive sums over the block's threads; `part` has one entry per warp.  Ends behind a barrier.
+__device__ __forceinline__ int64_t block_scan(int64_t v, int64_t* part) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+        const int64_t o = __shfl_up_sync(0xffffffffu, v, d);
+        if (lane >= d) v += o;
     }
-    const int64_t hi = A.causal ? min(len, pos + 1) : len;
-    const int64_t lo = A.window > 0 ? max((int64_t)0, pos - A.window + 1) : 0;
-    constexpr int E = D / 32;
-    for (int h = threadIdx.x >> 5; h < A.n_heads; h += 4) {
-        const int kv = h / (A.n_heads / H);
-        float q[E], o[E], m = -INFINITY, l = 0.0f;
-#pragma unroll
-        for (int e = 0; e < E; ++e) {
-            q[e] = widen16<DT>(A.q[t * A.ldq + h * D + lane + 32 * e]);
-            o[e] = 0.0f;
+    if (lane == 31) part[warp] = v;
+    __syncthreads();
+    for (int w = 0; w < warp; ++w) v += part[w];
+    __syncthreads();
+    return v;
+}
+
+// Four int8 codes (already offset by 128) as two pairs of fp16: 0x6400 | u is 1024 + u, and 1024 + 128 comes off.
+__device__ __forceinline__ uint32_t half_pair(uint32_t u, uint32_t pick) {
+    const uint32_t h = __byte_perm(u, 0x64646464u, pick);
+    const __half2 d = __hsub2(*reinterpret_cast<const __half2*>(&h), __halves2half2(__ushort_as_half(0x6480), __ushort_as_half(0x6480)));
+    return *reinterpret_cast<const uint32_t*>(&d);
+}
+__device__ __forceinline__ void mma_f16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+                 : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {
+    uint32_t y;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+    return y;
+}
+
+// Bytes of token t's entries from d on in a tile: rows of 128 bytes (two tokens of 64 entries, or half a token of 256 in
+// a plane of its own), 16-byte groups swizzled by the row as the tensor map leaves them.
+template <int D>
+__device__ __forceinline__ uint32_t tile_at(int t, int d) {
+    if (D == 64) {
+        const int row = t >> 1;
+        return row * 128 + ((((t & 1) * 4 + (d >> 4)) ^ (row & 7)) << 4) + (d & 15);
+    }
+    const int plane = D == 256 ? d >> 7 : 0, e = D == 256 ? d & 127 : d;
+    return plane * (kTile * 128) + t * 128 + (((e >> 4) ^ (t & 7)) << 4) + (e & 15);
+}
+
+// A lane's place in the m16n8k16 fragments: r = lane / 4, c = lane % 4.
+//   scores   S^T[token][row] = K Q^T: a lane reads 16 bytes of keys of tokens r and r + 8 at a time, which are the A
+//            entries of four instructions when the sum runs over the entries in the order 16 (2c + j) + 4 w + {0..3}
+//            (w the instruction, any order serves as long as Q has the same); for D = 64 the 16 bytes are group c.
+//   weights  the score fragment, rounded to fp16 and transposed eight by eight, is the B operand of
+//   output   O^T[entry][row] = V^T P^T: a lane reads D/8 neighbouring entries of tokens 2c, 2c+1, 2c+8, 2c+9 and pairs
+//            the tokens' bytes; entry i of its run is row r (i even) or r + 8 (i odd) of instruction i / 2.
+// So keys and values are read from shared memory once, 16 bytes a time and without bank conflicts for D >= 128, and a
+// lane ends up with D/8 neighbouring entries of two output rows.  Per code that is about 0.25 shared loads / 16 B and
+// 1.4 instructions to widen it, a third of the issue slots at the rate the memory delivers.
+template <int DT, int D, int NT>
+__global__ void __launch_bounds__(128, Rows<D, NT>::kPerSm)
+attention_rows_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUtensorMap vmap,
+                      const __grid_constant__ AttnArgs A) {
+    using C = Rows<D, NT>;
+    constexpr int kR = C::kR, kStages = C::kStages;
+    extern __shared__ uint8_t raw[];
+    __shared__ uint64_t bars[C::kWarps][kStages];
+    __shared__ int64_t scan[C::kWarps];
+    __shared__ int64_t start_base[C::kWarps];
+    __shared__ int start_seq[C::kWarps];
+    __shared__ float2 page_scale[C::kWarps][64];  // key and value scales of the last 64 pages asked for
+    __shared__ int failed[C::kWarps];
+    uint8_t* smem = raw + ((1024u - (tc5::smem_addr(raw) & 1023u)) & 1023u);
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, r = lane >> 2, c = lane & 3;
+    const int H = A.c.n_kv_heads, g = A.n_heads / H, P = A.c.page_tokens;
+    tc5::dependents_may_start();
+    if (lane == 0) {
+        for (int i = 0; i < kStages; ++i) tc5::mbar_init(&bars[warp][i], 1);
+        failed[warp] = 0;
+        tc5::mbar_init_fence();
+    }
+
+    // the total, this warp's run, and the sequence it starts in
+    int64_t total = 0;
+    for (int64_t base = 0; base < A.b.n_seq; base += blockDim.x) {
+        int64_t v = 0;
+        if (base + tid < A.b.n_seq) {
+            const SeqPlan p = seq_plan(A, base + tid, kR);
+            v = seq_tiles(A, p);
+            if (p.bad && blockIdx.x == 0 && A.word) atomicOr(A.word, kWordTable);
         }
-        for (int64_t j = lo; j < hi; ++j) {
-            const int64_t page = j / P;
-            const int id = page < A.b.ld_table ? A.b.table[s * A.b.ld_table + page] : -1;
-            if (id < 0 || id >= A.c.n_pages) {
-                if (lane == 0 && A.word) atomicOr(A.word, kWordTable);
-                continue;
+        v = block_scan(v, scan);
+        if (tid == (int)blockDim.x - 1) start_base[0] = v;
+        __syncthreads();
+        total += start_base[0];
+        __syncthreads();
+    }
+    const int64_t per = max((int64_t)1, (total + A.workers - 1) / A.workers);
+    const int worker = blockIdx.x * C::kWarps + warp;
+    const int64_t begin = worker * per, end = min(total, begin + per);
+    {
+        int64_t before = 0;
+        for (int64_t base = 0; base < A.b.n_seq; base += blockDim.x) {
+            int64_t v = 0;
+            if (base + tid < A.b.n_seq) v = seq_tiles(A, seq_plan(A, base + tid, kR));
+            const int64_t upto = before + block_scan(v, scan), from = upto - v;
+#pragma unroll
+            for (int w = 0; w < C::kWarps; ++w) {
+                const int64_t x = (blockIdx.x * C::kWarps + w) * per;
+                if (x < total && from <= x && x < upto) start_seq[w] = (int)(base + tid), start_base[w] = from;
             }
-            const int64_t at = (int64_t)id * H + kv, row = (at * P + j % P) * D;
-            float dot = 0.0f;
-#pragma unroll
-            for (int e = 0; e < E; ++e) dot = fmaf(q[e], (float)A.c.k_codes[row + lane + 32 * e], dot);
-#pragma unroll
-            for (int x = 16; x; x >>= 1) dot += __shfl_xor_sync(0xffffffffu, dot, x);
-            dot *= A.c.k_scale[at] * A.scale;
-            const float top = fmaxf(m, dot), keep = __expf(m - top), p = __expf(dot - top);
-            l = fmaf(l, keep, p);
-            const float pv = p * A.c.v_scale[at];
-#pragma unroll
-            for (int e = 0; e < E; ++e) o[e] = fmaf(o[e], keep, pv * (float)A.c.v_codes[row + lane + 32 * e]);
-            m = top;
+            if (tid == (int)blockDim.x - 1) scan[0] = upto;
+            __syncthreads();
+            before = scan[0];
+            __syncthreads();
         }
-        const float r = l > 0.0f ? 1.0f / l : 0.0f;
+    }
+    if (begin >= end) return;
+
+    int64_t s = start_seq[warp], base = start_base[warp];
+    uint8_t* ring = smem + warp * (kStages * 2 * C::kTileBytes);
+    uint64_t* bar = bars[warp];
+    volatile int* gave_up = &failed[warp];
+    int slot_in = 0, slot_out = 0, phase_out = 0;
+    const int per_tile = P < kTile ? kTile / P : 1;  // pages that a tile touches
+
+    for (int64_t x = begin; x < end;) {
+        const SeqPlan p = seq_plan(A, s, kR);
+        const int64_t all = seq_tiles(A, p);
+        if (x >= base + all) {  // also a sequence without tiles
+            base += all;
+            ++s;
+            continue;
+        }
+        const int64_t unit = (x - base) / p.tiles;
+        const int t_from = (int)((x - base) % p.tiles);
+        const int t_to = (int)min((int64_t)p.tiles, t_from + (end - x));  // tiles of this unit that are this worker's
+        const int head = (int)(unit / p.blocks), rb = (int)(unit % p.blocks);
+        const int rows = (int)min((int64_t)kR, p.n * g - (int64_t)rb * kR);
+        // positions of the block's first and last query; keys that any of them sees
+        const int64_t p0 = p.len - p.n + (rb * kR) / g, p1 = p.len - p.n + (rb * kR + rows - 1) / g;
+        const int64_t key_hi = A.causal ? max((int64_t)0, p1 + 1) : p.len;
+        const int64_t key_lo = A.window > 0 ? max((int64_t)0, p0 - A.window + 1) : 0;
+        const int live_from = max(t_from, (int)(key_lo / kTile) - p.tile0);
+        const int live_to = min(t_to, (int)((key_hi + kTile - 1) / kTile) - p.tile0);
+
+        // the queries, scaled into fp16
+        uint32_t qf[NT][D / 16][2];
+        float qs[NT][2];
 #pragma unroll
-        for (int e = 0; e < E; ++e) A.out[t * A.ldo + h * D + lane + 32 * e] = round16<DT>(o[e] * r);
-        if (A.lse && lane == 0) A.lse[t * A.n_heads + h] = l > 0.0f ? m + logf(l) : -INFINITY;
+        for (int nt = 0; nt < NT; ++nt) {
+            const int row = nt * 8 + r, i = (rb * kR + row) / g, h = head * g + (rb * kR + row) % g;
+            float f[D / 4];
+            float m = 0.0f;
+#pragma unroll
+            for (int e = 0; e < D / 4; e += 8) {  // e / 16 the group of 16 entries, 16 (2c + e/16) (D = 64: 16 c)
+                const int d = (D == 64 ? 16 * c : 16 * (2 * c + ((e >> 4) & 1)) + (e >> 5) * 128) + (e & 15);
+                float v[8];
+                if (row < rows) {
+                    const uint16_t* src = A.q + (p.first + i) * A.ldq + (int64_t)h * D + d;
+                    widen8<DT>(load8(src, 8, A.wide_q), v);
+                } else {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) v[j] = 0.0f;
+                }
+#pragma unroll
+                for (int j = 0; j < 8; ++j) f[e + j] = v[j], m = fmaxf(m, fabsf(v[j]));
+            }
+            m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 1));
+            m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 2));
+            const int ex = m > 0.0f ? ilogbf(m) : 0;
+            const float up = ldexpf(1.0f, ex), dn = ldexpf(1.0f, max(-126, -ex));
+#pragma unroll
+            for (int e = 0; e < D / 4; e += 2) {
+                const __half2 hh = __floats2half2_rn(f[e] * dn, f[e + 1] * dn);
+                qf[nt][e >> 2][(e >> 1) & 1] = *reinterpret_cast<const uint32_t*>(&hh);
+            }
+            const float mine = A.scale * up;  // of row r; the score fragment has rows 2c, 2c + 1
+            qs[nt][0] = __shfl_sync(0xffffffffu, mine, (2 * c) * 4);
+            qs[nt][1] = __shfl_sync(0xffffffffu, mine, (2 * c + 1) * 4);
+        }
+
+        float o[NT][D / 16][4], m2[NT][2], l[NT][2], ref = 0.0f;
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+            for (int i = 0; i < D / 16; ++i)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[nt][i][e] = 0.0f;
+            m2[nt][0] = m2[nt][1] = -INFINITY;
+            l[nt][0] = l[nt][1] = 0.0f;
+        }
+
+        // Pages are asked for 32 at a time, one per lane, with their scales; lane 0 has the copies of a tile made.
+        const int page0 = (int)(((int64_t)(p.tile0 + live_from) * kTile) / P);
+        const int page_end = (int)((p.len + P - 1) / P);
+        int my_page = -1, have = 0;  // pages page0 .. page0 + have are known
+        auto fetch_pages = [&]() {
+            const int page = page0 + have + lane;
+            my_page = -1;
+            float2 sc = make_float2(0.0f, 0.0f);
+            if (page < page_end) {
+                my_page = page < A.b.ld_table ? A.b.table[s * A.b.ld_table + page] : -1;
+                if (my_page < 0 || my_page >= A.c.n_pages) {
+                    my_page = -1;
+                    if (A.word) atomicOr(A.word, kWordTable);
+                } else {
+                    const int64_t at = (int64_t)my_page * H + head;
+                    sc = make_float2(A.c.k_scale[at], A.c.v_scale[at]);
+                }
+            }
+            page_scale[warp][(have + lane) & 63] = sc;
+            have += 32;
+            __syncwarp();
+        };
+        auto ask = [&](int t) {  // tile t of the unit
+            const int64_t token = (int64_t)(p.tile0 + t) * kTile;
+            const int page = (int)(token / P) - page0;
+            if (page >= have) fetch_pages();
+            const int id0 = __shfl_sync(0xffffffffu, my_page, page & 31);
+            const int id1 = per_tile > 1 ? __shfl_sync(0xffffffffu, my_page, (page + 1) & 31) : -1;
+            if (lane == 0) {
+                constexpr int kLine = D < 128 ? 128 / D : 1;  // tokens per row of the tensor map
+                const int tokens = min(P, kTile);
+                uint8_t* k = ring + slot_in * 2 * C::kTileBytes;
+                const uint32_t bytes = ((id0 >= 0) + (id1 >= 0)) * 2 * tokens * D;
+                tc5::mbar_expect_tx(bar + slot_in, bytes);
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    const int id = j ? id1 : id0;
+                    if (id < 0) continue;
+                    const int row = (int)((((int64_t)id * H + head) * P + (P > kTile ? token % P : 0)) / kLine);
+#pragma unroll
+                    for (int plane = 0; plane < (D + 127) / 128; ++plane) {
+                        const int to = plane * kTile * 128 + j * tokens * (D < 128 ? D : 128);
+                        tc5::tma_load_2d(k + to, &kmap, bar + slot_in, plane * 128, row);
+                        tc5::tma_load_2d(k + C::kTileBytes + to, &vmap, bar + slot_in, plane * 128, row);
+                    }
+                }
+            }
+            if (++slot_in == kStages) slot_in = 0;
+        };
+        int asked = live_from;
+        for (; asked < live_to && asked < live_from + kStages; ++asked) ask(asked);
+
+        for (int t = live_from; t < live_to; ++t) {
+            if (!tc5::mbar_wait(bar + slot_out, phase_out, gave_up)) break;
+            const uint8_t* kt = ring + slot_out * 2 * C::kTileBytes;
+            const uint8_t* vt = kt + C::kTileBytes;
+            const int64_t token = (int64_t)(p.tile0 + t) * kTile;
+            const int page = (int)(token / P) - page0;
+            float2 sc[2];
+            sc[0] = page_scale[warp][page & 63];
+            sc[1] = per_tile > 1 ? page_scale[warp][(page + 1) & 63] : sc[0];
+
+            float st[NT][2][4];
+#pragma unroll
+            for (int mt = 0; mt < 2; ++mt) {
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) st[nt][mt][e] = 0.0f;
+#pragma unroll
+                for (int j = 0; j < D / 64; ++j) {
+                    const int d = D == 64 ? 16 * c : 16 * (2 * c + (j & 1)) + (j >> 1) * 128;
+                    const uint4 lo = *reinterpret_cast<const uint4*>(kt + tile_at<D>(mt * 16 + r, d));
+                    const uint4 hi = *reinterpret_cast<const uint4*>(kt + tile_at<D>(mt * 16 + r + 8, d));
+                    const uint32_t a[4] = {lo.x, lo.y, lo.z, lo.w}, b[4] = {hi.x, hi.y, hi.z, hi.w};
+#pragma unroll
+                    for (int w = 0; w < 4; ++w) {
+                        const uint32_t ua = a[w] ^ 0x80808080u, ub = b[w] ^ 0x80808080u;
+                        const uint32_t a0 = half_pair(ua, 0x4140), a1 = half_pair(ub, 0x4140), a2 = half_pair(ua, 0x4342), a3 = half_pair(ub, 0x4342);
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt) mma_f16(st[nt][mt], a0, a1, a2, a3, qf[nt][4 * j + w][0], qf[nt][4 * j + w][1]);
+                    }
+                }
+            }
+            // scores in powers of two, what is not seen at -infinity
+            const bool inside = token + kTile <= p.len && (!A.causal || token + kTile - 1 <= p0) && (A.window == 0 || token > p1 - A.window);
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        float v = st[nt][mt][e] * (qs[nt][e & 1] * sc[mt].x);
+                        if (!inside) {
+                            const int64_t key = token + mt * 16 + r + (e >> 1) * 8;
+                            const int64_t pos = p.len - p.n + (rb * kR + nt * 8 + 2 * c + (e & 1)) / g;
+                            if (key >= p.len || (A.causal && key > pos) || (A.window > 0 && key <= pos - A.window)) v = -INFINITY;
+                        }
+                        st[nt][mt][e] = v;
+                    }
+            const float ref2 = fmaxf(ref, fmaxf(sc[0].y, sc[1].y)), inv_ref = ref2 > 0.0f ? 1.0f / ref2 : 0.0f;
+            const float vs[2] = {sc[0].y * inv_ref, sc[1].y * inv_ref};
+            const float shrink = ref * inv_ref;
+            ref = ref2;
+            uint32_t pf[NT][2][2];
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+                float keep[2];
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    float top = fmaxf(fmaxf(st[nt][0][e], st[nt][0][e + 2]), fmaxf(st[nt][1][e], st[nt][1][e + 2]));
+                    top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 4));
+                    top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 8));
+                    top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 16));
+                    top = fmaxf(top, m2[nt][e]);
+                    const float at = top == -INFINITY ? 0.0f : top;
+                    keep[e] = ex2(m2[nt][e] - at);
+                    m2[nt][e] = top;
+                    float sum = 0.0f;
+#pragma unroll
+                    for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+                        for (int k = 0; k < 2; ++k) {
+                            const float w = ex2(st[nt][mt][e + 2 * k] - at);
+                            sum += w;
+                            st[nt][mt][e + 2 * k] = w * vs[mt];
+                        }
+                    l[nt][e] = fmaf(l[nt][e], keep[e], sum);  // this lane's tokens only; joined at the end
+                    keep[e] *= shrink;
+                }
+#pragma unroll
+                for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+                    for (int k = 0; k < 2; ++k) {
+                        const __half2 hh = __floats2half2_rn(st[nt][mt][2 * k], st[nt][mt][2 * k + 1]);
+                        pf[nt][mt][k] = transpose8x8(*reinterpret_cast<const uint32_t*>(&hh));
+                    }
+                if (__any_sync(0xffffffffu, keep[0] != 1.0f || keep[1] != 1.0f)) {
+#pragma unroll
+                    for (int i = 0; i < D / 16; ++i)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) o[nt][i][e] *= keep[e & 1];
+                }
+            }
+#pragma unroll
+            for (int kt16 = 0; kt16 < 2; ++kt16)
+#pragma unroll
+                for (int half = 0; half < (D + 127) / 128; ++half) {
+                    constexpr int kW = D == 64 ? 2 : 4;  // words of a lane's run
+                    uint32_t v[4][kW];
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        const uint8_t* at = vt + tile_at<D>(kt16 * 16 + 2 * c + (k & 1) + (k >> 1) * 8, D == 64 ? 8 * r : half * 128 + 16 * r);
+                        if (D == 64) {
+                            const uint2 x = *reinterpret_cast<const uint2*>(at);
+                            v[k][0] = x.x ^ 0x80808080u, v[k][1] = x.y ^ 0x80808080u;
+                        } else {
+                            const uint4 x = *reinterpret_cast<const uint4*>(at);
+                            v[k][0] = x.x ^ 0x80808080u, v[k][1] = x.y ^ 0x80808080u;
+                            v[k][2 % kW] = x.z ^ 0x80808080u, v[k][3 % kW] = x.w ^ 0x80808080u;
+                        }
+                    }
+#pragma unroll
+                    for (int w = 0; w < kW; ++w) {
+                        const uint32_t a01 = __byte_perm(v[0][w], v[1][w], 0x5140), a23 = __byte_perm(v[0][w], v[1][w], 0x7362);
+                        const uint32_t b01 = __byte_perm(v[2][w], v[3][w], 0x5140), b23 = __byte_perm(v[2][w], v[3][w], 0x7362);
+                        const uint32_t f0 = half_pair(a01, 0x4140), f1 = half_pair(a01, 0x4342), f2 = half_pair(b01, 0x4140), f3 = half_pair(b01, 0x4342);
+                        const uint32_t h0 = half_pair(a23, 0x4140), h1 = half_pair(a23, 0x4342), h2 = half_pair(b23, 0x4140), h3 = half_pair(b23, 0x4342);
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt) {
+                            mma_f16(o[nt][half * 8 + 2 * w], f0, f1, f2, f3, pf[nt][kt16][0], pf[nt][kt16][1]);
+                            mma_f16(o[nt][half * 8 + 2 * w + 1], h0, h1, h2, h3, pf[nt][kt16][0], pf[nt][kt16][1]);
+                        }
+                    }
+                }
+            __syncwarp();  // every lane has read the stage
+            if (++slot_out == kStages) slot_out = 0, phase_out ^= 1;
+            if (asked < live_to) ask(asked++);
+        }
+        if (*gave_up) break;
+
+        // the unit's rows: whole, or this worker's part of them
+        const bool whole = t_from == 0 && t_to == p.tiles;
+        float* part = A.parts + ((int64_t)worker * 2 + (t_from == 0)) * C::kPart;
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                float sum = l[nt][e];
+                sum += __shfl_xor_sync(0xffffffffu, sum, 4);
+                sum += __shfl_xor_sync(0xffffffffu, sum, 8);
+                sum += __shfl_xor_sync(0xffffffffu, sum, 16);
+                const int row = nt * 8 + 2 * c + e;
+                if (row >= rows) continue;
+                const float f = whole ? (sum > 0.0f ? ref / sum : 0.0f) : ref;
+                // entries 16 r (8 r for D = 64) and following of the row, in order
+                if (whole) {
+                    const int i = (rb * kR + row) / g, h = head * g + (rb * kR + row) % g;
+                    uint16_t* dst = A.out + (p.first + i) * A.ldo + (int64_t)h * D;
+#pragma unroll
+                    for (int j = 0; j < D / 16; j += 4) {
+                        const int d = D == 64 ? 8 * r : (j >> 3) * 128 + 16 * r + (j & 7) * 2;
+                        uint32_t w[4];
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) w[k] = round16x2<DT>(o[nt][j + k][e] * f, o[nt][j + k][e + 2] * f);
+                        if (A.wide_o) {
+                            *reinterpret_cast<uint4*>(dst + d) = make_uint4(w[0], w[1], w[2], w[3]);
+                        } else {
+#pragma unroll
+                            for (int k = 0; k < 8; ++k) dst[d + k] = (uint16_t)(w[k >> 1] >> (16 * (k & 1)));
+                        }
+                    }
+                    if (A.lse && r == 0) A.lse[(p.first + i) * A.n_heads + h] = sum > 0.0f ? (m2[nt][e] + log2f(sum)) * kLn2 : -INFINITY;
+                } else {
+#pragma unroll
+                    for (int j = 0; j < D / 16; j += 2) {
+                        const int d = D == 64 ? 8 * r + 2 * j : (j >> 3) * 128 + 16 * r + (j & 7) * 2;
+                        *reinterpret_cast<float4*>(part + row * D + d) =
+                            make_float4(o[nt][j][e] * f, o[nt][j][e + 2] * f, o[nt][j + 1][e] * f, o[nt][j + 1][e + 2] * f);
+                    }
+                    if (r == 0) part[kR * D + 2 * row] = m2[nt][e], part[kR * D + 2 * row + 1] = sum;
+                }
+            }
+        x += t_to - t_from;
+    }
+    if (*gave_up) {  // copies that were asked for have to land before the shared memory is given back
+        const long long start = clock64();
+        while (clock64() - start < (1ll << 21)) __nanosleep(1000);
+        if (lane == 0 && A.word) atomicOr(A.word, kWordInternal);
     }
 }
 
-template <int DT>
-static void launch_rows(const AttnArgs& a, cudaStream_t st) {
-    const unsigned n = (unsigned)a.b.n_tok;
-    if (a.c.head_dim == 64) attention_row_kernel<DT, 64><<<n, 128, 0, st>>>(a);
-    else if (a.c.head_dim == 128) attention_row_kernel<DT, 128><<<n, 128, 0, st>>>(a);
-    else attention_row_kernel<DT, 256><<<n, 128, 0, st>>>(a);
+// Joins the parts of the units that were cut, a block per query row and key-value head: thread d holds entry d of a head
+// at a time.  Units that one worker finished are left alone.
+template <int DT, int D, int NT>
+__global__ void __launch_bounds__(D)
+attention_join_kernel(const __grid_constant__ AttnArgs A) {
+    using C = Rows<D, NT>;
+    constexpr int kR = C::kR;
+    __shared__ int64_t scan[D / 32], found[2];
+    const int H = A.c.n_kv_heads, g = A.n_heads / H, tid = threadIdx.x;
+    const int64_t token = blockIdx.x / H;
+    const int head = blockIdx.x % H;
+    const int32_t* off = A.b.tok_off;
+    const int s = block_count(A.b.n_seq, [&](int64_t i) { return off[i] <= token; });
+    if (s >= A.b.n_seq) {
+        tc5::wait_for_previous();  // on every path: this kernel must not end before the one in front of it
+        return;
+    }
+    int64_t total = 0, base = 0;
+    for (int64_t first = 0; first < A.b.n_seq; first += blockDim.x) {
+        int64_t v = 0;
+        if (first + tid < A.b.n_seq) v = seq_tiles(A, seq_plan(A, first + tid, kR));
+        const int64_t upto = block_scan(v, scan);
+        if (first + tid == s) found[0] = total + upto - v;
+        if (tid == (int)blockDim.x - 1) found[1] = upto;
+        __syncthreads();
+        total += found[1];
+        __syncthreads();
+    }
+    base = found[0];
+    const SeqPlan p = seq_plan(A, s, kR);
+    const int64_t per = max((int64_t)1, (total + A.workers - 1) / A.workers);
+    const int i = (int)(token - p.first);
+    tc5::wait_for_previous();
+    if (p.bad) return;
+    for (int j = 0; j < g; ++j) {
+        const int rb = (i * g + j) / kR, row = (i * g + j) % kR;
+        const int64_t from = base + ((int64_t)head * p.blocks + rb) * p.tiles, to = from + p.tiles;
+        const int64_t w0 = from / per, w1 = (to - 1) / per;
+        if (w0 == w1) continue;
+        // the first worker's part begins with the unit, the others' with their run
+        auto part = [&](int64_t w) { return A.parts + (2 * w + (w == w0)) * (int64_t)C::kPart; };
+        float top = -INFINITY;
+        for (int64_t w = w0; w <= w1; ++w) top = fmaxf(top, part(w)[kR * D + 2 * row]);
+        const float at = top == -INFINITY ? 0.0f : top;
+        float sum = 0.0f, o = 0.0f;
+#pragma unroll 4
+        for (int64_t w = w0; w <= w1; ++w) {
+            const float* x = part(w);
+            const float f = ex2(x[kR * D + 2 * row] - at);
+            sum = fmaf(f, x[kR * D + 2 * row + 1], sum);
+            o = fmaf(f, x[row * D + tid], o);
+        }
+        const int h = head * g + j;
+        A.out[token * A.ldo + (int64_t)h * D + tid] = round16<DT>(sum > 0.0f ? o / sum : 0.0f);
+        if (A.lse && tid == 0) A.lse[token * A.n_heads + h] = sum > 0.0f ? (top + log2f(sum)) * kLn2 : -INFINITY;
+    }
 }
+
+template <int DT, int D, int NT>
+static cmpq_status launch_rows(AttnArgs a, cudaStream_t st) {
+    using C = Rows<D, NT>;
+    const cmpq_cache& c = a.c;
+    CUtensorMap kmap, vmap;
+    const int64_t tokens = c.n_pages * c.n_kv_heads * c.page_tokens;
+    const int box_tokens = std::min(c.page_tokens, kTile);
+    const int64_t rows = D == 64 ? tokens / 2 : tokens, width = D == 256 ? 256 : 128;
+    if (rows > INT32_MAX) return CMPQ_ERR_UNSUPPORTED;
+    const int box = D == 64 ? box_tokens / 2 : box_tokens;
+    if (!make_byte_map(&kmap, c.k_codes, rows, width, width, box) || !make_byte_map(&vmap, c.v_codes, rows, width, width, box)) return CMPQ_ERR_CUDA;
+    static bool raised[64];
+    if (!raise_smem_limit_once(attention_rows_kernel<DT, D, NT>, C::kSmem, raised)) return CMPQ_ERR_CUDA;
+    const int blocks = sm_count() * C::kPerSm;
+    a.workers = blocks * C::kWarps;
+    attention_rows_kernel<DT, D, NT><<<blocks, 32 * C::kWarps, C::kSmem, st>>>(kmap, vmap, a);
+    if (cudaGetLastError() != cudaSuccess) return CMPQ_ERR_CUDA;
+    return launch_cluster(attention_join_kernel<DT, D, NT>, (unsigned)(a.b.n_tok * c.n_kv_heads), D, 0, 1, true, st, a);
+}
+
+template <int DT, int D>
+static cmpq_status launch_attention(const AttnArgs& a, cudaStream_t st) {
+    // row blocks of 8 while one holds all rows of a sequence, of 16 otherwise
+    const int64_t rows = a.max_new * (a.n_heads / a.c.n_kv_heads);
+    return rows <= 8 ? launch_rows<DT, D, 1>(a, st) : launch_rows<DT, D, 2>(a, st);
+}
+
+// Room for two parts per worker of the widest row block.
+static size_t parts_bytes(int head_dim) { return (size_t)sm_count() * 2 * 4 * 2 * 16 * (head_dim + 2) * sizeof(float); }
 
 }  // namespace cmpq
 
@@ -83,9 +594,9 @@ using namespace cmpq;
 extern "C" size_t cmpq_cache_attention_ws_bytes(int64_t n_seq, int64_t n_tok, int64_t max_new, int64_t max_len,
                                                 int32_t n_heads, int32_t n_kv_heads, int32_t head_dim) {
     if (n_seq < 0 || n_tok < 0 || max_new < 0 || max_len < 0 || n_heads < 1 || n_kv_heads < 1 || n_heads % n_kv_heads ||
-        head_dim < 1)
+        head_dim < 1 || head_dim > 256)
         return 0;
-    return 256;
+    return round_up(parts_bytes(head_dim), 256);
 }
 
 extern "C" cmpq_status cmpq_cache_attention(const cmpq_cache* cache, const cmpq_batch* batch, const void* q, int64_t ldq,
@@ -95,22 +606,25 @@ extern "C" cmpq_status cmpq_cache_attention(const cmpq_cache* cache, const cmpq_
     cmpq_status why;
     if (!cache_ok(cache, &why)) return why;
     if (!batch_ok(batch) || (dt != CMPQ_F16 && dt != CMPQ_BF16)) return CMPQ_ERR_INVALID_ARG;
-    if (n_heads < 1 || n_heads > 4096 || n_heads % cache->n_kv_heads || max_new < 0 || max_len < 0 || max_len > INT32_MAX)
+    if (n_heads < 1 || n_heads > 4096 || n_heads % cache->n_kv_heads || max_new < 0 || max_len < 0 || max_len > INT32_MAX - 256)
         return CMPQ_ERR_INVALID_ARG;
     if (window < 0 || (window > 0 && !causal) || !(scale > 0.0f) || isinf(scale)) return CMPQ_ERR_INVALID_ARG;
     const int64_t row = (int64_t)n_heads * cache->head_dim;
     if (ldq < row || ldo < row) return CMPQ_ERR_INVALID_ARG;
     if (batch->n_seq == 0 || batch->n_tok == 0) return CMPQ_OK;
     if (!q || !out || !aligned_to(q, 2) || !aligned_to(out, 2) || !aligned_to(lse, 4)) return CMPQ_ERR_INVALID_ARG;
+    if (batch->n_tok * cache->n_kv_heads > INT32_MAX) return CMPQ_ERR_UNSUPPORTED;
     if (!ws || !aligned_to(ws, 256) ||
         ws_bytes < cmpq_cache_attention_ws_bytes(batch->n_seq, batch->n_tok, max_new, max_len, n_heads, cache->n_kv_heads, cache->head_dim))
         return CMPQ_ERR_WORKSPACE;
     AttnArgs a{*cache, *batch, static_cast<const uint16_t*>(q), static_cast<uint16_t*>(out), lse, ldq, ldo, max_new, max_len,
-               window, scale, n_heads, causal != 0, word};
+               window, scale * kLog2e, n_heads, causal != 0, aligned_to(q, 16) && ldq % 8 == 0, aligned_to(out, 16) && ldo % 8 == 0,
+               word, static_cast<float*>(ws), 0};
     auto st = static_cast<cudaStream_t>(stream);
-    if (dt == CMPQ_BF16)
-        launch_rows<CMPQ_BF16>(a, st);
-    else
-        launch_rows<CMPQ_F16>(a, st);
-    return launch_status();
+    const bool bf = dt == CMPQ_BF16;
+    switch (cache->head_dim) {
+        case 64: return bf ? launch_attention<CMPQ_BF16, 64>(a, st) : launch_attention<CMPQ_F16, 64>(a, st);
+        case 128: return bf ? launch_attention<CMPQ_BF16, 128>(a, st) : launch_attention<CMPQ_F16, 128>(a, st);
+        default: return bf ? launch_attention<CMPQ_BF16, 256>(a, st) : launch_attention<CMPQ_F16, 256>(a, st);
+    }
 }

@@ -179,4 +179,30 @@ __device__ __forceinline__ void wait_for_previous() { asm volatile("griddepcontr
 // of box_rows x 128 bytes with the 128-byte swizzle; what lies outside reads as 0.
 bool make_byte_map(CUtensorMap* map, const void* base, int64_t rows, int64_t cols, int64_t ld, int box_rows);
 
+// A launch with clusters of `cluster` CTAs; `behind`: it may start before the kernel in front of it has ended.
+template <class Kernel, class... Args>
+inline cmpq_status launch_cluster(Kernel kern, unsigned grid, int threads, size_t smem, int cluster, bool behind, cudaStream_t st,
+                                  const Args&... args) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(grid);
+    cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[2];
+    unsigned n = 0;
+    if (cluster > 1) {
+        attr[n].id = cudaLaunchAttributeClusterDimension;
+        attr[n].val.clusterDim.x = cluster, attr[n].val.clusterDim.y = 1, attr[n].val.clusterDim.z = 1;
+        ++n;
+    }
+    if (behind) {
+        attr[n].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        attr[n].val.programmaticStreamSerializationAllowed = 1;
+        ++n;
+    }
+    cfg.attrs = attr;
+    cfg.numAttrs = n;
+    return cudaLaunchKernelEx(&cfg, kern, args...) == cudaSuccess ? launch_status() : CMPQ_ERR_CUDA;
+}
+
 }  // namespace cmpq
