@@ -456,14 +456,34 @@ def cmpq_transpose16(src, dst):
 
 
 # ---- serving in 8 bits -----------------------------------------------------------------------------------------
+# These calls are made per layer and token, so their marshalling is kept short: plain addresses, one look at strides.
+
+def _at(t):
+    return None if t is None else t.data_ptr()
+
+
+def _on(t):
+    """The current stream of t's device."""
+    return torch._C._cuda_getCurrentRawStream(t.get_device())
+
 
 def _rows(t, width, name):
     """Leading dimension of a 2-D or 3-D tensor whose rows of `width` elements are contiguous."""
-    inner = t.stride(-1) == 1 and (t.dim() == 2 or t.shape[1] == 1 or t.stride(1) == t.shape[2])
-    if not inner or (t.shape[0] and t[0].numel() != width):
+    shape, stride = t.shape, t.stride()
+    if len(shape) == 3:
+        ok = stride[2] == 1 and shape[1] * shape[2] == width and (stride[1] == shape[2] or shape[1] == 1)
+    else:
+        ok = len(shape) == 2 and shape[1] == width and (stride[1] == 1 or width == 1)
+    if not ok:
         raise ValueError("%s needs contiguous rows of %d elements, got shape %s, strides %s"
-                         % (name, width, tuple(t.shape), tuple(t.stride())))
-    return t.stride(0) if t.shape[0] > 1 else width
+                         % (name, width, tuple(shape), stride))
+    return stride[0] if shape[0] > 1 else width
+
+
+def _code_rows(t):
+    """Leading dimension of a code matrix (whose rows the library wants on multiples of 16 bytes)."""
+    n, d = t.shape
+    return t.stride(0) if n > 1 else (d + 15) // 16 * 16
 
 
 def cmpq_linear_i8_ws_bytes(n, d_in, d_out):
@@ -473,44 +493,46 @@ def cmpq_linear_i8_ws_bytes(n, d_in, d_out):
 def cmpq_quantize_tokens(X, codes, scale, nonfinite=None):
     """codes (int8 [n][d], rows on 16 bytes) and scale (fp32 [n]) of every row of X (fp16/bf16 [n][d])."""
     n, d = X.shape
-    _check(lib().cmpq_quantize_tokens(_ptr(X), dtype_code(X), n, d, _rows(X, d, "X"), _ptr(codes),
-                                      codes.stride(0) if n else (d + 15) // 16 * 16, _ptr(scale), _ptr(nonfinite),
-                                      _stream()), "cmpq_quantize_tokens")
+    _check(lib().cmpq_quantize_tokens(_at(X), dtype_code(X), n, d, _rows(X, d, "X"), _at(codes), _code_rows(codes),
+                                      _at(scale), _at(nonfinite), _on(X)), "cmpq_quantize_tokens")
 
 
 def cmpq_matmul_i8(xc, xs, wc, w_scale, bias, y, ws):
     """y [n][d_out] (fp16/bf16) = xc [n][d_in] times wc [d_out][d_in] (int8), scaled by xs and w_scale, plus bias."""
     n, d_in = xc.shape
-    _check(lib().cmpq_matmul_i8(_ptr(xc), xc.stride(0) if n else (d_in + 15) // 16 * 16, _ptr(xs), _ptr(wc), wc.stride(0),
-                                _ptr(w_scale), _ptr(bias), dtype_code(y), n, d_in, wc.shape[0], _ptr(y),
-                                _rows(y, wc.shape[0], "y"), _ptr(ws), ws.numel(), _stream()), "cmpq_matmul_i8")
+    d_out = wc.shape[0]
+    _check(lib().cmpq_matmul_i8(_at(xc), _code_rows(xc), _at(xs), _at(wc), _code_rows(wc), _at(w_scale), _at(bias),
+                                dtype_code(y), n, d_in, d_out, _at(y), _rows(y, d_out, "y"), _at(ws), ws.numel(),
+                                _on(y)), "cmpq_matmul_i8")
 
 
 def cmpq_linear_i8(X, wc, w_scale, bias, y, ws, nonfinite=None):
     """y = the 8-bit linear layer (wc, w_scale, bias) of X (fp16/bf16 [n][d_in])."""
     n, d_in = X.shape
-    _check(lib().cmpq_linear_i8(_ptr(X), dtype_code(X), n, d_in, _rows(X, d_in, "X"), _ptr(wc), wc.stride(0),
-                                _ptr(w_scale), _ptr(bias), wc.shape[0], _ptr(y), _rows(y, wc.shape[0], "y"),
-                                _ptr(nonfinite), _ptr(ws), ws.numel(), _stream()), "cmpq_linear_i8")
+    d_out = wc.shape[0]
+    _check(lib().cmpq_linear_i8(_at(X), dtype_code(X), n, d_in, _rows(X, d_in, "X"), _at(wc), _code_rows(wc),
+                                _at(w_scale), _at(bias), d_out, _at(y), _rows(y, d_out, "y"), _at(nonfinite), _at(ws),
+                                ws.numel(), _on(X)), "cmpq_linear_i8")
 
 
 def cmpq_check_cache(word):
     """Waits for the current stream; raises CmpqError when a cache call reported something in `word`."""
-    _check(lib().cmpq_check_cache(_ptr(word), _stream()), "cmpq_check_cache")
+    _check(lib().cmpq_check_cache(_at(word), _on(word)), "cmpq_check_cache")
 
 
 def cmpq_cache_append(cache, batch, k, v, cos=None, sin=None, interleaved=False, q=None, q_out=None, word=None):
     """cache, batch: Cache and Batch structures.  k, v: [n_tok][n_kv][d]; q, q_out: [n_tok][n_heads][d] or None;
     cos, sin: fp32 [n_pos][rot_dim / 2] or None."""
-    row = cache.n_kv_heads * cache.head_dim
-    heads = q.shape[1] if q is not None else 0
-    qrow = heads * cache.head_dim
-    _check(lib().cmpq_cache_append(cache, batch, _ptr(k), _rows(k, row, "k"), _ptr(v), _rows(v, row, "v"), dtype_code(k),
-                                   _ptr(cos), _ptr(sin), 0 if cos is None else cos.shape[0],
-                                   0 if cos is None else 2 * cos.shape[1], int(interleaved), _ptr(q),
-                                   0 if q is None else _rows(q, qrow, "q"), heads, _ptr(q_out),
-                                   0 if q is None else _rows(q_out, qrow, "q_out"), _ptr(word), _stream()),
-           "cmpq_cache_append")
+    d = cache.head_dim
+    row = cache.n_kv_heads * d
+    n_pos, half = (0, 0) if cos is None else cos.shape
+    heads = ldq = ldqo = 0
+    if q is not None:
+        heads = q.shape[1]
+        ldq, ldqo = _rows(q, heads * d, "q"), _rows(q_out, heads * d, "q_out")
+    _check(lib().cmpq_cache_append(cache, batch, k.data_ptr(), _rows(k, row, "k"), v.data_ptr(), _rows(v, row, "v"),
+                                   dtype_code(k), _at(cos), _at(sin), n_pos, 2 * half, int(interleaved), _at(q), ldq,
+                                   heads, _at(q_out), ldqo, _at(word), _on(k)), "cmpq_cache_append")
 
 
 def cmpq_cache_read(cache, batch, k_out, v_out, word=None):
@@ -519,8 +541,8 @@ def cmpq_cache_read(cache, batch, k_out, v_out, word=None):
     ld = _rows(k_out, row, "k_out")
     if _rows(v_out, row, "v_out") != ld or v_out.dtype != k_out.dtype:
         raise ValueError("k_out and v_out need one row stride and dtype")
-    _check(lib().cmpq_cache_read(cache, batch, dtype_code(k_out), _ptr(k_out), _ptr(v_out), ld, _ptr(word), _stream()),
-           "cmpq_cache_read")
+    _check(lib().cmpq_cache_read(cache, batch, dtype_code(k_out), k_out.data_ptr(), v_out.data_ptr(), ld, _at(word),
+                                 _on(k_out)), "cmpq_cache_read")
 
 
 def cmpq_cache_attention_ws_bytes(n_seq, n_tok, max_new, max_len, n_heads, n_kv_heads, head_dim):
@@ -531,6 +553,6 @@ def cmpq_cache_attention(cache, batch, q, max_new, max_len, scale, causal, windo
     """q, out: [n_tok][n_heads][d] fp16/bf16; lse: fp32 [n_tok][n_heads] or None."""
     heads = q.shape[1]
     row = heads * cache.head_dim
-    _check(lib().cmpq_cache_attention(cache, batch, _ptr(q), _rows(q, row, "q"), dtype_code(q), heads, max_new, max_len,
-                                      scale, int(causal), window, _ptr(out), _rows(out, row, "out"), _ptr(lse),
-                                      _ptr(word), _ptr(ws), ws.numel(), _stream()), "cmpq_cache_attention")
+    _check(lib().cmpq_cache_attention(cache, batch, q.data_ptr(), _rows(q, row, "q"), dtype_code(q), heads, max_new,
+                                      max_len, scale, int(causal), window, out.data_ptr(), _rows(out, row, "out"),
+                                      _at(lse), _at(word), ws.data_ptr(), ws.numel(), _on(q)), "cmpq_cache_attention")

@@ -16,9 +16,11 @@ struct AttnArgs {
     const uint16_t* q;
     uint16_t* out;
     float* lse;
-    int64_t ldq, ldo, max_new, max_len, window;
+    int64_t ldq, ldo;
+    int max_new, max_len, window;
     float scale;  // times log2(e): scores are kept in powers of two
-    int n_heads, causal;
+    int n_heads, group, causal;
+    int page_bits;  // log2 of a page's tokens
     int wide_q, wide_o;
     int32_t* word;
     float* parts;  // partial results of the workers, see there
@@ -37,42 +39,42 @@ __device__ __forceinline__ float ex2(float x) {
 //
 // The time is that of reading the cache once, so the keys are split over all warps of the GPU.  The rows of a sequence
 // and key-value head (its new tokens times the query heads of the group) are taken R = 8 NT at a time; such a unit is a
-// run of tiles of 32 tokens.  All units' tiles, one behind the other, are dealt to the workers (warps) in equal
+// run of tiles of 64 or 32 tokens.  All units' tiles, one behind the other, are dealt to the workers (warps) in equal
 // contiguous runs: sequences of any lengths balance, and a worker meets few unit borders.  A unit inside one worker's
 // run is finished there; the parts of one that is cut go to the work space and are joined by a second kernel in the
 // order of the workers (no atomics: the same bytes every time).
-constexpr int kTile = 32;
+constexpr int kMaxPerSm = 12;  // workers of an SM
 
 template <int D, int NT>
 struct Rows {
     static constexpr int kR = 8 * NT;
     static constexpr int kWarps = 4;
+    static constexpr int kTile = NT == 1 && D <= 128 ? 64 : 32;             // tokens; what the registers allow
     static constexpr int kTileBytes = kTile * D;                            // keys; as many for the values
-    static constexpr int kStages = D == 64 ? 6 : D == 128 ? 3 : 2;
-    static constexpr int kSmem = kWarps * kStages * 2 * kTileBytes + 1024;  // 97 KB (D 64, 128) or 129 KB
-    static constexpr int kPerSm = D == 256 ? 1 : 2;
+    static constexpr int kBuffers = kTile == 64 ? 1 : 2;
+    static constexpr int kPerSm = NT == 1 && D <= 128 ? 3 : D == 256 ? 1 : 2;
+    static constexpr int kSmem = kWarps * kBuffers * 2 * kTileBytes + 1024;
     static constexpr int kPart = kR * (D + 2);                              // floats of a partial result
 };
 
 struct SeqPlan {
-    int64_t first, n, len;  // row of the first query, queries, cached tokens
+    int first, n, len;  // row of the first query, queries, cached tokens
     int tile0, tiles, blocks;
     bool bad;
 };
 
 // What a sequence needs: its tiles per unit (one at least, so that rows without a key are written too) and its row
 // blocks.  `count` of its tiles is tiles * blocks * heads, 0 for a sequence without queries or with bad lengths.
-__device__ __forceinline__ SeqPlan seq_plan(const AttnArgs& A, int64_t s, int rows) {
+__device__ __forceinline__ SeqPlan seq_plan(const AttnArgs& A, int64_t s, int rows, int tile) {
     SeqPlan p;
     p.first = A.b.tok_off[s];
     p.n = A.b.tok_off[s + 1] - p.first;
     p.len = A.b.lens[s];
-    p.bad = p.len < 0 || p.len > A.max_len || p.n < 0 || p.n > A.max_new || p.first < 0 || p.first + p.n > A.b.n_tok;
-    const int64_t lo = A.window > 0 ? max((int64_t)0, p.len - p.n - A.window + 1) : 0;
-    p.tile0 = (int)(lo / kTile);
-    p.tiles = max(1, (int)((p.len + kTile - 1) / kTile) - p.tile0);
-    const int g = A.n_heads / A.c.n_kv_heads;
-    p.blocks = p.bad ? 0 : (int)((p.n * g + rows - 1) / rows);
+    p.bad = p.len < 0 || p.len > A.max_len || p.n < 0 || p.n > A.max_new || p.first < 0 || (int64_t)p.first + p.n > A.b.n_tok;
+    const int lo = A.window > 0 ? max(0, p.len - p.n - A.window + 1) : 0;
+    p.tile0 = lo / tile;
+    p.tiles = p.bad ? 1 : max(1, (p.len + tile - 1) / tile - p.tile0);
+    p.blocks = p.bad ? 0 : (p.n * A.group + rows - 1) / rows;
     return p;
 }
 __device__ __forceinline__ int64_t seq_tiles(const AttnArgs& A, const SeqPlan& p) {
@@ -113,14 +115,14 @@ __device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {
 
 // Bytes of token t's entries from d on in a tile: rows of 128 bytes (two tokens of 64 entries, or half a token of 256 in
 // a plane of its own), 16-byte groups swizzled by the row as the tensor map leaves them.
-template <int D>
+template <int D, int TILE>
 __device__ __forceinline__ uint32_t tile_at(int t, int d) {
     if (D == 64) {
         const int row = t >> 1;
         return row * 128 + ((((t & 1) * 4 + (d >> 4)) ^ (row & 7)) << 4) + (d & 15);
     }
     const int plane = D == 256 ? d >> 7 : 0, e = D == 256 ? d & 127 : d;
-    return plane * (kTile * 128) + t * 128 + (((e >> 4) ^ (t & 7)) << 4) + (e & 15);
+    return plane * (TILE * 128) + t * 128 + (((e >> 4) ^ (t & 7)) << 4) + (e & 15);
 }
 
 // A lane's place in the m16n8k16 fragments: r = lane / 4, c = lane % 4.
@@ -138,9 +140,9 @@ __global__ void __launch_bounds__(128, Rows<D, NT>::kPerSm)
 attention_rows_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUtensorMap vmap,
                       const __grid_constant__ AttnArgs A) {
     using C = Rows<D, NT>;
-    constexpr int kR = C::kR, kStages = C::kStages;
+    constexpr int kR = C::kR, kTile = C::kTile, kBuffers = C::kBuffers, MT = kTile / 16;
     extern __shared__ uint8_t raw[];
-    __shared__ uint64_t bars[C::kWarps][kStages];
+    __shared__ uint64_t bars[C::kWarps][2][kBuffers];
     __shared__ int64_t scan[C::kWarps];
     __shared__ int64_t start_base[C::kWarps];
     __shared__ int start_seq[C::kWarps];
@@ -148,60 +150,58 @@ attention_rows_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_con
     __shared__ int failed[C::kWarps];
     uint8_t* smem = raw + ((1024u - (tc5::smem_addr(raw) & 1023u)) & 1023u);
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, r = lane >> 2, c = lane & 3;
-    const int H = A.c.n_kv_heads, g = A.n_heads / H, P = A.c.page_tokens;
+    const int H = A.c.n_kv_heads, g = A.group, P = A.c.page_tokens, page_bits = A.page_bits;
     tc5::dependents_may_start();
     if (lane == 0) {
-        for (int i = 0; i < kStages; ++i) tc5::mbar_init(&bars[warp][i], 1);
+        for (int i = 0; i < kBuffers; ++i) tc5::mbar_init(&bars[warp][0][i], 1), tc5::mbar_init(&bars[warp][1][i], 1);
         failed[warp] = 0;
         tc5::mbar_init_fence();
     }
 
     // the total, this warp's run, and the sequence it starts in
-    int64_t total = 0;
+    int64_t total = 0, mine = 0, upto = 0;
     for (int64_t base = 0; base < A.b.n_seq; base += blockDim.x) {
-        int64_t v = 0;
+        mine = 0;
         if (base + tid < A.b.n_seq) {
-            const SeqPlan p = seq_plan(A, base + tid, kR);
-            v = seq_tiles(A, p);
+            const SeqPlan p = seq_plan(A, base + tid, kR, kTile);
+            mine = seq_tiles(A, p);
             if (p.bad && blockIdx.x == 0 && A.word) atomicOr(A.word, kWordTable);
         }
-        v = block_scan(v, scan);
-        if (tid == (int)blockDim.x - 1) start_base[0] = v;
+        upto = block_scan(mine, scan) + total;
+        if (tid == (int)blockDim.x - 1) start_base[0] = upto;
         __syncthreads();
-        total += start_base[0];
+        total = start_base[0];
         __syncthreads();
     }
     const int64_t per = max((int64_t)1, (total + A.workers - 1) / A.workers);
     const int worker = blockIdx.x * C::kWarps + warp;
     const int64_t begin = worker * per, end = min(total, begin + per);
-    {
-        int64_t before = 0;
-        for (int64_t base = 0; base < A.b.n_seq; base += blockDim.x) {
-            int64_t v = 0;
-            if (base + tid < A.b.n_seq) v = seq_tiles(A, seq_plan(A, base + tid, kR));
-            const int64_t upto = before + block_scan(v, scan), from = upto - v;
-#pragma unroll
-            for (int w = 0; w < C::kWarps; ++w) {
-                const int64_t x = (blockIdx.x * C::kWarps + w) * per;
-                if (x < total && from <= x && x < upto) start_seq[w] = (int)(base + tid), start_base[w] = from;
-            }
-            if (tid == (int)blockDim.x - 1) scan[0] = upto;
-            __syncthreads();
-            before = scan[0];
-            __syncthreads();
+    int64_t before = 0;
+    for (int64_t base = 0; base < A.b.n_seq; base += blockDim.x) {
+        if (A.b.n_seq > blockDim.x) {  // the sums again, chunk by chunk; of a single chunk they are still there
+            mine = base + tid < A.b.n_seq ? seq_tiles(A, seq_plan(A, base + tid, kR, kTile)) : 0;
+            upto = before + block_scan(mine, scan);
         }
+        const int64_t from = upto - mine;
+#pragma unroll
+        for (int w = 0; w < C::kWarps; ++w) {
+            const int64_t x = (blockIdx.x * C::kWarps + w) * per;
+            if (x < total && from <= x && x < upto) start_seq[w] = (int)(base + tid), start_base[w] = from;
+        }
+        if (tid == (int)blockDim.x - 1) scan[0] = upto;
+        __syncthreads();
+        before = scan[0];
+        __syncthreads();
     }
     if (begin >= end) return;
 
     int64_t s = start_seq[warp], base = start_base[warp];
-    uint8_t* ring = smem + warp * (kStages * 2 * C::kTileBytes);
-    uint64_t* bar = bars[warp];
+    uint8_t* ring = smem + warp * (kBuffers * 2 * C::kTileBytes);  // keys, then values
     volatile int* gave_up = &failed[warp];
-    int slot_in = 0, slot_out = 0, phase_out = 0;
-    const int per_tile = P < kTile ? kTile / P : 1;  // pages that a tile touches
+    int slot[2] = {0, 0}, phase[2] = {0, 0}, next[2] = {0, 0};  // of the keys and of the values: next to read, to fill
 
     for (int64_t x = begin; x < end;) {
-        const SeqPlan p = seq_plan(A, s, kR);
+        const SeqPlan p = seq_plan(A, s, kR, C::kTile);
         const int64_t all = seq_tiles(A, p);
         if (x >= base + all) {  // also a sequence without tiles
             base += all;
@@ -212,13 +212,20 @@ attention_rows_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_con
         const int t_from = (int)((x - base) % p.tiles);
         const int t_to = (int)min((int64_t)p.tiles, t_from + (end - x));  // tiles of this unit that are this worker's
         const int head = (int)(unit / p.blocks), rb = (int)(unit % p.blocks);
-        const int rows = (int)min((int64_t)kR, p.n * g - (int64_t)rb * kR);
+        const int rows = min(kR, p.n * g - rb * kR);
         // positions of the block's first and last query; keys that any of them sees
-        const int64_t p0 = p.len - p.n + (rb * kR) / g, p1 = p.len - p.n + (rb * kR + rows - 1) / g;
-        const int64_t key_hi = A.causal ? max((int64_t)0, p1 + 1) : p.len;
-        const int64_t key_lo = A.window > 0 ? max((int64_t)0, p0 - A.window + 1) : 0;
-        const int live_from = max(t_from, (int)(key_lo / kTile) - p.tile0);
-        const int live_to = min(t_to, (int)((key_hi + kTile - 1) / kTile) - p.tile0);
+        const int p0 = p.len - p.n + (rb * kR) / g, p1 = p.len - p.n + (rb * kR + rows - 1) / g;
+        const int key_hi = A.causal ? max(0, p1 + 1) : p.len;
+        const int key_lo = A.window > 0 ? max(0, p0 - A.window + 1) : 0;
+        const int live_from = max(t_from, key_lo / kTile - p.tile0);
+        const int live_to = min(t_to, (key_hi + kTile - 1) / kTile - p.tile0);
+        // from this token on some row does not see a tile whole, and up to this one
+        const int whole_hi = A.causal ? min(p.len, p0 + 1) : p.len, whole_lo = A.window > 0 ? p1 - A.window + 1 : 0;
+        int row_pos[NT][2];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) row_pos[nt][e] = p.len - p.n + (rb * kR + nt * 8 + 2 * c + e) / g;
 
         // the queries, scaled into fp16
         uint32_t qf[NT][D / 16][2];
@@ -233,7 +240,7 @@ attention_rows_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_con
                 const int d = (D == 64 ? 16 * c : 16 * (2 * c + ((e >> 4) & 1)) + (e >> 5) * 128) + (e & 15);
                 float v[8];
                 if (row < rows) {
-                    const uint16_t* src = A.q + (p.first + i) * A.ldq + (int64_t)h * D + d;
+                    const uint16_t* src = A.q + (int64_t)(p.first + i) * A.ldq + (int64_t)h * D + d;
                     widen8<DT>(load8(src, 8, A.wide_q), v);
                 } else {
 #pragma unroll
@@ -256,7 +263,7 @@ attention_rows_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_con
             qs[nt][1] = __shfl_sync(0xffffffffu, mine, (2 * c + 1) * 4);
         }
 
-        float o[NT][D / 16][4], m2[NT][2], l[NT][2], ref = 0.0f;
+        float o[NT][D / 16][4], m2[NT][2], l[NT][2], ref = 0.0f, inv_ref = 0.0f;
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
@@ -268,8 +275,8 @@ attention_rows_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_con
         }
 
         // Pages are asked for 32 at a time, one per lane, with their scales; lane 0 has the copies of a tile made.
-        const int page0 = (int)(((int64_t)(p.tile0 + live_from) * kTile) / P);
-        const int page_end = (int)((p.len + P - 1) / P);
+        const int page0 = ((p.tile0 + live_from) * kTile) >> page_bits;
+        const int page_end = (p.len + P - 1) >> page_bits;
         int my_page = -1, have = 0;  // pages page0 .. page0 + have are known
         auto fetch_pages = [&]() {
             const int page = page0 + have + lane;
@@ -289,49 +296,57 @@ attention_rows_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_con
             have += 32;
             __syncwarp();
         };
-        auto ask = [&](int t) {  // tile t of the unit
-            const int64_t token = (int64_t)(p.tile0 + t) * kTile;
-            const int page = (int)(token / P) - page0;
-            if (page >= have) fetch_pages();
-            const int id0 = __shfl_sync(0xffffffffu, my_page, page & 31);
-            const int id1 = per_tile > 1 ? __shfl_sync(0xffffffffu, my_page, (page + 1) & 31) : -1;
-            if (lane == 0) {
-                constexpr int kLine = D < 128 ? 128 / D : 1;  // tokens per row of the tensor map
-                const int tokens = min(P, kTile);
-                uint8_t* k = ring + slot_in * 2 * C::kTileBytes;
-                const uint32_t bytes = ((id0 >= 0) + (id1 >= 0)) * 2 * tokens * D;
-                tc5::mbar_expect_tx(bar + slot_in, bytes);
+        auto ask = [&](int t, int which) {  // keys (0) or values (1) of tile t of the unit
+            const int token = (p.tile0 + t) * kTile;
+            const int page = (token >> page_bits) - page0;
+            if (page >= have) fetch_pages();  // 32 pages hold whole tiles
+            constexpr int kLine = D < 128 ? 128 / D : 1;  // tokens per row of the tensor map
+            const int pieces = P < kTile ? kTile >> page_bits : 1, tokens = P < kTile ? P : kTile;
+            const int first_id = __shfl_sync(0xffffffffu, my_page, page & 31);
+            if (pieces == 1) {
+                if (lane == 0) {
+                    uint64_t* bar = &bars[warp][which][next[which]];
+                    uint8_t* to = ring + (which * kBuffers + next[which]) * C::kTileBytes;
+                    tc5::mbar_expect_tx(bar, first_id >= 0 ? C::kTileBytes : 0);
+                    if (first_id >= 0) {
+                        const int row = (int)(((((int64_t)first_id * H + head) << page_bits) + (token & (P - 1))) / kLine);
 #pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    const int id = j ? id1 : id0;
-                    if (id < 0) continue;
-                    const int row = (int)((((int64_t)id * H + head) * P + (P > kTile ? token % P : 0)) / kLine);
-#pragma unroll
-                    for (int plane = 0; plane < (D + 127) / 128; ++plane) {
-                        const int to = plane * kTile * 128 + j * tokens * (D < 128 ? D : 128);
-                        tc5::tma_load_2d(k + to, &kmap, bar + slot_in, plane * 128, row);
-                        tc5::tma_load_2d(k + C::kTileBytes + to, &vmap, bar + slot_in, plane * 128, row);
+                        for (int plane = 0; plane < (D + 127) / 128; ++plane)
+                            tc5::tma_load_2d(to + plane * kTile * 128, which ? &vmap : &kmap, bar, plane * 128, row);
                     }
                 }
+            } else {
+                // a lane per page: the first lanes look at the pages that follow
+                const int id = __shfl_sync(0xffffffffu, my_page, (page + lane) & 31);
+                const bool mine_too = lane < pieces && id >= 0;
+                const int n = __popc(__ballot_sync(0xffffffffu, mine_too));
+                uint64_t* bar = &bars[warp][which][next[which]];
+                if (lane == 0) tc5::mbar_expect_tx(bar, n * tokens * D);
+                __syncwarp();
+                if (mine_too) {
+                    uint8_t* to = ring + (which * kBuffers + next[which]) * C::kTileBytes + lane * tokens * (D < 128 ? D : 128);
+                    const int row = (int)((((int64_t)id * H + head) << page_bits) / kLine);
+#pragma unroll
+                    for (int plane = 0; plane < (D + 127) / 128; ++plane)
+                        tc5::tma_load_2d(to + plane * kTile * 128, which ? &vmap : &kmap, bar, plane * 128, row);
+                }
             }
-            if (++slot_in == kStages) slot_in = 0;
+            if (++next[which] == kBuffers) next[which] = 0;
         };
-        int asked = live_from;
-        for (; asked < live_to && asked < live_from + kStages; ++asked) ask(asked);
+        for (int t = live_from; t < live_to && t < live_from + kBuffers; ++t) ask(t, 0), ask(t, 1);
 
         for (int t = live_from; t < live_to; ++t) {
-            if (!tc5::mbar_wait(bar + slot_out, phase_out, gave_up)) break;
-            const uint8_t* kt = ring + slot_out * 2 * C::kTileBytes;
-            const uint8_t* vt = kt + C::kTileBytes;
-            const int64_t token = (int64_t)(p.tile0 + t) * kTile;
-            const int page = (int)(token / P) - page0;
-            float2 sc[2];
-            sc[0] = page_scale[warp][page & 63];
-            sc[1] = per_tile > 1 ? page_scale[warp][(page + 1) & 63] : sc[0];
-
-            float st[NT][2][4];
+            const int token = (p.tile0 + t) * kTile;
+            const int page = (token >> page_bits) - page0;
+            float2 sc[MT];
 #pragma unroll
-            for (int mt = 0; mt < 2; ++mt) {
+            for (int mt = 0; mt < MT; ++mt) sc[mt] = page_scale[warp][(page + ((mt * 16) >> page_bits)) & 63];
+
+            if (!tc5::mbar_wait(&bars[warp][0][slot[0]], phase[0], gave_up)) break;
+            const uint8_t* kt = ring + slot[0] * C::kTileBytes;
+            float st[NT][MT][4];
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt) {
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -339,8 +354,8 @@ attention_rows_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_con
 #pragma unroll
                 for (int j = 0; j < D / 64; ++j) {
                     const int d = D == 64 ? 16 * c : 16 * (2 * c + (j & 1)) + (j >> 1) * 128;
-                    const uint4 lo = *reinterpret_cast<const uint4*>(kt + tile_at<D>(mt * 16 + r, d));
-                    const uint4 hi = *reinterpret_cast<const uint4*>(kt + tile_at<D>(mt * 16 + r + 8, d));
+                    const uint4 lo = *reinterpret_cast<const uint4*>(kt + tile_at<D, kTile>(mt * 16 + r, d));
+                    const uint4 hi = *reinterpret_cast<const uint4*>(kt + tile_at<D, kTile>(mt * 16 + r + 8, d));
                     const uint32_t a[4] = {lo.x, lo.y, lo.z, lo.w}, b[4] = {hi.x, hi.y, hi.z, hi.w};
 #pragma unroll
                     for (int w = 0; w < 4; ++w) {
@@ -351,33 +366,52 @@ attention_rows_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_con
                     }
                 }
             }
+            __syncwarp();  // every lane has read the keys
+            if (++slot[0] == kBuffers) slot[0] = 0, phase[0] ^= 1;
+            if (t + kBuffers < live_to) ask(t + kBuffers, 0);
+
             // scores in powers of two, what is not seen at -infinity
-            const bool inside = token + kTile <= p.len && (!A.causal || token + kTile - 1 <= p0) && (A.window == 0 || token > p1 - A.window);
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                for (int mt = 0; mt < 2; ++mt)
+                for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) st[nt][mt][e] *= qs[nt][e & 1] * sc[mt].x;
+            if (token + kTile > whole_hi || token < whole_lo) {
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        float v = st[nt][mt][e] * (qs[nt][e & 1] * sc[mt].x);
-                        if (!inside) {
-                            const int64_t key = token + mt * 16 + r + (e >> 1) * 8;
-                            const int64_t pos = p.len - p.n + (rb * kR + nt * 8 + 2 * c + (e & 1)) / g;
-                            if (key >= p.len || (A.causal && key > pos) || (A.window > 0 && key <= pos - A.window)) v = -INFINITY;
+                        const int pos = row_pos[nt][e & 1];
+                        const int hi = A.causal ? min(p.len, pos + 1) : p.len, lo = A.window > 0 ? pos - A.window : -1;
+#pragma unroll
+                        for (int mt = 0; mt < MT; ++mt) {
+                            const int key = token + mt * 16 + r + (e >> 1) * 8;
+                            if (key >= hi || key <= lo) st[nt][mt][e] = -INFINITY;
                         }
-                        st[nt][mt][e] = v;
                     }
-            const float ref2 = fmaxf(ref, fmaxf(sc[0].y, sc[1].y)), inv_ref = ref2 > 0.0f ? 1.0f / ref2 : 0.0f;
-            const float vs[2] = {sc[0].y * inv_ref, sc[1].y * inv_ref};
-            const float shrink = ref * inv_ref;
-            ref = ref2;
-            uint32_t pf[NT][2][2];
+            }
+            // values are taken relative to the largest value scale so far, so that the weights fit fp16
+            float shrink = 1.0f;
+            {
+                float most = sc[0].y;
+#pragma unroll
+                for (int mt = 1; mt < MT; ++mt) most = fmaxf(most, sc[mt].y);
+                if (most > ref) {  // the same for the whole warp
+                    inv_ref = 1.0f / most;
+                    shrink = ref * inv_ref;
+                    ref = most;
+                }
+            }
+            uint32_t pf[NT][MT][2];
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
                 float keep[2];
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
-                    float top = fmaxf(fmaxf(st[nt][0][e], st[nt][0][e + 2]), fmaxf(st[nt][1][e], st[nt][1][e + 2]));
+                    float top = fmaxf(st[nt][0][e], st[nt][0][e + 2]);
+#pragma unroll
+                    for (int mt = 1; mt < MT; ++mt) top = fmaxf(top, fmaxf(st[nt][mt][e], st[nt][mt][e + 2]));
                     top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 4));
                     top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 8));
                     top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 16));
@@ -387,18 +421,20 @@ attention_rows_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_con
                     m2[nt][e] = top;
                     float sum = 0.0f;
 #pragma unroll
-                    for (int mt = 0; mt < 2; ++mt)
+                    for (int mt = 0; mt < MT; ++mt) {
+                        const float vs = sc[mt].y * inv_ref;
 #pragma unroll
                         for (int k = 0; k < 2; ++k) {
                             const float w = ex2(st[nt][mt][e + 2 * k] - at);
                             sum += w;
-                            st[nt][mt][e + 2 * k] = w * vs[mt];
+                            st[nt][mt][e + 2 * k] = w * vs;
                         }
+                    }
                     l[nt][e] = fmaf(l[nt][e], keep[e], sum);  // this lane's tokens only; joined at the end
                     keep[e] *= shrink;
                 }
 #pragma unroll
-                for (int mt = 0; mt < 2; ++mt)
+                for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
                     for (int k = 0; k < 2; ++k) {
                         const __half2 hh = __floats2half2_rn(st[nt][mt][2 * k], st[nt][mt][2 * k + 1]);
@@ -411,15 +447,17 @@ attention_rows_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_con
                         for (int e = 0; e < 4; ++e) o[nt][i][e] *= keep[e & 1];
                 }
             }
+            if (!tc5::mbar_wait(&bars[warp][1][slot[1]], phase[1], gave_up)) break;
+            const uint8_t* vt = ring + (kBuffers + slot[1]) * C::kTileBytes;
 #pragma unroll
-            for (int kt16 = 0; kt16 < 2; ++kt16)
+            for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
                 for (int half = 0; half < (D + 127) / 128; ++half) {
                     constexpr int kW = D == 64 ? 2 : 4;  // words of a lane's run
                     uint32_t v[4][kW];
 #pragma unroll
                     for (int k = 0; k < 4; ++k) {
-                        const uint8_t* at = vt + tile_at<D>(kt16 * 16 + 2 * c + (k & 1) + (k >> 1) * 8, D == 64 ? 8 * r : half * 128 + 16 * r);
+                        const uint8_t* at = vt + tile_at<D, kTile>(mt * 16 + 2 * c + (k & 1) + (k >> 1) * 8, D == 64 ? 8 * r : half * 128 + 16 * r);
                         if (D == 64) {
                             const uint2 x = *reinterpret_cast<const uint2*>(at);
                             v[k][0] = x.x ^ 0x80808080u, v[k][1] = x.y ^ 0x80808080u;
@@ -437,14 +475,14 @@ attention_rows_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_con
                         const uint32_t h0 = half_pair(a23, 0x4140), h1 = half_pair(a23, 0x4342), h2 = half_pair(b23, 0x4140), h3 = half_pair(b23, 0x4342);
 #pragma unroll
                         for (int nt = 0; nt < NT; ++nt) {
-                            mma_f16(o[nt][half * 8 + 2 * w], f0, f1, f2, f3, pf[nt][kt16][0], pf[nt][kt16][1]);
-                            mma_f16(o[nt][half * 8 + 2 * w + 1], h0, h1, h2, h3, pf[nt][kt16][0], pf[nt][kt16][1]);
+                            mma_f16(o[nt][half * 8 + 2 * w], f0, f1, f2, f3, pf[nt][mt][0], pf[nt][mt][1]);
+                            mma_f16(o[nt][half * 8 + 2 * w + 1], h0, h1, h2, h3, pf[nt][mt][0], pf[nt][mt][1]);
                         }
                     }
                 }
-            __syncwarp();  // every lane has read the stage
-            if (++slot_out == kStages) slot_out = 0, phase_out ^= 1;
-            if (asked < live_to) ask(asked++);
+            __syncwarp();  // every lane has read the values
+            if (++slot[1] == kBuffers) slot[1] = 0, phase[1] ^= 1;
+            if (t + kBuffers < live_to) ask(t + kBuffers, 1);
         }
         if (*gave_up) break;
 
@@ -465,7 +503,7 @@ attention_rows_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_con
                 // entries 16 r (8 r for D = 64) and following of the row, in order
                 if (whole) {
                     const int i = (rb * kR + row) / g, h = head * g + (rb * kR + row) % g;
-                    uint16_t* dst = A.out + (p.first + i) * A.ldo + (int64_t)h * D;
+                    uint16_t* dst = A.out + (int64_t)(p.first + i) * A.ldo + (int64_t)h * D;
 #pragma unroll
                     for (int j = 0; j < D / 16; j += 4) {
                         const int d = D == 64 ? 8 * r : (j >> 3) * 128 + 16 * r + (j & 7) * 2;
@@ -479,7 +517,7 @@ attention_rows_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_con
                             for (int k = 0; k < 8; ++k) dst[d + k] = (uint16_t)(w[k >> 1] >> (16 * (k & 1)));
                         }
                     }
-                    if (A.lse && r == 0) A.lse[(p.first + i) * A.n_heads + h] = sum > 0.0f ? (m2[nt][e] + log2f(sum)) * kLn2 : -INFINITY;
+                    if (A.lse && r == 0) A.lse[(int64_t)(p.first + i) * A.n_heads + h] = sum > 0.0f ? (m2[nt][e] + log2f(sum)) * kLn2 : -INFINITY;
                 } else {
 #pragma unroll
                     for (int j = 0; j < D / 16; j += 2) {
@@ -499,15 +537,19 @@ attention_rows_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_con
     }
 }
 
-// Joins the parts of the units that were cut, a block per query row and key-value head: thread d holds entry d of a head
-// at a time.  Units that one worker finished are left alone.
+// Joins the parts of the units that were cut, a block of eight warps per query row and key-value head.  The workers'
+// maxima and sums are read side by side, a thread each; then the warps take every eighth part, a lane D/32 neighbouring
+// entries.  The order of the sums goes by the parts' numbers alone.  Units that one worker finished are left alone.
+constexpr int kMaxWorkers = 2048;
+
 template <int DT, int D, int NT>
-__global__ void __launch_bounds__(D)
+__global__ void __launch_bounds__(256)
 attention_join_kernel(const __grid_constant__ AttnArgs A) {
     using C = Rows<D, NT>;
-    constexpr int kR = C::kR;
-    __shared__ int64_t scan[D / 32], found[2];
-    const int H = A.c.n_kv_heads, g = A.n_heads / H, tid = threadIdx.x;
+    constexpr int kR = C::kR, kE = D / 32;
+    __shared__ int64_t scan[8], found[2];
+    __shared__ float weight[kMaxWorkers], most[8], sums[8], joined[8][D];
+    const int H = A.c.n_kv_heads, g = A.group, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int64_t token = blockIdx.x / H;
     const int head = blockIdx.x % H;
     const int32_t* off = A.b.tok_off;
@@ -516,10 +558,10 @@ attention_join_kernel(const __grid_constant__ AttnArgs A) {
         tc5::wait_for_previous();  // on every path: this kernel must not end before the one in front of it
         return;
     }
-    int64_t total = 0, base = 0;
+    int64_t total = 0;
     for (int64_t first = 0; first < A.b.n_seq; first += blockDim.x) {
         int64_t v = 0;
-        if (first + tid < A.b.n_seq) v = seq_tiles(A, seq_plan(A, first + tid, kR));
+        if (first + tid < A.b.n_seq) v = seq_tiles(A, seq_plan(A, first + tid, kR, C::kTile));
         const int64_t upto = block_scan(v, scan);
         if (first + tid == s) found[0] = total + upto - v;
         if (tid == (int)blockDim.x - 1) found[1] = upto;
@@ -527,8 +569,8 @@ attention_join_kernel(const __grid_constant__ AttnArgs A) {
         total += found[1];
         __syncthreads();
     }
-    base = found[0];
-    const SeqPlan p = seq_plan(A, s, kR);
+    const int64_t base = found[0];
+    const SeqPlan p = seq_plan(A, s, kR, C::kTile);
     const int64_t per = max((int64_t)1, (total + A.workers - 1) / A.workers);
     const int i = (int)(token - p.first);
     tc5::wait_for_previous();
@@ -536,24 +578,55 @@ attention_join_kernel(const __grid_constant__ AttnArgs A) {
     for (int j = 0; j < g; ++j) {
         const int rb = (i * g + j) / kR, row = (i * g + j) % kR;
         const int64_t from = base + ((int64_t)head * p.blocks + rb) * p.tiles, to = from + p.tiles;
-        const int64_t w0 = from / per, w1 = (to - 1) / per;
-        if (w0 == w1) continue;
+        const int64_t w0 = from / per;
+        const int parts = (int)((to - 1) / per - w0) + 1;
+        if (parts == 1) continue;
         // the first worker's part begins with the unit, the others' with their run
-        auto part = [&](int64_t w) { return A.parts + (2 * w + (w == w0)) * (int64_t)C::kPart; };
+        auto part = [&](int k) { return A.parts + (2 * (w0 + k) + (k == 0)) * (int64_t)C::kPart; };
         float top = -INFINITY;
-        for (int64_t w = w0; w <= w1; ++w) top = fmaxf(top, part(w)[kR * D + 2 * row]);
-        const float at = top == -INFINITY ? 0.0f : top;
-        float sum = 0.0f, o = 0.0f;
-#pragma unroll 4
-        for (int64_t w = w0; w <= w1; ++w) {
-            const float* x = part(w);
-            const float f = ex2(x[kR * D + 2 * row] - at);
-            sum = fmaf(f, x[kR * D + 2 * row + 1], sum);
-            o = fmaf(f, x[row * D + tid], o);
+        for (int k = tid; k < parts; k += 256) {
+            const float m = part(k)[kR * D + 2 * row];
+            weight[k] = m;
+            top = fmaxf(top, m);
         }
+#pragma unroll
+        for (int x = 16; x; x >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, x));
+        if (lane == 0) most[warp] = top;
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < 8; ++w) top = fmaxf(top, most[w]);
+        const float at = top == -INFINITY ? 0.0f : top;
+        float sum = 0.0f, o[kE];
+#pragma unroll
+        for (int e = 0; e < kE; ++e) o[e] = 0.0f;
+#pragma unroll 4
+        for (int k = warp; k < parts; k += 8) {
+            const float* x = part(k);
+            const float f = ex2(weight[k] - at);
+            sum = fmaf(f, x[kR * D + 2 * row + 1], sum);
+#pragma unroll
+            for (int e = 0; e < kE; e += 2) {
+                const float2 v = *reinterpret_cast<const float2*>(x + row * D + lane * kE + e);
+                o[e] = fmaf(f, v.x, o[e]);
+                o[e + 1] = fmaf(f, v.y, o[e + 1]);
+            }
+        }
+        if (lane == 0) sums[warp] = sum;
+#pragma unroll
+        for (int e = 0; e < kE; ++e) joined[warp][lane * kE + e] = o[e];
+        __syncthreads();
         const int h = head * g + j;
-        A.out[token * A.ldo + (int64_t)h * D + tid] = round16<DT>(sum > 0.0f ? o / sum : 0.0f);
+        sum = 0.0f;
+#pragma unroll
+        for (int w = 0; w < 8; ++w) sum += sums[w];
+        if (tid < D) {
+            float v = 0.0f;
+#pragma unroll
+            for (int w = 0; w < 8; ++w) v += joined[w][tid];
+            A.out[token * A.ldo + (int64_t)h * D + tid] = round16<DT>(sum > 0.0f ? v / sum : 0.0f);
+        }
         if (A.lse && tid == 0) A.lse[token * A.n_heads + h] = sum > 0.0f ? (top + log2f(sum)) * kLn2 : -INFINITY;
+        __syncthreads();  // the shared arrays are used again
     }
 }
 
@@ -563,18 +636,18 @@ static cmpq_status launch_rows(AttnArgs a, cudaStream_t st) {
     const cmpq_cache& c = a.c;
     CUtensorMap kmap, vmap;
     const int64_t tokens = c.n_pages * c.n_kv_heads * c.page_tokens;
-    const int box_tokens = std::min(c.page_tokens, kTile);
+    const int box_tokens = std::min(c.page_tokens, C::kTile);
     const int64_t rows = D == 64 ? tokens / 2 : tokens, width = D == 256 ? 256 : 128;
     if (rows > INT32_MAX) return CMPQ_ERR_UNSUPPORTED;
     const int box = D == 64 ? box_tokens / 2 : box_tokens;
     if (!make_byte_map(&kmap, c.k_codes, rows, width, width, box) || !make_byte_map(&vmap, c.v_codes, rows, width, width, box)) return CMPQ_ERR_CUDA;
     static bool raised[64];
     if (!raise_smem_limit_once(attention_rows_kernel<DT, D, NT>, C::kSmem, raised)) return CMPQ_ERR_CUDA;
-    const int blocks = sm_count() * C::kPerSm;
+    const int blocks = std::min(sm_count() * C::kPerSm, kMaxWorkers / C::kWarps);
     a.workers = blocks * C::kWarps;
     attention_rows_kernel<DT, D, NT><<<blocks, 32 * C::kWarps, C::kSmem, st>>>(kmap, vmap, a);
     if (cudaGetLastError() != cudaSuccess) return CMPQ_ERR_CUDA;
-    return launch_cluster(attention_join_kernel<DT, D, NT>, (unsigned)(a.b.n_tok * c.n_kv_heads), D, 0, 1, true, st, a);
+    return launch_cluster(attention_join_kernel<DT, D, NT>, (unsigned)(a.b.n_tok * c.n_kv_heads), 256, 0, 1, true, st, a);
 }
 
 template <int DT, int D>
@@ -585,7 +658,7 @@ static cmpq_status launch_attention(const AttnArgs& a, cudaStream_t st) {
 }
 
 // Room for two parts per worker of the widest row block.
-static size_t parts_bytes(int head_dim) { return (size_t)sm_count() * 2 * 4 * 2 * 16 * (head_dim + 2) * sizeof(float); }
+static size_t parts_bytes(int head_dim) { return (size_t)std::max(1, sm_count()) * kMaxPerSm * 2 * 16 * (head_dim + 2) * sizeof(float); }
 
 }  // namespace cmpq
 
@@ -606,19 +679,20 @@ extern "C" cmpq_status cmpq_cache_attention(const cmpq_cache* cache, const cmpq_
     cmpq_status why;
     if (!cache_ok(cache, &why)) return why;
     if (!batch_ok(batch) || (dt != CMPQ_F16 && dt != CMPQ_BF16)) return CMPQ_ERR_INVALID_ARG;
-    if (n_heads < 1 || n_heads > 4096 || n_heads % cache->n_kv_heads || max_new < 0 || max_len < 0 || max_len > INT32_MAX - 256)
+    if (n_heads < 1 || n_heads > 4096 || n_heads % cache->n_kv_heads || max_new < 0 || max_new > INT32_MAX || max_len < 0 || max_len > INT32_MAX - 256)
         return CMPQ_ERR_INVALID_ARG;
     if (window < 0 || (window > 0 && !causal) || !(scale > 0.0f) || isinf(scale)) return CMPQ_ERR_INVALID_ARG;
     const int64_t row = (int64_t)n_heads * cache->head_dim;
     if (ldq < row || ldo < row) return CMPQ_ERR_INVALID_ARG;
     if (batch->n_seq == 0 || batch->n_tok == 0) return CMPQ_OK;
     if (!q || !out || !aligned_to(q, 2) || !aligned_to(out, 2) || !aligned_to(lse, 4)) return CMPQ_ERR_INVALID_ARG;
-    if (batch->n_tok * cache->n_kv_heads > INT32_MAX) return CMPQ_ERR_UNSUPPORTED;
+    if (batch->n_tok * std::max(n_heads, cache->n_kv_heads) > INT32_MAX - 64) return CMPQ_ERR_UNSUPPORTED;
     if (!ws || !aligned_to(ws, 256) ||
         ws_bytes < cmpq_cache_attention_ws_bytes(batch->n_seq, batch->n_tok, max_new, max_len, n_heads, cache->n_kv_heads, cache->head_dim))
         return CMPQ_ERR_WORKSPACE;
-    AttnArgs a{*cache, *batch, static_cast<const uint16_t*>(q), static_cast<uint16_t*>(out), lse, ldq, ldo, max_new, max_len,
-               window, scale * kLog2e, n_heads, causal != 0, aligned_to(q, 16) && ldq % 8 == 0, aligned_to(out, 16) && ldo % 8 == 0,
+    AttnArgs a{*cache, *batch, static_cast<const uint16_t*>(q), static_cast<uint16_t*>(out), lse, ldq, ldo, (int)max_new, (int)max_len,
+               (int)std::min<int64_t>(window, INT32_MAX), scale * kLog2e, n_heads, n_heads / cache->n_kv_heads, causal != 0,
+               31 - __builtin_clz(cache->page_tokens), aligned_to(q, 16) && ldq % 8 == 0, aligned_to(out, 16) && ldo % 8 == 0,
                word, static_cast<float*>(ws), 0};
     auto st = static_cast<cudaStream_t>(stream);
     const bool bf = dt == CMPQ_BF16;

@@ -45,7 +45,7 @@ class Int8Linear:
 
     def _workspace(self, n):
         # one per stream: calls on different streams may overlap
-        key = torch.cuda.current_stream().cuda_stream
+        key = B._on(self.w_codes)
         ws = self._ws.get(key)
         if ws is None or ws[0] < n:
             ws = (n, torch.empty(B.cmpq_linear_i8_ws_bytes(n, self.d_in, self.d_out), dtype=torch.uint8,
@@ -59,12 +59,13 @@ class Int8Linear:
             raise ValueError("x needs shape [n][%d] on the GPU, got %s on %s" % (self.d_in, tuple(x.shape), x.device))
         if self.bias is not None and self.bias.dtype != x.dtype:
             raise TypeError("bias is %s, x is %s" % (self.bias.dtype, x.dtype))
+        n = x.shape[0]
         if out is None:
-            out = torch.empty(x.shape[0], self.d_out, dtype=x.dtype, device=x.device)
-        elif out.dtype != x.dtype or tuple(out.shape) != (x.shape[0], self.d_out):
+            out = x.new_empty((n, self.d_out))
+        elif out.dtype != x.dtype or tuple(out.shape) != (n, self.d_out):
             raise ValueError("out needs shape [n][%d] and x's dtype" % self.d_out)
-        if x.shape[0]:
-            B.cmpq_linear_i8(x, self.w_codes, self.w_scale, self.bias, out, self._workspace(x.shape[0]), self.nonfinite)
+        if n:
+            B.cmpq_linear_i8(x, self.w_codes, self.w_scale, self.bias, out, self._workspace(n), self.nonfinite)
         return out
 
 
@@ -99,18 +100,19 @@ class PagedCache8:
 
     def _batch(self, tok_off, lens, table, n_tok):
         for name, t, dims in (("tok_off", tok_off, 1), ("lens", lens, 1), ("table", table, 2)):
-            if t.dtype != torch.int32 or t.dim() != dims or not t.is_cuda or (t.numel() > 1 and t.stride(-1) != 1):
+            if t.dtype != torch.int32 or t.dim() != dims or not t.is_cuda or (t.stride()[-1] != 1 and t.numel() > 1):
                 raise ValueError("%s needs an int32 CUDA tensor of %d dimensions" % (name, dims))
-        n_seq = lens.shape[0]
-        if tok_off.shape[0] != n_seq + 1 or table.shape[0] != n_seq:
-            raise ValueError("tok_off needs n_seq + 1 entries and table n_seq rows, n_seq = %d" % n_seq)
-        return B.Batch(tok_off.data_ptr(), lens.data_ptr(), table.data_ptr(),
-                       table.stride(0) if n_seq > 1 else table.shape[1], n_seq, n_tok)
+        n_seq, width = table.shape
+        if tok_off.numel() != n_seq + 1 or lens.numel() != n_seq:
+            raise ValueError("tok_off needs n_seq + 1 entries and table n_seq rows, n_seq = %d" % lens.numel())
+        return B.Batch(tok_off.data_ptr(), lens.data_ptr(), table.data_ptr(), table.stride(0) if n_seq > 1 else width,
+                       n_seq, n_tok)
 
     def _heads(self, t, name, heads=None):
-        if t.dim() != 3 or t.shape[2] != self.head_dim or (heads and t.shape[1] != heads) or not t.is_cuda:
+        shape = t.shape
+        if len(shape) != 3 or shape[2] != self.head_dim or (heads and shape[1] != heads) or not t.is_cuda:
             raise ValueError("%s needs shape [n_tok][%s][%d] on the GPU, got %s"
-                             % (name, heads or "heads", self.head_dim, tuple(t.shape)))
+                             % (name, heads or "heads", self.head_dim, tuple(shape)))
 
     def append(self, k, v, tok_off, lens, table, q=None, cos=None, sin=None, interleaved=False, q_out=None):
         """Writes new tokens' keys (rotated by cos, sin: fp32 [positions][rot_dim / 2]) and values into their pages;
@@ -128,7 +130,7 @@ class PagedCache8:
             if q.dtype != k.dtype or q.shape[0] != k.shape[0]:
                 raise ValueError("q needs k's dtype and token count")
             if q_out is None:
-                q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+                q_out = q.new_empty(q.shape)
             elif q_out.shape != q.shape or q_out.dtype != q.dtype:
                 raise ValueError("q_out needs q's shape and dtype")
         B.cmpq_cache_append(self._c, self._batch(tok_off, lens, table, k.shape[0]), k, v, cos, sin, interleaved, q, q_out,
@@ -137,7 +139,8 @@ class PagedCache8:
 
     def read(self, tok_off, lens, table, n_tok, dtype=torch.bfloat16):
         """The last tok_off[s+1] - tok_off[s] tokens of every sequence as 16-bit values: k, v [n_tok][n_kv][head_dim]."""
-        k, v = (torch.empty(n_tok, self.n_kv, self.head_dim, dtype=dtype, device=self.k_codes.device) for _ in range(2))
+        shape = (n_tok, self.n_kv, self.head_dim)
+        k, v = self.k_codes.new_empty(shape, dtype=dtype), self.k_codes.new_empty(shape, dtype=dtype)
         B.cmpq_cache_read(self._c, self._batch(tok_off, lens, table, n_tok), k, v, self.word)
         return k, v
 
@@ -152,13 +155,13 @@ class PagedCache8:
         if max_len is None:
             max_len = table.shape[1] * self.page_tokens
         if out is None:
-            out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+            out = q.new_empty(q.shape)
         elif out.shape != q.shape or out.dtype != q.dtype:
             raise ValueError("out needs q's shape and dtype")
-        lse = torch.empty(n, heads, dtype=torch.float32, device=q.device) if return_lse else None
+        lse = self.k_scale.new_empty((n, heads)) if return_lse else None
         batch = self._batch(tok_off, lens, table, n)
         need = B.cmpq_cache_attention_ws_bytes(batch.n_seq, n, max_new, max_len, heads, self.n_kv, d)
-        key = torch.cuda.current_stream().cuda_stream
+        key = B._on(q)  # one work space per stream: calls on different streams may overlap
         ws = self._ws.get(key)
         if ws is None or ws.numel() < need:
             ws = self._ws[key] = torch.empty(max(256, need), dtype=torch.uint8, device=q.device)
