@@ -17,7 +17,7 @@
  *  - All array arguments are DEVICE pointers owned by the caller unless the
  *    parameter comment says "host".  The library allocates no memory; scratch space
  *    is the caller's `ws` buffer of at least cmpq_workspace_bytes(op, ...) bytes,
- *    256-byte aligned, whose contents are undefined before and after the call.
+ *    256-byte aligned, whose contents are undefined before and after the call (one call says otherwise of its first bytes).
  *    The only state it keeps between calls is host state that the caller sets
  *    explicitly: the process-wide assignment method (cmpq_set_lloyd_assignment,
  *    which also decides what cmpq_workspace_bytes answers) and the one-shot event
@@ -520,7 +520,10 @@ cmpq_status cmpq_cache_read(const cmpq_cache* cache, const cmpq_batch* batch, cm
  * kernel and size the work space).  Probabilities and sums in fp32, products on the tensor cores in fp16 with
  * fp32 accumulation: codes are exact there, a query row is scaled by a power of two into fp16's range, and
  * probabilities are rounded to fp16.
- * ws: cmpq_cache_attention_ws_bytes(n_seq, n_tok, max_new, max_len, n_heads, n_kv_heads, head_dim). */
+ * ws: cmpq_cache_attention_ws_bytes(n_seq, n_tok, max_new, max_len, n_heads, n_kv_heads, head_dim).  Unlike other
+ * work spaces its first CMPQ_ATTENTION_ZEROED bytes have to be 0 when the call's kernels start, and are 0 again when
+ * they have ended (zero the buffer once, after allocating it and after bit 3 of `word`). */
+#define CMPQ_ATTENTION_ZEROED 4096
 size_t cmpq_cache_attention_ws_bytes(int64_t n_seq, int64_t n_tok, int64_t max_new, int64_t max_len, int32_t n_heads,
                                      int32_t n_kv_heads, int32_t head_dim);
 cmpq_status cmpq_cache_attention(const cmpq_cache* cache, const cmpq_batch* batch, const void* q, int64_t ldq,

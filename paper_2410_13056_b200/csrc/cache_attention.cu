@@ -23,7 +23,8 @@ struct AttnArgs {
     int page_bits;  // log2 of a page's tokens
     int wide_q, wide_o;
     int32_t* word;
-    float* parts;  // partial results of the workers, see there
+    int* counters;  // one per block, zero between calls
+    float* parts;   // two parts per block, then one per worker
     int workers;
 };
 
@@ -43,7 +44,7 @@ __device__ __forceinline__ float ex2(float x) {
 // contiguous runs: sequences of any lengths balance, and a worker meets few unit borders.  A unit inside one worker's
 // run is finished there; the parts of one that is cut go to the work space and are joined by a second kernel in the
 // order of the workers (no atomics: the same bytes every time).
-constexpr int kMaxPerSm = 12;  // workers of an SM
+constexpr int kMaxBlocks = 1024;
 
 template <int D, int NT>
 struct Rows {
@@ -53,7 +54,8 @@ struct Rows {
     static constexpr int kTileBytes = kTile * D;                            // keys; as many for the values
     static constexpr int kBuffers = kTile == 64 ? 1 : 2;
     static constexpr int kPerSm = NT == 1 && D <= 128 ? 3 : D == 256 ? 1 : 2;
-    static constexpr int kSmem = kWarps * kBuffers * 2 * kTileBytes + 1024;
+    static constexpr int kRing = kBuffers * 2 * kTileBytes > kR * (D + 2) * 4 ? kBuffers * 2 * kTileBytes : (kR * (D + 2) * 4 + 1023) / 1024 * 1024;
+    static constexpr int kSmem = kWarps * kRing + 1024;
     static constexpr int kPart = kR * (D + 2);                              // floats of a partial result
 };
 
@@ -125,6 +127,67 @@ __device__ __forceinline__ uint32_t tile_at(int t, int d) {
     return plane * (TILE * 128) + t * 128 + (((e >> 4) ^ (t & 7)) << 4) + (e & 15);
 }
 
+// A worker's part of a unit: tiles [from, to) are the unit's, rows at output rows first.. of the head, block rb.
+struct Piece {
+    int64_t from, to;
+    const float* at;
+    int first, head, rb, rows;
+};
+
+// Joins n parts (rows of D entries, then maximum and sum of each row) in their order: into `into`, or, where that is
+// null, into the output.  Every thread of the block; a thread takes four entries of a row at a time and eight parts'
+// values are under way together.
+template <int DT, int D, int R, class Part>
+__device__ __forceinline__ void join_parts(const AttnArgs& A, const Piece& u, int n, Part part, float* into) {
+    for (int i = threadIdx.x; i < u.rows * (D / 4); i += blockDim.x) {
+        const int row = i / (D / 4), d = i % (D / 4) * 4;
+        float top = -INFINITY, sum = 0.0f;
+        float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        for (int k = 0; k < n; k += 8) {
+            float2 ml[8];
+            float4 v[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                ml[j] = make_float2(-INFINITY, 0.0f);
+                v[j] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                if (k + j < n) {
+                    const float* p = part(k + j);
+                    ml[j] = *reinterpret_cast<const float2*>(p + R * D + 2 * row);
+                    v[j] = *reinterpret_cast<const float4*>(p + row * D + d);
+                }
+            }
+            float most = top;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) most = fmaxf(most, ml[j].x);
+            const float at = most == -INFINITY ? 0.0f : most, keep = ex2(top - at);
+            top = most;
+            sum *= keep, o.x *= keep, o.y *= keep, o.z *= keep, o.w *= keep;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const float f = ex2(ml[j].x - at);
+                sum = fmaf(f, ml[j].y, sum);
+                o.x = fmaf(f, v[j].x, o.x), o.y = fmaf(f, v[j].y, o.y), o.z = fmaf(f, v[j].z, o.z), o.w = fmaf(f, v[j].w, o.w);
+            }
+        }
+        if (into) {
+            *reinterpret_cast<float4*>(into + row * D + d) = o;
+            if (d == 0) *reinterpret_cast<float2*>(into + R * D + 2 * row) = make_float2(top, sum);
+            continue;
+        }
+        const float f = sum > 0.0f ? 1.0f / sum : 0.0f;
+        const int q = u.rb * R + row, h = u.head * A.group + q % A.group;
+        const int64_t t = u.first + q / A.group;
+        uint16_t* dst = A.out + t * A.ldo + (int64_t)h * D + d;
+        const uint2 w = make_uint2(round16x2<DT>(o.x * f, o.y * f), round16x2<DT>(o.z * f, o.w * f));
+        if (A.wide_o) {
+            *reinterpret_cast<uint2*>(dst) = w;
+        } else {
+            dst[0] = (uint16_t)w.x, dst[1] = (uint16_t)(w.x >> 16), dst[2] = (uint16_t)w.y, dst[3] = (uint16_t)(w.y >> 16);
+        }
+        if (A.lse && d == 0) A.lse[t * A.n_heads + h] = sum > 0.0f ? (top + log2f(sum)) * kLn2 : -INFINITY;
+    }
+}
+
 // A lane's place in the m16n8k16 fragments: r = lane / 4, c = lane % 4.
 //   scores   S^T[token][row] = K Q^T: a lane reads 16 bytes of keys of tokens r and r + 8 at a time, which are the A
 //            entries of four instructions when the sum runs over the entries in the order 16 (2c + j) + 4 w + {0..3}
@@ -147,14 +210,15 @@ attention_rows_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_con
     __shared__ int64_t start_base[C::kWarps];
     __shared__ int start_seq[C::kWarps];
     __shared__ float2 page_scale[C::kWarps][64];  // key and value scales of the last 64 pages asked for
-    __shared__ int failed[C::kWarps];
+    __shared__ int failed[C::kWarps], is_last;
+    __shared__ Piece pieces[C::kWarps][2];
     uint8_t* smem = raw + ((1024u - (tc5::smem_addr(raw) & 1023u)) & 1023u);
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, r = lane >> 2, c = lane & 3;
     const int H = A.c.n_kv_heads, g = A.group, P = A.c.page_tokens, page_bits = A.page_bits;
-    tc5::dependents_may_start();
     if (lane == 0) {
         for (int i = 0; i < kBuffers; ++i) tc5::mbar_init(&bars[warp][0][i], 1), tc5::mbar_init(&bars[warp][1][i], 1);
         failed[warp] = 0;
+        pieces[warp][0].at = pieces[warp][1].at = nullptr;
         tc5::mbar_init_fence();
     }
 
@@ -193,10 +257,8 @@ attention_rows_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_con
         before = scan[0];
         __syncthreads();
     }
-    if (begin >= end) return;
-
-    int64_t s = start_seq[warp], base = start_base[warp];
-    uint8_t* ring = smem + warp * (kBuffers * 2 * C::kTileBytes);  // keys, then values
+    int64_t s = begin < end ? start_seq[warp] : 0, base = begin < end ? start_base[warp] : 0;
+    uint8_t* ring = smem + warp * C::kRing;  // keys, then values
     volatile int* gave_up = &failed[warp];
     int slot[2] = {0, 0}, phase[2] = {0, 0}, next[2] = {0, 0};  // of the keys and of the values: next to read, to fill
 
@@ -486,9 +548,17 @@ attention_rows_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_con
         }
         if (*gave_up) break;
 
-        // the unit's rows: whole, or this worker's part of them
+        // The unit's rows: whole, or this worker's part of them.  A part after which the worker goes on to another unit
+        // is put into the work space, since the copies for that unit take the shared memory; the last stays there.
         const bool whole = t_from == 0 && t_to == p.tiles;
-        float* part = A.parts + ((int64_t)worker * 2 + (t_from == 0)) * C::kPart;
+        x += t_to - t_from;
+        float* part = x < end ? A.parts + (int64_t)(A.workers / C::kWarps * 2 + worker) * C::kPart : reinterpret_cast<float*>(ring);
+        if (!whole && lane == 0) {
+            Piece& e = pieces[warp][x < end ? 0 : 1];
+            e.from = base + unit * p.tiles, e.to = e.from + p.tiles;
+            e.at = part;
+            e.first = p.first, e.head = head, e.rb = rb, e.rows = rows;
+        }
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -528,105 +598,55 @@ attention_rows_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_con
                     if (r == 0) part[kR * D + 2 * row] = m2[nt][e], part[kR * D + 2 * row + 1] = sum;
                 }
             }
-        x += t_to - t_from;
     }
     if (*gave_up) {  // copies that were asked for have to land before the shared memory is given back
         const long long start = clock64();
         while (clock64() - start < (1ll << 21)) __nanosleep(1000);
         if (lane == 0 && A.word) atomicOr(A.word, kWordInternal);
     }
-}
+    __syncthreads();
 
-// Joins the parts of the units that were cut, a block of eight warps per query row and key-value head.  The workers'
-// maxima and sums are read side by side, a thread each; then the warps take every eighth part, a lane D/32 neighbouring
-// entries.  The order of the sums goes by the parts' numbers alone.  Units that one worker finished are left alone.
-constexpr int kMaxWorkers = 2048;
-
-template <int DT, int D, int NT>
-__global__ void __launch_bounds__(256)
-attention_join_kernel(const __grid_constant__ AttnArgs A) {
-    using C = Rows<D, NT>;
-    constexpr int kR = C::kR, kE = D / 32;
-    __shared__ int64_t scan[8], found[2];
-    __shared__ float weight[kMaxWorkers], most[8], sums[8], joined[8][D];
-    const int H = A.c.n_kv_heads, g = A.group, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    const int64_t token = blockIdx.x / H;
-    const int head = blockIdx.x % H;
-    const int32_t* off = A.b.tok_off;
-    const int s = block_count(A.b.n_seq, [&](int64_t i) { return off[i] <= token; });
-    if (s >= A.b.n_seq) {
-        tc5::wait_for_previous();  // on every path: this kernel must not end before the one in front of it
-        return;
-    }
-    int64_t total = 0;
-    for (int64_t first = 0; first < A.b.n_seq; first += blockDim.x) {
-        int64_t v = 0;
-        if (first + tid < A.b.n_seq) v = seq_tiles(A, seq_plan(A, first + tid, kR, C::kTile));
-        const int64_t upto = block_scan(v, scan);
-        if (first + tid == s) found[0] = total + upto - v;
-        if (tid == (int)blockDim.x - 1) found[1] = upto;
-        __syncthreads();
-        total += found[1];
-        __syncthreads();
-    }
-    const int64_t base = found[0];
-    const SeqPlan p = seq_plan(A, s, kR, C::kTile);
-    const int64_t per = max((int64_t)1, (total + A.workers - 1) / A.workers);
-    const int i = (int)(token - p.first);
-    tc5::wait_for_previous();
-    if (p.bad) return;
-    for (int j = 0; j < g; ++j) {
-        const int rb = (i * g + j) / kR, row = (i * g + j) % kR;
-        const int64_t from = base + ((int64_t)head * p.blocks + rb) * p.tiles, to = from + p.tiles;
-        const int64_t w0 = from / per;
-        const int parts = (int)((to - 1) / per - w0) + 1;
-        if (parts == 1) continue;
-        // the first worker's part begins with the unit, the others' with their run
-        auto part = [&](int k) { return A.parts + (2 * (w0 + k) + (k == 0)) * (int64_t)C::kPart; };
-        float top = -INFINITY;
-        for (int k = tid; k < parts; k += 256) {
-            const float m = part(k)[kR * D + 2 * row];
-            weight[k] = m;
-            top = fmaxf(top, m);
+    // Parts of one unit that this block's warps hold, one behind the other, are joined here: into the result if the
+    // unit lies in the block's run, otherwise into the block's part.  The block that adds the last of a unit's parts
+    // (a counter at the block that began the unit tells) joins those, in the blocks' order, and clears the counter.
+    const int64_t block_run = per * C::kWarps, block_from = blockIdx.x * block_run, block_to = block_from + block_run;
+    for (int first = 0; first < 2 * C::kWarps;) {
+        const Piece& e = (&pieces[0][0])[first];
+        if (e.at == nullptr) {
+            ++first;
+            continue;
         }
-#pragma unroll
-        for (int x = 16; x; x >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, x));
-        if (lane == 0) most[warp] = top;
-        __syncthreads();
-#pragma unroll
-        for (int w = 0; w < 8; ++w) top = fmaxf(top, most[w]);
-        const float at = top == -INFINITY ? 0.0f : top;
-        float sum = 0.0f, o[kE];
-#pragma unroll
-        for (int e = 0; e < kE; ++e) o[e] = 0.0f;
-#pragma unroll 4
-        for (int k = warp; k < parts; k += 8) {
-            const float* x = part(k);
-            const float f = ex2(weight[k] - at);
-            sum = fmaf(f, x[kR * D + 2 * row + 1], sum);
-#pragma unroll
-            for (int e = 0; e < kE; e += 2) {
-                const float2 v = *reinterpret_cast<const float2*>(x + row * D + lane * kE + e);
-                o[e] = fmaf(f, v.x, o[e]);
-                o[e + 1] = fmaf(f, v.y, o[e + 1]);
+        int last = first + 1, n = 1;
+        while (last < 2 * C::kWarps) {
+            const Piece& f = (&pieces[0][0])[last];
+            if (f.at != nullptr && f.from != e.from) break;
+            if (f.at != nullptr) ++n;
+            ++last;
+        }
+        const int from_piece = first;
+        auto local = [&](int k) {  // the k-th part of the group
+            int i = from_piece;
+            for (;; ++i)
+                if ((&pieces[0][0])[i].at != nullptr && k-- == 0) break;
+            return (&pieces[0][0])[i].at;
+        };
+        const bool complete = e.from >= block_from && e.to <= block_to;
+        float* mine_out = A.parts + ((int64_t)blockIdx.x * 2 + (e.from >= block_from)) * C::kPart;
+        join_parts<DT, D, kR>(A, e, n, local, complete ? nullptr : mine_out);
+        if (!complete) {
+            const int64_t b0 = e.from / block_run, b1 = (e.to - 1) / block_run;
+            __threadfence();
+            __syncthreads();
+            if (tid == 0) is_last = atomicAdd(A.counters + b0, 1) == (int)(b1 - b0);
+            __syncthreads();
+            if (is_last) {
+                __threadfence();
+                auto far = [&](int k) { return (const float*)(A.parts + ((b0 + k) * 2 + (k == 0)) * (int64_t)C::kPart); };
+                join_parts<DT, D, kR>(A, e, (int)(b1 - b0) + 1, far, nullptr);
+                if (tid == 0) A.counters[b0] = 0;
             }
         }
-        if (lane == 0) sums[warp] = sum;
-#pragma unroll
-        for (int e = 0; e < kE; ++e) joined[warp][lane * kE + e] = o[e];
-        __syncthreads();
-        const int h = head * g + j;
-        sum = 0.0f;
-#pragma unroll
-        for (int w = 0; w < 8; ++w) sum += sums[w];
-        if (tid < D) {
-            float v = 0.0f;
-#pragma unroll
-            for (int w = 0; w < 8; ++w) v += joined[w][tid];
-            A.out[token * A.ldo + (int64_t)h * D + tid] = round16<DT>(sum > 0.0f ? v / sum : 0.0f);
-        }
-        if (A.lse && tid == 0) A.lse[token * A.n_heads + h] = sum > 0.0f ? (top + log2f(sum)) * kLn2 : -INFINITY;
-        __syncthreads();  // the shared arrays are used again
+        first = last;
     }
 }
 
@@ -643,11 +663,10 @@ static cmpq_status launch_rows(AttnArgs a, cudaStream_t st) {
     if (!make_byte_map(&kmap, c.k_codes, rows, width, width, box) || !make_byte_map(&vmap, c.v_codes, rows, width, width, box)) return CMPQ_ERR_CUDA;
     static bool raised[64];
     if (!raise_smem_limit_once(attention_rows_kernel<DT, D, NT>, C::kSmem, raised)) return CMPQ_ERR_CUDA;
-    const int blocks = std::min(sm_count() * C::kPerSm, kMaxWorkers / C::kWarps);
+    const int blocks = std::min(sm_count() * C::kPerSm, kMaxBlocks);
     a.workers = blocks * C::kWarps;
     attention_rows_kernel<DT, D, NT><<<blocks, 32 * C::kWarps, C::kSmem, st>>>(kmap, vmap, a);
-    if (cudaGetLastError() != cudaSuccess) return CMPQ_ERR_CUDA;
-    return launch_cluster(attention_join_kernel<DT, D, NT>, (unsigned)(a.b.n_tok * c.n_kv_heads), 256, 0, 1, true, st, a);
+    return launch_status();
 }
 
 template <int DT, int D>
@@ -657,8 +676,12 @@ static cmpq_status launch_attention(const AttnArgs& a, cudaStream_t st) {
     return rows <= 8 ? launch_rows<DT, D, 1>(a, st) : launch_rows<DT, D, 2>(a, st);
 }
 
-// Room for two parts per worker of the widest row block.
-static size_t parts_bytes(int head_dim) { return (size_t)std::max(1, sm_count()) * kMaxPerSm * 2 * 16 * (head_dim + 2) * sizeof(float); }
+// The counters, then two parts per block and one per worker, of the kernel that has most.
+static size_t rows_ws_bytes(int d) {
+    const size_t narrow = (size_t)Rows<64, 1>::kPerSm * 6 * 8, wide = (size_t)Rows<64, 2>::kPerSm * 6 * 16;
+    const size_t blocks = std::min(std::max(1, sm_count()), kMaxBlocks / Rows<64, 1>::kPerSm);
+    return kMaxBlocks * sizeof(int) + blocks * std::max(narrow, wide) * (d + 2) * sizeof(float);
+}
 
 }  // namespace cmpq
 
@@ -669,7 +692,7 @@ extern "C" size_t cmpq_cache_attention_ws_bytes(int64_t n_seq, int64_t n_tok, in
     if (n_seq < 0 || n_tok < 0 || max_new < 0 || max_len < 0 || n_heads < 1 || n_kv_heads < 1 || n_heads % n_kv_heads ||
         head_dim < 1 || head_dim > 256)
         return 0;
-    return round_up(parts_bytes(head_dim), 256);
+    return round_up(rows_ws_bytes(head_dim), 256);
 }
 
 extern "C" cmpq_status cmpq_cache_attention(const cmpq_cache* cache, const cmpq_batch* batch, const void* q, int64_t ldq,
@@ -693,7 +716,7 @@ extern "C" cmpq_status cmpq_cache_attention(const cmpq_cache* cache, const cmpq_
     AttnArgs a{*cache, *batch, static_cast<const uint16_t*>(q), static_cast<uint16_t*>(out), lse, ldq, ldo, (int)max_new, (int)max_len,
                (int)std::min<int64_t>(window, INT32_MAX), scale * kLog2e, n_heads, n_heads / cache->n_kv_heads, causal != 0,
                31 - __builtin_clz(cache->page_tokens), aligned_to(q, 16) && ldq % 8 == 0, aligned_to(out, 16) && ldo % 8 == 0,
-               word, static_cast<float*>(ws), 0};
+               word, static_cast<int*>(ws), reinterpret_cast<float*>(static_cast<int*>(ws) + kMaxBlocks), 0};
     auto st = static_cast<cudaStream_t>(stream);
     const bool bf = dt == CMPQ_BF16;
     switch (cache->head_dim) {

@@ -164,7 +164,7 @@ class PagedCache8:
         key = B._on(q)  # one work space per stream: calls on different streams may overlap
         ws = self._ws.get(key)
         if ws is None or ws.numel() < need:
-            ws = self._ws[key] = torch.empty(max(256, need), dtype=torch.uint8, device=q.device)
+            ws = self._ws[key] = torch.zeros(need, dtype=torch.uint8, device=q.device)  # its counters start at 0
         B.cmpq_cache_attention(self._c, batch, q, max_new, max_len, 1.0 / math.sqrt(d) if scale is None else scale,
                                causal, window, out, lse, ws, self.word)
         return (out, lse) if return_lse else out
