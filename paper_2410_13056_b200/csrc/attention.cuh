@@ -1,0 +1,45 @@
+// Shared by the attention kernels on the paged 8-bit cache.
+#pragma once
+
+#include "cache.cuh"
+#include "tc5.cuh"
+
+namespace cmpq {
+
+struct AttnArgs {
+    cmpq_cache c;
+    cmpq_batch b;
+    const uint16_t* q;
+    uint16_t* out;
+    float* lse;
+    int64_t ldq, ldo;
+    int max_new, max_len, window;
+    float scale;  // times log2(e): scores are kept in powers of two
+    int n_heads, group, causal;
+    int page_bits;  // log2 of a page's tokens
+    int wide_q, wide_o;
+    int32_t* word;
+    int* counters;  // one per block, zero between calls
+    float* parts;   // two parts per block, then one per worker
+    int workers;
+};
+
+constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
+
+__device__ __forceinline__ float ex2(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+// Four int8 codes (already offset by 128) as two pairs of fp16: 0x6400 | u is 1024 + u, and 1024 + 128 comes off.
+__device__ __forceinline__ uint32_t half_pair(uint32_t u, uint32_t pick) {
+    const uint32_t h = __byte_perm(u, 0x64646464u, pick);
+    const __half2 d = __hsub2(*reinterpret_cast<const __half2*>(&h), __halves2half2(__ushort_as_half(0x6480), __ushort_as_half(0x6480)));
+    return *reinterpret_cast<const uint32_t*>(&d);
+}
+
+// Whole prompts (cache_prefill.cu): head_dim 64 and 128.
+cmpq_status launch_prefill(const AttnArgs& a, cmpq_dtype dt, cudaStream_t st);
+
+}  // namespace cmpq

@@ -5,36 +5,9 @@
 // or of its weights (values); a query row is scaled by a power of two into fp16's range first.
 #include <algorithm>
 
-#include "cache.cuh"
-#include "tc5.cuh"
+#include "attention.cuh"
 
 namespace cmpq {
-
-struct AttnArgs {
-    cmpq_cache c;
-    cmpq_batch b;
-    const uint16_t* q;
-    uint16_t* out;
-    float* lse;
-    int64_t ldq, ldo;
-    int max_new, max_len, window;
-    float scale;  // times log2(e): scores are kept in powers of two
-    int n_heads, group, causal;
-    int page_bits;  // log2 of a page's tokens
-    int wide_q, wide_o;
-    int32_t* word;
-    int* counters;  // one per block, zero between calls
-    float* parts;   // two parts per block, then one per worker
-    int workers;
-};
-
-constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
-
-__device__ __forceinline__ float ex2(float x) {
-    float y;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
 
 // ---- few query rows: warps share out the cache -------------------------------------------------------------------
 //
@@ -98,12 +71,6 @@ __device__ __forceinline__ int64_t block_scan(int64_t v, int64_t* part) {
     return v;
 }
 
-// Four int8 codes (already offset by 128) as two pairs of fp16: 0x6400 | u is 1024 + u, and 1024 + 128 comes off.
-__device__ __forceinline__ uint32_t half_pair(uint32_t u, uint32_t pick) {
-    const uint32_t h = __byte_perm(u, 0x64646464u, pick);
-    const __half2 d = __hsub2(*reinterpret_cast<const __half2*>(&h), __halves2half2(__ushort_as_half(0x6480), __ushort_as_half(0x6480)));
-    return *reinterpret_cast<const uint32_t*>(&d);
-}
 __device__ __forceinline__ void mma_f16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
     asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                  : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
@@ -719,6 +686,7 @@ extern "C" cmpq_status cmpq_cache_attention(const cmpq_cache* cache, const cmpq_
                word, static_cast<int*>(ws), reinterpret_cast<float*>(static_cast<int*>(ws) + kMaxBlocks), 0};
     auto st = static_cast<cudaStream_t>(stream);
     const bool bf = dt == CMPQ_BF16;
+    if (cache->head_dim <= 128 && max_new * a.group > 32) return launch_prefill(a, dt, st);
     switch (cache->head_dim) {
         case 64: return bf ? launch_attention<CMPQ_BF16, 64>(a, st) : launch_attention<CMPQ_F16, 64>(a, st);
         case 128: return bf ? launch_attention<CMPQ_BF16, 128>(a, st) : launch_attention<CMPQ_F16, 128>(a, st);

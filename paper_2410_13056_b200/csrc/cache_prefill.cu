@@ -1,0 +1,391 @@
+// Attention of many query rows over the paged 8-bit cache: both products on tcgen05, accumulators in TMEM.
+#include "attention.cuh"
+
+namespace cmpq {
+
+// A block takes 256 query rows of a sequence and key-value head (its new tokens times the query heads of the group,
+// next to each other, so that grouped heads share the keys) as two tiles of 128 and walks over the keys 128 at a time:
+//   4 warps   widen the tile's keys and values from int8 to fp16 into shared memory, a buffer ahead
+//   1 thread  issues S_w = Q_w K^T and O_w += P_w V for the two row tiles in turn
+//   2 x 4 warps, a thread per row: weights P_w = exp2(S_w - m) in fp16 over S_w's own TMEM columns
+// While one row tile's weights are made the other's products run.  TMEM holds S (2 x 128 columns) and O (2 x D).
+// The weights carry the value scale of their page relative to the largest of all pages that the block meets, as part
+// of the exponent; the row's sum takes it out again page by page.  The reference maximum m follows the true one only
+// when it has grown by more than 2^8, which fp16 has room for: then, rarely after the first tiles, O is multiplied in
+// TMEM.  Rows of keys and of queries keep the order of their entries 16 c + 8 p + e as plane p, group c, entry e, so
+// that the 16 codes a lane widens go to the same group of two planes and a row's lanes to different banks.
+constexpr int kPfKeys = 128, kPfThreads = 13 * 32;
+constexpr float kPfSlack = 8.0f;
+
+template <int D>
+struct Prefill {
+    static constexpr int kPlanes = D / 64;
+    static constexpr int kTileBytes = 128 * D * 2;                      // 128 rows or keys in fp16
+    static constexpr int kSmem = 2 * kTileBytes + 4 * kTileBytes + 1024;  // queries; keys and values, two buffers each
+};
+
+// Where group (of eight entries) j of row t lies in a tile of 128 rows: see above for the order of the groups.
+template <int D>
+__device__ __forceinline__ uint32_t pf_at(int t, int j) {
+    const int c = j >> 1, p = j & 1;
+    if (D == 128) return p * (128 * 128) + t * 128 + ((c ^ (t & 7)) << 4);
+    return t * 128 + (((p * 4 + c) ^ (t & 7)) << 4);
+}
+
+template <int DT, int D>
+__global__ void __launch_bounds__(kPfThreads, 1)
+attention_prefill_kernel(const __grid_constant__ AttnArgs A, const int row_blocks) {
+    using C = Prefill<D>;
+    extern __shared__ uint8_t raw[];
+    uint8_t* smem = raw + ((1024u - (tc5::smem_addr(raw) & 1023u)) & 1023u);
+    uint8_t* const sq = smem;
+    uint8_t* const sk = smem + 2 * C::kTileBytes;
+    uint8_t* const sv = smem + 4 * C::kTileBytes;
+    __shared__ uint64_t q_full, k_full[2], k_empty[2], v_full[2], v_empty[2], s_full[2], p_full[2], o_full[2];
+    __shared__ uint32_t tmem_at;
+    __shared__ int failed;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int H = A.c.n_kv_heads, g = A.group, page_bits = A.page_bits;
+    const int rb = row_blocks - 1 - blockIdx.x % row_blocks, s = blockIdx.x / row_blocks / H, head = blockIdx.x / row_blocks % H;
+
+    const int first = A.b.tok_off[s], n = A.b.tok_off[s + 1] - first, len = A.b.lens[s];
+    if (len < 0 || len > A.max_len || n < 0 || n > A.max_new || first < 0 || (int64_t)first + n > A.b.n_tok) {
+        if (tid == 0 && A.word) atomicOr(A.word, kWordTable);
+        return;
+    }
+    const int rows = min(256, n * g - rb * 256);
+    if (rows <= 0) return;
+    const bool two = rows > 128;
+    // positions of the first and last query, keys that any of them sees, tiles of keys
+    const int p0 = len - n + (rb * 256) / g, p1 = len - n + (rb * 256 + rows - 1) / g;
+    const int key_hi = A.causal ? max(0, p1 + 1) : len, key_lo = A.window > 0 ? max(0, p0 - A.window + 1) : 0;
+    const int t0 = key_lo / kPfKeys, tiles = key_hi > key_lo ? (key_hi + kPfKeys - 1) / kPfKeys - t0 : 0;
+    const int32_t* table = A.b.table + (int64_t)s * A.b.ld_table;
+    const int pages = (len + (1 << page_bits) - 1) >> page_bits;
+    auto page_of = [&](int page) {  // -1 where there is none
+        const int id = page < pages && page < A.b.ld_table ? __ldg(table + page) : -1;
+        if (id >= 0 && id < A.c.n_pages) return id;
+        if (page < pages && A.word) atomicOr(A.word, kWordTable);
+        return -1;
+    };
+
+    if (tid == 0) {
+        tc5::mbar_init(&q_full, 8);
+        for (int i = 0; i < 2; ++i) {
+            tc5::mbar_init(k_full + i, 4), tc5::mbar_init(v_full + i, 4);
+            tc5::mbar_init(k_empty + i, 1), tc5::mbar_init(v_empty + i, 1);
+            tc5::mbar_init(s_full + i, 1), tc5::mbar_init(p_full + i, 4), tc5::mbar_init(o_full + i, 1);
+        }
+        failed = 0;
+        tc5::mbar_init_fence();
+    }
+    if (warp == 12) tc5::tmem_alloc<1>(&tmem_at, 512);
+    tc5::fence_before_sync();
+    __syncthreads();
+    tc5::fence_after_sync();
+    const uint32_t tmem = tmem_at, tmem_o = tmem + 256;
+
+    if (warp == 12) {
+        if (tc5::elect_one() && tiles > 0) {
+            constexpr uint32_t kScores = tc5::idesc_f16(128, 128), kOut = tc5::idesc_f16(128, D) | tc5::kTransposedB;
+            const uint32_t aq = tc5::smem_addr(sq), ak = tc5::smem_addr(sk), av = tc5::smem_addr(sv);
+            auto scores = [&](int w, int t) {
+                const uint64_t a = tc5::desc_k_sw128(aq + w * C::kTileBytes), b = tc5::desc_k_sw128(ak + (t & 1) * C::kTileBytes);
+#pragma unroll
+                for (int j = 0; j < D / 16; ++j) {
+                    const uint32_t at = (j >> 2) * (128 * 128 >> 4) + (j & 3) * 2;
+                    tc5::mma_f16_ss(tmem + w * 128, a + at, b + at, kScores, j != 0);
+                }
+                tc5::mma_commit(s_full + w);
+            };
+            bool ok = tc5::mbar_wait(&q_full, 0, &failed) && tc5::mbar_wait(k_full, 0, &failed);
+            tc5::fence_after_sync();
+            if (ok) {
+                scores(0, 0);
+                if (two) scores(1, 0);
+                tc5::mma_commit(k_empty);
+            }
+            for (int t = 0; ok && t < tiles; ++t) {
+                const int slot = t & 1, next = (t + 1) & 1;
+                ok = tc5::mbar_wait(v_full + slot, (t >> 1) & 1, &failed);
+                if (ok && t + 1 < tiles) ok = tc5::mbar_wait(k_full + next, ((t + 1) >> 1) & 1, &failed);
+#pragma unroll 1
+                for (int w = 0; ok && w < (two ? 2 : 1); ++w) {
+                    if (!(ok = tc5::mbar_wait(p_full + w, t & 1, &failed))) break;
+                    tc5::fence_after_sync();
+                    const uint64_t b = tc5::desc_mn_sw128(av + slot * C::kTileBytes, 128 * 128);
+#pragma unroll
+                    for (int j = 0; j < kPfKeys / 16; ++j)
+                        tc5::mma_f16_ts(tmem_o + w * 128, tmem + w * 128 + j * 8, b + j * (2048 >> 4), kOut, (t | j) != 0);
+                    if (t + 1 < tiles) {
+                        scores(w, t + 1);
+                    } else {
+                        tc5::mma_commit(o_full + w);
+                    }
+                }
+                tc5::mma_commit(v_empty + slot);
+                if (t + 1 < tiles) tc5::mma_commit(k_empty + next);
+            }
+        }
+        __syncwarp();
+    } else if (warp >= 8) {
+        // a row's lanes: D/16 of them, 16 codes each
+        constexpr int kLanes = D / 16, kRows = 32 / kLanes, kSteps = 32 / kRows;  // rows of a warp at a time, times per tile
+        const int w = warp - 8, c = lane % kLanes, q = lane / kLanes;
+        const int r0 = D == 64 ? (q & 1) * 4 + (q >> 1) : q;  // eight neighbouring lanes write to different banks
+        uint4 kc[kSteps], vc[kSteps];
+        auto fetch = [&](int t, const int8_t* codes, uint4 (&x)[kSteps]) {
+#pragma unroll
+            for (int i = 0; i < kSteps; ++i) {
+                const int key = (t0 + t) * kPfKeys + w * 32 + i * kRows + r0;
+                const int id = page_of(key >> page_bits);
+                x[i] = make_uint4(0u, 0u, 0u, 0u);
+                if (id >= 0)
+                    x[i] = __ldg(reinterpret_cast<const uint4*>(
+                        codes + (((((int64_t)id * H + head) << page_bits) + (key & ((1 << page_bits) - 1))) * D + 16 * c)));
+            }
+        };
+        auto put = [&](uint8_t* tile, const uint4 (&x)[kSteps]) {
+#pragma unroll
+            for (int i = 0; i < kSteps; ++i) {
+                const int row = w * 32 + i * kRows + r0;
+                const uint32_t a = x[i].x ^ 0x80808080u, b = x[i].y ^ 0x80808080u, d = x[i].z ^ 0x80808080u, e = x[i].w ^ 0x80808080u;
+                *reinterpret_cast<uint4*>(tile + pf_at<D>(row, 2 * c)) =
+                    make_uint4(half_pair(a, 0x4140), half_pair(a, 0x4342), half_pair(b, 0x4140), half_pair(b, 0x4342));
+                *reinterpret_cast<uint4*>(tile + pf_at<D>(row, 2 * c + 1)) =
+                    make_uint4(half_pair(d, 0x4140), half_pair(d, 0x4342), half_pair(e, 0x4140), half_pair(e, 0x4342));
+            }
+        };
+        if (tiles > 0) fetch(0, A.c.k_codes, kc), fetch(0, A.c.v_codes, vc);
+        for (int t = 0; t < tiles; ++t) {
+            const int slot = t & 1, phase = ((t >> 1) & 1) ^ 1;
+            if (!tc5::mbar_wait(k_empty + slot, phase, &failed)) break;
+            put(sk + slot * C::kTileBytes, kc);
+            tc5::fence_async_smem();
+            __syncwarp();
+            if (lane == 0) tc5::mbar_arrive(k_full + slot);
+            if (t + 1 < tiles) fetch(t + 1, A.c.k_codes, kc);
+            if (!tc5::mbar_wait(v_empty + slot, phase, &failed)) break;
+            put(sv + slot * C::kTileBytes, vc);
+            tc5::fence_async_smem();
+            __syncwarp();
+            if (lane == 0) tc5::mbar_arrive(v_full + slot);
+            if (t + 1 < tiles) fetch(t + 1, A.c.v_codes, vc);
+        }
+    } else {
+        const int w = warp >> 2, local = tid & 127, row = rb * 256 + w * 128 + local;
+        const bool real = w * 128 + local < rows;
+        const int i = row / g, h = head * g + row % g, pos = len - n + i;
+        // this row's query into shared memory, scaled by a power of two into fp16's range
+        float qs = 0.0f;
+        {
+            const uint16_t* src = A.q + (int64_t)(first + i) * A.ldq + (int64_t)h * D;
+            uint4 x[D / 8];
+            uint32_t m = 0;
+#pragma unroll
+            for (int j = 0; j < D / 8; ++j) {
+                x[j] = real ? load8(src + 8 * j, 8, A.wide_q) : make_uint4(0u, 0u, 0u, 0u);
+                const uint32_t e[4] = {x[j].x, x[j].y, x[j].z, x[j].w};
+#pragma unroll
+                for (int k = 0; k < 4; ++k) m = max(m, max(e[k] & 0x7fffu, e[k] >> 16 & 0x7fffu));
+            }
+            const float amax = widen16<DT>((uint16_t)m);
+            const int ex = amax > 0.0f ? ilogbf(amax) : 0;
+            const float up = ldexpf(1.0f, ex), dn = ldexpf(1.0f, max(-126, -ex));
+#pragma unroll
+            for (int j = 0; j < D / 8; ++j) {
+                float f[8];
+                uint32_t y[4];
+                widen8<DT>(x[j], f);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) y[k] = round16x2<CMPQ_F16>(f[2 * k] * dn, f[2 * k + 1] * dn);
+                *reinterpret_cast<uint4*>(sq + w * C::kTileBytes + pf_at<D>(local, j)) = make_uint4(y[0], y[1], y[2], y[3]);
+            }
+            qs = A.scale * up;
+            tc5::fence_async_smem();
+            __syncwarp();
+            if (lane == 0) tc5::mbar_arrive(&q_full);
+        }
+        // the largest value scale of the pages that the block meets (warps of the second tile, if idle, help nobody)
+        float ref = 0.0f;
+        {
+            const int from = (t0 * kPfKeys) >> page_bits, to = min(pages, ((t0 + tiles) * kPfKeys) >> page_bits);
+#pragma unroll 4
+            for (int page = from + lane; page < to; page += 32) {
+                const int id = page_of(page);
+                if (id >= 0) ref = fmaxf(ref, __ldg(A.c.v_scale + (int64_t)id * H + head));
+            }
+#pragma unroll
+            for (int x = 16; x; x >>= 1) ref = fmaxf(ref, __shfl_xor_sync(0xffffffffu, ref, x));
+        }
+        const float inv_ref = ref > 0.0f ? 1.0f / ref : 0.0f;
+        const uint32_t lanes = (uint32_t)(warp & 3) << 21, ts = tmem + w * 128 + lanes, to = tmem_o + w * 128 + lanes;
+        const int page_span = min(kPfKeys, 1 << page_bits), per_tile = kPfKeys / page_span;
+        // lane k holds the scales of the tile's k-th page, those of the next tile are under way
+        float2 sc, sc_next = make_float2(0.0f, 0.0f);
+        auto scales = [&](int t) {
+            float2 x = make_float2(0.0f, 0.0f);
+            if (lane < per_tile) {
+                const int id = page_of(((t0 + t) * kPfKeys >> page_bits) + lane);
+                if (id >= 0) x = make_float2(__ldg(A.c.k_scale + (int64_t)id * H + head), __ldg(A.c.v_scale + (int64_t)id * H + head));
+            }
+            return x;
+        };
+        const bool work = w == 0 || two;
+        if (work && tiles > 0) sc_next = scales(0);
+        float m = -INFINITY, l = 0.0f;
+        // keys [lo, hi) are seen by this row; a tile inside [all_lo, all_hi) is seen whole by the warp's rows
+        const int hi = real ? (A.causal ? min(len, pos + 1) : len) : INT32_MAX, lo = real && A.window > 0 ? pos - A.window + 1 : 0;
+        const int all_hi = __reduce_min_sync(0xffffffffu, hi), all_lo = __reduce_max_sync(0xffffffffu, lo);
+        bool ok = true;
+        for (int t = 0; work && t < tiles; ++t) {
+            sc = sc_next;
+            const float vs = fmaxf(sc.y * inv_ref, 0x1p-100f), bias = log2f(vs), inv_vs = 1.0f / vs;
+            if (t + 1 < tiles) sc_next = scales(t + 1);
+            if (!(ok = tc5::mbar_wait(s_full + w, t & 1, &failed))) break;
+            tc5::fence_after_sync();
+            const int key0 = (t0 + t) * kPfKeys;
+            const bool masked = key0 + kPfKeys > all_hi || key0 < all_lo;
+            const int from = lo - key0, upto = hi - key0;
+
+            // largest score of the row: page by page, the key scale is positive
+            float top = -INFINITY;
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                uint32_t x[64];
+                tc5::tmem_ld32(ts + half * 64, x);
+                tc5::tmem_ld32(ts + half * 64 + 32, x + 32);
+                tc5::tmem_ld_wait();
+#pragma unroll
+                for (int part = 0; part < 4; ++part) {  // 16 keys are never on two pages
+                    const int col = half * 64 + part * 16;
+                    const float f = qs * __shfl_sync(0xffffffffu, sc.x, col / page_span);
+                    float most = -INFINITY;
+                    if (masked) {
+#pragma unroll
+                        for (int j = 0; j < 16; ++j)
+                            if (col + j >= from && col + j < upto) most = fmaxf(most, __uint_as_float(x[part * 16 + j]));
+                    } else {
+#pragma unroll
+                        for (int j = 0; j < 16; ++j) most = fmaxf(most, __uint_as_float(x[part * 16 + j]));
+                    }
+                    if (most > -INFINITY) top = fmaxf(top, most * f);
+                }
+            }
+            const bool grown = top > m + kPfSlack;
+            if (__any_sync(0xffffffffu, grown)) {
+                const float now = grown ? top : m, keep = grown ? ex2(m - now) : 1.0f;
+                m = now;
+                l *= keep;
+                if (t > 0) {  // the products into O that came before have ended: S was committed after them
+#pragma unroll
+                    for (int c = 0; c < D; c += 32) {
+                        uint32_t x[32];
+                        tc5::tmem_ld32(to + c, x);
+                        tc5::tmem_ld_wait();
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) x[j] = __float_as_uint(__uint_as_float(x[j]) * keep);
+                        tc5::tmem_st32(to + c, x);
+                    }
+                }
+            }
+            const float at = m == -INFINITY ? 0.0f : m;
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                uint32_t x[64], y[32];
+                tc5::tmem_ld32(ts + half * 64, x);
+                tc5::tmem_ld32(ts + half * 64 + 32, x + 32);
+                tc5::tmem_ld_wait();
+#pragma unroll
+                for (int part = 0; part < 4; ++part) {
+                    const int col = half * 64 + part * 16, k = col / page_span;
+                    const float f = qs * __shfl_sync(0xffffffffu, sc.x, k), add = __shfl_sync(0xffffffffu, bias, k) - at;
+                    float sum = 0.0f;
+#pragma unroll
+                    for (int j = 0; j < 16; j += 2) {
+                        float a = ex2(fmaf(__uint_as_float(x[part * 16 + j]), f, add)), b = ex2(fmaf(__uint_as_float(x[part * 16 + j + 1]), f, add));
+                        if (masked) {
+                            if (col + j < from || col + j >= upto) a = 0.0f;
+                            if (col + j + 1 < from || col + j + 1 >= upto) b = 0.0f;
+                        }
+                        sum += a + b;
+                        y[part * 8 + j / 2] = round16x2<CMPQ_F16>(a, b);
+                    }
+                    l = fmaf(sum, __shfl_sync(0xffffffffu, inv_vs, k), l);
+                }
+                tc5::tmem_st32(ts + half * 32, y);
+            }
+            tc5::tmem_st_wait();
+            tc5::fence_before_sync();
+            __syncwarp();
+            if (lane == 0) tc5::mbar_arrive(p_full + w);
+        }
+        if (work && ok && tiles > 0) ok = tc5::mbar_wait(o_full + w, 0, &failed);
+        if (work && ok) {
+            tc5::fence_after_sync();
+            const float f = l > 0.0f ? ref / l : 0.0f;
+            uint16_t* dst = A.out + (int64_t)(first + i) * A.ldo + (int64_t)h * D;
+#pragma unroll
+            for (int c = 0; c < D / 2; c += 32) {  // columns c.. and D/2 + c..: groups 2 j and 2 j + 1 of eight entries
+                uint32_t x[32], y[32];
+                if (tiles > 0) {
+                    tc5::tmem_ld32(to + c, x);
+                    tc5::tmem_ld32(to + D / 2 + c, y);
+                    tc5::tmem_ld_wait();
+                } else {
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) x[j] = y[j] = 0u;
+                }
+                if (!real) continue;
+#pragma unroll
+                for (int j = 0; j < 32; j += 8) {
+                    uint32_t a[8];
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        a[k] = round16x2<DT>(__uint_as_float(x[j + 2 * k]) * f, __uint_as_float(x[j + 2 * k + 1]) * f);
+                        a[4 + k] = round16x2<DT>(__uint_as_float(y[j + 2 * k]) * f, __uint_as_float(y[j + 2 * k + 1]) * f);
+                    }
+                    uint16_t* o = dst + 2 * (c + j);
+                    if (A.wide_o) {
+                        *reinterpret_cast<uint4*>(o) = make_uint4(a[0], a[1], a[2], a[3]);
+                        *reinterpret_cast<uint4*>(o + 8) = make_uint4(a[4], a[5], a[6], a[7]);
+                    } else {
+#pragma unroll
+                        for (int k = 0; k < 16; ++k) o[k] = (uint16_t)(a[k >> 1] >> (16 * (k & 1)));
+                    }
+                }
+            }
+            if (A.lse && real) A.lse[(int64_t)(first + i) * A.n_heads + h] = l > 0.0f ? (m + log2f(l)) * kLn2 : -INFINITY;
+        }
+        tc5::fence_before_sync();
+    }
+    __syncwarp();
+    __syncthreads();
+    if (failed) {  // products and arrivals that were asked for have to end before the memory is given back
+        if (tid == 0) {
+            const long long start = clock64();
+            while (clock64() - start < (1ll << 21)) __nanosleep(1000);
+            if (A.word) atomicOr(A.word, kWordInternal);
+        }
+        __syncthreads();
+    }
+    if (warp == 12) tc5::tmem_free<1>(tmem, 512);
+}
+
+template <int DT, int D>
+static cmpq_status launch_prefill_of(const AttnArgs& a, cudaStream_t st) {
+    static bool raised[64];
+    if (!raise_smem_limit_once(attention_prefill_kernel<DT, D>, Prefill<D>::kSmem, raised)) return CMPQ_ERR_CUDA;
+    const int64_t row_blocks = ((int64_t)a.max_new * a.group + 255) / 256, blocks = row_blocks * a.b.n_seq * a.c.n_kv_heads;
+    if (blocks > INT32_MAX) return CMPQ_ERR_UNSUPPORTED;
+    attention_prefill_kernel<DT, D><<<(unsigned)blocks, kPfThreads, Prefill<D>::kSmem, st>>>(a, (int)row_blocks);
+    return launch_status();
+}
+
+cmpq_status launch_prefill(const AttnArgs& a, cmpq_dtype dt, cudaStream_t st) {
+    const bool bf = dt == CMPQ_BF16;
+    if (a.c.head_dim == 64) return bf ? launch_prefill_of<CMPQ_BF16, 64>(a, st) : launch_prefill_of<CMPQ_F16, 64>(a, st);
+    return bf ? launch_prefill_of<CMPQ_BF16, 128>(a, st) : launch_prefill_of<CMPQ_F16, 128>(a, st);
+}
+
+}  // namespace cmpq
