@@ -1,4 +1,6 @@
 // Attention of many query rows over the paged 8-bit cache: both products on tcgen05, accumulators in TMEM.
+#include <type_traits>
+
 #include "attention.cuh"
 
 namespace cmpq {
@@ -32,6 +34,25 @@ __device__ __forceinline__ uint32_t pf_at(int t, int j) {
     return t * 128 + (((p * 4 + c) ^ (t & 7)) << 4);
 }
 
+// Two floats in one register pair, and the instructions on such pairs.
+__device__ __forceinline__ uint64_t pair(float lo, float hi) {
+    uint64_t p;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(p) : "f"(lo), "f"(hi));
+    return p;
+}
+__device__ __forceinline__ float low(uint64_t p) { return __uint_as_float((uint32_t)p); }
+__device__ __forceinline__ float high(uint64_t p) { return __uint_as_float((uint32_t)(p >> 32)); }
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+    uint64_t d;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+    return d;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+    uint64_t d;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
+
 template <int DT, int D>
 __global__ void __launch_bounds__(kPfThreads, 1)
 attention_prefill_kernel(const __grid_constant__ AttnArgs A, const int row_blocks) {
@@ -46,7 +67,9 @@ attention_prefill_kernel(const __grid_constant__ AttnArgs A, const int row_block
     __shared__ int failed;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int H = A.c.n_kv_heads, g = A.group, page_bits = A.page_bits;
-    const int rb = row_blocks - 1 - blockIdx.x % row_blocks, s = blockIdx.x / row_blocks / H, head = blockIdx.x / row_blocks % H;
+    // the last row blocks see most keys and come first
+    const int units = gridDim.x / row_blocks;
+    const int rb = row_blocks - 1 - blockIdx.x / units, s = blockIdx.x % units / H, head = blockIdx.x % H;
 
     const int first = A.b.tok_off[s], n = A.b.tok_off[s + 1] - first, len = A.b.lens[s];
     if (len < 0 || len > A.max_len || n < 0 || n > A.max_new || first < 0 || (int64_t)first + n > A.b.n_tok) {
@@ -134,15 +157,21 @@ attention_prefill_kernel(const __grid_constant__ AttnArgs A, const int row_block
         const int w = warp - 8, c = lane % kLanes, q = lane / kLanes;
         const int r0 = D == 64 ? (q & 1) * 4 + (q >> 1) : q;  // eight neighbouring lanes write to different banks
         uint4 kc[kSteps], vc[kSteps];
-        auto fetch = [&](int t, const int8_t* codes, uint4 (&x)[kSteps]) {
+        // the warp's 32 keys lie on one page or, of 16 tokens, on two
+        int64_t at[2];
+        auto pages_of = [&](int t) {
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                const int key = (t0 + t) * kPfKeys + w * 32 + k * 16, id = page_of(key >> page_bits);
+                at[k] = id < 0 ? -1 : ((((int64_t)id * H + head) << page_bits) + (key & ((1 << page_bits) - 1)) + r0) * D + 16 * c;
+            }
+        };
+        auto fetch = [&](const int8_t* codes, uint4 (&x)[kSteps]) {
 #pragma unroll
             for (int i = 0; i < kSteps; ++i) {
-                const int key = (t0 + t) * kPfKeys + w * 32 + i * kRows + r0;
-                const int id = page_of(key >> page_bits);
+                const int k = i * kRows / 16;
                 x[i] = make_uint4(0u, 0u, 0u, 0u);
-                if (id >= 0)
-                    x[i] = __ldg(reinterpret_cast<const uint4*>(
-                        codes + (((((int64_t)id * H + head) << page_bits) + (key & ((1 << page_bits) - 1))) * D + 16 * c)));
+                if (at[k] >= 0) x[i] = __ldg(reinterpret_cast<const uint4*>(codes + at[k] + (i * kRows - 16 * k) * D));
             }
         };
         auto put = [&](uint8_t* tile, const uint4 (&x)[kSteps]) {
@@ -156,7 +185,7 @@ attention_prefill_kernel(const __grid_constant__ AttnArgs A, const int row_block
                     make_uint4(half_pair(d, 0x4140), half_pair(d, 0x4342), half_pair(e, 0x4140), half_pair(e, 0x4342));
             }
         };
-        if (tiles > 0) fetch(0, A.c.k_codes, kc), fetch(0, A.c.v_codes, vc);
+        if (tiles > 0) pages_of(0), fetch(A.c.k_codes, kc), fetch(A.c.v_codes, vc);
         for (int t = 0; t < tiles; ++t) {
             const int slot = t & 1, phase = ((t >> 1) & 1) ^ 1;
             if (!tc5::mbar_wait(k_empty + slot, phase, &failed)) break;
@@ -164,13 +193,13 @@ attention_prefill_kernel(const __grid_constant__ AttnArgs A, const int row_block
             tc5::fence_async_smem();
             __syncwarp();
             if (lane == 0) tc5::mbar_arrive(k_full + slot);
-            if (t + 1 < tiles) fetch(t + 1, A.c.k_codes, kc);
+            if (t + 1 < tiles) pages_of(t + 1), fetch(A.c.k_codes, kc);
             if (!tc5::mbar_wait(v_empty + slot, phase, &failed)) break;
             put(sv + slot * C::kTileBytes, vc);
             tc5::fence_async_smem();
             __syncwarp();
             if (lane == 0) tc5::mbar_arrive(v_full + slot);
-            if (t + 1 < tiles) fetch(t + 1, A.c.v_codes, vc);
+            if (t + 1 < tiles) fetch(A.c.v_codes, vc);
         }
     } else {
         const int w = warp >> 2, local = tid & 127, row = rb * 256 + w * 128 + local;
@@ -220,7 +249,7 @@ attention_prefill_kernel(const __grid_constant__ AttnArgs A, const int row_block
         }
         const float inv_ref = ref > 0.0f ? 1.0f / ref : 0.0f;
         const uint32_t lanes = (uint32_t)(warp & 3) << 21, ts = tmem + w * 128 + lanes, to = tmem_o + w * 128 + lanes;
-        const int page_span = min(kPfKeys, 1 << page_bits), per_tile = kPfKeys / page_span;
+        const int span_bits = min(7, page_bits), per_tile = kPfKeys >> span_bits;
         // lane k holds the scales of the tile's k-th page, those of the next tile are under way
         float2 sc, sc_next = make_float2(0.0f, 0.0f);
         auto scales = [&](int t) {
@@ -237,6 +266,34 @@ attention_prefill_kernel(const __grid_constant__ AttnArgs A, const int row_block
         // keys [lo, hi) are seen by this row; a tile inside [all_lo, all_hi) is seen whole by the warp's rows
         const int hi = real ? (A.causal ? min(len, pos + 1) : len) : INT32_MAX, lo = real && A.window > 0 ? pos - A.window + 1 : 0;
         const int all_hi = __reduce_min_sync(0xffffffffu, hi), all_lo = __reduce_max_sync(0xffffffffu, lo);
+        // The reference maximum has moved before keys 32 step.. of tile t: what was weighted with the old one.
+        auto rescale = [&](int t, int step, float keep) {
+            if (t > 0) {  // the products into O that came before have ended: S was committed after them
+#pragma unroll 1
+                for (int c = 0; c < D; c += 16) {
+                    uint32_t x[16];
+                    tc5::tmem_ld16(to + c, x);
+                    tc5::tmem_ld_wait();
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) x[j] = __float_as_uint(__uint_as_float(x[j]) * keep);
+                    tc5::tmem_st16(to + c, x);
+                }
+            }
+#pragma unroll 1
+            for (int k = 0; k < step; ++k) {  // weights of this tile
+                uint32_t x[16];
+                tc5::tmem_st_wait();
+                tc5::tmem_ld16(ts + k * 16, x);
+                tc5::tmem_ld_wait();
+                const __half2 by = __float2half2_rn(keep);
+#pragma unroll
+                for (int j = 0; j < 16; ++j) {
+                    const __half2 y = __hmul2(*reinterpret_cast<const __half2*>(&x[j]), by);
+                    x[j] = *reinterpret_cast<const uint32_t*>(&y);
+                }
+                tc5::tmem_st16(ts + k * 16, x);
+            }
+        };
         bool ok = true;
         for (int t = 0; work && t < tiles; ++t) {
             sc = sc_next;
@@ -245,76 +302,60 @@ attention_prefill_kernel(const __grid_constant__ AttnArgs A, const int row_block
             if (!(ok = tc5::mbar_wait(s_full + w, t & 1, &failed))) break;
             tc5::fence_after_sync();
             const int key0 = (t0 + t) * kPfKeys;
-            const bool masked = key0 + kPfKeys > all_hi || key0 < all_lo;
             const int from = lo - key0, upto = hi - key0;
-
-            // largest score of the row: page by page, the key scale is positive
-            float top = -INFINITY;
+            auto tile = [&](auto masked) {
+                uint32_t x[2][32];
+                tc5::tmem_ld32(ts, x[0]);
 #pragma unroll
-            for (int half = 0; half < 2; ++half) {
-                uint32_t x[64];
-                tc5::tmem_ld32(ts + half * 64, x);
-                tc5::tmem_ld32(ts + half * 64 + 32, x + 32);
-                tc5::tmem_ld_wait();
+                for (int step = 0; step < 4; ++step) {  // 32 keys: on two pages at most
+                    uint32_t(&v)[32] = x[step & 1];
+                    tc5::tmem_ld_wait();
+                    if (step < 3) tc5::tmem_ld32(ts + (step + 1) * 32, x[(step + 1) & 1]);
+                    if (decltype(masked)::value) {
 #pragma unroll
-                for (int part = 0; part < 4; ++part) {  // 16 keys are never on two pages
-                    const int col = half * 64 + part * 16;
-                    const float f = qs * __shfl_sync(0xffffffffu, sc.x, col / page_span);
-                    float most = -INFINITY;
-                    if (masked) {
-#pragma unroll
-                        for (int j = 0; j < 16; ++j)
-                            if (col + j >= from && col + j < upto) most = fmaxf(most, __uint_as_float(x[part * 16 + j]));
-                    } else {
-#pragma unroll
-                        for (int j = 0; j < 16; ++j) most = fmaxf(most, __uint_as_float(x[part * 16 + j]));
+                        for (int j = 0; j < 32; ++j)
+                            if (step * 32 + j < from || step * 32 + j >= upto) v[j] = 0xff800000u;  // -infinity
                     }
-                    if (most > -INFINITY) top = fmaxf(top, most * f);
-                }
-            }
-            const bool grown = top > m + kPfSlack;
-            if (__any_sync(0xffffffffu, grown)) {
-                const float now = grown ? top : m, keep = grown ? ex2(m - now) : 1.0f;
-                m = now;
-                l *= keep;
-                if (t > 0) {  // the products into O that came before have ended: S was committed after them
+                    float f[2], add[2], top = -INFINITY;
 #pragma unroll
-                    for (int c = 0; c < D; c += 32) {
-                        uint32_t x[32];
-                        tc5::tmem_ld32(to + c, x);
-                        tc5::tmem_ld_wait();
+                    for (int k = 0; k < 2; ++k) {
+                        f[k] = fmaxf(qs * __shfl_sync(0xffffffffu, sc.x, (step * 32 + k * 16) >> span_bits), 0x1p-126f);
+                        float most = fmaxf(__uint_as_float(v[k * 16]), __uint_as_float(v[k * 16 + 1]));
 #pragma unroll
-                        for (int j = 0; j < 32; ++j) x[j] = __float_as_uint(__uint_as_float(x[j]) * keep);
-                        tc5::tmem_st32(to + c, x);
+                        for (int j = 2; j < 16; j += 2) most = fmaxf(fmaxf(most, __uint_as_float(v[k * 16 + j])), __uint_as_float(v[k * 16 + j + 1]));
+                        top = fmaxf(top, most * f[k]);
                     }
-                }
-            }
-            const float at = m == -INFINITY ? 0.0f : m;
+                    const bool grown = top > m + kPfSlack;
+                    if (__any_sync(0xffffffffu, grown)) {
+                        const float now = grown ? top : m, keep = grown ? ex2(m - now) : 1.0f;
+                        m = now;
+                        l *= keep;
+                        rescale(t, step, keep);
+                    }
+                    const float at = m == -INFINITY ? 0.0f : m;
+                    uint32_t y[16];
 #pragma unroll
-            for (int half = 0; half < 2; ++half) {
-                uint32_t x[64], y[32];
-                tc5::tmem_ld32(ts + half * 64, x);
-                tc5::tmem_ld32(ts + half * 64 + 32, x + 32);
-                tc5::tmem_ld_wait();
+                    for (int k = 0; k < 2; ++k) {
+                        const int page = (step * 32 + k * 16) >> span_bits;
+                        add[k] = __shfl_sync(0xffffffffu, bias, page) - at;
+                        const uint64_t ff = pair(f[k], f[k]), aa = pair(add[k], add[k]);
+                        uint64_t sum = 0;
 #pragma unroll
-                for (int part = 0; part < 4; ++part) {
-                    const int col = half * 64 + part * 16, k = col / page_span;
-                    const float f = qs * __shfl_sync(0xffffffffu, sc.x, k), add = __shfl_sync(0xffffffffu, bias, k) - at;
-                    float sum = 0.0f;
-#pragma unroll
-                    for (int j = 0; j < 16; j += 2) {
-                        float a = ex2(fmaf(__uint_as_float(x[part * 16 + j]), f, add)), b = ex2(fmaf(__uint_as_float(x[part * 16 + j + 1]), f, add));
-                        if (masked) {
-                            if (col + j < from || col + j >= upto) a = 0.0f;
-                            if (col + j + 1 < from || col + j + 1 >= upto) b = 0.0f;
+                        for (int j = 0; j < 16; j += 2) {
+                            const uint64_t z = fma2(pair(__uint_as_float(v[k * 16 + j]), __uint_as_float(v[k * 16 + j + 1])), ff, aa);
+                            const float a = ex2(low(z)), b = ex2(high(z));
+                            sum = add2(sum, pair(a, b));
+                            y[k * 8 + j / 2] = round16x2<CMPQ_F16>(a, b);
                         }
-                        sum += a + b;
-                        y[part * 8 + j / 2] = round16x2<CMPQ_F16>(a, b);
+                        l = fmaf(low(sum) + high(sum), __shfl_sync(0xffffffffu, inv_vs, page), l);
                     }
-                    l = fmaf(sum, __shfl_sync(0xffffffffu, inv_vs, k), l);
+                    tc5::tmem_st16(ts + step * 16, y);
                 }
-                tc5::tmem_st32(ts + half * 32, y);
-            }
+            };
+            if (key0 + kPfKeys > all_hi || key0 < all_lo)
+                tile(std::true_type());
+            else
+                tile(std::false_type());
             tc5::tmem_st_wait();
             tc5::fence_before_sync();
             __syncwarp();

@@ -185,6 +185,11 @@ __device__ __forceinline__ void tmem_st32(uint32_t addr, const uint32_t* r) {
         CMPQ_I8(r, 8), CMPQ_I8(r, 16), CMPQ_I8(r, 24), "r"(addr)
         : "memory");
 }
+__device__ __forceinline__ void tmem_st16(uint32_t addr, const uint32_t* r) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15};" ::CMPQ_I8(r, 0), CMPQ_I8(r, 8), "r"(addr)
+        : "memory");
+}
 #undef CMPQ_R8
 #undef CMPQ_I8
 __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
