@@ -112,8 +112,8 @@ constexpr int kMmThreads = 192;  // a warp for the loads, one for the products, 
 constexpr int kMmMaxStages = 8;
 
 // Few tokens: the weights are read once and their bytes are the time.  A cluster of up to eight CTAs splits the sum
-// of one tile, so that there are enough CTAs to keep every SM's loads in flight; the int32 parts are joined through
-// distributed shared memory (integers: the order does not matter), CTA r finishing the tokens r, r + S, ...  Launched
+// of one tile, so that there are enough CTAs to keep every SM's loads in flight; every CTA
+// pushes its int32 parts into the shared memory of the CTA that finishes the token (integers: the order does not matter).  Launched
 // behind the quantization of its tokens, it fetches its first weights before that has ended.
 template <int DT, int BN>
 __global__ void __launch_bounds__(kMmThreads)
@@ -184,7 +184,10 @@ matmul_i8_split_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_co
         const bool real = o < A.d_out;
         const float ws = real ? __ldg(A.ws + o) : 0.0f, bias = real && A.bias ? widen16<DT>(A.bias[o]) : 0.0f;
         const int t0 = nt * BN, left = min(BN, A.n - t0);
-        int* part = reinterpret_cast<int*>(smem);  // [token][128]: the loads into it have all been consumed
+        // token j's sums meet in CTA j % splits, at [source CTA][j / splits][channel] behind the stages
+        const uint32_t part = tc5::smem_addr(smem + A.stages * kStage) + 4u * row;
+        const int slots = (BN + splits - 1) / splits;
+        int owner = 0, slot = rank * slots;
         for (int c = 0; c < left; c += 16) {
             uint32_t r[16];
             tc5::tmem_ld16(tmem + ((uint32_t)quad << 21) + c, r);
@@ -193,29 +196,29 @@ matmul_i8_split_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_co
             for (int j = 0; j < 16; ++j) {
                 if (c + j >= left) break;
                 if (splits > 1) {
-                    part[(c + j) * 128 + row] = (int)r[j];
+                    tc5::st_cluster_u32(part + slot * 512, owner, r[j]);
+                    if (++owner == splits) owner = 0, ++slot;
                 } else if (real) {
                     const int64_t t = t0 + c + j;
-                    A.y[t * A.ldy + o] = scaled<DT>((int)r[j], A.xs[t], ws, bias, A.bias != nullptr);
+                    A.y[t * A.ldy + o] = scaled<DT>((int)r[j], __ldg(A.xs + t), ws, bias, A.bias != nullptr);
                 }
             }
         }
         tc5::fence_before_sync();
         if (splits > 1) {
             tc5::cluster_sync();
-            const uint32_t at = tc5::smem_addr(part);
-            for (int j = rank; j < left; j += splits) {
+            const int* mine = reinterpret_cast<const int*>(smem + A.stages * kStage) + row;
+            for (int i = 0, t = t0 + rank; t < t0 + left; ++i, t += splits) {
                 int acc = 0;
-                for (int s = 0; s < splits; ++s) acc += tc5::ld_cluster_s32(at + 4u * (j * 128 + row), s);
-                const int64_t t = t0 + j;
-                if (real) A.y[t * A.ldy + o] = scaled<DT>(acc, A.xs[t], ws, bias, A.bias != nullptr);
+#pragma unroll
+                for (int s = 0; s < 8; ++s)
+                    if (s < splits) acc += mine[(s * slots + i) * 128];
+                if (real) A.y[(int64_t)t * A.ldy + o] = scaled<DT>(acc, __ldg(A.xs + t), ws, bias, A.bias != nullptr);
             }
-            tc5::cluster_sync();
         }
     }
     if (splits > 1 && warp < 2) {
         __syncwarp();
-        tc5::cluster_sync();
         tc5::cluster_sync();
     }
     __syncthreads();
@@ -345,18 +348,18 @@ matmul_i8_pair_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_con
     if (warp == 1) tc5::tmem_free<2>(tmem, 512);
 }
 
-constexpr size_t kSplitSmem = 100 << 10;  // two CTAs share an SM
-
 template <int DT, int BN>
 static cmpq_status launch_split(const CUtensorMap& wmap, const CUtensorMap& xmap, ProductArgs a, bool behind, cudaStream_t st) {
     constexpr int kStage = (128 + BN) * 128;
+    constexpr size_t kSplitSmem = BN == 128 ? 200 << 10 : 112 << 10;  // two CTAs share an SM, or one has it
     const int64_t tiles = (int64_t)a.m_tiles * a.n_tiles;
-    // enough CTAs for two per SM, at least two blocks of the sum each
-    const int want = (int)std::max<int64_t>(1, std::min<int64_t>(8, (2 * sm_count() + tiles - 1) / tiles));
+    // as many CTAs as find room at once, at least two blocks of the sum each
+    const int want = (int)std::max<int64_t>(1, std::min<int64_t>(8, ((BN == 128 ? 1 : 2) * sm_count() / tiles)));
     a.per = std::max((a.kblocks + want - 1) / want, std::min(2, a.kblocks));
     const int splits = (a.kblocks + a.per - 1) / a.per;
-    a.stages = std::min({(int)((kSplitSmem - 1024) / kStage), kMmMaxStages, std::max(a.per, 2)});
-    const size_t smem = (size_t)std::max(a.stages * kStage, 128 * BN * 4) + 1024;
+    const size_t parts = splits > 1 ? (size_t)(BN + splits - 1) / splits * splits * 512 : 0;
+    a.stages = std::min({(int)((kSplitSmem - 1024 - parts) / kStage), kMmMaxStages, std::max(a.per, 1)});
+    const size_t smem = a.stages * kStage + parts + 1024;
     static bool raised[64];
     if (!raise_smem_limit_once(matmul_i8_split_kernel<DT, BN>, kSplitSmem, raised)) return CMPQ_ERR_CUDA;
     if (tiles * splits > INT32_MAX) return CMPQ_ERR_UNSUPPORTED;
