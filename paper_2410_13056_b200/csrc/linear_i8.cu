@@ -81,146 +81,136 @@ quantize_tokens_kernel(const uint16_t* __restrict__ X, int64_t d, int64_t ldx, i
 
 // ---- the product --------------------------------------------------------------------------------------------
 //
-// Both kernels compute the transposed product: 128 weight rows (output channels) are the rows of the accumulator, a
-// TMEM lane each, and the tokens its columns.  A thread of the epilogue then owns one channel (its scale and bias are
-// registers) and a warp's store is 32 neighbouring channels of one token, so y is written in whole 64-byte runs
-// without a detour, for any token count and row stride.  Weight and token codes are both K-major as they lie in
-// memory; 128 bytes of the sum are one swizzled TMA box and four instructions of K = 32.
+// Tokens are the rows of the accumulator (a TMEM lane each), output channels its columns: a thread of the epilogue owns
+// a token, whose scale is a register, and writes neighbouring channels, 16 bytes at a time; the channels' scales and
+// biases come from shared memory.  Codes of both sides are K-major as they lie in memory; 128 bytes of the sum are one
+// swizzled TMA box and four instructions of K = 32.
 
 struct ProductArgs {
     const float *xs, *ws;
     const uint16_t* bias;
     uint16_t* y;
     int64_t ldy;
-    int n, d_out;
-    int kblocks;    // 128-byte blocks of the sum
-    int per;        // split kernel: blocks per CTA of a cluster
-    int n_tiles;    // token tiles
-    int m_tiles;    // channel tiles
-    int stages;     // split kernel
+    int n, d_out, kblocks;  // kblocks: 128-byte blocks of the sum
+    int wide;               // y takes 16-byte stores
+    int n_tiles, m_tiles;   // tiles of channels, of tokens
+    int stages, bn, rows;   // tile kernel: stages, channels of a tile, token rows that a box brings
     int32_t* failed;
 };
 
+constexpr int kMmThreads = 320;  // a warp for the loads, one for the products, eight for the epilogue
+constexpr int kMmMaxStages = 12;
+
+// Columns [c0, c1) of a warp's 32 accumulator rows: fl16(fl(fl(sum * xs) * ws) + bias) into y + column, of which `left`
+// exist.  c0 and c1 are multiples of 16; scale_bias holds (ws, bias) of the tile's columns.
 template <int DT>
-__device__ __forceinline__ uint16_t scaled(int acc, float xs, float ws, float bias, bool has_bias) {
-    float v = (float)acc * xs * ws;
-    if (has_bias) v += bias;
-    return round16<DT>(v);
+__device__ __forceinline__ void store_rows(uint32_t tmem, int c0, int c1, const float2* scale_bias, bool has_bias, float xs, bool real,
+                                           uint16_t* y, int left, bool wide) {
+    for (int c = c0; c < c1; c += 16) {
+        uint32_t r[16], w[8];
+        tc5::tmem_ld16(tmem + c, r);
+        tc5::tmem_ld_wait();
+#pragma unroll
+        for (int j = 0; j < 16; j += 2) {
+            const float4 sb = *reinterpret_cast<const float4*>(scale_bias + c + j);
+            float a = (float)(int)r[j] * xs * sb.x, b = (float)(int)r[j + 1] * xs * sb.z;
+            if (has_bias) a += sb.y, b += sb.w;
+            w[j / 2] = round16x2<DT>(a, b);
+        }
+        if (!real) continue;
+        if (wide && c + 16 <= left) {
+            *reinterpret_cast<uint4*>(y + c) = make_uint4(w[0], w[1], w[2], w[3]);
+            *reinterpret_cast<uint4*>(y + c + 8) = make_uint4(w[4], w[5], w[6], w[7]);
+        } else {
+#pragma unroll
+            for (int j = 0; j < 16; ++j)
+                if (c + j < left) y[c + j] = (uint16_t)(w[j >> 1] >> (16 * (j & 1)));
+        }
+    }
 }
 
-constexpr int kMmThreads = 192;  // a warp for the loads, one for the products, four for the epilogue
-constexpr int kMmMaxStages = 8;
-
-// Few tokens: the weights are read once and their bytes are the time.  A cluster of up to eight CTAs splits the sum
-// of one tile, so that there are enough CTAs to keep every SM's loads in flight; every CTA
-// pushes its int32 parts into the shared memory of the CTA that finishes the token (integers: the order does not matter).  Launched
-// behind the quantization of its tokens, it fetches its first weights before that has ended.
-template <int DT, int BN>
+// Few tiles: a block takes 128 tokens (all of them, mostly) and `bn` channels, a multiple of 16 chosen so that the
+// blocks fill the SMs; the weights pass through once and are the time while tokens are few.  Launched behind the
+// quantization of its tokens, a block asks for its first weights before that has ended.  Rows of the token tile that do
+// not exist are not loaded: what the shared memory holds there only reaches accumulator rows that are not stored.
+template <int DT>
 __global__ void __launch_bounds__(kMmThreads)
-matmul_i8_split_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__ CUtensorMap xmap,
-                       const __grid_constant__ ProductArgs A, const int splits) {
+matmul_i8_tile_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__ CUtensorMap xmap,
+                      const __grid_constant__ ProductArgs A) {
     extern __shared__ uint8_t raw[];
     uint8_t* smem = raw + ((1024u - (tc5::smem_addr(raw) & 1023u)) & 1023u);
     __shared__ uint64_t full[kMmMaxStages], empty[kMmMaxStages], done;
+    __shared__ float4 scale_bias[128];
     __shared__ uint32_t tmem_at;
     __shared__ int failed;
-    constexpr int kStage = (128 + BN) * 128, kCols = BN < 32 ? 32 : BN;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int rank = splits > 1 ? (int)tc5::cluster_rank() : 0;
-    const int tile = blockIdx.x / splits, nt = tile % A.n_tiles, mt = tile / A.n_tiles;
-    const int k0 = rank * A.per, k1 = min(A.kblocks, k0 + A.per), count = k1 - k0;
+    const int nt = blockIdx.x / A.m_tiles, mt = blockIdx.x % A.m_tiles, bn = A.bn;
+    const int stage = (128 + bn) * 128, columns = bn <= 32 ? 32 : bn <= 64 ? 64 : bn <= 128 ? 128 : 256;
     if (threadIdx.x == 0) {
         for (int i = 0; i < A.stages; ++i) tc5::mbar_init(full + i, 1), tc5::mbar_init(empty + i, 1);
         tc5::mbar_init(&done, 1);
         failed = 0;
         tc5::mbar_init_fence();
     }
-    if (warp == 1) tc5::tmem_alloc<1>(&tmem_at, kCols);
+    if (warp == 1) tc5::tmem_alloc<1>(&tmem_at, columns);
     tc5::fence_before_sync();
     __syncthreads();
     tc5::fence_after_sync();
     const uint32_t tmem = tmem_at;
     if (warp == 0) {
         if (tc5::elect_one()) {
-            const int first = min(count, A.stages);
+            const int first = min(A.kblocks, A.stages), bytes = (A.rows + bn) * 128;
             for (int i = 0; i < first; ++i) {
-                tc5::mbar_expect_tx(full + i, kStage);
-                tc5::tma_load_2d(smem + i * kStage, &wmap, full + i, (k0 + i) * 128, mt * 128);
+                tc5::mbar_expect_tx(full + i, bytes);
+                tc5::tma_load_2d(smem + i * stage + 128 * 128, &wmap, full + i, i * 128, nt * bn);
             }
             tc5::wait_for_previous();
-            for (int i = 0; i < first; ++i)
-                tc5::tma_load_2d(smem + i * kStage + 128 * 128, &xmap, full + i, (k0 + i) * 128, nt * BN);
+            for (int i = 0; i < first; ++i) tc5::tma_load_2d(smem + i * stage, &xmap, full + i, i * 128, mt * 128);
             int slot = 0, phase = 0;
-            for (int i = first; i < count; ++i) {
+            for (int i = first; i < A.kblocks; ++i) {
                 if (!tc5::mbar_wait(empty + slot, phase, &failed)) break;
-                tc5::mbar_expect_tx(full + slot, kStage);
-                tc5::tma_load_2d(smem + slot * kStage, &wmap, full + slot, (k0 + i) * 128, mt * 128);
-                tc5::tma_load_2d(smem + slot * kStage + 128 * 128, &xmap, full + slot, (k0 + i) * 128, nt * BN);
+                tc5::mbar_expect_tx(full + slot, bytes);
+                tc5::tma_load_2d(smem + slot * stage + 128 * 128, &wmap, full + slot, i * 128, nt * bn);
+                tc5::tma_load_2d(smem + slot * stage, &xmap, full + slot, i * 128, mt * 128);
                 if (++slot == A.stages) slot = 0, phase ^= 1;
             }
         }
     } else if (warp == 1) {
         if (tc5::elect_one()) {
+            const uint32_t idesc = tc5::idesc_i8(128, bn);
             int slot = 0, phase = 0;
-            for (int i = 0; i < count; ++i) {
+            for (int i = 0; i < A.kblocks; ++i) {
                 if (!tc5::mbar_wait(full + slot, phase, &failed)) break;
                 tc5::fence_after_sync();
-                const uint32_t at = tc5::smem_addr(smem + slot * kStage);
+                const uint32_t at = tc5::smem_addr(smem + slot * stage);
                 const uint64_t a = tc5::desc_k_sw128(at), b = tc5::desc_k_sw128(at + 128 * 128);
 #pragma unroll
-                for (int k = 0; k < 4; ++k)
-                    tc5::mma_i8<1>(tmem, a + 2 * k, b + 2 * k, tc5::idesc_i8(128, BN), (i | k) != 0);
+                for (int k = 0; k < 4; ++k) tc5::mma_i8<1>(tmem, a + 2 * k, b + 2 * k, idesc, (i | k) != 0);
                 tc5::mma_commit(empty + slot);
                 if (++slot == A.stages) slot = 0, phase ^= 1;
             }
             tc5::mma_commit(&done);
         }
     } else {
+        float2* sb = reinterpret_cast<float2*>(scale_bias);
+        const int o0 = nt * bn, left = min(bn, A.d_out - o0), i = threadIdx.x - 64;
+        if (i < bn) {
+            const int o = min(o0 + i, A.d_out - 1);
+            sb[i] = make_float2(__ldg(A.ws + o), A.bias ? widen16<DT>(A.bias[o]) : 0.0f);
+        }
         tc5::wait_for_previous();  // the tokens' scales
+        const int quad = warp & 3, t = mt * 128 + quad * 32 + lane, half = (bn / 16 + 1) / 2 * 16;
+        const bool real = t < A.n, upper = warp >= 6;
+        const float xs = real ? __ldg(A.xs + t) : 0.0f;
+        asm volatile("bar.sync 1, 256;" ::: "memory");
         tc5::mbar_wait(&done, 0, &failed);
         tc5::fence_after_sync();
-        const int quad = warp & 3, row = quad * 32 + lane;
-        const int64_t o = (int64_t)mt * 128 + row;
-        const bool real = o < A.d_out;
-        const float ws = real ? __ldg(A.ws + o) : 0.0f, bias = real && A.bias ? widen16<DT>(A.bias[o]) : 0.0f;
-        const int t0 = nt * BN, left = min(BN, A.n - t0);
-        // token j's sums meet in CTA j % splits, at [source CTA][j / splits][channel] behind the stages
-        const uint32_t part = tc5::smem_addr(smem + A.stages * kStage) + 4u * row;
-        const int slots = (BN + splits - 1) / splits;
-        int owner = 0, slot = rank * slots;
-        for (int c = 0; c < left; c += 16) {
-            uint32_t r[16];
-            tc5::tmem_ld16(tmem + ((uint32_t)quad << 21) + c, r);
-            tc5::tmem_ld_wait();
-#pragma unroll
-            for (int j = 0; j < 16; ++j) {
-                if (c + j >= left) break;
-                if (splits > 1) {
-                    tc5::st_cluster_u32(part + slot * 512, owner, r[j]);
-                    if (++owner == splits) owner = 0, ++slot;
-                } else if (real) {
-                    const int64_t t = t0 + c + j;
-                    A.y[t * A.ldy + o] = scaled<DT>((int)r[j], __ldg(A.xs + t), ws, bias, A.bias != nullptr);
-                }
-            }
-        }
+        if (mt * 128 + quad * 32 < A.n)
+            store_rows<DT>(tmem + ((uint32_t)quad << 21), upper ? half : 0, upper ? bn : half, sb, A.bias != nullptr, xs, real,
+                           A.y + (int64_t)t * A.ldy + o0, left, A.wide);
         tc5::fence_before_sync();
-        if (splits > 1) {
-            tc5::cluster_sync();
-            const int* mine = reinterpret_cast<const int*>(smem + A.stages * kStage) + row;
-            for (int i = 0, t = t0 + rank; t < t0 + left; ++i, t += splits) {
-                int acc = 0;
-#pragma unroll
-                for (int s = 0; s < 8; ++s)
-                    if (s < splits) acc += mine[(s * slots + i) * 128];
-                if (real) A.y[(int64_t)t * A.ldy + o] = scaled<DT>(acc, __ldg(A.xs + t), ws, bias, A.bias != nullptr);
-            }
-        }
     }
-    if (splits > 1 && warp < 2) {
-        __syncwarp();
-        tc5::cluster_sync();
-    }
+    __syncwarp();
     __syncthreads();
     if (failed) {  // the loads that were asked for have to land before the shared memory is given back
         if (threadIdx.x == 0) {
@@ -230,16 +220,16 @@ matmul_i8_split_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_co
         }
         __syncthreads();
     }
-    if (warp == 1) tc5::tmem_free<1>(tmem, kCols);
+    if (warp == 1) tc5::tmem_free<1>(tmem, columns);
 }
 
 constexpr int kPairStages = 6, kPairStageBytes = 2 * 128 * 128;
 constexpr size_t kPairSmem = kPairStages * kPairStageBytes + 1024;
 
-// Many tokens: pairs of CTAs stay on their SMs and walk over tiles of 256 channels x 256 tokens (cta_group::2).  A CTA
-// loads its 128 channels and half of the tokens, so each byte that an SM reads feeds 512 products; six stages of 32 KB.  Two accumulators
-// of 256 columns alternate, the epilogue of one tile runs under the products of the next.  Token tiles go fastest: the
-// pairs at work share a few weight tiles and the token codes stay in L2.
+// Many tokens: pairs of CTAs stay on their SMs and walk over tiles of 256 tokens x 256 channels (cta_group::2).  A CTA
+// loads its 128 tokens and half of the channels, so each byte that an SM reads feeds 512 products; six stages of 32 KB.
+// Two accumulators of 256 columns alternate, the epilogue of one tile runs under the products of the next.  Token tiles
+// go fastest: the pairs at work share a few weight tiles and the token codes stay in L2.
 template <int DT>
 __global__ void __launch_bounds__(kMmThreads, 1)
 matmul_i8_pair_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__ CUtensorMap xmap,
@@ -247,6 +237,7 @@ matmul_i8_pair_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_con
     extern __shared__ uint8_t raw[];
     uint8_t* smem = raw + ((1024u - (tc5::smem_addr(raw) & 1023u)) & 1023u);
     __shared__ uint64_t full[kPairStages], empty[kPairStages], acc_full[2], acc_empty[2];
+    __shared__ float4 scale_bias[2][128];
     __shared__ uint32_t tmem_at;
     __shared__ int failed;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -254,7 +245,7 @@ matmul_i8_pair_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_con
     const int tiles = A.n_tiles * A.m_tiles, first = blockIdx.x >> 1, step = gridDim.x >> 1;
     if (threadIdx.x == 0) {
         for (int i = 0; i < kPairStages; ++i) tc5::mbar_init(full + i, 1), tc5::mbar_init(empty + i, 1);
-        for (int i = 0; i < 2; ++i) tc5::mbar_init(acc_full + i, 1), tc5::mbar_init(acc_empty + i, 8);
+        for (int i = 0; i < 2; ++i) tc5::mbar_init(acc_full + i, 1), tc5::mbar_init(acc_empty + i, 16);
         failed = 0;
         tc5::mbar_init_fence();
     }
@@ -270,13 +261,13 @@ matmul_i8_pair_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_con
             int slot = 0, phase = 1;  // a new barrier counts as empty
             bool ok = true;
             for (int tile = first; ok && tile < tiles; tile += step) {
-                const int nt = tile % A.n_tiles, mt = tile / A.n_tiles;
+                const int mt = tile % A.m_tiles, nt = tile / A.m_tiles;
                 for (int k = 0; k < A.kblocks; ++k) {
                     if (!(ok = tc5::mbar_wait(empty + slot, phase, &failed))) break;
                     if (rank == 0) tc5::mbar_expect_tx(full + slot, 2 * kPairStageBytes);
                     uint8_t* at = smem + slot * kPairStageBytes;
-                    tc5::tma_load_2d_pair(at, &wmap, full + slot, k * 128, mt * 256 + rank * 128);
-                    tc5::tma_load_2d_pair(at + 128 * 128, &xmap, full + slot, k * 128, nt * 256 + rank * 128);
+                    tc5::tma_load_2d_pair(at, &xmap, full + slot, k * 128, mt * 256 + rank * 128);
+                    tc5::tma_load_2d_pair(at + 128 * 128, &wmap, full + slot, k * 128, nt * 256 + rank * 128);
                     if (++slot == kPairStages) slot = 0, phase ^= 1;
                 }
             }
@@ -305,28 +296,22 @@ matmul_i8_pair_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_con
             }
         }
     } else {
-        const int quad = warp & 3;
+        const int quad = warp & 3, upper = warp >= 6, i = threadIdx.x - 64;
         int acc = 0, phase = 0;
         for (int tile = first; tile < tiles; tile += step) {
-            const int nt = tile % A.n_tiles, mt = tile / A.n_tiles;
-            const int64_t o = (int64_t)mt * 256 + rank * 128 + quad * 32 + lane;
-            const bool real = o < A.d_out;
-            const float ws = real ? __ldg(A.ws + o) : 0.0f, bias = real && A.bias ? widen16<DT>(A.bias[o]) : 0.0f;
-            const int t0 = nt * 256, left = min(256, A.n - t0);
+            const int mt = tile % A.m_tiles, nt = tile / A.m_tiles;
+            const int o0 = nt * 256, left = min(256, A.d_out - o0), row0 = mt * 256 + rank * 128 + quad * 32, t = row0 + lane;
+            const bool real = t < A.n;
+            const float xs = real ? __ldg(A.xs + t) : 0.0f;
+            float2* sb = reinterpret_cast<float2*>(scale_bias[acc]);
+            const int o = min(o0 + i, A.d_out - 1);
+            sb[i] = make_float2(__ldg(A.ws + o), A.bias ? widen16<DT>(A.bias[o]) : 0.0f);
+            asm volatile("bar.sync 1, 256;" ::: "memory");
             if (!tc5::mbar_wait(acc_full + acc, phase, &failed)) break;
             tc5::fence_after_sync();
-            const uint32_t at = tmem + ((uint32_t)quad << 21) + acc * 256;
-            for (int c = 0; c < left; c += 16) {
-                uint32_t r[16];
-                tc5::tmem_ld16(at + c, r);
-                tc5::tmem_ld_wait();
-                uint16_t* y = A.y + (int64_t)(t0 + c) * A.ldy + o;
-#pragma unroll
-                for (int j = 0; j < 16; ++j) {
-                    if (c + j < left && real)
-                        y[j * A.ldy] = scaled<DT>((int)r[j], __ldg(A.xs + t0 + c + j), ws, bias, A.bias != nullptr);
-                }
-            }
+            if (row0 < A.n)
+                store_rows<DT>(tmem + ((uint32_t)quad << 21) + acc * 256, upper * 128, upper * 128 + 128, sb, A.bias != nullptr, xs, real,
+                               A.y + (int64_t)t * A.ldy + o0, left, A.wide);
             tc5::fence_before_sync();
             __syncwarp();
             if (lane == 0) tc5::mbar_arrive_remote(acc_empty + acc, 0);
@@ -348,47 +333,47 @@ matmul_i8_pair_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_con
     if (warp == 1) tc5::tmem_free<2>(tmem, 512);
 }
 
-template <int DT, int BN>
-static cmpq_status launch_split(const CUtensorMap& wmap, const CUtensorMap& xmap, ProductArgs a, bool behind, cudaStream_t st) {
-    constexpr int kStage = (128 + BN) * 128;
-    constexpr size_t kSplitSmem = BN == 128 ? 200 << 10 : 112 << 10;  // two CTAs share an SM, or one has it
-    const int64_t tiles = (int64_t)a.m_tiles * a.n_tiles;
-    // as many CTAs as find room at once, at least two blocks of the sum each
-    const int want = (int)std::max<int64_t>(1, std::min<int64_t>(8, ((BN == 128 ? 1 : 2) * sm_count() / tiles)));
-    a.per = std::max((a.kblocks + want - 1) / want, std::min(2, a.kblocks));
-    const int splits = (a.kblocks + a.per - 1) / a.per;
-    const size_t parts = splits > 1 ? (size_t)(BN + splits - 1) / splits * splits * 512 : 0;
-    a.stages = std::min({(int)((kSplitSmem - 1024 - parts) / kStage), kMmMaxStages, std::max(a.per, 1)});
-    const size_t smem = a.stages * kStage + parts + 1024;
-    static bool raised[64];
-    if (!raise_smem_limit_once(matmul_i8_split_kernel<DT, BN>, kSplitSmem, raised)) return CMPQ_ERR_CUDA;
-    if (tiles * splits > INT32_MAX) return CMPQ_ERR_UNSUPPORTED;
-    return launch_cluster(matmul_i8_split_kernel<DT, BN>, (unsigned)(tiles * splits), kMmThreads, smem, splits, behind, st, wmap, xmap, a, splits);
+// Cycles that a way to cover the product would take, as far as sizes tell: rounds of blocks over the SMs times blocks of
+// the sum times the longer of the products' time and the loads'.
+static int64_t tile_cycles(const ProductArgs& a, int bn) {
+    const int64_t blocks = (int64_t)((a.n + 127) / 128) * ((a.d_out + bn - 1) / bn), sms = sm_count();
+    const int64_t products = 4 * std::max(32, bn / 2), loads = (bn + std::min(a.n, 128)) * 128 / 48;
+    return (blocks + sms - 1) / sms * a.kblocks * std::max(products, loads) + 40 * bn;
+}
+static int64_t pair_cycles(const ProductArgs& a) {
+    const int64_t tiles = (int64_t)((a.n + 255) / 256) * ((a.d_out + 255) / 256), pairs = sm_count() / 2;
+    return (tiles + pairs - 1) / pairs * a.kblocks * 600 + 8000;
 }
 
 template <int DT>
 static cmpq_status launch_product(const int8_t* xc, int64_t ldxc, const int8_t* wc, int64_t ldwc, int64_t d_in, ProductArgs a, bool behind,
                                   cudaStream_t st) {
     a.kblocks = (int)((d_in + 127) / 128);
-    const int64_t pairs = (int64_t)((a.d_out + 255) / 256) * ((a.n + 255) / 256);
+    a.wide = aligned_to(a.y, 16) && a.ldy % 8 == 0;
+    a.bn = 32;
+    for (int bn = 48; bn <= 256; bn += 16)
+        if (tile_cycles(a, bn) < tile_cycles(a, a.bn)) a.bn = bn;
+    const bool pair = a.n > 128 && pair_cycles(a) < tile_cycles(a, a.bn);
+    a.rows = pair ? 128 : std::min(128, (a.n + 7) / 8 * 8);
     CUtensorMap wmap, xmap;
-    const bool pair = a.n > 128 && pairs * 4 >= sm_count();
-    const int bn = pair ? 128 : a.n <= 16 ? 16 : a.n <= 32 ? 32 : a.n <= 64 ? 64 : 128;
-    if (!make_byte_map(&wmap, wc, a.d_out, d_in, ldwc, 128) || !make_byte_map(&xmap, xc, a.n, d_in, ldxc, bn)) return CMPQ_ERR_CUDA;
+    if (!make_byte_map(&wmap, wc, a.d_out, d_in, ldwc, pair ? 128 : a.bn) || !make_byte_map(&xmap, xc, a.n, d_in, ldxc, a.rows)) return CMPQ_ERR_CUDA;
     if (pair) {
-        a.n_tiles = (a.n + 255) / 256, a.m_tiles = (a.d_out + 255) / 256;
+        a.m_tiles = (a.n + 255) / 256, a.n_tiles = (a.d_out + 255) / 256;
         static bool raised[64];
         if (!raise_smem_limit_once(matmul_i8_pair_kernel<DT>, kPairSmem, raised)) return CMPQ_ERR_CUDA;
-        return launch_cluster(matmul_i8_pair_kernel<DT>, 2 * (unsigned)std::min<int64_t>(pairs, sm_count() / 2), kMmThreads, kPairSmem, 2, behind, st,
+        const int64_t tiles = (int64_t)a.m_tiles * a.n_tiles;
+        return launch_cluster(matmul_i8_pair_kernel<DT>, 2 * (unsigned)std::min<int64_t>(tiles, sm_count() / 2), kMmThreads, kPairSmem, 2, behind, st,
                               wmap, xmap, a);
     }
-    a.n_tiles = (a.n + bn - 1) / bn, a.m_tiles = (a.d_out + 127) / 128;
-    switch (bn) {
-        case 16: return launch_split<DT, 16>(wmap, xmap, a, behind, st);
-        case 32: return launch_split<DT, 32>(wmap, xmap, a, behind, st);
-        case 64: return launch_split<DT, 64>(wmap, xmap, a, behind, st);
-        default: return launch_split<DT, 128>(wmap, xmap, a, behind, st);
-    }
+    a.m_tiles = (a.n + 127) / 128, a.n_tiles = (a.d_out + a.bn - 1) / a.bn;
+    // shared memory of one block, or of one of two that share an SM where there are more blocks than SMs
+    const int64_t blocks = (int64_t)a.m_tiles * a.n_tiles;
+    const size_t room = (blocks > sm_count() ? 110 : 200) << 10, stage = (128 + a.bn) * 128;
+    a.stages = std::min({(int)((room - 1024) / stage), kMmMaxStages, a.kblocks});
+    static bool raised[64];
+    if (!raise_smem_limit_once(matmul_i8_tile_kernel<DT>, 200 << 10, raised)) return CMPQ_ERR_CUDA;
+    if (blocks > INT32_MAX) return CMPQ_ERR_UNSUPPORTED;
+    return launch_cluster(matmul_i8_tile_kernel<DT>, (unsigned)blocks, kMmThreads, a.stages * stage + 1024, 1, behind, st, wmap, xmap, a);
 }
 
 size_t linear_i8_codes_bytes(int64_t n, int64_t d_in) { return round_up((size_t)n * round_up(d_in, 16), 256); }
