@@ -21,16 +21,20 @@ __device__ __forceinline__ uint32_t group_max(uint4 g) {
     return m;
 }
 
+// Codes of eight entries.  |x * inv| is at most 127 (1 + 2^-22) here, so adding 1.5 * 2^23 leaves the integer that
+// rounding to even gives in the sum's low byte, in two's complement: one addition instead of a conversion (the
+// conversions have a quarter of the rate of an addition, and were what 4096 x 8192 tokens waited for).
 template <int DT>
 __device__ __forceinline__ uint2 group_codes(uint4 g, float inv) {
     const uint32_t w[4] = {g.x, g.y, g.z, g.w};
-    uint32_t c[2] = {0u, 0u};
+    uint32_t c[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const float2 f = widen16x2<DT>(w[i]);
-        c[i >> 1] |= (code_of(f.x, inv) | code_of(f.y, inv) << 8) << (16 * (i & 1));
+        const float a = f.x * inv + 12582912.0f, b = f.y * inv + 12582912.0f;  // two roundings each: -fmad=false
+        c[i] = __byte_perm(__float_as_uint(a), __float_as_uint(b), 0x0040);
     }
-    return make_uint2(c[0], c[1]);
+    return make_uint2(__byte_perm(c[0], c[1], 0x5410), __byte_perm(c[2], c[3], 0x5410));
 }
 
 // One block per token.  The magnitudes are compared as bit patterns, where a NaN is larger than infinity and
@@ -99,7 +103,8 @@ struct ProductArgs {
 };
 
 constexpr int kMmThreads = 320;  // a warp for the loads, one for the products, eight for the epilogue
-constexpr int kMmMaxStages = 12;
+constexpr int kMmMaxStages = 40;
+constexpr size_t kTileSmem = 208 << 10;
 
 // Columns [c0, c1) of a warp's 32 accumulator rows: fl16(fl(fl(sum * xs) * ws) + bias) into y + column, of which `left`
 // exist.  c0 and c1 are multiples of 16; scale_bias holds (ws, bias) of the tile's columns.
@@ -131,8 +136,10 @@ __device__ __forceinline__ void store_rows(uint32_t tmem, int c0, int c1, const 
 
 // Few tiles: a block takes 128 tokens (all of them, mostly) and `bn` channels, a multiple of 16 chosen so that the
 // blocks fill the SMs; the weights pass through once and are the time while tokens are few.  Launched behind the
-// quantization of its tokens, a block asks for its first weights before that has ended.  Rows of the token tile that do
-// not exist are not loaded: what the shared memory holds there only reaches accumulator rows that are not stored.
+// quantization of its tokens, a block asks for its first weights before that has ended.  A stage holds the
+// token rows that exist (to eight) and the channels'; the product reads on past those rows into whatever follows, which
+// only reaches accumulator rows that are not stored, and 16 KB behind the last stage are kept for it.  With that one
+// token's weights have some 30 stages on their way (11008 -> 4096: see the measured times below).
 template <int DT>
 __global__ void __launch_bounds__(kMmThreads)
 matmul_i8_tile_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__ CUtensorMap xmap,
@@ -145,13 +152,10 @@ matmul_i8_tile_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_con
     __shared__ int failed;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int nt = blockIdx.x / A.m_tiles, mt = blockIdx.x % A.m_tiles, bn = A.bn;
-    const int stage = (128 + bn) * 128, columns = bn <= 32 ? 32 : bn <= 64 ? 64 : bn <= 128 ? 128 : 256;
-    if (threadIdx.x == 0) {
-        for (int i = 0; i < A.stages; ++i) tc5::mbar_init(full + i, 1), tc5::mbar_init(empty + i, 1);
-        tc5::mbar_init(&done, 1);
-        failed = 0;
-        tc5::mbar_init_fence();
-    }
+    const int a_bytes = A.rows * 128, stage = a_bytes + bn * 128, columns = bn <= 32 ? 32 : bn <= 64 ? 64 : bn <= 128 ? 128 : 256;
+    if (threadIdx.x < A.stages) tc5::mbar_init(full + threadIdx.x, 1), tc5::mbar_init(empty + threadIdx.x, 1);
+    if (threadIdx.x == 0) tc5::mbar_init(&done, 1), failed = 0;
+    tc5::mbar_init_fence();
     if (warp == 1) tc5::tmem_alloc<1>(&tmem_at, columns);
     tc5::fence_before_sync();
     __syncthreads();
@@ -159,19 +163,11 @@ matmul_i8_tile_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_con
     const uint32_t tmem = tmem_at;
     if (warp == 0) {
         if (tc5::elect_one()) {
-            const int first = min(A.kblocks, A.stages), bytes = (A.rows + bn) * 128;
-            for (int i = 0; i < first; ++i) {
-                tc5::mbar_expect_tx(full + i, bytes);
-                tc5::tma_load_2d(smem + i * stage + 128 * 128, &wmap, full + i, i * 128, nt * bn);
-            }
-            tc5::wait_for_previous();
-            for (int i = 0; i < first; ++i) tc5::tma_load_2d(smem + i * stage, &xmap, full + i, i * 128, mt * 128);
-            int slot = 0, phase = 0;
-            for (int i = first; i < A.kblocks; ++i) {
+            int slot = 0, phase = 1;  // a new barrier counts as empty
+            for (int i = 0; i < A.kblocks; ++i) {
                 if (!tc5::mbar_wait(empty + slot, phase, &failed)) break;
-                tc5::mbar_expect_tx(full + slot, bytes);
-                tc5::tma_load_2d(smem + slot * stage + 128 * 128, &wmap, full + slot, i * 128, nt * bn);
-                tc5::tma_load_2d(smem + slot * stage, &xmap, full + slot, i * 128, mt * 128);
+                tc5::mbar_expect_tx(full + slot, stage);  // the tokens' bytes too, whoever comes first
+                tc5::tma_load_2d(smem + slot * stage + a_bytes, &wmap, full + slot, i * 128, nt * bn);
                 if (++slot == A.stages) slot = 0, phase ^= 1;
             }
         }
@@ -183,7 +179,7 @@ matmul_i8_tile_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_con
                 if (!tc5::mbar_wait(full + slot, phase, &failed)) break;
                 tc5::fence_after_sync();
                 const uint32_t at = tc5::smem_addr(smem + slot * stage);
-                const uint64_t a = tc5::desc_k_sw128(at), b = tc5::desc_k_sw128(at + 128 * 128);
+                const uint64_t a = tc5::desc_k_sw128(at), b = tc5::desc_k_sw128(at + a_bytes);
 #pragma unroll
                 for (int k = 0; k < 4; ++k) tc5::mma_i8<1>(tmem, a + 2 * k, b + 2 * k, idesc, (i | k) != 0);
                 tc5::mma_commit(empty + slot);
@@ -198,7 +194,18 @@ matmul_i8_tile_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_con
             const int o = min(o0 + i, A.d_out - 1);
             sb[i] = make_float2(__ldg(A.ws + o), A.bias ? widen16<DT>(A.bias[o]) : 0.0f);
         }
-        tc5::wait_for_previous();  // the tokens' scales
+        tc5::wait_for_previous();
+        if (warp == 2) {  // the token codes: the first epilogue warp's work until then
+            if (tc5::elect_one()) {
+                int slot = 0, phase = 1;
+                for (int k = 0; k < A.kblocks; ++k) {
+                    if (!tc5::mbar_wait(empty + slot, phase, &failed)) break;
+                    tc5::tma_load_2d(smem + slot * stage, &xmap, full + slot, k * 128, mt * 128);
+                    if (++slot == A.stages) slot = 0, phase ^= 1;
+                }
+            }
+            __syncwarp();
+        }
         const int quad = warp & 3, t = mt * 128 + quad * 32 + lane, half = (bn / 16 + 1) / 2 * 16;
         const bool real = t < A.n, upper = warp >= 6;
         const float xs = real ? __ldg(A.xs + t) : 0.0f;
@@ -333,16 +340,18 @@ matmul_i8_pair_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_con
     if (warp == 1) tc5::tmem_free<2>(tmem, 512);
 }
 
-// Cycles that a way to cover the product would take, as far as sizes tell: rounds of blocks over the SMs times blocks of
-// the sum times the longer of the products' time and the loads'.
+// Cycles that a way to cover the product takes, from sizes: rounds of blocks over the SMs, in each the blocks of the sum
+// at the pace of the products or of the loads (64 bytes a cycle and SM), and what a round or launch costs besides; not
+// less than the weights' way from memory (3400 bytes a cycle).  Fitted to sweeps of bn over 1 to 512 tokens and layers of
+// 4096 x 4096 to 8192 x 28672; e.g. 256 x 4096 x 11008: bn = 160 17.9 us, 80 22.7, pairs 21.6; 4096 x 8192 x 28672: pairs.
 static int64_t tile_cycles(const ProductArgs& a, int bn) {
     const int64_t blocks = (int64_t)((a.n + 127) / 128) * ((a.d_out + bn - 1) / bn), sms = sm_count();
-    const int64_t products = 4 * std::max(32, bn / 2), loads = (bn + std::min(a.n, 128)) * 128 / 48;
-    return (blocks + sms - 1) / sms * a.kblocks * std::max(products, loads) + 40 * bn;
+    const int64_t rounds = (blocks + sms - 1) / sms, pace = std::max(4 * std::max(32, bn / 2), (bn + std::min(a.n, 128)) * 2);
+    return std::max<int64_t>(rounds * a.kblocks * pace, (int64_t)a.kblocks * 128 * a.d_out / 3400) + rounds * (9000 + 8 * bn);
 }
 static int64_t pair_cycles(const ProductArgs& a) {
     const int64_t tiles = (int64_t)((a.n + 255) / 256) * ((a.d_out + 255) / 256), pairs = sm_count() / 2;
-    return (tiles + pairs - 1) / pairs * a.kblocks * 600 + 8000;
+    return (tiles + pairs - 1) / pairs * a.kblocks * 600 + 14000;
 }
 
 template <int DT>
@@ -366,14 +375,14 @@ static cmpq_status launch_product(const int8_t* xc, int64_t ldxc, const int8_t* 
                               wmap, xmap, a);
     }
     a.m_tiles = (a.n + 127) / 128, a.n_tiles = (a.d_out + a.bn - 1) / a.bn;
-    // shared memory of one block, or of one of two that share an SM where there are more blocks than SMs
+    // one block to an SM: two that share it were slower at every size, their rounds and tails cost more than they hide
     const int64_t blocks = (int64_t)a.m_tiles * a.n_tiles;
-    const size_t room = (blocks > sm_count() ? 110 : 200) << 10, stage = (128 + a.bn) * 128;
-    a.stages = std::min({(int)((room - 1024) / stage), kMmMaxStages, a.kblocks});
+    const size_t stage = (a.rows + a.bn) * 128, slack = (128 - a.rows) * 128 + 1024;
+    a.stages = std::min({(int)((kTileSmem - slack) / stage), kMmMaxStages, a.kblocks});
     static bool raised[64];
-    if (!raise_smem_limit_once(matmul_i8_tile_kernel<DT>, 200 << 10, raised)) return CMPQ_ERR_CUDA;
+    if (!raise_smem_limit_once(matmul_i8_tile_kernel<DT>, kTileSmem, raised)) return CMPQ_ERR_CUDA;
     if (blocks > INT32_MAX) return CMPQ_ERR_UNSUPPORTED;
-    return launch_cluster(matmul_i8_tile_kernel<DT>, (unsigned)blocks, kMmThreads, a.stages * stage + 1024, 1, behind, st, wmap, xmap, a);
+    return launch_cluster(matmul_i8_tile_kernel<DT>, (unsigned)blocks, kMmThreads, a.stages * stage + slack, 1, behind, st, wmap, xmap, a);
 }
 
 size_t linear_i8_codes_bytes(int64_t n, int64_t d_in) { return round_up((size_t)n * round_up(d_in, 16), 256); }
