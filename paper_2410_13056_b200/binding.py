@@ -471,13 +471,24 @@ def _rows(t, width, name):
     """Leading dimension of a 2-D or 3-D tensor whose rows of `width` elements are contiguous."""
     shape, stride = t.shape, t.stride()
     if len(shape) == 3:
-        ok = stride[2] == 1 and shape[1] * shape[2] == width and (stride[1] == shape[2] or shape[1] == 1)
-    else:
-        ok = len(shape) == 2 and shape[1] == width and (stride[1] == 1 or width == 1)
-    if not ok:
-        raise ValueError("%s needs contiguous rows of %d elements, got shape %s, strides %s"
-                         % (name, width, tuple(shape), stride))
-    return stride[0] if shape[0] > 1 else width
+        n, h, d = shape
+        if h * d == width and (stride[1:] == (d, 1) or (h == 1 and stride[2] == 1)):
+            return stride[0] if n > 1 else width
+    elif len(shape) == 2 and shape[1] == width and (stride[1] == 1 or width == 1):
+        return stride[0] if shape[0] > 1 else width
+    raise ValueError("%s needs contiguous rows of %d elements, got shape %s, strides %s"
+                     % (name, width, tuple(shape), stride))
+
+
+_CODES = {torch.float16: F16, torch.bfloat16: BF16}
+
+
+def _code(t):
+    """dtype_code with one look-up."""
+    code = _CODES.get(t.dtype)
+    if code is None:
+        raise TypeError("expected a float16 or bfloat16 tensor, got %s" % t.dtype)
+    return code
 
 
 def _code_rows(t):
@@ -493,7 +504,7 @@ def cmpq_linear_i8_ws_bytes(n, d_in, d_out):
 def cmpq_quantize_tokens(X, codes, scale, nonfinite=None):
     """codes (int8 [n][d], rows on 16 bytes) and scale (fp32 [n]) of every row of X (fp16/bf16 [n][d])."""
     n, d = X.shape
-    _check(lib().cmpq_quantize_tokens(_at(X), dtype_code(X), n, d, _rows(X, d, "X"), _at(codes), _code_rows(codes),
+    _check(lib().cmpq_quantize_tokens(_at(X), _code(X), n, d, _rows(X, d, "X"), _at(codes), _code_rows(codes),
                                       _at(scale), _at(nonfinite), _on(X)), "cmpq_quantize_tokens")
 
 
@@ -502,7 +513,7 @@ def cmpq_matmul_i8(xc, xs, wc, w_scale, bias, y, ws):
     n, d_in = xc.shape
     d_out = wc.shape[0]
     _check(lib().cmpq_matmul_i8(_at(xc), _code_rows(xc), _at(xs), _at(wc), _code_rows(wc), _at(w_scale), _at(bias),
-                                dtype_code(y), n, d_in, d_out, _at(y), _rows(y, d_out, "y"), _at(ws), ws.numel(),
+                                _code(y), n, d_in, d_out, _at(y), _rows(y, d_out, "y"), _at(ws), ws.numel(),
                                 _on(y)), "cmpq_matmul_i8")
 
 
@@ -510,9 +521,11 @@ def cmpq_linear_i8(X, wc, w_scale, bias, y, ws, nonfinite=None):
     """y = the 8-bit linear layer (wc, w_scale, bias) of X (fp16/bf16 [n][d_in])."""
     n, d_in = X.shape
     d_out = wc.shape[0]
-    _check(lib().cmpq_linear_i8(_at(X), dtype_code(X), n, d_in, _rows(X, d_in, "X"), _at(wc), _code_rows(wc),
-                                _at(w_scale), _at(bias), d_out, _at(y), _rows(y, d_out, "y"), _at(nonfinite), _at(ws),
-                                ws.numel(), _on(X)), "cmpq_linear_i8")
+    st = lib().cmpq_linear_i8(X.data_ptr(), _code(X), n, d_in, _rows(X, d_in, "X"), wc.data_ptr(), _code_rows(wc),
+                              w_scale.data_ptr(), _at(bias), d_out, y.data_ptr(), _rows(y, d_out, "y"), _at(nonfinite),
+                              ws.data_ptr(), ws.numel(), _on(X))
+    if st:
+        raise CmpqError(st, "cmpq_linear_i8")
 
 
 def cmpq_check_cache(word):
@@ -531,7 +544,7 @@ def cmpq_cache_append(cache, batch, k, v, cos=None, sin=None, interleaved=False,
         heads = q.shape[1]
         ldq, ldqo = _rows(q, heads * d, "q"), _rows(q_out, heads * d, "q_out")
     _check(lib().cmpq_cache_append(cache, batch, k.data_ptr(), _rows(k, row, "k"), v.data_ptr(), _rows(v, row, "v"),
-                                   dtype_code(k), _at(cos), _at(sin), n_pos, 2 * half, int(interleaved), _at(q), ldq,
+                                   _code(k), _at(cos), _at(sin), n_pos, 2 * half, int(interleaved), _at(q), ldq,
                                    heads, _at(q_out), ldqo, _at(word), _on(k)), "cmpq_cache_append")
 
 
@@ -541,7 +554,7 @@ def cmpq_cache_read(cache, batch, k_out, v_out, word=None):
     ld = _rows(k_out, row, "k_out")
     if _rows(v_out, row, "v_out") != ld or v_out.dtype != k_out.dtype:
         raise ValueError("k_out and v_out need one row stride and dtype")
-    _check(lib().cmpq_cache_read(cache, batch, dtype_code(k_out), k_out.data_ptr(), v_out.data_ptr(), ld, _at(word),
+    _check(lib().cmpq_cache_read(cache, batch, _code(k_out), k_out.data_ptr(), v_out.data_ptr(), ld, _at(word),
                                  _on(k_out)), "cmpq_cache_read")
 
 
@@ -553,6 +566,6 @@ def cmpq_cache_attention(cache, batch, q, max_new, max_len, scale, causal, windo
     """q, out: [n_tok][n_heads][d] fp16/bf16; lse: fp32 [n_tok][n_heads] or None."""
     heads = q.shape[1]
     row = heads * cache.head_dim
-    _check(lib().cmpq_cache_attention(cache, batch, q.data_ptr(), _rows(q, row, "q"), dtype_code(q), heads, max_new,
+    _check(lib().cmpq_cache_attention(cache, batch, q.data_ptr(), _rows(q, row, "q"), _code(q), heads, max_new,
                                       max_len, scale, int(causal), window, out.data_ptr(), _rows(out, row, "out"),
                                       _at(lse), _at(word), ws.data_ptr(), ws.numel(), _on(q)), "cmpq_cache_attention")

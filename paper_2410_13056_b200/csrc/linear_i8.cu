@@ -7,7 +7,6 @@
 namespace cmpq {
 
 constexpr int kQtThreads = 256;
-constexpr int kQtKeep = 8;  // groups of eight elements a thread keeps in registers between the two passes
 
 template <int DT>
 __device__ __forceinline__ uint32_t group_max(uint4 g) {
@@ -38,9 +37,10 @@ __device__ __forceinline__ uint2 group_codes(uint4 g, float inv) {
 }
 
 // One block per token.  The magnitudes are compared as bit patterns, where a NaN is larger than infinity and
-// infinity larger than every number, so the maximum also tells whether the row is finite.  A thread keeps its
-// first kQtKeep groups in registers (rows of up to 16384 entries are read once); longer rows are read again.
-template <int DT>
+// infinity larger than every number, so the maximum also tells whether the row is finite.  A thread keeps
+// KEEP groups of eight in registers, chosen by the row's length so that more blocks share an SM where rows are short;
+// rows of up to 16384 entries are read once, the rest of a longer one is read again.
+template <int DT, int KEEP>
 __global__ void __launch_bounds__(kQtThreads)
 quantize_tokens_kernel(const uint16_t* __restrict__ X, int64_t d, int64_t ldx, int wide, int8_t* __restrict__ codes,
                        int64_t ldc, float* __restrict__ scale, int32_t* __restrict__ nonfinite) {
@@ -49,17 +49,17 @@ quantize_tokens_kernel(const uint16_t* __restrict__ X, int64_t d, int64_t ldx, i
     int8_t* out = codes + blockIdx.x * ldc;
     const int t = threadIdx.x;
     const int64_t groups = (d + 15) / 16 * 2;  // the codes' padding up to 16 is written too
-    uint4 keep[kQtKeep];
+    uint4 keep[KEEP];
     uint32_t m = 0;
 #pragma unroll
-    for (int i = 0; i < kQtKeep; ++i) {
+    for (int i = 0; i < KEEP; ++i) {
         const int64_t g = t + (int64_t)i * kQtThreads;
         keep[i] = make_uint4(0u, 0u, 0u, 0u);
         if (g < groups) keep[i] = load8(row + 8 * g, d - 8 * g, wide);
     }
 #pragma unroll
-    for (int i = 0; i < kQtKeep; ++i) m = max(m, group_max<DT>(keep[i]));
-    for (int64_t g = t + (int64_t)kQtKeep * kQtThreads; g < groups; g += kQtThreads)
+    for (int i = 0; i < KEEP; ++i) m = max(m, group_max<DT>(keep[i]));
+    for (int64_t g = t + (int64_t)KEEP * kQtThreads; g < groups; g += kQtThreads)
         m = max(m, group_max<DT>(load8(row + 8 * g, d - 8 * g, wide)));
     __shared__ uint32_t part[kQtThreads / 32];
     m = __reduce_max_sync(0xffffffffu, m);
@@ -75,11 +75,11 @@ quantize_tokens_kernel(const uint16_t* __restrict__ X, int64_t d, int64_t ldx, i
         if (m >= 0x7f800000u && nonfinite) atomicOr(nonfinite, 1);
     }
 #pragma unroll
-    for (int i = 0; i < kQtKeep; ++i) {
+    for (int i = 0; i < KEEP; ++i) {
         const int64_t g = t + (int64_t)i * kQtThreads;
         if (g < groups) *reinterpret_cast<uint2*>(out + 8 * g) = group_codes<DT>(keep[i], inv);
     }
-    for (int64_t g = t + (int64_t)kQtKeep * kQtThreads; g < groups; g += kQtThreads)
+    for (int64_t g = t + (int64_t)KEEP * kQtThreads; g < groups; g += kQtThreads)
         *reinterpret_cast<uint2*>(out + 8 * g) = group_codes<DT>(load8(row + 8 * g, d - 8 * g, wide), inv);
 }
 
@@ -410,10 +410,13 @@ extern "C" cmpq_status cmpq_quantize_tokens(const void* X, cmpq_dtype dt, int64_
     const int wide = aligned_to(X, 16) && ldx % 8 == 0;
     const auto* x = static_cast<const uint16_t*>(X);
     auto st = static_cast<cudaStream_t>(stream);
+    const unsigned rows = (unsigned)n;
+    const int64_t keep = (d + 8 * kQtThreads - 1) / (8 * kQtThreads);
+    auto launch = [&](auto kernel) { kernel<<<rows, kQtThreads, 0, st>>>(x, d, ldx, wide, codes, ldc, scale, nonfinite); };
     if (dt == CMPQ_BF16)
-        quantize_tokens_kernel<CMPQ_BF16><<<(unsigned)n, kQtThreads, 0, st>>>(x, d, ldx, wide, codes, ldc, scale, nonfinite);
+        keep <= 2 ? launch(quantize_tokens_kernel<CMPQ_BF16, 2>) : keep <= 4 ? launch(quantize_tokens_kernel<CMPQ_BF16, 4>) : launch(quantize_tokens_kernel<CMPQ_BF16, 8>);
     else
-        quantize_tokens_kernel<CMPQ_F16><<<(unsigned)n, kQtThreads, 0, st>>>(x, d, ldx, wide, codes, ldc, scale, nonfinite);
+        keep <= 2 ? launch(quantize_tokens_kernel<CMPQ_F16, 2>) : keep <= 4 ? launch(quantize_tokens_kernel<CMPQ_F16, 4>) : launch(quantize_tokens_kernel<CMPQ_F16, 8>);
     return launch_status();
 }
 

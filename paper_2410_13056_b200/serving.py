@@ -45,13 +45,9 @@ class Int8Linear:
 
     def _workspace(self, n):
         # one per stream: calls on different streams may overlap
-        key = B._on(self.w_codes)
-        ws = self._ws.get(key)
-        if ws is None or ws[0] < n:
-            ws = (n, torch.empty(B.cmpq_linear_i8_ws_bytes(n, self.d_in, self.d_out), dtype=torch.uint8,
-                                 device=self.w_codes.device))
-            self._ws[key] = ws
-        return ws[1]
+        ws = self._ws[B._on(self.w_codes)] = (n, torch.empty(B.cmpq_linear_i8_ws_bytes(n, self.d_in, self.d_out),
+                                                             dtype=torch.uint8, device=self.w_codes.device))
+        return ws
 
     def __call__(self, x, out=None):
         """x: fp16/bf16 [n][d_in].  Returns out [n][d_out] of x's dtype."""
@@ -65,7 +61,10 @@ class Int8Linear:
         elif out.dtype != x.dtype or tuple(out.shape) != (n, self.d_out):
             raise ValueError("out needs shape [n][%d] and x's dtype" % self.d_out)
         if n:
-            B.cmpq_linear_i8(x, self.w_codes, self.w_scale, self.bias, out, self._workspace(n), self.nonfinite)
+            ws = self._ws.get(B._on(x))
+            if ws is None or ws[0] < n:
+                ws = self._workspace(n)
+            B.cmpq_linear_i8(x, self.w_codes, self.w_scale, self.bias, out, ws[1], self.nonfinite)
         return out
 
 
@@ -87,10 +86,11 @@ class PagedCache8:
             raise ValueError("the cache's tensors need to be contiguous")
         self.k_codes, self.k_scale, self.v_codes, self.v_scale = k_codes, k_scale, v_codes, v_scale
         self.n_pages, self.n_kv, self.page_tokens, self.head_dim = k_codes.shape
-        self.word = torch.zeros(1, dtype=torch.int32, device=k_codes.device)
+        self.device = k_codes.device
+        self.word = torch.zeros(1, dtype=torch.int32, device=self.device)
         self._c = B.Cache(k_codes.data_ptr(), k_scale.data_ptr(), v_codes.data_ptr(), v_scale.data_ptr(), self.n_pages,
                           self.n_kv, self.head_dim, self.page_tokens)
-        self._ws = {}
+        self._ws, self._need = {}, {}
 
     @classmethod
     def empty(cls, n_pages, n_kv, head_dim, page_tokens=64, device="cuda"):
@@ -99,14 +99,16 @@ class PagedCache8:
         return cls(codes[0], scale[0], codes[1], scale[1])
 
     def _batch(self, tok_off, lens, table, n_tok):
-        for name, t, dims in (("tok_off", tok_off, 1), ("lens", lens, 1), ("table", table, 2)):
-            if t.dtype != torch.int32 or t.dim() != dims or not t.is_cuda or (t.stride()[-1] != 1 and t.numel() > 1):
-                raise ValueError("%s needs an int32 CUDA tensor of %d dimensions" % (name, dims))
         n_seq, width = table.shape
-        if tok_off.numel() != n_seq + 1 or lens.numel() != n_seq:
-            raise ValueError("tok_off needs n_seq + 1 entries and table n_seq rows, n_seq = %d" % lens.numel())
-        return B.Batch(tok_off.data_ptr(), lens.data_ptr(), table.data_ptr(), table.stride(0) if n_seq > 1 else width,
-                       n_seq, n_tok)
+        stride = table.stride()
+        if (tok_off.dtype is not torch.int32 or lens.dtype is not torch.int32 or table.dtype is not torch.int32
+                or tok_off.shape != (n_seq + 1,) or lens.shape != (n_seq,)):
+            raise ValueError("tok_off [n_seq + 1], lens [n_seq] and table [n_seq][pages] need to be int32 tensors, got %s, "
+                             "%s, %s" % tuple((t.dtype, tuple(t.shape)) for t in (tok_off, lens, table)))
+        if not (tok_off.is_cuda and lens.is_cuda and table.is_cuda and tok_off.is_contiguous() and lens.is_contiguous()
+                and (stride[1] == 1 or width <= 1)):
+            raise ValueError("tok_off, lens and table need contiguous rows on the GPU")
+        return B.Batch(tok_off.data_ptr(), lens.data_ptr(), table.data_ptr(), stride[0] if n_seq > 1 else width, n_seq, n_tok)
 
     def _heads(self, t, name, heads=None):
         shape = t.shape
@@ -139,8 +141,7 @@ class PagedCache8:
 
     def read(self, tok_off, lens, table, n_tok, dtype=torch.bfloat16):
         """The last tok_off[s+1] - tok_off[s] tokens of every sequence as 16-bit values: k, v [n_tok][n_kv][head_dim]."""
-        shape = (n_tok, self.n_kv, self.head_dim)
-        k, v = self.k_codes.new_empty(shape, dtype=dtype), self.k_codes.new_empty(shape, dtype=dtype)
+        k, v = torch.empty((2, n_tok, self.n_kv, self.head_dim), dtype=dtype, device=self.device).unbind(0)
         B.cmpq_cache_read(self._c, self._batch(tok_off, lens, table, n_tok), k, v, self.word)
         return k, v
 
@@ -160,11 +161,15 @@ class PagedCache8:
             raise ValueError("out needs q's shape and dtype")
         lse = self.k_scale.new_empty((n, heads)) if return_lse else None
         batch = self._batch(tok_off, lens, table, n)
-        need = B.cmpq_cache_attention_ws_bytes(batch.n_seq, n, max_new, max_len, heads, self.n_kv, d)
-        key = B._on(q)  # one work space per stream: calls on different streams may overlap
-        ws = self._ws.get(key)
+        size, stream = (lens.shape[0], n, max_new, max_len, heads), B._on(q)
+        need = self._need.get(size)
+        if need is None:
+            if len(self._need) > 1000:
+                self._need.clear()
+            need = self._need[size] = B.cmpq_cache_attention_ws_bytes(*size, self.n_kv, d)
+        ws = self._ws.get(stream)  # one work space per stream: calls on different streams may overlap
         if ws is None or ws.numel() < need:
-            ws = self._ws[key] = torch.zeros(need, dtype=torch.uint8, device=q.device)  # its counters start at 0
+            ws = self._ws[stream] = torch.zeros(need, dtype=torch.uint8, device=q.device)  # its counters start at 0
         B.cmpq_cache_attention(self._c, batch, q, max_new, max_len, 1.0 / math.sqrt(d) if scale is None else scale,
                                causal, window, out, lse, ws, self.word)
         return (out, lse) if return_lse else out
