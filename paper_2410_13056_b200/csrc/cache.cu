@@ -1,4 +1,6 @@
 // Paged 8-bit cache of keys and values: append with the rotation on the way, and the values read back.
+#include <algorithm>
+
 #include "cache.cuh"
 
 namespace cmpq {
@@ -14,9 +16,10 @@ struct AppendArgs {
     int rot, interleaved, n_heads;
     int wide_k, wide_v, wide_q;
     int32_t* word;
-    int groups;    // groups of eight entries rotate with groups of eight, cosines and sines can be read four at a time
+    int groups;    // rot_dim is a multiple of 16, cosines and sines can be read four at a time
     int few;       // few new tokens a sequence
     int q_tokens, q_heads;  // tokens and heads that a block of the queries takes
+    int kv_heads;           // heads that a block of the keys or values takes
     unsigned kv_blocks;
 };
 
@@ -49,7 +52,7 @@ __device__ __forceinline__ void rotated8(const AppendArgs& A, const uint16_t* ro
         }
         return;
     }
-    if (A.groups) {  // the partners of eight entries are eight neighbouring entries
+    if (half % 8 == 0 && A.groups) {  // the partners of eight entries are eight neighbouring entries
         float g[8], c[8], s[8];
         const bool low = j < half;
         const int jj = low ? j : j - half;
@@ -75,49 +78,69 @@ __device__ __forceinline__ uint4 round8(const float (&f)[8]) {
     return make_uint4(round16x2<DT>(f[0], f[1]), round16x2<DT>(f[2], f[3]), round16x2<DT>(f[4], f[5]), round16x2<DT>(f[6], f[7]));
 }
 
-// Heads [first, last) of the queries of one token.  Where groups of eight rotate with groups of eight, a thread takes such a pair of groups
-// (or a group that has no partner) of every head that is `heads` further on: its cosines and sines are loaded once for
-// all heads, what it reads it alone writes, and several heads' loads are under way together.
+// Sixteen entries of a head as two groups of eight from entries a and b on.  Where rot_dim is a multiple of 16 a thread's
+// unit is closed under the rotation: a group and its partner group (1), or pairs inside the groups (2), or nothing turns.
+struct Unit {
+    int a, b, mode;
+    __device__ __forceinline__ Unit(int u, int rot, bool interleaved) {
+        const int pairs = interleaved ? 0 : rot / 16;
+        a = u < pairs ? 8 * u : (interleaved ? 0 : rot) + 16 * (u - pairs);
+        b = u < pairs ? rot / 2 + 8 * u : a + 8;
+        mode = u < pairs ? 1 : interleaved && 16 * u < rot ? 2 : 0;
+    }
+};
+
+// The unit's entries in fp32, turned.  c, s: cosines and sines 8 u .. of the position, in both modes.
+template <int DT>
+__device__ __forceinline__ void turned(uint4 a, uint4 b, int mode, const float (&c)[8], const float (&s)[8], float (&x)[8], float (&y)[8]) {
+    widen8<DT>(a, x);
+    widen8<DT>(b, y);
+    if (mode == 1) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float p = x[i], q = y[i];
+            x[i] = p * c[i] - q * s[i];
+            y[i] = q * c[i] + p * s[i];
+        }
+    } else if (mode == 2) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float p = x[2 * i], q = x[2 * i + 1], v = y[2 * i], w = y[2 * i + 1];
+            x[2 * i] = p * c[i] - q * s[i];
+            x[2 * i + 1] = q * c[i] + p * s[i];
+            y[2 * i] = v * c[4 + i] - w * s[4 + i];
+            y[2 * i + 1] = w * c[4 + i] + v * s[4 + i];
+        }
+    }
+}
+
+// Heads [first, last) of the queries of one token.  A thread takes a unit of every head that is `heads` further on: its
+// cosines and sines are loaded once for all of them, and what it reads it alone writes.
 template <int DT>
 __device__ __forceinline__ void rotate_queries(const AppendArgs& A, const uint16_t* src, uint16_t* dst, int64_t pos, int first, int last) {
-    const int D = A.c.head_dim, G = D / 8, rot = A.rot, half = rot / 2, tid = threadIdx.x;
+    const int D = A.c.head_dim, G = D / 8, half = A.rot / 2, tid = threadIdx.x;
     if (A.groups && A.wide_q) {
-        const int pairs = A.interleaved ? 0 : rot / 16, units = A.interleaved ? G : G - pairs, heads = (int)blockDim.x / units;
-        const int u = tid % units, h0 = tid / units;
-        if (h0 >= heads) return;
-        if (u < pairs) {
-            float c[8], s[8];
-            load_floats(A.cos + pos * half + 8 * u, c);
-            load_floats(A.sin + pos * half + 8 * u, s);
-#pragma unroll 4
-            for (int h = first + h0; h < last; h += heads) {
-                float x[8], y[8], a[8], b[8];
-                widen8<DT>(*reinterpret_cast<const uint4*>(src + h * D + 8 * u), x);
-                widen8<DT>(*reinterpret_cast<const uint4*>(src + h * D + half + 8 * u), y);
+        const int u = tid % (D / 16), h0 = tid / (D / 16), heads = (int)blockDim.x / (D / 16);
+        const Unit at(u, A.rot, A.interleaved);
+        float c[8], s[8];
+        if (at.mode) load_floats(A.cos + pos * half + 8 * u, c), load_floats(A.sin + pos * half + 8 * u, s);
+        constexpr int kAtOnce = 4;  // heads loaded before the first store: in place the compiler may not move a load past one
+        for (int h = first + h0; h < last; h += kAtOnce * heads) {
+            uint4 p[kAtOnce], q[kAtOnce];
 #pragma unroll
-                for (int i = 0; i < 8; ++i) a[i] = x[i] * c[i] - y[i] * s[i], b[i] = y[i] * c[i] + x[i] * s[i];
-                *reinterpret_cast<uint4*>(dst + h * D + 8 * u) = round8<DT>(a);
-                *reinterpret_cast<uint4*>(dst + h * D + half + 8 * u) = round8<DT>(b);
-            }
-        } else if (A.interleaved && 8 * u < rot) {
-            const float4 c = __ldg(reinterpret_cast<const float4*>(A.cos + pos * half + 4 * u)), s = __ldg(reinterpret_cast<const float4*>(A.sin + pos * half + 4 * u));
-            const float cc[4] = {c.x, c.y, c.z, c.w}, ss[4] = {s.x, s.y, s.z, s.w};
-#pragma unroll 4
-            for (int h = first + h0; h < last; h += heads) {
-                float x[8], a[8];
-                widen8<DT>(*reinterpret_cast<const uint4*>(src + h * D + 8 * u), x);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    a[2 * i] = x[2 * i] * cc[i] - x[2 * i + 1] * ss[i];
-                    a[2 * i + 1] = x[2 * i + 1] * cc[i] + x[2 * i] * ss[i];
+            for (int k = 0; k < kAtOnce; ++k)
+                if (h + k * heads < last) {
+                    p[k] = *reinterpret_cast<const uint4*>(src + (h + k * heads) * D + at.a);
+                    q[k] = *reinterpret_cast<const uint4*>(src + (h + k * heads) * D + at.b);
                 }
-                *reinterpret_cast<uint4*>(dst + h * D + 8 * u) = round8<DT>(a);
-            }
-        } else if (src != dst) {
-            const int j = A.interleaved ? 8 * u : rot + 8 * (u - pairs);
-#pragma unroll 4
-            for (int h = first + h0; h < last; h += heads)
-                *reinterpret_cast<uint4*>(dst + h * D + j) = *reinterpret_cast<const uint4*>(src + h * D + j);
+#pragma unroll
+            for (int k = 0; k < kAtOnce; ++k)
+                if (h + k * heads < last) {
+                    float x[8], y[8];
+                    turned<DT>(p[k], q[k], at.mode, c, s, x, y);
+                    *reinterpret_cast<uint4*>(dst + (h + k * heads) * D + at.a) = round8<DT>(x);
+                    *reinterpret_cast<uint4*>(dst + (h + k * heads) * D + at.b) = round8<DT>(y);
+                }
         }
         return;
     }
@@ -140,85 +163,130 @@ __device__ __forceinline__ void rotate_queries(const AppendArgs& A, const uint16
     }
 }
 
-// The first kv_blocks blocks take (page of a sequence, head, keys or values); the others rotate q_heads heads of
-// the queries of q_tokens tokens.
+// q_heads heads of the queries of q_tokens tokens.
+template <int DT>
+__device__ __forceinline__ void query_block(const AppendArgs& A, int block) {
+    const int32_t* off = A.b.tok_off;
+    const int chunks = (A.n_heads + A.q_heads - 1) / A.q_heads, first = block % chunks * A.q_heads;
+    const int64_t t0 = (int64_t)(block / chunks) * A.q_tokens;
+    int s = block_count(A.b.n_seq, [&](int64_t i) { return off[i] <= t0; });
+    for (int64_t t = t0; t < min(t0 + A.q_tokens, A.b.n_tok); ++t) {
+        while (s < A.b.n_seq && off[s + 1] <= t) ++s;
+        if (s >= A.b.n_seq) return;  // a row past the last sequence
+        const int64_t pos = (int64_t)A.b.lens[s] - off[s + 1] + t;
+        if (pos < 0 || (A.rot && pos >= A.n_pos)) {
+            if (threadIdx.x == 0) report(A.word, kWordTable);
+            continue;
+        }
+        rotate_queries<DT>(A, A.q + t * A.ldq, A.q_out + t * A.ldqo, pos, first, min(A.n_heads, first + A.q_heads));
+    }
+}
+
+template <int DT>
+__global__ void __launch_bounds__(256, 2)
+cache_queries_kernel(const __grid_constant__ AppendArgs A) {
+    query_block<DT>(A, blockIdx.x);
+}
+
+// The page of a sequence that a block fills.
 //
 // The pages of sequence s start at slot tok_off[s] / P + 2 s: n new tokens touch at most (n + 2P - 2) / P pages,
 // and that many slots lie between two neighbouring starts.  So a block finds its sequence from its index alone
 // and the grid needs no length from the device; a slot without a page ends at once.
-//
-// A block reads its new tokens, keeps the first NIT groups of a thread rotated in fp32 registers (all of them for
-// prompts; blocks of one warp, which are for single tokens, read a later row again), agrees on the largest magnitude,
-// and writes codes; earlier codes of the page are touched only when the scale grows.  Each row of a head is D/8 threads
-// of eight entries, so global accesses are 16 bytes (inputs) and 8 bytes (codes), whole lines per row.
+struct Place {
+    int64_t page_id;  // -1: nothing to do
+    int64_t row;      // first new token's row in k and v
+    int64_t pos;      // and its position
+    int held, fresh;  // tokens that the page holds already, new ones
+};
+__device__ __forceinline__ Place place_of(const AppendArgs& A, int64_t slot, bool keys) {
+    const int P = A.c.page_tokens;
+    const int32_t* off = A.b.tok_off;
+    Place p;
+    p.page_id = -1;
+    const int s = block_count(A.b.n_seq - 1, [&](int64_t i) { return off[i] / P + 2 * i <= slot; });
+    const int64_t from = off[s], n = off[s + 1] - from, len = A.b.lens[s], start = len - n;
+    if (n <= 0) return p;
+    if (start < 0 || from < 0 || from + n > A.b.n_tok) {
+        if (threadIdx.x == 0) report(A.word, kWordTable);
+        return p;
+    }
+    const int64_t page = start / P + (slot - (from / P + 2 * (int64_t)s));
+    if (page * P >= len || page < start / P) return p;
+    const int64_t lo = max(start, page * P), hi = min(len, (page + 1) * P);
+    const int id = page < A.b.ld_table ? A.b.table[s * A.b.ld_table + page] : -1;
+    if (id < 0 || id >= A.c.n_pages || (keys && A.rot && hi > A.n_pos)) {
+        if (threadIdx.x == 0) report(A.word, kWordTable);
+        return p;
+    }
+    p.page_id = id;
+    p.row = from + (lo - start);
+    p.pos = lo;
+    p.held = (int)(lo - page * P), p.fresh = (int)(hi - lo);
+    return p;
+}
+
+__device__ __forceinline__ float grown_scale(float before, uint32_t max_bits) {
+    return fmaxf(before, fminf(fmaxf(__uint_as_float(max_bits) * (1.0f / 127.0f), kScaleLo), kScaleHi));
+}
+
+// The page's earlier codes under a scale that has grown.
+__device__ __forceinline__ void scale_again(int8_t* codes, int count, float by) {
+    for (int i = threadIdx.x; i < count / 8; i += blockDim.x) {
+        uint2* p = reinterpret_cast<uint2*>(codes) + i;
+        const uint2 c = *p;
+        float x[8];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            x[e] = (float)(int8_t)(c.x >> (8 * e));
+            x[4 + e] = (float)(int8_t)(c.y >> (8 * e));
+        }
+        *p = codes_of(x, by);
+    }
+}
+
+// Any alignment and rotation.  The first kv_blocks blocks take (page of a sequence, head, keys or values).  Blocks of
+// one warp are for single tokens: no barriers, and the blocks behind rotate the queries, so that a step of generation is
+// one launch.  A block reads its new tokens, keeps the first NIT groups of a thread rotated in fp32 registers, agrees on
+// the largest magnitude and writes codes; later rows of a thread are read again for that.  Each row of a head is D/8
+// threads of eight entries, so global accesses are 16 bytes (inputs) and 8 bytes (codes), whole lines per row.
 template <int DT, int NIT, int THREADS>
 __global__ void __launch_bounds__(THREADS)
 cache_append_kernel(const __grid_constant__ AppendArgs A) {
-    const int D = A.c.head_dim, P = A.c.page_tokens, G = D / 8;
-    const int32_t* off = A.b.tok_off;
-    const int tid = threadIdx.x;
-    if (blockIdx.x >= A.kv_blocks) {
-        const int chunks = (A.n_heads + A.q_heads - 1) / A.q_heads, block = blockIdx.x - A.kv_blocks, first = block % chunks * A.q_heads;
-        const int64_t t0 = (int64_t)(block / chunks) * A.q_tokens;
-        int s = block_count(A.b.n_seq, [&](int64_t i) { return off[i] <= t0; });
-        for (int64_t t = t0; t < min(t0 + A.q_tokens, A.b.n_tok); ++t) {
-            while (s < A.b.n_seq && off[s + 1] <= t) ++s;
-            if (s >= A.b.n_seq) return;  // a row past the last sequence
-            const int64_t pos = (int64_t)A.b.lens[s] - off[s + 1] + t;
-            if (pos < 0 || (A.rot && pos >= A.n_pos)) {
-                if (tid == 0) report(A.word, kWordTable);
-                continue;
-            }
-            rotate_queries<DT>(A, A.q + t * A.ldq, A.q_out + t * A.ldqo, pos, first, min(A.n_heads, first + A.q_heads));
-        }
+    if (THREADS == 32 && blockIdx.x >= A.kv_blocks) {
+        query_block<DT>(A, blockIdx.x - A.kv_blocks);
         return;
     }
+    const int D = A.c.head_dim, P = A.c.page_tokens, G = D / 8, H = A.c.n_kv_heads, tid = threadIdx.x;
     const int g = tid % G, r0 = tid / G, rows_at_once = THREADS / G;
-    const int H = A.c.n_kv_heads;
     const bool is_v = blockIdx.x & 1;
     const int head = (blockIdx.x >> 1) % H;
-    const int64_t slot = (blockIdx.x >> 1) / H;
-    const int s = block_count(A.b.n_seq - 1, [&](int64_t i) { return off[i] / P + 2 * i <= slot; });
-    const int64_t n = off[s + 1] - off[s], len = A.b.lens[s], start = len - n;
-    if (n <= 0) return;
-    if (start < 0 || off[s] < 0 || off[s + 1] > A.b.n_tok) {
-        if (tid == 0) report(A.word, kWordTable);
-        return;
-    }
-    const int64_t page = start / P + (slot - (off[s] / P + 2 * (int64_t)s));
-    if (page * P >= len || page < start / P) return;
-    const int64_t lo = max(start, page * P), hi = min(len, (page + 1) * P);
-    const int id = page < A.b.ld_table ? A.b.table[s * A.b.ld_table + page] : -1;
-    if (id < 0 || id >= A.c.n_pages || (!is_v && A.rot && hi > A.n_pos)) {
-        if (tid == 0) report(A.word, kWordTable);
-        return;
-    }
-    const int64_t at = (int64_t)id * H + head;
-    float* scale = (is_v ? A.c.v_scale : A.c.k_scale) + at;
-    int8_t* codes = (is_v ? A.c.v_codes : A.c.k_codes) + at * P * D;
-    const int held = (int)(lo - page * P), fresh = (int)(hi - lo);
-    const float before = held ? *scale : 0.0f;
-    const int64_t t0 = off[s] + (lo - start), ld = is_v ? A.ldv : A.ldk;
-    const uint16_t* src = (is_v ? A.v : A.k) + t0 * ld + head * D;
+    const Place at = place_of(A, (blockIdx.x >> 1) / H, !is_v);
+    if (at.page_id < 0) return;
+    float* scale = (is_v ? A.c.v_scale : A.c.k_scale) + at.page_id * H + head;
+    int8_t* codes = (is_v ? A.c.v_codes : A.c.k_codes) + (at.page_id * H + head) * P * D;
+    const float before = at.held ? *scale : 0.0f;
+    const int64_t ld = is_v ? A.ldv : A.ldk;
+    const uint16_t* src = (is_v ? A.v : A.k) + at.row * ld + head * D;
 
     auto entries = [&](int r, float (&f)[8]) {
         if (is_v)
             widen8<DT>(load8(src + r * ld + 8 * g, 8, A.wide_v), f);
         else
-            rotated8<DT>(A, src + r * ld, 8 * g, A.wide_k, lo + r, f);
+            rotated8<DT>(A, src + r * ld, 8 * g, A.wide_k, at.pos + r, f);
     };
     float f[NIT][8];
     uint32_t m = 0;
 #pragma unroll
     for (int i = 0; i < NIT; ++i) {
         const int r = r0 + i * rows_at_once;
-        if (r < fresh) {
+        if (r < at.fresh) {
             entries(r, f[i]);
 #pragma unroll
             for (int e = 0; e < 8; ++e) m = max(m, __float_as_uint(f[i][e]) & 0x7fffffffu);
         }
     }
-    for (int r = r0 + NIT * rows_at_once; r < fresh; r += rows_at_once) {
+    for (int r = r0 + NIT * rows_at_once; r < at.fresh; r += rows_at_once) {
         float x[8];
         entries(r, x);
 #pragma unroll
@@ -232,36 +300,104 @@ cache_append_kernel(const __grid_constant__ AppendArgs A) {
 #pragma unroll
         for (int i = 0; i < THREADS / 32; ++i) m = max(m, part[i]);
     }
-    const float step = __uint_as_float(m) * (1.0f / 127.0f);
-    const float after = fmaxf(before, fminf(fmaxf(step, kScaleLo), kScaleHi)), inv = 1.0f / after;
+    const float after = grown_scale(before, m), inv = 1.0f / after;
     __syncwarp();
     if (tid == 0) {
         if (m >= 0x7f800000u) report(A.word, kWordNonfinite);
         *scale = after;
     }
-    if (after > before) {
-        const float again = before * inv;
-        for (int i = tid; i < held * G; i += THREADS) {
-            uint2* p = reinterpret_cast<uint2*>(codes) + i;
-            const uint2 c = *p;
-            float x[8];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                x[e] = (float)(int8_t)(c.x >> (8 * e));
-                x[4 + e] = (float)(int8_t)(c.y >> (8 * e));
-            }
-            *p = codes_of(x, again);
-        }
-    }
+    if (after > before) scale_again(codes, at.held * D, before * inv);
 #pragma unroll
     for (int i = 0; i < NIT; ++i) {
         const int r = r0 + i * rows_at_once;
-        if (r < fresh) *reinterpret_cast<uint2*>(codes + (int64_t)(held + r) * D + 8 * g) = codes_of(f[i], inv);
+        if (r < at.fresh) *reinterpret_cast<uint2*>(codes + (int64_t)(at.held + r) * D + 8 * g) = codes_of(f[i], inv);
     }
-    for (int r = r0 + NIT * rows_at_once; r < fresh; r += rows_at_once) {
+    for (int r = r0 + NIT * rows_at_once; r < at.fresh; r += rows_at_once) {
         float x[8];
         entries(r, x);
-        *reinterpret_cast<uint2*>(codes + (int64_t)(held + r) * D + 8 * g) = codes_of(x, inv);
+        *reinterpret_cast<uint2*>(codes + (int64_t)(at.held + r) * D + 8 * g) = codes_of(x, inv);
+    }
+}
+
+// Prompts: a block takes a page's keys or values of a run of heads, one head after the other, a thread the same unit of
+// 16 entries of NIT rows in each.  The place is looked up and the cosines and sines are read once for all heads, and the
+// next head's entries and scale are on their way while this one's are turned, compared and written.
+template <int DT, int NIT, int THREADS>
+__global__ void __launch_bounds__(THREADS)
+cache_fill_kernel(const __grid_constant__ AppendArgs A) {
+    const int D = A.c.head_dim, P = A.c.page_tokens, U = D / 16, H = A.c.n_kv_heads, tid = threadIdx.x;
+    const int u = tid % U, r0 = tid / U, rows_at_once = THREADS / U;
+    const bool is_v = blockIdx.x & 1;
+    const int chunks = (H + A.kv_heads - 1) / A.kv_heads, first = (blockIdx.x >> 1) % chunks * A.kv_heads, last = min(H, first + A.kv_heads);
+    const Place at = place_of(A, (blockIdx.x >> 1) / chunks, !is_v);
+    if (at.page_id < 0) return;
+    float* scales = (is_v ? A.c.v_scale : A.c.k_scale) + at.page_id * H;
+    int8_t* pages = (is_v ? A.c.v_codes : A.c.k_codes) + at.page_id * H * P * D;
+    const int64_t ld = is_v ? A.ldv : A.ldk;
+    const uint16_t* src = (is_v ? A.v : A.k) + at.row * ld;
+    const Unit unit(u, is_v ? 0 : A.rot, is_v || A.interleaved);
+
+    float c[NIT][8], s[NIT][8];
+    if (unit.mode) {
+#pragma unroll
+        for (int i = 0; i < NIT; ++i) {
+            const int64_t row = (at.pos + min(r0 + i * rows_at_once, at.fresh - 1)) * (A.rot / 2) + 8 * u;
+            load_floats(A.cos + row, c[i]);
+            load_floats(A.sin + row, s[i]);
+        }
+    }
+    uint4 p[NIT], q[NIT];
+    float before = 0.0f;
+    auto fetch = [&](int head) {
+#pragma unroll
+        for (int i = 0; i < NIT; ++i) {
+            const int r = r0 + i * rows_at_once;
+            p[i] = q[i] = make_uint4(0u, 0u, 0u, 0u);
+            if (r < at.fresh) {
+                p[i] = __ldg(reinterpret_cast<const uint4*>(src + r * ld + head * D + unit.a));
+                q[i] = __ldg(reinterpret_cast<const uint4*>(src + r * ld + head * D + unit.b));
+            }
+        }
+        if (at.held) before = scales[head];
+    };
+    __shared__ uint32_t part[2][THREADS / 32];
+    fetch(first);
+    for (int head = first; head < last; ++head) {
+        float x[NIT][8], y[NIT][8];
+        uint32_t m = 0;
+#pragma unroll
+        for (int i = 0; i < NIT; ++i) {
+            turned<DT>(p[i], q[i], unit.mode, c[i], s[i], x[i], y[i]);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) m = max(m, max(__float_as_uint(x[i][e]) & 0x7fffffffu, __float_as_uint(y[i][e]) & 0x7fffffffu));
+        }
+        const float was = before;
+        if (head + 1 < last) fetch(head + 1);
+        m = __reduce_max_sync(0xffffffffu, m);
+        if ((tid & 31) == 0) part[head & 1][tid >> 5] = m;
+        __syncthreads();  // every thread has this head's scale; the other half of `part` is free again after the next one
+#pragma unroll
+        for (int i = 0; i < THREADS / 32; ++i) m = max(m, part[head & 1][i]);
+        const float after = grown_scale(was, m), inv = 1.0f / after;
+        if (tid == 0) {
+            if (m >= 0x7f800000u) report(A.word, kWordNonfinite);
+            scales[head] = after;
+        }
+        int8_t* codes = pages + (int64_t)head * P * D;
+        if (after > was) scale_again(codes, at.held * D, was * inv);
+#pragma unroll
+        for (int i = 0; i < NIT; ++i) {
+            const int r = r0 + i * rows_at_once;
+            if (r >= at.fresh) continue;
+            int8_t* o = codes + (at.held + r) * D;
+            const uint2 a = codes_of(x[i], inv), b = codes_of(y[i], inv);
+            if (unit.mode == 1) {
+                *reinterpret_cast<uint2*>(o + unit.a) = a;
+                *reinterpret_cast<uint2*>(o + unit.b) = b;
+            } else {
+                *reinterpret_cast<uint4*>(o + unit.a) = make_uint4(a.x, a.y, b.x, b.y);
+            }
+        }
     }
 }
 
@@ -335,18 +471,22 @@ cache_read_kernel(const __grid_constant__ ReadArgs A) {
 }
 
 template <int DT>
-static void launch_append(const AppendArgs& a, unsigned blocks, cudaStream_t st) {
+static void launch_append(const AppendArgs& a, unsigned q_blocks, cudaStream_t st) {
+    const unsigned kv = a.kv_blocks;
     if (a.few) {
-        cache_append_kernel<DT, 2, 32><<<blocks, 32, 0, st>>>(a);
+        cache_append_kernel<DT, 2, 32><<<kv + q_blocks, 32, 0, st>>>(a);
         return;
     }
-    switch (a.c.head_dim * a.c.page_tokens / 2048) {  // groups of eight entries per thread of a 256-thread block
-        case 0: case 1: cache_append_kernel<DT, 1, 256><<<blocks, 256, 0, st>>>(a); break;
-        case 2: cache_append_kernel<DT, 2, 256><<<blocks, 256, 0, st>>>(a); break;
-        case 4: cache_append_kernel<DT, 4, 256><<<blocks, 256, 0, st>>>(a); break;
-        case 8: cache_append_kernel<DT, 8, 256><<<blocks, 256, 0, st>>>(a); break;
-        default: cache_append_kernel<DT, 8, 512><<<blocks, 512, 0, st>>>(a); break;
+    if (a.groups && a.wide_k && a.wide_v) {
+        const int units = a.c.head_dim * a.c.page_tokens / 16;
+        if (units <= 256) cache_fill_kernel<DT, 1, 256><<<kv, 256, 0, st>>>(a);
+        else if (units == 512) cache_fill_kernel<DT, 2, 256><<<kv, 256, 0, st>>>(a);
+        else if (units == 1024) cache_fill_kernel<DT, 2, 512><<<kv, 512, 0, st>>>(a);
+        else cache_fill_kernel<DT, 4, 512><<<kv, 512, 0, st>>>(a);
+    } else {
+        cache_append_kernel<DT, 2, 256><<<kv, 256, 0, st>>>(a);
     }
+    if (q_blocks) cache_queries_kernel<DT><<<q_blocks, 256, 0, st>>>(a);
 }
 
 template <int DT>
@@ -399,21 +539,25 @@ extern "C" cmpq_status cmpq_cache_append(const cmpq_cache* cache, const cmpq_bat
     a.wide_v = aligned_to(v, 16) && ldv % 8 == 0;
     a.wide_q = aligned_to(q, 16) && aligned_to(q_out, 16) && ldq % 8 == 0 && ldqo % 8 == 0;
     a.word = word;
-    const int64_t kv = (batch->n_tok / cache->page_tokens + 2 * batch->n_seq) * cache->n_kv_heads * 2;
-    a.groups = rot_dim % (interleaved ? 8 : 16) == 0 && aligned_to(cos, 16) && aligned_to(sin, 16);
+    a.groups = rot_dim % 16 == 0 && aligned_to(cos, 16) && aligned_to(sin, 16);
     // Four new tokens a sequence or fewer: blocks of one warp, without barriers, for a page and head or 16 heads of a
     // query; otherwise all threads that a full page occupies, and the queries of four tokens once that leaves enough blocks.
     a.few = batch->n_tok <= 4 * batch->n_seq;
     a.q_tokens = !a.few && batch->n_tok >= 4096 ? 4 : 1;
     a.q_heads = a.few ? 16 : n_heads;
-    const int64_t blocks = kv + (q ? (batch->n_tok + a.q_tokens - 1) / a.q_tokens * ((n_heads + a.q_heads - 1) / a.q_heads) : 0);
-    if (blocks > INT32_MAX) return CMPQ_ERR_UNSUPPORTED;
+    const int64_t slots = batch->n_tok / cache->page_tokens + 2 * batch->n_seq, heads = cache->n_kv_heads;
+    // as many heads to a block as leave about eight blocks an SM
+    const bool fill = !a.few && a.groups && a.wide_k && a.wide_v;
+    a.kv_heads = fill ? (int)std::max<int64_t>(1, std::min(heads, slots * 2 * heads / (8 * std::max(1, sm_count())))) : 1;
+    const int64_t kv = slots * ((heads + a.kv_heads - 1) / a.kv_heads) * 2;
+    const int64_t q_blocks = q ? (batch->n_tok + a.q_tokens - 1) / a.q_tokens * ((n_heads + a.q_heads - 1) / a.q_heads) : 0;
+    if (kv + q_blocks > INT32_MAX) return CMPQ_ERR_UNSUPPORTED;
     a.kv_blocks = (unsigned)kv;
     auto st = static_cast<cudaStream_t>(stream);
     if (dt == CMPQ_BF16)
-        launch_append<CMPQ_BF16>(a, (unsigned)blocks, st);
+        launch_append<CMPQ_BF16>(a, (unsigned)q_blocks, st);
     else
-        launch_append<CMPQ_F16>(a, (unsigned)blocks, st);
+        launch_append<CMPQ_F16>(a, (unsigned)q_blocks, st);
     return launch_status();
 }
 
