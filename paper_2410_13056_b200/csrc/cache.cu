@@ -124,7 +124,7 @@ __device__ __forceinline__ void rotate_queries(const AppendArgs& A, const uint16
         const Unit at(u, A.rot, A.interleaved);
         float c[8], s[8];
         if (at.mode) load_floats(A.cos + pos * half + 8 * u, c), load_floats(A.sin + pos * half + 8 * u, s);
-        constexpr int kAtOnce = 4;  // heads loaded before the first store: in place the compiler may not move a load past one
+        constexpr int kAtOnce = 2;  // heads loaded before the first store: in place the compiler may not move a load past one
         for (int h = first + h0; h < last; h += kAtOnce * heads) {
             uint4 p[kAtOnce], q[kAtOnce];
 #pragma unroll
@@ -183,7 +183,7 @@ __device__ __forceinline__ void query_block(const AppendArgs& A, int block) {
 }
 
 template <int DT>
-__global__ void __launch_bounds__(256, 2)
+__global__ void __launch_bounds__(256, 4)
 cache_queries_kernel(const __grid_constant__ AppendArgs A) {
     query_block<DT>(A, blockIdx.x);
 }
@@ -235,12 +235,13 @@ __device__ __forceinline__ void scale_again(int8_t* codes, int count, float by) 
     for (int i = threadIdx.x; i < count / 8; i += blockDim.x) {
         uint2* p = reinterpret_cast<uint2*>(codes) + i;
         const uint2 c = *p;
-        float x[8];
+        float x[8], y[4];
+        widen_codes(c.x, y);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            x[e] = (float)(int8_t)(c.x >> (8 * e));
-            x[4 + e] = (float)(int8_t)(c.y >> (8 * e));
-        }
+        for (int e = 0; e < 4; ++e) x[e] = y[e];
+        widen_codes(c.y, y);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[4 + e] = y[e];
         *p = codes_of(x, by);
     }
 }
@@ -455,9 +456,11 @@ cache_read_kernel(const __grid_constant__ ReadArgs A) {
             const uint32_t x[4] = {c[j].x, c[j].y, c[j].z, c[j].w};
             uint32_t w[8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const uint32_t two = x[e >> 1] >> (16 * (e & 1));
-                w[e] = round16x2<DT>((float)(int8_t)two * sc[j], (float)(int8_t)(two >> 8) * sc[j]);
+            for (int e = 0; e < 4; ++e) {
+                float f[4];
+                widen_codes(x[e], f);
+                w[2 * e] = round16x2<DT>(f[0] * sc[j], f[1] * sc[j]);
+                w[2 * e + 1] = round16x2<DT>(f[2] * sc[j], f[3] * sc[j]);
             }
             uint16_t* o = (is_v ? A.v : A.k) + (t0 + j) * A.ldo + h * D + 16 * g;
             if (A.wide) {
@@ -543,7 +546,7 @@ extern "C" cmpq_status cmpq_cache_append(const cmpq_cache* cache, const cmpq_bat
     // Four new tokens a sequence or fewer: blocks of one warp, without barriers, for a page and head or 16 heads of a
     // query; otherwise all threads that a full page occupies, and the queries of four tokens once that leaves enough blocks.
     a.few = batch->n_tok <= 4 * batch->n_seq;
-    a.q_tokens = !a.few && batch->n_tok >= 4096 ? 4 : 1;
+    a.q_tokens = !a.few && batch->n_tok >= 4096 ? 2 : 1;
     a.q_heads = a.few ? 16 : n_heads;
     const int64_t slots = batch->n_tok / cache->page_tokens + 2 * batch->n_seq, heads = cache->n_kv_heads;
     // as many heads to a block as leave about eight blocks an SM

@@ -54,15 +54,24 @@ __device__ __forceinline__ void widen8(uint4 g, float (&f)[8]) {
     }
 }
 
-__device__ __forceinline__ uint32_t code_of(float x, float inv) {
-    return (uint32_t)max(-127, min(127, __float2int_rn(x * inv))) & 0xffu;
+// Codes of entries whose scale may have been cut off at its upper end: clamped, then rounded to even by adding
+// 1.5 * 2^23, which leaves the integer in the sum's low byte (a conversion has a quarter of an addition's rate).  A NaN
+// gives -127.
+__device__ __forceinline__ uint32_t code_bits(float x, float inv) {
+    return __float_as_uint(fminf(fmaxf(x * inv, -127.0f), 127.0f) + 12582912.0f);
+}
+__device__ __forceinline__ uint32_t codes4(float a, float b, float c, float d, float inv) {
+    return __byte_perm(__byte_perm(code_bits(a, inv), code_bits(b, inv), 0x0040), __byte_perm(code_bits(c, inv), code_bits(d, inv), 0x0040), 0x5410);
+}
+__device__ __forceinline__ uint2 codes_of(const float (&f)[8], float inv) {
+    return make_uint2(codes4(f[0], f[1], f[2], f[3], inv), codes4(f[4], f[5], f[6], f[7], inv));
 }
 
-__device__ __forceinline__ uint2 codes_of(const float (&f)[8], float inv) {
-    uint2 c;
-    c.x = code_of(f[0], inv) | code_of(f[1], inv) << 8 | code_of(f[2], inv) << 16 | code_of(f[3], inv) << 24;
-    c.y = code_of(f[4], inv) | code_of(f[5], inv) << 8 | code_of(f[6], inv) << 16 | code_of(f[7], inv) << 24;
-    return c;
+// Four codes as floats: 0x4b000000 | u is 2^23 + u.
+__device__ __forceinline__ void widen_codes(uint32_t c, float (&f)[4]) {
+    const uint32_t u = c ^ 0x80808080u;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) f[e] = __uint_as_float(__byte_perm(u, 0x4b000000u, 0x7440 + e)) - 8388736.0f;
 }
 
 // The number of i in [1, last] with `below(i)`, for a predicate that holds up to some i and not after it; every
