@@ -18,8 +18,7 @@ struct AppendArgs {
     int32_t* word;
     int groups;    // rot_dim is a multiple of 16, cosines and sines can be read four at a time
     int few;       // few new tokens a sequence
-    int q_tokens, q_heads;  // tokens and heads that a block of the queries takes
-    int kv_heads;           // heads that a block of the keys or values takes
+    int q_heads, kv_heads;  // heads that a block of the queries, of the keys or values takes
     unsigned kv_blocks;
 };
 
@@ -163,29 +162,69 @@ __device__ __forceinline__ void rotate_queries(const AppendArgs& A, const uint16
     }
 }
 
-// q_heads heads of the queries of q_tokens tokens.
+// q_heads heads of the queries of a token.
 template <int DT>
 __device__ __forceinline__ void query_block(const AppendArgs& A, int block) {
     const int32_t* off = A.b.tok_off;
     const int chunks = (A.n_heads + A.q_heads - 1) / A.q_heads, first = block % chunks * A.q_heads;
-    const int64_t t0 = (int64_t)(block / chunks) * A.q_tokens;
-    int s = block_count(A.b.n_seq, [&](int64_t i) { return off[i] <= t0; });
-    for (int64_t t = t0; t < min(t0 + A.q_tokens, A.b.n_tok); ++t) {
-        while (s < A.b.n_seq && off[s + 1] <= t) ++s;
-        if (s >= A.b.n_seq) return;  // a row past the last sequence
-        const int64_t pos = (int64_t)A.b.lens[s] - off[s + 1] + t;
-        if (pos < 0 || (A.rot && pos >= A.n_pos)) {
-            if (threadIdx.x == 0) report(A.word, kWordTable);
-            continue;
-        }
-        rotate_queries<DT>(A, A.q + t * A.ldq, A.q_out + t * A.ldqo, pos, first, min(A.n_heads, first + A.q_heads));
+    const int64_t t = block / chunks;
+    const int s = block_count(A.b.n_seq, [&](int64_t i) { return off[i] <= t; });
+    if (s >= A.b.n_seq) return;  // a row past the last sequence
+    const int64_t pos = (int64_t)A.b.lens[s] - off[s + 1] + t;
+    if (pos < 0 || (A.rot && pos >= A.n_pos)) {
+        if (threadIdx.x == 0) report(A.word, kWordTable);
+        return;
     }
+    rotate_queries<DT>(A, A.q + t * A.ldq, A.q_out + t * A.ldqo, pos, first, min(A.n_heads, first + A.q_heads));
 }
 
 template <int DT>
+__global__ void __launch_bounds__(256)
+cache_queries_any_kernel(const __grid_constant__ AppendArgs A) {
+    query_block<DT>(A, blockIdx.x);
+}
+
+// The queries of prompts where units are closed under the rotation: a block to a token, two units of a thread at a time.
+// The first entries, whose place needs no position, are asked for before the sequence is looked up.
+template <int DT>
 __global__ void __launch_bounds__(256, 4)
 cache_queries_kernel(const __grid_constant__ AppendArgs A) {
-    query_block<DT>(A, blockIdx.x);
+    const int D = A.c.head_dim, U = D / 16, half = A.rot / 2, tid = threadIdx.x, u = tid % U, h0 = tid / U, heads = 256 / U;
+    const int32_t* off = A.b.tok_off;
+    const Unit at(u, A.rot, A.interleaved);
+    const int64_t t = blockIdx.x;
+    const uint16_t* src = A.q + t * A.ldq;
+    uint16_t* dst = A.q_out + t * A.ldqo;
+    uint4 p[2], q[2];
+    auto fetch = [&](int h) {
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+            if (h + k * heads < A.n_heads) {
+                p[k] = *reinterpret_cast<const uint4*>(src + (h + k * heads) * D + at.a);
+                q[k] = *reinterpret_cast<const uint4*>(src + (h + k * heads) * D + at.b);
+            }
+    };
+    fetch(h0);
+    const int s = block_count(A.b.n_seq, [&](int64_t i) { return off[i] <= t; });
+    if (s >= A.b.n_seq) return;  // a row past the last sequence
+    const int64_t pos = (int64_t)A.b.lens[s] - off[s + 1] + t;
+    if (pos < 0 || (A.rot && pos >= A.n_pos)) {
+        if (tid == 0) report(A.word, kWordTable);
+        return;
+    }
+    float c[8], sn[8];
+    if (at.mode) load_floats(A.cos + pos * half + 8 * u, c), load_floats(A.sin + pos * half + 8 * u, sn);
+    for (int h = h0; h < A.n_heads; h += 2 * heads) {
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+            if (h + k * heads < A.n_heads) {
+                float a[8], b[8];
+                turned<DT>(p[k], q[k], at.mode, c, sn, a, b);
+                *reinterpret_cast<uint4*>(dst + (h + k * heads) * D + at.a) = round8<DT>(a);
+                *reinterpret_cast<uint4*>(dst + (h + k * heads) * D + at.b) = round8<DT>(b);
+            }
+        fetch(h + 2 * heads);
+    }
 }
 
 // The page of a sequence that a block fills.
@@ -489,7 +528,10 @@ static void launch_append(const AppendArgs& a, unsigned q_blocks, cudaStream_t s
     } else {
         cache_append_kernel<DT, 2, 256><<<kv, 256, 0, st>>>(a);
     }
-    if (q_blocks) cache_queries_kernel<DT><<<q_blocks, 256, 0, st>>>(a);
+    if (q_blocks && a.groups && a.wide_q)
+        cache_queries_kernel<DT><<<q_blocks, 256, 0, st>>>(a);
+    else if (q_blocks)
+        cache_queries_any_kernel<DT><<<q_blocks, 256, 0, st>>>(a);
 }
 
 template <int DT>
@@ -544,16 +586,15 @@ extern "C" cmpq_status cmpq_cache_append(const cmpq_cache* cache, const cmpq_bat
     a.word = word;
     a.groups = rot_dim % 16 == 0 && aligned_to(cos, 16) && aligned_to(sin, 16);
     // Four new tokens a sequence or fewer: blocks of one warp, without barriers, for a page and head or 16 heads of a
-    // query; otherwise all threads that a full page occupies, and the queries of four tokens once that leaves enough blocks.
+    // query; otherwise all threads that a full page occupies, and a block to the queries of a token.
     a.few = batch->n_tok <= 4 * batch->n_seq;
-    a.q_tokens = !a.few && batch->n_tok >= 4096 ? 2 : 1;
     a.q_heads = a.few ? 16 : n_heads;
     const int64_t slots = batch->n_tok / cache->page_tokens + 2 * batch->n_seq, heads = cache->n_kv_heads;
     // as many heads to a block as leave about eight blocks an SM
     const bool fill = !a.few && a.groups && a.wide_k && a.wide_v;
     a.kv_heads = fill ? (int)std::max<int64_t>(1, std::min(heads, slots * 2 * heads / (8 * std::max(1, sm_count())))) : 1;
     const int64_t kv = slots * ((heads + a.kv_heads - 1) / a.kv_heads) * 2;
-    const int64_t q_blocks = q ? (batch->n_tok + a.q_tokens - 1) / a.q_tokens * ((n_heads + a.q_heads - 1) / a.q_heads) : 0;
+    const int64_t q_blocks = q ? batch->n_tok * ((n_heads + a.q_heads - 1) / a.q_heads) : 0;
     if (kv + q_blocks > INT32_MAX) return CMPQ_ERR_UNSUPPORTED;
     a.kv_blocks = (unsigned)kv;
     auto st = static_cast<cudaStream_t>(stream);
