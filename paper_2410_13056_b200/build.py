@@ -7,6 +7,7 @@ _ROOT = os.path.dirname(_PKG)
 CSRC = os.path.join(_PKG, "csrc")
 INCLUDE = os.path.join(_ROOT, "include")
 LIB_PATH = os.path.join(_PKG, "libcmpq.so")
+EXT_PATH = os.path.join(_PKG, "_serving.so")  # marshals the serving calls on torch tensors
 SOURCES = ["api.cu", "stats.cu", "stats_static.cu", "alloc.cu", "lloyd.cu", "lloyd_weighted.cu", "lloyd_hist.cu", "outliers.cu", "pack.cu", "matvec.cu", "transpose.cu", "probe.cu", "lut_store.cu",
            "linear_i8.cu", "cache.cu", "cache_attention.cu", "cache_prefill.cu"]
 NVCC_FLAGS = ["-O3", "-std=c++17", "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo",
@@ -52,7 +53,30 @@ def build(force=False, verbose=False):
         subprocess.run([nvcc, "-shared", "--cudart", "static", "-gencode", "arch=compute_100a,code=sm_100a",
                         "-o", tmp] + objects, check=True)
         os.replace(tmp, LIB_PATH)
+    _build_extension(force)
     return LIB_PATH
+
+
+def _build_extension(force=False):
+    """Compiles csrc/serving_ext.cpp against torch's headers; it links to libcmpq.so next to it."""
+    import sysconfig
+
+    from torch.utils import cpp_extension
+
+    src = os.path.join(CSRC, "serving_ext.cpp")
+    newest = max(os.path.getmtime(src), os.path.getmtime(os.path.join(INCLUDE, "cmpq.h")))
+    if not force and os.path.exists(EXT_PATH) and os.path.getmtime(EXT_PATH) >= newest:
+        return
+    import torch
+
+    libs = os.path.join(os.path.dirname(torch.__file__), "lib")
+    include = [INCLUDE, sysconfig.get_paths()["include"], "/usr/local/cuda/include"] + cpp_extension.include_paths()
+    tmp = EXT_PATH + ".tmp%d" % os.getpid()
+    subprocess.run(["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-w", "-DTORCH_EXTENSION_NAME=_serving",
+                    "-D_GLIBCXX_USE_CXX11_ABI=%d" % torch._C._GLIBCXX_USE_CXX11_ABI]
+                   + [x for d in include for x in ("-I", d)] + [src, "-o", tmp, "-L", _PKG, "-l:libcmpq.so", "-L", libs, "-lc10",
+                   "-lc10_cuda", "-ltorch_cpu", "-ltorch_python", "-Wl,-rpath,$ORIGIN:" + libs], check=True)
+    os.replace(tmp, EXT_PATH)
 
 
 if __name__ == "__main__":

@@ -3,19 +3,25 @@
 `Int8Linear` is a linear layer with 8-bit weight codes, `PagedCache8` a paged cache of keys and values with a scale
 per page and head (append, read back, attend), `AttentionLayer8` the attention block that runs them together: the
 projections, the append with the rotation on the way, the attention over the cache and the output projection.
-Everything is enqueued on the current torch stream; nothing is computed here.
+Everything is enqueued on the current torch stream; nothing is computed here.  The calls of the first two are
+marshalled in C++ (csrc/serving_ext.cpp, built next to the library): wrong shapes and types raise ValueError and
+TypeError, a status of the library CmpqError.
 """
-import math
-
 import torch
 
 from . import binding as B
+from . import build as _build
 
 
-def _need(t, dtype, name, dims):
-    if not t.is_cuda or t.dtype != dtype or t.dim() != dims:
-        raise ValueError("%s needs a %d-dimensional CUDA tensor of %s, got %s %s on %s"
-                         % (name, dims, dtype, tuple(t.shape), t.dtype, t.device))
+def _ext():
+    """The extension module; raises if it was not built (run paper_2410_13056_b200/build.py)."""
+    B.lib()
+    try:
+        from . import _serving
+    except ImportError as e:
+        raise RuntimeError("extension %s is missing or does not load: build it with `python -m paper_2410_13056_b200.build`"
+                           % _build.EXT_PATH) from e
+    return _serving
 
 
 class Int8Linear:
@@ -23,16 +29,10 @@ class Int8Linear:
     w_scale: fp32 [d_out]; bias: fp16/bf16 [d_out] or None (its dtype is then the activations')."""
 
     def __init__(self, w_codes, w_scale, bias=None):
-        _need(w_codes, torch.int8, "w_codes", 2)
-        _need(w_scale, torch.float32, "w_scale", 1)
-        if w_codes.stride(1) != 1 or w_codes.stride(0) % 16 or w_codes.data_ptr() % 16:
-            raise ValueError("w_codes needs rows that start on multiples of 16 bytes")
-        if w_scale.shape[0] != w_codes.shape[0] or (bias is not None and tuple(bias.shape) != (w_codes.shape[0],)):
-            raise ValueError("w_scale and bias need one entry per row of w_codes")
-        self.w_codes, self.w_scale, self.bias = w_codes, w_scale.contiguous(), None if bias is None else bias.contiguous()
+        self._impl = _ext().Linear(w_codes, w_scale, bias)
+        self.w_codes, self.w_scale, self.bias = w_codes, self._impl.w_scale, self._impl.bias
         self.d_out, self.d_in = w_codes.shape
-        self.nonfinite = torch.zeros(1, dtype=torch.int32, device=w_codes.device)
-        self._ws = {}
+        self.nonfinite = self._impl.nonfinite  # bit 0: some token so far held a NaN or an infinity
 
     @classmethod
     def from_weight(cls, weight, bias=None):
@@ -43,29 +43,9 @@ class Int8Linear:
         B.cmpq_quantize_tokens(weight, codes, scale)
         return cls(codes, scale, bias)
 
-    def _workspace(self, n):
-        # one per stream: calls on different streams may overlap
-        ws = self._ws[B._on(self.w_codes)] = (n, torch.empty(B.cmpq_linear_i8_ws_bytes(n, self.d_in, self.d_out),
-                                                             dtype=torch.uint8, device=self.w_codes.device))
-        return ws
-
     def __call__(self, x, out=None):
         """x: fp16/bf16 [n][d_in].  Returns out [n][d_out] of x's dtype."""
-        if x.dim() != 2 or x.shape[1] != self.d_in or not x.is_cuda:
-            raise ValueError("x needs shape [n][%d] on the GPU, got %s on %s" % (self.d_in, tuple(x.shape), x.device))
-        if self.bias is not None and self.bias.dtype != x.dtype:
-            raise TypeError("bias is %s, x is %s" % (self.bias.dtype, x.dtype))
-        n = x.shape[0]
-        if out is None:
-            out = x.new_empty((n, self.d_out))
-        elif out.dtype != x.dtype or tuple(out.shape) != (n, self.d_out):
-            raise ValueError("out needs shape [n][%d] and x's dtype" % self.d_out)
-        if n:
-            ws = self._ws.get(B._on(x))
-            if ws is None or ws[0] < n:
-                ws = self._workspace(n)
-            B.cmpq_linear_i8(x, self.w_codes, self.w_scale, self.bias, out, ws[1], self.nonfinite)
-        return out
+        return self._impl(x, out)
 
 
 class PagedCache8:
@@ -76,21 +56,10 @@ class PagedCache8:
     reports through check()."""
 
     def __init__(self, k_codes, k_scale, v_codes, v_scale):
-        for name, t in (("k_codes", k_codes), ("v_codes", v_codes)):
-            _need(t, torch.int8, name, 4)
-        for name, t in (("k_scale", k_scale), ("v_scale", v_scale)):
-            _need(t, torch.float32, name, 2)
-        if k_codes.shape != v_codes.shape or k_scale.shape != k_codes.shape[:2] or v_scale.shape != k_scale.shape:
-            raise ValueError("codes need shape [n_pages][n_kv][page_tokens][head_dim] and scales [n_pages][n_kv]")
-        if not all(t.is_contiguous() for t in (k_codes, k_scale, v_codes, v_scale)):
-            raise ValueError("the cache's tensors need to be contiguous")
+        self._impl = _ext().Cache(k_codes, k_scale, v_codes, v_scale)
         self.k_codes, self.k_scale, self.v_codes, self.v_scale = k_codes, k_scale, v_codes, v_scale
         self.n_pages, self.n_kv, self.page_tokens, self.head_dim = k_codes.shape
-        self.device = k_codes.device
-        self.word = torch.zeros(1, dtype=torch.int32, device=self.device)
-        self._c = B.Cache(k_codes.data_ptr(), k_scale.data_ptr(), v_codes.data_ptr(), v_scale.data_ptr(), self.n_pages,
-                          self.n_kv, self.head_dim, self.page_tokens)
-        self._ws, self._need = {}, {}
+        self.word = self._impl.word
 
     @classmethod
     def empty(cls, n_pages, n_kv, head_dim, page_tokens=64, device="cuda"):
@@ -98,89 +67,28 @@ class PagedCache8:
         scale = [torch.zeros(n_pages, n_kv, dtype=torch.float32, device=device) for _ in range(2)]
         return cls(codes[0], scale[0], codes[1], scale[1])
 
-    def _batch(self, tok_off, lens, table, n_tok):
-        n_seq, width = table.shape
-        stride = table.stride()
-        if (tok_off.dtype is not torch.int32 or lens.dtype is not torch.int32 or table.dtype is not torch.int32
-                or tok_off.shape != (n_seq + 1,) or lens.shape != (n_seq,)):
-            raise ValueError("tok_off [n_seq + 1], lens [n_seq] and table [n_seq][pages] need to be int32 tensors, got %s, "
-                             "%s, %s" % tuple((t.dtype, tuple(t.shape)) for t in (tok_off, lens, table)))
-        if not (tok_off.is_cuda and lens.is_cuda and table.is_cuda and tok_off.is_contiguous() and lens.is_contiguous()
-                and (stride[1] == 1 or width <= 1)):
-            raise ValueError("tok_off, lens and table need contiguous rows on the GPU")
-        return B.Batch(tok_off.data_ptr(), lens.data_ptr(), table.data_ptr(), stride[0] if n_seq > 1 else width, n_seq, n_tok)
-
-    def _heads(self, t, name, heads=None):
-        shape = t.shape
-        if len(shape) != 3 or shape[2] != self.head_dim or (heads and shape[1] != heads) or not t.is_cuda:
-            raise ValueError("%s needs shape [n_tok][%s][%d] on the GPU, got %s"
-                             % (name, heads or "heads", self.head_dim, tuple(shape)))
-
     def append(self, k, v, tok_off, lens, table, q=None, cos=None, sin=None, interleaved=False, q_out=None):
-        """Writes new tokens' keys (rotated by cos, sin: fp32 [positions][rot_dim / 2]) and values into their pages;
-        returns the rotated queries where q is given."""
-        self._heads(k, "k", self.n_kv)
-        self._heads(v, "v", self.n_kv)
-        if v.dtype != k.dtype or v.shape[0] != k.shape[0]:
-            raise ValueError("k and v need one dtype and token count")
-        if (cos is None) != (sin is None) or (cos is not None and (cos.shape != sin.shape or not cos.is_contiguous()
-                                                                   or not sin.is_contiguous()
-                                                                   or cos.dtype != torch.float32 or sin.dtype != torch.float32)):
-            raise ValueError("cos and sin need to be contiguous fp32 tensors of one shape")
-        if q is not None:
-            self._heads(q, "q")
-            if q.dtype != k.dtype or q.shape[0] != k.shape[0]:
-                raise ValueError("q needs k's dtype and token count")
-            if q_out is None:
-                q_out = q.new_empty(q.shape)
-            elif q_out.shape != q.shape or q_out.dtype != q.dtype:
-                raise ValueError("q_out needs q's shape and dtype")
-        B.cmpq_cache_append(self._c, self._batch(tok_off, lens, table, k.shape[0]), k, v, cos, sin, interleaved, q, q_out,
-                            self.word)
-        return q_out
+        """Writes new tokens' keys (rotated by cos, sin: fp32 [positions][rot_dim / 2]) and values ([n_tok][n_kv][head_dim])
+        into their pages; returns the rotated queries ([n_tok][heads][head_dim]) where q is given."""
+        return self._impl.append(k, v, tok_off, lens, table, q, cos, sin, interleaved, q_out)
 
     def read(self, tok_off, lens, table, n_tok, dtype=torch.bfloat16):
         """The last tok_off[s+1] - tok_off[s] tokens of every sequence as 16-bit values: k, v [n_tok][n_kv][head_dim]."""
-        k, v = torch.empty((2, n_tok, self.n_kv, self.head_dim), dtype=dtype, device=self.device).unbind(0)
-        B.cmpq_cache_read(self._c, self._batch(tok_off, lens, table, n_tok), k, v, self.word)
-        return k, v
+        if dtype not in (torch.float16, torch.bfloat16):
+            raise TypeError("expected float16 or bfloat16, got %s" % dtype)
+        return self._impl.read(tok_off, lens, table, n_tok, dtype is torch.bfloat16)
 
     def attend(self, q, tok_off, lens, table, max_new, max_len=None, scale=None, causal=True, window=0, out=None,
                return_lse=False):
         """Attention of q [n_tok][heads][head_dim] over the cached tokens.  max_new, max_len: bounds of the new and of
         the cached tokens of a sequence (max_len defaults to what the table can hold)."""
-        self._heads(q, "q")
-        n, heads, d = q.shape
-        if heads % self.n_kv:
-            raise ValueError("%d query heads are no multiple of the cache's %d heads" % (heads, self.n_kv))
-        if max_len is None:
-            max_len = table.shape[1] * self.page_tokens
-        if out is None:
-            out = q.new_empty(q.shape)
-        elif out.shape != q.shape or out.dtype != q.dtype:
-            raise ValueError("out needs q's shape and dtype")
-        lse = self.k_scale.new_empty((n, heads)) if return_lse else None
-        batch = self._batch(tok_off, lens, table, n)
-        size, stream = (lens.shape[0], n, max_new, max_len, heads), B._on(q)
-        need = self._need.get(size)
-        if need is None:
-            if len(self._need) > 1000:
-                self._need.clear()
-            need = self._need[size] = B.cmpq_cache_attention_ws_bytes(*size, self.n_kv, d)
-        ws = self._ws.get(stream)  # one work space per stream: calls on different streams may overlap
-        if ws is None or ws.numel() < need:
-            ws = self._ws[stream] = torch.zeros(need, dtype=torch.uint8, device=q.device)  # its counters start at 0
-        B.cmpq_cache_attention(self._c, batch, q, max_new, max_len, 1.0 / math.sqrt(d) if scale is None else scale,
-                               causal, window, out, lse, ws, self.word)
-        return (out, lse) if return_lse else out
+        result = self._impl.attend(q, tok_off, lens, table, max_new, max_len, scale, causal, window, out, return_lse)
+        return result if return_lse else result[0]
 
     def check(self):
         """Waits for the current stream and raises CmpqError if a call so far met a NaN or an infinity (status 6) or
         lengths and tables that do not fit (status 1); forgets what it reported."""
-        try:
-            B.cmpq_check_cache(self.word)
-        finally:
-            self.word.zero_()
+        self._impl.check()
 
 
 class AttentionLayer8:
