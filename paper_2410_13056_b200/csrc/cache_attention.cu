@@ -256,6 +256,72 @@ attention_rows_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_con
 #pragma unroll
             for (int e = 0; e < 2; ++e) row_pos[nt][e] = p.len - p.n + (rb * kR + nt * 8 + 2 * c + e) / g;
 
+        // Pages are looked up 32 at a time, one per lane.  The first tiles are asked for as soon as their pages are known;
+        // the queries and the pages' scales are fetched under way.
+        const int page0 = ((p.tile0 + live_from) * kTile) >> page_bits;
+        const int page_end = (p.len + P - 1) >> page_bits;
+        int my_page = -1, have = 0;  // pages page0 .. page0 + have are known
+        auto fetch_pages = [&]() {
+            const int page = page0 + have + lane;
+            my_page = -1;
+            if (page < page_end) {
+                my_page = page < A.b.ld_table ? __ldg(A.b.table + s * A.b.ld_table + page) : -1;
+                if (my_page < 0 || my_page >= A.c.n_pages) {
+                    my_page = -1;
+                    if (A.word) atomicOr(A.word, kWordTable);
+                }
+            }
+            have += 32;
+        };
+        auto fetch_scales = [&]() {  // of the pages looked up last
+            float2 sc = make_float2(0.0f, 0.0f);
+            if (my_page >= 0) {
+                const int64_t at = (int64_t)my_page * H + head;
+                sc = make_float2(__ldg(A.c.k_scale + at), __ldg(A.c.v_scale + at));
+            }
+            page_scale[warp][(have - 32 + lane) & 63] = sc;
+            __syncwarp();
+        };
+        auto ask = [&](int t, int which) {  // keys (0) or values (1) of tile t of the unit
+            const int token = (p.tile0 + t) * kTile;
+            const int page = (token >> page_bits) - page0;
+            if (page >= have) fetch_pages(), fetch_scales();  // 32 pages hold whole tiles
+            constexpr int kLine = D < 128 ? 128 / D : 1;  // tokens per row of the tensor map
+            const int pieces = P < kTile ? kTile >> page_bits : 1, tokens = P < kTile ? P : kTile;
+            const int first_id = __shfl_sync(0xffffffffu, my_page, page & 31);
+            if (pieces == 1) {
+                if (lane == 0) {
+                    uint64_t* bar = &bars[warp][which][next[which]];
+                    uint8_t* to = ring + (which * kBuffers + next[which]) * C::kTileBytes;
+                    tc5::mbar_expect_tx(bar, first_id >= 0 ? C::kTileBytes : 0);
+                    if (first_id >= 0) {
+                        const int row = (int)(((((int64_t)first_id * H + head) << page_bits) + (token & (P - 1))) / kLine);
+#pragma unroll
+                        for (int plane = 0; plane < (D + 127) / 128; ++plane)
+                            tc5::tma_load_2d(to + plane * kTile * 128, which ? &vmap : &kmap, bar, plane * 128, row);
+                    }
+                }
+            } else {
+                // a lane per page: the first lanes look at the pages that follow
+                const int id = __shfl_sync(0xffffffffu, my_page, (page + lane) & 31);
+                const bool mine_too = lane < pieces && id >= 0;
+                const int n = __popc(__ballot_sync(0xffffffffu, mine_too));
+                uint64_t* bar = &bars[warp][which][next[which]];
+                if (lane == 0) tc5::mbar_expect_tx(bar, n * tokens * D);
+                __syncwarp();
+                if (mine_too) {
+                    uint8_t* to = ring + (which * kBuffers + next[which]) * C::kTileBytes + lane * tokens * (D < 128 ? D : 128);
+                    const int row = (int)((((int64_t)id * H + head) << page_bits) / kLine);
+#pragma unroll
+                    for (int plane = 0; plane < (D + 127) / 128; ++plane)
+                        tc5::tma_load_2d(to + plane * kTile * 128, which ? &vmap : &kmap, bar, plane * 128, row);
+                }
+            }
+            if (++next[which] == kBuffers) next[which] = 0;
+        };
+        fetch_pages();
+        for (int t = live_from; t < live_to && t < live_from + kBuffers; ++t) ask(t, 0), ask(t, 1);
+
         // the queries, scaled into fp16
         uint32_t qf[NT][D / 16][2];
         float qs[NT][2];
@@ -303,66 +369,7 @@ attention_rows_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_con
             l[nt][0] = l[nt][1] = 0.0f;
         }
 
-        // Pages are asked for 32 at a time, one per lane, with their scales; lane 0 has the copies of a tile made.
-        const int page0 = ((p.tile0 + live_from) * kTile) >> page_bits;
-        const int page_end = (p.len + P - 1) >> page_bits;
-        int my_page = -1, have = 0;  // pages page0 .. page0 + have are known
-        auto fetch_pages = [&]() {
-            const int page = page0 + have + lane;
-            my_page = -1;
-            float2 sc = make_float2(0.0f, 0.0f);
-            if (page < page_end) {
-                my_page = page < A.b.ld_table ? A.b.table[s * A.b.ld_table + page] : -1;
-                if (my_page < 0 || my_page >= A.c.n_pages) {
-                    my_page = -1;
-                    if (A.word) atomicOr(A.word, kWordTable);
-                } else {
-                    const int64_t at = (int64_t)my_page * H + head;
-                    sc = make_float2(A.c.k_scale[at], A.c.v_scale[at]);
-                }
-            }
-            page_scale[warp][(have + lane) & 63] = sc;
-            have += 32;
-            __syncwarp();
-        };
-        auto ask = [&](int t, int which) {  // keys (0) or values (1) of tile t of the unit
-            const int token = (p.tile0 + t) * kTile;
-            const int page = (token >> page_bits) - page0;
-            if (page >= have) fetch_pages();  // 32 pages hold whole tiles
-            constexpr int kLine = D < 128 ? 128 / D : 1;  // tokens per row of the tensor map
-            const int pieces = P < kTile ? kTile >> page_bits : 1, tokens = P < kTile ? P : kTile;
-            const int first_id = __shfl_sync(0xffffffffu, my_page, page & 31);
-            if (pieces == 1) {
-                if (lane == 0) {
-                    uint64_t* bar = &bars[warp][which][next[which]];
-                    uint8_t* to = ring + (which * kBuffers + next[which]) * C::kTileBytes;
-                    tc5::mbar_expect_tx(bar, first_id >= 0 ? C::kTileBytes : 0);
-                    if (first_id >= 0) {
-                        const int row = (int)(((((int64_t)first_id * H + head) << page_bits) + (token & (P - 1))) / kLine);
-#pragma unroll
-                        for (int plane = 0; plane < (D + 127) / 128; ++plane)
-                            tc5::tma_load_2d(to + plane * kTile * 128, which ? &vmap : &kmap, bar, plane * 128, row);
-                    }
-                }
-            } else {
-                // a lane per page: the first lanes look at the pages that follow
-                const int id = __shfl_sync(0xffffffffu, my_page, (page + lane) & 31);
-                const bool mine_too = lane < pieces && id >= 0;
-                const int n = __popc(__ballot_sync(0xffffffffu, mine_too));
-                uint64_t* bar = &bars[warp][which][next[which]];
-                if (lane == 0) tc5::mbar_expect_tx(bar, n * tokens * D);
-                __syncwarp();
-                if (mine_too) {
-                    uint8_t* to = ring + (which * kBuffers + next[which]) * C::kTileBytes + lane * tokens * (D < 128 ? D : 128);
-                    const int row = (int)((((int64_t)id * H + head) << page_bits) / kLine);
-#pragma unroll
-                    for (int plane = 0; plane < (D + 127) / 128; ++plane)
-                        tc5::tma_load_2d(to + plane * kTile * 128, which ? &vmap : &kmap, bar, plane * 128, row);
-                }
-            }
-            if (++next[which] == kBuffers) next[which] = 0;
-        };
-        for (int t = live_from; t < live_to && t < live_from + kBuffers; ++t) ask(t, 0), ask(t, 1);
+        fetch_scales();
 
         for (int t = live_from; t < live_to; ++t) {
             const int token = (p.tile0 + t) * kTile;
