@@ -56,19 +56,25 @@ __device__ __forceinline__ int64_t seq_tiles(const AttnArgs& A, const SeqPlan& p
     return (int64_t)p.tiles * p.blocks * A.c.n_kv_heads;
 }
 
-// Inclusive sums over the block's threads; `part` has one entry per warp.  Ends behind a barrier.
-__device__ __forceinline__ int64_t block_scan(int64_t v, int64_t* part) {
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+// Inclusive sums over the warp's lanes.
+__device__ __forceinline__ int64_t warp_scan(int64_t v) {
+    const int lane = threadIdx.x & 31;
 #pragma unroll
     for (int d = 1; d < 32; d <<= 1) {
         const int64_t o = __shfl_up_sync(0xffffffffu, v, d);
         if (lane >= d) v += o;
     }
-    if (lane == 31) part[warp] = v;
-    __syncthreads();
-    for (int w = 0; w < warp; ++w) v += part[w];
-    __syncthreads();
     return v;
+}
+// Quotient and remainder of a dividend that nearly always has 32 bits.
+__device__ __forceinline__ int64_t divide(int64_t a, int64_t b, int* rest) {
+    if ((uint64_t)a >> 32 == 0 && (uint64_t)b >> 32 == 0) {
+        const uint32_t q = (uint32_t)a / (uint32_t)b;
+        *rest = (int)((uint32_t)a - q * (uint32_t)b);
+        return q;
+    }
+    *rest = (int)(a % b);
+    return a / b;
 }
 
 __device__ __forceinline__ void mma_f16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
@@ -173,12 +179,10 @@ attention_rows_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_con
     constexpr int kR = C::kR, kTile = C::kTile, kBuffers = C::kBuffers, MT = kTile / 16;
     extern __shared__ uint8_t raw[];
     __shared__ uint64_t bars[C::kWarps][2][kBuffers];
-    __shared__ int64_t scan[C::kWarps];
-    __shared__ int64_t start_base[C::kWarps];
-    __shared__ int start_seq[C::kWarps];
     __shared__ float2 page_scale[C::kWarps][64];  // key and value scales of the last 64 pages asked for
     __shared__ int failed[C::kWarps], is_last;
-    __shared__ Piece pieces[C::kWarps][2];
+    __shared__ Piece pieces[C::kWarps][2], list[2 * C::kWarps];
+    __shared__ int listed;
     uint8_t* smem = raw + ((1024u - (tc5::smem_addr(raw) & 1023u)) & 1023u);
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, r = lane >> 2, c = lane & 3;
     const int H = A.c.n_kv_heads, g = A.group, P = A.c.page_tokens, page_bits = A.page_bits;
@@ -189,42 +193,38 @@ attention_rows_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_con
         tc5::mbar_init_fence();
     }
 
-    // the total, this warp's run, and the sequence it starts in
+    // The total, this warp's run, and the sequence it starts in: every warp for itself, 32 sequences at a time.
     int64_t total = 0, mine = 0, upto = 0;
-    for (int64_t base = 0; base < A.b.n_seq; base += blockDim.x) {
+    for (int64_t at = 0; at < A.b.n_seq; at += 32) {
         mine = 0;
-        if (base + tid < A.b.n_seq) {
-            const SeqPlan p = seq_plan(A, base + tid, kR, kTile);
+        if (at + lane < A.b.n_seq) {
+            const SeqPlan p = seq_plan(A, at + lane, kR, kTile);
             mine = seq_tiles(A, p);
-            if (p.bad && blockIdx.x == 0 && A.word) atomicOr(A.word, kWordTable);
+            if (p.bad && blockIdx.x == 0 && warp == 0 && A.word) atomicOr(A.word, kWordTable);
         }
-        upto = block_scan(mine, scan) + total;
-        if (tid == (int)blockDim.x - 1) start_base[0] = upto;
-        __syncthreads();
-        total = start_base[0];
-        __syncthreads();
+        upto = total + warp_scan(mine);
+        total = __shfl_sync(0xffffffffu, upto, 31);
     }
     const int64_t per = max((int64_t)1, (total + A.workers - 1) / A.workers);
     const int worker = blockIdx.x * C::kWarps + warp;
     const int64_t begin = worker * per, end = min(total, begin + per);
-    int64_t before = 0;
-    for (int64_t base = 0; base < A.b.n_seq; base += blockDim.x) {
-        if (A.b.n_seq > blockDim.x) {  // the sums again, chunk by chunk; of a single chunk they are still there
-            mine = base + tid < A.b.n_seq ? seq_tiles(A, seq_plan(A, base + tid, kR, kTile)) : 0;
-            upto = before + block_scan(mine, scan);
+    int64_t s = 0, base = 0;
+    if (begin < end) {
+        for (int64_t at = 0, before = 0;; at += 32) {
+            if (A.b.n_seq > 32) {  // the sums again; of 32 sequences or fewer they are still there
+                mine = at + lane < A.b.n_seq ? seq_tiles(A, seq_plan(A, at + lane, kR, kTile)) : 0;
+                upto = before + warp_scan(mine);
+                before = __shfl_sync(0xffffffffu, upto, 31);
+            }
+            const unsigned here = __ballot_sync(0xffffffffu, upto - mine <= begin && begin < upto);
+            if (here) {
+                const int l = __ffs(here) - 1;
+                s = at + l, base = __shfl_sync(0xffffffffu, upto - mine, l);
+                break;
+            }
         }
-        const int64_t from = upto - mine;
-#pragma unroll
-        for (int w = 0; w < C::kWarps; ++w) {
-            const int64_t x = (blockIdx.x * C::kWarps + w) * per;
-            if (x < total && from <= x && x < upto) start_seq[w] = (int)(base + tid), start_base[w] = from;
-        }
-        if (tid == (int)blockDim.x - 1) scan[0] = upto;
-        __syncthreads();
-        before = scan[0];
-        __syncthreads();
     }
-    int64_t s = begin < end ? start_seq[warp] : 0, base = begin < end ? start_base[warp] : 0;
+
     uint8_t* ring = smem + warp * C::kRing;  // keys, then values
     volatile int* gave_up = &failed[warp];
     int slot[2] = {0, 0}, phase[2] = {0, 0}, next[2] = {0, 0};  // of the keys and of the values: next to read, to fill
@@ -237,10 +237,10 @@ attention_rows_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_con
             ++s;
             continue;
         }
-        const int64_t unit = (x - base) / p.tiles;
-        const int t_from = (int)((x - base) % p.tiles);
+        int t_from, rb;
+        const int64_t unit = divide(x - base, p.tiles, &t_from);
+        const int head = (int)divide(unit, p.blocks, &rb);
         const int t_to = (int)min((int64_t)p.tiles, t_from + (end - x));  // tiles of this unit that are this worker's
-        const int head = (int)(unit / p.blocks), rb = (int)(unit % p.blocks);
         const int rows = min(kR, p.n * g - rb * kR);
         // positions of the block's first and last query; keys that any of them sees
         const int p0 = p.len - p.n + (rb * kR) / g, p1 = p.len - p.n + (rb * kR + rows - 1) / g;
@@ -583,27 +583,20 @@ attention_rows_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_con
     // Parts of one unit that this block's warps hold, one behind the other, are joined here: into the result if the
     // unit lies in the block's run, otherwise into the block's part.  The block that adds the last of a unit's parts
     // (a counter at the block that began the unit tells) joins those, in the blocks' order, and clears the counter.
+    if (warp == 0) {  // the parts there are, without gaps
+        const Piece* mine_at = &pieces[0][0] + lane;
+        const bool there = lane < 2 * C::kWarps && mine_at->at != nullptr;
+        const unsigned all = __ballot_sync(0xffffffffu, there);
+        if (there) list[__popc(all & ((1u << lane) - 1))] = *mine_at;
+        if (lane == 0) listed = __popc(all);
+    }
+    __syncthreads();
     const int64_t block_run = per * C::kWarps, block_from = blockIdx.x * block_run, block_to = block_from + block_run;
-    for (int first = 0; first < 2 * C::kWarps;) {
-        const Piece& e = (&pieces[0][0])[first];
-        if (e.at == nullptr) {
-            ++first;
-            continue;
-        }
-        int last = first + 1, n = 1;
-        while (last < 2 * C::kWarps) {
-            const Piece& f = (&pieces[0][0])[last];
-            if (f.at != nullptr && f.from != e.from) break;
-            if (f.at != nullptr) ++n;
-            ++last;
-        }
-        const int from_piece = first;
-        auto local = [&](int k) {  // the k-th part of the group
-            int i = from_piece;
-            for (;; ++i)
-                if ((&pieces[0][0])[i].at != nullptr && k-- == 0) break;
-            return (&pieces[0][0])[i].at;
-        };
+    for (int first = 0; first < listed;) {
+        const Piece& e = list[first];
+        int n = 1;
+        while (first + n < listed && list[first + n].from == e.from) ++n;
+        auto local = [&](int k) { return list[first + k].at; };
         const bool complete = e.from >= block_from && e.to <= block_to;
         float* mine_out = A.parts + ((int64_t)blockIdx.x * 2 + (e.from >= block_from)) * C::kPart;
         join_parts<DT, D, kR>(A, e, n, local, complete ? nullptr : mine_out);
@@ -620,7 +613,7 @@ attention_rows_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_con
                 if (tid == 0) A.counters[b0] = 0;
             }
         }
-        first = last;
+        first += n;
     }
 }
 
