@@ -41,5 +41,6 @@ __device__ __forceinline__ uint32_t half_pair(uint32_t u, uint32_t pick) {
 
 // Whole prompts (cache_prefill.cu): head_dim 64 and 128.
 cmpq_status launch_prefill(const AttnArgs& a, cmpq_dtype dt, cudaStream_t st);
+size_t prefill_parts_bytes(int head_dim);  // behind the counters
 
 }  // namespace cmpq

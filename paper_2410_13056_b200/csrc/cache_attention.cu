@@ -4,6 +4,7 @@
 // products run on the tensor cores in fp16 with fp32 accumulation, a page's scale being one factor of its scores (keys)
 // or of its weights (values); a query row is scaled by a power of two into fp16's range first.
 #include <algorithm>
+#include <cmath>
 
 #include "attention.cuh"
 
@@ -17,7 +18,7 @@ namespace cmpq {
 // contiguous runs: sequences of any lengths balance, and a worker meets few unit borders.  A unit inside one worker's
 // run is finished there; the parts of one that is cut go to the work space and are joined by a second kernel in the
 // order of the workers (no atomics: the same bytes every time).
-constexpr int kMaxBlocks = 1024;
+constexpr int kMaxBlocks = 512;  // counters: one per block here, behind them those of the prompts' kernel
 
 template <int D, int NT>
 struct Rows {
@@ -108,19 +109,21 @@ struct Piece {
 };
 
 // Joins n parts (rows of D entries, then maximum and sum of each row) in their order: into `into`, or, where that is
-// null, into the output.  Every thread of the block; a thread takes four entries of a row at a time and eight parts'
-// values are under way together.
+// null, into the output.  Every thread of the block; a thread takes four entries of a row at a time and sixteen parts'
+// values are under way together (eight: 111 instead of 109 us for two streams of up to 131072 tokens, which join 28
+// parts).
 template <int DT, int D, int R, class Part>
 __device__ __forceinline__ void join_parts(const AttnArgs& A, const Piece& u, int n, Part part, float* into) {
+    constexpr int kAtOnce = 16;
     for (int i = threadIdx.x; i < u.rows * (D / 4); i += blockDim.x) {
         const int row = i / (D / 4), d = i % (D / 4) * 4;
         float top = -INFINITY, sum = 0.0f;
         float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-        for (int k = 0; k < n; k += 8) {
-            float2 ml[8];
-            float4 v[8];
+        for (int k = 0; k < n; k += kAtOnce) {
+            float2 ml[kAtOnce];
+            float4 v[kAtOnce];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
+            for (int j = 0; j < kAtOnce; ++j) {
                 ml[j] = make_float2(-INFINITY, 0.0f);
                 v[j] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
                 if (k + j < n) {
@@ -131,12 +134,12 @@ __device__ __forceinline__ void join_parts(const AttnArgs& A, const Piece& u, in
             }
             float most = top;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) most = fmaxf(most, ml[j].x);
+            for (int j = 0; j < kAtOnce; ++j) most = fmaxf(most, ml[j].x);
             const float at = most == -INFINITY ? 0.0f : most, keep = ex2(top - at);
             top = most;
             sum *= keep, o.x *= keep, o.y *= keep, o.z *= keep, o.w *= keep;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
+            for (int j = 0; j < kAtOnce; ++j) {
                 const float f = ex2(ml[j].x - at);
                 sum = fmaf(f, ml[j].y, sum);
                 o.x = fmaf(f, v[j].x, o.x), o.y = fmaf(f, v[j].y, o.y), o.z = fmaf(f, v[j].z, o.z), o.w = fmaf(f, v[j].w, o.w);
@@ -643,11 +646,27 @@ static cmpq_status launch_attention(const AttnArgs& a, cudaStream_t st) {
     return rows <= 8 ? launch_rows<DT, D, 1>(a, st) : launch_rows<DT, D, 2>(a, st);
 }
 
-// The counters, then two parts per block and one per worker, of the kernel that has most.
-static size_t rows_ws_bytes(int d) {
+// Which kernel takes a batch.  Up to 32 rows of a sequence and key-value head the warps that share out the cache, above
+// 128 the one for prompts.  Between, microseconds from sizes (the lengths are taken as 0.6 of the longest unless a window
+// evens them out): warps read a row block of 16 at about 1.3 a tile of 32 keys, the other kernel two tiles of 128 keys in
+// 2.9, in rounds over the SMs.  Measured, D = 128 / 64, 40 rows: 16 sequences to 4093 tokens, 8 heads: warps 55 / 40, other
+// 71 / 57; the same with a window of 1024, D = 64: 29 and 23; 64 rows, 64 sequences to 2048: 138 and 121.
+static bool prefill_pays(const AttnArgs& a) {
+    const int64_t rows = (int64_t)a.max_new * a.group;
+    if (a.c.head_dim > 128 || rows <= 32) return false;
+    if (rows > 128) return true;
+    const bool windowed = a.window > 0 && (int64_t)a.window + a.max_new < a.max_len;
+    const double keys = windowed ? a.window + a.max_new : a.max_len, even = windowed ? 1.0 : 0.6, units = (double)a.b.n_seq * a.c.n_kv_heads;
+    const double sms = sm_count(), warps = 12 + 1.3 * even * units * ((rows + 15) / 16) * (keys / 32) / (8 * sms);
+    const double splits = std::max(1.0, std::min(8.0, std::floor(sms / units)));
+    return 10 + 2.9 * (keys / 256) / splits * std::max(1.0, units / sms) < warps;
+}
+
+// The counters, then two parts per block and one per worker, of the kernel that has most, or the parts of the prompts'.
+static size_t attention_ws_bytes(int d) {
     const size_t narrow = (size_t)Rows<64, 1>::kPerSm * 6 * 8, wide = (size_t)Rows<64, 2>::kPerSm * 6 * 16;
     const size_t blocks = std::min(std::max(1, sm_count()), kMaxBlocks / Rows<64, 1>::kPerSm);
-    return kMaxBlocks * sizeof(int) + blocks * std::max(narrow, wide) * (d + 2) * sizeof(float);
+    return CMPQ_ATTENTION_ZEROED + std::max(blocks * std::max(narrow, wide) * (d + 2) * sizeof(float), prefill_parts_bytes(d));
 }
 
 }  // namespace cmpq
@@ -659,7 +678,7 @@ extern "C" size_t cmpq_cache_attention_ws_bytes(int64_t n_seq, int64_t n_tok, in
     if (n_seq < 0 || n_tok < 0 || max_new < 0 || max_len < 0 || n_heads < 1 || n_kv_heads < 1 || n_heads % n_kv_heads ||
         head_dim < 1 || head_dim > 256)
         return 0;
-    return round_up(rows_ws_bytes(head_dim), 256);
+    return round_up(attention_ws_bytes(head_dim), 256);
 }
 
 extern "C" cmpq_status cmpq_cache_attention(const cmpq_cache* cache, const cmpq_batch* batch, const void* q, int64_t ldq,
@@ -683,10 +702,10 @@ extern "C" cmpq_status cmpq_cache_attention(const cmpq_cache* cache, const cmpq_
     AttnArgs a{*cache, *batch, static_cast<const uint16_t*>(q), static_cast<uint16_t*>(out), lse, ldq, ldo, (int)max_new, (int)max_len,
                (int)std::min<int64_t>(window, INT32_MAX), scale * kLog2e, n_heads, n_heads / cache->n_kv_heads, causal != 0,
                31 - __builtin_clz(cache->page_tokens), aligned_to(q, 16) && ldq % 8 == 0, aligned_to(out, 16) && ldo % 8 == 0,
-               word, static_cast<int*>(ws), reinterpret_cast<float*>(static_cast<int*>(ws) + kMaxBlocks), 0};
+               word, static_cast<int*>(ws), reinterpret_cast<float*>(static_cast<char*>(ws) + CMPQ_ATTENTION_ZEROED), 0};
     auto st = static_cast<cudaStream_t>(stream);
     const bool bf = dt == CMPQ_BF16;
-    if (cache->head_dim <= 128 && max_new * a.group > 32) return launch_prefill(a, dt, st);
+    if (prefill_pays(a)) return launch_prefill(a, dt, st);
     switch (cache->head_dim) {
         case 64: return bf ? launch_attention<CMPQ_BF16, 64>(a, st) : launch_attention<CMPQ_F16, 64>(a, st);
         case 128: return bf ? launch_attention<CMPQ_BF16, 128>(a, st) : launch_attention<CMPQ_F16, 128>(a, st);

@@ -1,4 +1,5 @@
 // Attention of many query rows over the paged 8-bit cache: both products on tcgen05, accumulators in TMEM.
+#include <algorithm>
 #include <type_traits>
 
 #include "attention.cuh"
@@ -53,9 +54,55 @@ __device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
     return d;
 }
 
+// How the units (row block, sequence, key-value head) are dealt to blocks: `splits` blocks share out a unit's keys.
+struct PrefillPlan {
+    int row_blocks, per_row_block, splits;
+};
+constexpr int kPfSplits = 8, kPfCounters = 512;  // most blocks to a unit; where its counters begin
+
+// A row's entries, times f, as 16 bits into `dst` or as they are into `part`.  columns(c, x, y) gives the accumulator's
+// columns c.. and D/2 + c.. and is called by all lanes; `real`: the row exists.
+template <int DT, int D, class Columns>
+__device__ __forceinline__ void store_row(Columns columns, float f, bool real, float* part, uint16_t* dst, bool wide) {
+#pragma unroll
+    for (int c = 0; c < D / 2; c += 32) {
+        uint32_t x[32], y[32];
+        __syncwarp();
+        columns(c, x, y);
+        if (!real) continue;
+#pragma unroll
+        for (int j = 0; j < 32; ++j) x[j] = __float_as_uint(__uint_as_float(x[j]) * f), y[j] = __float_as_uint(__uint_as_float(y[j]) * f);
+#pragma unroll
+        for (int j = 0; j < 32; j += 8) {
+            if (part) {
+                uint4* o = reinterpret_cast<uint4*>(part + 2 * (c + j));
+                o[0] = make_uint4(x[j], x[j + 1], x[j + 2], x[j + 3]);
+                o[1] = make_uint4(x[j + 4], x[j + 5], x[j + 6], x[j + 7]);
+                o[2] = make_uint4(y[j], y[j + 1], y[j + 2], y[j + 3]);
+                o[3] = make_uint4(y[j + 4], y[j + 5], y[j + 6], y[j + 7]);
+                continue;
+            }
+            uint32_t a[8];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                a[k] = round16x2<DT>(__uint_as_float(x[j + 2 * k]), __uint_as_float(x[j + 2 * k + 1]));
+                a[4 + k] = round16x2<DT>(__uint_as_float(y[j + 2 * k]), __uint_as_float(y[j + 2 * k + 1]));
+            }
+            uint16_t* o = dst + 2 * (c + j);
+            if (wide) {
+                *reinterpret_cast<uint4*>(o) = make_uint4(a[0], a[1], a[2], a[3]);
+                *reinterpret_cast<uint4*>(o + 8) = make_uint4(a[4], a[5], a[6], a[7]);
+            } else {
+#pragma unroll
+                for (int k = 0; k < 16; ++k) o[k] = (uint16_t)(a[k >> 1] >> (16 * (k & 1)));
+            }
+        }
+    }
+}
+
 template <int DT, int D>
 __global__ void __launch_bounds__(kPfThreads, 1)
-attention_prefill_kernel(const __grid_constant__ AttnArgs A, const int row_blocks) {
+attention_prefill_kernel(const __grid_constant__ AttnArgs A, const __grid_constant__ PrefillPlan plan) {
     using C = Prefill<D>;
     extern __shared__ uint8_t raw[];
     uint8_t* smem = raw + ((1024u - (tc5::smem_addr(raw) & 1023u)) & 1023u);
@@ -64,12 +111,13 @@ attention_prefill_kernel(const __grid_constant__ AttnArgs A, const int row_block
     uint8_t* const sv = smem + 4 * C::kTileBytes;
     __shared__ uint64_t q_full, k_full[2], k_empty[2], v_full[2], v_empty[2], s_full[2], p_full[2], o_full[2];
     __shared__ uint32_t tmem_at;
-    __shared__ int failed;
+    __shared__ int failed, is_last;
+    __shared__ float2 half_ml[128];
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int H = A.c.n_kv_heads, g = A.group, page_bits = A.page_bits;
     // the last row blocks see most keys and come first
-    const int units = gridDim.x / row_blocks;
-    const int rb = row_blocks - 1 - blockIdx.x / units, s = blockIdx.x % units / H, head = blockIdx.x % H;
+    const int splits = plan.splits, unit = blockIdx.x / splits, z = blockIdx.x % splits;
+    const int rb = plan.row_blocks - 1 - unit / plan.per_row_block, s = unit % plan.per_row_block / H, head = unit % H;
 
     const int first = A.b.tok_off[s], n = A.b.tok_off[s + 1] - first, len = A.b.lens[s];
     if (len < 0 || len > A.max_len || n < 0 || n > A.max_new || first < 0 || (int64_t)first + n > A.b.n_tok) {
@@ -82,7 +130,8 @@ attention_prefill_kernel(const __grid_constant__ AttnArgs A, const int row_block
     // positions of the first and last query, keys that any of them sees, tiles of keys
     const int p0 = len - n + (rb * 256) / g, p1 = len - n + (rb * 256 + rows - 1) / g;
     const int key_hi = A.causal ? max(0, p1 + 1) : len, key_lo = A.window > 0 ? max(0, p0 - A.window + 1) : 0;
-    const int t0 = key_lo / kPfKeys, tiles = key_hi > key_lo ? (key_hi + kPfKeys - 1) / kPfKeys - t0 : 0;
+    const int tile0 = key_lo / kPfKeys, all_tiles = key_hi > key_lo ? (key_hi + kPfKeys - 1) / kPfKeys - tile0 : 0;
+    const int t0 = tile0 + all_tiles * z / splits, tiles = tile0 + all_tiles * (z + 1) / splits - t0;  // this block's
     const int32_t* table = A.b.table + (int64_t)s * A.b.ld_table;
     const int pages = (len + (1 << page_bits) - 1) >> page_bits;
     auto page_of = [&](int page) {  // -1 where there is none
@@ -113,7 +162,7 @@ attention_prefill_kernel(const __grid_constant__ AttnArgs A, const int row_block
             constexpr uint32_t kScores = tc5::idesc_f16(128, 128), kOut = tc5::idesc_f16(128, D) | tc5::kTransposedB;
             const uint32_t aq = tc5::smem_addr(sq), ak = tc5::smem_addr(sk), av = tc5::smem_addr(sv);
             auto scores = [&](int w, int t) {
-                const uint64_t a = tc5::desc_k_sw128(aq + w * C::kTileBytes), b = tc5::desc_k_sw128(ak + (t & 1) * C::kTileBytes);
+                const uint64_t a = tc5::desc_k_sw128(aq + (two ? w : 0) * C::kTileBytes), b = tc5::desc_k_sw128(ak + (t & 1) * C::kTileBytes);
 #pragma unroll
                 for (int j = 0; j < D / 16; ++j) {
                     const uint32_t at = (j >> 2) * (128 * 128 >> 4) + (j & 3) * 2;
@@ -121,33 +170,60 @@ attention_prefill_kernel(const __grid_constant__ AttnArgs A, const int row_block
                 }
                 tc5::mma_commit(s_full + w);
             };
+            auto outputs = [&](int w, int t) {
+                const uint64_t b = tc5::desc_mn_sw128(av + (t & 1) * C::kTileBytes, 128 * 128);
+#pragma unroll
+                for (int j = 0; j < kPfKeys / 16; ++j)
+                    tc5::mma_f16_ts(tmem_o + w * 128, tmem + w * 128 + j * 8, b + j * (2048 >> 4), kOut, (two ? t : t >> 1) != 0 || j != 0);
+            };
             bool ok = tc5::mbar_wait(&q_full, 0, &failed) && tc5::mbar_wait(k_full, 0, &failed);
             tc5::fence_after_sync();
-            if (ok) {
+            if (ok && two) {
                 scores(0, 0);
-                if (two) scores(1, 0);
+                scores(1, 0);
                 tc5::mma_commit(k_empty);
-            }
-            for (int t = 0; ok && t < tiles; ++t) {
-                const int slot = t & 1, next = (t + 1) & 1;
-                ok = tc5::mbar_wait(v_full + slot, (t >> 1) & 1, &failed);
-                if (ok && t + 1 < tiles) ok = tc5::mbar_wait(k_full + next, ((t + 1) >> 1) & 1, &failed);
+                for (int t = 0; ok && t < tiles; ++t) {
+                    const int slot = t & 1, next = (t + 1) & 1;
+                    ok = tc5::mbar_wait(v_full + slot, (t >> 1) & 1, &failed);
+                    if (ok && t + 1 < tiles) ok = tc5::mbar_wait(k_full + next, ((t + 1) >> 1) & 1, &failed);
 #pragma unroll 1
-                for (int w = 0; ok && w < (two ? 2 : 1); ++w) {
-                    if (!(ok = tc5::mbar_wait(p_full + w, t & 1, &failed))) break;
+                    for (int w = 0; ok && w < 2; ++w) {
+                        if (!(ok = tc5::mbar_wait(p_full + w, t & 1, &failed))) break;
+                        tc5::fence_after_sync();
+                        outputs(w, t);
+                        if (t + 1 < tiles) {
+                            scores(w, t + 1);
+                        } else {
+                            tc5::mma_commit(o_full + w);
+                        }
+                    }
+                    tc5::mma_commit(v_empty + slot);
+                    if (t + 1 < tiles) tc5::mma_commit(k_empty + next);
+                }
+            } else if (ok) {  // one row tile: the two accumulators take every other tile of keys
+                scores(0, 0);
+                tc5::mma_commit(k_empty);
+                if (tiles > 1) {
+                    ok = tc5::mbar_wait(k_full + 1, 0, &failed);
                     tc5::fence_after_sync();
-                    const uint64_t b = tc5::desc_mn_sw128(av + slot * C::kTileBytes, 128 * 128);
-#pragma unroll
-                    for (int j = 0; j < kPfKeys / 16; ++j)
-                        tc5::mma_f16_ts(tmem_o + w * 128, tmem + w * 128 + j * 8, b + j * (2048 >> 4), kOut, (t | j) != 0);
-                    if (t + 1 < tiles) {
-                        scores(w, t + 1);
+                    scores(1, 1);
+                    tc5::mma_commit(k_empty + 1);
+                }
+                for (int t = 0; ok && t < tiles; ++t) {
+                    const int w = t & 1, phase = (t >> 1) & 1;
+                    ok = tc5::mbar_wait(v_full + w, phase, &failed) && tc5::mbar_wait(p_full + w, phase, &failed);
+                    if (ok && t + 2 < tiles) ok = tc5::mbar_wait(k_full + w, phase ^ 1, &failed);
+                    if (!ok) break;
+                    tc5::fence_after_sync();
+                    outputs(w, t);
+                    tc5::mma_commit(v_empty + w);
+                    if (t + 2 < tiles) {
+                        scores(w, t + 2);
+                        tc5::mma_commit(k_empty + w);
                     } else {
                         tc5::mma_commit(o_full + w);
                     }
                 }
-                tc5::mma_commit(v_empty + slot);
-                if (t + 1 < tiles) tc5::mma_commit(k_empty + next);
             }
         }
         __syncwarp();
@@ -202,8 +278,8 @@ attention_prefill_kernel(const __grid_constant__ AttnArgs A, const int row_block
             if (t + 1 < tiles) fetch(A.c.v_codes, vc);
         }
     } else {
-        const int w = warp >> 2, local = tid & 127, row = rb * 256 + w * 128 + local;
-        const bool real = w * 128 + local < rows;
+        const int w = warp >> 2, local = tid & 127, in_block = (two ? w : 0) * 128 + local, row = rb * 256 + in_block;
+        const bool real = in_block < rows;
         const int i = row / g, h = head * g + row % g, pos = len - n + i;
         // this row's query into shared memory, scaled by a power of two into fp16's range
         float qs = 0.0f;
@@ -228,14 +304,14 @@ attention_prefill_kernel(const __grid_constant__ AttnArgs A, const int row_block
                 widen8<DT>(x[j], f);
 #pragma unroll
                 for (int k = 0; k < 4; ++k) y[k] = round16x2<CMPQ_F16>(f[2 * k] * dn, f[2 * k + 1] * dn);
-                *reinterpret_cast<uint4*>(sq + w * C::kTileBytes + pf_at<D>(local, j)) = make_uint4(y[0], y[1], y[2], y[3]);
+                if (two || w == 0) *reinterpret_cast<uint4*>(sq + w * C::kTileBytes + pf_at<D>(local, j)) = make_uint4(y[0], y[1], y[2], y[3]);
             }
             qs = A.scale * up;
             tc5::fence_async_smem();
             __syncwarp();
             if (lane == 0) tc5::mbar_arrive(&q_full);
         }
-        // the largest value scale of the pages that the block meets (warps of the second tile, if idle, help nobody)
+        // the largest value scale of the pages that the block meets
         float ref = 0.0f;
         {
             const int from = (t0 * kPfKeys) >> page_bits, to = min(pages, ((t0 + tiles) * kPfKeys) >> page_bits);
@@ -260,15 +336,17 @@ attention_prefill_kernel(const __grid_constant__ AttnArgs A, const int row_block
             }
             return x;
         };
-        const bool work = w == 0 || two;
-        if (work && tiles > 0) sc_next = scales(0);
+        // with one row tile the second four warps take every other tile of keys
+        const int t_first = two ? 0 : w, t_step = two ? 1 : 2;
+        const bool work = t_first < tiles;
+        if (work) sc_next = scales(t_first);
         float m = -INFINITY, l = 0.0f;
         // keys [lo, hi) are seen by this row; a tile inside [all_lo, all_hi) is seen whole by the warp's rows
         const int hi = real ? (A.causal ? min(len, pos + 1) : len) : INT32_MAX, lo = real && A.window > 0 ? pos - A.window + 1 : 0;
         const int all_hi = __reduce_min_sync(0xffffffffu, hi), all_lo = __reduce_max_sync(0xffffffffu, lo);
         // The reference maximum has moved before keys 32 step.. of tile t: what was weighted with the old one.
         auto rescale = [&](int t, int step, float keep) {
-            if (t > 0) {  // the products into O that came before have ended: S was committed after them
+            if (t > t_first) {  // the products into O that came before have ended: S was committed after them
 #pragma unroll 1
                 for (int c = 0; c < D; c += 16) {
                     uint32_t x[16];
@@ -295,11 +373,11 @@ attention_prefill_kernel(const __grid_constant__ AttnArgs A, const int row_block
             }
         };
         bool ok = true;
-        for (int t = 0; work && t < tiles; ++t) {
+        for (int t = t_first; t < tiles; t += t_step) {
             sc = sc_next;
             const float vs = fmaxf(sc.y * inv_ref, 0x1p-100f), bias = log2f(vs), inv_vs = 1.0f / vs;
-            if (t + 1 < tiles) sc_next = scales(t + 1);
-            if (!(ok = tc5::mbar_wait(s_full + w, t & 1, &failed))) break;
+            if (t + t_step < tiles) sc_next = scales(t + t_step);
+            if (!(ok = tc5::mbar_wait(s_full + w, (two ? t : t >> 1) & 1, &failed))) break;
             tc5::fence_after_sync();
             const int key0 = (t0 + t) * kPfKeys;
             const int from = lo - key0, upto = hi - key0;
@@ -361,47 +439,121 @@ attention_prefill_kernel(const __grid_constant__ AttnArgs A, const int row_block
             __syncwarp();
             if (lane == 0) tc5::mbar_arrive(p_full + w);
         }
-        if (work && ok && tiles > 0) ok = tc5::mbar_wait(o_full + w, 0, &failed);
-        if (work && ok) {
-            tc5::fence_after_sync();
-            const float f = l > 0.0f ? ref / l : 0.0f;
-            uint16_t* dst = A.out + (int64_t)(first + i) * A.ldo + (int64_t)h * D;
+        if (work && ok) ok = tc5::mbar_wait(o_full + w, 0, &failed);
+        if (!two && w == 1 && tiles > 0 && ok) ok = tc5::mbar_wait(o_full, 0, &failed);  // all products have ended
+        ok = __all_sync(0xffffffffu, ok);
+        tc5::fence_after_sync();
+        // entries 2 c .. 2 c + 63 of the row: columns c.. and D/2 + c.., whose groups 2 j and 2 j + 1 alternate
+        auto columns = [&](int c, uint32_t (&x)[32], uint32_t (&y)[32]) {
+            if (work) {
+                tc5::tmem_ld32(to + c, x);
+                tc5::tmem_ld32(to + D / 2 + c, y);
+                tc5::tmem_ld_wait();
+            } else {
 #pragma unroll
-            for (int c = 0; c < D / 2; c += 32) {  // columns c.. and D/2 + c..: groups 2 j and 2 j + 1 of eight entries
-                uint32_t x[32], y[32];
-                if (tiles > 0) {
-                    tc5::tmem_ld32(to + c, x);
-                    tc5::tmem_ld32(to + D / 2 + c, y);
-                    tc5::tmem_ld_wait();
-                } else {
+                for (int j = 0; j < 32; ++j) x[j] = y[j] = 0u;
+            }
+        };
+        float mine = 1.0f, others = 0.0f;
+        if (!two) {  // the second half's sums, by way of the keys' shared memory: no product reads it any more
+            float* held = reinterpret_cast<float*>(sk) + local;
+            if (w == 1) {
+                half_ml[local] = make_float2(m, l);
 #pragma unroll
-                    for (int j = 0; j < 32; ++j) x[j] = y[j] = 0u;
-                }
-                if (!real) continue;
+                for (int c = 0; c < D / 2; c += 32) {
+                    uint32_t x[32], y[32];
+                    columns(c, x, y);
 #pragma unroll
-                for (int j = 0; j < 32; j += 8) {
-                    uint32_t a[8];
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        a[k] = round16x2<DT>(__uint_as_float(x[j + 2 * k]) * f, __uint_as_float(x[j + 2 * k + 1]) * f);
-                        a[4 + k] = round16x2<DT>(__uint_as_float(y[j + 2 * k]) * f, __uint_as_float(y[j + 2 * k + 1]) * f);
-                    }
-                    uint16_t* o = dst + 2 * (c + j);
-                    if (A.wide_o) {
-                        *reinterpret_cast<uint4*>(o) = make_uint4(a[0], a[1], a[2], a[3]);
-                        *reinterpret_cast<uint4*>(o + 8) = make_uint4(a[4], a[5], a[6], a[7]);
-                    } else {
-#pragma unroll
-                        for (int k = 0; k < 16; ++k) o[k] = (uint16_t)(a[k >> 1] >> (16 * (k & 1)));
-                    }
+                    for (int j = 0; j < 32; ++j) held[(c + j) * 128] = __uint_as_float(x[j]), held[(D / 2 + c + j) * 128] = __uint_as_float(y[j]);
                 }
             }
-            if (A.lse && real) A.lse[(int64_t)(first + i) * A.n_heads + h] = l > 0.0f ? (m + log2f(l)) * kLn2 : -INFINITY;
+            asm volatile("bar.sync 1, 256;" ::: "memory");
+            const float2 o = half_ml[local];
+            const float top = fmaxf(m, o.x), at = top == -INFINITY ? 0.0f : top;
+            mine = ex2(m - at), others = ex2(o.x - at);
+            l = l * mine + o.y * others;
+            m = top;
+        }
+        if (ok && (two || w == 0)) {  // all lanes: the warp reads TMEM together
+            // whole: the normalised row; a part: times its own reference scale only, with maximum and sum behind the rows
+            float* part = splits > 1 ? A.parts + (int64_t)blockIdx.x * (256 * (D + 2)) : nullptr;
+            const float f = part ? ref : l > 0.0f ? ref / l : 0.0f;
+            uint16_t* dst = A.out + (int64_t)(first + i) * A.ldo + (int64_t)h * D;
+            const float* held = reinterpret_cast<const float*>(sk) + local;
+            store_row<DT, D>(
+                [&](int c, uint32_t (&x)[32], uint32_t (&y)[32]) {
+                    columns(c, x, y);
+                    if (!two) {
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) {
+                            x[j] = __float_as_uint(fmaf(__uint_as_float(x[j]), mine, held[(c + j) * 128] * others));
+                            y[j] = __float_as_uint(fmaf(__uint_as_float(y[j]), mine, held[(D / 2 + c + j) * 128] * others));
+                        }
+                    }
+                },
+                f, real, part ? part + in_block * D : nullptr, dst, A.wide_o);
+            if (part && real) {
+                reinterpret_cast<float2*>(part + 256 * D)[in_block] = make_float2(m, l);
+                __threadfence();
+            } else if (real && A.lse) {
+                A.lse[(int64_t)(first + i) * A.n_heads + h] = l > 0.0f ? (m + log2f(l)) * kLn2 : -INFINITY;
+            }
         }
         tc5::fence_before_sync();
     }
     __syncwarp();
     __syncthreads();
+    if (splits > 1) {  // the block that adds a unit's last part joins them, in order, a thread per row
+        const int first_part = blockIdx.x - z;
+        if (tid == 0) {
+            __threadfence();
+            is_last = atomicAdd(A.counters + kPfCounters + unit, 1) == splits - 1;
+        }
+        __syncthreads();
+        if (is_last && tid < 256 && tid < rows) {
+            __threadfence();
+            const float* parts = A.parts + (int64_t)first_part * (256 * (D + 2));
+            constexpr int kStep = 256 * (D + 2);
+            float m = -INFINITY, l = 0.0f, by[kPfSplits];
+#pragma unroll
+            for (int k = 0; k < kPfSplits; ++k) {
+                by[k] = -INFINITY;
+                if (k < splits) by[k] = reinterpret_cast<const float2*>(parts + k * kStep + 256 * D)[tid].x;
+                m = fmaxf(m, by[k]);
+            }
+            const float at = m == -INFINITY ? 0.0f : m;
+#pragma unroll
+            for (int k = 0; k < kPfSplits; ++k) {
+                by[k] = ex2(by[k] - at);
+                if (k < splits) l = fmaf(by[k], reinterpret_cast<const float2*>(parts + k * kStep + 256 * D)[tid].y, l);
+            }
+            const int row = rb * 256 + tid, i = row / g, h = head * g + row % g;
+            const float f = l > 0.0f ? 1.0f / l : 0.0f;
+            uint16_t* dst = A.out + (int64_t)(first + i) * A.ldo + (int64_t)h * D;
+            for (int c = 0; c < D; c += 8) {
+                float o[8] = {};
+#pragma unroll
+                for (int k = 0; k < kPfSplits; ++k)
+                    if (k < splits) {
+                        const float4* p = reinterpret_cast<const float4*>(parts + k * kStep + tid * D + c);
+                        const float4 a = p[0], b = p[1];
+                        o[0] = fmaf(by[k], a.x, o[0]), o[1] = fmaf(by[k], a.y, o[1]), o[2] = fmaf(by[k], a.z, o[2]), o[3] = fmaf(by[k], a.w, o[3]);
+                        o[4] = fmaf(by[k], b.x, o[4]), o[5] = fmaf(by[k], b.y, o[5]), o[6] = fmaf(by[k], b.z, o[6]), o[7] = fmaf(by[k], b.w, o[7]);
+                    }
+                uint32_t w[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) w[k] = round16x2<DT>(o[2 * k] * f, o[2 * k + 1] * f);
+                if (A.wide_o) {
+                    *reinterpret_cast<uint4*>(dst + c) = make_uint4(w[0], w[1], w[2], w[3]);
+                } else {
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) dst[c + k] = (uint16_t)(w[k >> 1] >> (16 * (k & 1)));
+                }
+            }
+            if (A.lse) A.lse[(int64_t)(first + i) * A.n_heads + h] = l > 0.0f ? (m + log2f(l)) * kLn2 : -INFINITY;
+        }
+        if (is_last && tid == 0) A.counters[kPfCounters + unit] = 0;
+    }
     if (failed) {  // products and arrivals that were asked for have to end before the memory is given back
         if (tid == 0) {
             const long long start = clock64();
@@ -417,11 +569,19 @@ template <int DT, int D>
 static cmpq_status launch_prefill_of(const AttnArgs& a, cudaStream_t st) {
     static bool raised[64];
     if (!raise_smem_limit_once(attention_prefill_kernel<DT, D>, Prefill<D>::kSmem, raised)) return CMPQ_ERR_CUDA;
-    const int64_t row_blocks = ((int64_t)a.max_new * a.group + 255) / 256, blocks = row_blocks * a.b.n_seq * a.c.n_kv_heads;
+    const int64_t row_blocks = ((int64_t)a.max_new * a.group + 255) / 256, per = a.b.n_seq * a.c.n_kv_heads, units = row_blocks * per, sms = sm_count();
+    // Fewer units than SMs: each is split over the keys, three tiles of them to a block at least.  Splitting the last round
+    // of many does not pay: 2 x 2048 queries, 32 heads (512 units, 3.5 rounds) took 334 us so, and 314 whole, since the
+    // blocks of the earlier rounds do not end together.
+    const int splits = units < sms ? (int)std::max<int64_t>(1, std::min({sms / units, (int64_t)kPfSplits, ((int64_t)a.max_len + kPfKeys - 1) / kPfKeys / 3})) : 1;
+    const int64_t blocks = units * splits;
     if (blocks > INT32_MAX) return CMPQ_ERR_UNSUPPORTED;
-    attention_prefill_kernel<DT, D><<<(unsigned)blocks, kPfThreads, Prefill<D>::kSmem, st>>>(a, (int)row_blocks);
+    const PrefillPlan plan{(int)row_blocks, (int)per, splits};
+    attention_prefill_kernel<DT, D><<<(unsigned)blocks, kPfThreads, Prefill<D>::kSmem, st>>>(a, plan);
     return launch_status();
 }
+
+size_t prefill_parts_bytes(int d) { return d > 128 ? 0 : (size_t)std::max(1, sm_count()) * 256 * (d + 2) * sizeof(float); }
 
 cmpq_status launch_prefill(const AttnArgs& a, cmpq_dtype dt, cudaStream_t st) {
     const bool bf = dt == CMPQ_BF16;
