@@ -9,8 +9,14 @@
     python profile_cases.py sweep --config c3_mlp7b --layer 0 --launches 5
     python profile_cases.py stack --config c4_stack7b --budget 3.0
     python profile_cases.py layer --config c3_mlp7b --layer 0 --budget 3.0 --launches 5
+    python profile_cases.py linear8 --tokens 37 --d-in 4096 --d-out 11008 --launches 20
+    python profile_cases.py attend8 --streams 24 --tokens 8191 --new 1 --heads 64 --kv-heads 8 --launches 3
+    python profile_cases.py append8 --streams 5 --tokens 4096 --new 2048 --heads 64 --kv-heads 8 --launches 3
+    python profile_cases.py serve --streams 8 --tokens 1000 --heads 32 --kv-heads 32 --launches 32
 
 `layer` runs the whole pass on one layer of a named workload and prints the time per C-ABI call.
+`serve` runs an attention block in 8 bits (projections, append with rotation, attention over the cache, output) on
+the prompts of some streams and then token by token; `linear8`, `append8` and `attend8` are its single calls.
 `stack` quantizes every layer of a multi-block workload (all 32 x 7 layers of the Llama-7B-shaped stack) and
 prints the total device time of the passes; under torchrun the layers are dealt round-robin to the ranks.
 
@@ -191,9 +197,130 @@ def run_matvec(a, dt):
           % (cold, algo / cold / 1e6, warm, algo / warm / 1e6, a.launches))
 
 
+def _timed(fn, launches):
+    fn()
+    torch.cuda.synchronize()
+    e0, e1 = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+    e0.record()
+    for _ in range(launches):
+        fn()
+    e1.record()
+    torch.cuda.synchronize()
+    return e0.elapsed_time(e1) / launches
+
+
+def run_linear8(a):
+    from paper_2410_13056_b200 import serving
+
+    dt = torch.bfloat16 if a.dtype == "bf16" else torch.float16
+    # weights of several layers in turn, so that small ones do not stay in L2
+    layers = [serving.Int8Linear.from_weight((torch.randn(a.d_out, a.d_in, device="cuda") * 0.02).to(dt))
+              for _ in range(max(1, min(16, int(3e8 // (a.d_in * a.d_out)))))]
+    x = inputs.make_activations(a.tokens, a.d_in, inputs.BF16 if a.dtype == "bf16" else inputs.F16, 1, device="cuda")
+    y = torch.empty(a.tokens, a.d_out, dtype=dt, device="cuda")
+    ms = _timed(lambda: [layer(x, out=y) for layer in layers], a.launches) / len(layers)
+    print("linear8: %d tokens, %d -> %d, %s: %.4f ms per layer (%.0f GB/s of weights, %.0f TOP/s)"
+          % (a.tokens, a.d_in, a.d_out, a.dtype, ms, a.d_in * a.d_out / ms / 1e6, 2 * a.tokens * a.d_in * a.d_out / ms / 1e9))
+
+
+def _served(a, length):
+    """A cache for `streams` sequences of up to `length` tokens on shuffled pages, its table, and rotation tables."""
+    from paper_2410_13056_b200 import serving
+
+    d, page = a.head_dim, a.page
+    per = -(-length // page)
+    cache = serving.PagedCache8.empty(a.streams * per, a.kv_heads, d, page)
+    table = torch.randperm(a.streams * per, device="cuda").to(torch.int32).view(a.streams, per)
+    angle = torch.arange(length, device="cuda")[:, None] * 10000.0 ** (-torch.arange(0, d, 2, device="cuda") / d)
+    return cache, table, angle.cos().float().contiguous(), angle.sin().float().contiguous()
+
+
+def _i32(x):
+    return torch.tensor(x, dtype=torch.int32, device="cuda")
+
+
+def run_cache8(a):
+    """append8: `new` tokens join `tokens - new` cached ones in every stream; attend8: they attend to all."""
+    import random
+
+    dt = torch.bfloat16 if a.dtype == "bf16" else torch.float16
+    cache, table, cos, sin = _served(a, a.tokens)
+    d, r = a.head_dim, random.Random(1)
+    lens = [a.tokens] + [r.randint(max(a.new, a.tokens // 8), a.tokens) for _ in range(a.streams - 1)]
+    n = a.new * a.streams
+    for codes, scale in ((cache.k_codes, cache.k_scale), (cache.v_codes, cache.v_scale)):
+        codes.copy_(torch.randint(-127, 128, codes.shape, device="cuda", dtype=torch.int8))
+        scale.fill_(0.01)
+    q = torch.randn(n, a.heads, d, device="cuda").to(dt)
+    k, v = (torch.randn(n, a.kv_heads, d, device="cuda").to(dt) for _ in range(2))
+    off, lens_t = _i32([a.new * s for s in range(a.streams + 1)]), _i32(lens)
+    if a.case == "append8":
+        ms = _timed(lambda: cache.append(k, v, off, lens_t, table, q=q, cos=cos, sin=sin), a.launches)
+        moved = n * d * (4 * a.heads + 6 * a.kv_heads)
+    else:
+        ms = _timed(lambda: cache.attend(q, off, lens_t, table, max_new=a.new, max_len=a.tokens), a.launches)
+        moved = 2 * sum(lens) * a.kv_heads * d + 4 * n * a.heads * d
+    cache.check()
+    flops = 4 * d * a.heads * sum(a.new * (m - a.new) + a.new * (a.new + 1) // 2 for m in lens)
+    print("%s: %d streams to %d tokens, %d new each, %d/%d heads of %d, pages of %d, %s: %.4f ms (%.0f GB/s%s)"
+          % (a.case, a.streams, a.tokens, a.new, a.heads, a.kv_heads, d, a.page, a.dtype, ms, moved / ms / 1e6,
+             "" if a.case == "append8" else ", %.0f TFLOP/s" % (flops / ms / 1e9)))
+
+
+def run_serve(a):
+    """An attention block in 8 bits over the prompts of `streams` sequences (`tokens` at most, uneven), then
+    `launches` generated tokens each; compared with the same block in fp32 on the prompts."""
+    import math
+    import random
+
+    from paper_2410_13056_b200 import serving
+
+    h, kv, d, dt = a.heads, a.kv_heads, a.head_dim, torch.bfloat16 if a.dtype == "bf16" else torch.float16
+    d_model, r = h * d, random.Random(1)
+    new = [a.tokens] + [r.randint(max(1, a.tokens // 4), a.tokens) for _ in range(a.streams - 1)]
+    cache, table, cos, sin = _served(a, a.tokens + a.launches)
+    g = torch.Generator(device="cuda").manual_seed(1)
+    w = (torch.randn((h + 2 * kv) * d, d_model, device="cuda", generator=g) * 0.02).to(dt)
+    wo = (torch.randn(d_model, d_model, device="cuda", generator=g) * 0.02).to(dt)
+    layer = serving.AttentionLayer8(serving.Int8Linear.from_weight(w), serving.Int8Linear.from_weight(wo), cache, h, cos, sin)
+    off = [sum(new[:s]) for s in range(a.streams + 1)]
+    x = torch.randn(off[-1], d_model, device="cuda", generator=g).to(dt)
+    args = (_i32(off), _i32(new), table)
+    ms = _timed(lambda: layer(x, *args, max_new=max(new), max_len=a.tokens), 3)
+    y = layer(x, *args, max_new=max(new), max_len=a.tokens)
+    print("serve: prompts of %d streams, %d tokens: %.3f ms a block" % (a.streams, off[-1], ms))
+    # the first stream in fp32, from the 16-bit weights
+    n = new[0]
+    qkv = x[:n].float() @ w.float().t()
+    q, k, v = (qkv[:, lo * d: hi * d].unflatten(1, (hi - lo, d)) for lo, hi in ((0, h), (h, h + kv), (h + kv, h + 2 * kv)))
+
+    def turn(t):
+        lo, hi = t[..., : d // 2], t[..., d // 2:]
+        c, s = cos[:n, None], sin[:n, None]
+        return torch.cat((lo * c - hi * s, hi * c + lo * s), -1)
+
+    q, k, v = turn(q).transpose(0, 1), turn(k).repeat_interleave(h // kv, 1).transpose(0, 1), v.repeat_interleave(h // kv, 1).transpose(0, 1)
+    p = (q @ k.transpose(1, 2) / math.sqrt(d)).masked_fill(torch.ones(n, n, device="cuda", dtype=torch.bool).triu(1), -math.inf).softmax(-1)
+    want = (p @ v).transpose(0, 1).flatten(1) @ wo.float().t()
+    print("   first stream against fp32: relative error %.4f" % float((y[:n].float() - want).norm() / want.norm()))
+    one = _i32(list(range(a.streams + 1)))
+    token = torch.randn(a.streams, d_model, device="cuda", generator=g).to(dt)
+    lens = args[1].clone()
+    torch.cuda.synchronize()
+    e0, e1 = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+    e0.record()
+    for _ in range(a.launches):
+        lens += 1
+        token = layer(token, one, lens, table, max_new=1, max_len=a.tokens + a.launches)
+    e1.record()
+    cache.check()
+    print("   generation: %.4f ms a token and block for %d streams" % (e0.elapsed_time(e1) / a.launches, a.streams))
+
+
 def main():
     ap = argparse.ArgumentParser()
-    ap.add_argument("case", choices=["lloyd", "stats", "pack", "outliers", "protect", "layer", "matvec", "stack", "transpose", "sweep"])
+    ap.add_argument("case", choices=["lloyd", "stats", "pack", "outliers", "protect", "layer", "matvec", "stack", "transpose", "sweep",
+                                     "linear8", "append8", "attend8", "serve"])
     ap.add_argument("--config", default="c2_attn7b")
     ap.add_argument("--layer", type=int, default=0)
     ap.add_argument("--budget", type=float, default=3.0)
@@ -204,6 +331,12 @@ def main():
     ap.add_argument("--iters", type=int, default=20)
     ap.add_argument("--launches", type=int, default=3)
     ap.add_argument("--dtype", default="bf16", choices=["bf16", "f16"])
+    ap.add_argument("--streams", type=int, default=8)
+    ap.add_argument("--new", type=int, default=1)
+    ap.add_argument("--heads", type=int, default=32)
+    ap.add_argument("--kv-heads", type=int, default=32)
+    ap.add_argument("--head-dim", type=int, default=128)
+    ap.add_argument("--page", type=int, default=64)
     ap.add_argument("--fused", action="store_true",
                     help="layer case: outlier protection and final fit through cmpq_protect_and_quantize")
     ap.add_argument("--weighted", action="store_true",
@@ -214,6 +347,9 @@ def main():
     dt = inputs.BF16 if a.dtype == "bf16" else inputs.F16
     torch.cuda.set_device(int(os.environ.get("LOCAL_RANK", "0")))
     B.cmpq_set_lloyd_assignment(B.ASSIGN_ALL_PAIRS if a.assign == "all_pairs" else B.ASSIGN_ORDERED)
+    if a.case in ("linear8", "append8", "attend8", "serve"):
+        {"linear8": run_linear8, "serve": run_serve}.get(a.case, run_cache8)(a)
+        return
     if a.case == "layer":
         run_layer(a)
         return

@@ -110,3 +110,21 @@ def test_attention(L, p):
     size = B.cmpq_cache_attention_ws_bytes
     assert size(2, 3, 1, 100, 4, 3, 64) == 0 and size(-1, 3, 1, 100, 4, 2, 64) == 0 and size(2, 3, 1, 100, 4, 2, 0) == 0
     assert size(2, 3, 1, 100, 4, 2, 64) >= 256
+
+
+def test_extension_is_built_and_refuses_what_is_not_on_the_gpu(L, monkeypatch):
+    import torch
+
+    from paper_2410_13056_b200 import serving
+
+    assert serving._ext().__file__ == cuda_build.EXT_PATH
+    codes, scale = torch.zeros(4, 16, dtype=torch.int8), torch.zeros(4)
+    with pytest.raises(ValueError, match="CUDA"):
+        serving.Int8Linear(codes, scale)
+    pages, scales = torch.zeros(2, 1, 16, 64, dtype=torch.int8), torch.zeros(2, 1)
+    with pytest.raises(ValueError, match="CUDA"):
+        serving.PagedCache8(pages, scales, pages, scales)
+    monkeypatch.setattr(B, "_lib", None)
+    monkeypatch.setattr(B, "_LIB_PATH", "/nonexistent/libcmpq.so")
+    with pytest.raises(RuntimeError, match="missing"):
+        serving.Int8Linear(codes, scale)
