@@ -9,7 +9,7 @@ namespace cmpq {
 // A block takes 256 query rows of a sequence and key-value head (its new tokens times the query heads of the group,
 // next to each other, so that grouped heads share the keys) as two tiles of 128 and walks over the keys 128 at a time:
 //   4 warps   widen the tile's keys and values from int8 to fp16 into shared memory, a buffer ahead
-//   1 thread  issues S_w = Q_w K^T and O_w += P_w V for the two row tiles in turn
+//   1 thread  (of four warps, the others idle) issues S_w = Q_w K^T and O_w += P_w V for the two row tiles in turn
 //   2 x 4 warps, a thread per row: weights P_w = exp2(S_w - m) in fp16 over S_w's own TMEM columns
 // While one row tile's weights are made the other's products run.  TMEM holds S (2 x 128 columns) and O (2 x D).
 // The weights carry the value scale of their page relative to the largest of all pages that the block meets, as part
@@ -17,8 +17,11 @@ namespace cmpq {
 // when it has grown by more than 2^8, which fp16 has room for: then, rarely after the first tiles, O is multiplied in
 // TMEM.  Rows of keys and of queries keep the order of their entries 16 c + 8 p + e as plane p, group c, entry e, so
 // that the 16 codes a lane widens go to the same group of two planes and a row's lanes to different banks.
-constexpr int kPfKeys = 128, kPfThreads = 13 * 32;
+constexpr int kPfKeys = 128, kPfThreads = 16 * 32;
 constexpr float kPfSlack = 8.0f;
+// Registers a thread: launched with 128, four warps of each of the four groups; 2 x 168 + 112 + 64 = 4 x 128.
+constexpr int kPfRegsRows = 168, kPfRegsWiden = 112, kPfRegsOther = 64;
+static_assert(2 * kPfRegsRows + kPfRegsWiden + kPfRegsOther <= 4 * (65536 / kPfThreads), "shares of what the block is launched with");
 
 template <int D>
 struct Prefill {
@@ -157,8 +160,9 @@ attention_prefill_kernel(const __grid_constant__ AttnArgs A, const __grid_consta
     tc5::fence_after_sync();
     const uint32_t tmem = tmem_at, tmem_o = tmem + 256;
 
-    if (warp == 12) {
-        if (tc5::elect_one() && tiles > 0) {
+    if (warp >= 12) {
+        tc5::give_registers<kPfRegsOther>();
+        if (warp == 12 && tiles > 0 && tc5::elect_one()) {
             constexpr uint32_t kScores = tc5::idesc_f16(128, 128), kOut = tc5::idesc_f16(128, D) | tc5::kTransposedB;
             const uint32_t aq = tc5::smem_addr(sq), ak = tc5::smem_addr(sk), av = tc5::smem_addr(sv);
             auto scores = [&](int w, int t) {
@@ -228,6 +232,7 @@ attention_prefill_kernel(const __grid_constant__ AttnArgs A, const __grid_consta
         }
         __syncwarp();
     } else if (warp >= 8) {
+        tc5::give_registers<kPfRegsWiden>();
         // a row's lanes: D/16 of them, 16 codes each
         constexpr int kLanes = D / 16, kRows = 32 / kLanes, kSteps = 32 / kRows;  // rows of a warp at a time, times per tile
         const int w = warp - 8, c = lane % kLanes, q = lane / kLanes;
@@ -278,6 +283,7 @@ attention_prefill_kernel(const __grid_constant__ AttnArgs A, const __grid_consta
             if (t + 1 < tiles) fetch(A.c.v_codes, vc);
         }
     } else {
+        tc5::take_registers<kPfRegsRows>();
         const int w = warp >> 2, local = tid & 127, in_block = (two ? w : 0) * 128 + local, row = rb * 256 + in_block;
         const bool real = in_block < rows;
         const int i = row / g, h = head * g + row % g, pos = len - n + i;
@@ -500,60 +506,61 @@ attention_prefill_kernel(const __grid_constant__ AttnArgs A, const __grid_consta
             }
         }
         tc5::fence_before_sync();
+        if (splits > 1) {  // the block that adds a unit's last part joins them, in order, a thread per row
+            const int first_part = blockIdx.x - z;
+            asm volatile("bar.sync 1, 256;" ::: "memory");  // all rows' parts are written
+            if (tid == 0) {
+                __threadfence();
+                is_last = atomicAdd(A.counters + kPfCounters + unit, 1) == splits - 1;
+            }
+            asm volatile("bar.sync 1, 256;" ::: "memory");
+            if (is_last && tid < rows) {
+                __threadfence();
+                const float* parts = A.parts + (int64_t)first_part * (256 * (D + 2));
+                constexpr int kStep = 256 * (D + 2);
+                float m = -INFINITY, l = 0.0f, by[kPfSplits];
+#pragma unroll
+                for (int k = 0; k < kPfSplits; ++k) {
+                    by[k] = -INFINITY;
+                    if (k < splits) by[k] = reinterpret_cast<const float2*>(parts + k * kStep + 256 * D)[tid].x;
+                    m = fmaxf(m, by[k]);
+                }
+                const float at = m == -INFINITY ? 0.0f : m;
+#pragma unroll
+                for (int k = 0; k < kPfSplits; ++k) {
+                    by[k] = ex2(by[k] - at);
+                    if (k < splits) l = fmaf(by[k], reinterpret_cast<const float2*>(parts + k * kStep + 256 * D)[tid].y, l);
+                }
+                const int row = rb * 256 + tid, i = row / g, h = head * g + row % g;
+                const float f = l > 0.0f ? 1.0f / l : 0.0f;
+                uint16_t* dst = A.out + (int64_t)(first + i) * A.ldo + (int64_t)h * D;
+                for (int c = 0; c < D; c += 8) {
+                    float o[8] = {};
+#pragma unroll
+                    for (int k = 0; k < kPfSplits; ++k)
+                        if (k < splits) {
+                            const float4* p = reinterpret_cast<const float4*>(parts + k * kStep + tid * D + c);
+                            const float4 a = p[0], b = p[1];
+                            o[0] = fmaf(by[k], a.x, o[0]), o[1] = fmaf(by[k], a.y, o[1]), o[2] = fmaf(by[k], a.z, o[2]), o[3] = fmaf(by[k], a.w, o[3]);
+                            o[4] = fmaf(by[k], b.x, o[4]), o[5] = fmaf(by[k], b.y, o[5]), o[6] = fmaf(by[k], b.z, o[6]), o[7] = fmaf(by[k], b.w, o[7]);
+                        }
+                    uint32_t w[4];
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) w[k] = round16x2<DT>(o[2 * k] * f, o[2 * k + 1] * f);
+                    if (A.wide_o) {
+                        *reinterpret_cast<uint4*>(dst + c) = make_uint4(w[0], w[1], w[2], w[3]);
+                    } else {
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) dst[c + k] = (uint16_t)(w[k >> 1] >> (16 * (k & 1)));
+                    }
+                }
+                if (A.lse) A.lse[(int64_t)(first + i) * A.n_heads + h] = l > 0.0f ? (m + log2f(l)) * kLn2 : -INFINITY;
+            }
+            if (is_last && tid == 0) A.counters[kPfCounters + unit] = 0;
+        }
     }
     __syncwarp();
     __syncthreads();
-    if (splits > 1) {  // the block that adds a unit's last part joins them, in order, a thread per row
-        const int first_part = blockIdx.x - z;
-        if (tid == 0) {
-            __threadfence();
-            is_last = atomicAdd(A.counters + kPfCounters + unit, 1) == splits - 1;
-        }
-        __syncthreads();
-        if (is_last && tid < 256 && tid < rows) {
-            __threadfence();
-            const float* parts = A.parts + (int64_t)first_part * (256 * (D + 2));
-            constexpr int kStep = 256 * (D + 2);
-            float m = -INFINITY, l = 0.0f, by[kPfSplits];
-#pragma unroll
-            for (int k = 0; k < kPfSplits; ++k) {
-                by[k] = -INFINITY;
-                if (k < splits) by[k] = reinterpret_cast<const float2*>(parts + k * kStep + 256 * D)[tid].x;
-                m = fmaxf(m, by[k]);
-            }
-            const float at = m == -INFINITY ? 0.0f : m;
-#pragma unroll
-            for (int k = 0; k < kPfSplits; ++k) {
-                by[k] = ex2(by[k] - at);
-                if (k < splits) l = fmaf(by[k], reinterpret_cast<const float2*>(parts + k * kStep + 256 * D)[tid].y, l);
-            }
-            const int row = rb * 256 + tid, i = row / g, h = head * g + row % g;
-            const float f = l > 0.0f ? 1.0f / l : 0.0f;
-            uint16_t* dst = A.out + (int64_t)(first + i) * A.ldo + (int64_t)h * D;
-            for (int c = 0; c < D; c += 8) {
-                float o[8] = {};
-#pragma unroll
-                for (int k = 0; k < kPfSplits; ++k)
-                    if (k < splits) {
-                        const float4* p = reinterpret_cast<const float4*>(parts + k * kStep + tid * D + c);
-                        const float4 a = p[0], b = p[1];
-                        o[0] = fmaf(by[k], a.x, o[0]), o[1] = fmaf(by[k], a.y, o[1]), o[2] = fmaf(by[k], a.z, o[2]), o[3] = fmaf(by[k], a.w, o[3]);
-                        o[4] = fmaf(by[k], b.x, o[4]), o[5] = fmaf(by[k], b.y, o[5]), o[6] = fmaf(by[k], b.z, o[6]), o[7] = fmaf(by[k], b.w, o[7]);
-                    }
-                uint32_t w[4];
-#pragma unroll
-                for (int k = 0; k < 4; ++k) w[k] = round16x2<DT>(o[2 * k] * f, o[2 * k + 1] * f);
-                if (A.wide_o) {
-                    *reinterpret_cast<uint4*>(dst + c) = make_uint4(w[0], w[1], w[2], w[3]);
-                } else {
-#pragma unroll
-                    for (int k = 0; k < 8; ++k) dst[c + k] = (uint16_t)(w[k >> 1] >> (16 * (k & 1)));
-                }
-            }
-            if (A.lse) A.lse[(int64_t)(first + i) * A.n_heads + h] = l > 0.0f ? (m + log2f(l)) * kLn2 : -INFINITY;
-        }
-        if (is_last && tid == 0) A.counters[kPfCounters + unit] = 0;
-    }
     if (failed) {  // products and arrivals that were asked for have to end before the memory is given back
         if (tid == 0) {
             const long long start = clock64();
