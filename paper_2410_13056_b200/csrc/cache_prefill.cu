@@ -388,22 +388,21 @@ attention_prefill_kernel(const __grid_constant__ AttnArgs A, const __grid_consta
             const int key0 = (t0 + t) * kPfKeys;
             const int from = lo - key0, upto = hi - key0;
             auto tile = [&](auto masked) {
-                uint32_t x[2][32];
-                tc5::tmem_ld32(ts, x[0]);
-#pragma unroll
-                for (int step = 0; step < 4; ++step) {  // 32 keys: on two pages at most
-                    uint32_t(&v)[32] = x[step & 1];
+                #pragma unroll
+                for (int step = 0; step < 2; ++step) {  // 64 keys: on four pages at most
+                    uint32_t v[64];
+                    tc5::tmem_ld32(ts + step * 64, v);
+                    tc5::tmem_ld32(ts + step * 64 + 32, v + 32);
                     tc5::tmem_ld_wait();
-                    if (step < 3) tc5::tmem_ld32(ts + (step + 1) * 32, x[(step + 1) & 1]);
                     if (decltype(masked)::value) {
 #pragma unroll
-                        for (int j = 0; j < 32; ++j)
-                            if (step * 32 + j < from || step * 32 + j >= upto) v[j] = 0xff800000u;  // -infinity
+                        for (int j = 0; j < 64; ++j)
+                            if (step * 64 + j < from || step * 64 + j >= upto) v[j] = 0xff800000u;  // -infinity
                     }
-                    float f[2], add[2], top = -INFINITY;
+                    float f[4], add[4], top = -INFINITY;
 #pragma unroll
-                    for (int k = 0; k < 2; ++k) {
-                        f[k] = fmaxf(qs * __shfl_sync(0xffffffffu, sc.x, (step * 32 + k * 16) >> span_bits), 0x1p-126f);
+                    for (int k = 0; k < 4; ++k) {
+                        f[k] = fmaxf(qs * __shfl_sync(0xffffffffu, sc.x, (step * 64 + k * 16) >> span_bits), 0x1p-126f);
                         float most = fmaxf(__uint_as_float(v[k * 16]), __uint_as_float(v[k * 16 + 1]));
 #pragma unroll
                         for (int j = 2; j < 16; j += 2) most = fmaxf(fmaxf(most, __uint_as_float(v[k * 16 + j])), __uint_as_float(v[k * 16 + j + 1]));
@@ -414,13 +413,13 @@ attention_prefill_kernel(const __grid_constant__ AttnArgs A, const __grid_consta
                         const float now = grown ? top : m, keep = grown ? ex2(m - now) : 1.0f;
                         m = now;
                         l *= keep;
-                        rescale(t, step, keep);
+                        rescale(t, 2 * step, keep);
                     }
                     const float at = m == -INFINITY ? 0.0f : m;
-                    uint32_t y[16];
+                    uint32_t y[32];
 #pragma unroll
-                    for (int k = 0; k < 2; ++k) {
-                        const int page = (step * 32 + k * 16) >> span_bits;
+                    for (int k = 0; k < 4; ++k) {
+                        const int page = (step * 64 + k * 16) >> span_bits;
                         add[k] = __shfl_sync(0xffffffffu, bias, page) - at;
                         const uint64_t ff = pair(f[k], f[k]), aa = pair(add[k], add[k]);
                         uint64_t sum = 0;
@@ -433,7 +432,7 @@ attention_prefill_kernel(const __grid_constant__ AttnArgs A, const __grid_consta
                         }
                         l = fmaf(low(sum) + high(sum), __shfl_sync(0xffffffffu, inv_vs, page), l);
                     }
-                    tc5::tmem_st16(ts + step * 16, y);
+                    tc5::tmem_st32(ts + step * 32, y);
                 }
             };
             if (key0 + kPfKeys > all_hi || key0 < all_lo)
