@@ -103,7 +103,8 @@ __device__ __forceinline__ void store_row(Columns columns, float f, bool real, f
     }
 }
 
-template <int DT, int D>
+// PAGES: pages that 64 neighbouring keys lie on at most.
+template <int DT, int D, int PAGES>
 __global__ void __launch_bounds__(kPfThreads, 1)
 attention_prefill_kernel(const __grid_constant__ AttnArgs A, const __grid_constant__ PrefillPlan plan) {
     using C = Prefill<D>;
@@ -389,7 +390,8 @@ attention_prefill_kernel(const __grid_constant__ AttnArgs A, const __grid_consta
             const int from = lo - key0, upto = hi - key0;
             auto tile = [&](auto masked) {
                 #pragma unroll
-                for (int step = 0; step < 2; ++step) {  // 64 keys: on four pages at most
+                for (int step = 0; step < 2; ++step) {  // 64 keys, on PAGES pages at most
+                    constexpr int kCols = 64 / PAGES;
                     uint32_t v[64];
                     tc5::tmem_ld32(ts + step * 64, v);
                     tc5::tmem_ld32(ts + step * 64 + 32, v + 32);
@@ -399,14 +401,16 @@ attention_prefill_kernel(const __grid_constant__ AttnArgs A, const __grid_consta
                         for (int j = 0; j < 64; ++j)
                             if (step * 64 + j < from || step * 64 + j >= upto) v[j] = 0xff800000u;  // -infinity
                     }
-                    float f[4], add[4], top = -INFINITY;
+                    float f[PAGES], top = -INFINITY;
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        f[k] = fmaxf(qs * __shfl_sync(0xffffffffu, sc.x, (step * 64 + k * 16) >> span_bits), 0x1p-126f);
-                        float most = fmaxf(__uint_as_float(v[k * 16]), __uint_as_float(v[k * 16 + 1]));
+                    for (int k = 0; k < PAGES; ++k) {
+                        f[k] = fmaxf(qs * __shfl_sync(0xffffffffu, sc.x, (step * 64 + k * kCols) >> span_bits), 0x1p-126f);
+                        float most[4];  // side by side
 #pragma unroll
-                        for (int j = 2; j < 16; j += 2) most = fmaxf(fmaxf(most, __uint_as_float(v[k * 16 + j])), __uint_as_float(v[k * 16 + j + 1]));
-                        top = fmaxf(top, most * f[k]);
+                        for (int j = 0; j < 4; ++j) most[j] = __uint_as_float(v[k * kCols + j]);
+#pragma unroll
+                        for (int j = 4; j < kCols; j += 2) most[j >> 1 & 3] = fmaxf(fmaxf(most[j >> 1 & 3], __uint_as_float(v[k * kCols + j])), __uint_as_float(v[k * kCols + j + 1]));
+                        top = fmaxf(top, fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3])) * f[k]);
                     }
                     const bool grown = top > m + kPfSlack;
                     if (__any_sync(0xffffffffu, grown)) {
@@ -418,19 +422,20 @@ attention_prefill_kernel(const __grid_constant__ AttnArgs A, const __grid_consta
                     const float at = m == -INFINITY ? 0.0f : m;
                     uint32_t y[32];
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        const int page = (step * 64 + k * 16) >> span_bits;
-                        add[k] = __shfl_sync(0xffffffffu, bias, page) - at;
-                        const uint64_t ff = pair(f[k], f[k]), aa = pair(add[k], add[k]);
-                        uint64_t sum = 0;
+                    for (int k = 0; k < PAGES; ++k) {
+                        const int page = (step * 64 + k * kCols) >> span_bits;
+                        const float add = __shfl_sync(0xffffffffu, bias, page) - at;
+                        const uint64_t ff = pair(f[k], f[k]), aa = pair(add, add);
+                        uint64_t sum[2] = {0, 0};
 #pragma unroll
-                        for (int j = 0; j < 16; j += 2) {
-                            const uint64_t z = fma2(pair(__uint_as_float(v[k * 16 + j]), __uint_as_float(v[k * 16 + j + 1])), ff, aa);
+                        for (int j = 0; j < kCols; j += 2) {
+                            const uint64_t z = fma2(pair(__uint_as_float(v[k * kCols + j]), __uint_as_float(v[k * kCols + j + 1])), ff, aa);
                             const float a = ex2(low(z)), b = ex2(high(z));
-                            sum = add2(sum, pair(a, b));
-                            y[k * 8 + j / 2] = round16x2<CMPQ_F16>(a, b);
+                            sum[j >> 1 & 1] = add2(sum[j >> 1 & 1], pair(a, b));
+                            y[(k * kCols + j) / 2] = round16x2<CMPQ_F16>(a, b);
                         }
-                        l = fmaf(low(sum) + high(sum), __shfl_sync(0xffffffffu, inv_vs, page), l);
+                        const uint64_t both = add2(sum[0], sum[1]);
+                        l = fmaf(low(both) + high(both), __shfl_sync(0xffffffffu, inv_vs, page), l);
                     }
                     tc5::tmem_st32(ts + step * 32, y);
                 }
@@ -571,10 +576,10 @@ attention_prefill_kernel(const __grid_constant__ AttnArgs A, const __grid_consta
     if (warp == 12) tc5::tmem_free<1>(tmem, 512);
 }
 
-template <int DT, int D>
+template <int DT, int D, int PAGES>
 static cmpq_status launch_prefill_of(const AttnArgs& a, cudaStream_t st) {
     static bool raised[64];
-    if (!raise_smem_limit_once(attention_prefill_kernel<DT, D>, Prefill<D>::kSmem, raised)) return CMPQ_ERR_CUDA;
+    if (!raise_smem_limit_once(attention_prefill_kernel<DT, D, PAGES>, Prefill<D>::kSmem, raised)) return CMPQ_ERR_CUDA;
     const int64_t row_blocks = ((int64_t)a.max_new * a.group + 255) / 256, per = a.b.n_seq * a.c.n_kv_heads, units = row_blocks * per, sms = sm_count();
     // Fewer units than SMs: each is split over the keys, three tiles of them to a block at least.  Splitting the last round
     // of many does not pay: 2 x 2048 queries, 32 heads (512 units, 3.5 rounds) took 334 us so, and 314 whole, since the
@@ -583,16 +588,20 @@ static cmpq_status launch_prefill_of(const AttnArgs& a, cudaStream_t st) {
     const int64_t blocks = units * splits;
     if (blocks > INT32_MAX) return CMPQ_ERR_UNSUPPORTED;
     const PrefillPlan plan{(int)row_blocks, (int)per, splits};
-    attention_prefill_kernel<DT, D><<<(unsigned)blocks, kPfThreads, Prefill<D>::kSmem, st>>>(a, plan);
+    attention_prefill_kernel<DT, D, PAGES><<<(unsigned)blocks, kPfThreads, Prefill<D>::kSmem, st>>>(a, plan);
     return launch_status();
 }
 
 size_t prefill_parts_bytes(int d) { return d > 128 ? 0 : (size_t)std::max(1, sm_count()) * 256 * (d + 2) * sizeof(float); }
 
 cmpq_status launch_prefill(const AttnArgs& a, cmpq_dtype dt, cudaStream_t st) {
-    const bool bf = dt == CMPQ_BF16;
-    if (a.c.head_dim == 64) return bf ? launch_prefill_of<CMPQ_BF16, 64>(a, st) : launch_prefill_of<CMPQ_F16, 64>(a, st);
-    return bf ? launch_prefill_of<CMPQ_BF16, 128>(a, st) : launch_prefill_of<CMPQ_F16, 128>(a, st);
+    const bool bf = dt == CMPQ_BF16, small = a.c.page_tokens < 64;
+    if (a.c.head_dim == 64) {
+        if (small) return bf ? launch_prefill_of<CMPQ_BF16, 64, 4>(a, st) : launch_prefill_of<CMPQ_F16, 64, 4>(a, st);
+        return bf ? launch_prefill_of<CMPQ_BF16, 64, 1>(a, st) : launch_prefill_of<CMPQ_F16, 64, 1>(a, st);
+    }
+    if (small) return bf ? launch_prefill_of<CMPQ_BF16, 128, 4>(a, st) : launch_prefill_of<CMPQ_F16, 128, 4>(a, st);
+    return bf ? launch_prefill_of<CMPQ_BF16, 128, 1>(a, st) : launch_prefill_of<CMPQ_F16, 128, 1>(a, st);
 }
 
 }  // namespace cmpq
