@@ -333,20 +333,22 @@ attention_prefill_kernel(const __grid_constant__ AttnArgs A, const __grid_consta
         const float inv_ref = ref > 0.0f ? 1.0f / ref : 0.0f;
         const uint32_t lanes = (uint32_t)(warp & 3) << 21, ts = tmem + w * 128 + lanes, to = tmem_o + w * 128 + lanes;
         const int span_bits = min(7, page_bits), per_tile = kPfKeys >> span_bits;
-        // lane k holds the scales of the tile's k-th page, those of the next tile are under way
+        // Lane k holds the scales of the tile's k-th page.  Those of the next tile are under way, and so is the look-up of the
+        // page in the tile behind that: neither is waited for (one look-up at a time stalled each tile for a memory latency).
         float2 sc, sc_next = make_float2(0.0f, 0.0f);
-        auto scales = [&](int t) {
-            float2 x = make_float2(0.0f, 0.0f);
-            if (lane < per_tile) {
-                const int id = page_of(((t0 + t) * kPfKeys >> page_bits) + lane);
-                if (id >= 0) x = make_float2(__ldg(A.c.k_scale + (int64_t)id * H + head), __ldg(A.c.v_scale + (int64_t)id * H + head));
-            }
-            return x;
+        int id_next = -1;
+        auto look_up = [&](int t) {  // not looked at here; the warps that widen the codes report what is no page
+            const int page = ((t0 + t) * kPfKeys >> page_bits) + lane;
+            return lane < per_tile && t < tiles && page < min(pages, (int)min((int64_t)INT32_MAX, A.b.ld_table)) ? __ldg(table + page) : -1;
+        };
+        auto scales = [&](int id) {
+            return id < 0 || id >= A.c.n_pages ? make_float2(0.0f, 0.0f)
+                                               : make_float2(__ldg(A.c.k_scale + (int64_t)id * H + head), __ldg(A.c.v_scale + (int64_t)id * H + head));
         };
         // with one row tile the second four warps take every other tile of keys
         const int t_first = two ? 0 : w, t_step = two ? 1 : 2;
         const bool work = t_first < tiles;
-        if (work) sc_next = scales(t_first);
+        if (work) sc_next = scales(look_up(t_first)), id_next = look_up(t_first + t_step);
         float m = -INFINITY, l = 0.0f;
         // keys [lo, hi) are seen by this row; a tile inside [all_lo, all_hi) is seen whole by the warp's rows
         const int hi = real ? (A.causal ? min(len, pos + 1) : len) : INT32_MAX, lo = real && A.window > 0 ? pos - A.window + 1 : 0;
@@ -383,7 +385,8 @@ attention_prefill_kernel(const __grid_constant__ AttnArgs A, const __grid_consta
         for (int t = t_first; t < tiles; t += t_step) {
             sc = sc_next;
             const float vs = fmaxf(sc.y * inv_ref, 0x1p-100f), bias = log2f(vs), inv_vs = 1.0f / vs;
-            if (t + t_step < tiles) sc_next = scales(t + t_step);
+            sc_next = scales(id_next);
+            id_next = look_up(t + 2 * t_step);
             if (!(ok = tc5::mbar_wait(s_full + w, (two ? t : t >> 1) & 1, &failed))) break;
             tc5::fence_after_sync();
             const int key0 = (t0 + t) * kPfKeys;
