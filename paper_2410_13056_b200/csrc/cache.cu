@@ -2,6 +2,7 @@
 #include <algorithm>
 
 #include "cache.cuh"
+#include "tc5.cuh"
 
 namespace cmpq {
 
@@ -181,6 +182,7 @@ __device__ __forceinline__ void query_block(const AppendArgs& A, int block) {
 template <int DT>
 __global__ void __launch_bounds__(256)
 cache_queries_any_kernel(const __grid_constant__ AppendArgs A) {
+    tc5::chained();
     query_block<DT>(A, blockIdx.x);
 }
 
@@ -189,6 +191,7 @@ cache_queries_any_kernel(const __grid_constant__ AppendArgs A) {
 template <int DT>
 __global__ void __launch_bounds__(256, 4)
 cache_queries_kernel(const __grid_constant__ AppendArgs A) {
+    tc5::chained();
     const int D = A.c.head_dim, U = D / 16, half = A.rot / 2, tid = threadIdx.x, u = tid % U, h0 = tid / U, heads = 256 / U;
     const int32_t* off = A.b.tok_off;
     const Unit at(u, A.rot, A.interleaved);
@@ -293,6 +296,7 @@ __device__ __forceinline__ void scale_again(int8_t* codes, int count, float by) 
 template <int DT, int NIT, int THREADS>
 __global__ void __launch_bounds__(THREADS)
 cache_append_kernel(const __grid_constant__ AppendArgs A) {
+    tc5::chained();
     if (THREADS == 32 && blockIdx.x >= A.kv_blocks) {
         query_block<DT>(A, blockIdx.x - A.kv_blocks);
         return;
@@ -365,6 +369,7 @@ cache_append_kernel(const __grid_constant__ AppendArgs A) {
 template <int DT, int NIT, int THREADS>
 __global__ void __launch_bounds__(THREADS)
 cache_fill_kernel(const __grid_constant__ AppendArgs A) {
+    tc5::chained();
     const int D = A.c.head_dim, P = A.c.page_tokens, U = D / 16, H = A.c.n_kv_heads, tid = threadIdx.x;
     const int u = tid % U, r0 = tid / U, rows_at_once = THREADS / U;
     const bool is_v = blockIdx.x & 1;
@@ -455,6 +460,7 @@ struct ReadArgs {
 template <int DT, int TOKENS>
 __global__ void __launch_bounds__(256)
 cache_read_kernel(const __grid_constant__ ReadArgs A) {
+    tc5::chained();
     const int D = A.c.head_dim, P = A.c.page_tokens, H = A.c.n_kv_heads, G = D / 16;
     const int32_t* off = A.b.tok_off;
     const int64_t t0 = (int64_t)blockIdx.x * TOKENS;
@@ -512,35 +518,34 @@ cache_read_kernel(const __grid_constant__ ReadArgs A) {
     }
 }
 
-template <int DT>
-static void launch_append(const AppendArgs& a, unsigned q_blocks, cudaStream_t st) {
-    const unsigned kv = a.kv_blocks;
-    if (a.few) {
-        cache_append_kernel<DT, 2, 32><<<kv + q_blocks, 32, 0, st>>>(a);
-        return;
-    }
-    if (a.groups && a.wide_k && a.wide_v) {
-        const int units = a.c.head_dim * a.c.page_tokens / 16;
-        if (units <= 256) cache_fill_kernel<DT, 1, 256><<<kv, 256, 0, st>>>(a);
-        else if (units == 512) cache_fill_kernel<DT, 2, 256><<<kv, 256, 0, st>>>(a);
-        else if (units == 1024) cache_fill_kernel<DT, 2, 512><<<kv, 512, 0, st>>>(a);
-        else cache_fill_kernel<DT, 4, 512><<<kv, 512, 0, st>>>(a);
-    } else {
-        cache_append_kernel<DT, 2, 256><<<kv, 256, 0, st>>>(a);
-    }
-    if (q_blocks && a.groups && a.wide_q)
-        cache_queries_kernel<DT><<<q_blocks, 256, 0, st>>>(a);
-    else if (q_blocks)
-        cache_queries_any_kernel<DT><<<q_blocks, 256, 0, st>>>(a);
+template <class Kernel, class Args>
+static cmpq_status launch(Kernel kernel, unsigned blocks, int threads, const Args& a, cudaStream_t st) {
+    return launch_cluster(kernel, blocks, threads, 0, 1, true, st, a);
 }
 
 template <int DT>
-static void launch_read(const ReadArgs& a, cudaStream_t st) {
+static cmpq_status launch_append(const AppendArgs& a, unsigned q_blocks, cudaStream_t st) {
+    const unsigned kv = a.kv_blocks;
+    if (a.few) return launch(cache_append_kernel<DT, 2, 32>, kv + q_blocks, 32, a, st);
+    cmpq_status done;
+    if (a.groups && a.wide_k && a.wide_v) {
+        const int units = a.c.head_dim * a.c.page_tokens / 16;
+        done = units <= 256    ? launch(cache_fill_kernel<DT, 1, 256>, kv, 256, a, st)
+               : units == 512  ? launch(cache_fill_kernel<DT, 2, 256>, kv, 256, a, st)
+               : units == 1024 ? launch(cache_fill_kernel<DT, 2, 512>, kv, 512, a, st)
+                               : launch(cache_fill_kernel<DT, 4, 512>, kv, 512, a, st);
+    } else {
+        done = launch(cache_append_kernel<DT, 2, 256>, kv, 256, a, st);
+    }
+    if (done != CMPQ_OK || !q_blocks) return done;
+    return a.groups && a.wide_q ? launch(cache_queries_kernel<DT>, q_blocks, 256, a, st) : launch(cache_queries_any_kernel<DT>, q_blocks, 256, a, st);
+}
+
+template <int DT>
+static cmpq_status launch_read(const ReadArgs& a, cudaStream_t st) {
     // four tokens to a block once that leaves blocks enough
-    if (a.b.n_tok >= 4096)
-        cache_read_kernel<DT, 4><<<(unsigned)((a.b.n_tok + 3) / 4), 256, 0, st>>>(a);
-    else
-        cache_read_kernel<DT, 1><<<(unsigned)a.b.n_tok, 256, 0, st>>>(a);
+    return a.b.n_tok >= 4096 ? launch(cache_read_kernel<DT, 4>, (unsigned)((a.b.n_tok + 3) / 4), 256, a, st)
+                             : launch(cache_read_kernel<DT, 1>, (unsigned)a.b.n_tok, 256, a, st);
 }
 
 }  // namespace cmpq
@@ -598,11 +603,7 @@ extern "C" cmpq_status cmpq_cache_append(const cmpq_cache* cache, const cmpq_bat
     if (kv + q_blocks > INT32_MAX) return CMPQ_ERR_UNSUPPORTED;
     a.kv_blocks = (unsigned)kv;
     auto st = static_cast<cudaStream_t>(stream);
-    if (dt == CMPQ_BF16)
-        launch_append<CMPQ_BF16>(a, (unsigned)q_blocks, st);
-    else
-        launch_append<CMPQ_F16>(a, (unsigned)q_blocks, st);
-    return launch_status();
+    return dt == CMPQ_BF16 ? launch_append<CMPQ_BF16>(a, (unsigned)q_blocks, st) : launch_append<CMPQ_F16>(a, (unsigned)q_blocks, st);
 }
 
 extern "C" cmpq_status cmpq_cache_read(const cmpq_cache* cache, const cmpq_batch* batch, cmpq_dtype dt, void* k_out,
@@ -616,9 +617,5 @@ extern "C" cmpq_status cmpq_cache_read(const cmpq_cache* cache, const cmpq_batch
     ReadArgs a{*cache, *batch, static_cast<uint16_t*>(k_out), static_cast<uint16_t*>(v_out), ldo,
                aligned_to(k_out, 16) && aligned_to(v_out, 16) && ldo % 8 == 0, word};
     auto st = static_cast<cudaStream_t>(stream);
-    if (dt == CMPQ_BF16)
-        launch_read<CMPQ_BF16>(a, st);
-    else
-        launch_read<CMPQ_F16>(a, st);
-    return launch_status();
+    return dt == CMPQ_BF16 ? launch_read<CMPQ_BF16>(a, st) : launch_read<CMPQ_F16>(a, st);
 }

@@ -196,6 +196,7 @@ attention_rows_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_con
         tc5::mbar_init_fence();
     }
 
+    tc5::chained();
     // The total, this warp's run, and the sequence it starts in: every warp for itself, 32 sequences at a time.
     int64_t total = 0, mine = 0, upto = 0;
     for (int64_t at = 0; at < A.b.n_seq; at += 32) {
@@ -635,8 +636,7 @@ static cmpq_status launch_rows(AttnArgs a, cudaStream_t st) {
     if (!raise_smem_limit_once(attention_rows_kernel<DT, D, NT>, C::kSmem, raised)) return CMPQ_ERR_CUDA;
     const int blocks = std::min(sm_count() * C::kPerSm, kMaxBlocks);
     a.workers = blocks * C::kWarps;
-    attention_rows_kernel<DT, D, NT><<<blocks, 32 * C::kWarps, C::kSmem, st>>>(kmap, vmap, a);
-    return launch_status();
+    return launch_cluster(attention_rows_kernel<DT, D, NT>, blocks, 32 * C::kWarps, C::kSmem, 1, true, st, kmap, vmap, a);
 }
 
 template <int DT, int D>

@@ -119,6 +119,7 @@ attention_prefill_kernel(const __grid_constant__ AttnArgs A, const __grid_consta
     __shared__ float2 half_ml[128];
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int H = A.c.n_kv_heads, g = A.group, page_bits = A.page_bits;
+    tc5::chained();
     // the last row blocks see most keys and come first
     const int splits = plan.splits, unit = blockIdx.x / splits, z = blockIdx.x % splits;
     const int rb = plan.row_blocks - 1 - unit / plan.per_row_block, s = unit % plan.per_row_block / H, head = unit % H;
@@ -591,8 +592,7 @@ static cmpq_status launch_prefill_of(const AttnArgs& a, cudaStream_t st) {
     const int64_t blocks = units * splits;
     if (blocks > INT32_MAX) return CMPQ_ERR_UNSUPPORTED;
     const PrefillPlan plan{(int)row_blocks, (int)per, splits};
-    attention_prefill_kernel<DT, D, PAGES><<<(unsigned)blocks, kPfThreads, Prefill<D>::kSmem, st>>>(a, plan);
-    return launch_status();
+    return launch_cluster(attention_prefill_kernel<DT, D, PAGES>, (unsigned)blocks, kPfThreads, Prefill<D>::kSmem, 1, true, st, a, plan);
 }
 
 size_t prefill_parts_bytes(int d) { return d > 128 ? 0 : (size_t)std::max(1, sm_count()) * 256 * (d + 2) * sizeof(float); }

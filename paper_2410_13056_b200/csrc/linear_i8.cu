@@ -44,7 +44,7 @@ template <int DT, int KEEP>
 __global__ void __launch_bounds__(kQtThreads)
 quantize_tokens_kernel(const uint16_t* __restrict__ X, int64_t d, int64_t ldx, int wide, int8_t* __restrict__ codes,
                        int64_t ldc, float* __restrict__ scale, int32_t* __restrict__ nonfinite) {
-    tc5::dependents_may_start();
+    tc5::chained();
     const uint16_t* row = X + blockIdx.x * ldx;
     int8_t* out = codes + blockIdx.x * ldc;
     const int t = threadIdx.x;
@@ -152,6 +152,7 @@ matmul_i8_tile_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_con
     __shared__ int failed;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int nt = blockIdx.x / A.m_tiles, mt = blockIdx.x % A.m_tiles, bn = A.bn;
+    tc5::dependents_may_start();
     const int a_bytes = A.rows * 128, stage = a_bytes + bn * 128, columns = bn <= 32 ? 32 : bn <= 64 ? 64 : bn <= 128 ? 128 : 256;
     if (threadIdx.x < A.stages) tc5::mbar_init(full + threadIdx.x, 1), tc5::mbar_init(empty + threadIdx.x, 1);
     if (threadIdx.x == 0) tc5::mbar_init(&done, 1), failed = 0;
@@ -249,6 +250,7 @@ matmul_i8_pair_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_con
     __shared__ int failed;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int rank = (int)tc5::cluster_rank();
+    tc5::dependents_may_start();
     const int tiles = A.n_tiles * A.m_tiles, first = blockIdx.x >> 1, step = gridDim.x >> 1;
     if (threadIdx.x == 0) {
         for (int i = 0; i < kPairStages; ++i) tc5::mbar_init(full + i, 1), tc5::mbar_init(empty + i, 1);
@@ -412,12 +414,14 @@ extern "C" cmpq_status cmpq_quantize_tokens(const void* X, cmpq_dtype dt, int64_
     auto st = static_cast<cudaStream_t>(stream);
     const unsigned rows = (unsigned)n;
     const int64_t keep = (d + 8 * kQtThreads - 1) / (8 * kQtThreads);
-    auto launch = [&](auto kernel) { kernel<<<rows, kQtThreads, 0, st>>>(x, d, ldx, wide, codes, ldc, scale, nonfinite); };
+    auto launch = [&](auto kernel) { return launch_cluster(kernel, rows, kQtThreads, 0, 1, true, st, x, d, ldx, wide, codes, ldc, scale, nonfinite); };
     if (dt == CMPQ_BF16)
-        keep <= 2 ? launch(quantize_tokens_kernel<CMPQ_BF16, 2>) : keep <= 4 ? launch(quantize_tokens_kernel<CMPQ_BF16, 4>) : launch(quantize_tokens_kernel<CMPQ_BF16, 8>);
-    else
-        keep <= 2 ? launch(quantize_tokens_kernel<CMPQ_F16, 2>) : keep <= 4 ? launch(quantize_tokens_kernel<CMPQ_F16, 4>) : launch(quantize_tokens_kernel<CMPQ_F16, 8>);
-    return launch_status();
+        return keep <= 2   ? launch(quantize_tokens_kernel<CMPQ_BF16, 2>)
+               : keep <= 4 ? launch(quantize_tokens_kernel<CMPQ_BF16, 4>)
+                           : launch(quantize_tokens_kernel<CMPQ_BF16, 8>);
+    return keep <= 2   ? launch(quantize_tokens_kernel<CMPQ_F16, 2>)
+           : keep <= 4 ? launch(quantize_tokens_kernel<CMPQ_F16, 4>)
+                       : launch(quantize_tokens_kernel<CMPQ_F16, 8>);
 }
 
 // The caller has checked everything.  The last 256 bytes of the work space take the mark of a kernel that gave up.
