@@ -8,16 +8,20 @@ namespace cmpq {
 
 constexpr int kQtThreads = 256;
 
+// The larger magnitudes of two packed pairs, entry by entry; a NaN stays.
 template <int DT>
-__device__ __forceinline__ uint32_t group_max(uint4 g) {
-    uint32_t m = 0;
-    const uint32_t w[4] = {g.x, g.y, g.z, g.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const float2 f = widen16x2<DT>(w[i]);
-        m = max(m, max(__float_as_uint(f.x) & 0x7fffffffu, __float_as_uint(f.y) & 0x7fffffffu));
+__device__ __forceinline__ uint32_t larger2(uint32_t a, uint32_t b) {
+    if (DT == CMPQ_BF16) {
+        const __nv_bfloat162 m = __hmax2_nan(*reinterpret_cast<const __nv_bfloat162*>(&a), __habs2(*reinterpret_cast<const __nv_bfloat162*>(&b)));
+        return *reinterpret_cast<const uint32_t*>(&m);
+    } else {
+        const __half2 m = __hmax2_nan(*reinterpret_cast<const __half2*>(&a), __habs2(*reinterpret_cast<const __half2*>(&b)));
+        return *reinterpret_cast<const uint32_t*>(&m);
     }
-    return m;
+}
+template <int DT>
+__device__ __forceinline__ uint32_t group_max(uint32_t m, uint4 g) {
+    return larger2<DT>(larger2<DT>(larger2<DT>(larger2<DT>(m, g.x), g.y), g.z), g.w);
 }
 
 // Codes of eight entries.  |x * inv| is at most 127 (1 + 2^-22) here, so adding 1.5 * 2^23 leaves the integer that
@@ -36,8 +40,9 @@ __device__ __forceinline__ uint2 group_codes(uint4 g, float inv) {
     return make_uint2(__byte_perm(c[0], c[1], 0x5410), __byte_perm(c[2], c[3], 0x5410));
 }
 
-// One block per token.  The magnitudes are compared as bit patterns, where a NaN is larger than infinity and
-// infinity larger than every number, so the maximum also tells whether the row is finite.  A thread keeps
+// One block per token.  Magnitudes are compared two at a time in their own type and, between lanes, as bit patterns,
+// where a NaN is larger than infinity and infinity larger than every number: the maximum also tells whether the row is
+// finite.  A thread keeps
 // KEEP groups of eight in registers, chosen by the row's length so that more blocks share an SM where rows are short;
 // rows of up to 16384 entries are read once, the rest of a longer one is read again.
 template <int DT, int KEEP>
@@ -58,21 +63,21 @@ quantize_tokens_kernel(const uint16_t* __restrict__ X, int64_t d, int64_t ldx, i
         if (g < groups) keep[i] = load8(row + 8 * g, d - 8 * g, wide);
     }
 #pragma unroll
-    for (int i = 0; i < KEEP; ++i) m = max(m, group_max<DT>(keep[i]));
+    for (int i = 0; i < KEEP; ++i) m = group_max<DT>(m, keep[i]);
     for (int64_t g = t + (int64_t)KEEP * kQtThreads; g < groups; g += kQtThreads)
-        m = max(m, group_max<DT>(load8(row + 8 * g, d - 8 * g, wide)));
+        m = group_max<DT>(m, load8(row + 8 * g, d - 8 * g, wide));
     __shared__ uint32_t part[kQtThreads / 32];
-    m = __reduce_max_sync(0xffffffffu, m);
+    m = __reduce_max_sync(0xffffffffu, max(m & 0x7fffu, m >> 16 & 0x7fffu));  // of magnitudes, as bit patterns
     if ((t & 31) == 0) part[t >> 5] = m;
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < kQtThreads / 32; ++i) m = max(m, part[i]);
-    const float amax = __uint_as_float(m);
+    const float amax = widen16<DT>((uint16_t)m);
     float s = amax * (1.0f / 127.0f), inv = 1.0f / s;
     if (amax < 0x1p-120f) s = inv = 0.0f;
     if (t == 0) {
         scale[blockIdx.x] = s;
-        if (m >= 0x7f800000u && nonfinite) atomicOr(nonfinite, 1);
+        if (m >= (DT == CMPQ_BF16 ? 0x7f80u : 0x7c00u) && nonfinite) atomicOr(nonfinite, 1);
     }
 #pragma unroll
     for (int i = 0; i < KEEP; ++i) {
