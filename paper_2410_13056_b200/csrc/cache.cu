@@ -367,7 +367,7 @@ cache_append_kernel(const __grid_constant__ AppendArgs A) {
 // 16 entries of NIT rows in each.  The place is looked up and the cosines and sines are read once for all heads, and the
 // next head's entries and scale are on their way while this one's are turned, compared and written.
 template <int DT, int NIT, int THREADS>
-__global__ void __launch_bounds__(THREADS)
+__global__ void __launch_bounds__(THREADS, THREADS == 512 ? 1 : NIT == 1 ? 3 : 2)
 cache_fill_kernel(const __grid_constant__ AppendArgs A) {
     tc5::chained();
     const int D = A.c.head_dim, P = A.c.page_tokens, U = D / 16, H = A.c.n_kv_heads, tid = threadIdx.x;
