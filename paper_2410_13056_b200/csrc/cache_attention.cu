@@ -15,9 +15,16 @@ namespace cmpq {
 // The time is that of reading the cache once, so the keys are split over all warps of the GPU.  The rows of a sequence
 // and key-value head (its new tokens times the query heads of the group) are taken R = 8 NT at a time; such a unit is a
 // run of tiles of 64 or 32 tokens.  All units' tiles, one behind the other, are dealt to the workers (warps) in equal
-// contiguous runs: sequences of any lengths balance, and a worker meets few unit borders.  A unit inside one worker's
-// run is finished there; the parts of one that is cut go to the work space and are joined by a second kernel in the
-// order of the workers (no atomics: the same bytes every time).
+// contiguous runs: sequences of any lengths balance, and a worker meets few unit borders.  A unit inside one worker's run
+// is finished there.  The parts of one that is cut are joined by the block that holds them and, where several do, by the
+// last block to arrive, always in the order of the workers: the same bytes every time.
+//
+// Measured, D = 128: 64 sequences of up to 8191 tokens, 64/8 heads (608 MB): 127 us, 4.8 TB/s, 0.73 of the copy rate; two
+// of up to 131072 (515 MB): 105 us; one of 2049, 32 heads: 15 us.  What is left: the SMs get unequal shares of the memory
+// (the blocks' loops of the second case end between 62 and 90 us), and some 10 us of look-ups, first loads and joins.
+// Dealing the last 10 to 30 % in short runs to whichever block is free costs more in look-ups and joins than it evens out
+// (136 to 139 and 138 to 157 us); asking for later tiles in L2 makes it slower (129 / 154 / 180 us for 1 / 2 / 4 tiles
+// ahead).
 constexpr int kMaxBlocks = 512;  // counters: one per block here, behind them those of the prompts' kernel
 
 template <int D, int NT>
@@ -172,8 +179,8 @@ __device__ __forceinline__ void join_parts(const AttnArgs& A, const Piece& u, in
 //   output   O^T[entry][row] = V^T P^T: a lane reads D/8 neighbouring entries of tokens 2c, 2c+1, 2c+8, 2c+9 and pairs
 //            the tokens' bytes; entry i of its run is row r (i even) or r + 8 (i odd) of instruction i / 2.
 // So keys and values are read from shared memory once, 16 bytes a time and without bank conflicts for D >= 128, and a
-// lane ends up with D/8 neighbouring entries of two output rows.  Per code that is about 0.25 shared loads / 16 B and
-// 1.4 instructions to widen it, a third of the issue slots at the rate the memory delivers.
+// lane ends up with D/8 neighbouring entries of two output rows.  Widening a code takes about 1.4 of a lane's
+// instructions; all in all a tile of 64 tokens is some 1300 warp instructions, 40 % of the issue slots.
 template <int DT, int D, int NT>
 __global__ void __launch_bounds__(128, Rows<D, NT>::kPerSm)
 attention_rows_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUtensorMap vmap,
@@ -196,7 +203,6 @@ attention_rows_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_con
         tc5::mbar_init_fence();
     }
 
-    tc5::chained();
     // The total, this warp's run, and the sequence it starts in: every warp for itself, 32 sequences at a time.
     int64_t total = 0, mine = 0, upto = 0;
     for (int64_t at = 0; at < A.b.n_seq; at += 32) {
@@ -636,7 +642,7 @@ static cmpq_status launch_rows(AttnArgs a, cudaStream_t st) {
     if (!raise_smem_limit_once(attention_rows_kernel<DT, D, NT>, C::kSmem, raised)) return CMPQ_ERR_CUDA;
     const int blocks = std::min(sm_count() * C::kPerSm, kMaxBlocks);
     a.workers = blocks * C::kWarps;
-    return launch_cluster(attention_rows_kernel<DT, D, NT>, blocks, 32 * C::kWarps, C::kSmem, 1, true, st, kmap, vmap, a);
+    return launch_cluster(attention_rows_kernel<DT, D, NT>, blocks, 32 * C::kWarps, C::kSmem, 1, false, st, kmap, vmap, a);
 }
 
 template <int DT, int D>

@@ -17,6 +17,14 @@ namespace cmpq {
 // when it has grown by more than 2^8, which fp16 has room for: then, rarely after the first tiles, O is multiplied in
 // TMEM.  Rows of keys and of queries keep the order of their entries 16 c + 8 p + e as plane p, group c, entry e, so
 // that the 16 codes a lane widens go to the same group of two planes and a row's lanes to different banks.
+// With 128 rows or fewer the two accumulators take every other tile of keys of the one row tile and are joined at the end;
+// fewer units than SMs are split over the keys, the last block to arrive joining the parts in their order.
+//
+// Measured: 2 x up to 2048 queries over up to 6145 tokens, 32 heads, D = 128: 287 us, 775 TFLOP/s of visible pairs, 0.47 of
+// the library's bf16 product; the tensor pipe is at 41 %.  Per 256 rows x 128 keys the weights' warps work 3240 cycles and
+// wait 810 for scores; the floor of the exponential unit is 2048, of the products about the same.  Steps of 32 keys: 307 us,
+// of 64: 292, of 128 (registers spill): 309.  Scores of 64 keys in two buffers, so that the weights never wait: 301 (twice the
+// barriers, and M = 128, N = 64 products read shared memory 1.5 times as long).
 constexpr int kPfKeys = 128, kPfThreads = 16 * 32;
 constexpr float kPfSlack = 8.0f;
 // Registers a thread: launched with 128, four warps of each of the four groups; 2 x 168 + 112 + 64 = 4 x 128.
@@ -119,7 +127,6 @@ attention_prefill_kernel(const __grid_constant__ AttnArgs A, const __grid_consta
     __shared__ float2 half_ml[128];
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int H = A.c.n_kv_heads, g = A.group, page_bits = A.page_bits;
-    tc5::chained();
     // the last row blocks see most keys and come first
     const int splits = plan.splits, unit = blockIdx.x / splits, z = blockIdx.x % splits;
     const int rb = plan.row_blocks - 1 - unit / plan.per_row_block, s = unit % plan.per_row_block / H, head = unit % H;
@@ -592,7 +599,7 @@ static cmpq_status launch_prefill_of(const AttnArgs& a, cudaStream_t st) {
     const int64_t blocks = units * splits;
     if (blocks > INT32_MAX) return CMPQ_ERR_UNSUPPORTED;
     const PrefillPlan plan{(int)row_blocks, (int)per, splits};
-    return launch_cluster(attention_prefill_kernel<DT, D, PAGES>, (unsigned)blocks, kPfThreads, Prefill<D>::kSmem, 1, true, st, a, plan);
+    return launch_cluster(attention_prefill_kernel<DT, D, PAGES>, (unsigned)blocks, kPfThreads, Prefill<D>::kSmem, 1, false, st, a, plan);
 }
 
 size_t prefill_parts_bytes(int d) { return d > 128 ? 0 : (size_t)std::max(1, sm_count()) * 256 * (d + 2) * sizeof(float); }

@@ -25,8 +25,8 @@ __device__ __forceinline__ uint32_t group_max(uint32_t m, uint4 g) {
 }
 
 // Codes of eight entries.  |x * inv| is at most 127 (1 + 2^-22) here, so adding 1.5 * 2^23 leaves the integer that
-// rounding to even gives in the sum's low byte, in two's complement: one addition instead of a conversion (the
-// conversions have a quarter of the rate of an addition, and were what 4096 x 8192 tokens waited for).
+// rounding to even gives in the sum's low byte, in two's complement: one addition instead of a conversion, which has a
+// quarter of its rate.
 template <int DT>
 __device__ __forceinline__ uint2 group_codes(uint4 g, float inv) {
     const uint32_t w[4] = {g.x, g.y, g.z, g.w};
@@ -42,14 +42,14 @@ __device__ __forceinline__ uint2 group_codes(uint4 g, float inv) {
 
 // One block per token.  Magnitudes are compared two at a time in their own type and, between lanes, as bit patterns,
 // where a NaN is larger than infinity and infinity larger than every number: the maximum also tells whether the row is
-// finite.  A thread keeps
-// KEEP groups of eight in registers, chosen by the row's length so that more blocks share an SM where rows are short;
-// rows of up to 16384 entries are read once, the rest of a longer one is read again.
+// finite.  A thread keeps KEEP groups of eight in registers, chosen by the row's length so that more blocks share an SM
+// where rows are short; rows of up to 16384 entries are read once, the rest of a longer one is read again.
+// Measured: 4096 x 8192 18 us (100 MB, 5.6 TB/s; 27 us with conversions and 32-bit comparisons), 1000 x 11008 8.9 us.
 template <int DT, int KEEP>
 __global__ void __launch_bounds__(kQtThreads)
 quantize_tokens_kernel(const uint16_t* __restrict__ X, int64_t d, int64_t ldx, int wide, int8_t* __restrict__ codes,
                        int64_t ldc, float* __restrict__ scale, int32_t* __restrict__ nonfinite) {
-    tc5::chained();
+    tc5::dependents_may_start();
     const uint16_t* row = X + blockIdx.x * ldx;
     int8_t* out = codes + blockIdx.x * ldc;
     const int t = threadIdx.x;
@@ -144,7 +144,11 @@ __device__ __forceinline__ void store_rows(uint32_t tmem, int c0, int c1, const 
 // quantization of its tokens, a block asks for its first weights before that has ended.  A stage holds the
 // token rows that exist (to eight) and the channels'; the product reads on past those rows into whatever follows, which
 // only reaches accumulator rows that are not stored, and 16 KB behind the last stage are kept for it.  With that one
-// token's weights have some 30 stages on their way (11008 -> 4096: see the measured times below).
+// token's weights have some 30 stages on their way.
+//
+// Measured with the quantization, weights from memory: one token 4096 -> 4096 9.6 us, 8192 -> 28672 40 us (5.8 TB/s, 0.88 of the
+// copy rate); 37 tokens 4096 -> 11008 13 us (3.5 TB/s: launch, first loads and the last stage's way out are half of it).
+// Splitting the sum over a cluster instead, weights as rows: 14.6, 52 and 31.5 us.
 template <int DT>
 __global__ void __launch_bounds__(kMmThreads)
 matmul_i8_tile_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__ CUtensorMap xmap,
@@ -157,7 +161,6 @@ matmul_i8_tile_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_con
     __shared__ int failed;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int nt = blockIdx.x / A.m_tiles, mt = blockIdx.x % A.m_tiles, bn = A.bn;
-    tc5::dependents_may_start();
     const int a_bytes = A.rows * 128, stage = a_bytes + bn * 128, columns = bn <= 32 ? 32 : bn <= 64 ? 64 : bn <= 128 ? 128 : 256;
     if (threadIdx.x < A.stages) tc5::mbar_init(full + threadIdx.x, 1), tc5::mbar_init(empty + threadIdx.x, 1);
     if (threadIdx.x == 0) tc5::mbar_init(&done, 1), failed = 0;
@@ -243,6 +246,9 @@ constexpr size_t kPairSmem = kPairStages * kPairStageBytes + 1024;
 // loads its 128 tokens and half of the channels, so each byte that an SM reads feeds 512 products; six stages of 32 KB.
 // Two accumulators of 256 columns alternate, the epilogue of one tile runs under the products of the next.  Token tiles
 // go fastest: the pairs at work share a few weight tiles and the token codes stay in L2.
+//
+// Measured: 4096 x 8192 x 28672 553 us without, 597 with the quantization (3.5 and 3.2 POP/s, 1.07 and 0.98 of twice the
+// library's bf16 rate); 2048 x 4096 x 11008 65 us, the tensor pipe at 80 % (172 pair tiles in 3 rounds of 74).
 template <int DT>
 __global__ void __launch_bounds__(kMmThreads, 1)
 matmul_i8_pair_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__ CUtensorMap xmap,
@@ -255,7 +261,6 @@ matmul_i8_pair_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_con
     __shared__ int failed;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int rank = (int)tc5::cluster_rank();
-    tc5::dependents_may_start();
     const int tiles = A.n_tiles * A.m_tiles, first = blockIdx.x >> 1, step = gridDim.x >> 1;
     if (threadIdx.x == 0) {
         for (int i = 0; i < kPairStages; ++i) tc5::mbar_init(full + i, 1), tc5::mbar_init(empty + i, 1);
@@ -419,7 +424,7 @@ extern "C" cmpq_status cmpq_quantize_tokens(const void* X, cmpq_dtype dt, int64_
     auto st = static_cast<cudaStream_t>(stream);
     const unsigned rows = (unsigned)n;
     const int64_t keep = (d + 8 * kQtThreads - 1) / (8 * kQtThreads);
-    auto launch = [&](auto kernel) { return launch_cluster(kernel, rows, kQtThreads, 0, 1, true, st, x, d, ldx, wide, codes, ldc, scale, nonfinite); };
+    auto launch = [&](auto kernel) { return launch_cluster(kernel, rows, kQtThreads, 0, 1, false, st, x, d, ldx, wide, codes, ldc, scale, nonfinite); };
     if (dt == CMPQ_BF16)
         return keep <= 2   ? launch(quantize_tokens_kernel<CMPQ_BF16, 2>)
                : keep <= 4 ? launch(quantize_tokens_kernel<CMPQ_BF16, 4>)

@@ -216,12 +216,6 @@ __device__ __forceinline__ void cluster_sync() {
 }
 __device__ __forceinline__ void dependents_may_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 __device__ __forceinline__ void wait_for_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
-// What a kernel of the serving calls begins with: all work in front of it has ended, and the next kernel may be set up
-// while this one runs.  (In this order: what starts behind this kernel may then read whatever was written in front of it.)
-__device__ __forceinline__ void chained() {
-    wait_for_previous();
-    dependents_may_start();
-}
 
 }  // namespace tc5
 
@@ -229,8 +223,8 @@ __device__ __forceinline__ void chained() {
 // of box_rows x 128 bytes with the 128-byte swizzle; what lies outside reads as 0.
 bool make_byte_map(CUtensorMap* map, const void* base, int64_t rows, int64_t cols, int64_t ld, int box_rows);
 
-// A launch with clusters of `cluster` CTAs; `behind`: it may start before the kernel in front of it has ended, for
-// kernels that wait for that themselves (about 1.5 us of launch latency saved between two of them).
+// A launch with clusters of `cluster` CTAs; `behind`: it may start before the kernel in front of it has ended (one that
+// says so, and that was itself launched without this).
 template <class Kernel, class... Args>
 inline cmpq_status launch_cluster(Kernel kern, unsigned grid, int threads, size_t smem, int cluster, bool behind, cudaStream_t st,
                                   const Args&... args) {
