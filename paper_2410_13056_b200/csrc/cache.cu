@@ -455,63 +455,68 @@ struct ReadArgs {
     int32_t* word;
 };
 
-// A block takes TOKENS tokens, a thread 16 codes of each at a time (keys of all heads, then values): the tokens' loads
-// are under way together.  Measured: 13.5 thousand tokens, 8 heads of 128 (83 MB) 28 us.
-template <int DT, int TOKENS>
+// A block takes TOKENS tokens: the first threads find a token's page each, then all read and widen, a thread 16 codes of
+// AT_ONCE tokens at a time (keys of all heads, then values), whose loads are under way together.
+template <int DT, int TOKENS, int AT_ONCE>
 __global__ void __launch_bounds__(256)
 cache_read_kernel(const __grid_constant__ ReadArgs A) {
     const int D = A.c.head_dim, P = A.c.page_tokens, H = A.c.n_kv_heads, G = D / 16;
     const int32_t* off = A.b.tok_off;
     const int64_t t0 = (int64_t)blockIdx.x * TOKENS;
-    int s = block_count(A.b.n_seq, [&](int64_t i) { return off[i] <= t0; });
-    int id[TOKENS], in_page[TOKENS];
-#pragma unroll
-    for (int j = 0; j < TOKENS; ++j) {
-        const int64_t t = t0 + j;
-        id[j] = -1, in_page[j] = 0;
-        if (t < A.b.n_tok) {
-            while (s < A.b.n_seq && off[s + 1] <= t) ++s;
-            if (s < A.b.n_seq) {
-                const int64_t pos = (int64_t)A.b.lens[s] - off[s + 1] + t, page = pos >= 0 ? pos / P : 0;
-                id[j] = pos >= 0 && page < A.b.ld_table ? A.b.table[s * A.b.ld_table + page] : -1;
-                in_page[j] = (int)(pos - page * P);
-                if (id[j] < 0 || id[j] >= A.c.n_pages) {
-                    id[j] = -1;
-                    if (threadIdx.x == 0) report(A.word, kWordTable);
-                }
+    __shared__ int id[TOKENS], in_page[TOKENS];
+    const int s0 = block_count(A.b.n_seq, [&](int64_t i) { return off[i] <= t0; });
+    if (threadIdx.x < TOKENS) {
+        const int64_t t = t0 + threadIdx.x;
+        int found = -1, place = 0, s = s0;
+        while (s < A.b.n_seq && off[s + 1] <= t) ++s;
+        if (t < A.b.n_tok && s < A.b.n_seq) {
+            const int64_t pos = (int64_t)A.b.lens[s] - off[s + 1] + t, page = pos >= 0 ? pos / P : 0;
+            found = pos >= 0 && page < A.b.ld_table ? A.b.table[s * A.b.ld_table + page] : -1;
+            place = (int)(pos - page * P);
+            if (found < 0 || found >= A.c.n_pages) {
+                found = -1;
+                report(A.word, kWordTable);
             }
         }
+        id[threadIdx.x] = found, in_page[threadIdx.x] = place;
     }
+    __syncthreads();
     for (int i = threadIdx.x; i < 2 * H * G; i += blockDim.x) {
         const bool is_v = i >= H * G;
         const int k = is_v ? i - H * G : i, h = k / G, g = k % G;
-        uint4 c[TOKENS];
-        float sc[TOKENS];
+        const int8_t* codes = (is_v ? A.c.v_codes : A.c.k_codes) + (int64_t)h * P * D + 16 * g;
+        const float* scales = (is_v ? A.c.v_scale : A.c.k_scale) + h;
+        uint16_t* out = (is_v ? A.v : A.k) + t0 * A.ldo + h * D + 16 * g;
+#pragma unroll 1
+        for (int first = 0; first < TOKENS; first += AT_ONCE) {
+            uint4 c[AT_ONCE];
+            float sc[AT_ONCE];
 #pragma unroll
-        for (int j = 0; j < TOKENS; ++j) {
-            if (id[j] < 0) continue;
-            const int64_t at = (int64_t)id[j] * H + h;
-            c[j] = __ldg(reinterpret_cast<const uint4*>((is_v ? A.c.v_codes : A.c.k_codes) + (at * P + in_page[j]) * D) + g);
-            sc[j] = __ldg((is_v ? A.c.v_scale : A.c.k_scale) + at);
-        }
-#pragma unroll
-        for (int j = 0; j < TOKENS; ++j) {
-            if (id[j] < 0) continue;
-            const uint32_t x[4] = {c[j].x, c[j].y, c[j].z, c[j].w};
-            uint32_t w[8];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                float f[4];
-                widen_codes(x[e], f);
-                w[2 * e] = round16x2<DT>(f[0] * sc[j], f[1] * sc[j]);
-                w[2 * e + 1] = round16x2<DT>(f[2] * sc[j], f[3] * sc[j]);
+            for (int j = 0; j < AT_ONCE; ++j) {
+                const int page = id[first + j];
+                if (page < 0) continue;
+                c[j] = __ldg(reinterpret_cast<const uint4*>(codes + ((int64_t)page * H * P + in_page[first + j]) * D));
+                sc[j] = __ldg(scales + (int64_t)page * H);
             }
-            uint16_t* o = (is_v ? A.v : A.k) + (t0 + j) * A.ldo + h * D + 16 * g;
-            if (A.wide) {
-                *reinterpret_cast<uint4*>(o) = make_uint4(w[0], w[1], w[2], w[3]);
-                *reinterpret_cast<uint4*>(o + 8) = make_uint4(w[4], w[5], w[6], w[7]);
-            } else {
-                for (int e = 0; e < 16; ++e) o[e] = (uint16_t)(w[e >> 1] >> (16 * (e & 1)));
+#pragma unroll
+            for (int j = 0; j < AT_ONCE; ++j) {
+                if (id[first + j] < 0) continue;
+                const uint32_t x[4] = {c[j].x, c[j].y, c[j].z, c[j].w};
+                uint32_t w[8];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    float f[4];
+                    widen_codes(x[e], f);
+                    w[2 * e] = round16x2<DT>(f[0] * sc[j], f[1] * sc[j]);
+                    w[2 * e + 1] = round16x2<DT>(f[2] * sc[j], f[3] * sc[j]);
+                }
+                uint16_t* o = out + (first + j) * A.ldo;
+                if (A.wide) {
+                    *reinterpret_cast<uint4*>(o) = make_uint4(w[0], w[1], w[2], w[3]);
+                    *reinterpret_cast<uint4*>(o + 8) = make_uint4(w[4], w[5], w[6], w[7]);
+                } else {
+                    for (int e = 0; e < 16; ++e) o[e] = (uint16_t)(w[e >> 1] >> (16 * (e & 1)));
+                }
             }
         }
     }
@@ -542,9 +547,9 @@ static cmpq_status launch_append(const AppendArgs& a, unsigned q_blocks, cudaStr
 
 template <int DT>
 static cmpq_status launch_read(const ReadArgs& a, cudaStream_t st) {
-    // four tokens to a block once that leaves blocks enough
-    return a.b.n_tok >= 4096 ? launch(cache_read_kernel<DT, 4>, (unsigned)((a.b.n_tok + 3) / 4), 256, a, st)
-                             : launch(cache_read_kernel<DT, 1>, (unsigned)a.b.n_tok, 256, a, st);
+    // 16 tokens to a block once that leaves about four blocks an SM
+    return a.b.n_tok >= 8192 ? launch(cache_read_kernel<DT, 16, 4>, (unsigned)((a.b.n_tok + 15) / 16), 256, a, st)
+                             : launch(cache_read_kernel<DT, 1, 1>, (unsigned)a.b.n_tok, 256, a, st);
 }
 
 }  // namespace cmpq

@@ -139,6 +139,32 @@ def test_append_grows_page_by_page_like_one_call():
     assert (one.k_codes.int() - steps.k_codes.int()).abs().max() <= 8
 
 
+@pytest.mark.parametrize("P,d", [(16, 64), (64, 128)])
+def test_append_and_read_many_tokens(P, d):
+    """Prompts of thousands of tokens, some sequences without any, and all of them read back in one call."""
+    lens, new, H = [5000, 0, 3301, 77, 1], [4990, 0, 3301, 20, 1], 2
+    cache, table = make(lens, H, d, P, 4, garbage=False)
+    off = np.concatenate(([0], np.cumsum(new)))
+    k, v = (tokens(int(off[-1]), H, d, torch.bfloat16, s).cuda() for s in (1, 2))
+    cos, sin = rope(5000, d)
+    c = up(cache)
+    q = tokens(int(off[-1]), 3, d, torch.bfloat16, 3).cuda()
+    out = c.append(k, v, i32(off), i32(lens), i32(table), q=q, cos=torch.from_numpy(cos).cuda(), sin=torch.from_numpy(sin).cuda())
+    ref.append(cache, off, lens, table, k.float().cpu().numpy(), v.float().cpu().numpy(), cos, sin)
+    pos = np.concatenate([np.arange(m - w, m) for m, w in zip(lens, new)]).astype(int)
+    assert torch.equal(out.cpu(), torch.from_numpy(ref.rotate(q.float().cpu().numpy(), pos, cos, sin, False)).bfloat16())
+    for x in "kv":
+        assert np.array_equal(getattr(c, x + "_scale").cpu().numpy(), cache[x + "_scale"]), x
+        assert np.array_equal(getattr(c, x + "_codes").cpu().numpy(), cache[x + "_codes"]), x
+    all_off = np.concatenate(([0], np.cumsum(lens)))
+    got = c.read(i32(all_off), i32(lens), i32(table), int(all_off[-1]), torch.float16)
+    for x, t in zip("kv", got):
+        vals = cache[x + "_codes"].astype(np.float32) * cache[x + "_scale"][..., None, None]
+        rows = [vals[table[s][p // P], :, p % P] for s, m in enumerate(lens) for p in range(m)]
+        assert torch.equal(t.cpu(), torch.from_numpy(np.stack(rows)).half()), x
+    c.check()
+
+
 def test_append_extremes():
     """Zeros take the smallest scale, huge values the largest, NaN and infinity are reported; no fault, no spill."""
     H, d, P = 1, 64, 16

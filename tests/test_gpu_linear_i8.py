@@ -183,3 +183,20 @@ def test_from_weight_and_refusals():
     with pytest.raises(B.CmpqError) as e:
         B.cmpq_linear_i8(x, layer.w_codes[:, :120], layer.w_scale, None, y, torch.empty(0, dtype=torch.uint8, device="cuda"))
     assert torch.all(y == 3.0)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("n,d_in,d_out", [(1900, 520, 4400), (2500, 129, 6001), (300, 1040, 18950)])
+def test_many_tiles(n, d_in, d_out, dtype):
+    """More tiles than SMs, so that blocks walk over several; sums of integers below 2^53 are exact in float64."""
+    x = _tokens(n, d_in, dtype, 7)
+    wc, ws = _weights(d_out, d_in, 8)
+    bias = torch.from_numpy(np.random.default_rng(9).normal(size=d_out)).to(dtype).cuda()
+    y = serving.Int8Linear(wc, ws, bias)(x.cuda())
+    codes, scale = ref.quantize_tokens(x.float().numpy())
+    acc = codes.astype(np.float64) @ wc.cpu().numpy().astype(np.float64).T
+    want = acc * scale[:, None].astype(np.float64) * ws.cpu().numpy().astype(np.float64)
+    b = bias.float().cpu().numpy().astype(np.float64)
+    tol = 4 * 2.0 ** -24 * (np.abs(want) + np.abs(b)) + ref.half_ulp(np.abs(want + b) * (1 + 2.0 ** -7), dtype)
+    bad = np.abs(y.float().cpu().numpy().astype(np.float64) - (want + b)) > tol
+    assert not bad.any(), (int(bad.sum()), np.argwhere(bad)[:5])
