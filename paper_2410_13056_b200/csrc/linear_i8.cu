@@ -232,7 +232,7 @@ matmul_i8_tile_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_con
         if (threadIdx.x == 0) {
             const long long start = clock64();
             while (clock64() - start < (1ll << 21)) __nanosleep(1000);
-            atomicExch(A.failed, 1);
+            atomicOr(A.failed, kWordInternal);
         }
         __syncthreads();
     }
@@ -344,7 +344,7 @@ matmul_i8_pair_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_con
         if (threadIdx.x == 0) {
             const long long start = clock64();
             while (clock64() - start < (1ll << 21)) __nanosleep(1000);
-            atomicExch(A.failed, 1);
+            atomicOr(A.failed, kWordInternal);
         }
         __syncthreads();
     }
@@ -434,16 +434,17 @@ extern "C" cmpq_status cmpq_quantize_tokens(const void* X, cmpq_dtype dt, int64_
                        : launch(quantize_tokens_kernel<CMPQ_F16, 8>);
 }
 
-// The caller has checked everything.  The last 256 bytes of the work space take the mark of a kernel that gave up.
+// The caller has checked everything.  `word`, or the last 256 bytes of the work space where there is none, takes the mark
+// of a kernel that gave up.
 static cmpq_status product(const int8_t* xc, int64_t ldxc, const float* xs, const int8_t* wc, int64_t ldwc, const float* w_scale, const void* bias,
-                           cmpq_dtype dt, int64_t n, int64_t d_in, int64_t d_out, void* y, int64_t ldy, void* ws, bool behind, void* stream) {
+                           cmpq_dtype dt, int64_t n, int64_t d_in, int64_t d_out, void* y, int64_t ldy, int32_t* word, void* ws, bool behind, void* stream) {
     ProductArgs a = {};
     a.xs = xs, a.ws = w_scale;
     a.bias = static_cast<const uint16_t*>(bias);
     a.y = static_cast<uint16_t*>(y);
     a.ldy = ldy;
     a.n = (int)n, a.d_out = (int)d_out;
-    a.failed = reinterpret_cast<int32_t*>(static_cast<char*>(ws) + cmpq_linear_i8_ws_bytes(n, d_in, d_out) - 256);
+    a.failed = word ? word : reinterpret_cast<int32_t*>(static_cast<char*>(ws) + cmpq_linear_i8_ws_bytes(n, d_in, d_out) - 256);
     auto st = static_cast<cudaStream_t>(stream);
     return dt == CMPQ_BF16 ? launch_product<CMPQ_BF16>(xc, ldxc, wc, ldwc, d_in, a, behind, st)
                            : launch_product<CMPQ_F16>(xc, ldxc, wc, ldwc, d_in, a, behind, st);
@@ -459,7 +460,7 @@ extern "C" cmpq_status cmpq_matmul_i8(const int8_t* xc, int64_t ldxc, const floa
         !aligned_to(w_scale, 4) || !aligned_to(y, 2) || !aligned_to(bias, 2))
         return CMPQ_ERR_INVALID_ARG;
     if (!ws || !aligned_to(ws, 256) || ws_bytes < cmpq_linear_i8_ws_bytes(n, d_in, d_out)) return CMPQ_ERR_WORKSPACE;
-    return product(xc, ldxc, xs, wc, ldwc, w_scale, bias, dt, n, d_in, d_out, y, ldy, ws, false, stream);
+    return product(xc, ldxc, xs, wc, ldwc, w_scale, bias, dt, n, d_in, d_out, y, ldy, nullptr, ws, false, stream);
 }
 
 extern "C" cmpq_status cmpq_linear_i8(const void* X, cmpq_dtype dt, int64_t n, int64_t d_in, int64_t ldx,
@@ -479,5 +480,5 @@ extern "C" cmpq_status cmpq_linear_i8(const void* X, cmpq_dtype dt, int64_t n, i
     cmpq_status st = cmpq_quantize_tokens(X, dt, n, d_in, ldx, codes, ldc, scale, nonfinite, stream);
     if (st != CMPQ_OK) return st;
     // the quantization lets the product start early; it was itself started after everything before it, the weights too
-    return product(codes, ldc, scale, wc, ldwc, w_scale, bias, dt, n, d_in, d_out, y, ldy, ws, true, stream);
+    return product(codes, ldc, scale, wc, ldwc, w_scale, bias, dt, n, d_in, d_out, y, ldy, nonfinite, ws, true, stream);
 }

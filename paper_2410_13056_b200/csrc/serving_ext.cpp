@@ -213,6 +213,7 @@ struct Cache {
         const c10::cuda::CUDAGuard guard(word.device());
         const cmpq_status s = cmpq_check_cache(word.data_ptr<int32_t>(), stream_of(word));
         word.zero_();
+        if (s == CMPQ_ERR_INTERNAL) work.held.clear();  // a kernel gave up: its counters may not be 0
         check(s, "cmpq_check_cache");
     }
 };
