@@ -520,7 +520,7 @@ cmpq_status cmpq_cache_read(const cmpq_cache* cache, const cmpq_batch* batch, cm
  * q [n_tok][ldq], out [n_tok][ldo] of `dt`, heads next to each other; queries finite.
  * max_new >= every count of new tokens and max_len >= every length are the caller's bounds (they choose the
  * kernel and size the work space).  Probabilities and sums in fp32, products on the tensor cores in fp16 with
- * fp32 accumulation: codes are exact there, a query row is scaled by a power of two into fp16's range, and
+ * fp32 accumulation: codes are exact there, a query row is scaled by a power of two into fp16's range (any finite row), and
  * probabilities are rounded to fp16.
  * ws: cmpq_cache_attention_ws_bytes(n_seq, n_tok, max_new, max_len, n_heads, n_kv_heads, head_dim).  Unlike other
  * work spaces its first CMPQ_ATTENTION_ZEROED bytes have to be 0 when the call's kernels start, and are 0 again when

@@ -32,6 +32,17 @@ __device__ __forceinline__ float ex2(float x) {
     return y;
 }
 
+// A query row's way into fp16 and back: its entries times `down`, its scores times `up`, both powers of two with a product
+// of 1.  The largest magnitude lands in [2^13, 2^14), so entries down to 2^-27 of it keep all their bits; the exponent is
+// held to [-113, 126], where both powers are normal numbers: rows of bf16 subnormals stay smaller, of 2^127 end below 2^15.
+struct RowScale {
+    float down, up;
+};
+__device__ __forceinline__ RowScale row_scale(float largest) {
+    const int e = min(max((int)(__float_as_uint(largest) >> 23) - 127, -113), 126);
+    return {__uint_as_float((uint32_t)(127 + 13 - e) << 23), __uint_as_float((uint32_t)(127 - 13 + e) << 23)};
+}
+
 // Four int8 codes (already offset by 128) as two pairs of fp16: 0x6400 | u is 1024 + u, and 1024 + 128 comes off.
 __device__ __forceinline__ uint32_t half_pair(uint32_t u, uint32_t pick) {
     const uint32_t h = __byte_perm(u, 0x64646464u, pick);

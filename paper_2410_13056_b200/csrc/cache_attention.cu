@@ -356,14 +356,13 @@ attention_rows_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_con
             }
             m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 1));
             m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 2));
-            const int ex = m > 0.0f ? ilogbf(m) : 0;
-            const float up = ldexpf(1.0f, ex), dn = ldexpf(1.0f, max(-126, -ex));
+            const RowScale by = row_scale(m);
 #pragma unroll
             for (int e = 0; e < D / 4; e += 2) {
-                const __half2 hh = __floats2half2_rn(f[e] * dn, f[e + 1] * dn);
+                const __half2 hh = __floats2half2_rn(f[e] * by.down, f[e + 1] * by.down);
                 qf[nt][e >> 2][(e >> 1) & 1] = *reinterpret_cast<const uint32_t*>(&hh);
             }
-            const float mine = A.scale * up;  // of row r; the score fragment has rows 2c, 2c + 1
+            const float mine = A.scale * by.up;  // of row r; the score fragment has rows 2c, 2c + 1
             qs[nt][0] = __shfl_sync(0xffffffffu, mine, (2 * c) * 4);
             qs[nt][1] = __shfl_sync(0xffffffffu, mine, (2 * c + 1) * 4);
         }

@@ -309,19 +309,17 @@ attention_prefill_kernel(const __grid_constant__ AttnArgs A, const __grid_consta
 #pragma unroll
                 for (int k = 0; k < 4; ++k) m = max(m, max(e[k] & 0x7fffu, e[k] >> 16 & 0x7fffu));
             }
-            const float amax = widen16<DT>((uint16_t)m);
-            const int ex = amax > 0.0f ? ilogbf(amax) : 0;
-            const float up = ldexpf(1.0f, ex), dn = ldexpf(1.0f, max(-126, -ex));
+            const RowScale by = row_scale(widen16<DT>((uint16_t)m));
 #pragma unroll
             for (int j = 0; j < D / 8; ++j) {
                 float f[8];
                 uint32_t y[4];
                 widen8<DT>(x[j], f);
 #pragma unroll
-                for (int k = 0; k < 4; ++k) y[k] = round16x2<CMPQ_F16>(f[2 * k] * dn, f[2 * k + 1] * dn);
+                for (int k = 0; k < 4; ++k) y[k] = round16x2<CMPQ_F16>(f[2 * k] * by.down, f[2 * k + 1] * by.down);
                 if (two || w == 0) *reinterpret_cast<uint4*>(sq + w * C::kTileBytes + pf_at<D>(local, j)) = make_uint4(y[0], y[1], y[2], y[3]);
             }
-            qs = A.scale * up;
+            qs = A.scale * by.up;
             tc5::fence_async_smem();
             __syncwarp();
             if (lane == 0) tc5::mbar_arrive(&q_full);

@@ -407,3 +407,25 @@ def test_layer_runs_them_together():
         assert (y.double() - want.double()).norm() <= 0.02 * want.double().norm()
         lens, new = lens + 1, np.array([1, 1])
     cache.check()
+
+
+@pytest.mark.parametrize("new", [1, 5, 140])
+def test_attend_queries_at_the_ends_of_bf16(new):
+    """Rows of subnormals with zeros between, down to the smallest, and rows that reach 2^127: `scale` and the keys'
+    scales bring their scores to ordinary size, so the tolerance stays as sharp as elsewhere."""
+    H, d, P, heads, lens = 2, 128, 32, 4, [300]
+    g = np.random.default_rng(11)
+    cache, table = make(lens, H, d, P, 6, garbage=False)
+    for exponents, scale, keys in (((-133, -131, -129, -126), 2.0 ** 100, 2.0 ** 28), ((127, 126, 127, 125), 2.0 ** -90, 2.0 ** -34)):
+        x = np.zeros((new, heads, d))
+        for h, e in enumerate(exponents):
+            steps = g.integers(-3, 4, size=(new, d)) * (g.random((new, d)) < 0.6)
+            steps[:, 0] = 1                                # no row is zero, none is larger than 1.75 * 2^e
+            x[:, h] = steps * 2.0 ** e * (1.0 if e == -133 else 0.5)
+        q = torch.from_numpy(x).to(torch.bfloat16)
+        assert np.array_equal(q.double().numpy(), x)       # bf16 holds them
+        c = {**cache, "k_scale": (cache["k_scale"] * np.float32(keys)).astype(np.float32)}
+        held = up(c)
+        out, lse = held.attend(q.cuda(), i32([0, new]), i32(lens), i32(table), max_new=new, max_len=300, scale=scale, return_lse=True)
+        held.check()
+        check_attend(c, [0, new], lens, table, q, scale, True, 0, out, lse, torch.bfloat16)
