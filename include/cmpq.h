@@ -521,7 +521,9 @@ cmpq_status cmpq_cache_read(const cmpq_cache* cache, const cmpq_batch* batch, cm
  * max_new >= every count of new tokens and max_len >= every length are the caller's bounds (they choose the
  * kernel and size the work space).  Probabilities and sums in fp32, products on the tensor cores in fp16 with
  * fp32 accumulation: codes are exact there, a query row is scaled by a power of two into fp16's range (any finite row), and
- * probabilities are rounded to fp16.
+ * probabilities times value scales are rounded to fp16, where the largest of a row lies in [2^7, 2^15]: they keep 11 bits
+ * down to 2^-21 of it and vanish below 2^-32.  The softmax's sum is not rounded; it misses keys whose probability times
+ * value scale is below 2^-133 of the row's largest.
  * ws: cmpq_cache_attention_ws_bytes(n_seq, n_tok, max_new, max_len, n_heads, n_kv_heads, head_dim).  Unlike other
  * work spaces its first CMPQ_ATTENTION_ZEROED bytes have to be 0 when the call's kernels start, and are 0 again when
  * they have ended (zero the buffer once, after allocating it and after bit 3 of `word`). */

@@ -24,6 +24,9 @@ struct AttnArgs {
     int workers;
 };
 
+// Weights are kept relative to 2^kWeightBits: times their value scale the largest of a row are near the top of fp16, whose
+// 30 octaves below that all count.
+constexpr float kWeightBits = 15.0f;
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 
 __device__ __forceinline__ float ex2(float x) {

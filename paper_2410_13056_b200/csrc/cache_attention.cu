@@ -2,7 +2,8 @@
 //
 // out = softmax(scale q K^T) V with K = S_k[page] c, V = S_v[page] c, c int8.  The codes are exact in fp16, so both
 // products run on the tensor cores in fp16 with fp32 accumulation, a page's scale being one factor of its scores (keys)
-// or of its weights (values); a query row is scaled by a power of two into fp16's range first.
+// or of its weights (values); a query row is scaled by a power of two into fp16's range first, and a row's weights, times
+// their value scales, by one that puts the largest near fp16's top.
 #include <algorithm>
 #include <cmath>
 
@@ -167,8 +168,13 @@ __device__ __forceinline__ void join_parts(const AttnArgs& A, const Piece& u, in
         } else {
             dst[0] = (uint16_t)w.x, dst[1] = (uint16_t)(w.x >> 16), dst[2] = (uint16_t)w.y, dst[3] = (uint16_t)(w.y >> 16);
         }
-        if (A.lse && d == 0) A.lse[t * A.n_heads + h] = sum > 0.0f ? (top + log2f(sum)) * kLn2 : -INFINITY;
+        if (A.lse && d == 0) A.lse[t * A.n_heads + h] = sum > 0.0f ? (top - kWeightBits + log2f(sum)) * kLn2 : -INFINITY;
     }
+}
+
+// The exponent e of a page's value scale in [2^(e-1), 2^e); what is below 2^-60, a page of zeros, counts as that.
+__device__ __forceinline__ float scale_exponent(float scale) {
+    return __uint_as_float(0x4b000000u | max(__float_as_uint(scale), __float_as_uint(kScaleLo)) >> 23) - 8388734.0f;  // 2^23 + 126
 }
 
 // A lane's place in the m16n8k16 fragments: r = lane / 4, c = lane % 4.
@@ -367,7 +373,7 @@ attention_rows_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_con
             qs[nt][1] = __shfl_sync(0xffffffffu, mine, (2 * c + 1) * 4);
         }
 
-        float o[NT][D / 16][4], m2[NT][2], l[NT][2], ref = 0.0f, inv_ref = 0.0f;
+        float o[NT][D / 16][4], m2[NT][2], l[NT][2];
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
@@ -436,47 +442,37 @@ attention_rows_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_con
                         }
                     }
             }
-            // values are taken relative to the largest value scale so far, so that the weights fit fp16
-            float shrink = 1.0f;
-            {
-                float most = sc[0].y;
+            // m2 is the row's largest score plus its page's value exponent so far: what goes to fp16 is weight times value
+            // scale, and the largest of those that the row sees ends in [2^14, 2^15]
+            float above[MT];
 #pragma unroll
-                for (int mt = 1; mt < MT; ++mt) most = fmaxf(most, sc[mt].y);
-                if (most > ref) {  // the same for the whole warp
-                    inv_ref = 1.0f / most;
-                    shrink = ref * inv_ref;
-                    ref = most;
-                }
-            }
+            for (int mt = 0; mt < MT; ++mt) above[mt] = scale_exponent(sc[mt].y);
             uint32_t pf[NT][MT][2];
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
                 float keep[2];
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
-                    float top = fmaxf(st[nt][0][e], st[nt][0][e + 2]);
+                    float top = fmaxf(st[nt][0][e], st[nt][0][e + 2]) + above[0];
 #pragma unroll
-                    for (int mt = 1; mt < MT; ++mt) top = fmaxf(top, fmaxf(st[nt][mt][e], st[nt][mt][e + 2]));
+                    for (int mt = 1; mt < MT; ++mt) top = fmaxf(top, fmaxf(st[nt][mt][e], st[nt][mt][e + 2]) + above[mt]);
                     top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 4));
                     top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 8));
                     top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 16));
                     top = fmaxf(top, m2[nt][e]);
-                    const float at = top == -INFINITY ? 0.0f : top;
-                    keep[e] = ex2(m2[nt][e] - at);
+                    const float ref = top == -INFINITY ? 0.0f : top, at = ref - kWeightBits;
+                    keep[e] = ex2(m2[nt][e] - ref);
                     m2[nt][e] = top;
                     float sum = 0.0f;
 #pragma unroll
-                    for (int mt = 0; mt < MT; ++mt) {
-                        const float vs = sc[mt].y * inv_ref;
+                    for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
                         for (int k = 0; k < 2; ++k) {
                             const float w = ex2(st[nt][mt][e + 2 * k] - at);
                             sum += w;
-                            st[nt][mt][e + 2 * k] = w * vs;
+                            st[nt][mt][e + 2 * k] = w * sc[mt].y;
                         }
-                    }
                     l[nt][e] = fmaf(l[nt][e], keep[e], sum);  // this lane's tokens only; joined at the end
-                    keep[e] *= shrink;
                 }
 #pragma unroll
                 for (int mt = 0; mt < MT; ++mt)
@@ -552,7 +548,7 @@ attention_rows_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_con
                 sum += __shfl_xor_sync(0xffffffffu, sum, 16);
                 const int row = nt * 8 + 2 * c + e;
                 if (row >= rows) continue;
-                const float f = whole ? (sum > 0.0f ? ref / sum : 0.0f) : ref;
+                const float f = whole && sum > 0.0f ? 1.0f / sum : 0.0f;
                 // entries 16 r (8 r for D = 64) and following of the row, in order
                 if (whole) {
                     const int i = (rb * kR + row) / g, h = head * g + (rb * kR + row) % g;
@@ -570,13 +566,13 @@ attention_rows_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_con
                             for (int k = 0; k < 8; ++k) dst[d + k] = (uint16_t)(w[k >> 1] >> (16 * (k & 1)));
                         }
                     }
-                    if (A.lse && r == 0) A.lse[(int64_t)(p.first + i) * A.n_heads + h] = sum > 0.0f ? (m2[nt][e] + log2f(sum)) * kLn2 : -INFINITY;
+                    if (A.lse && r == 0) A.lse[(int64_t)(p.first + i) * A.n_heads + h] = sum > 0.0f ? (m2[nt][e] - kWeightBits + log2f(sum)) * kLn2 : -INFINITY;
                 } else {
 #pragma unroll
                     for (int j = 0; j < D / 16; j += 2) {
                         const int d = D == 64 ? 8 * r + 2 * j : (j >> 3) * 128 + 16 * r + (j & 7) * 2;
                         *reinterpret_cast<float4*>(part + row * D + d) =
-                            make_float4(o[nt][j][e] * f, o[nt][j][e + 2] * f, o[nt][j + 1][e] * f, o[nt][j + 1][e + 2] * f);
+                            make_float4(o[nt][j][e], o[nt][j][e + 2], o[nt][j + 1][e], o[nt][j + 1][e + 2]);
                     }
                     if (r == 0) part[kR * D + 2 * row] = m2[nt][e], part[kR * D + 2 * row + 1] = sum;
                 }

@@ -12,10 +12,11 @@ namespace cmpq {
 //   1 thread  (of four warps, the others idle) issues S_w = Q_w K^T and O_w += P_w V for the two row tiles in turn
 //   2 x 4 warps, a thread per row: weights P_w = exp2(S_w - m) in fp16 over S_w's own TMEM columns
 // While one row tile's weights are made the other's products run.  TMEM holds S (2 x 128 columns) and O (2 x D).
-// The weights carry the value scale of their page relative to the largest of all pages that the block meets, as part
-// of the exponent; the row's sum takes it out again page by page.  The reference maximum m follows the true one only
-// when it has grown by more than 2^8, which fp16 has room for: then, rarely after the first tiles, O is multiplied in
-// TMEM.  Rows of keys and of queries keep the order of their entries 16 c + 8 p + e as plane p, group c, entry e, so
+// The weights carry the value scale of their page as part of the exponent, and the row's sum takes it out again page by
+// page.  The reference m is the row's own largest of score plus log2 of the value scale, over keys that it sees, so pages
+// that it does not see, or hardly weighs, cost the others no bits of fp16.  It follows the true maximum only when that
+// has grown by more than 2^8, so what goes to fp16 ends in [2^7, 2^15]: then, rarely after the first tiles, O is multiplied
+// in TMEM.  Rows of keys and of queries keep the order of their entries 16 c + 8 p + e as plane p, group c, entry e, so
 // that the 16 codes a lane widens go to the same group of two planes and a row's lanes to different banks.
 // With 128 rows or fewer the two accumulators take every other tile of keys of the one row tile and are joined at the end;
 // fewer units than SMs are split over the keys, the last block to arrive joining the parts in their order.
@@ -324,19 +325,6 @@ attention_prefill_kernel(const __grid_constant__ AttnArgs A, const __grid_consta
             __syncwarp();
             if (lane == 0) tc5::mbar_arrive(&q_full);
         }
-        // the largest value scale of the pages that the block meets
-        float ref = 0.0f;
-        {
-            const int from = (t0 * kPfKeys) >> page_bits, to = min(pages, ((t0 + tiles) * kPfKeys) >> page_bits);
-#pragma unroll 4
-            for (int page = from + lane; page < to; page += 32) {
-                const int id = page_of(page);
-                if (id >= 0) ref = fmaxf(ref, __ldg(A.c.v_scale + (int64_t)id * H + head));
-            }
-#pragma unroll
-            for (int x = 16; x; x >>= 1) ref = fmaxf(ref, __shfl_xor_sync(0xffffffffu, ref, x));
-        }
-        const float inv_ref = ref > 0.0f ? 1.0f / ref : 0.0f;
         const uint32_t lanes = (uint32_t)(warp & 3) << 21, ts = tmem + w * 128 + lanes, to = tmem_o + w * 128 + lanes;
         const int span_bits = min(7, page_bits), per_tile = kPfKeys >> span_bits;
         // Lane k holds the scales of the tile's k-th page.  Those of the next tile are under way, and so is the look-up of the
@@ -390,7 +378,7 @@ attention_prefill_kernel(const __grid_constant__ AttnArgs A, const __grid_consta
         bool ok = true;
         for (int t = t_first; t < tiles; t += t_step) {
             sc = sc_next;
-            const float vs = fmaxf(sc.y * inv_ref, 0x1p-100f), bias = log2f(vs), inv_vs = 1.0f / vs;
+            const float bias = log2f(fmaxf(sc.y, 0x1p-80f)), inv_vs = ex2(-bias);  // a page of zeros has scale 0
             sc_next = scales(id_next);
             id_next = look_up(t + 2 * t_step);
             if (!(ok = tc5::mbar_wait(s_full + w, (two ? t : t >> 1) & 1, &failed))) break;
@@ -410,16 +398,17 @@ attention_prefill_kernel(const __grid_constant__ AttnArgs A, const __grid_consta
                         for (int j = 0; j < 64; ++j)
                             if (step * 64 + j < from || step * 64 + j >= upto) v[j] = 0xff800000u;  // -infinity
                     }
-                    float f[PAGES], top = -INFINITY;
+                    float f[PAGES], b[PAGES], top = -INFINITY;
 #pragma unroll
                     for (int k = 0; k < PAGES; ++k) {
                         f[k] = fmaxf(qs * __shfl_sync(0xffffffffu, sc.x, (step * 64 + k * kCols) >> span_bits), 0x1p-126f);
+                        b[k] = __shfl_sync(0xffffffffu, bias, (step * 64 + k * kCols) >> span_bits);
                         float most[4];  // side by side
 #pragma unroll
                         for (int j = 0; j < 4; ++j) most[j] = __uint_as_float(v[k * kCols + j]);
 #pragma unroll
                         for (int j = 4; j < kCols; j += 2) most[j >> 1 & 3] = fmaxf(fmaxf(most[j >> 1 & 3], __uint_as_float(v[k * kCols + j])), __uint_as_float(v[k * kCols + j + 1]));
-                        top = fmaxf(top, fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3])) * f[k]);
+                        top = fmaxf(top, fmaf(fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3])), f[k], b[k]));
                     }
                     const bool grown = top > m + kPfSlack;
                     if (__any_sync(0xffffffffu, grown)) {
@@ -428,12 +417,12 @@ attention_prefill_kernel(const __grid_constant__ AttnArgs A, const __grid_consta
                         l *= keep;
                         rescale(t, 2 * step, keep);
                     }
-                    const float at = m == -INFINITY ? 0.0f : m;
+                    const float at = (m == -INFINITY ? 0.0f : m) - (kWeightBits - kPfSlack);
                     uint32_t y[32];
 #pragma unroll
                     for (int k = 0; k < PAGES; ++k) {
                         const int page = (step * 64 + k * kCols) >> span_bits;
-                        const float add = __shfl_sync(0xffffffffu, bias, page) - at;
+                        const float add = b[k] - at;
                         const uint64_t ff = pair(f[k], f[k]), aa = pair(add, add);
                         uint64_t sum[2] = {0, 0};
 #pragma unroll
@@ -494,9 +483,9 @@ attention_prefill_kernel(const __grid_constant__ AttnArgs A, const __grid_consta
             m = top;
         }
         if (ok && (two || w == 0)) {  // all lanes: the warp reads TMEM together
-            // whole: the normalised row; a part: times its own reference scale only, with maximum and sum behind the rows
+            // whole: the normalised row; a part: as it is, with maximum and sum behind the rows
             float* part = splits > 1 ? A.parts + (int64_t)blockIdx.x * (256 * (D + 2)) : nullptr;
-            const float f = part ? ref : l > 0.0f ? ref / l : 0.0f;
+            const float f = part ? 1.0f : l > 0.0f ? 1.0f / l : 0.0f;
             uint16_t* dst = A.out + (int64_t)(first + i) * A.ldo + (int64_t)h * D;
             const float* held = reinterpret_cast<const float*>(sk) + local;
             store_row<DT, D>(
@@ -515,7 +504,7 @@ attention_prefill_kernel(const __grid_constant__ AttnArgs A, const __grid_consta
                 reinterpret_cast<float2*>(part + 256 * D)[in_block] = make_float2(m, l);
                 __threadfence();
             } else if (real && A.lse) {
-                A.lse[(int64_t)(first + i) * A.n_heads + h] = l > 0.0f ? (m + log2f(l)) * kLn2 : -INFINITY;
+                A.lse[(int64_t)(first + i) * A.n_heads + h] = l > 0.0f ? (m - (kWeightBits - kPfSlack) + log2f(l)) * kLn2 : -INFINITY;
             }
         }
         tc5::fence_before_sync();
@@ -567,7 +556,7 @@ attention_prefill_kernel(const __grid_constant__ AttnArgs A, const __grid_consta
                         for (int k = 0; k < 8; ++k) dst[c + k] = (uint16_t)(w[k >> 1] >> (16 * (k & 1)));
                     }
                 }
-                if (A.lse) A.lse[(int64_t)(first + i) * A.n_heads + h] = l > 0.0f ? (m + log2f(l)) * kLn2 : -INFINITY;
+                if (A.lse) A.lse[(int64_t)(first + i) * A.n_heads + h] = l > 0.0f ? (m - (kWeightBits - kPfSlack) + log2f(l)) * kLn2 : -INFINITY;
             }
             if (is_last && tid == 0) A.counters[kPfCounters + unit] = 0;
         }

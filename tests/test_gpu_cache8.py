@@ -429,3 +429,86 @@ def test_attend_queries_at_the_ends_of_bf16(new):
         out, lse = held.attend(q.cuda(), i32([0, new]), i32(lens), i32(table), max_new=new, max_len=300, scale=scale, return_lse=True)
         held.check()
         check_attend(c, [0, new], lens, table, q, scale, True, 0, out, lse, torch.bfloat16)
+
+
+def check_weights(cache, pages, q, scale, got, lse, length, window=0):
+    """One sequence, against float64, with nothing in the tolerance that is relative to values a row hardly weighs.  Weights
+    times value scales are rounded to fp16 with the largest of a row, w, at 2^7 or above: relative 2^-11, or 2^-25 absolute,
+    which is 2^-32 w.  So |out - ref| <= (2^-10 + 4 ds) sum p|v| + L 2^-32 * 127 w + half ulp."""
+    n, heads, d = q.shape
+    H, P = cache["k_codes"].shape[1], cache["k_codes"].shape[2]
+    kc, vc = (cache[x][pages].transpose(0, 2, 1, 3).reshape(-1, H, d)[:length].astype(np.float64) for x in ("k_codes", "v_codes"))
+    ks, vs = (np.repeat(cache[x][pages].astype(np.float64), P, 0)[:length] for x in ("k_scale", "v_scale"))
+    x, y = q.double().cpu().numpy(), got.double().cpu().numpy()
+    for h in range(heads):
+        kh = h // (heads // H)
+        k, S = kc[:, kh] * ks[:, kh, None], vs[:, kh]
+        s = scale * (x[:, h] @ k.T)
+        pos, key = np.arange(length - n, length)[:, None], np.arange(length)
+        s[(key > pos) | ((key <= pos - window) if window else False)] = -np.inf
+        top = s.max(1, keepdims=True)
+        p = np.exp(s - top)
+        total = p.sum(1, keepdims=True)
+        p /= total
+        ds = (d + 8) * 2.0 ** -23 * scale * (np.abs(x[:, h]) @ np.abs(k).T * np.isfinite(s)).max(1)
+        want, size = (p * S) @ vc[:, kh], (p * S) @ np.abs(vc[:, kh])
+        floor = length * 2.0 ** -32 * 127 * (p * S).max(1)
+        tol = (2.0 ** -10 + 4 * ds)[:, None] * size + floor[:, None] + ref.half_ulp(np.abs(want) + 2.0 ** -9 * size, got.dtype)
+        bad = ~(np.abs(y[:, h] - want) <= tol)
+        assert not bad.any(), (h, int(bad.sum()), np.argwhere(bad)[:4], y[:, h][bad][:4], want[bad][:4])
+        l = (top + np.log(total))[:, 0]
+        assert np.all(np.abs(lse[:, h].double().cpu().numpy() - l) <= 2 * ds + 2.0 ** -20 * (1 + np.abs(l)))
+
+
+@pytest.mark.parametrize("ratio", [2.0 ** -16, 2.0 ** -27, 2.0 ** -60])
+@pytest.mark.parametrize("new,d,P,window", [(1, 64, 16, 0), (1, 128, 64, 0), (1, 256, 32, 0), (7, 128, 16, 0), (7, 128, 128, 150), (140, 64, 32, 0),
+                                            (300, 128, 16, 0), (300, 128, 64, 64), (300, 256, 128, 0), (513, 64, 128, 0)])
+def test_attend_value_scales_of_pages_that_a_row_does_not_weigh(new, d, P, window, ratio):
+    """Value scales that are far apart.  Head 0: small ones on the early pages, large ones on the pages that only later rows
+    see.  Head 1: small ones on every other page, and all of a row's weight there.  Head 2: the large ones on the first page,
+    far behind a window or hardly weighed."""
+    H, L = 3, 700
+    g = np.random.default_rng(d + P)
+    cache, table = make([L], H, d, P, 2, garbage=False)
+    pages = table[0][: -(-L // P)].astype(int)
+    sign = g.choice([-1, 1], size=(2, d)).astype(np.int8)
+    small = np.zeros((len(pages), H), bool)
+    small[: max(1, len(pages) // 2), 0] = True
+    small[::2, 1] = True
+    small[1:, 2] = True
+    cache["k_scale"][:] = np.float32(0.01)
+    cache["v_scale"][pages] *= np.where(small, np.float32(ratio), np.float32(1))
+    turn = g.integers(1, 60, size=(len(pages), P, d)).astype(np.int8) * sign[0]
+    cache["k_codes"][pages, 1] = np.where(small[:, 1, None, None], turn, -turn)
+    cache["k_codes"][pages, 2] = np.where(small[:, 2, None, None], turn, -turn)
+    q = tokens(new, H, d, torch.float16, 3).float().numpy()
+    q[:, 1:] = np.abs(q[:, 1:]) * sign[0] * (0.5 + 4.0 / np.sqrt(d))
+    q = torch.from_numpy(q).half().cuda()
+    c = up(cache)
+    scale = 12 / math.sqrt(d)                              # heads 1 and 2: the large pages lie some e^-40 behind
+    out, lse = c.attend(q, i32([0, new]), i32([L]), i32(table), max_new=new, max_len=L, scale=scale, window=window, return_lse=True)
+    c.check()
+    check_weights(cache, pages, q, scale, out, lse, L, window)
+    low = c.attend(q.bfloat16(), i32([0, new]), i32([L]), i32(table), max_new=new, max_len=L, scale=scale, window=window, return_lse=True)
+    check_weights(cache, pages, q.bfloat16(), scale, *low, L, window)
+
+
+@pytest.mark.parametrize("new", [1, 65])
+def test_attend_many_keys_of_small_weight(new):
+    """131072 keys, one of them with 2^25.5 times the weight of each other one and values of zero: all of the output comes
+    from weights that plain fp16 would round to nothing."""
+    H, d, P, L = 1, 64, 128, 131072
+    cache, table = make([L], H, d, P, 3, garbage=False)
+    pages = table[0][: L // P].astype(int)
+    cache["k_codes"][:] = 0
+    cache["k_scale"][:] = np.float32(0.125)
+    cache["k_codes"][pages[7], 0, 5] = 64
+    cache["v_codes"][:] = np.abs(cache["v_codes"])
+    cache["v_codes"][pages[7], 0, 5] = 0
+    cache["v_scale"][:] = np.float32(0.02)
+    q = torch.full((new, 2, d), 0.5, dtype=torch.bfloat16, device="cuda")
+    scale = 25.5 * math.log(2) / (64 * 0.125 * 0.5 * d)
+    c = up(cache)
+    out, lse = c.attend(q, i32([0, new]), i32([L]), i32(table), max_new=new, max_len=L, scale=scale, return_lse=True)
+    c.check()
+    check_weights(cache, pages, q, scale, out, lse, L)
