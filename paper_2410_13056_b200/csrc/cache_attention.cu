@@ -55,7 +55,7 @@ __device__ __forceinline__ SeqPlan seq_plan(const AttnArgs& A, int64_t s, int ro
     p.n = A.b.tok_off[s + 1] - p.first;
     p.len = A.b.lens[s];
     p.bad = p.len < 0 || p.len > A.max_len || p.n < 0 || p.n > A.max_new || p.first < 0 || (int64_t)p.first + p.n > A.b.n_tok;
-    const int lo = A.window > 0 ? max(0, p.len - p.n - A.window + 1) : 0;
+    const int lo = A.window > 0 ? max(0, max(0, p.len - p.n) - A.window + 1) : 0;  // a position may be far below 0
     p.tile0 = lo / tile;
     p.tiles = p.bad ? 1 : max(1, (p.len + tile - 1) / tile - p.tile0);
     p.blocks = p.bad ? 0 : (p.n * A.group + rows - 1) / rows;
@@ -261,11 +261,11 @@ attention_rows_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_con
         // positions of the block's first and last query; keys that any of them sees
         const int p0 = p.len - p.n + (rb * kR) / g, p1 = p.len - p.n + (rb * kR + rows - 1) / g;
         const int key_hi = A.causal ? max(0, p1 + 1) : p.len;
-        const int key_lo = A.window > 0 ? max(0, p0 - A.window + 1) : 0;
+        const int key_lo = A.window > 0 ? max(0, max(0, p0) - A.window + 1) : 0;
         const int live_from = max(t_from, key_lo / kTile - p.tile0);
         const int live_to = min(t_to, (key_hi + kTile - 1) / kTile - p.tile0);
         // from this token on some row does not see a tile whole, and up to this one
-        const int whole_hi = A.causal ? min(p.len, p0 + 1) : p.len, whole_lo = A.window > 0 ? p1 - A.window + 1 : 0;
+        const int whole_hi = A.causal ? min(p.len, p0 + 1) : p.len, whole_lo = A.window > 0 ? max(0, p1) - A.window + 1 : 0;
         int row_pos[NT][2];
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
@@ -434,7 +434,7 @@ attention_rows_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_con
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
                         const int pos = row_pos[nt][e & 1];
-                        const int hi = A.causal ? min(p.len, pos + 1) : p.len, lo = A.window > 0 ? pos - A.window : -1;
+                        const int hi = A.causal ? min(p.len, pos + 1) : p.len, lo = A.window > 0 ? max(0, pos) - A.window : -1;
 #pragma unroll
                         for (int mt = 0; mt < MT; ++mt) {
                             const int key = token + mt * 16 + r + (e >> 1) * 8;
@@ -705,6 +705,7 @@ extern "C" cmpq_status cmpq_cache_attention(const cmpq_cache* cache, const cmpq_
                31 - __builtin_clz(cache->page_tokens), aligned_to(q, 16) && ldq % 8 == 0, aligned_to(out, 16) && ldo % 8 == 0,
                word, static_cast<int*>(ws), reinterpret_cast<float*>(static_cast<char*>(ws) + CMPQ_ATTENTION_ZEROED), 0};
     auto st = static_cast<cudaStream_t>(stream);
+    if (window >= max_len) a.window = 0;  // it reaches every key: a position is below max_len
     const bool bf = dt == CMPQ_BF16;
     if (prefill_pays(a)) return launch_prefill(a, dt, st);
     switch (cache->head_dim) {

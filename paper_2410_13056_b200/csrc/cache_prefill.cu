@@ -142,7 +142,7 @@ attention_prefill_kernel(const __grid_constant__ AttnArgs A, const __grid_consta
     const bool two = rows > 128;
     // positions of the first and last query, keys that any of them sees, tiles of keys
     const int p0 = len - n + (rb * 256) / g, p1 = len - n + (rb * 256 + rows - 1) / g;
-    const int key_hi = A.causal ? max(0, p1 + 1) : len, key_lo = A.window > 0 ? max(0, p0 - A.window + 1) : 0;
+    const int key_hi = A.causal ? max(0, p1 + 1) : len, key_lo = A.window > 0 ? max(0, max(0, p0) - A.window + 1) : 0;  // p0 may be far below 0
     const int tile0 = key_lo / kPfKeys, all_tiles = key_hi > key_lo ? (key_hi + kPfKeys - 1) / kPfKeys - tile0 : 0;
     const int t0 = tile0 + all_tiles * z / splits, tiles = tile0 + all_tiles * (z + 1) / splits - t0;  // this block's
     const int32_t* table = A.b.table + (int64_t)s * A.b.ld_table;
@@ -345,7 +345,7 @@ attention_prefill_kernel(const __grid_constant__ AttnArgs A, const __grid_consta
         if (work) sc_next = scales(look_up(t_first)), id_next = look_up(t_first + t_step);
         float m = -INFINITY, l = 0.0f;
         // keys [lo, hi) are seen by this row; a tile inside [all_lo, all_hi) is seen whole by the warp's rows
-        const int hi = real ? (A.causal ? min(len, pos + 1) : len) : INT32_MAX, lo = real && A.window > 0 ? pos - A.window + 1 : 0;
+        const int hi = real ? (A.causal ? min(len, pos + 1) : len) : INT32_MAX, lo = real && A.window > 0 ? max(0, pos) - A.window + 1 : 0;
         const int all_hi = __reduce_min_sync(0xffffffffu, hi), all_lo = __reduce_max_sync(0xffffffffu, lo);
         // The reference maximum has moved before keys 32 step.. of tile t: what was weighted with the old one.
         auto rescale = [&](int t, int step, float keep) {

@@ -512,3 +512,23 @@ def test_attend_many_keys_of_small_weight(new):
     out, lse = c.attend(q, i32([0, new]), i32([L]), i32(table), max_new=new, max_len=L, scale=scale, return_lse=True)
     c.check()
     check_weights(cache, pages, q, scale, out, lse, L)
+
+
+@pytest.mark.parametrize("lens,new,d", [([2, 5, 40], [6, 7, 40], 64), ([3, 1], [9, 260], 128), ([3, 200], [300, 140], 128), ([2, 30], [9, 30], 256)])
+def test_attend_windows_that_reach_everything(lens, new, d):
+    """`No limit` written as the largest integer, with rows before the first token: the same bytes as no window.  A bound of
+    the lengths that is nearly as large keeps the window, and the answer."""
+    H, P, heads = 2, 16, 4
+    cache, table = make(lens, H, d, P, 3)
+    off = np.concatenate(([0], np.cumsum(new)))
+    q = tokens(int(off[-1]), heads, d, torch.bfloat16, 5).cuda()
+    c = up(cache)
+    run = lambda **kw: c.attend(q, i32(off), i32(lens), i32(table), max_new=max(new), return_lse=True, **kw)
+    out, lse = run(max_len=max(lens))
+    check_attend(cache, off, lens, table, q, 1 / math.sqrt(d), True, 0, out, lse, torch.bfloat16)
+    for window in (2 ** 31 - 1, 2 ** 31 - 3, 2 ** 40):
+        o, l = run(max_len=max(lens), window=window)
+        assert torch.equal(o, out) and torch.equal(l, lse)
+    o, l = run(max_len=2 ** 31 - 257, window=2 ** 31 - 258)
+    check_attend(cache, off, lens, table, q, 1 / math.sqrt(d), True, 0, o, l, torch.bfloat16)
+    c.check()
