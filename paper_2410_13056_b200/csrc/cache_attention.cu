@@ -643,7 +643,7 @@ static cmpq_status launch_rows(AttnArgs a, cudaStream_t st) {
 template <int DT, int D>
 static cmpq_status launch_attention(const AttnArgs& a, cudaStream_t st) {
     // row blocks of 8 while one holds all rows of a sequence, of 16 otherwise
-    const int64_t rows = a.max_new * (a.n_heads / a.c.n_kv_heads);
+    const int64_t rows = (int64_t)a.max_new * a.group;
     return rows <= 8 ? launch_rows<DT, D, 1>(a, st) : launch_rows<DT, D, 2>(a, st);
 }
 
@@ -705,6 +705,7 @@ extern "C" cmpq_status cmpq_cache_attention(const cmpq_cache* cache, const cmpq_
                31 - __builtin_clz(cache->page_tokens), aligned_to(q, 16) && ldq % 8 == 0, aligned_to(out, 16) && ldo % 8 == 0,
                word, static_cast<int*>(ws), reinterpret_cast<float*>(static_cast<char*>(ws) + CMPQ_ATTENTION_ZEROED), 0};
     auto st = static_cast<cudaStream_t>(stream);
+    a.max_new = (int)std::min<int64_t>(max_new, batch->n_tok);  // a sequence has no more: a loose bound costs nothing
     if (window >= max_len) a.window = 0;  // it reaches every key: a position is below max_len
     const bool bf = dt == CMPQ_BF16;
     if (prefill_pays(a)) return launch_prefill(a, dt, st);

@@ -532,3 +532,17 @@ def test_attend_windows_that_reach_everything(lens, new, d):
     o, l = run(max_len=2 ** 31 - 257, window=2 ** 31 - 258)
     check_attend(cache, off, lens, table, q, 1 / math.sqrt(d), True, 0, o, l, torch.bfloat16)
     c.check()
+
+
+@pytest.mark.parametrize("d", [64, 256])
+def test_attend_with_a_loose_bound_of_the_new_tokens(d):
+    """max_new is a bound: the largest integer gives the answer that the exact one gives, in the same bytes where that
+    bound names as many tokens as there are."""
+    lens, H, P, heads = [30] * 200, 2, 16, 4
+    cache, table = make(lens, H, d, P, 3)
+    q = tokens(200, heads, d, torch.float16, 5).cuda()
+    c, off = up(cache), np.arange(201)
+    a = c.attend(q, i32(off), i32(lens), i32(table), max_new=2 ** 31 - 1, max_len=30)
+    assert torch.equal(a, c.attend(q, i32(off), i32(lens), i32(table), max_new=200, max_len=30))
+    check_attend(cache, off, lens, table, q, 1 / math.sqrt(d), True, 0, a, None, torch.float16)
+    c.check()
