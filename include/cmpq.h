@@ -526,7 +526,8 @@ cmpq_status cmpq_cache_read(const cmpq_cache* cache, const cmpq_batch* batch, cm
  * value scale is below 2^-133 of the row's largest.
  * ws: cmpq_cache_attention_ws_bytes(n_seq, n_tok, max_new, max_len, n_heads, n_kv_heads, head_dim).  Unlike other
  * work spaces its first CMPQ_ATTENTION_ZEROED bytes have to be 0 when the call's kernels start, and are 0 again when
- * they have ended (zero the buffer once, after allocating it and after bit 3 of `word`). */
+ * they have ended: zero them once, after allocating the buffer and after bit 3 of `word`, which every call on the buffer
+ * reports from then on.  Calls that may run at the same time, graphs' replays among them, need buffers of their own. */
 #define CMPQ_ATTENTION_ZEROED 4096
 size_t cmpq_cache_attention_ws_bytes(int64_t n_seq, int64_t n_tok, int64_t max_new, int64_t max_len, int32_t n_heads,
                                      int32_t n_kv_heads, int32_t head_dim);

@@ -19,7 +19,7 @@ struct AttnArgs {
     int page_bits;  // log2 of a page's tokens
     int wide_q, wide_o;
     int32_t* word;
-    int* counters;  // one per block, zero between calls
+    int* counters;  // one per block, zero between calls; the last is set when a kernel gave up, so that later calls tell too
     float* parts;   // two parts per block, then one per worker
     int workers;
 };
@@ -27,6 +27,7 @@ struct AttnArgs {
 // Weights are kept relative to 2^kWeightBits: times their value scale the largest of a row are near the top of fp16, whose
 // 30 octaves below that all count.
 constexpr float kWeightBits = 15.0f;
+constexpr int kGaveUp = CMPQ_ATTENTION_ZEROED / (int)sizeof(int) - 1;
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 
 __device__ __forceinline__ float ex2(float x) {
@@ -51,6 +52,15 @@ __device__ __forceinline__ uint32_t half_pair(uint32_t u, uint32_t pick) {
     const uint32_t h = __byte_perm(u, 0x64646464u, pick);
     const __half2 d = __hsub2(*reinterpret_cast<const __half2*>(&h), __halves2half2(__ushort_as_half(0x6480), __ushort_as_half(0x6480)));
     return *reinterpret_cast<const uint32_t*>(&d);
+}
+
+// An earlier call on this work space gave up: its counters cannot be relied on.
+__device__ __forceinline__ void report_stale(const AttnArgs& A) {
+    if (A.word && A.counters[kGaveUp]) atomicOr(A.word, kWordInternal);
+}
+__device__ __forceinline__ void report_gave_up(const AttnArgs& A) {
+    atomicOr(A.counters + kGaveUp, 1);
+    if (A.word) atomicOr(A.word, kWordInternal);
 }
 
 // Whole prompts (cache_prefill.cu): head_dim 64 and 128.

@@ -26,7 +26,7 @@ namespace cmpq {
 // Dealing the last 10 to 30 % in short runs to whichever block is free costs more in look-ups and joins than it evens out
 // (136 to 139 and 138 to 157 us); asking for later tiles in L2 makes it slower (129 / 154 / 180 us for 1 / 2 / 4 tiles
 // ahead).
-constexpr int kMaxBlocks = 512;  // counters: one per block here, behind them those of the prompts' kernel
+constexpr int kMaxBlocks = 512;  // counters: one per block here, behind them those of the prompts' kernel, the last for kGaveUp
 
 template <int D, int NT>
 struct Rows {
@@ -208,6 +208,8 @@ attention_rows_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_con
         pieces[warp][0].at = pieces[warp][1].at = nullptr;
         tc5::mbar_init_fence();
     }
+
+    if (blockIdx.x == gridDim.x - 1 && tid == 127) report_stale(A);
 
     // The total, this warp's run, and the sequence it starts in: every warp for itself, 32 sequences at a time.
     int64_t total = 0, mine = 0, upto = 0;
@@ -581,7 +583,7 @@ attention_rows_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_con
     if (*gave_up) {  // copies that were asked for have to land before the shared memory is given back
         const long long start = clock64();
         while (clock64() - start < (1ll << 21)) __nanosleep(1000);
-        if (lane == 0 && A.word) atomicOr(A.word, kWordInternal);
+        if (lane == 0) report_gave_up(A);
     }
     __syncthreads();
 

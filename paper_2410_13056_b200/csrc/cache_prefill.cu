@@ -128,6 +128,7 @@ attention_prefill_kernel(const __grid_constant__ AttnArgs A, const __grid_consta
     __shared__ float2 half_ml[128];
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int H = A.c.n_kv_heads, g = A.group, page_bits = A.page_bits;
+    if (blockIdx.x == 0 && tid == kPfThreads - 1) report_stale(A);
     // the last row blocks see most keys and come first
     const int splits = plan.splits, unit = blockIdx.x / splits, z = blockIdx.x % splits;
     const int rb = plan.row_blocks - 1 - unit / plan.per_row_block, s = unit % plan.per_row_block / H, head = unit % H;
@@ -567,7 +568,7 @@ attention_prefill_kernel(const __grid_constant__ AttnArgs A, const __grid_consta
         if (tid == 0) {
             const long long start = clock64();
             while (clock64() - start < (1ll << 21)) __nanosleep(1000);
-            if (A.word) atomicOr(A.word, kWordInternal);
+            report_gave_up(A);
         }
         __syncthreads();
     }

@@ -2,13 +2,14 @@
 // longer than the kernels (append and read back of one token: 29 us against 7), so it is done here: checks of shapes and
 // types, outputs and work spaces, the current stream.  Nothing is computed.
 #include <ATen/ATen.h>
+#include <c10/cuda/CUDAGraphsC10Utils.h>
 #include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/extension.h>
 
 #include <cmath>
 #include <optional>
-#include <unordered_map>
+#include <map>
 
 #include "cmpq.h"
 
@@ -56,24 +57,42 @@ int64_t rows(const Tensor& t, const char* name) {
     return n > 1 ? t.stride(0) : width;
 }
 
-// One buffer per stream: calls on different streams may overlap.
-struct Work {
-    std::unordered_map<void*, Tensor> held;
-    Tensor& get(void* stream, size_t bytes, const at::Device& device, bool zeroed) {
-        Tensor& t = held[stream];
-        if (!t.defined() || (size_t)t.numel() < bytes) {
-            const auto options = at::TensorOptions().dtype(at::kByte).device(device);
-            t = zeroed ? at::zeros({(int64_t)bytes}, options) : at::empty({(int64_t)bytes}, options);
-        }
+// Work spaces.  Eager calls of a device and stream share one buffer (they run one after the other), whatever layer or cache
+// they are of.  A call that is being captured takes its own from the graph's memory, zeroed by a node of that graph, and
+// leaves nothing behind: a graph never depends on another one, on eager calls, or on the stream that it is replayed on.
+struct Spaces {
+    bool zeroed;  // the first CMPQ_ATTENTION_ZEROED bytes are counters that start at 0
+    std::map<std::pair<int, void*>, Tensor> held;
+
+    Tensor get(const at::Device& device, void* stream, size_t bytes) {
+        if (c10::cuda::currentStreamCaptureStatusMayInitCtx() != c10::cuda::CaptureStatus::None) return fresh(device, bytes);
+        Tensor& t = held[{device.index(), stream}];
+        if (!t.defined() || (size_t)t.numel() < bytes) t = fresh(device, bytes);
         return t;
     }
+    Tensor fresh(const at::Device& device, size_t bytes) const {
+        Tensor t = at::empty({(int64_t)bytes}, at::TensorOptions().dtype(at::kByte).device(device));
+        if (zeroed) t.narrow(0, 0, CMPQ_ATTENTION_ZEROED).zero_();
+        return t;
+    }
+    void drop(const at::Device& device) {
+        for (auto i = held.begin(); i != held.end();) i = i->first.first == device.index() ? held.erase(i) : std::next(i);
+    }
 };
+// Never destroyed: the allocator may be gone before static objects are.
+Spaces& linear_spaces() {
+    static Spaces* s = new Spaces{false, {}};
+    return *s;
+}
+Spaces& attention_spaces() {
+    static Spaces* s = new Spaces{true, {}};
+    return *s;
+}
 
 struct Linear {
     Tensor w, scale;
     OptTensor bias;
     Tensor nonfinite;
-    Work work;
     int64_t d_in, d_out;
 
     Linear(const Tensor& w_codes, const Tensor& w_scale, const OptTensor& b) : w(w_codes), scale(w_scale) {
@@ -99,7 +118,7 @@ struct Linear {
         Tensor y = into ? *into : at::empty({n, d_out}, x.options());
         if (n == 0) return y;
         void* stream = stream_of(x);
-        const Tensor& ws = work.get(stream, cmpq_linear_i8_ws_bytes(n, d_in, d_out), x.device(), false);
+        const Tensor ws = linear_spaces().get(x.device(), stream, cmpq_linear_i8_ws_bytes(n, d_in, d_out));
         check(cmpq_linear_i8(x.data_ptr(), dt, n, d_in, rows(x, "x"), w.data_ptr<int8_t>(), d_out > 1 ? w.stride(0) : (d_in + 15) / 16 * 16,
                              scale.data_ptr<float>(), bias ? bias->data_ptr() : nullptr, d_out, y.data_ptr(), rows(y, "out"),
                              nonfinite.data_ptr<int32_t>(), ws.data_ptr(), ws.numel(), stream),
@@ -111,7 +130,6 @@ struct Linear {
 struct Cache {
     Tensor k_codes, k_scale, v_codes, v_scale, word;
     cmpq_cache c;
-    Work work;
 
     Cache(const Tensor& kc, const Tensor& ks, const Tensor& vc, const Tensor& vs) : k_codes(kc), k_scale(ks), v_codes(vc), v_scale(vs) {
         for (const Tensor* t : {&kc, &vc}) {
@@ -201,7 +219,7 @@ struct Cache {
         if (want_lse) lse = at::empty({n, h}, q.options().dtype(at::kFloat));
         void* stream = stream_of(q);
         const size_t bytes = cmpq_cache_attention_ws_bytes(b.n_seq, n, max_new, longest, (int32_t)h, c.n_kv_heads, c.head_dim);
-        const Tensor& ws = work.get(stream, bytes, q.device(), true);  // its counters start at 0
+        const Tensor ws = attention_spaces().get(q.device(), stream, bytes);
         check(cmpq_cache_attention(&c, &b, q.data_ptr(), rows(q, "q"), dt, (int32_t)h, max_new, longest,
                                    scale ? (float)*scale : 1.0f / std::sqrt((float)c.head_dim), causal, window, out.data_ptr(), rows(out, "out"),
                                    lse ? lse->data_ptr<float>() : nullptr, word.data_ptr<int32_t>(), ws.data_ptr(), ws.numel(), stream),
@@ -213,7 +231,7 @@ struct Cache {
         const c10::cuda::CUDAGuard guard(word.device());
         const cmpq_status s = cmpq_check_cache(word.data_ptr<int32_t>(), stream_of(word));
         word.zero_();
-        if (s == CMPQ_ERR_INTERNAL) work.held.clear();  // a kernel gave up: its counters may not be 0
+        if (s == CMPQ_ERR_INTERNAL) attention_spaces().drop(word.device());  // a kernel gave up: its counters may not be 0
         check(s, "cmpq_check_cache");
     }
 };

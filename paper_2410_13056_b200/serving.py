@@ -6,6 +6,9 @@ projections, the append with the rotation on the way, the attention over the cac
 Everything is enqueued on the current torch stream; nothing is computed here.  The calls of the first two are
 marshalled in C++ (csrc/serving_ext.cpp, built next to the library): wrong shapes and types raise ValueError and
 TypeError, a status of the library CmpqError.
+
+Work spaces: eager calls share one per device and stream, whatever layer or cache makes them.  All calls can be captured in
+CUDA graphs; a captured call takes its work space from its graph, so graphs may be replayed in any order and on any stream.
 """
 import torch
 
@@ -87,7 +90,7 @@ class PagedCache8:
 
     def check(self):
         """Waits for the current stream and raises CmpqError if a call so far met a NaN or an infinity (status 6) or
-        lengths and tables that do not fit (status 1); forgets what it reported."""
+        lengths and tables that do not fit (status 1), or if a kernel gave up waiting (status 5); forgets what it reported."""
         self._impl.check()
 
 
