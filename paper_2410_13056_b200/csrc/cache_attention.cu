@@ -395,7 +395,7 @@ attention_rows_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_con
 #pragma unroll
             for (int mt = 0; mt < MT; ++mt) sc[mt] = page_scale[warp][(page + ((mt * 16) >> page_bits)) & 63];
 
-            if (!tc5::mbar_wait(&bars[warp][0][slot[0]], phase[0], gave_up)) break;
+            if (!tc5::mbar_wait_warp(&bars[warp][0][slot[0]], phase[0], gave_up)) break;
             const uint8_t* kt = ring + slot[0] * C::kTileBytes;
             float st[NT][MT][4];
 #pragma unroll
@@ -490,7 +490,7 @@ attention_rows_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_con
                         for (int e = 0; e < 4; ++e) o[nt][i][e] *= keep[e & 1];
                 }
             }
-            if (!tc5::mbar_wait(&bars[warp][1][slot[1]], phase[1], gave_up)) break;
+            if (!tc5::mbar_wait_warp(&bars[warp][1][slot[1]], phase[1], gave_up)) break;
             const uint8_t* vt = ring + (kBuffers + slot[1]) * C::kTileBytes;
 #pragma unroll
             for (int mt = 0; mt < MT; ++mt)

@@ -280,13 +280,13 @@ attention_prefill_kernel(const __grid_constant__ AttnArgs A, const __grid_consta
         if (tiles > 0) pages_of(0), fetch(A.c.k_codes, kc), fetch(A.c.v_codes, vc);
         for (int t = 0; t < tiles; ++t) {
             const int slot = t & 1, phase = ((t >> 1) & 1) ^ 1;
-            if (!tc5::mbar_wait(k_empty + slot, phase, &failed)) break;
+            if (!tc5::mbar_wait_warp(k_empty + slot, phase, &failed)) break;
             put(sk + slot * C::kTileBytes, kc);
             tc5::fence_async_smem();
             __syncwarp();
             if (lane == 0) tc5::mbar_arrive(k_full + slot);
             if (t + 1 < tiles) pages_of(t + 1), fetch(A.c.k_codes, kc);
-            if (!tc5::mbar_wait(v_empty + slot, phase, &failed)) break;
+            if (!tc5::mbar_wait_warp(v_empty + slot, phase, &failed)) break;
             put(sv + slot * C::kTileBytes, vc);
             tc5::fence_async_smem();
             __syncwarp();
@@ -382,7 +382,7 @@ attention_prefill_kernel(const __grid_constant__ AttnArgs A, const __grid_consta
             const float bias = log2f(fmaxf(sc.y, 0x1p-80f)), inv_vs = ex2(-bias);  // a page of zeros has scale 0
             sc_next = scales(id_next);
             id_next = look_up(t + 2 * t_step);
-            if (!(ok = tc5::mbar_wait(s_full + w, (two ? t : t >> 1) & 1, &failed))) break;
+            if (!(ok = tc5::mbar_wait_warp(s_full + w, (two ? t : t >> 1) & 1, &failed))) break;
             tc5::fence_after_sync();
             const int key0 = (t0 + t) * kPfKeys;
             const int from = lo - key0, upto = hi - key0;
@@ -448,9 +448,8 @@ attention_prefill_kernel(const __grid_constant__ AttnArgs A, const __grid_consta
             __syncwarp();
             if (lane == 0) tc5::mbar_arrive(p_full + w);
         }
-        if (work && ok) ok = tc5::mbar_wait(o_full + w, 0, &failed);
-        if (!two && w == 1 && tiles > 0 && ok) ok = tc5::mbar_wait(o_full, 0, &failed);  // all products have ended
-        ok = __all_sync(0xffffffffu, ok);
+        if (work && ok) ok = tc5::mbar_wait_warp(o_full + w, 0, &failed);
+        if (!two && w == 1 && tiles > 0 && ok) ok = tc5::mbar_wait_warp(o_full, 0, &failed);  // all products have ended
         tc5::fence_after_sync();
         // entries 2 c .. 2 c + 63 of the row: columns c.. and D/2 + c.., whose groups 2 j and 2 j + 1 alternate
         auto columns = [&](int c, uint32_t (&x)[32], uint32_t (&y)[32]) {

@@ -3,6 +3,7 @@
 
 #include "cache.cuh"
 #include "tc5.cuh"
+#include "walk.cuh"
 
 namespace cmpq {
 
@@ -219,7 +220,7 @@ matmul_i8_tile_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_con
         const bool real = t < A.n, upper = warp >= 6;
         const float xs = real ? __ldg(A.xs + t) : 0.0f;
         asm volatile("bar.sync 1, 256;" ::: "memory");
-        tc5::mbar_wait(&done, 0, &failed);
+        tc5::mbar_wait_warp(&done, 0, &failed);
         tc5::fence_after_sync();
         if (mt * 128 + quad * 32 < A.n)
             store_rows<DT>(tmem + ((uint32_t)quad << 21), upper ? half : 0, upper ? bn : half, sb, A.bias != nullptr, xs, real,
@@ -316,27 +317,27 @@ matmul_i8_pair_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_con
         }
     } else {
         const int quad = warp & 3, upper = warp >= 6, i = threadIdx.x - 64;
-        int acc = 0, phase = 0;
-        for (int tile = first; tile < tiles; tile += step) {
-            const int mt = tile % A.m_tiles, nt = tile / A.m_tiles;
-            const int o0 = nt * 256, left = min(256, A.d_out - o0), row0 = mt * 256 + rank * 128 + quad * 32, t = row0 + lane;
-            const bool real = t < A.n;
-            const float xs = real ? __ldg(A.xs + t) : 0.0f;
-            float2* sb = reinterpret_cast<float2*>(scale_bias[acc]);
-            const int o = min(o0 + i, A.d_out - 1);
-            sb[i] = make_float2(__ldg(A.ws + o), A.bias ? widen16<DT>(A.bias[o]) : 0.0f);
-            asm volatile("bar.sync 1, 256;" ::: "memory");
-            if (!tc5::mbar_wait(acc_full + acc, phase, &failed)) break;
-            tc5::fence_after_sync();
-            if (row0 < A.n)
-                store_rows<DT>(tmem + ((uint32_t)quad << 21) + acc * 256, upper * 128, upper * 128 + 128, sb, A.bias != nullptr, xs, real,
-                               A.y + (int64_t)t * A.ldy + o0, left, A.wide);
-            tc5::fence_before_sync();
-            __syncwarp();
-            if (lane == 0) tc5::mbar_arrive_remote(acc_empty + acc, 0);
-            acc ^= 1;
-            if (acc == 0) phase ^= 1;
-        }
+        float xs = 0.0f;
+        walk_tiles(
+            first, tiles, step,
+            [&](int tile, int acc) {
+                const int t = tile % A.m_tiles * 256 + rank * 128 + quad * 32 + lane;
+                xs = t < A.n ? __ldg(A.xs + t) : 0.0f;
+                const int o = min(tile / A.m_tiles * 256 + i, A.d_out - 1);
+                reinterpret_cast<float2*>(scale_bias[acc])[i] = make_float2(__ldg(A.ws + o), A.bias ? widen16<DT>(A.bias[o]) : 0.0f);
+                asm volatile("bar.sync 1, 256;" ::: "memory");
+            },
+            [&](int acc, int parity) { return tc5::mbar_wait_warp(acc_full + acc, parity, &failed); },
+            [&](int tile, int acc) {
+                const int o0 = tile / A.m_tiles * 256, row0 = tile % A.m_tiles * 256 + rank * 128 + quad * 32, t = row0 + lane;
+                tc5::fence_after_sync();
+                if (row0 < A.n)
+                    store_rows<DT>(tmem + ((uint32_t)quad << 21) + acc * 256, upper * 128, upper * 128 + 128, reinterpret_cast<float2*>(scale_bias[acc]),
+                                   A.bias != nullptr, xs, t < A.n, A.y + (int64_t)t * A.ldy + o0, min(256, A.d_out - o0), A.wide);
+                tc5::fence_before_sync();
+                __syncwarp();
+                if (lane == 0) tc5::mbar_arrive_remote(acc_empty + acc, 0);
+            });
     }
     __syncwarp();
     __syncthreads();
