@@ -218,7 +218,7 @@ matmul_i8_tile_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_con
         }
         const int quad = warp & 3, t = mt * 128 + quad * 32 + lane, half = (bn / 16 + 1) / 2 * 16;
         const bool real = t < A.n, upper = warp >= 6;
-        const float xs = real ? __ldg(A.xs + t) : 0.0f;
+        const float xs = real ? __ldcg(A.xs + t) : 0.0f;  // written while this kernel was on its way: not the read-only path
         asm volatile("bar.sync 1, 256;" ::: "memory");
         tc5::mbar_wait_warp(&done, 0, &failed);
         tc5::fence_after_sync();
@@ -322,7 +322,7 @@ matmul_i8_pair_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_con
             first, tiles, step,
             [&](int tile, int acc) {
                 const int t = tile % A.m_tiles * 256 + rank * 128 + quad * 32 + lane;
-                xs = t < A.n ? __ldg(A.xs + t) : 0.0f;
+                xs = t < A.n ? __ldcg(A.xs + t) : 0.0f;  // see the other kernel
                 const int o = min(tile / A.m_tiles * 256 + i, A.d_out - 1);
                 reinterpret_cast<float2*>(scale_bias[acc])[i] = make_float2(__ldg(A.ws + o), A.bias ? widen16<DT>(A.bias[o]) : 0.0f);
                 asm volatile("bar.sync 1, 256;" ::: "memory");

@@ -200,3 +200,19 @@ def test_many_tiles(n, d_in, d_out, dtype):
     tol = 4 * 2.0 ** -24 * (np.abs(want) + np.abs(b)) + ref.half_ulp(np.abs(want + b) * (1 + 2.0 ** -7), dtype)
     bad = np.abs(y.float().cpu().numpy().astype(np.float64) - (want + b)) > tol
     assert not bad.any(), (int(bad.sum()), np.argwhere(bad)[:5])
+
+
+@pytest.mark.parametrize("n", [1, 37, 300])
+def test_calls_one_behind_the_other_see_their_own_scales(n):
+    """The product starts while its tokens are quantized, in the work space of the call before: inputs whose scales are
+    2^12 apart take turns, in a stream of calls that is never waited for."""
+    wc, ws = _weights(1500, 640, 4)
+    layer = serving.Int8Linear(wc, ws)
+    x = [(_tokens(n, 640, torch.bfloat16, 1).float() * f).bfloat16().cuda() for f in (1.0, 2.0 ** 12, 2.0 ** -12)]
+    want = [layer(t) for t in x]
+    torch.cuda.synchronize()
+    got = [layer(x[i % 3]) for i in range(600)]
+    torch.cuda.synchronize()
+    assert all(torch.equal(y, want[i % 3]) for i, y in enumerate(got))
+    codes, scale = ref.quantize_tokens(x[1].float().cpu().numpy())
+    _check_product(want[1], codes, scale, wc, ws, None, torch.bfloat16)
