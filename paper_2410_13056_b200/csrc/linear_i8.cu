@@ -49,7 +49,7 @@ __device__ __forceinline__ uint2 group_codes(uint4 g, float inv) {
 template <int DT, int KEEP>
 __global__ void __launch_bounds__(kQtThreads)
 quantize_tokens_kernel(const uint16_t* __restrict__ X, int64_t d, int64_t ldx, int wide, int8_t* __restrict__ codes,
-                       int64_t ldc, float* __restrict__ scale, int32_t* __restrict__ nonfinite) {
+                       int64_t ldc, float* __restrict__ scale, int32_t* __restrict__ nonfinite, int32_t* __restrict__ clear) {
     tc5::dependents_may_start();
     const uint16_t* row = X + blockIdx.x * ldx;
     int8_t* out = codes + blockIdx.x * ldc;
@@ -78,6 +78,7 @@ quantize_tokens_kernel(const uint16_t* __restrict__ X, int64_t d, int64_t ldx, i
     if (amax < 0x1p-120f) s = inv = 0.0f;
     if (t == 0) {
         scale[blockIdx.x] = s;
+        if (clear && blockIdx.x == 0) *clear = 0;  // the mark of the product behind this, which sets it only after waiting for this kernel
         if (m >= (DT == CMPQ_BF16 ? 0x7f80u : 0x7c00u) && nonfinite) atomicOr(nonfinite, 1);
     }
 #pragma unroll
@@ -413,9 +414,8 @@ extern "C" size_t cmpq_linear_i8_ws_bytes(int64_t n, int64_t d_in, int64_t d_out
     return linear_i8_codes_bytes(n, d_in) + round_up((size_t)n * sizeof(float), 256) + 256;
 }
 
-extern "C" cmpq_status cmpq_quantize_tokens(const void* X, cmpq_dtype dt, int64_t n, int64_t d, int64_t ldx,
-                                            int8_t* codes, int64_t ldc, float* scale, int32_t* nonfinite,
-                                            void* stream) {
+static cmpq_status quantize(const void* X, cmpq_dtype dt, int64_t n, int64_t d, int64_t ldx, int8_t* codes, int64_t ldc, float* scale,
+                            int32_t* nonfinite, int32_t* clear, void* stream) {
     if (dt != CMPQ_F16 && dt != CMPQ_BF16) return CMPQ_ERR_INVALID_ARG;
     if (n < 0 || n > INT32_MAX || d < 1 || d > CMPQ_MAX_D_IN || ldx < d || ldc < d || ldc % 16) return CMPQ_ERR_INVALID_ARG;
     if (n == 0) return CMPQ_OK;
@@ -425,7 +425,7 @@ extern "C" cmpq_status cmpq_quantize_tokens(const void* X, cmpq_dtype dt, int64_
     auto st = static_cast<cudaStream_t>(stream);
     const unsigned rows = (unsigned)n;
     const int64_t keep = (d + 8 * kQtThreads - 1) / (8 * kQtThreads);
-    auto launch = [&](auto kernel) { return launch_cluster(kernel, rows, kQtThreads, 0, 1, false, st, x, d, ldx, wide, codes, ldc, scale, nonfinite); };
+    auto launch = [&](auto kernel) { return launch_cluster(kernel, rows, kQtThreads, 0, 1, false, st, x, d, ldx, wide, codes, ldc, scale, nonfinite, clear); };
     if (dt == CMPQ_BF16)
         return keep <= 2   ? launch(quantize_tokens_kernel<CMPQ_BF16, 2>)
                : keep <= 4 ? launch(quantize_tokens_kernel<CMPQ_BF16, 4>)
@@ -435,17 +435,27 @@ extern "C" cmpq_status cmpq_quantize_tokens(const void* X, cmpq_dtype dt, int64_
                        : launch(quantize_tokens_kernel<CMPQ_F16, 8>);
 }
 
-// The caller has checked everything.  `word`, or the last 256 bytes of the work space where there is none, takes the mark
-// of a kernel that gave up.
+extern "C" cmpq_status cmpq_quantize_tokens(const void* X, cmpq_dtype dt, int64_t n, int64_t d, int64_t ldx,
+                                            int8_t* codes, int64_t ldc, float* scale, int32_t* nonfinite,
+                                            void* stream) {
+    return quantize(X, dt, n, d, ldx, codes, ldc, scale, nonfinite, nullptr, stream);
+}
+
+// Where a call without a word of the caller's keeps the mark of a kernel that gave up; it starts from 0 in every call.
+static int32_t* mark_of(void* ws, int64_t n, int64_t d_in, int64_t d_out) {
+    return reinterpret_cast<int32_t*>(static_cast<char*>(ws) + cmpq_linear_i8_ws_bytes(n, d_in, d_out) - 256);
+}
+
+// The caller has checked everything.
 static cmpq_status product(const int8_t* xc, int64_t ldxc, const float* xs, const int8_t* wc, int64_t ldwc, const float* w_scale, const void* bias,
-                           cmpq_dtype dt, int64_t n, int64_t d_in, int64_t d_out, void* y, int64_t ldy, int32_t* word, void* ws, bool behind, void* stream) {
+                           cmpq_dtype dt, int64_t n, int64_t d_in, int64_t d_out, void* y, int64_t ldy, int32_t* word, bool behind, void* stream) {
     ProductArgs a = {};
     a.xs = xs, a.ws = w_scale;
     a.bias = static_cast<const uint16_t*>(bias);
     a.y = static_cast<uint16_t*>(y);
     a.ldy = ldy;
     a.n = (int)n, a.d_out = (int)d_out;
-    a.failed = word ? word : reinterpret_cast<int32_t*>(static_cast<char*>(ws) + cmpq_linear_i8_ws_bytes(n, d_in, d_out) - 256);
+    a.failed = word;
     auto st = static_cast<cudaStream_t>(stream);
     return dt == CMPQ_BF16 ? launch_product<CMPQ_BF16>(xc, ldxc, wc, ldwc, d_in, a, behind, st)
                            : launch_product<CMPQ_F16>(xc, ldxc, wc, ldwc, d_in, a, behind, st);
@@ -461,7 +471,9 @@ extern "C" cmpq_status cmpq_matmul_i8(const int8_t* xc, int64_t ldxc, const floa
         !aligned_to(w_scale, 4) || !aligned_to(y, 2) || !aligned_to(bias, 2))
         return CMPQ_ERR_INVALID_ARG;
     if (!ws || !aligned_to(ws, 256) || ws_bytes < cmpq_linear_i8_ws_bytes(n, d_in, d_out)) return CMPQ_ERR_WORKSPACE;
-    return product(xc, ldxc, xs, wc, ldwc, w_scale, bias, dt, n, d_in, d_out, y, ldy, nullptr, ws, false, stream);
+    int32_t* mark = mark_of(ws, n, d_in, d_out);
+    if (cudaMemsetAsync(mark, 0, sizeof(*mark), static_cast<cudaStream_t>(stream)) != cudaSuccess) return CMPQ_ERR_CUDA;
+    return product(xc, ldxc, xs, wc, ldwc, w_scale, bias, dt, n, d_in, d_out, y, ldy, mark, false, stream);
 }
 
 extern "C" cmpq_status cmpq_linear_i8(const void* X, cmpq_dtype dt, int64_t n, int64_t d_in, int64_t ldx,
@@ -478,8 +490,9 @@ extern "C" cmpq_status cmpq_linear_i8(const void* X, cmpq_dtype dt, int64_t n, i
     int8_t* codes = w.take<int8_t>(linear_i8_codes_bytes(n, d_in));
     float* scale = w.take<float>(n);
     const int64_t ldc = (int64_t)round_up(d_in, 16);
-    cmpq_status st = cmpq_quantize_tokens(X, dt, n, d_in, ldx, codes, ldc, scale, nonfinite, stream);
+    int32_t* mark = mark_of(ws, n, d_in, d_out);
+    cmpq_status st = quantize(X, dt, n, d_in, ldx, codes, ldc, scale, nonfinite, nonfinite ? nullptr : mark, stream);
     if (st != CMPQ_OK) return st;
     // the quantization lets the product start early; it was itself started after everything before it, the weights too
-    return product(codes, ldc, scale, wc, ldwc, w_scale, bias, dt, n, d_in, d_out, y, ldy, nonfinite, ws, true, stream);
+    return product(codes, ldc, scale, wc, ldwc, w_scale, bias, dt, n, d_in, d_out, y, ldy, nonfinite ? nonfinite : mark, true, stream);
 }

@@ -216,3 +216,26 @@ def test_calls_one_behind_the_other_see_their_own_scales(n):
     assert all(torch.equal(y, want[i % 3]) for i, y in enumerate(got))
     codes, scale = ref.quantize_tokens(x[1].float().cpu().numpy())
     _check_product(want[1], codes, scale, wc, ws, None, torch.bfloat16)
+
+
+@pytest.mark.parametrize("n", [1, 300])
+def test_mark_in_the_work_space_starts_from_zero(n):
+    """Calls without a word keep the mark of a kernel that gave up in the work space, whose contents are undefined before
+    the call: it reads 0 after a product that ended well, and the caller's word is used where there is one."""
+    d_in, d_out = 256, 512
+    wc, ws = _weights(d_out, d_in, 4)
+    x = _tokens(n, d_in, torch.float16, 2).cuda()
+    xc, xs = torch.empty(n, d_in, dtype=torch.int8, device="cuda"), torch.empty(n, device="cuda")
+    B.cmpq_quantize_tokens(x, xc, xs)
+    size = B.cmpq_linear_i8_ws_bytes(n, d_in, d_out)
+    want = serving.Int8Linear(wc, ws)(x)
+    for call in ("matmul", "linear", "word"):
+        buf = torch.full((size,), 255, dtype=torch.uint8, device="cuda")
+        mark = buf[size - 256: size - 252].view(torch.int32)
+        y, word = torch.empty_like(want), torch.zeros(1, dtype=torch.int32, device="cuda")
+        if call == "matmul":
+            B.cmpq_matmul_i8(xc, xs, wc, ws, None, y, buf)
+        else:
+            B.cmpq_linear_i8(x, wc, ws, None, y, buf, word if call == "word" else None)
+        assert int(mark if call != "word" else word) == 0 and torch.equal(y, want), call
+        B.cmpq_check_cache(mark if call != "word" else word)
