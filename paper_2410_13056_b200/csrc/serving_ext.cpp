@@ -89,6 +89,14 @@ Spaces& attention_spaces() {
     return *s;
 }
 
+// What the calls on this word have reported, once the current stream of its device has got there; it starts again from 0.
+cmpq_status take_word(const Tensor& word) {
+    const c10::cuda::CUDAGuard guard(word.device());
+    const cmpq_status s = cmpq_check_cache(word.data_ptr<int32_t>(), stream_of(word));
+    if (s != CMPQ_OK) word.zero_();
+    return s;
+}
+
 struct Linear {
     Tensor w, scale;
     OptTensor bias;
@@ -125,6 +133,8 @@ struct Linear {
               "cmpq_linear_i8");
         return y;
     }
+
+    void look() { check(take_word(nonfinite), "cmpq_linear_i8"); }
 };
 
 struct Cache {
@@ -228,9 +238,7 @@ struct Cache {
     }
 
     void look() {
-        const c10::cuda::CUDAGuard guard(word.device());
-        const cmpq_status s = cmpq_check_cache(word.data_ptr<int32_t>(), stream_of(word));
-        word.zero_();
+        const cmpq_status s = take_word(word);
         if (s == CMPQ_ERR_INTERNAL) attention_spaces().drop(word.device());  // a kernel gave up: its counters may not be 0
         check(s, "cmpq_check_cache");
     }
@@ -250,6 +258,7 @@ PYBIND11_MODULE(_serving, m) {
     py::class_<Linear>(m, "Linear")
         .def(py::init<const Tensor&, const Tensor&, const OptTensor&>())
         .def("__call__", &Linear::call, py::arg("x"), py::arg("out") = py::none())
+        .def("check", &Linear::look)
         .def_readonly("w_codes", &Linear::w)
         .def_readonly("w_scale", &Linear::scale)
         .def_readonly("bias", &Linear::bias)

@@ -35,7 +35,7 @@ class Int8Linear:
         self._impl = _ext().Linear(w_codes, w_scale, bias)
         self.w_codes, self.w_scale, self.bias = w_codes, self._impl.w_scale, self._impl.bias
         self.d_out, self.d_in = w_codes.shape
-        self.nonfinite = self._impl.nonfinite  # bit 0: some token so far held a NaN or an infinity
+        self.nonfinite = self._impl.nonfinite  # what check() looks at: bit 0 a NaN or an infinity, bit 3 a kernel gave up waiting
 
     @classmethod
     def from_weight(cls, weight, bias=None):
@@ -49,6 +49,11 @@ class Int8Linear:
     def __call__(self, x, out=None):
         """x: fp16/bf16 [n][d_in].  Returns out [n][d_out] of x's dtype."""
         return self._impl(x, out)
+
+    def check(self):
+        """Waits for the current stream and raises CmpqError if a token of a call so far held a NaN or an infinity (status
+        6) or a kernel gave up waiting, its output unspecified (status 5); forgets what it reported."""
+        self._impl.check()
 
 
 class PagedCache8:
@@ -114,3 +119,14 @@ class AttentionLayer8:
         self.cache.append(k, v, tok_off, lens, table, q=q, cos=self.cos, sin=self.sin, interleaved=self.interleaved, q_out=q)
         a = self.cache.attend(q, tok_off, lens, table, max_new, max_len, window=window)
         return self.out(a.flatten(1))
+
+    def check(self):
+        """check() of both projections and of the cache; raises the first of their errors, and all forget theirs."""
+        errors = []
+        for part in (self.qkv, self.cache, self.out):
+            try:
+                part.check()
+            except B.CmpqError as e:
+                errors.append(e)
+        if errors:
+            raise errors[0]

@@ -147,3 +147,32 @@ def test_a_work_space_that_a_kernel_gave_up_on_is_reported_by_later_calls(new):
     with pytest.raises(B.CmpqError) as e:
         B.cmpq_check_cache(word)
     assert e.value.status == 5
+
+
+def test_layer_reports_what_its_calls_met():
+    """NaN and infinity in the activations reach the user through check(), once; so does the mark of a kernel that gave up."""
+    step, page = _step(3, 0)
+    layer = _layer(page)
+    layer(**step)
+    layer.check()
+    step["x"][1, 7] = float("nan")
+    layer(**step)
+    for part in (layer.qkv, layer):                        # the projection's report, then the cache's and the output's
+        with pytest.raises(B.CmpqError) as e:
+            part.check()
+        assert e.value.status == 6
+    layer.check()
+    linear = layer.out
+    x = torch.zeros(2, HEADS * D, dtype=torch.float16, device="cuda")
+    x[1, 3] = float("inf")
+    linear(x)
+    with pytest.raises(B.CmpqError) as e:
+        linear.check()
+    assert e.value.status == 6
+    linear(x[:1])
+    linear.check()
+    linear.nonfinite.fill_(8)
+    with pytest.raises(B.CmpqError) as e:
+        linear.check()
+    assert e.value.status == 5
+    linear.check()
