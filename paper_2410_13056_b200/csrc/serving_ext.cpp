@@ -48,6 +48,14 @@ void on_gpu(const Tensor& t, const char* name, int64_t dims) {
     if (!t.is_cuda() || t.dim() != dims) refuse(std::string(name) + " needs to be a " + std::to_string(dims) + "-dimensional CUDA tensor, got shape " + shape_of(t));
 }
 
+// A kernel runs on one device and takes addresses as they are.
+void beside(const Tensor& t, const Tensor& home, const char* name) {
+    if (t.device() != home.device()) refuse(std::string(name) + " is on " + t.device().str() + ", the rest on " + home.device().str());
+}
+void beside(const OptTensor& t, const Tensor& home, const char* name) {
+    if (t) beside(*t, home, name);
+}
+
 // Leading dimension of [n][width] or [n][heads][d] with contiguous rows.
 int64_t rows(const Tensor& t, const char* name) {
     const bool three = t.dim() == 3;
@@ -106,6 +114,7 @@ struct Linear {
     Linear(const Tensor& w_codes, const Tensor& w_scale, const OptTensor& b) : w(w_codes), scale(w_scale) {
         on_gpu(w, "w_codes", 2);
         on_gpu(scale, "w_scale", 1);
+        beside(scale, w, "w_scale"), beside(b, w, "bias");
         if (w.scalar_type() != at::kChar || scale.scalar_type() != at::kFloat) refuse("w_codes needs to be int8, w_scale float32");
         if (w.stride(1) != 1 || w.stride(0) % 16 || (uintptr_t)w.data_ptr() % 16) refuse("w_codes needs rows that start on multiples of 16 bytes");
         d_out = w.size(0), d_in = w.size(1);
@@ -117,6 +126,7 @@ struct Linear {
 
     Tensor call(const Tensor& x, const OptTensor& into) {
         if (x.dim() != 2 || x.size(1) != d_in || !x.is_cuda()) refuse("x needs shape [n][" + std::to_string(d_in) + "] on the GPU, got " + shape_of(x));
+        beside(x, w, "x"), beside(into, w, "out");
         const cmpq_dtype dt = code(x);
         if (bias && bias->scalar_type() != x.scalar_type()) throw py::type_error("bias and x need one dtype");
         const int64_t n = x.size(0);
@@ -150,18 +160,21 @@ struct Cache {
             on_gpu(*t, "scales", 2);
             if (t->scalar_type() != at::kFloat) refuse("scales need to be float32");
         }
+        beside(ks, kc, "k_scale"), beside(vc, kc, "v_codes"), beside(vs, kc, "v_scale");
         if (kc.sizes() != vc.sizes() || ks.sizes() != kc.sizes().slice(0, 2) || vs.sizes() != ks.sizes())
             refuse("codes need shape [n_pages][n_kv][page_tokens][head_dim] and scales [n_pages][n_kv]");
         if (!kc.is_contiguous() || !vc.is_contiguous() || !ks.is_contiguous() || !vs.is_contiguous()) refuse("the cache's tensors need to be contiguous");
-        c = {kc.data_ptr<int8_t>(), ks.data_ptr<float>(), vc.data_ptr<int8_t>(), vs.data_ptr<float>(), kc.size(0),
-             (int32_t)kc.size(1), (int32_t)kc.size(3), (int32_t)kc.size(2)};
+        c = {static_cast<int8_t*>(kc.data_ptr()), static_cast<float*>(ks.data_ptr()), static_cast<int8_t*>(vc.data_ptr()),
+             static_cast<float*>(vs.data_ptr()),  kc.size(0),                         (int32_t)kc.size(1),
+             (int32_t)kc.size(3),                 (int32_t)kc.size(2)};
         word = at::zeros({1}, at::TensorOptions().dtype(at::kInt).device(kc.device()));
     }
 
-    static cmpq_batch batch(const Tensor& off, const Tensor& lens, const Tensor& table, int64_t n_tok) {
+    cmpq_batch batch(const Tensor& off, const Tensor& lens, const Tensor& table, int64_t n_tok) const {
         on_gpu(off, "tok_off", 1);
         on_gpu(lens, "lens", 1);
         on_gpu(table, "table", 2);
+        beside(off, k_codes, "tok_off"), beside(lens, k_codes, "lens"), beside(table, k_codes, "table");
         if (off.scalar_type() != at::kInt || lens.scalar_type() != at::kInt || table.scalar_type() != at::kInt) refuse("tok_off, lens and table need to be int32");
         const int64_t n = table.size(0);
         if (off.size(0) != n + 1 || lens.size(0) != n) refuse("tok_off needs n_seq + 1 entries and table n_seq rows, n_seq = " + std::to_string(lens.size(0)));
@@ -173,6 +186,7 @@ struct Cache {
         if (t.dim() != 3 || t.size(2) != c.head_dim || (count && t.size(1) != count) || !t.is_cuda())
             refuse(std::string(name) + " needs shape [n_tok][" + (count ? std::to_string(count) : std::string("heads")) + "][" + std::to_string(c.head_dim) +
                    "] on the GPU, got " + shape_of(t));
+        beside(t, k_codes, name);
     }
 
     OptTensor append(const Tensor& k, const Tensor& v, const Tensor& off, const Tensor& lens, const Tensor& table, const OptTensor& q, const OptTensor& cos,
@@ -185,15 +199,16 @@ struct Cache {
         if (cos && (cos->dim() != 2 || cos->sizes() != sin->sizes() || !cos->is_contiguous() || !sin->is_contiguous() || cos->scalar_type() != at::kFloat ||
                     sin->scalar_type() != at::kFloat || !cos->is_cuda() || !sin->is_cuda()))
             refuse("cos and sin need to be contiguous fp32 CUDA tensors of one shape");
+        beside(cos, k_codes, "cos"), beside(sin, k_codes, "sin"), beside(q_into, k_codes, "q_out");
+        if (q) heads(*q, "q", 0);
+        const cmpq_batch b = batch(off, lens, table, k.size(0));
         const c10::cuda::CUDAGuard guard(k.device());
         OptTensor q_out;
         if (q) {
-            heads(*q, "q", 0);
             if (q->scalar_type() != k.scalar_type() || q->size(0) != k.size(0)) refuse("q needs k's dtype and token count");
             if (q_into && (q_into->sizes() != q->sizes() || q_into->scalar_type() != q->scalar_type() || !q_into->is_cuda())) refuse("q_out needs q's shape and dtype");
             q_out = q_into ? *q_into : at::empty(q->sizes(), q->options());
         }
-        const cmpq_batch b = batch(off, lens, table, k.size(0));
         check(cmpq_cache_append(&c, &b, k.data_ptr(), rows(k, "k"), v.data_ptr(), rows(v, "v"), dt, cos ? cos->data_ptr<float>() : nullptr,
                                 sin ? sin->data_ptr<float>() : nullptr, cos ? cos->size(0) : 0, cos ? (int32_t)(2 * cos->size(1)) : 0, interleaved,
                                 q ? q->data_ptr() : nullptr, q ? rows(*q, "q") : 0, q ? (int32_t)q->size(1) : 0, q ? q_out->data_ptr() : nullptr,
@@ -203,10 +218,10 @@ struct Cache {
     }
 
     std::pair<Tensor, Tensor> read(const Tensor& off, const Tensor& lens, const Tensor& table, int64_t n_tok, bool bf16) {
+        const cmpq_batch b = batch(off, lens, table, n_tok);
         const c10::cuda::CUDAGuard guard(k_codes.device());
         const auto options = k_codes.options().dtype(bf16 ? at::kBFloat16 : at::kHalf);
         Tensor k = at::empty({n_tok, c.n_kv_heads, c.head_dim}, options), v = at::empty({n_tok, c.n_kv_heads, c.head_dim}, options);
-        const cmpq_batch b = batch(off, lens, table, n_tok);
         check(cmpq_cache_read(&c, &b, bf16 ? CMPQ_BF16 : CMPQ_F16, k.data_ptr(), v.data_ptr(), (int64_t)c.n_kv_heads * c.head_dim, word.data_ptr<int32_t>(),
                               stream_of(k_codes)),
               "cmpq_cache_read");
@@ -221,8 +236,9 @@ struct Cache {
         const int64_t n = q.size(0), h = q.size(1);
         if (h == 0 || h % c.n_kv_heads) refuse(std::to_string(h) + " query heads are no multiple of the cache's " + std::to_string(c.n_kv_heads) + " heads");
         if (into && (into->sizes() != q.sizes() || into->scalar_type() != q.scalar_type() || !into->is_cuda())) refuse("out needs q's shape and dtype");
-        const c10::cuda::CUDAGuard guard(q.device());
+        beside(into, k_codes, "out");
         const cmpq_batch b = batch(off, lens, table, n);
+        const c10::cuda::CUDAGuard guard(q.device());
         const int64_t longest = max_len ? *max_len : table.size(1) * c.page_tokens;
         Tensor out = into ? *into : at::empty(q.sizes(), q.options());
         OptTensor lse;
