@@ -486,6 +486,7 @@ typedef struct {
     int64_t ld_table;
     int64_t n_seq;
     int64_t n_tok;
+    int64_t table_cols; /* entries of a table row that may be read; 0: ld_table (a row that is part of a wider one has fewer) */
 } cmpq_batch;
 
 cmpq_status cmpq_check_cache(const int32_t* word, void* stream);

@@ -47,7 +47,8 @@ class Cache(ctypes.Structure):
 class Batch(ctypes.Structure):
     """cmpq_batch"""
     _fields_ = [("tok_off", ctypes.c_void_p), ("lens", ctypes.c_void_p), ("table", ctypes.c_void_p),
-                ("ld_table", ctypes.c_int64), ("n_seq", ctypes.c_int64), ("n_tok", ctypes.c_int64)]
+                ("ld_table", ctypes.c_int64), ("n_seq", ctypes.c_int64), ("n_tok", ctypes.c_int64),
+                ("table_cols", ctypes.c_int64)]
 
 
 _LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libcmpq.so")

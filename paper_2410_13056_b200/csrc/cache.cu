@@ -256,7 +256,7 @@ __device__ __forceinline__ Place place_of(const AppendArgs& A, int64_t slot, boo
     const int64_t page = start / P + (slot - (from / P + 2 * (int64_t)s));
     if (page * P >= len || page < start / P) return p;
     const int64_t lo = max(start, page * P), hi = min(len, (page + 1) * P);
-    const int id = page < A.b.ld_table ? A.b.table[s * A.b.ld_table + page] : -1;
+    const int id = page < A.b.table_cols ? A.b.table[s * A.b.ld_table + page] : -1;
     if (id < 0 || id >= A.c.n_pages || (keys && A.rot && hi > A.n_pos)) {
         if (threadIdx.x == 0) report(A.word, kWordTable);
         return p;
@@ -471,7 +471,7 @@ cache_read_kernel(const __grid_constant__ ReadArgs A) {
         while (s < A.b.n_seq && off[s + 1] <= t) ++s;
         if (t < A.b.n_tok && s < A.b.n_seq) {
             const int64_t pos = (int64_t)A.b.lens[s] - off[s + 1] + t, page = pos >= 0 ? pos / P : 0;
-            found = pos >= 0 && page < A.b.ld_table ? A.b.table[s * A.b.ld_table + page] : -1;
+            found = pos >= 0 && page < A.b.table_cols ? A.b.table[s * A.b.ld_table + page] : -1;
             place = (int)(pos - page * P);
             if (found < 0 || found >= A.c.n_pages) {
                 found = -1;
@@ -581,7 +581,7 @@ extern "C" cmpq_status cmpq_cache_append(const cmpq_cache* cache, const cmpq_bat
     if (!k || !v || !aligned_to(k, 2) || !aligned_to(v, 2) || !aligned_to(q, 2) || !aligned_to(q_out, 2)) return CMPQ_ERR_INVALID_ARG;
     AppendArgs a;
     a.c = *cache;
-    a.b = *batch;
+    a.b = bounded(*batch);
     a.k = static_cast<const uint16_t*>(k);
     a.v = static_cast<const uint16_t*>(v);
     a.q = static_cast<const uint16_t*>(q);
@@ -618,7 +618,7 @@ extern "C" cmpq_status cmpq_cache_read(const cmpq_cache* cache, const cmpq_batch
     if (ldo < (int64_t)cache->n_kv_heads * cache->head_dim) return CMPQ_ERR_INVALID_ARG;
     if (batch->n_seq == 0 || batch->n_tok == 0) return CMPQ_OK;
     if (!k_out || !v_out || !aligned_to(k_out, 2) || !aligned_to(v_out, 2)) return CMPQ_ERR_INVALID_ARG;
-    ReadArgs a{*cache, *batch, static_cast<uint16_t*>(k_out), static_cast<uint16_t*>(v_out), ldo,
+    ReadArgs a{*cache, bounded(*batch), static_cast<uint16_t*>(k_out), static_cast<uint16_t*>(v_out), ldo,
                aligned_to(k_out, 16) && aligned_to(v_out, 16) && ldo % 8 == 0, word};
     auto st = static_cast<cudaStream_t>(stream);
     return dt == CMPQ_BF16 ? launch_read<CMPQ_BF16>(a, st) : launch_read<CMPQ_F16>(a, st);

@@ -105,10 +105,16 @@ inline bool cache_ok(const cmpq_cache* c, cmpq_status* why) {
 }
 
 inline bool batch_ok(const cmpq_batch* b) {
-    return b && b->n_seq >= 0 && b->n_seq <= 65536 && b->n_tok >= 0 && b->n_tok < INT32_MAX && b->ld_table >= 0 &&
+    return b && b->n_seq >= 0 && b->n_seq <= 65536 && b->n_tok >= 0 && b->n_tok < INT32_MAX && b->ld_table >= 0 && b->table_cols >= 0 &&
            (b->n_seq == 0 || b->n_tok == 0 ||
             (b->tok_off && b->lens && b->table && b->ld_table >= 1 && aligned_to(b->tok_off, 4) && aligned_to(b->lens, 4) &&
              aligned_to(b->table, 4)));
+}
+
+// The batch with the number of entries that a table row has.
+inline cmpq_batch bounded(cmpq_batch b) {
+    if (b.table_cols == 0) b.table_cols = b.ld_table;
+    return b;
 }
 
 }  // namespace cmpq

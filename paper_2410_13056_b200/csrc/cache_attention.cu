@@ -283,7 +283,7 @@ attention_rows_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_con
             const int page = page0 + have + lane;
             my_page = -1;
             if (page < page_end) {
-                my_page = page < A.b.ld_table ? __ldg(A.b.table + s * A.b.ld_table + page) : -1;
+                my_page = page < A.b.table_cols ? __ldg(A.b.table + s * A.b.ld_table + page) : -1;
                 if (my_page < 0 || my_page >= A.c.n_pages) {
                     my_page = -1;
                     if (A.word) atomicOr(A.word, kWordTable);
@@ -702,7 +702,7 @@ extern "C" cmpq_status cmpq_cache_attention(const cmpq_cache* cache, const cmpq_
     if (!ws || !aligned_to(ws, 256) ||
         ws_bytes < cmpq_cache_attention_ws_bytes(batch->n_seq, batch->n_tok, max_new, max_len, n_heads, cache->n_kv_heads, cache->head_dim))
         return CMPQ_ERR_WORKSPACE;
-    AttnArgs a{*cache, *batch, static_cast<const uint16_t*>(q), static_cast<uint16_t*>(out), lse, ldq, ldo, (int)max_new, (int)max_len,
+    AttnArgs a{*cache, bounded(*batch), static_cast<const uint16_t*>(q), static_cast<uint16_t*>(out), lse, ldq, ldo, (int)max_new, (int)max_len,
                (int)std::min<int64_t>(window, INT32_MAX), scale * kLog2e, n_heads, n_heads / cache->n_kv_heads, causal != 0,
                31 - __builtin_clz(cache->page_tokens), aligned_to(q, 16) && ldq % 8 == 0, aligned_to(out, 16) && ldo % 8 == 0,
                word, static_cast<int*>(ws), reinterpret_cast<float*>(static_cast<char*>(ws) + CMPQ_ATTENTION_ZEROED), 0};

@@ -149,7 +149,7 @@ attention_prefill_kernel(const __grid_constant__ AttnArgs A, const __grid_consta
     const int32_t* table = A.b.table + (int64_t)s * A.b.ld_table;
     const int pages = (len + (1 << page_bits) - 1) >> page_bits;
     auto page_of = [&](int page) {  // -1 where there is none
-        const int id = page < pages && page < A.b.ld_table ? __ldg(table + page) : -1;
+        const int id = page < pages && page < A.b.table_cols ? __ldg(table + page) : -1;
         if (id >= 0 && id < A.c.n_pages) return id;
         if (page < pages && A.word) atomicOr(A.word, kWordTable);
         return -1;
@@ -334,7 +334,7 @@ attention_prefill_kernel(const __grid_constant__ AttnArgs A, const __grid_consta
         int id_next = -1;
         auto look_up = [&](int t) {  // not looked at here; the warps that widen the codes report what is no page
             const int page = ((t0 + t) * kPfKeys >> page_bits) + lane;
-            return lane < per_tile && t < tiles && page < min(pages, (int)min((int64_t)INT32_MAX, A.b.ld_table)) ? __ldg(table + page) : -1;
+            return lane < per_tile && t < tiles && page < min(pages, (int)min((int64_t)INT32_MAX, A.b.table_cols)) ? __ldg(table + page) : -1;
         };
         auto scales = [&](int id) {
             return id < 0 || id >= A.c.n_pages ? make_float2(0.0f, 0.0f)

@@ -179,7 +179,7 @@ struct Cache {
         const int64_t n = table.size(0);
         if (off.size(0) != n + 1 || lens.size(0) != n) refuse("tok_off needs n_seq + 1 entries and table n_seq rows, n_seq = " + std::to_string(lens.size(0)));
         if (!off.is_contiguous() || !lens.is_contiguous() || (table.size(1) > 1 && table.stride(1) != 1)) refuse("tok_off, lens and table need contiguous rows");
-        return {off.data_ptr<int32_t>(), lens.data_ptr<int32_t>(), table.data_ptr<int32_t>(), n > 1 ? table.stride(0) : table.size(1), n, n_tok};
+        return {off.data_ptr<int32_t>(), lens.data_ptr<int32_t>(), table.data_ptr<int32_t>(), n > 1 ? table.stride(0) : table.size(1), n, n_tok, table.size(1)};
     }
 
     void heads(const Tensor& t, const char* name, int64_t count) const {

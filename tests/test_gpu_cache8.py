@@ -546,3 +546,37 @@ def test_attend_with_a_loose_bound_of_the_new_tokens(d):
     assert torch.equal(a, c.attend(q, i32(off), i32(lens), i32(table), max_new=200, max_len=30))
     check_attend(cache, off, lens, table, q, 1 / math.sqrt(d), True, 0, a, None, torch.float16)
     c.check()
+
+
+@pytest.mark.parametrize("row", [0, 2], ids=["first", "last"])
+def test_a_table_that_is_part_of_a_wider_one_ends_with_its_columns(row):
+    """Lengths that need more pages than the columns of the table given: reported, and nothing beyond the columns is used,
+    though the wider table has pages there (and memory ends behind its last row)."""
+    H, d, P = 2, 64, 16
+    wide = i32(np.arange(18).reshape(3, 6))
+    table = wide[:, 3:5]                                   # two pages a sequence, row stride 6
+    lens = [20, 20, 20]
+    k = tokens(3, H, d, torch.float16, 1).cuda()
+    c = serving.PagedCache8.empty(18, H, d, P)
+    args = (i32([0, 1, 2, 3]), i32(lens), table)
+    c.append(k, k, *args)
+    c.check()
+    same = serving.PagedCache8.empty(18, H, d, P)
+    same.append(k, k, args[0], args[1], table.contiguous())
+    assert torch.equal(c.k_codes, same.k_codes) and torch.equal(c.attend(k, *args, 1), same.attend(k, *args[:2], table.contiguous(), 1))
+    lens[row] = 33
+    for new in (1, 70):                                    # few rows; many, in the kernel for prompts
+        before = [t.clone() for t in (c.k_codes, c.k_scale, c.v_codes, c.v_scale)]
+        off = np.arange(4) if new == 1 else np.concatenate(([0], np.cumsum([new if s == row else 0 for s in range(3)])))
+        lens[row] = 33 if new == 1 else 100
+        x = tokens(int(off[-1]), H, d, torch.float16, 2).cuda()
+        q = tokens(int(off[-1]), 4 * H, d, torch.float16, 3).cuda()
+        for call in (lambda: c.append(x, x, i32(off), i32(lens), table), lambda: c.read(i32(off), i32(lens), table, int(off[-1])),
+                     lambda: c.attend(q, i32(off), i32(lens), table, new, 200)):
+            call()
+            with pytest.raises(B.CmpqError) as e:
+                c.check()
+            assert e.value.status == 1
+        others = [p for p in range(18) if p not in wide[:, 3:5].flatten().tolist()]
+        for t, was in zip((c.k_codes, c.k_scale, c.v_codes, c.v_scale), before):
+            assert torch.equal(t[others], was[others])
