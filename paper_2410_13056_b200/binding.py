@@ -498,6 +498,17 @@ def _code_rows(t):
     return t.stride(0) if n > 1 else (d + 15) // 16 * 16
 
 
+def _code_room(t):
+    """_code_rows of a code matrix that is written, whose rows are filled up with zeros to a multiple of 16: there has to be
+    room for that, in every row."""
+    n, d = t.shape
+    full = (d + 15) // 16 * 16
+    ld = t.stride(0) if n > 1 or t.stride(0) % 16 == 0 else d
+    if n and (ld < full or t.untyped_storage().nbytes() - t.storage_offset() < (n - 1) * ld + full):
+        raise ValueError("codes needs rows with room for %d bytes, got shape %s, strides %s" % (full, tuple(t.shape), t.stride()))
+    return ld
+
+
 def cmpq_linear_i8_ws_bytes(n, d_in, d_out):
     return int(lib().cmpq_linear_i8_ws_bytes(n, d_in, d_out))
 
@@ -505,7 +516,7 @@ def cmpq_linear_i8_ws_bytes(n, d_in, d_out):
 def cmpq_quantize_tokens(X, codes, scale, nonfinite=None):
     """codes (int8 [n][d], rows on 16 bytes) and scale (fp32 [n]) of every row of X (fp16/bf16 [n][d])."""
     n, d = X.shape
-    _check(lib().cmpq_quantize_tokens(_at(X), _code(X), n, d, _rows(X, d, "X"), _at(codes), _code_rows(codes),
+    _check(lib().cmpq_quantize_tokens(_at(X), _code(X), n, d, _rows(X, d, "X"), _at(codes), _code_room(codes),
                                       _at(scale), _at(nonfinite), _on(X)), "cmpq_quantize_tokens")
 
 

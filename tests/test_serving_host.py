@@ -128,3 +128,16 @@ def test_extension_is_built_and_refuses_what_is_not_on_the_gpu(L, monkeypatch):
     monkeypatch.setattr(B, "_LIB_PATH", "/nonexistent/libcmpq.so")
     with pytest.raises(RuntimeError, match="missing"):
         serving.Int8Linear(codes, scale)
+
+
+def test_codes_need_room_for_their_padding():
+    """Rows of codes are filled up to 16 bytes when they are written: a row without that room is refused, a single one too."""
+    import torch
+
+    zeros = lambda *shape: torch.zeros(*shape, dtype=torch.int8)
+    for good, ld in ((zeros(1, 16)[:, :5], 16), (zeros(1, 32), 32), (zeros(4, 48)[:, :33], 48), (zeros(6, 16)[5:, :1], 16), (zeros(3, 16), 16),
+                     (zeros(64)[16:].view(3, 16)[:, :9], 16), (zeros(0, 5), 5)):
+        assert B._code_room(good) == ld, good.shape
+    for bad in (zeros(1, 5), zeros(8, 5)[3:4], zeros(2, 20), zeros(64)[59:].view(1, 5), zeros(37).as_strided((2, 5), (32, 1))):
+        with pytest.raises(ValueError, match="room"):
+            B._code_room(bad)
