@@ -435,8 +435,8 @@ cmpq_status cmpq_quantize_tokens(const void* X, cmpq_dtype dt, int64_t n, int64_
  * 16-byte aligned, leading dimensions multiples of 16 (what lies between d_in and the leading dimension does
  * not matter); bias [d_out] of `dt` or NULL; y [n][ldy >= d_out] of `dt`.  d_out <= CMPQ_MAX_D_IN.
  * cmpq_linear_i8: both steps in one call, X [n][ldx] of `dt` as in cmpq_quantize_tokens.
- * ws: cmpq_linear_i8_ws_bytes(n, d_in, d_out) for either call (0 for arguments out of range; n may be 0, then
- * nothing is done).  Products run on tensor maps made from the arguments inside the call.  A kernel that gave up waiting
+ * ws: cmpq_linear_i8_ws_bytes(n, d_in, d_out) for either call (0 for arguments out of range, n above
+ * 2^31 - 257 among them; n may be 0, then nothing is done).  Products run on tensor maps made from the arguments inside the call.  A kernel that gave up waiting
  * for its own copies (about a second; never seen) ORs bit 3 into *nonfinite.  cmpq_matmul_i8, which has no such word, and
  * cmpq_linear_i8 with NULL for it keep the bit in the int32 256 bytes before the end of the work space's asked size: 0 when
  * the product has ended well.  cmpq_check_cache takes either word. */

@@ -406,7 +406,7 @@ size_t linear_i8_codes_bytes(int64_t n, int64_t d_in) { return round_up((size_t)
 using namespace cmpq;
 
 static bool linear_sizes_ok(int64_t n, int64_t d_in, int64_t d_out) {
-    return n >= 0 && n <= INT32_MAX && d_in >= 1 && d_in <= CMPQ_MAX_D_IN_I8 && d_out >= 1 && d_out <= CMPQ_MAX_D_IN;
+    return n >= 0 && n <= INT32_MAX - 256 /* tiles of tokens end past the last one */ && d_in >= 1 && d_in <= CMPQ_MAX_D_IN_I8 && d_out >= 1 && d_out <= CMPQ_MAX_D_IN;
 }
 
 extern "C" size_t cmpq_linear_i8_ws_bytes(int64_t n, int64_t d_in, int64_t d_out) {

@@ -141,3 +141,11 @@ def test_codes_need_room_for_their_padding():
     for bad in (zeros(1, 5), zeros(8, 5)[3:4], zeros(2, 20), zeros(64)[59:].view(1, 5), zeros(37).as_strided((2, 5), (32, 1))):
         with pytest.raises(ValueError, match="room"):
             B._code_room(bad)
+
+
+def test_token_counts_that_tiles_would_carry_past_32_bits(L, p):
+    for n in ((1 << 31) - 1, (1 << 31) - 256):
+        assert B.cmpq_linear_i8_ws_bytes(n, 16, 1) == 0
+        assert L.cmpq_linear_i8(p, 0, n, 16, 16, p, 16, p, None, 1, p, 1, None, p, 1 << 60, None) == INVALID
+        assert L.cmpq_matmul_i8(p, 16, p, p, 16, p, None, 0, n, 16, 1, p, 1, p, 1 << 60, None) == INVALID
+    assert B.cmpq_linear_i8_ws_bytes((1 << 31) - 257, 16, 1) > 0
