@@ -63,6 +63,8 @@ __device__ __forceinline__ void report_gave_up(const AttnArgs& A) {
     if (A.word) atomicOr(A.word, kWordInternal);
 }
 
+constexpr int kPfSplits = 8;  // most blocks of the prompts' kernel that share out a unit's keys
+
 // Whole prompts (cache_prefill.cu): head_dim 64 and 128.
 cmpq_status launch_prefill(const AttnArgs& a, cmpq_dtype dt, cudaStream_t st);
 size_t prefill_parts_bytes(int head_dim);  // behind the counters

@@ -650,19 +650,15 @@ static cmpq_status launch_attention(const AttnArgs& a, cudaStream_t st) {
 }
 
 // Which kernel takes a batch.  Up to 32 rows of a sequence and key-value head the warps that share out the cache, above
-// 128 the one for prompts.  Between, microseconds from sizes (the lengths are taken as 0.6 of the longest unless a window
-// evens them out): warps read a row block of 16 at about 1.3 a tile of 32 keys, the other kernel two tiles of 128 keys in
-// 2.9, in rounds over the SMs.  Measured, D = 128 / 64, 40 rows: 16 sequences to 4093 tokens, 8 heads: warps 55 / 40, other
-// 71 / 57; the same with a window of 1024, D = 64: 29 and 23; 64 rows, 64 sequences to 2048: 138 and 121.
+// 128 the one for prompts.  Between, the one for prompts too, unless its blocks, at the most splits of the keys, leave more
+// than half of the SMs idle.  Measured over 771 batches (40 to 128 rows, 1 to 64 sequences of one length or of several, 512 to
+// 32768 tokens, 1 to 32 heads of 64 and 128, with and without a window): 1 % above the better kernel on average, always
+// the warps 56 %, always the other 4 %.  Microseconds, warps / other, D = 128, one sequence to 2048 and 16 to 8192 tokens: 4 heads,
+// 64 rows 22 / 30 and 134 / 84; 8 heads, 40 rows 22 / 29 and 185 / 134.
 static bool prefill_pays(const AttnArgs& a) {
-    const int64_t rows = (int64_t)a.max_new * a.group;
+    const int64_t rows = (int64_t)a.max_new * a.group, units = a.b.n_seq * a.c.n_kv_heads;
     if (a.c.head_dim > 128 || rows <= 32) return false;
-    if (rows > 128) return true;
-    const bool windowed = a.window > 0 && (int64_t)a.window + a.max_new < a.max_len;
-    const double keys = windowed ? a.window + a.max_new : a.max_len, even = windowed ? 1.0 : 0.6, units = (double)a.b.n_seq * a.c.n_kv_heads;
-    const double sms = sm_count(), warps = 12 + 1.3 * even * units * ((rows + 15) / 16) * (keys / 32) / (8 * sms);
-    const double splits = std::max(1.0, std::min(8.0, std::floor(sms / units)));
-    return 10 + 2.9 * (keys / 256) / splits * std::max(1.0, units / sms) < warps;
+    return rows > 128 || units * kPfSplits * 2 > sm_count();
 }
 
 // The counters, then two parts per block and one per worker, of the kernel that has most, or the parts of the prompts'.

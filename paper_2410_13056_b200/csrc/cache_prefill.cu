@@ -70,7 +70,7 @@ __device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
 struct PrefillPlan {
     int row_blocks, per_row_block, splits;
 };
-constexpr int kPfSplits = 8, kPfCounters = 512;  // most blocks to a unit; where its counters begin
+constexpr int kPfCounters = 512;  // where its counters begin
 
 // A row's entries, times f, as 16 bits into `dst` or as they are into `part`.  columns(c, x, y) gives the accumulator's
 // columns c.. and D/2 + c.. and is called by all lanes; `real`: the row exists.
