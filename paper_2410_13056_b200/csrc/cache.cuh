@@ -10,16 +10,7 @@ namespace cmpq {
 constexpr int kWordNonfinite = 1, kWordTable = 4, kWordInternal = 8;  // bits of the device word
 constexpr float kScaleLo = 0x1p-60f, kScaleHi = 0x1p60f;
 
-template <int DT>
-__device__ __forceinline__ uint16_t round16(float x) {
-    if (DT == CMPQ_BF16) {
-        return __bfloat16_as_ushort(__float2bfloat16_rn(x));
-    } else {
-        return __half_as_ushort(__float2half_rn(x));
-    }
-}
-
-// Two floats rounded into one word, `lo` in the low half.
+// Two floats rounded to 16 bits into one word, `lo` in the low half.
 template <int DT>
 __device__ __forceinline__ uint32_t round16x2(float lo, float hi) {
     if (DT == CMPQ_BF16) {

@@ -580,3 +580,34 @@ def test_a_table_that_is_part_of_a_wider_one_ends_with_its_columns(row):
         others = [p for p in range(18) if p not in wide[:, 3:5].flatten().tolist()]
         for t, was in zip((c.k_codes, c.k_scale, c.v_codes, c.v_scale), before):
             assert torch.equal(t[others], was[others])
+
+
+def test_binding_of_the_c_calls():
+    """The ctypes wrappers make the calls that the extension makes: same bytes, same errors."""
+    H, d, P, heads, lens = 2, 64, 16, 4, [40, 17]
+    k, v, q = tokens(20, H, d, torch.float16, 1).cuda(), tokens(20, H, d, torch.float16, 2).cuda(), tokens(20, heads, d, torch.float16, 3).cuda()
+    cos, sin = (torch.from_numpy(x).cuda() for x in rope(64, d))
+    off, length, table = i32([0, 3, 20]), i32(lens), i32([[0, 1, 2], [4, 5, 6]])
+    one, two = (up(make(lens, H, d, P, 8, garbage=False)[0]) for _ in range(2))
+    assert one.n_pages >= 7
+    want_q = one.append(k, v, off, length, table, q=q, cos=cos, sin=sin)
+    want_k, want_v = one.read(off, length, table, 20, torch.float16)
+    want, want_lse = one.attend(want_q, off, length, table, 17, 48, return_lse=True)
+    c = B.Cache(*(t.data_ptr() for t in (two.k_codes, two.k_scale, two.v_codes, two.v_scale)), two.n_pages, H, d, P)
+    b = B.Batch(off.data_ptr(), length.data_ptr(), table.data_ptr(), 3, 2, 20, 3)
+    got_q, got_k, got_v, out, word = torch.empty_like(q), torch.empty_like(k), torch.empty_like(v), torch.empty_like(q), i32([0])
+    lse = torch.empty(20, heads, device="cuda")
+    B.cmpq_cache_append(c, b, k, v, cos, sin, False, q, got_q, word)
+    B.cmpq_cache_read(c, b, got_k, got_v, word)
+    ws = torch.zeros(B.cmpq_cache_attention_ws_bytes(2, 20, 17, 48, heads, H, d), dtype=torch.uint8, device="cuda")
+    B.cmpq_cache_attention(c, b, got_q, 17, 48, 1 / math.sqrt(d), True, 0, out, lse, ws, word)
+    B.cmpq_check_cache(word)
+    for x, y in ((got_q, want_q), (got_k, want_k), (got_v, want_v), (out, want), (lse, want_lse), (two.k_codes, one.k_codes), (two.v_scale, one.v_scale)):
+        assert torch.equal(x, y)
+    length[1] = 49                                         # past the table
+    B.cmpq_cache_read(c, b, got_k, got_v, word)
+    with pytest.raises(B.CmpqError) as e:
+        B.cmpq_check_cache(word)
+    assert e.value.status == 1
+    with pytest.raises(ValueError):
+        B.cmpq_cache_read(c, b, got_k, got_v[:, :, :32], word)
