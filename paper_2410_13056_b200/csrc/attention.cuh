@@ -47,6 +47,13 @@ __device__ __forceinline__ RowScale row_scale(float largest) {
     return {__uint_as_float((uint32_t)(127 + 13 - e) << 23), __uint_as_float((uint32_t)(127 - 13 + e) << 23)};
 }
 
+// log2 of a page's value scale; a page of zeros has scale 0 and counts as 2^-80.
+__device__ __forceinline__ float scale_log2(float scale) {
+    float y;
+    asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(fmaxf(scale, 0x1p-80f)));
+    return y;
+}
+
 // Four int8 codes (already offset by 128) as two pairs of fp16: 0x6400 | u is 1024 + u, and 1024 + 128 comes off.
 __device__ __forceinline__ uint32_t half_pair(uint32_t u, uint32_t pick) {
     const uint32_t h = __byte_perm(u, 0x64646464u, pick);

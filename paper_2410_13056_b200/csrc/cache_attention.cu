@@ -172,11 +172,6 @@ __device__ __forceinline__ void join_parts(const AttnArgs& A, const Piece& u, in
     }
 }
 
-// The exponent e of a page's value scale in [2^(e-1), 2^e); what is below 2^-60, a page of zeros, counts as that.
-__device__ __forceinline__ float scale_exponent(float scale) {
-    return __uint_as_float(0x4b000000u | max(__float_as_uint(scale), __float_as_uint(kScaleLo)) >> 23) - 8388734.0f;  // 2^23 + 126
-}
-
 // A lane's place in the m16n8k16 fragments: r = lane / 4, c = lane % 4.
 //   scores   S^T[token][row] = K Q^T: a lane reads 16 bytes of keys of tokens r and r + 8 at a time, which are the A
 //            entries of four instructions when the sum runs over the entries in the order 16 (2c + j) + 4 w + {0..3}
@@ -444,11 +439,12 @@ attention_rows_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_con
                         }
                     }
             }
-            // m2 is the row's largest score plus its page's value exponent so far: what goes to fp16 is weight times value
-            // scale, and the largest of those that the row sees ends in [2^14, 2^15]
+            // m2 is the row's largest score plus log2 of its page's value scale so far: what goes to fp16 is weight times value
+            // scale, and the largest of those that the row sees is 2^15, which fp16 has: a row with one key that counts loses
+            // nothing
             float above[MT];
 #pragma unroll
-            for (int mt = 0; mt < MT; ++mt) above[mt] = scale_exponent(sc[mt].y);
+            for (int mt = 0; mt < MT; ++mt) above[mt] = scale_log2(sc[mt].y);
             uint32_t pf[NT][MT][2];
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {

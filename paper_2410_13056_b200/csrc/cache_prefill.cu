@@ -379,7 +379,7 @@ attention_prefill_kernel(const __grid_constant__ AttnArgs A, const __grid_consta
         bool ok = true;
         for (int t = t_first; t < tiles; t += t_step) {
             sc = sc_next;
-            const float bias = log2f(fmaxf(sc.y, 0x1p-80f)), inv_vs = ex2(-bias);  // a page of zeros has scale 0
+            const float bias = scale_log2(sc.y), inv_vs = ex2(-bias);
             sc_next = scales(id_next);
             id_next = look_up(t + 2 * t_step);
             if (!(ok = tc5::mbar_wait_warp(s_full + w, (two ? t : t >> 1) & 1, &failed))) break;

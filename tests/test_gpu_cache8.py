@@ -611,3 +611,24 @@ def test_binding_of_the_c_calls():
     assert e.value.status == 1
     with pytest.raises(ValueError):
         B.cmpq_cache_read(c, b, got_k, got_v[:, :, :32], word)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("new,d,P", [(1, 64, 16), (1, 128, 64), (3, 256, 32), (9, 128, 16), (40, 64, 64), (200, 128, 32), (300, 64, 16)])
+def test_attend_rows_that_see_one_key_return_its_value(new, d, P, dtype):
+    """With a window of one a row's output is its own token's value: the largest weight times scale is a power of two in
+    fp16, so nothing but the fp32 division (2^-20 of the value) and the last rounding is between them."""
+    H, heads, L = 2, 4, 310
+    cache, table = make([L], H, d, P, 7, garbage=False)
+    q = tokens(new, heads, d, dtype, 3).cuda()
+    c = up(cache)
+    out, lse = c.attend(q, i32([0, new]), i32([L]), i32(table), max_new=new, max_len=L, window=1, return_lse=True)
+    c.check()
+    pages = table[0][: -(-L // P)].astype(int)
+    v, k = ((cache[x + "_codes"][pages].astype(np.float64) * cache[x + "_scale"][pages].astype(np.float64)[..., None, None])
+            .transpose(0, 2, 1, 3).reshape(-1, H, d)[L - new: L].repeat(heads // H, 1) for x in "vk")
+    got = out.double().cpu().numpy()
+    assert np.all(np.abs(got - v) <= 2.0 ** -20 * np.abs(v) + ref.half_ulp(np.abs(v) * (1 + 2.0 ** -20), dtype))
+    x = q.double().cpu().numpy()
+    s, ds = (x * k).sum(2) / math.sqrt(d), (d + 8) * 2.0 ** -23 * (np.abs(x) * np.abs(k)).sum(2) / math.sqrt(d)
+    assert np.all(np.abs(lse.double().cpu().numpy() - s) <= 2 * ds + 2.0 ** -20 * (1 + np.abs(s)))
