@@ -187,7 +187,7 @@ cache_queries_any_kernel(const __grid_constant__ AppendArgs A) {
 
 // The queries of prompts where units are closed under the rotation: a block to a token, two units of a thread at a time.
 // The first entries, whose place needs no position, are asked for before the sequence is looked up.
-// Measured: 13.5 thousand tokens of 64 heads of 128 (440 MB) 82 us, 5.4 TB/s; several tokens to a block one after the other
+// Measured: 13.5 thousand tokens of 64 heads of 128 (440 MB) 84 us, 5.3 TB/s; several tokens to a block one after the other
 // 92 to 185 us (the look-ups of each are waited for).
 template <int DT>
 __global__ void __launch_bounds__(256, 4)
@@ -293,7 +293,7 @@ __device__ __forceinline__ void scale_again(int8_t* codes, int count, float by) 
 // one launch.  A block reads its new tokens, keeps the first NIT groups of a thread rotated in fp32 registers, agrees on
 // the largest magnitude and writes codes; later rows of a thread are read again for that.  Each row of a head is D/8
 // threads of eight entries, so global accesses are 16 bytes (inputs) and 8 bytes (codes), whole lines per row.
-// Measured: one token of 64 sequences, 64/8 heads, 6 us, nearly all of it five dependent loads and the launch.
+// Measured: one token of 64 sequences, 64/8 heads, 6.2 us a call, 3.6 in a graph, nearly all of it five dependent loads.
 template <int DT, int NIT, int THREADS>
 __global__ void __launch_bounds__(THREADS)
 cache_append_kernel(const __grid_constant__ AppendArgs A) {
@@ -457,6 +457,8 @@ struct ReadArgs {
 
 // A block takes TOKENS tokens: the first threads find a token's page each, then all read and widen, a thread 16 codes of
 // AT_ONCE tokens at a time (keys of all heads, then values), whose loads are under way together.
+// Measured: 10 thousand tokens of 8 heads of 128 (63 MB) 22.5 us, 2.8 TB/s, the issue slots at 34 %: two batches of loads
+// behind the look-up are all that a block does, and 640 blocks are little more than one round.
 template <int DT, int TOKENS, int AT_ONCE>
 __global__ void __launch_bounds__(256)
 cache_read_kernel(const __grid_constant__ ReadArgs A) {

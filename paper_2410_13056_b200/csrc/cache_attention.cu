@@ -20,9 +20,10 @@ namespace cmpq {
 // is finished there.  The parts of one that is cut are joined by the block that holds them and, where several do, by the
 // last block to arrive, always in the order of the workers: the same bytes every time.
 //
-// Measured, D = 128: 64 sequences of up to 8191 tokens, 64/8 heads (608 MB): 127 us, 4.8 TB/s, 0.73 of the copy rate; two
-// of up to 131072 (515 MB): 105 us; one of 2049, 32 heads: 15 us.  What is left: the SMs get unequal shares of the memory
-// (the blocks' loops of the second case end between 62 and 90 us), and some 10 us of look-ups, first loads and joins.
+// Measured, D = 128: 64 sequences of up to 8191 tokens, 64/8 heads (608 MB): 126 to 131 us, 4.7 TB/s, 0.72 of the copy rate;
+// two of up to 131072 (515 MB): 107 us; one of 2049, 32 heads: 16.2 us in a stream of calls.  What is left: the SMs get
+// unequal shares of the memory (the blocks' loops of the second case end between 62 and 90 us), and some 10 us of look-ups,
+// first loads and joins.
 // Dealing the last 10 to 30 % in short runs to whichever block is free costs more in look-ups and joins than it evens out
 // (136 to 139 and 138 to 157 us); asking for later tiles in L2 makes it slower (129 / 154 / 180 us for 1 / 2 / 4 tiles
 // ahead).

@@ -21,11 +21,12 @@ namespace cmpq {
 // With 128 rows or fewer the two accumulators take every other tile of keys of the one row tile and are joined at the end;
 // fewer units than SMs are split over the keys, the last block to arrive joining the parts in their order.
 //
-// Measured: 2 x up to 2048 queries over up to 6145 tokens, 32 heads, D = 128: 287 us, 775 TFLOP/s of visible pairs, 0.47 of
-// the library's bf16 product; the tensor pipe is at 41 %.  Per 256 rows x 128 keys the weights' warps work 3240 cycles and
-// wait 810 for scores; the floor of the exponential unit is 2048, of the products about the same.  Steps of 32 keys: 307 us,
-// of 64: 292, of 128 (registers spill): 309.  Scores of 64 keys in two buffers, so that the weights never wait: 301 (twice the
-// barriers, and M = 128, N = 64 products read shared memory 1.5 times as long).
+// Measured: 2 x up to 2048 queries over up to 6145 tokens, 32 heads, D = 128: 292 us, 762 TFLOP/s of visible pairs, 0.47 of
+// the library's bf16 product; the tensor pipe is at 43 %.  Per 256 rows x 128 keys the weights' warps work 3000 cycles and
+// wait 1050 for scores, the warps that widen wait 1220, the products' thread 1490 of 4100; the floor of the exponential unit
+// is 2048, of the products about the same.  Tried when the whole took 292 us: steps of 32 keys 307, of 128 (registers spill)
+// 309; scores of 64 keys in two buffers, so that the weights never wait, 301 (twice the barriers, and M = 128, N = 64 products
+// read shared memory 1.5 times as long).
 constexpr int kPfKeys = 128, kPfThreads = 16 * 32;
 constexpr float kPfSlack = 8.0f;
 // Registers a thread: launched with 128, four warps of each of the four groups; 2 x 168 + 112 + 64 = 4 x 128.

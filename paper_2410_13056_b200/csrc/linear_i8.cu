@@ -45,7 +45,8 @@ __device__ __forceinline__ uint2 group_codes(uint4 g, float inv) {
 // where a NaN is larger than infinity and infinity larger than every number: the maximum also tells whether the row is
 // finite.  A thread keeps KEEP groups of eight in registers, chosen by the row's length so that more blocks share an SM
 // where rows are short; rows of up to 16384 entries are read once, the rest of a longer one is read again.
-// Measured: 4096 x 8192 18 us (100 MB, 5.6 TB/s; 27 us with conversions and 32-bit comparisons), 1000 x 11008 8.9 us.
+// Measured in a stream of calls: 4096 x 8192 20 us (100 MB, 5.0 TB/s), 1000 x 11008 10.3 us; the first took 1.5 times as long
+// with conversions and 32-bit comparisons.
 template <int DT, int KEEP>
 __global__ void __launch_bounds__(kQtThreads)
 quantize_tokens_kernel(const uint16_t* __restrict__ X, int64_t d, int64_t ldx, int wide, int8_t* __restrict__ codes,
@@ -148,9 +149,9 @@ __device__ __forceinline__ void store_rows(uint32_t tmem, int c0, int c1, const 
 // only reaches accumulator rows that are not stored, and 16 KB behind the last stage are kept for it.  With that one
 // token's weights have some 30 stages on their way.
 //
-// Measured with the quantization, weights from memory: one token 4096 -> 4096 9.6 us, 8192 -> 28672 40 us (5.8 TB/s, 0.88 of the
-// copy rate); 37 tokens 4096 -> 11008 13 us (3.5 TB/s: launch, first loads and the last stage's way out are half of it).
-// Splitting the sum over a cluster instead, weights as rows: 14.6, 52 and 31.5 us.
+// Measured with the quantization in a stream of calls, weights from memory: one token 4096 -> 4096 10.3 us, 8192 -> 28672 42 us
+// (5.6 TB/s, 0.86 of the copy rate); 37 tokens 4096 -> 11008 14.3 us (3.2 TB/s: launch, first loads and the last stage's way
+// out are half of it).  Splitting the sum over a cluster instead, weights as rows, took 1.5, 1.3 and 2.4 times as long.
 template <int DT>
 __global__ void __launch_bounds__(kMmThreads)
 matmul_i8_tile_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__ CUtensorMap xmap,
@@ -249,8 +250,9 @@ constexpr size_t kPairSmem = kPairStages * kPairStageBytes + 1024;
 // Two accumulators of 256 columns alternate, the epilogue of one tile runs under the products of the next.  Token tiles
 // go fastest: the pairs at work share a few weight tiles and the token codes stay in L2.
 //
-// Measured: 4096 x 8192 x 28672 553 us without, 597 with the quantization (3.5 and 3.2 POP/s, 1.07 and 0.98 of twice the
-// library's bf16 rate); 2048 x 4096 x 11008 65 us, the tensor pipe at 80 % (172 pair tiles in 3 rounds of 74).
+// Measured: 4096 x 8192 x 28672 with the quantization 610 us in a few calls after a rest (3.15 POP/s, 0.96 of twice the library's
+// bf16 rate) and 680 to 694 in a long stream, where the power limit holds the clock; 2048 x 4096 x 11008 67 us, 72 with the
+// quantization, the tensor pipe at 81 % (172 pair tiles in 3 rounds of 74).
 template <int DT>
 __global__ void __launch_bounds__(kMmThreads, 1)
 matmul_i8_pair_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__ CUtensorMap xmap,

@@ -240,7 +240,7 @@ def _i32(x):
 
 
 def run_cache8(a):
-    """append8: `new` tokens join `tokens - new` cached ones in every stream; attend8: they attend to all."""
+    """append8: `new` tokens join `tokens - new` cached ones in every stream, and are read back; attend8: they attend to all."""
     import random
 
     dt = torch.bfloat16 if a.dtype == "bf16" else torch.float16
@@ -257,6 +257,8 @@ def run_cache8(a):
     if a.case == "append8":
         ms = _timed(lambda: cache.append(k, v, off, lens_t, table, q=q, cos=cos, sin=sin), a.launches)
         moved = n * d * (4 * a.heads + 6 * a.kv_heads)
+        back = _timed(lambda: cache.read(off, lens_t, table, n, dt), a.launches)
+        print("read back: %.4f ms (%.0f GB/s)" % (back, n * d * 6 * a.kv_heads / back / 1e6))
     else:
         ms = _timed(lambda: cache.attend(q, off, lens_t, table, max_new=a.new, max_len=a.tokens), a.launches)
         moved = 2 * sum(lens) * a.kv_heads * d + 4 * n * a.heads * d
@@ -313,7 +315,7 @@ def run_serve(a):
         lens += 1
         token = layer(token, one, lens, table, max_new=1, max_len=a.tokens + a.launches)
     e1.record()
-    cache.check()
+    layer.check()
     print("   generation: %.4f ms a token and block for %d streams" % (e0.elapsed_time(e1) / a.launches, a.streams))
 
 
