@@ -435,11 +435,11 @@ cmpq_status cmpq_quantize_tokens(const void* X, cmpq_dtype dt, int64_t n, int64_
  * 16-byte aligned, leading dimensions multiples of 16 (what lies between d_in and the leading dimension does
  * not matter); bias [d_out] of `dt` or NULL; y [n][ldy >= d_out] of `dt`.  d_out <= CMPQ_MAX_D_IN.
  * cmpq_linear_i8: both steps in one call, X [n][ldx] of `dt` as in cmpq_quantize_tokens.
- * ws: cmpq_linear_i8_ws_bytes(n, d_in, d_out) for either call (0 for arguments out of range, n above
- * 2^31 - 257 among them; n may be 0, then nothing is done).  Products run on tensor maps made from the arguments inside the call.  A kernel that gave up waiting
- * for its own copies (about a second; never seen) ORs bit 3 into *nonfinite.  cmpq_matmul_i8, which has no such word, and
- * cmpq_linear_i8 with NULL for it keep the bit in the int32 256 bytes before the end of the work space's asked size: 0 when
- * the product has ended well.  cmpq_check_cache takes either word. */
+ * ws: cmpq_linear_i8_ws_bytes(n, d_in, d_out) for either call (0 for arguments out of range, n above 2^31 - 257 among
+ * them; n may be 0, then nothing is done).  Products run on tensor maps made from the arguments inside the call.
+ * A kernel that gave up waiting for its own copies (about a second; never seen) ORs bit 3 into *nonfinite.
+ * cmpq_matmul_i8, which has no such word, and cmpq_linear_i8 with NULL for it keep the bit in the int32 256 bytes before
+ * the end of the work space's asked size: 0 when the product has ended well.  cmpq_check_cache takes either word. */
 #define CMPQ_MAX_D_IN_I8 131072
 size_t cmpq_linear_i8_ws_bytes(int64_t n, int64_t d_in, int64_t d_out);
 cmpq_status cmpq_matmul_i8(const int8_t* xc, int64_t ldxc, const float* xs, const int8_t* wc, int64_t ldwc,
@@ -521,7 +521,7 @@ cmpq_status cmpq_cache_read(const cmpq_cache* cache, const cmpq_batch* batch, cm
  * [n_tok][n_heads]) receives the natural logarithm of the softmax's sum, -infinity for such a row.
  * q [n_tok][ldq], out [n_tok][ldo] of `dt`, heads next to each other; queries finite.
  * max_new >= every count of new tokens and max_len >= every length are the caller's bounds (they choose the
- * kernel and size the work space).  Probabilities and sums in fp32, products on the tensor cores in fp16 with
+ * kernel and size the work space; a max_new above n_tok counts as n_tok).  Probabilities and sums in fp32, products on the tensor cores in fp16 with
  * fp32 accumulation: codes are exact there, a query row is scaled by a power of two into fp16's range (any finite row), and
  * probabilities times value scales are rounded to fp16, where the largest of a row lies in [2^7, 2^15]: they keep 11 bits
  * down to 2^-21 of it and vanish below 2^-32.  The softmax's sum is not rounded; it misses keys whose probability times
