@@ -449,6 +449,50 @@ cmpq_status cmpq_linear_i8(const void* X, cmpq_dtype dt, int64_t n, int64_t d_in
                            int64_t ldwc, const float* w_scale, const void* bias, int64_t d_out, void* y, int64_t ldy,
                            int32_t* nonfinite, void* ws, size_t ws_bytes, void* stream);
 
+/* ---- serving in 8 bits: what stands around the products of a layer ------------------------------
+ * cmpq_norm_quantize_tokens: cmpq_quantize_tokens with a root-mean-square norm in front.  norm: [d] of `dt` (NULL: none,
+ * and eps is not looked at), eps a normal positive number.  For every row, each step one fp32 operation:
+ *   v_j = fl(x_j * norm_j)     s = fl(max_j |v_j| * fl(1/127))     codes[t][j] = clamp(rint(fl(v_j * fl(1/s))), -127, 127)
+ *   scale[t] = fl(s * r)       r = 1 / sqrt(mean_j x_j^2 + eps)
+ * (a row's codes do not depend on its norm).  r is within (d / 2048 + 24) * 2^-24 of its value.  scale and codes are 0 where
+ * max |v_j| is below 2^-120.  A product v_j that passes fp32 is reported like an infinity among the inputs.
+ *
+ * cmpq_linear_i8_fused: y[t][o] = fl16(fl(act(z[t][o])) + residual[t][o]), z = the linear layer of X behind that norm before
+ * its rounding to 16 bits (see cmpq_matmul_i8).  residual: [n][ldr >= d_out] of `dt` or NULL; it may be y with ldr = ldy,
+ * or X; y may be X.  act: z, max(z, 0), z / (1 + e^-z), z Phi(z) or z / (1 + e^-w), w = sqrt(8/pi) (z + 0.044715 z^3); off by at most
+ * (5 + |z|), (5 + z^2) or (5 + 3 |w|) times 2^-22 of its value, or by 2^-100.
+ * Everything else as cmpq_linear_i8, which is this call without norm, act and residual; the same work space and mark. */
+typedef enum { CMPQ_ACT_NONE = 0, CMPQ_ACT_RELU = 1, CMPQ_ACT_SILU = 2, CMPQ_ACT_GELU = 3, CMPQ_ACT_GELU_TANH = 4 } cmpq_act;
+typedef struct {
+    const int8_t* codes; /* [d_out][ld], 16-byte aligned, ld a multiple of 16 */
+    int64_t ld;
+    const float* scale; /* [d_out] */
+    const void* bias;   /* [d_out] of the call's dtype, or NULL */
+} cmpq_weight_i8;
+cmpq_status cmpq_norm_quantize_tokens(const void* X, cmpq_dtype dt, int64_t n, int64_t d, int64_t ldx, const void* norm,
+                                      float eps, int8_t* codes, int64_t ldc, float* scale, int32_t* nonfinite, void* stream);
+cmpq_status cmpq_linear_i8_fused(const void* X, cmpq_dtype dt, int64_t n, int64_t d_in, int64_t ldx, const void* norm,
+                                 float eps, const cmpq_weight_i8* weight, int64_t d_out, cmpq_act act, const void* residual,
+                                 int64_t ldr, void* y, int64_t ldy, int32_t* nonfinite, void* ws, size_t ws_bytes, void* stream);
+
+/* cmpq_gated_i8: a gated feed-forward block.  With q(.) the quantization of cmpq_norm_quantize_tokens (norm and eps for X, none
+ * for h) and z_gate, z_up, z_down the linear layers' values before their rounding to 16 bits:
+ *   h[t][f] = fl16(fl(act(z_gate[t][f]) * z_up[t][f]))  from q(X),  f < d_ff      y[t][o] = fl16(z_down[t][o] + residual[t][o])  from q(h)
+ * Both projections, the activation and the product are one kernel; X is quantized once for both.  d_in and d_ff up to
+ * CMPQ_MAX_D_IN_I8, d_out up to CMPQ_MAX_D_IN.  residual as in cmpq_linear_i8_fused.
+ * `word` (optional device int32, zeroed by the caller): bit 0 when a token or an h is a NaN or an infinity (an h beyond
+ * 65504 in fp16 is one), bit 3 when a kernel gave up waiting (about a second; never seen).  cmpq_check_cache takes it.
+ * ws: cmpq_gated_i8_ws_bytes(n, d_in, d_ff, d_out), 0 for arguments out of range.  Its first CMPQ_GATED_ZEROED bytes have to be
+ * 0 when the call's kernels start, and are 0 again when they have ended: zero them once, after allocating the buffer and
+ * after bit 3, which every call on the buffer reports from then on.  Calls that may run at the same time, graphs' replays
+ * among them, need buffers of their own. */
+#define CMPQ_GATED_ZEROED 4096
+size_t cmpq_gated_i8_ws_bytes(int64_t n, int64_t d_in, int64_t d_ff, int64_t d_out);
+cmpq_status cmpq_gated_i8(const void* X, cmpq_dtype dt, int64_t n, int64_t d_in, int64_t ldx, const void* norm, float eps,
+                          const cmpq_weight_i8* gate, const cmpq_weight_i8* up, const cmpq_weight_i8* down, int64_t d_ff,
+                          int64_t d_out, cmpq_act act, const void* residual, int64_t ldr, void* y, int64_t ldy, int32_t* word,
+                          void* ws, size_t ws_bytes, void* stream);
+
 /* ---- serving in 8 bits: paged cache of keys and values -----------------------------------------
  * A cache is n_pages pages of page_tokens tokens.  Codes are [n_pages][n_kv_heads][page_tokens][head_dim]
  * int8 in [-127, 127], 16-byte aligned; scales [n_pages][n_kv_heads] fp32: one per page and head, for keys

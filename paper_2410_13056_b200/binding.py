@@ -32,6 +32,7 @@ EXPORTS = (
     "cmpq_matvec_f16lut", "cmpq_lut_bytes", "cmpq_store_lut", "cmpq_load_lut", "cmpq_table_bits_per_weight",
     "cmpq_quantize_tokens", "cmpq_matmul_i8", "cmpq_linear_i8", "cmpq_linear_i8_ws_bytes", "cmpq_check_cache",
     "cmpq_cache_append", "cmpq_cache_read", "cmpq_cache_attention", "cmpq_cache_attention_ws_bytes",
+    "cmpq_norm_quantize_tokens", "cmpq_linear_i8_fused", "cmpq_gated_i8", "cmpq_gated_i8_ws_bytes",
 )
 
 MAX_D_IN_I8 = 131072
@@ -50,6 +51,13 @@ class Batch(ctypes.Structure):
                 ("ld_table", ctypes.c_int64), ("n_seq", ctypes.c_int64), ("n_tok", ctypes.c_int64),
                 ("table_cols", ctypes.c_int64)]
 
+
+class Weight8(ctypes.Structure):
+    """cmpq_weight_i8"""
+    _fields_ = [("codes", ctypes.c_void_p), ("ld", ctypes.c_int64), ("scale", ctypes.c_void_p), ("bias", ctypes.c_void_p)]
+
+
+ACTS = {None: 0, "none": 0, "relu": 1, "silu": 2, "gelu": 3, "gelu_tanh": 4}
 
 _LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libcmpq.so")
 _lib = None
@@ -149,6 +157,14 @@ def lib():
         L.cmpq_matmul_i8.argtypes = [vp, i64, vp, vp, i64, vp, vp, ci, i64, i64, i64, vp, i64, vp, sz, vp]
         L.cmpq_linear_i8.argtypes = [vp, ci, i64, i64, i64, vp, i64, vp, vp, i64, vp, i64, vp, vp, sz, vp]
         L.cmpq_linear_i8_ws_bytes.argtypes = [i64, i64, i64]
+        w8 = ctypes.POINTER(Weight8)
+        L.cmpq_norm_quantize_tokens.argtypes = [vp, ci, i64, i64, i64, vp, f32, vp, i64, vp, vp, vp]
+        L.cmpq_linear_i8_fused.argtypes = [vp, ci, i64, i64, i64, vp, f32, w8, i64, ci, vp, i64, vp, i64, vp, vp, sz, vp]
+        L.cmpq_gated_i8.argtypes = [vp, ci, i64, i64, i64, vp, f32, w8, w8, w8, i64, i64, ci, vp, i64, vp, i64, vp, vp, sz, vp]
+        L.cmpq_gated_i8_ws_bytes.argtypes = [i64, i64, i64, i64]
+        L.cmpq_gated_i8_ws_bytes.restype = sz
+        for name in ("cmpq_norm_quantize_tokens", "cmpq_linear_i8_fused", "cmpq_gated_i8"):
+            getattr(L, name).restype = ci
         L.cmpq_check_cache.argtypes = [vp, vp]
         L.cmpq_cache_append.argtypes = [cache, batch, vp, i64, vp, i64, ci, vp, vp, i64, i32, i32, vp, i64, i32, vp,
                                         i64, vp, vp]
@@ -538,6 +554,48 @@ def cmpq_linear_i8(X, wc, w_scale, bias, y, ws, nonfinite=None):
                               ws.data_ptr(), ws.numel(), _on(X))
     if st:
         raise CmpqError(st, "cmpq_linear_i8")
+
+
+def weight8(codes, scale, bias=None):
+    """Weight8 structure of a layer's codes (int8 [d_out][d_in], rows on 16 bytes), scales (fp32 [d_out]) and bias."""
+    return Weight8(codes.data_ptr(), _code_rows(codes), scale.data_ptr(), None if bias is None else bias.data_ptr())
+
+
+def cmpq_norm_quantize_tokens(X, norm, eps, codes, scale, nonfinite=None):
+    """cmpq_quantize_tokens behind a root-mean-square norm with weight `norm` ([d] of X's dtype, or None)."""
+    n, d = X.shape
+    if norm is not None and (norm.dtype != X.dtype or tuple(norm.shape) != (d,) or not norm.is_contiguous() or norm.device != X.device):
+        raise ValueError("norm needs %d contiguous entries of X's dtype beside it" % d)
+    _check(lib().cmpq_norm_quantize_tokens(_at(X), _code(X), n, d, _rows(X, d, "X"), _at(norm), eps, _at(codes), _code_room(codes),
+                                           _at(scale), _at(nonfinite), _on(X)), "cmpq_norm_quantize_tokens")
+
+
+def _residual(residual, n, d_out, X):
+    if residual is None:
+        return None, 0
+    if residual.dtype != X.dtype or tuple(residual.shape) != (n, d_out):
+        raise ValueError("residual needs shape [%d][%d] and X's dtype" % (n, d_out))
+    return _at(residual), _rows(residual, d_out, "residual")
+
+
+def cmpq_linear_i8_fused(X, weight, d_out, y, ws, norm=None, eps=1e-6, act=None, residual=None, nonfinite=None):
+    """y = act(the 8-bit linear layer `weight` (a Weight8) of norm(X)) + residual."""
+    n, d_in = X.shape
+    _check(lib().cmpq_linear_i8_fused(_at(X), _code(X), n, d_in, _rows(X, d_in, "X"), _at(norm), eps, weight, d_out, ACTS[act],
+                                      *_residual(residual, n, d_out, X), _at(y), _rows(y, d_out, "y"), _at(nonfinite), _at(ws),
+                                      ws.numel(), _on(X)), "cmpq_linear_i8_fused")
+
+
+def cmpq_gated_i8_ws_bytes(n, d_in, d_ff, d_out):
+    return int(lib().cmpq_gated_i8_ws_bytes(n, d_in, d_ff, d_out))
+
+
+def cmpq_gated_i8(X, gate, up, down, d_ff, d_out, y, ws, norm=None, eps=1e-6, act="silu", residual=None, word=None):
+    """y = the gated block of norm(X), plus residual; gate, up, down: Weight8.  ws: see the header, its first bytes are 0."""
+    n, d_in = X.shape
+    _check(lib().cmpq_gated_i8(_at(X), _code(X), n, d_in, _rows(X, d_in, "X"), _at(norm), eps, gate, up, down, d_ff, d_out, ACTS[act],
+                               *_residual(residual, n, d_out, X), _at(y), _rows(y, d_out, "y"), _at(word), _at(ws), ws.numel(), _on(X)),
+           "cmpq_gated_i8")
 
 
 def cmpq_check_cache(word):

@@ -1,8 +1,9 @@
 // 8-bit linear layers: quantization of tokens and the integer product with scales per token and channel.
 #include <algorithm>
+#include <cfloat>
 
-#include "cache.cuh"
-#include "tc5.cuh"
+#include "epilogue.cuh"
+#include "linear_i8.cuh"
 #include "walk.cuh"
 
 namespace cmpq {
@@ -91,6 +92,112 @@ quantize_tokens_kernel(const uint16_t* __restrict__ X, int64_t d, int64_t ldx, i
         *reinterpret_cast<uint2*>(out + 8 * g) = group_codes<DT>(load8(row + 8 * g, d - 8 * g, wide), inv);
 }
 
+// Largest of the block's `m` and total of its `s`, the same bits in every thread.
+__device__ __forceinline__ void block_max_sum(uint32_t& m, float& s, uint32_t* part_m, float* part_s) {
+    m = __reduce_max_sync(0xffffffffu, m);
+#pragma unroll
+    for (int i = 16; i; i >>= 1) s += __shfl_xor_sync(0xffffffffu, s, i);
+    if ((threadIdx.x & 31) == 0) part_m[threadIdx.x >> 5] = m, part_s[threadIdx.x >> 5] = s;
+    __syncthreads();
+    s = 0.0f;
+#pragma unroll
+    for (int i = 0; i < kQtThreads / 32; ++i) m = max(m, part_m[i]), s += part_s[i];
+}
+
+// The squares of eight entries times f, added up as a tree: a row of 16384 entries goes through at most 8 + 3 + 5 + 8
+// additions one after the other.
+__device__ __forceinline__ float sum_squares(const float (&x)[8], float f) {
+    float q[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) q[i] = x[i] * f * (x[i] * f);
+    return ((q[0] + q[1]) + (q[2] + q[3])) + ((q[4] + q[5]) + (q[6] + q[7]));
+}
+
+// The same with a root-mean-square norm in front.  A row's codes do not depend on its norm: code = rint(v 127 / max|v|) with
+// v = x g, whatever v is divided by; the norm enters the scale alone.  So nothing waits for the sum of squares, and the
+// codes are as exact as without a norm.  v is one fp32 product, so magnitudes are compared in fp32 here.  A sum that passes
+// fp32 (entries above 2^54 or so) is taken again of entries times 2^-80; entries that vanish there vanish beside it too.
+template <int DT, int KEEP>
+__global__ void __launch_bounds__(kQtThreads)
+norm_quantize_kernel(const uint16_t* __restrict__ X, int64_t d, int64_t ldx, int wide, const uint16_t* __restrict__ norm, int wide_norm, float eps,
+                     int8_t* __restrict__ codes, int64_t ldc, float* __restrict__ scale, int32_t* __restrict__ nonfinite, int32_t* __restrict__ clear) {
+    tc5::dependents_may_start();
+    const uint16_t* row = X + blockIdx.x * ldx;
+    int8_t* out = codes + blockIdx.x * ldc;
+    const int t = threadIdx.x;
+    const int64_t groups = (d + 15) / 16 * 2;
+    uint4 keep[KEEP];
+#pragma unroll
+    for (int i = 0; i < KEEP; ++i) {
+        const int64_t g = t + (int64_t)i * kQtThreads;
+        keep[i] = make_uint4(0u, 0u, 0u, 0u);
+        if (g < groups) keep[i] = load8(row + 8 * g, d - 8 * g, wide);
+    }
+    uint32_t m = 0;
+    float sum = 0.0f;
+    auto look = [&](uint4 raw, int64_t g) {
+        float x[8], w[8];
+        widen8<DT>(raw, x);
+        widen8<DT>(load8(norm + 8 * g, d - 8 * g, wide_norm), w);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) m = max(m, __float_as_uint(x[j] * w[j]) & 0x7fffffffu);  // as bit patterns: NaN above infinity
+        sum += sum_squares(x, 1.0f);
+    };
+#pragma unroll
+    for (int i = 0; i < KEEP; ++i) {
+        const int64_t g = t + (int64_t)i * kQtThreads;
+        if (g < groups) look(keep[i], g);
+    }
+    for (int64_t g = t + (int64_t)KEEP * kQtThreads; g < groups; g += kQtThreads) look(load8(row + 8 * g, d - 8 * g, wide), g);
+    __shared__ uint32_t part_m[kQtThreads / 32];
+    __shared__ float part_s[kQtThreads / 32];
+    block_max_sum(m, sum, part_m, part_s);
+    const float amax = __uint_as_float(m);
+    float s = amax * (1.0f / 127.0f), inv = 1.0f / s;
+    if (amax < 0x1p-120f) s = inv = 0.0f;
+    auto store = [&](uint4 raw, int64_t g) {
+        float x[8], w[8];
+        widen8<DT>(raw, x);
+        widen8<DT>(load8(norm + 8 * g, d - 8 * g, wide_norm), w);
+        uint32_t c[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const float a = x[2 * j] * w[2 * j] * inv + 12582912.0f, b = x[2 * j + 1] * w[2 * j + 1] * inv + 12582912.0f;  // see group_codes
+            c[j] = __byte_perm(__float_as_uint(a), __float_as_uint(b), 0x0040);
+        }
+        *reinterpret_cast<uint2*>(out + 8 * g) = make_uint2(__byte_perm(c[0], c[1], 0x5410), __byte_perm(c[2], c[3], 0x5410));
+    };
+#pragma unroll
+    for (int i = 0; i < KEEP; ++i) {
+        const int64_t g = t + (int64_t)i * kQtThreads;
+        if (g < groups) store(keep[i], g);
+    }
+    for (int64_t g = t + (int64_t)KEEP * kQtThreads; g < groups; g += kQtThreads) store(load8(row + 8 * g, d - 8 * g, wide), g);
+    float f = 1.0f;
+    if (sum > FLT_MAX && m < 0x7f800000u) {  // the same in all threads; not a row with a NaN
+        f = 0x1p-80f, sum = 0.0f;
+#pragma unroll
+        for (int i = 0; i < KEEP; ++i) {
+            float x[8];
+            widen8<DT>(keep[i], x);
+            sum += sum_squares(x, f);
+        }
+        for (int64_t g = t + (int64_t)KEEP * kQtThreads; g < groups; g += kQtThreads) {
+            float x[8];
+            widen8<DT>(load8(row + 8 * g, d - 8 * g, wide), x);
+            sum += sum_squares(x, f);
+        }
+        __syncthreads();  // the parts have been read
+        block_max_sum(m, sum, part_m, part_s);
+    }
+    if (t == 0) {
+        if (s > 0.0f) s *= f / sqrtf(sum / (float)d + eps * f * f);
+        scale[blockIdx.x] = s;
+        if (clear && blockIdx.x == 0) *clear = 0;  // see the other kernel
+        if (m >= 0x7f800000u && nonfinite) atomicOr(nonfinite, 1);
+    }
+}
+
 // ---- the product --------------------------------------------------------------------------------------------
 //
 // Tokens are the rows of the accumulator (a TMEM lane each), output channels its columns: a thread of the epilogue owns
@@ -99,11 +206,15 @@ quantize_tokens_kernel(const uint16_t* __restrict__ X, int64_t d, int64_t ldx, i
 // swizzled TMA box and four instructions of K = 32.
 
 struct ProductArgs {
-    const float *xs, *ws;
-    const uint16_t* bias;
+    const float *xs, *ws, *us;         // us, ubias: of the second projection of a gated product
+    const uint16_t *bias, *ubias;
     uint16_t* y;
     int64_t ldy;
+    const uint16_t* residual;          // or null
+    int64_t ldr;
+    int act, wide_residual;
     int n, d_out, kblocks;  // kblocks: 128-byte blocks of the sum
+    int64_t cols;           // rows of weights: d_out, or twice that
     int wide;               // y takes 16-byte stores
     int n_tiles, m_tiles;   // tiles of channels, of tokens
     int stages, bn, rows;   // tile kernel: stages, channels of a tile, token rows that a box brings
@@ -142,6 +253,97 @@ __device__ __forceinline__ void store_rows(uint32_t tmem, int c0, int c1, const 
     }
 }
 
+// Sixteen 16-bit entries of a row, of which `left` exist, as floats.
+template <int DT>
+__device__ __forceinline__ void load16(const uint16_t* p, int left, bool wide, float (&f)[16]) {
+    float a[8], b[8];
+    widen8<DT>(load8(p, left, wide), a);
+    widen8<DT>(load8(p + 8, left - 8, wide), b);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) f[i] = a[i], f[i + 8] = b[i];
+}
+
+// The same with fl16(act(...) + residual).  y may be the residual: a thread reads its sixteen entries before it writes them.
+template <int DT>
+__device__ __forceinline__ void store_finished(uint32_t tmem, int c0, int c1, const float2* scale_bias, const ProductArgs& A, float xs, bool real,
+                                               uint16_t* y, const uint16_t* residual, int left) {
+    with_act(A.act, [&](auto act) {
+        for (int c = c0; c < c1; c += 16) {
+            uint32_t r[16], w[8];
+            float f[16];
+            tc5::tmem_ld16(tmem + c, r);
+            if (A.residual && real) load16<DT>(residual + c, left - c, A.wide_residual, f);
+            tc5::tmem_ld_wait();
+#pragma unroll
+            for (int j = 0; j < 16; j += 2) {
+                const float4 sb = *reinterpret_cast<const float4*>(scale_bias + c + j);
+                float a = (float)(int)r[j] * xs * sb.x, b = (float)(int)r[j + 1] * xs * sb.z;
+                if (A.bias) a += sb.y, b += sb.w;
+                a = activate<decltype(act)::value>(a), b = activate<decltype(act)::value>(b);
+                if (A.residual) a += f[j], b += f[j + 1];
+                w[j / 2] = round16x2<DT>(a, b);
+            }
+            if (!real) continue;
+            if (A.wide && c + 16 <= left) {
+                *reinterpret_cast<uint4*>(y + c) = make_uint4(w[0], w[1], w[2], w[3]);
+                *reinterpret_cast<uint4*>(y + c + 8) = make_uint4(w[4], w[5], w[6], w[7]);
+            } else {
+#pragma unroll
+                for (int j = 0; j < 16; ++j)
+                    if (c + j < left) y[c + j] = (uint16_t)(w[j >> 1] >> (16 * (j & 1)));
+            }
+        }
+    });
+}
+
+// Columns [c0, c1), multiples of 8, of a gated product: the accumulator's and scale_bias's first `half` columns are the gate,
+// the others the second projection; y = fl16(act(gate) * second), rows of y on 16 bytes.
+template <int DT>
+__device__ __forceinline__ void store_gated(uint32_t tmem, int c0, int c1, int half, const float2* scale_bias, const ProductArgs& A, float xs, bool real,
+                                            uint16_t* y, int left) {
+    with_act(A.act, [&](auto act) {
+        for (int c = c0; c < c1; c += 8) {
+            uint32_t g[8], u[8], w[4];
+            tc5::tmem_ld8(tmem + c, g);
+            tc5::tmem_ld8(tmem + half + c, u);
+            tc5::tmem_ld_wait();
+#pragma unroll
+            for (int j = 0; j < 8; j += 2) {
+                const float4 gs = *reinterpret_cast<const float4*>(scale_bias + c + j), us = *reinterpret_cast<const float4*>(scale_bias + half + c + j);
+                float g0 = (float)(int)g[j] * xs * gs.x, g1 = (float)(int)g[j + 1] * xs * gs.z;
+                float u0 = (float)(int)u[j] * xs * us.x, u1 = (float)(int)u[j + 1] * xs * us.z;
+                if (A.bias) g0 += gs.y, g1 += gs.w;
+                if (A.ubias) u0 += us.y, u1 += us.w;
+                w[j / 2] = round16x2<DT>(activate<decltype(act)::value>(g0) * u0, activate<decltype(act)::value>(g1) * u1);
+            }
+            if (!real) continue;
+            if (c + 8 <= left) {
+                *reinterpret_cast<uint4*>(y + c) = make_uint4(w[0], w[1], w[2], w[3]);
+            } else {
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    if (c + j < left) y[c + j] = (uint16_t)(w[j >> 1] >> (16 * (j & 1)));
+            }
+        }
+    });
+}
+
+// Scale and bias of column i of a tile whose channels begin at o0: of a gated tile the first half's, then the second's.
+template <int DT, int KIND>
+__device__ __forceinline__ float2 column_scale(const ProductArgs& A, int o0, int i, int columns) {
+    const bool second = KIND == kGated && i >= columns / 2;
+    const int o = min(o0 + (second ? i - columns / 2 : i), A.d_out - 1);
+    const uint16_t* bias = second ? A.ubias : A.bias;
+    return make_float2(__ldg((second ? A.us : A.ws) + o), bias ? widen16<DT>(bias[o]) : 0.0f);
+}
+
+// A thread's columns [c0, c1) of the residual, on their way into L2 while the products run.
+__device__ __forceinline__ void ask_for(const uint16_t* row, int c0, int c1) {
+    const uintptr_t end = reinterpret_cast<uintptr_t>(row + c1);
+    for (uintptr_t p = reinterpret_cast<uintptr_t>(row + c0) & ~(uintptr_t)127; c0 < c1 && p < end; p += 128)
+        asm volatile("prefetch.global.L2 [%0];" ::"l"(p));
+}
+
 // Few tiles: a block takes 128 tokens (all of them, mostly) and `bn` channels, a multiple of 16 chosen so that the
 // blocks fill the SMs; the weights pass through once and are the time while tokens are few.  Launched behind the
 // quantization of its tokens, a block asks for its first weights before that has ended.  A stage holds the
@@ -152,9 +354,11 @@ __device__ __forceinline__ void store_rows(uint32_t tmem, int c0, int c1, const 
 // Measured with the quantization in a stream of calls, weights from memory: one token 4096 -> 4096 10.3 us, 8192 -> 28672 42 us
 // (5.6 TB/s, 0.86 of the copy rate); 37 tokens 4096 -> 11008 14.3 us (3.2 TB/s: launch, first loads and the last stage's way
 // out are half of it).  Splitting the sum over a cluster instead, weights as rows, took 1.5, 1.3 and 2.4 times as long.
-template <int DT>
+//
+// A gated tile's columns are bn / 2 channels of the gate and the same ones of the second projection, from maps of their own.
+template <int DT, int KIND>
 __global__ void __launch_bounds__(kMmThreads)
-matmul_i8_tile_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__ CUtensorMap xmap,
+matmul_i8_tile_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__ CUtensorMap umap, const __grid_constant__ CUtensorMap xmap,
                       const __grid_constant__ ProductArgs A) {
     extern __shared__ uint8_t raw[];
     uint8_t* smem = raw + ((1024u - (tc5::smem_addr(raw) & 1023u)) & 1023u);
@@ -179,7 +383,13 @@ matmul_i8_tile_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_con
             for (int i = 0; i < A.kblocks; ++i) {
                 if (!tc5::mbar_wait(empty + slot, phase, &failed)) break;
                 tc5::mbar_expect_tx(full + slot, stage);  // the tokens' bytes too, whoever comes first
-                tc5::tma_load_2d(smem + slot * stage + a_bytes, &wmap, full + slot, i * 128, nt * bn);
+                uint8_t* at = smem + slot * stage + a_bytes;
+                if (KIND == kGated) {
+                    tc5::tma_load_2d(at, &wmap, full + slot, i * 128, nt * (bn / 2));
+                    tc5::tma_load_2d(at + bn / 2 * 128, &umap, full + slot, i * 128, nt * (bn / 2));
+                } else {
+                    tc5::tma_load_2d(at, &wmap, full + slot, i * 128, nt * bn);
+                }
                 if (++slot == A.stages) slot = 0, phase ^= 1;
             }
         }
@@ -201,11 +411,9 @@ matmul_i8_tile_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_con
         }
     } else {
         float2* sb = reinterpret_cast<float2*>(scale_bias);
-        const int o0 = nt * bn, left = min(bn, A.d_out - o0), i = threadIdx.x - 64;
-        if (i < bn) {
-            const int o = min(o0 + i, A.d_out - 1);
-            sb[i] = make_float2(__ldg(A.ws + o), A.bias ? widen16<DT>(A.bias[o]) : 0.0f);
-        }
+        const int wide = KIND == kGated ? bn / 2 : bn;  // channels of the tile
+        const int o0 = nt * wide, left = min(wide, A.d_out - o0), i = threadIdx.x - 64;
+        if (i < bn) sb[i] = column_scale<DT, KIND>(A, o0, i, bn);
         tc5::wait_for_previous();
         if (warp == 2) {  // the token codes: the first epilogue warp's work until then
             if (tc5::elect_one()) {
@@ -218,15 +426,21 @@ matmul_i8_tile_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_con
             }
             __syncwarp();
         }
-        const int quad = warp & 3, t = mt * 128 + quad * 32 + lane, half = (bn / 16 + 1) / 2 * 16;
+        const int step = KIND == kGated ? 8 : 16, quad = warp & 3, t = mt * 128 + quad * 32 + lane, half = (wide / step + 1) / 2 * step;
         const bool real = t < A.n, upper = warp >= 6;
+        const int c0 = upper ? half : 0, c1 = upper ? wide : half;
+        if (KIND == kFinish && A.residual && real) ask_for(A.residual + (int64_t)t * A.ldr + o0, c0, min(c1, left));
         const float xs = real ? __ldcg(A.xs + t) : 0.0f;  // written while this kernel was on its way: not the read-only path
         asm volatile("bar.sync 1, 256;" ::: "memory");
         tc5::mbar_wait_warp(&done, 0, &failed);
         tc5::fence_after_sync();
-        if (mt * 128 + quad * 32 < A.n)
-            store_rows<DT>(tmem + ((uint32_t)quad << 21), upper ? half : 0, upper ? bn : half, sb, A.bias != nullptr, xs, real,
-                           A.y + (int64_t)t * A.ldy + o0, left, A.wide);
+        if (mt * 128 + quad * 32 < A.n) {
+            const uint32_t rows = tmem + ((uint32_t)quad << 21);
+            uint16_t* y = A.y + (int64_t)t * A.ldy + o0;
+            if (KIND == kPlain) store_rows<DT>(rows, c0, c1, sb, A.bias != nullptr, xs, real, y, left, A.wide);
+            if (KIND == kFinish) store_finished<DT>(rows, c0, c1, sb, A, xs, real, y, A.residual + (int64_t)t * A.ldr + o0, left);
+            if (KIND == kGated) store_gated<DT>(rows, c0, c1, wide, sb, A, xs, real, y, left);
+        }
         tc5::fence_before_sync();
     }
     __syncwarp();
@@ -253,10 +467,14 @@ constexpr size_t kPairSmem = kPairStages * kPairStageBytes + 1024;
 // Measured: 4096 x 8192 x 28672 with the quantization 610 us in a few calls after a rest (3.15 POP/s, 0.96 of twice the library's
 // bf16 rate) and 680 to 694 in a long stream, where the power limit holds the clock; 2048 x 4096 x 11008 67 us, 72 with the
 // quantization, the tensor pipe at 81 % (172 pair tiles in 3 rounds of 74).
-template <int DT>
+//
+// A gated tile is 256 tokens x 128 channels of both projections: the even CTA's half of the columns is the gate, the odd
+// one's the second projection, so a thread of the epilogue finds both of a channel in its accumulator row.
+template <int DT, int KIND>
 __global__ void __launch_bounds__(kMmThreads, 1)
-matmul_i8_pair_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__ CUtensorMap xmap,
+matmul_i8_pair_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__ CUtensorMap umap, const __grid_constant__ CUtensorMap xmap,
                       const __grid_constant__ ProductArgs A) {
+    constexpr int kWide = KIND == kGated ? 128 : 256;  // channels of a tile
     extern __shared__ uint8_t raw[];
     uint8_t* smem = raw + ((1024u - (tc5::smem_addr(raw) & 1023u)) & 1023u);
     __shared__ uint64_t full[kPairStages], empty[kPairStages], acc_full[2], acc_empty[2];
@@ -290,7 +508,10 @@ matmul_i8_pair_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_con
                     if (rank == 0) tc5::mbar_expect_tx(full + slot, 2 * kPairStageBytes);
                     uint8_t* at = smem + slot * kPairStageBytes;
                     tc5::tma_load_2d_pair(at, &xmap, full + slot, k * 128, mt * 256 + rank * 128);
-                    tc5::tma_load_2d_pair(at + 128 * 128, &wmap, full + slot, k * 128, nt * 256 + rank * 128);
+                    if (KIND == kGated)
+                        tc5::tma_load_2d_pair(at + 128 * 128, rank ? &umap : &wmap, full + slot, k * 128, nt * 128);
+                    else
+                        tc5::tma_load_2d_pair(at + 128 * 128, &wmap, full + slot, k * 128, nt * 256 + rank * 128);
                     if (++slot == kPairStages) slot = 0, phase ^= 1;
                 }
             }
@@ -326,17 +547,25 @@ matmul_i8_pair_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_con
             [&](int tile, int acc) {
                 const int t = tile % A.m_tiles * 256 + rank * 128 + quad * 32 + lane;
                 xs = t < A.n ? __ldcg(A.xs + t) : 0.0f;  // see the other kernel
-                const int o = min(tile / A.m_tiles * 256 + i, A.d_out - 1);
-                reinterpret_cast<float2*>(scale_bias[acc])[i] = make_float2(__ldg(A.ws + o), A.bias ? widen16<DT>(A.bias[o]) : 0.0f);
+                const int o0 = tile / A.m_tiles * kWide;
+                reinterpret_cast<float2*>(scale_bias[acc])[i] = column_scale<DT, KIND>(A, o0, i, 256);
+                if (KIND == kFinish && A.residual && t < A.n)
+                    ask_for(A.residual + (int64_t)t * A.ldr + o0, min(upper * 128, A.d_out - o0), min(upper * 128 + 128, A.d_out - o0));
                 asm volatile("bar.sync 1, 256;" ::: "memory");
             },
             [&](int acc, int parity) { return tc5::mbar_wait_warp(acc_full + acc, parity, &failed); },
             [&](int tile, int acc) {
-                const int o0 = tile / A.m_tiles * 256, row0 = tile % A.m_tiles * 256 + rank * 128 + quad * 32, t = row0 + lane;
+                const int o0 = tile / A.m_tiles * kWide, row0 = tile % A.m_tiles * 256 + rank * 128 + quad * 32, t = row0 + lane;
+                const int left = min(kWide, A.d_out - o0), c0 = upper * (kWide / 2), c1 = c0 + kWide / 2;
                 tc5::fence_after_sync();
-                if (row0 < A.n)
-                    store_rows<DT>(tmem + ((uint32_t)quad << 21) + acc * 256, upper * 128, upper * 128 + 128, reinterpret_cast<float2*>(scale_bias[acc]),
-                                   A.bias != nullptr, xs, t < A.n, A.y + (int64_t)t * A.ldy + o0, min(256, A.d_out - o0), A.wide);
+                if (row0 < A.n) {
+                    const float2* sb = reinterpret_cast<float2*>(scale_bias[acc]);
+                    const uint32_t rows = tmem + ((uint32_t)quad << 21) + acc * 256;
+                    uint16_t* y = A.y + (int64_t)t * A.ldy + o0;
+                    if (KIND == kPlain) store_rows<DT>(rows, c0, c1, sb, A.bias != nullptr, xs, t < A.n, y, left, A.wide);
+                    if (KIND == kFinish) store_finished<DT>(rows, c0, c1, sb, A, xs, t < A.n, y, A.residual + (int64_t)t * A.ldr + o0, left);
+                    if (KIND == kGated) store_gated<DT>(rows, c0, c1, 128, sb, A, xs, t < A.n, y, left);
+                }
                 tc5::fence_before_sync();
                 __syncwarp();
                 if (lane == 0) tc5::mbar_arrive_remote(acc_empty + acc, 0);
@@ -361,44 +590,101 @@ matmul_i8_pair_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_con
 // less than the weights' way from memory (3400 bytes a cycle).  Fitted to sweeps of bn over 1 to 512 tokens and layers of
 // 4096 x 4096 to 8192 x 28672; e.g. 256 x 4096 x 11008: bn = 160 17.9 us, 80 22.7, pairs 21.6; 4096 x 8192 x 28672: pairs.
 static int64_t tile_cycles(const ProductArgs& a, int bn) {
-    const int64_t blocks = (int64_t)((a.n + 127) / 128) * ((a.d_out + bn - 1) / bn), sms = sm_count();
+    const int64_t blocks = (int64_t)((a.n + 127) / 128) * ((a.cols + bn - 1) / bn), sms = sm_count();
     const int64_t rounds = (blocks + sms - 1) / sms, pace = std::max(4 * std::max(32, bn / 2), (bn + std::min(a.n, 128)) * 2);
-    return std::max<int64_t>(rounds * a.kblocks * pace, (int64_t)a.kblocks * 128 * a.d_out / 3400) + rounds * (9000 + 8 * bn);
+    return std::max<int64_t>(rounds * a.kblocks * pace, (int64_t)a.kblocks * 128 * a.cols / 3400) + rounds * (9000 + 8 * bn);
 }
 static int64_t pair_cycles(const ProductArgs& a) {
-    const int64_t tiles = (int64_t)((a.n + 255) / 256) * ((a.d_out + 255) / 256), pairs = sm_count() / 2;
+    const int64_t tiles = (int64_t)((a.n + 255) / 256) * ((a.cols + 255) / 256), pairs = sm_count() / 2;
     return (tiles + pairs - 1) / pairs * a.kblocks * 600 + 14000;
 }
 
-template <int DT>
-static cmpq_status launch_product(const int8_t* xc, int64_t ldxc, const int8_t* wc, int64_t ldwc, int64_t d_in, ProductArgs a, bool behind,
-                                  cudaStream_t st) {
+template <int DT, int KIND>
+static cmpq_status launch_kind(const TokenCodes& x, int64_t d_in, const Weight8& w, const Weight8* u, ProductArgs a, bool behind, cudaStream_t st) {
     a.kblocks = (int)((d_in + 127) / 128);
     a.wide = aligned_to(a.y, 16) && a.ldy % 8 == 0;
+    a.wide_residual = aligned_to(a.residual, 16) && a.ldr % 8 == 0;
+    a.cols = (KIND == kGated ? 2 : 1) * (int64_t)a.d_out;
     a.bn = 32;
     for (int bn = 48; bn <= 256; bn += 16)
         if (tile_cycles(a, bn) < tile_cycles(a, a.bn)) a.bn = bn;
     const bool pair = a.n > 128 && pair_cycles(a) < tile_cycles(a, a.bn);
     a.rows = pair ? 128 : std::min(128, (a.n + 7) / 8 * 8);
-    CUtensorMap wmap, xmap;
-    if (!make_byte_map(&wmap, wc, a.d_out, d_in, ldwc, pair ? 128 : a.bn) || !make_byte_map(&xmap, xc, a.n, d_in, ldxc, a.rows)) return CMPQ_ERR_CUDA;
+    CUtensorMap wmap, umap, xmap;
+    const int box = pair ? 128 : KIND == kGated ? a.bn / 2 : a.bn, wide = pair ? (KIND == kGated ? 128 : 256) : box;
+    if (!make_byte_map(&wmap, w.codes, a.d_out, d_in, w.ld, box) || !make_byte_map(&xmap, x.codes, a.n, d_in, x.ld, a.rows)) return CMPQ_ERR_CUDA;
+    umap = wmap;
+    if (u && !make_byte_map(&umap, u->codes, a.d_out, d_in, u->ld, box)) return CMPQ_ERR_CUDA;
+    a.n_tiles = (a.d_out + wide - 1) / wide;
+    static bool raised[2][64];
     if (pair) {
-        a.m_tiles = (a.n + 255) / 256, a.n_tiles = (a.d_out + 255) / 256;
-        static bool raised[64];
-        if (!raise_smem_limit_once(matmul_i8_pair_kernel<DT>, kPairSmem, raised)) return CMPQ_ERR_CUDA;
+        a.m_tiles = (a.n + 255) / 256;
+        if (!raise_smem_limit_once(matmul_i8_pair_kernel<DT, KIND>, kPairSmem, raised[0])) return CMPQ_ERR_CUDA;
         const int64_t tiles = (int64_t)a.m_tiles * a.n_tiles;
-        return launch_cluster(matmul_i8_pair_kernel<DT>, 2 * (unsigned)std::min<int64_t>(tiles, sm_count() / 2), kMmThreads, kPairSmem, 2, behind, st,
-                              wmap, xmap, a);
+        return launch_cluster(matmul_i8_pair_kernel<DT, KIND>, 2 * (unsigned)std::min<int64_t>(tiles, sm_count() / 2), kMmThreads, kPairSmem, 2, behind,
+                              st, wmap, umap, xmap, a);
     }
-    a.m_tiles = (a.n + 127) / 128, a.n_tiles = (a.d_out + a.bn - 1) / a.bn;
+    a.m_tiles = (a.n + 127) / 128;
     // one block to an SM: two that share it were slower at every size, their rounds and tails cost more than they hide
     const int64_t blocks = (int64_t)a.m_tiles * a.n_tiles;
     const size_t stage = (a.rows + a.bn) * 128, slack = (128 - a.rows) * 128 + 1024;
     a.stages = std::min({(int)((kTileSmem - slack) / stage), kMmMaxStages, a.kblocks});
-    static bool raised[64];
-    if (!raise_smem_limit_once(matmul_i8_tile_kernel<DT>, kTileSmem, raised)) return CMPQ_ERR_CUDA;
+    if (!raise_smem_limit_once(matmul_i8_tile_kernel<DT, KIND>, kTileSmem, raised[1])) return CMPQ_ERR_CUDA;
     if (blocks > INT32_MAX) return CMPQ_ERR_UNSUPPORTED;
-    return launch_cluster(matmul_i8_tile_kernel<DT>, (unsigned)blocks, kMmThreads, a.stages * stage + slack, 1, behind, st, wmap, xmap, a);
+    return launch_cluster(matmul_i8_tile_kernel<DT, KIND>, (unsigned)blocks, kMmThreads, a.stages * stage + slack, 1, behind, st, wmap, umap, xmap, a);
+}
+
+template <int DT>
+static cmpq_status launch_product(const TokenCodes& x, int64_t n, int64_t d_in, const Weight8& w, int64_t d_out, const Weight8* u, const Finish& f,
+                                  void* y, int64_t ldy, int32_t* word, bool behind, cudaStream_t st) {
+    ProductArgs a = {};
+    a.xs = x.scale, a.ws = w.scale;
+    a.bias = static_cast<const uint16_t*>(w.bias);
+    a.y = static_cast<uint16_t*>(y);
+    a.ldy = ldy;
+    a.residual = static_cast<const uint16_t*>(f.residual);
+    a.ldr = f.ldr, a.act = f.act;
+    a.n = (int)n, a.d_out = (int)d_out;
+    a.failed = word;
+    if (u) {
+        a.us = u->scale;
+        a.ubias = static_cast<const uint16_t*>(u->bias);
+        return launch_kind<DT, kGated>(x, d_in, w, u, a, behind, st);
+    }
+    return f.act == CMPQ_ACT_NONE && !f.residual ? launch_kind<DT, kPlain>(x, d_in, w, nullptr, a, behind, st)
+                                                 : launch_kind<DT, kFinish>(x, d_in, w, nullptr, a, behind, st);
+}
+
+cmpq_status enqueue_product(const TokenCodes& x, cmpq_dtype dt, int64_t n, int64_t d_in, const Weight8& w, int64_t d_out, const Weight8* u,
+                            const Finish& f, void* y, int64_t ldy, int32_t* word, bool behind, cudaStream_t st) {
+    return dt == CMPQ_BF16 ? launch_product<CMPQ_BF16>(x, n, d_in, w, d_out, u, f, y, ldy, word, behind, st)
+                           : launch_product<CMPQ_F16>(x, n, d_in, w, d_out, u, f, y, ldy, word, behind, st);
+}
+
+template <int DT>
+static cmpq_status launch_quantize(const uint16_t* x, int64_t n, int64_t d, int64_t ldx, const uint16_t* norm, float eps, int8_t* codes, int64_t ldc,
+                                   float* scale, int32_t* word, int32_t* clear, cudaStream_t st) {
+    const int wide = aligned_to(x, 16) && ldx % 8 == 0, wide_norm = aligned_to(norm, 16);
+    const int64_t keep = (d + 8 * kQtThreads - 1) / (8 * kQtThreads);
+    const unsigned rows = (unsigned)n;
+    auto plain = [&](auto kernel) { return launch_cluster(kernel, rows, kQtThreads, 0, 1, false, st, x, d, ldx, wide, codes, ldc, scale, word, clear); };
+    auto normed = [&](auto kernel) {
+        return launch_cluster(kernel, rows, kQtThreads, 0, 1, false, st, x, d, ldx, wide, norm, wide_norm, eps, codes, ldc, scale, word, clear);
+    };
+    if (norm)
+        return keep <= 2   ? normed(norm_quantize_kernel<DT, 2>)
+               : keep <= 4 ? normed(norm_quantize_kernel<DT, 4>)
+                           : normed(norm_quantize_kernel<DT, 8>);
+    return keep <= 2   ? plain(quantize_tokens_kernel<DT, 2>)
+           : keep <= 4 ? plain(quantize_tokens_kernel<DT, 4>)
+                       : plain(quantize_tokens_kernel<DT, 8>);
+}
+
+cmpq_status enqueue_quantize(const void* X, cmpq_dtype dt, int64_t n, int64_t d, int64_t ldx, const void* norm, float eps, int8_t* codes, int64_t ldc,
+                             float* scale, int32_t* word, int32_t* clear, cudaStream_t st) {
+    const auto *x = static_cast<const uint16_t*>(X), *g = static_cast<const uint16_t*>(norm);
+    return dt == CMPQ_BF16 ? launch_quantize<CMPQ_BF16>(x, n, d, ldx, g, eps, codes, ldc, scale, word, clear, st)
+                           : launch_quantize<CMPQ_F16>(x, n, d, ldx, g, eps, codes, ldc, scale, word, clear, st);
 }
 
 size_t linear_i8_codes_bytes(int64_t n, int64_t d_in) { return round_up((size_t)n * round_up(d_in, 16), 256); }
@@ -407,40 +693,24 @@ size_t linear_i8_codes_bytes(int64_t n, int64_t d_in) { return round_up((size_t)
 
 using namespace cmpq;
 
-static bool linear_sizes_ok(int64_t n, int64_t d_in, int64_t d_out) {
-    return n >= 0 && n <= INT32_MAX - 256 /* tiles of tokens end past the last one */ && d_in >= 1 && d_in <= CMPQ_MAX_D_IN_I8 && d_out >= 1 && d_out <= CMPQ_MAX_D_IN;
-}
-
 extern "C" size_t cmpq_linear_i8_ws_bytes(int64_t n, int64_t d_in, int64_t d_out) {
     if (!linear_sizes_ok(n, d_in, d_out)) return 0;
     return linear_i8_codes_bytes(n, d_in) + round_up((size_t)n * sizeof(float), 256) + 256;
 }
 
-static cmpq_status quantize(const void* X, cmpq_dtype dt, int64_t n, int64_t d, int64_t ldx, int8_t* codes, int64_t ldc, float* scale,
-                            int32_t* nonfinite, int32_t* clear, void* stream) {
+extern "C" cmpq_status cmpq_norm_quantize_tokens(const void* X, cmpq_dtype dt, int64_t n, int64_t d, int64_t ldx, const void* norm, float eps,
+                                                 int8_t* codes, int64_t ldc, float* scale, int32_t* nonfinite, void* stream) {
     if (dt != CMPQ_F16 && dt != CMPQ_BF16) return CMPQ_ERR_INVALID_ARG;
-    if (n < 0 || n > INT32_MAX || d < 1 || d > CMPQ_MAX_D_IN || ldx < d || ldc < d || ldc % 16) return CMPQ_ERR_INVALID_ARG;
+    if (n < 0 || n > INT32_MAX || d < 1 || d > CMPQ_MAX_D_IN || ldx < d || ldc < d || ldc % 16 || !norm_ok(norm, eps)) return CMPQ_ERR_INVALID_ARG;
     if (n == 0) return CMPQ_OK;
     if (!X || !codes || !scale || !aligned_to(X, 2) || !aligned_to(codes, 16) || !aligned_to(scale, 4)) return CMPQ_ERR_INVALID_ARG;
-    const int wide = aligned_to(X, 16) && ldx % 8 == 0;
-    const auto* x = static_cast<const uint16_t*>(X);
-    auto st = static_cast<cudaStream_t>(stream);
-    const unsigned rows = (unsigned)n;
-    const int64_t keep = (d + 8 * kQtThreads - 1) / (8 * kQtThreads);
-    auto launch = [&](auto kernel) { return launch_cluster(kernel, rows, kQtThreads, 0, 1, false, st, x, d, ldx, wide, codes, ldc, scale, nonfinite, clear); };
-    if (dt == CMPQ_BF16)
-        return keep <= 2   ? launch(quantize_tokens_kernel<CMPQ_BF16, 2>)
-               : keep <= 4 ? launch(quantize_tokens_kernel<CMPQ_BF16, 4>)
-                           : launch(quantize_tokens_kernel<CMPQ_BF16, 8>);
-    return keep <= 2   ? launch(quantize_tokens_kernel<CMPQ_F16, 2>)
-           : keep <= 4 ? launch(quantize_tokens_kernel<CMPQ_F16, 4>)
-                       : launch(quantize_tokens_kernel<CMPQ_F16, 8>);
+    return enqueue_quantize(X, dt, n, d, ldx, norm, eps, codes, ldc, scale, nonfinite, nullptr, static_cast<cudaStream_t>(stream));
 }
 
 extern "C" cmpq_status cmpq_quantize_tokens(const void* X, cmpq_dtype dt, int64_t n, int64_t d, int64_t ldx,
                                             int8_t* codes, int64_t ldc, float* scale, int32_t* nonfinite,
                                             void* stream) {
-    return quantize(X, dt, n, d, ldx, codes, ldc, scale, nonfinite, nullptr, stream);
+    return cmpq_norm_quantize_tokens(X, dt, n, d, ldx, nullptr, 0.0f, codes, ldc, scale, nonfinite, stream);
 }
 
 // Where a call without a word of the caller's keeps the mark of a kernel that gave up; it starts from 0 in every call.
@@ -448,53 +718,43 @@ static int32_t* mark_of(void* ws, int64_t n, int64_t d_in, int64_t d_out) {
     return reinterpret_cast<int32_t*>(static_cast<char*>(ws) + cmpq_linear_i8_ws_bytes(n, d_in, d_out) - 256);
 }
 
-// The caller has checked everything.
-static cmpq_status product(const int8_t* xc, int64_t ldxc, const float* xs, const int8_t* wc, int64_t ldwc, const float* w_scale, const void* bias,
-                           cmpq_dtype dt, int64_t n, int64_t d_in, int64_t d_out, void* y, int64_t ldy, int32_t* word, bool behind, void* stream) {
-    ProductArgs a = {};
-    a.xs = xs, a.ws = w_scale;
-    a.bias = static_cast<const uint16_t*>(bias);
-    a.y = static_cast<uint16_t*>(y);
-    a.ldy = ldy;
-    a.n = (int)n, a.d_out = (int)d_out;
-    a.failed = word;
-    auto st = static_cast<cudaStream_t>(stream);
-    return dt == CMPQ_BF16 ? launch_product<CMPQ_BF16>(xc, ldxc, wc, ldwc, d_in, a, behind, st)
-                           : launch_product<CMPQ_F16>(xc, ldxc, wc, ldwc, d_in, a, behind, st);
-}
-
 extern "C" cmpq_status cmpq_matmul_i8(const int8_t* xc, int64_t ldxc, const float* xs, const int8_t* wc, int64_t ldwc,
                                       const float* w_scale, const void* bias, cmpq_dtype dt, int64_t n, int64_t d_in,
                                       int64_t d_out, void* y, int64_t ldy, void* ws, size_t ws_bytes, void* stream) {
+    const cmpq_weight_i8 w = {wc, ldwc, w_scale, bias};
     if (dt != CMPQ_F16 && dt != CMPQ_BF16) return CMPQ_ERR_INVALID_ARG;
-    if (!linear_sizes_ok(n, d_in, d_out) || ldxc < d_in || ldwc < d_in || ldxc % 16 || ldwc % 16 || ldy < d_out) return CMPQ_ERR_INVALID_ARG;
+    if (!linear_sizes_ok(n, d_in, d_out) || ldxc < d_in || ldxc % 16 || ldy < d_out || !weight_rows_ok(w, d_in)) return CMPQ_ERR_INVALID_ARG;
     if (n == 0) return CMPQ_OK;
-    if (!xc || !xs || !wc || !w_scale || !y || !aligned_to(xc, 16) || !aligned_to(wc, 16) || !aligned_to(xs, 4) ||
-        !aligned_to(w_scale, 4) || !aligned_to(y, 2) || !aligned_to(bias, 2))
-        return CMPQ_ERR_INVALID_ARG;
+    if (!xc || !xs || !y || !weight_ok(w) || !aligned_to(xc, 16) || !aligned_to(xs, 4) || !aligned_to(y, 2)) return CMPQ_ERR_INVALID_ARG;
     if (!ws || !aligned_to(ws, 256) || ws_bytes < cmpq_linear_i8_ws_bytes(n, d_in, d_out)) return CMPQ_ERR_WORKSPACE;
     int32_t* mark = mark_of(ws, n, d_in, d_out);
     if (cudaMemsetAsync(mark, 0, sizeof(*mark), static_cast<cudaStream_t>(stream)) != cudaSuccess) return CMPQ_ERR_CUDA;
-    return product(xc, ldxc, xs, wc, ldwc, w_scale, bias, dt, n, d_in, d_out, y, ldy, mark, false, stream);
+    return enqueue_product({xc, ldxc, xs}, dt, n, d_in, w, d_out, nullptr, {}, y, ldy, mark, false, static_cast<cudaStream_t>(stream));
 }
 
-extern "C" cmpq_status cmpq_linear_i8(const void* X, cmpq_dtype dt, int64_t n, int64_t d_in, int64_t ldx,
-                                      const int8_t* wc, int64_t ldwc, const float* w_scale, const void* bias,
-                                      int64_t d_out, void* y, int64_t ldy, int32_t* nonfinite, void* ws,
-                                      size_t ws_bytes, void* stream) {
-    if (!linear_sizes_ok(n, d_in, d_out) || ldwc < d_in || ldwc % 16 || ldy < d_out || ldx < d_in) return CMPQ_ERR_INVALID_ARG;
-    if (dt != CMPQ_F16 && dt != CMPQ_BF16) return CMPQ_ERR_INVALID_ARG;
+extern "C" cmpq_status cmpq_linear_i8_fused(const void* X, cmpq_dtype dt, int64_t n, int64_t d_in, int64_t ldx, const void* norm, float eps,
+                                            const cmpq_weight_i8* weight, int64_t d_out, cmpq_act act, const void* residual, int64_t ldr, void* y,
+                                            int64_t ldy, int32_t* nonfinite, void* ws, size_t ws_bytes, void* stream) {
+    if (!weight || !linear_sizes_ok(n, d_in, d_out) || !weight_rows_ok(*weight, d_in) || ldy < d_out || ldx < d_in) return CMPQ_ERR_INVALID_ARG;
+    if ((dt != CMPQ_F16 && dt != CMPQ_BF16) || !norm_ok(norm, eps) || !finish_ok(act, residual, ldr, d_out)) return CMPQ_ERR_INVALID_ARG;
     if (n == 0) return CMPQ_OK;
-    if (!wc || !w_scale || !y || !aligned_to(wc, 16) || !aligned_to(w_scale, 4) || !aligned_to(y, 2) || !aligned_to(bias, 2))
-        return CMPQ_ERR_INVALID_ARG;
+    if (!X || !y || !weight_ok(*weight) || !aligned_to(X, 2) || !aligned_to(y, 2)) return CMPQ_ERR_INVALID_ARG;
     if (!ws || !aligned_to(ws, 256) || ws_bytes < cmpq_linear_i8_ws_bytes(n, d_in, d_out)) return CMPQ_ERR_WORKSPACE;
     Workspace w(ws, ws_bytes);
     int8_t* codes = w.take<int8_t>(linear_i8_codes_bytes(n, d_in));
     float* scale = w.take<float>(n);
     const int64_t ldc = (int64_t)round_up(d_in, 16);
     int32_t* mark = mark_of(ws, n, d_in, d_out);
-    cmpq_status st = quantize(X, dt, n, d_in, ldx, codes, ldc, scale, nonfinite, nonfinite ? nullptr : mark, stream);
-    if (st != CMPQ_OK) return st;
+    const auto st = static_cast<cudaStream_t>(stream);
+    const cmpq_status s = enqueue_quantize(X, dt, n, d_in, ldx, norm, eps, codes, ldc, scale, nonfinite, nonfinite ? nullptr : mark, st);
+    if (s != CMPQ_OK) return s;
     // the quantization lets the product start early; it was itself started after everything before it, the weights too
-    return product(codes, ldc, scale, wc, ldwc, w_scale, bias, dt, n, d_in, d_out, y, ldy, nonfinite ? nonfinite : mark, true, stream);
+    return enqueue_product({codes, ldc, scale}, dt, n, d_in, *weight, d_out, nullptr, {act, residual, ldr}, y, ldy, nonfinite ? nonfinite : mark, true, st);
+}
+
+extern "C" cmpq_status cmpq_linear_i8(const void* X, cmpq_dtype dt, int64_t n, int64_t d_in, int64_t ldx, const int8_t* wc,
+                                      int64_t ldwc, const float* w_scale, const void* bias, int64_t d_out, void* y, int64_t ldy,
+                                      int32_t* nonfinite, void* ws, size_t ws_bytes, void* stream) {
+    const cmpq_weight_i8 w = {wc, ldwc, w_scale, bias};
+    return cmpq_linear_i8_fused(X, dt, n, d_in, ldx, nullptr, 0.0f, &w, d_out, CMPQ_ACT_NONE, nullptr, 0, y, ldy, nonfinite, ws, ws_bytes, stream);
 }

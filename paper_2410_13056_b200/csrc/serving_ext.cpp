@@ -69,7 +69,7 @@ int64_t rows(const Tensor& t, const char* name) {
 // they are of.  A call that is being captured takes its own from the graph's memory, zeroed by a node of that graph, and
 // leaves nothing behind: a graph never depends on another one, on eager calls, or on the stream that it is replayed on.
 struct Spaces {
-    bool zeroed;  // the first CMPQ_ATTENTION_ZEROED bytes are counters that start at 0
+    int64_t zeroed;  // the first bytes, counters that start at 0
     std::map<std::pair<int, void*>, Tensor> held;
 
     Tensor get(const at::Device& device, void* stream, size_t bytes) {
@@ -80,7 +80,7 @@ struct Spaces {
     }
     Tensor fresh(const at::Device& device, size_t bytes) const {
         Tensor t = at::empty({(int64_t)bytes}, at::TensorOptions().dtype(at::kByte).device(device));
-        if (zeroed) t.narrow(0, 0, CMPQ_ATTENTION_ZEROED).zero_();
+        if (zeroed) t.narrow(0, 0, zeroed).zero_();
         return t;
     }
     void drop(const at::Device& device) {
@@ -89,11 +89,15 @@ struct Spaces {
 };
 // Never destroyed: the allocator may be gone before static objects are.
 Spaces& linear_spaces() {
-    static Spaces* s = new Spaces{false, {}};
+    static Spaces* s = new Spaces{0, {}};
     return *s;
 }
 Spaces& attention_spaces() {
-    static Spaces* s = new Spaces{true, {}};
+    static Spaces* s = new Spaces{CMPQ_ATTENTION_ZEROED, {}};
+    return *s;
+}
+Spaces& gated_spaces() {
+    static Spaces* s = new Spaces{CMPQ_GATED_ZEROED, {}};
     return *s;
 }
 
@@ -104,6 +108,37 @@ cmpq_status take_word(const Tensor& word) {
     if (s != CMPQ_OK) word.zero_();
     return s;
 }
+
+cmpq_act act_of(const std::optional<std::string>& name) {
+    static const char* const names[] = {"none", "relu", "silu", "gelu", "gelu_tanh"};  // in the order of cmpq_act
+    if (!name) return CMPQ_ACT_NONE;
+    for (int i = 0; i < 5; ++i)
+        if (*name == names[i]) return (cmpq_act)i;
+    refuse("activation needs to be none, relu, silu, gelu or gelu_tanh, got " + *name);
+}
+
+// Checks of what the calls of a layer take beside its weights, of which `home` is one.
+struct Around {
+    cmpq_dtype dt;
+    int64_t n, ldr = 0;
+    const void *norm = nullptr, *residual = nullptr;
+
+    Around(const Tensor& x, int64_t d_in, int64_t d_out, const Tensor& home, const OptTensor& into, const OptTensor& res, const OptTensor& weight) {
+        if (x.dim() != 2 || x.size(1) != d_in || !x.is_cuda()) refuse("x needs shape [n][" + std::to_string(d_in) + "] on the GPU, got " + shape_of(x));
+        beside(x, home, "x"), beside(into, home, "out"), beside(res, home, "residual"), beside(weight, home, "norm");
+        dt = code(x);
+        n = x.size(0);
+        for (const auto& [t, name] : {std::pair<const OptTensor&, const char*>(into, "out"), {res, "residual"}})
+            if (t && (t->dim() != 2 || t->size(0) != n || t->size(1) != d_out || t->scalar_type() != x.scalar_type() || !t->is_cuda()))
+                refuse(std::string(name) + " needs shape [n][" + std::to_string(d_out) + "] and x's dtype");
+        if (res) residual = res->data_ptr(), ldr = rows(*res, "residual");
+        if (weight) {
+            if (weight->dim() != 1 || weight->size(0) != d_in || weight->scalar_type() != x.scalar_type() || !weight->is_contiguous())
+                refuse("norm needs " + std::to_string(d_in) + " contiguous entries of x's dtype");
+            norm = weight->data_ptr();
+        }
+    }
+};
 
 struct Linear {
     Tensor w, scale;
@@ -124,27 +159,67 @@ struct Linear {
         nonfinite = at::zeros({1}, at::TensorOptions().dtype(at::kInt).device(w.device()));
     }
 
-    Tensor call(const Tensor& x, const OptTensor& into) {
-        if (x.dim() != 2 || x.size(1) != d_in || !x.is_cuda()) refuse("x needs shape [n][" + std::to_string(d_in) + "] on the GPU, got " + shape_of(x));
-        beside(x, w, "x"), beside(into, w, "out");
-        const cmpq_dtype dt = code(x);
+    cmpq_weight_i8 weight() const {
+        return {w.data_ptr<int8_t>(), d_out > 1 ? w.stride(0) : (d_in + 15) / 16 * 16, scale.data_ptr<float>(), bias ? bias->data_ptr() : nullptr};
+    }
+
+    void takes(const Tensor& x) const {
         if (bias && bias->scalar_type() != x.scalar_type()) throw py::type_error("bias and x need one dtype");
-        const int64_t n = x.size(0);
-        if (into && (into->dim() != 2 || into->size(0) != n || into->size(1) != d_out || into->scalar_type() != x.scalar_type() || !into->is_cuda()))
-            refuse("out needs shape [n][" + std::to_string(d_out) + "] and x's dtype");
+    }
+
+    Tensor call(const Tensor& x, const OptTensor& into, const std::optional<std::string>& activation, const OptTensor& residual, const OptTensor& norm,
+                double eps) {
+        const Around a(x, d_in, d_out, w, into, residual, norm);
+        takes(x);
+        const cmpq_act act = act_of(activation);
         const c10::cuda::CUDAGuard guard(x.device());
-        Tensor y = into ? *into : at::empty({n, d_out}, x.options());
-        if (n == 0) return y;
+        Tensor y = into ? *into : at::empty({a.n, d_out}, x.options());
+        if (a.n == 0) return y;
         void* stream = stream_of(x);
-        const Tensor ws = linear_spaces().get(x.device(), stream, cmpq_linear_i8_ws_bytes(n, d_in, d_out));
-        check(cmpq_linear_i8(x.data_ptr(), dt, n, d_in, rows(x, "x"), w.data_ptr<int8_t>(), d_out > 1 ? w.stride(0) : (d_in + 15) / 16 * 16,
-                             scale.data_ptr<float>(), bias ? bias->data_ptr() : nullptr, d_out, y.data_ptr(), rows(y, "out"),
-                             nonfinite.data_ptr<int32_t>(), ws.data_ptr(), ws.numel(), stream),
+        const Tensor ws = linear_spaces().get(x.device(), stream, cmpq_linear_i8_ws_bytes(a.n, d_in, d_out));
+        const cmpq_weight_i8 weights = weight();
+        check(cmpq_linear_i8_fused(x.data_ptr(), a.dt, a.n, d_in, rows(x, "x"), a.norm, (float)eps, &weights, d_out, act, a.residual, a.ldr, y.data_ptr(),
+                                   rows(y, "out"), nonfinite.data_ptr<int32_t>(), ws.data_ptr(), ws.numel(), stream),
               "cmpq_linear_i8");
         return y;
     }
 
     void look() { check(take_word(nonfinite), "cmpq_linear_i8"); }
+};
+
+struct Gated {
+    Linear gate, up, down;
+    cmpq_act act;
+    Tensor word;
+
+    Gated(const Linear& g, const Linear& u, const Linear& d, const std::optional<std::string>& activation) : gate(g), up(u), down(d), act(act_of(activation)) {
+        beside(u.w, g.w, "up"), beside(d.w, g.w, "down");
+        if (u.d_in != g.d_in || u.d_out != g.d_out || d.d_in != g.d_out)
+            refuse("gate [" + std::to_string(g.d_out) + "][" + std::to_string(g.d_in) + "], up [" + std::to_string(u.d_out) + "][" + std::to_string(u.d_in) +
+                   "] and down [" + std::to_string(d.d_out) + "][" + std::to_string(d.d_in) + "] do not fit together");
+        word = at::zeros({1}, at::TensorOptions().dtype(at::kInt).device(g.w.device()));
+    }
+
+    Tensor call(const Tensor& x, const OptTensor& into, const OptTensor& residual, const OptTensor& norm, double eps) {
+        const Around a(x, gate.d_in, down.d_out, gate.w, into, residual, norm);
+        gate.takes(x), up.takes(x), down.takes(x);
+        const c10::cuda::CUDAGuard guard(x.device());
+        Tensor y = into ? *into : at::empty({a.n, down.d_out}, x.options());
+        if (a.n == 0) return y;
+        void* stream = stream_of(x);
+        const Tensor ws = gated_spaces().get(x.device(), stream, cmpq_gated_i8_ws_bytes(a.n, gate.d_in, gate.d_out, down.d_out));
+        const cmpq_weight_i8 g = gate.weight(), u = up.weight(), d = down.weight();
+        check(cmpq_gated_i8(x.data_ptr(), a.dt, a.n, gate.d_in, rows(x, "x"), a.norm, (float)eps, &g, &u, &d, gate.d_out, down.d_out, act, a.residual, a.ldr,
+                            y.data_ptr(), rows(y, "out"), word.data_ptr<int32_t>(), ws.data_ptr(), ws.numel(), stream),
+              "cmpq_gated_i8");
+        return y;
+    }
+
+    void look() {
+        const cmpq_status s = take_word(word);
+        if (s == CMPQ_ERR_INTERNAL) gated_spaces().drop(word.device());  // see Cache::look
+        check(s, "cmpq_gated_i8");
+    }
 };
 
 struct Cache {
@@ -273,7 +348,8 @@ PYBIND11_MODULE(_serving, m) {
     });
     py::class_<Linear>(m, "Linear")
         .def(py::init<const Tensor&, const Tensor&, const OptTensor&>())
-        .def("__call__", &Linear::call, py::arg("x"), py::arg("out") = py::none())
+        .def("__call__", &Linear::call, py::arg("x"), py::arg("out") = py::none(), py::arg("activation") = py::none(), py::arg("residual") = py::none(),
+             py::arg("norm") = py::none(), py::arg("eps") = 1e-6)
         .def("check", &Linear::look)
         .def_readonly("w_codes", &Linear::w)
         .def_readonly("w_scale", &Linear::scale)
@@ -281,6 +357,12 @@ PYBIND11_MODULE(_serving, m) {
         .def_readonly("nonfinite", &Linear::nonfinite)
         .def_readonly("d_in", &Linear::d_in)
         .def_readonly("d_out", &Linear::d_out);
+    py::class_<Gated>(m, "Gated")
+        .def(py::init<const Linear&, const Linear&, const Linear&, const std::optional<std::string>&>())
+        .def("__call__", &Gated::call, py::arg("x"), py::arg("out") = py::none(), py::arg("residual") = py::none(), py::arg("norm") = py::none(),
+             py::arg("eps") = 1e-6)
+        .def("check", &Gated::look)
+        .def_readonly("word", &Gated::word);
     py::class_<Cache>(m, "Cache")
         .def(py::init<const Tensor&, const Tensor&, const Tensor&, const Tensor&>())
         .def("append", &Cache::append, py::arg("k"), py::arg("v"), py::arg("tok_off"), py::arg("lens"), py::arg("table"), py::arg("q") = py::none(),

@@ -1,10 +1,11 @@
 """Serving with 8-bit activations and an 8-bit cache: what holds the buffers of those C-ABI calls.
 
-`Int8Linear` is a linear layer with 8-bit weight codes, `PagedCache8` a paged cache of keys and values with a scale
+`Int8Linear` is a linear layer with 8-bit weight codes (a norm before it, an activation and a residual behind it where they
+are given), `GatedMLP8` a gated feed-forward block of three of them, `PagedCache8` a paged cache of keys and values with a scale
 per page and head (append, read back, attend), `AttentionLayer8` the attention block that runs them together: the
 projections, the append with the rotation on the way, the attention over the cache and the output projection.
-Everything is enqueued on the current torch stream; nothing is computed here.  The calls of the first two are
-marshalled in C++ (csrc/serving_ext.cpp, built next to the library): wrong shapes and types raise ValueError and
+`DecoderLayer8` is the whole layer.  Everything is enqueued on the current torch stream; nothing is computed here.  The calls
+of linear layer, gated block and cache are marshalled in C++ (csrc/serving_ext.cpp, built next to the library): wrong shapes and types raise ValueError and
 TypeError, a status of the library CmpqError.
 
 Work spaces: eager calls share one per device and stream, whatever layer or cache makes them.  All calls can be captured in
@@ -27,6 +28,16 @@ def _ext():
     return _serving
 
 
+def quantize_tokens(x, norm=None, eps=1e-6):
+    """int8 codes [n][d] and fp32 scales [n] of the rows of x (fp16/bf16 [n][d]), behind a root-mean-square norm where its weight
+    (x's dtype, [d]) is given: the form in which the products take their tokens."""
+    n, d = x.shape
+    codes = torch.empty(n, (d + 15) // 16 * 16, dtype=torch.int8, device=x.device)[:, :d]
+    scale = torch.empty(n, dtype=torch.float32, device=x.device)
+    B.cmpq_norm_quantize_tokens(x, norm, eps, codes, scale)
+    return codes, scale
+
+
 class Int8Linear:
     """y = x W^T + b with 8-bit codes on both sides.  w_codes: int8 [d_out][d_in], rows on multiples of 16 bytes;
     w_scale: fp32 [d_out]; bias: fp16/bf16 [d_out] or None (its dtype is then the activations')."""
@@ -46,13 +57,37 @@ class Int8Linear:
         B.cmpq_quantize_tokens(weight, codes, scale)
         return cls(codes, scale, bias)
 
-    def __call__(self, x, out=None):
-        """x: fp16/bf16 [n][d_in].  Returns out [n][d_out] of x's dtype."""
-        return self._impl(x, out)
+    def __call__(self, x, out=None, *, activation=None, residual=None, norm=None, eps=1e-6):
+        """x: fp16/bf16 [n][d_in].  Returns out [n][d_out] of x's dtype: activation(layer(x)) + residual.  activation: None,
+        "relu", "silu", "gelu" or "gelu_tanh"; residual: [n][d_out] of x's dtype, which out may be; norm: [d_in] of x's dtype,
+        the weight of a root-mean-square norm (with eps) that x goes through first."""
+        return self._impl(x, out, activation, residual, norm, eps)
 
     def check(self):
         """Waits for the current stream and raises CmpqError if a token of a call so far held a NaN or an infinity (status
         6) or a kernel gave up waiting, its output unspecified (status 5); forgets what it reported."""
+        self._impl.check()
+
+
+class GatedMLP8:
+    """The gated feed-forward block of a served layer in 8 bits: down(activation(gate(x)) * up(x)), of three Int8Linear.  The
+    activated product is rounded to x's dtype and quantized per token.  What its own calls meet is reported by its check(), not
+    by the parts'."""
+
+    def __init__(self, gate, up, down, activation="silu"):
+        self._impl = _ext().Gated(gate._impl, up._impl, down._impl, activation)
+        self.gate, self.up, self.down, self.activation = gate, up, down, activation
+        self.d_in, self.d_ff, self.d_out = gate.d_in, gate.d_out, down.d_out
+        self.word = self._impl.word
+
+    def __call__(self, x, out=None, *, residual=None, norm=None, eps=1e-6):
+        """x: fp16/bf16 [n][d_in].  Returns out [n][d_out] of x's dtype: block(x) + residual; residual, norm and eps as for
+        Int8Linear."""
+        return self._impl(x, out, residual, norm, eps)
+
+    def check(self):
+        """Waits for the current stream and raises CmpqError if a call so far met a NaN or an infinity among its tokens or
+        between the projections (status 6) or a kernel gave up waiting (status 5); forgets what it reported."""
         self._impl.check()
 
 
@@ -111,22 +146,50 @@ class AttentionLayer8:
         self.qkv, self.out, self.cache, self.n_heads = qkv, out, cache, n_heads
         self.cos, self.sin, self.interleaved = cos, sin, interleaved
 
-    def __call__(self, x, tok_off, lens, table, max_new, max_len=None, window=0):
-        """x: fp16/bf16 [n_tok][d_model], the new tokens of a batch (see PagedCache8).  Returns [n_tok][out.d_out]."""
+    def __call__(self, x, tok_off, lens, table, max_new, max_len=None, window=0, *, residual=None, norm=None, eps=1e-6):
+        """x: fp16/bf16 [n_tok][d_model], the new tokens of a batch (see PagedCache8).  Returns [n_tok][out.d_out]; norm and eps
+        as for the projection of x, residual as for the output's (see Int8Linear)."""
         h, kv, d = self.n_heads, self.cache.n_kv, self.cache.head_dim
-        y = self.qkv(x)
+        y = self.qkv(x, norm=norm, eps=eps)
         q, k, v = (y[:, a * d: b * d].unflatten(1, (b - a, d)) for a, b in ((0, h), (h, h + kv), (h + kv, h + 2 * kv)))
         self.cache.append(k, v, tok_off, lens, table, q=q, cos=self.cos, sin=self.sin, interleaved=self.interleaved, q_out=q)
         a = self.cache.attend(q, tok_off, lens, table, max_new, max_len, window=window)
-        return self.out(a.flatten(1))
+        return self.out(a.flatten(1), residual=residual)
 
     def check(self):
         """check() of both projections and of the cache; raises the first of their errors, and all forget theirs."""
-        errors = []
-        for part in (self.qkv, self.cache, self.out):
-            try:
-                part.check()
-            except B.CmpqError as e:
-                errors.append(e)
-        if errors:
-            raise errors[0]
+        _check_all(self.qkv, self.cache, self.out)
+
+
+class DecoderLayer8:
+    """A decoder layer in 8 bits: x + attention(norm(x)), then that plus the feed-forward block of its norm.  attention: an
+    AttentionLayer8; mlp: a GatedMLP8; attention_norm, mlp_norm: the weights of the two root-mean-square norms, fp16/bf16
+    [d_model]."""
+
+    def __init__(self, attention, mlp, attention_norm, mlp_norm, eps=1e-6):
+        d = attention.qkv.d_in
+        if attention.out.d_out != d or mlp.d_in != d or mlp.d_out != d:
+            raise ValueError("attention [%d -> %d] and feed-forward block [%d -> %d] do not fit into one layer"
+                             % (d, attention.out.d_out, mlp.d_in, mlp.d_out))
+        self.attention, self.mlp = attention, mlp
+        self.attention_norm, self.mlp_norm, self.eps = attention_norm, mlp_norm, eps
+
+    def __call__(self, x, tok_off, lens, table, max_new, max_len=None, window=0):
+        """x: fp16/bf16 [n_tok][d_model], the new tokens of a batch (see PagedCache8).  Returns the same shape."""
+        a = self.attention(x, tok_off, lens, table, max_new, max_len, window, residual=x, norm=self.attention_norm, eps=self.eps)
+        return self.mlp(a, out=a, residual=a, norm=self.mlp_norm, eps=self.eps)
+
+    def check(self):
+        """check() of the attention block and of the feed-forward block; raises the first of their errors, and all forget theirs."""
+        _check_all(self.attention, self.mlp)
+
+
+def _check_all(*parts):
+    errors = []
+    for part in parts:
+        try:
+            part.check()
+        except B.CmpqError as e:
+            errors.append(e)
+    if errors:
+        raise errors[0]
