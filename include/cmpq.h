@@ -482,16 +482,16 @@ cmpq_status cmpq_linear_i8_fused(const void* X, cmpq_dtype dt, int64_t n, int64_
  * CMPQ_MAX_D_IN_I8, d_out up to CMPQ_MAX_D_IN.  residual as in cmpq_linear_i8_fused.
  * `word` (optional device int32, zeroed by the caller): bit 0 when a token or an h is a NaN or an infinity (an h beyond
  * 65504 in fp16 is one), bit 3 when a kernel gave up waiting (about a second; never seen).  cmpq_check_cache takes it.
- * ws: cmpq_gated_i8_ws_bytes(n, d_in, d_ff, d_out), 0 for arguments out of range.  Its first CMPQ_GATED_ZEROED bytes have to be
- * 0 when the call's kernels start, and are 0 again when they have ended: zero them once, after allocating the buffer and
- * after bit 3, which every call on the buffer reports from then on.  Calls that may run at the same time, graphs' replays
- * among them, need buffers of their own. */
-#define CMPQ_GATED_ZEROED 4096
+ * state: CMPQ_GATED_STATE_BYTES bytes, 16-byte aligned, in which the blocks of a kernel meet.  They have to be 0 when the call's
+ * kernels start, and are 0 again when they have ended: zero them once, when they are allocated, and after bit 3, which calls
+ * with this state may report from then on.  Calls that may run at the same time, graphs' replays among them, need states and work
+ * spaces of their own.  ws: cmpq_gated_i8_ws_bytes(n, d_in, d_ff, d_out), 0 for arguments out of range. */
+#define CMPQ_GATED_STATE_BYTES 256
 size_t cmpq_gated_i8_ws_bytes(int64_t n, int64_t d_in, int64_t d_ff, int64_t d_out);
 cmpq_status cmpq_gated_i8(const void* X, cmpq_dtype dt, int64_t n, int64_t d_in, int64_t ldx, const void* norm, float eps,
                           const cmpq_weight_i8* gate, const cmpq_weight_i8* up, const cmpq_weight_i8* down, int64_t d_ff,
                           int64_t d_out, cmpq_act act, const void* residual, int64_t ldr, void* y, int64_t ldy, int32_t* word,
-                          void* ws, size_t ws_bytes, void* stream);
+                          void* state, void* ws, size_t ws_bytes, void* stream);
 
 /* ---- serving in 8 bits: paged cache of keys and values -----------------------------------------
  * A cache is n_pages pages of page_tokens tokens.  Codes are [n_pages][n_kv_heads][page_tokens][head_dim]

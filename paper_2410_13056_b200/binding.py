@@ -160,7 +160,7 @@ def lib():
         w8 = ctypes.POINTER(Weight8)
         L.cmpq_norm_quantize_tokens.argtypes = [vp, ci, i64, i64, i64, vp, f32, vp, i64, vp, vp, vp]
         L.cmpq_linear_i8_fused.argtypes = [vp, ci, i64, i64, i64, vp, f32, w8, i64, ci, vp, i64, vp, i64, vp, vp, sz, vp]
-        L.cmpq_gated_i8.argtypes = [vp, ci, i64, i64, i64, vp, f32, w8, w8, w8, i64, i64, ci, vp, i64, vp, i64, vp, vp, sz, vp]
+        L.cmpq_gated_i8.argtypes = [vp, ci, i64, i64, i64, vp, f32, w8, w8, w8, i64, i64, ci, vp, i64, vp, i64, vp, vp, vp, sz, vp]
         L.cmpq_gated_i8_ws_bytes.argtypes = [i64, i64, i64, i64]
         L.cmpq_gated_i8_ws_bytes.restype = sz
         for name in ("cmpq_norm_quantize_tokens", "cmpq_linear_i8_fused", "cmpq_gated_i8"):
@@ -590,12 +590,15 @@ def cmpq_gated_i8_ws_bytes(n, d_in, d_ff, d_out):
     return int(lib().cmpq_gated_i8_ws_bytes(n, d_in, d_ff, d_out))
 
 
-def cmpq_gated_i8(X, gate, up, down, d_ff, d_out, y, ws, norm=None, eps=1e-6, act="silu", residual=None, word=None):
-    """y = the gated block of norm(X), plus residual; gate, up, down: Weight8.  ws: see the header, its first bytes are 0."""
+GATED_STATE_BYTES = 256
+
+
+def cmpq_gated_i8(X, gate, up, down, d_ff, d_out, y, state, ws, norm=None, eps=1e-6, act="silu", residual=None, word=None):
+    """y = the gated block of norm(X), plus residual; gate, up, down: Weight8.  state: GATED_STATE_BYTES bytes that are 0."""
     n, d_in = X.shape
     _check(lib().cmpq_gated_i8(_at(X), _code(X), n, d_in, _rows(X, d_in, "X"), _at(norm), eps, gate, up, down, d_ff, d_out, ACTS[act],
-                               *_residual(residual, n, d_out, X), _at(y), _rows(y, d_out, "y"), _at(word), _at(ws), ws.numel(), _on(X)),
-           "cmpq_gated_i8")
+                               *_residual(residual, n, d_out, X), _at(y), _rows(y, d_out, "y"), _at(word), _at(state), _at(ws), ws.numel(),
+                               _on(X)), "cmpq_gated_i8")
 
 
 def cmpq_check_cache(word):

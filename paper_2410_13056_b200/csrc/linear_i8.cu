@@ -1,14 +1,10 @@
 // 8-bit linear layers: quantization of tokens and the integer product with scales per token and channel.
 #include <algorithm>
-#include <cfloat>
 
-#include "epilogue.cuh"
-#include "linear_i8.cuh"
+#include "product_i8.cuh"
 #include "walk.cuh"
 
 namespace cmpq {
-
-constexpr int kQtThreads = 256;
 
 // The larger magnitudes of two packed pairs, entry by entry; a NaN stays.
 template <int DT>
@@ -92,110 +88,18 @@ quantize_tokens_kernel(const uint16_t* __restrict__ X, int64_t d, int64_t ldx, i
         *reinterpret_cast<uint2*>(out + 8 * g) = group_codes<DT>(load8(row + 8 * g, d - 8 * g, wide), inv);
 }
 
-// Largest of the block's `m` and total of its `s`, the same bits in every thread.
-__device__ __forceinline__ void block_max_sum(uint32_t& m, float& s, uint32_t* part_m, float* part_s) {
-    m = __reduce_max_sync(0xffffffffu, m);
-#pragma unroll
-    for (int i = 16; i; i >>= 1) s += __shfl_xor_sync(0xffffffffu, s, i);
-    if ((threadIdx.x & 31) == 0) part_m[threadIdx.x >> 5] = m, part_s[threadIdx.x >> 5] = s;
-    __syncthreads();
-    s = 0.0f;
-#pragma unroll
-    for (int i = 0; i < kQtThreads / 32; ++i) m = max(m, part_m[i]), s += part_s[i];
-}
-
-// The squares of eight entries times f, added up as a tree: a row of 16384 entries goes through at most 8 + 3 + 5 + 8
-// additions one after the other.
-__device__ __forceinline__ float sum_squares(const float (&x)[8], float f) {
-    float q[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) q[i] = x[i] * f * (x[i] * f);
-    return ((q[0] + q[1]) + (q[2] + q[3])) + ((q[4] + q[5]) + (q[6] + q[7]));
-}
-
-// The same with a root-mean-square norm in front.  A row's codes do not depend on its norm: code = rint(v 127 / max|v|) with
-// v = x g, whatever v is divided by; the norm enters the scale alone.  So nothing waits for the sum of squares, and the
-// codes are as exact as without a norm.  v is one fp32 product, so magnitudes are compared in fp32 here.  A sum that passes
-// fp32 (entries above 2^54 or so) is taken again of entries times 2^-80; entries that vanish there vanish beside it too.
+// The same behind a norm.
 template <int DT, int KEEP>
 __global__ void __launch_bounds__(kQtThreads)
-norm_quantize_kernel(const uint16_t* __restrict__ X, int64_t d, int64_t ldx, int wide, const uint16_t* __restrict__ norm, int wide_norm, float eps,
-                     int8_t* __restrict__ codes, int64_t ldc, float* __restrict__ scale, int32_t* __restrict__ nonfinite, int32_t* __restrict__ clear) {
+norm_quantize_kernel(const uint16_t* __restrict__ X, int64_t d, int64_t ldx, int wide, RowNorm norm, int8_t* __restrict__ codes, int64_t ldc,
+                     float* __restrict__ scale, int32_t* __restrict__ nonfinite, int32_t* __restrict__ clear) {
     tc5::dependents_may_start();
+    __shared__ RowParts parts;
+    if (threadIdx.x == 0 && clear && blockIdx.x == 0) *clear = 0;  // see the other kernel
     const uint16_t* row = X + blockIdx.x * ldx;
-    int8_t* out = codes + blockIdx.x * ldc;
-    const int t = threadIdx.x;
-    const int64_t groups = (d + 15) / 16 * 2;
-    uint4 keep[KEEP];
-#pragma unroll
-    for (int i = 0; i < KEEP; ++i) {
-        const int64_t g = t + (int64_t)i * kQtThreads;
-        keep[i] = make_uint4(0u, 0u, 0u, 0u);
-        if (g < groups) keep[i] = load8(row + 8 * g, d - 8 * g, wide);
-    }
-    uint32_t m = 0;
-    float sum = 0.0f;
-    auto look = [&](uint4 raw, int64_t g) {
-        float x[8], w[8];
-        widen8<DT>(raw, x);
-        widen8<DT>(load8(norm + 8 * g, d - 8 * g, wide_norm), w);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) m = max(m, __float_as_uint(x[j] * w[j]) & 0x7fffffffu);  // as bit patterns: NaN above infinity
-        sum += sum_squares(x, 1.0f);
-    };
-#pragma unroll
-    for (int i = 0; i < KEEP; ++i) {
-        const int64_t g = t + (int64_t)i * kQtThreads;
-        if (g < groups) look(keep[i], g);
-    }
-    for (int64_t g = t + (int64_t)KEEP * kQtThreads; g < groups; g += kQtThreads) look(load8(row + 8 * g, d - 8 * g, wide), g);
-    __shared__ uint32_t part_m[kQtThreads / 32];
-    __shared__ float part_s[kQtThreads / 32];
-    block_max_sum(m, sum, part_m, part_s);
-    const float amax = __uint_as_float(m);
-    float s = amax * (1.0f / 127.0f), inv = 1.0f / s;
-    if (amax < 0x1p-120f) s = inv = 0.0f;
-    auto store = [&](uint4 raw, int64_t g) {
-        float x[8], w[8];
-        widen8<DT>(raw, x);
-        widen8<DT>(load8(norm + 8 * g, d - 8 * g, wide_norm), w);
-        uint32_t c[4];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const float a = x[2 * j] * w[2 * j] * inv + 12582912.0f, b = x[2 * j + 1] * w[2 * j + 1] * inv + 12582912.0f;  // see group_codes
-            c[j] = __byte_perm(__float_as_uint(a), __float_as_uint(b), 0x0040);
-        }
-        *reinterpret_cast<uint2*>(out + 8 * g) = make_uint2(__byte_perm(c[0], c[1], 0x5410), __byte_perm(c[2], c[3], 0x5410));
-    };
-#pragma unroll
-    for (int i = 0; i < KEEP; ++i) {
-        const int64_t g = t + (int64_t)i * kQtThreads;
-        if (g < groups) store(keep[i], g);
-    }
-    for (int64_t g = t + (int64_t)KEEP * kQtThreads; g < groups; g += kQtThreads) store(load8(row + 8 * g, d - 8 * g, wide), g);
-    float f = 1.0f;
-    if (sum > FLT_MAX && m < 0x7f800000u) {  // the same in all threads; not a row with a NaN
-        f = 0x1p-80f, sum = 0.0f;
-#pragma unroll
-        for (int i = 0; i < KEEP; ++i) {
-            float x[8];
-            widen8<DT>(keep[i], x);
-            sum += sum_squares(x, f);
-        }
-        for (int64_t g = t + (int64_t)KEEP * kQtThreads; g < groups; g += kQtThreads) {
-            float x[8];
-            widen8<DT>(load8(row + 8 * g, d - 8 * g, wide), x);
-            sum += sum_squares(x, f);
-        }
-        __syncthreads();  // the parts have been read
-        block_max_sum(m, sum, part_m, part_s);
-    }
-    if (t == 0) {
-        if (s > 0.0f) s *= f / sqrtf(sum / (float)d + eps * f * f);
-        scale[blockIdx.x] = s;
-        if (clear && blockIdx.x == 0) *clear = 0;  // see the other kernel
-        if (m >= 0x7f800000u && nonfinite) atomicOr(nonfinite, 1);
-    }
+    RowHeld<KEEP, true> held;
+    held.load(row, d, wide, norm, threadIdx.x);
+    quantize_row<DT>(held, row, d, wide, norm, codes + blockIdx.x * ldc, scale + blockIdx.x, nonfinite, threadIdx.x, parts, [] { __syncthreads(); });
 }
 
 // ---- the product --------------------------------------------------------------------------------------------
@@ -205,144 +109,9 @@ norm_quantize_kernel(const uint16_t* __restrict__ X, int64_t d, int64_t ldx, int
 // biases come from shared memory.  Codes of both sides are K-major as they lie in memory; 128 bytes of the sum are one
 // swizzled TMA box and four instructions of K = 32.
 
-struct ProductArgs {
-    const float *xs, *ws, *us;         // us, ubias: of the second projection of a gated product
-    const uint16_t *bias, *ubias;
-    uint16_t* y;
-    int64_t ldy;
-    const uint16_t* residual;          // or null
-    int64_t ldr;
-    int act, wide_residual;
-    int n, d_out, kblocks;  // kblocks: 128-byte blocks of the sum
-    int64_t cols;           // rows of weights: d_out, or twice that
-    int wide;               // y takes 16-byte stores
-    int n_tiles, m_tiles;   // tiles of channels, of tokens
-    int stages, bn, rows;   // tile kernel: stages, channels of a tile, token rows that a box brings
-    int32_t* failed;
-};
-
 constexpr int kMmThreads = 320;  // a warp for the loads, one for the products, eight for the epilogue
 constexpr int kMmMaxStages = 40;
 constexpr size_t kTileSmem = 208 << 10;
-
-// Columns [c0, c1) of a warp's 32 accumulator rows: fl16(fl(fl(sum * xs) * ws) + bias) into y + column, of which `left`
-// exist.  c0 and c1 are multiples of 16; scale_bias holds (ws, bias) of the tile's columns.
-template <int DT>
-__device__ __forceinline__ void store_rows(uint32_t tmem, int c0, int c1, const float2* scale_bias, bool has_bias, float xs, bool real,
-                                           uint16_t* y, int left, bool wide) {
-    for (int c = c0; c < c1; c += 16) {
-        uint32_t r[16], w[8];
-        tc5::tmem_ld16(tmem + c, r);
-        tc5::tmem_ld_wait();
-#pragma unroll
-        for (int j = 0; j < 16; j += 2) {
-            const float4 sb = *reinterpret_cast<const float4*>(scale_bias + c + j);
-            float a = (float)(int)r[j] * xs * sb.x, b = (float)(int)r[j + 1] * xs * sb.z;
-            if (has_bias) a += sb.y, b += sb.w;
-            w[j / 2] = round16x2<DT>(a, b);
-        }
-        if (!real) continue;
-        if (wide && c + 16 <= left) {
-            *reinterpret_cast<uint4*>(y + c) = make_uint4(w[0], w[1], w[2], w[3]);
-            *reinterpret_cast<uint4*>(y + c + 8) = make_uint4(w[4], w[5], w[6], w[7]);
-        } else {
-#pragma unroll
-            for (int j = 0; j < 16; ++j)
-                if (c + j < left) y[c + j] = (uint16_t)(w[j >> 1] >> (16 * (j & 1)));
-        }
-    }
-}
-
-// Sixteen 16-bit entries of a row, of which `left` exist, as floats.
-template <int DT>
-__device__ __forceinline__ void load16(const uint16_t* p, int left, bool wide, float (&f)[16]) {
-    float a[8], b[8];
-    widen8<DT>(load8(p, left, wide), a);
-    widen8<DT>(load8(p + 8, left - 8, wide), b);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) f[i] = a[i], f[i + 8] = b[i];
-}
-
-// The same with fl16(act(...) + residual).  y may be the residual: a thread reads its sixteen entries before it writes them.
-template <int DT>
-__device__ __forceinline__ void store_finished(uint32_t tmem, int c0, int c1, const float2* scale_bias, const ProductArgs& A, float xs, bool real,
-                                               uint16_t* y, const uint16_t* residual, int left) {
-    with_act(A.act, [&](auto act) {
-        for (int c = c0; c < c1; c += 16) {
-            uint32_t r[16], w[8];
-            float f[16];
-            tc5::tmem_ld16(tmem + c, r);
-            if (A.residual && real) load16<DT>(residual + c, left - c, A.wide_residual, f);
-            tc5::tmem_ld_wait();
-#pragma unroll
-            for (int j = 0; j < 16; j += 2) {
-                const float4 sb = *reinterpret_cast<const float4*>(scale_bias + c + j);
-                float a = (float)(int)r[j] * xs * sb.x, b = (float)(int)r[j + 1] * xs * sb.z;
-                if (A.bias) a += sb.y, b += sb.w;
-                a = activate<decltype(act)::value>(a), b = activate<decltype(act)::value>(b);
-                if (A.residual) a += f[j], b += f[j + 1];
-                w[j / 2] = round16x2<DT>(a, b);
-            }
-            if (!real) continue;
-            if (A.wide && c + 16 <= left) {
-                *reinterpret_cast<uint4*>(y + c) = make_uint4(w[0], w[1], w[2], w[3]);
-                *reinterpret_cast<uint4*>(y + c + 8) = make_uint4(w[4], w[5], w[6], w[7]);
-            } else {
-#pragma unroll
-                for (int j = 0; j < 16; ++j)
-                    if (c + j < left) y[c + j] = (uint16_t)(w[j >> 1] >> (16 * (j & 1)));
-            }
-        }
-    });
-}
-
-// Columns [c0, c1), multiples of 8, of a gated product: the accumulator's and scale_bias's first `half` columns are the gate,
-// the others the second projection; y = fl16(act(gate) * second), rows of y on 16 bytes.
-template <int DT>
-__device__ __forceinline__ void store_gated(uint32_t tmem, int c0, int c1, int half, const float2* scale_bias, const ProductArgs& A, float xs, bool real,
-                                            uint16_t* y, int left) {
-    with_act(A.act, [&](auto act) {
-        for (int c = c0; c < c1; c += 8) {
-            uint32_t g[8], u[8], w[4];
-            tc5::tmem_ld8(tmem + c, g);
-            tc5::tmem_ld8(tmem + half + c, u);
-            tc5::tmem_ld_wait();
-#pragma unroll
-            for (int j = 0; j < 8; j += 2) {
-                const float4 gs = *reinterpret_cast<const float4*>(scale_bias + c + j), us = *reinterpret_cast<const float4*>(scale_bias + half + c + j);
-                float g0 = (float)(int)g[j] * xs * gs.x, g1 = (float)(int)g[j + 1] * xs * gs.z;
-                float u0 = (float)(int)u[j] * xs * us.x, u1 = (float)(int)u[j + 1] * xs * us.z;
-                if (A.bias) g0 += gs.y, g1 += gs.w;
-                if (A.ubias) u0 += us.y, u1 += us.w;
-                w[j / 2] = round16x2<DT>(activate<decltype(act)::value>(g0) * u0, activate<decltype(act)::value>(g1) * u1);
-            }
-            if (!real) continue;
-            if (c + 8 <= left) {
-                *reinterpret_cast<uint4*>(y + c) = make_uint4(w[0], w[1], w[2], w[3]);
-            } else {
-#pragma unroll
-                for (int j = 0; j < 8; ++j)
-                    if (c + j < left) y[c + j] = (uint16_t)(w[j >> 1] >> (16 * (j & 1)));
-            }
-        }
-    });
-}
-
-// Scale and bias of column i of a tile whose channels begin at o0: of a gated tile the first half's, then the second's.
-template <int DT, int KIND>
-__device__ __forceinline__ float2 column_scale(const ProductArgs& A, int o0, int i, int columns) {
-    const bool second = KIND == kGated && i >= columns / 2;
-    const int o = min(o0 + (second ? i - columns / 2 : i), A.d_out - 1);
-    const uint16_t* bias = second ? A.ubias : A.bias;
-    return make_float2(__ldg((second ? A.us : A.ws) + o), bias ? widen16<DT>(bias[o]) : 0.0f);
-}
-
-// A thread's columns [c0, c1) of the residual, on their way into L2 while the products run.
-__device__ __forceinline__ void ask_for(const uint16_t* row, int c0, int c1) {
-    const uintptr_t end = reinterpret_cast<uintptr_t>(row + c1);
-    for (uintptr_t p = reinterpret_cast<uintptr_t>(row + c0) & ~(uintptr_t)127; c0 < c1 && p < end; p += 128)
-        asm volatile("prefetch.global.L2 [%0];" ::"l"(p));
-}
 
 // Few tiles: a block takes 128 tokens (all of them, mostly) and `bn` channels, a multiple of 16 chosen so that the
 // blocks fill the SMs; the weights pass through once and are the time while tokens are few.  Launched behind the
@@ -368,7 +137,7 @@ matmul_i8_tile_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_con
     __shared__ int failed;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int nt = blockIdx.x / A.m_tiles, mt = blockIdx.x % A.m_tiles, bn = A.bn;
-    const int a_bytes = A.rows * 128, stage = a_bytes + bn * 128, columns = bn <= 32 ? 32 : bn <= 64 ? 64 : bn <= 128 ? 128 : 256;
+    const int a_bytes = A.rows * 128, b_bytes = bn * 128, stage = A.per_stage * (a_bytes + b_bytes), columns = bn <= 32 ? 32 : bn <= 64 ? 64 : bn <= 128 ? 128 : 256;
     if (threadIdx.x < A.stages) tc5::mbar_init(full + threadIdx.x, 1), tc5::mbar_init(empty + threadIdx.x, 1);
     if (threadIdx.x == 0) tc5::mbar_init(&done, 1), failed = 0;
     tc5::mbar_init_fence();
@@ -380,15 +149,18 @@ matmul_i8_tile_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_con
     if (warp == 0) {
         if (tc5::elect_one()) {
             int slot = 0, phase = 1;  // a new barrier counts as empty
-            for (int i = 0; i < A.kblocks; ++i) {
+            for (int k = 0; k < A.kblocks; k += A.per_stage) {
                 if (!tc5::mbar_wait(empty + slot, phase, &failed)) break;
-                tc5::mbar_expect_tx(full + slot, stage);  // the tokens' bytes too, whoever comes first
-                uint8_t* at = smem + slot * stage + a_bytes;
-                if (KIND == kGated) {
-                    tc5::tma_load_2d(at, &wmap, full + slot, i * 128, nt * (bn / 2));
-                    tc5::tma_load_2d(at + bn / 2 * 128, &umap, full + slot, i * 128, nt * (bn / 2));
-                } else {
-                    tc5::tma_load_2d(at, &wmap, full + slot, i * 128, nt * bn);
+                const int count = min(A.per_stage, A.kblocks - k);
+                tc5::mbar_expect_tx(full + slot, count * (a_bytes + b_bytes));  // the tokens' bytes too, whoever comes first
+                uint8_t* at = smem + slot * stage + A.per_stage * a_bytes;
+                for (int i = k; i < k + count; ++i, at += b_bytes) {
+                    if (KIND == kGated) {
+                        tc5::tma_load_2d(at, &wmap, full + slot, i * 128, nt * (bn / 2));
+                        tc5::tma_load_2d(at + b_bytes / 2, &umap, full + slot, i * 128, nt * (bn / 2));
+                    } else {
+                        tc5::tma_load_2d(at, &wmap, full + slot, i * 128, nt * bn);
+                    }
                 }
                 if (++slot == A.stages) slot = 0, phase ^= 1;
             }
@@ -397,13 +169,14 @@ matmul_i8_tile_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_con
         if (tc5::elect_one()) {
             const uint32_t idesc = tc5::idesc_i8(128, bn);
             int slot = 0, phase = 0;
-            for (int i = 0; i < A.kblocks; ++i) {
+            for (int k = 0; k < A.kblocks; k += A.per_stage) {
                 if (!tc5::mbar_wait(full + slot, phase, &failed)) break;
                 tc5::fence_after_sync();
                 const uint32_t at = tc5::smem_addr(smem + slot * stage);
-                const uint64_t a = tc5::desc_k_sw128(at), b = tc5::desc_k_sw128(at + a_bytes);
+                uint64_t a = tc5::desc_k_sw128(at), b = tc5::desc_k_sw128(at + A.per_stage * a_bytes);  // in units of 16 bytes
+                for (int i = k; i < min(k + A.per_stage, A.kblocks); ++i, a += a_bytes / 16, b += b_bytes / 16)
 #pragma unroll
-                for (int k = 0; k < 4; ++k) tc5::mma_i8<1>(tmem, a + 2 * k, b + 2 * k, idesc, (i | k) != 0);
+                    for (int j = 0; j < 4; ++j) tc5::mma_i8<1>(tmem, a + 2 * j, b + 2 * j, idesc, (i | j) != 0);
                 tc5::mma_commit(empty + slot);
                 if (++slot == A.stages) slot = 0, phase ^= 1;
             }
@@ -418,9 +191,10 @@ matmul_i8_tile_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_con
         if (warp == 2) {  // the token codes: the first epilogue warp's work until then
             if (tc5::elect_one()) {
                 int slot = 0, phase = 1;
-                for (int k = 0; k < A.kblocks; ++k) {
+                for (int k = 0; k < A.kblocks; k += A.per_stage) {
                     if (!tc5::mbar_wait(empty + slot, phase, &failed)) break;
-                    tc5::tma_load_2d(smem + slot * stage, &xmap, full + slot, k * 128, mt * 128);
+                    for (int i = 0; i < min(A.per_stage, A.kblocks - k); ++i)
+                        tc5::tma_load_2d(smem + slot * stage + i * a_bytes, &xmap, full + slot, (k + i) * 128, mt * 128);
                     if (++slot == A.stages) slot = 0, phase ^= 1;
                 }
             }
@@ -504,7 +278,7 @@ matmul_i8_pair_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_con
             for (int tile = first; ok && tile < tiles; tile += step) {
                 const int mt = tile % A.m_tiles, nt = tile / A.m_tiles;
                 for (int k = 0; k < A.kblocks; ++k) {
-                    if (!(ok = tc5::mbar_wait(empty + slot, phase, &failed))) break;
+                    if (!(ok = tc5::mbar_wait<true>(empty + slot, phase, &failed))) break;
                     if (rank == 0) tc5::mbar_expect_tx(full + slot, 2 * kPairStageBytes);
                     uint8_t* at = smem + slot * kPairStageBytes;
                     tc5::tma_load_2d_pair(at, &xmap, full + slot, k * 128, mt * 256 + rank * 128);
@@ -521,10 +295,10 @@ matmul_i8_pair_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_con
             int slot = 0, phase = 0, acc = 0, acc_phase = 1;
             bool ok = true;
             for (int tile = first; ok && tile < tiles; tile += step) {
-                if (!tc5::mbar_wait(acc_empty + acc, acc_phase, &failed)) break;
+                if (!tc5::mbar_wait<true>(acc_empty + acc, acc_phase, &failed)) break;
                 tc5::fence_after_sync();
                 for (int k = 0; k < A.kblocks; ++k) {
-                    if (!(ok = tc5::mbar_wait(full + slot, phase, &failed))) break;
+                    if (!(ok = tc5::mbar_wait<true>(full + slot, phase, &failed))) break;
                     tc5::fence_after_sync();
                     const uint32_t at = tc5::smem_addr(smem + slot * kPairStageBytes);
                     const uint64_t a = tc5::desc_k_sw128(at), b = tc5::desc_k_sw128(at + 128 * 128);
@@ -553,7 +327,7 @@ matmul_i8_pair_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_con
                     ask_for(A.residual + (int64_t)t * A.ldr + o0, min(upper * 128, A.d_out - o0), min(upper * 128 + 128, A.d_out - o0));
                 asm volatile("bar.sync 1, 256;" ::: "memory");
             },
-            [&](int acc, int parity) { return tc5::mbar_wait_warp(acc_full + acc, parity, &failed); },
+            [&](int acc, int parity) { return tc5::mbar_wait_warp<true>(acc_full + acc, parity, &failed); },
             [&](int tile, int acc) {
                 const int o0 = tile / A.m_tiles * kWide, row0 = tile % A.m_tiles * 256 + rank * 128 + quad * 32, t = row0 + lane;
                 const int left = min(kWide, A.d_out - o0), c0 = upper * (kWide / 2), c1 = c0 + kWide / 2;
@@ -627,8 +401,10 @@ static cmpq_status launch_kind(const TokenCodes& x, int64_t d_in, const Weight8&
     a.m_tiles = (a.n + 127) / 128;
     // one block to an SM: two that share it were slower at every size, their rounds and tails cost more than they hide
     const int64_t blocks = (int64_t)a.m_tiles * a.n_tiles;
-    const size_t stage = (a.rows + a.bn) * 128, slack = (128 - a.rows) * 128 + 1024;
-    a.stages = std::min({(int)((kTileSmem - slack) / stage), kMmMaxStages, a.kblocks});
+    const int block = (a.rows + a.bn) * 128;
+    a.per_stage = std::max(1, std::min((a.n > 32 ? 64 << 10 : 48 << 10) / block, a.kblocks));
+    const size_t stage = a.per_stage * block, slack = (128 - a.rows) * 128 + 1024;
+    a.stages = std::min({(int)((kTileSmem - slack) / stage), kMmMaxStages, (a.kblocks + a.per_stage - 1) / a.per_stage});
     if (!raise_smem_limit_once(matmul_i8_tile_kernel<DT, KIND>, kTileSmem, raised[1])) return CMPQ_ERR_CUDA;
     if (blocks > INT32_MAX) return CMPQ_ERR_UNSUPPORTED;
     return launch_cluster(matmul_i8_tile_kernel<DT, KIND>, (unsigned)blocks, kMmThreads, a.stages * stage + slack, 1, behind, st, wmap, umap, xmap, a);
@@ -664,12 +440,12 @@ cmpq_status enqueue_product(const TokenCodes& x, cmpq_dtype dt, int64_t n, int64
 template <int DT>
 static cmpq_status launch_quantize(const uint16_t* x, int64_t n, int64_t d, int64_t ldx, const uint16_t* norm, float eps, int8_t* codes, int64_t ldc,
                                    float* scale, int32_t* word, int32_t* clear, cudaStream_t st) {
-    const int wide = aligned_to(x, 16) && ldx % 8 == 0, wide_norm = aligned_to(norm, 16);
+    const int wide = aligned_to(x, 16) && ldx % 8 == 0;
     const int64_t keep = (d + 8 * kQtThreads - 1) / (8 * kQtThreads);
     const unsigned rows = (unsigned)n;
     auto plain = [&](auto kernel) { return launch_cluster(kernel, rows, kQtThreads, 0, 1, false, st, x, d, ldx, wide, codes, ldc, scale, word, clear); };
     auto normed = [&](auto kernel) {
-        return launch_cluster(kernel, rows, kQtThreads, 0, 1, false, st, x, d, ldx, wide, norm, wide_norm, eps, codes, ldc, scale, word, clear);
+        return launch_cluster(kernel, rows, kQtThreads, 0, 1, false, st, x, d, ldx, wide, RowNorm{norm, aligned_to(norm, 16), eps}, codes, ldc, scale, word, clear);
     };
     if (norm)
         return keep <= 2   ? normed(norm_quantize_kernel<DT, 2>)

@@ -1,0 +1,270 @@
+// Device side of the 8-bit linear layers and the gated block: a row's quantization, what a product does with its sums.
+#pragma once
+
+#include <cfloat>
+
+#include "epilogue.cuh"
+#include "linear_i8.cuh"
+
+namespace cmpq {
+
+constexpr int kQtThreads = 256;
+
+struct RowParts {  // in shared memory
+    uint32_t m[kQtThreads / 32];
+    float s[kQtThreads / 32];
+};
+
+// Largest of the threads' `m` and total of their `s`, the same bits in each of them.
+template <class Sync>
+__device__ __forceinline__ void all_max_sum(uint32_t& m, float& s, int t, RowParts& parts, Sync sync) {
+    m = __reduce_max_sync(0xffffffffu, m);
+#pragma unroll
+    for (int i = 16; i; i >>= 1) s += __shfl_xor_sync(0xffffffffu, s, i);
+    if ((t & 31) == 0) parts.m[t >> 5] = m, parts.s[t >> 5] = s;
+    sync();
+    s = 0.0f;
+#pragma unroll
+    for (int i = 0; i < kQtThreads / 32; ++i) m = max(m, parts.m[i]), s += parts.s[i];
+}
+
+// The squares of eight entries times f, added up as a tree: a row of 16384 entries goes through at most 8 + 3 + 5 + 8
+// additions one after the other.
+__device__ __forceinline__ float sum_squares(const float (&x)[8], float f) {
+    float q[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) q[i] = x[i] * f * (x[i] * f);
+    return ((q[0] + q[1]) + (q[2] + q[3])) + ((q[4] + q[5]) + (q[6] + q[7]));
+}
+
+struct RowNorm {
+    const uint16_t* weight;  // or null
+    int wide;                // 16-byte aligned
+    float eps;
+};
+
+// What a thread keeps of a row and of its norm's weight: KEEP groups of eight, asked for all at once.
+template <int KEEP, bool NORM>
+struct RowHeld {
+    uint4 x[KEEP], w[NORM ? KEEP : 1];
+
+    __device__ __forceinline__ void load(const uint16_t* row, int64_t d, bool wide, const RowNorm& norm, int t) {
+#pragma unroll
+        for (int i = 0; i < KEEP; ++i) {
+            const int64_t g = t + (int64_t)i * kQtThreads;
+            x[i] = make_uint4(0u, 0u, 0u, 0u);
+            if (NORM) w[i] = x[i];
+            if (8 * g < d) x[i] = load8(row + 8 * g, d - 8 * g, wide);
+            if (NORM && 8 * g < d) w[i] = load8(norm.weight + 8 * g, d - 8 * g, norm.wide);
+        }
+    }
+};
+
+// Codes of eight values: |v * inv| is at most 127 (1 + 2^-22), so adding 1.5 * 2^23 leaves the integer that rounding to even
+// gives in the sum's low byte, in two's complement: one addition instead of a conversion, which has a quarter of its rate.
+__device__ __forceinline__ uint2 round_codes(const float (&v)[8], float inv) {
+    uint32_t c[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const float a = v[2 * j] * inv + 12582912.0f, b = v[2 * j + 1] * inv + 12582912.0f;  // two roundings each: -fmad=false
+        c[j] = __byte_perm(__float_as_uint(a), __float_as_uint(b), 0x0040);
+    }
+    return make_uint2(__byte_perm(c[0], c[1], 0x5410), __byte_perm(c[2], c[3], 0x5410));
+}
+
+// Scale of a row whose largest magnitude is given, and what its values are multiplied with.
+__device__ __forceinline__ float2 scale_of(float amax) {
+    const float s = amax * (1.0f / 127.0f);
+    return amax < 0x1p-120f ? make_float2(0.0f, 0.0f) : make_float2(s, 1.0f / s);
+}
+
+// Codes and scale of a row by 256 threads (t is a thread's number, sync() their barrier), behind a root-mean-square norm where
+// NORM.  A row's codes do not depend on its norm: code = rint(v 127 / max|v|) with v = x g, whatever v is divided by; the norm
+// enters the scale alone.  So nothing waits for the sum of squares, and the codes are as exact as without a norm.  v is one
+// fp32 product, so magnitudes are compared in fp32 here.  A sum that passes fp32 (entries above 2^54 or so) is taken again of
+// entries times 2^-80; entries that vanish there vanish beside it too.  What is not held is read again.
+template <int DT, int KEEP, bool NORM, class Sync>
+__device__ __forceinline__ void quantize_row(const RowHeld<KEEP, NORM>& held, const uint16_t* row, int64_t d, bool wide, const RowNorm& norm, int8_t* out,
+                                             float* scale, int32_t* nonfinite, int t, RowParts& parts, Sync sync) {
+    const int64_t groups = (d + 15) / 16 * 2;  // the codes' padding up to 16 is written too
+    auto load = [&](const uint16_t* p, int64_t g, bool on_16) { return load8(p + 8 * g, d - 8 * g, on_16); };
+    // f(group, its entries, v) for the thread's groups
+    auto every = [&](auto f) {
+        float x[8], v[8];
+        auto one = [&](int64_t g, uint4 rx, uint4 rw) {
+            widen8<DT>(rx, x);
+            if (NORM) widen8<DT>(rw, v);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] = NORM ? x[j] * v[j] : x[j];
+            f(g, x, v);
+        };
+#pragma unroll
+        for (int i = 0; i < KEEP; ++i) {
+            const int64_t g = t + (int64_t)i * kQtThreads;
+            if (g < groups) one(g, held.x[i], held.w[NORM ? i : 0]);
+        }
+        for (int64_t g = t + (int64_t)KEEP * kQtThreads; g < groups; g += kQtThreads)
+            one(g, load(row, g, wide), NORM ? load(norm.weight, g, norm.wide) : make_uint4(0u, 0u, 0u, 0u));
+    };
+    uint32_t m = 0;
+    float sum = 0.0f;
+    every([&](int64_t, const float(&x)[8], const float(&v)[8]) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) m = max(m, __float_as_uint(v[j]) & 0x7fffffffu);  // as bit patterns: NaN above infinity
+        if (NORM) sum += sum_squares(x, 1.0f);
+    });
+    all_max_sum(m, sum, t, parts, sync);
+    float2 s = scale_of(__uint_as_float(m));
+    every([&](int64_t g, const float(&)[8], const float(&v)[8]) { *reinterpret_cast<uint2*>(out + 8 * g) = round_codes(v, s.y); });
+    float f = 1.0f;
+    if (NORM && sum > FLT_MAX && m < 0x7f800000u) {  // the same in all threads; not a row with a NaN
+        f = 0x1p-80f, sum = 0.0f;
+        every([&](int64_t, const float(&x)[8], const float(&)[8]) { sum += sum_squares(x, f); });
+        sync();  // the parts have been read
+        all_max_sum(m, sum, t, parts, sync);
+    }
+    if (t == 0) {
+        if (NORM && s.x > 0.0f) s.x *= f / sqrtf(sum / (float)d + norm.eps * f * f);
+        *scale = s.x;
+        if (m >= 0x7f800000u && nonfinite) atomicOr(nonfinite, 1);
+    }
+}
+
+// ---- products ----
+
+struct ProductArgs {
+    const float *xs, *ws, *us;         // us, ubias: of the second projection of a gated product
+    const uint16_t *bias, *ubias;
+    uint16_t* y;
+    int64_t ldy;
+    const uint16_t* residual;          // or null
+    int64_t ldr;
+    int act, wide_residual;
+    int n, d_out, kblocks;  // kblocks: 128-byte blocks of the sum
+    int64_t cols;           // rows of weights: d_out, or twice that
+    int wide;               // y takes 16-byte stores
+    int n_tiles, m_tiles;   // tiles of channels, of tokens
+    int stages, per_stage, bn, rows;  // tile kernel: stages, blocks of the sum in each, columns of a tile, token rows that a box brings
+    int32_t* failed;
+};
+
+// Columns [c0, c1) of a warp's 32 accumulator rows: fl16(fl(fl(sum * xs) * ws) + bias) into y + column, of which `left`
+// exist.  c0 and c1 are multiples of 16; scale_bias holds (ws, bias) of the tile's columns.
+template <int DT>
+__device__ __forceinline__ void store_rows(uint32_t tmem, int c0, int c1, const float2* scale_bias, bool has_bias, float xs, bool real,
+                                           uint16_t* y, int left, bool wide) {
+    for (int c = c0; c < c1; c += 16) {
+        uint32_t r[16], w[8];
+        tc5::tmem_ld16(tmem + c, r);
+        tc5::tmem_ld_wait();
+#pragma unroll
+        for (int j = 0; j < 16; j += 2) {
+            const float4 sb = *reinterpret_cast<const float4*>(scale_bias + c + j);
+            float a = (float)(int)r[j] * xs * sb.x, b = (float)(int)r[j + 1] * xs * sb.z;
+            if (has_bias) a += sb.y, b += sb.w;
+            w[j / 2] = round16x2<DT>(a, b);
+        }
+        if (!real) continue;
+        if (wide && c + 16 <= left) {
+            *reinterpret_cast<uint4*>(y + c) = make_uint4(w[0], w[1], w[2], w[3]);
+            *reinterpret_cast<uint4*>(y + c + 8) = make_uint4(w[4], w[5], w[6], w[7]);
+        } else {
+#pragma unroll
+            for (int j = 0; j < 16; ++j)
+                if (c + j < left) y[c + j] = (uint16_t)(w[j >> 1] >> (16 * (j & 1)));
+        }
+    }
+}
+
+// Sixteen 16-bit entries of a row, of which `left` exist, as floats.
+template <int DT>
+__device__ __forceinline__ void load16(const uint16_t* p, int left, bool wide, float (&f)[16]) {
+    float a[8], b[8];
+    widen8<DT>(load8(p, left, wide), a);
+    widen8<DT>(load8(p + 8, left - 8, wide), b);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) f[i] = a[i], f[i + 8] = b[i];
+}
+
+// The same with fl16(act(...) + residual).  y may be the residual: a thread reads its sixteen entries before it writes them.
+template <int DT>
+__device__ __forceinline__ void store_finished(uint32_t tmem, int c0, int c1, const float2* scale_bias, const ProductArgs& A, float xs, bool real,
+                                               uint16_t* y, const uint16_t* residual, int left) {
+    with_act(A.act, [&](auto act) {
+        for (int c = c0; c < c1; c += 16) {
+            uint32_t r[16], w[8];
+            float f[16];
+            tc5::tmem_ld16(tmem + c, r);
+            if (A.residual && real) load16<DT>(residual + c, left - c, A.wide_residual, f);
+            tc5::tmem_ld_wait();
+#pragma unroll
+            for (int j = 0; j < 16; j += 2) {
+                const float4 sb = *reinterpret_cast<const float4*>(scale_bias + c + j);
+                float a = (float)(int)r[j] * xs * sb.x, b = (float)(int)r[j + 1] * xs * sb.z;
+                if (A.bias) a += sb.y, b += sb.w;
+                a = activate<decltype(act)::value>(a), b = activate<decltype(act)::value>(b);
+                if (A.residual) a += f[j], b += f[j + 1];
+                w[j / 2] = round16x2<DT>(a, b);
+            }
+            if (!real) continue;
+            if (A.wide && c + 16 <= left) {
+                *reinterpret_cast<uint4*>(y + c) = make_uint4(w[0], w[1], w[2], w[3]);
+                *reinterpret_cast<uint4*>(y + c + 8) = make_uint4(w[4], w[5], w[6], w[7]);
+            } else {
+#pragma unroll
+                for (int j = 0; j < 16; ++j)
+                    if (c + j < left) y[c + j] = (uint16_t)(w[j >> 1] >> (16 * (j & 1)));
+            }
+        }
+    });
+}
+
+// Columns [c0, c1), multiples of 8, of a gated product: the accumulator's and scale_bias's first `half` columns are the gate,
+// the others the second projection; y = fl16(act(gate) * second), rows of y on 16 bytes.
+template <int DT>
+__device__ __forceinline__ void store_gated(uint32_t tmem, int c0, int c1, int half, const float2* scale_bias, const ProductArgs& A, float xs, bool real,
+                                            uint16_t* y, int left) {
+    with_act(A.act, [&](auto act) {
+        for (int c = c0; c < c1; c += 8) {
+            uint32_t g[8], u[8], w[4];
+            tc5::tmem_ld8(tmem + c, g);
+            tc5::tmem_ld8(tmem + half + c, u);
+            tc5::tmem_ld_wait();
+#pragma unroll
+            for (int j = 0; j < 8; j += 2) {
+                const float4 gs = *reinterpret_cast<const float4*>(scale_bias + c + j), us = *reinterpret_cast<const float4*>(scale_bias + half + c + j);
+                float g0 = (float)(int)g[j] * xs * gs.x, g1 = (float)(int)g[j + 1] * xs * gs.z;
+                float u0 = (float)(int)u[j] * xs * us.x, u1 = (float)(int)u[j + 1] * xs * us.z;
+                if (A.bias) g0 += gs.y, g1 += gs.w;
+                if (A.ubias) u0 += us.y, u1 += us.w;
+                w[j / 2] = round16x2<DT>(activate<decltype(act)::value>(g0) * u0, activate<decltype(act)::value>(g1) * u1);
+            }
+            if (!real) continue;
+            if (c + 8 <= left) {
+                *reinterpret_cast<uint4*>(y + c) = make_uint4(w[0], w[1], w[2], w[3]);
+            } else {
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    if (c + j < left) y[c + j] = (uint16_t)(w[j >> 1] >> (16 * (j & 1)));
+            }
+        }
+    });
+}
+
+// Scale and bias of column i of a tile whose channels begin at o0: of a gated tile the first half's, then the second's.
+template <int DT, int KIND>
+__device__ __forceinline__ float2 column_scale(const ProductArgs& A, int o0, int i, int columns) {
+    const bool second = KIND == kGated && i >= columns / 2;
+    const int o = min(o0 + (second ? i - columns / 2 : i), A.d_out - 1);
+    const uint16_t* bias = second ? A.ubias : A.bias;
+    return make_float2(__ldg((second ? A.us : A.ws) + o), bias ? widen16<DT>(bias[o]) : 0.0f);
+}
+
+// A thread's columns [c0, c1) of the residual, on their way into L2 while the products run.
+__device__ __forceinline__ void ask_for(const uint16_t* row, int c0, int c1) {
+    const uintptr_t end = reinterpret_cast<uintptr_t>(row + c1);
+    for (uintptr_t p = reinterpret_cast<uintptr_t>(row + c0) & ~(uintptr_t)127; c0 < c1 && p < end; p += 128)
+        asm volatile("prefetch.global.L2 [%0];" ::"l"(p));
+}
+
+}  // namespace cmpq

@@ -97,7 +97,11 @@ Spaces& attention_spaces() {
     return *s;
 }
 Spaces& gated_spaces() {
-    static Spaces* s = new Spaces{CMPQ_GATED_ZEROED, {}};
+    static Spaces* s = new Spaces{0, {}};
+    return *s;
+}
+Spaces& gated_states() {
+    static Spaces* s = new Spaces{CMPQ_GATED_STATE_BYTES, {}};
     return *s;
 }
 
@@ -191,6 +195,11 @@ struct Gated {
     Linear gate, up, down;
     cmpq_act act;
     Tensor word;
+    // States for captured calls, one each, 0 from here on: a node that zeroed it would cost every replay 2 us.  They live as
+    // long as the weights have to; calls beyond them take theirs from the graph, with such a node.
+    static constexpr int64_t kCaptured = 64;
+    Tensor kept;
+    int64_t taken = 0;
 
     Gated(const Linear& g, const Linear& u, const Linear& d, const std::optional<std::string>& activation) : gate(g), up(u), down(d), act(act_of(activation)) {
         beside(u.w, g.w, "up"), beside(d.w, g.w, "down");
@@ -198,6 +207,12 @@ struct Gated {
             refuse("gate [" + std::to_string(g.d_out) + "][" + std::to_string(g.d_in) + "], up [" + std::to_string(u.d_out) + "][" + std::to_string(u.d_in) +
                    "] and down [" + std::to_string(d.d_out) + "][" + std::to_string(d.d_in) + "] do not fit together");
         word = at::zeros({1}, at::TensorOptions().dtype(at::kInt).device(g.w.device()));
+        kept = at::zeros({kCaptured, CMPQ_GATED_STATE_BYTES}, at::TensorOptions().dtype(at::kByte).device(g.w.device()));
+    }
+
+    Tensor state(void* stream) {
+        const bool captured = c10::cuda::currentStreamCaptureStatusMayInitCtx() != c10::cuda::CaptureStatus::None;
+        return captured && taken < kCaptured ? kept[taken++] : gated_states().get(word.device(), stream, CMPQ_GATED_STATE_BYTES);
     }
 
     Tensor call(const Tensor& x, const OptTensor& into, const OptTensor& residual, const OptTensor& norm, double eps) {
@@ -208,16 +223,17 @@ struct Gated {
         if (a.n == 0) return y;
         void* stream = stream_of(x);
         const Tensor ws = gated_spaces().get(x.device(), stream, cmpq_gated_i8_ws_bytes(a.n, gate.d_in, gate.d_out, down.d_out));
+        const Tensor st = state(stream);
         const cmpq_weight_i8 g = gate.weight(), u = up.weight(), d = down.weight();
         check(cmpq_gated_i8(x.data_ptr(), a.dt, a.n, gate.d_in, rows(x, "x"), a.norm, (float)eps, &g, &u, &d, gate.d_out, down.d_out, act, a.residual, a.ldr,
-                            y.data_ptr(), rows(y, "out"), word.data_ptr<int32_t>(), ws.data_ptr(), ws.numel(), stream),
+                            y.data_ptr(), rows(y, "out"), word.data_ptr<int32_t>(), st.data_ptr(), ws.data_ptr(), ws.numel(), stream),
               "cmpq_gated_i8");
         return y;
     }
 
     void look() {
         const cmpq_status s = take_word(word);
-        if (s == CMPQ_ERR_INTERNAL) gated_spaces().drop(word.device());  // see Cache::look
+        if (s == CMPQ_ERR_INTERNAL) gated_states().drop(word.device()), kept.zero_();  // see Cache::look
         check(s, "cmpq_gated_i8");
     }
 };

@@ -73,6 +73,21 @@ def test_norm_quantize_codes_bit_exact(n, d, dtype):
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
+def test_norm_of_rows_whose_squares_pass_float32(dtype):
+    """In one kernel, in the kernels of their own, and beside rows of ordinary size."""
+    d, ff = 1024, 6000
+    block, g = _block(1, d, ff, d, dtype, "silu", False), _norm(d, dtype, 8)
+    x = _tokens(5, d, dtype, 7)
+    want = block(x, norm=g, eps=2.0 ** -60)
+    if dtype == torch.bfloat16:                            # powers of two that the norm takes out again
+        for row, p in ((0, 90), (2, -20), (3, 100)):
+            x[row] = (x[row].float() * 2.0 ** p).to(dtype)
+    for n in (5, 4):
+        assert torch.equal(block(x[:n], norm=g, eps=2.0 ** -60), want[:n])
+    block.check()
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
 def test_norm_quantize_strides_and_extremes(dtype):
     big, gs = _tokens(6, 107, dtype, 5), _norm(108, dtype, 6)
     for view, g in ((big[:, 3:104], gs[1:102]), (big[::2, 1:], gs[2:]), (big[1:, :96], gs[:96]), (big[:, 8:104], gs[3:99])):
@@ -167,17 +182,23 @@ GATED = [(1, 1, 1, 1), (1, 16, 8, 16), (1, 512, 1408, 512), (2, 100, 37, 33), (3
          (129, 255, 257, 300), (300, 384, 1000, 520), (513, 200, 640, 200), (1500, 130, 1100, 260)]
 
 
+# one kernel does all of these: large layers, a few tokens; long and short sums, many tiles and parts for a block, sizes that
+# fill nothing
+FEW = [(1, 2050, 5461, 2049), (2, 4096, 2001, 4097), (3, 130, 80000, 65), (4, 12800, 700, 300), (1, 64, 131072, 64), (4, 8, 1000, 20000), (2, 16, 64, 262144),
+       (4, 1024, 6000, 1024), (3, 8192, 1000, 8192), (1, 1536, 4096, 1536), (4, 13000, 700, 300)]
+
+
 def _block(n, d_in, d_ff, d_out, dtype, act, bias):
     gate, up = (_weights(d_ff, d_in, dtype, s, bias, pad=16 * (n % 2)) for s in (1, 2))
     return serving.GatedMLP8(gate, up, _weights(d_out, d_ff, dtype, 3, bias), act)
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
-@pytest.mark.parametrize("n,d_in,d_ff,d_out", GATED)
+@pytest.mark.parametrize("n,d_in,d_ff,d_out", GATED + FEW)
 def test_gated_block(n, d_in, d_ff, d_out, dtype):
     x = _tokens(n, d_in, dtype, n + d_in)
     res = _tokens(n + 1, d_out + 3, dtype, 2)
-    for i, act in enumerate(ACTS if n < 500 else ["silu", "gelu"]):
+    for i, act in enumerate(ACTS if n < 500 and (n, d_in, d_ff, d_out) not in FEW else ["silu", "gelu"]):
         block = _block(n, d_in, d_ff, d_out, dtype, act, i % 2 == 1)
         g = _norm(d_in, dtype, 4) if i % 3 != 1 else None
         r = (res[:n, :d_out], None, res[1:, 3:])[i % 3]
@@ -194,16 +215,16 @@ def test_gated_block(n, d_in, d_ff, d_out, dtype):
         block.check()
 
 
+@pytest.mark.parametrize("d,ff", [(384, 1500), (1024, 6000)])
 @pytest.mark.parametrize("dtype", DTYPES)
-def test_a_token_has_the_same_bytes_in_every_batch(dtype):
+def test_a_token_has_the_same_bytes_in_every_batch(dtype, d, ff):
     """Kernels are chosen by the number of tokens; what a token gets does not depend on it."""
-    d, ff = 384, 1500
     block, x, g = _block(1, d, ff, d, dtype, "silu", True), _tokens(600, d, dtype, 1), _norm(d, dtype, 2)
     layer = block.down
     h = _tokens(600, ff, dtype, 3)
     y = block(x, residual=x, norm=g)
     z = layer(h, activation="gelu", residual=x)
-    for n in (1, 2, 7, 8, 9, 32, 64, 65, 128, 129, 300):
+    for n in (1, 2, 3, 4, 5, 8, 9, 32, 64, 65, 128, 129, 300):
         for at in (0, 600 - n):
             part = slice(at, at + n)
             assert torch.equal(block(x[part], residual=x[part], norm=g), y[part]), n
@@ -309,21 +330,25 @@ def test_no_tokens_and_refusals():
 
 
 def test_c_calls_through_the_binding():
-    n, d, ff, dtype = 5, 96, 130, torch.bfloat16
+    n, d, ff, dtype = 4, 1024, 6000, torch.bfloat16
     block, x, g = _block(n, d, ff, d, dtype, "gelu", True), _tokens(n, d, dtype, 1), _norm(d, dtype, 2)
     w = [B.weight8(p.w_codes, p.w_scale, p.bias) for p in (block.gate, block.up, block.down)]
     y, word = torch.empty_like(x), torch.zeros(1, dtype=torch.int32, device="cuda")
     size = B.cmpq_gated_i8_ws_bytes(n, d, ff, d)
+    state = torch.zeros(B.GATED_STATE_BYTES, dtype=torch.uint8, device="cuda")
     for word_or_none in (word, None):
         ws = torch.full((size,), 255, dtype=torch.uint8, device="cuda")
-        ws[:4096] = 0
         for _ in range(3):
             y.zero_()
-            B.cmpq_gated_i8(x, *w, ff, d, y, ws, g, EPS, "gelu", x, word_or_none)
-            assert torch.equal(y, block(x, residual=x, norm=g, eps=EPS)) and int(word) == 0 and not ws[:4096].any()
+            B.cmpq_gated_i8(x, *w, ff, d, y, state, ws, g, EPS, "gelu", x, word_or_none)
+            assert torch.equal(y, block(x, residual=x, norm=g, eps=EPS)) and int(word) == 0 and not state.any()
     with pytest.raises(B.CmpqError) as e:
-        B.cmpq_gated_i8(x, *w, ff, d, y, ws[: size - 256], g, EPS, "gelu", x, word)
+        B.cmpq_gated_i8(x, *w, ff, d, y, state, ws[: size - 256], g, EPS, "gelu", x, word)
     assert e.value.status == 3
+    state[-4] = 8                                         # the mark of a kernel that gave up
+    B.cmpq_gated_i8(x[:1], *w, ff, d, torch.empty_like(x[:1]), state, ws, word=word)
+    assert int(word) == 8
+    word.zero_()
     ws = torch.empty(B.cmpq_linear_i8_ws_bytes(n, d, ff), dtype=torch.uint8, device="cuda")
     z = torch.empty(n, ff, dtype=dtype, device="cuda")
     B.cmpq_linear_i8_fused(x, w[0], ff, z, ws, g, EPS, "silu", None, word)
@@ -414,16 +439,17 @@ def test_decoder_layer_refuses_parts_that_do_not_fit():
         serving.DecoderLayer8(layer.attention, wrong, layer.attention_norm, layer.mlp_norm)
 
 
-SERVED = (1, 5, 64, 400)
+SERVED = (1, 4, 64, 400)
 
 
-def test_graphs_streams_and_eager_calls_together():
+@pytest.mark.parametrize("d,ff", [(256, 1000), (1024, 6000)])
+def test_graphs_streams_and_eager_calls_together(d, ff):
     """Blocks and layers of several batch sizes, captured, replayed in any order and on several streams, with eager calls
     between: every result has the bytes of a call that ran alone."""
     dtype = torch.bfloat16
-    block, layer = _block(1, 256, 1000, 256, dtype, "silu", False), _weights(700, 256, dtype, 9, True)
-    g = _norm(256, dtype, 1)
-    xs = {n: _tokens(n, 256, dtype, n) for n in SERVED}
+    block, layer = _block(1, d, ff, d, dtype, "silu", False), _weights(700, d, dtype, 9, True)
+    g = _norm(d, dtype, 1)
+    xs = {n: _tokens(n, d, dtype, n) for n in SERVED}
     call = lambda n: (block(xs[n], residual=xs[n], norm=g), layer(xs[n], norm=g, activation="gelu"))
     stream, graphs, out = torch.cuda.Stream(), {}, {}
     for n in SERVED:                                      # the first calls of all are captured ones

@@ -66,22 +66,22 @@ def test_linear(L, p):
 
 
 def test_gated(L, p):
-    def g(X=p, dt=0, n=2, d_in=20, ldx=20, norm=p, eps=1e-6, gate="", up="", down="", d_ff=30, d_out=5, act=2, res=p, ldr=5, y=p, ldy=5, ws=p, wb=1 << 40):
+    def g(X=p, dt=0, n=2, d_in=20, ldx=20, norm=p, eps=1e-6, gate="", up="", down="", d_ff=30, d_out=5, act=2, res=p, ldr=5, y=p, ldy=5, state=p, ws=p, wb=1 << 40):
         w = [_w(p) if x == "" else x for x in (gate, up, down)]
-        return L.cmpq_gated_i8(X, dt, n, d_in, ldx, norm, eps, *w, d_ff, d_out, act, res, ldr, y, ldy, None, ws, wb, None)
+        return L.cmpq_gated_i8(X, dt, n, d_in, ldx, norm, eps, *w, d_ff, d_out, act, res, ldr, y, ldy, None, state, ws, wb, None)
 
-    for bad in (dict(X=None), dict(y=None), dict(dt=2), dict(n=-1), dict(d_in=0), dict(d_ff=0), dict(d_out=0), dict(d_in=131073, ldx=131073), dict(d_ff=131073),
+    for bad in (dict(state=None), dict(state=_off(p, 8)), dict(X=None), dict(y=None), dict(dt=2), dict(n=-1), dict(d_in=0), dict(d_ff=0), dict(d_out=0), dict(d_in=131073, ldx=131073), dict(d_ff=131073),
                 dict(d_out=262145, ldy=262145, ldr=262145), dict(ldx=19), dict(ldy=4), dict(act=7), dict(ldr=4), dict(res=_off(p, 1)), dict(norm=_off(p, 1)),
                 dict(eps=float("nan")), dict(gate=None), dict(up=None), dict(down=None), dict(X=_off(p, 1)), dict(y=_off(p, 1)), dict(n=(1 << 31) - 256)):
         assert g(**bad) == INVALID, bad
     for what in BAD_WEIGHTS:
         for part in ("gate", "up", "down"):
             assert g(**{part: _bad(p, what)}) == INVALID, (part, what)
-    assert g(ws=None) == WORKSPACE and g(wb=4096) == WORKSPACE and g(ws=_off(p, 64)) == WORKSPACE
+    assert g(ws=None) == WORKSPACE and g(wb=256) == WORKSPACE and g(ws=_off(p, 64)) == WORKSPACE
     assert g(n=0, X=None, ws=None) == 0
     size = B.cmpq_gated_i8_ws_bytes
     assert size(-1, 4, 4, 4) == size(1, 0, 4, 4) == size(1, 4, 0, 4) == size(1, 4, 4, 0) == size(1, 4, 131073, 4) == 0
-    assert size(7, 33, 100, 9) >= 4096 + 7 * (2 * 100 + 112 + 8)
+    assert size(7, 33, 100, 9) >= 7 * (2 * 100 + 112 + 8)
     # rows of h and codes whose bytes pass 32 bits are counted in 64
     assert size(1 << 20, 4096, 131072, 4096) >= (1 << 20) * 131072 * 3
 
