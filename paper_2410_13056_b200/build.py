@@ -9,7 +9,7 @@ INCLUDE = os.path.join(_ROOT, "include")
 LIB_PATH = os.path.join(_PKG, "libcmpq.so")
 EXT_PATH = os.path.join(_PKG, "_serving.so")  # marshals the serving calls on torch tensors
 SOURCES = ["api.cu", "stats.cu", "stats_static.cu", "alloc.cu", "lloyd.cu", "lloyd_weighted.cu", "lloyd_hist.cu", "outliers.cu", "pack.cu", "matvec.cu", "transpose.cu", "probe.cu", "lut_store.cu",
-           "linear_i8.cu", "gated_i8.cu", "cache.cu", "cache_attention.cu", "cache_prefill.cu"]
+           "linear_i8.cu", "few_i8.cu", "gated_i8.cu", "cache.cu", "cache_attention.cu", "cache_prefill.cu"]
 NVCC_FLAGS = ["-O3", "-std=c++17", "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo",
               "-Xcompiler", "-fPIC", "--fmad=false", "--cudart", "static", "-I", INCLUDE, "-I", CSRC]
 

@@ -1,0 +1,166 @@
+// Products for up to four tokens, shared by the linear layer and the gated block: every block quantizes all tokens into its
+// shared memory while its first weights are on their way.
+#pragma once
+
+#include <algorithm>
+
+#include "product_i8.cuh"
+
+namespace cmpq {
+
+constexpr int kFewThreads = 320;  // a warp for the weights, one for the products, eight that compute
+constexpr int kFewMaxStages = 64;
+constexpr int kFewSmem = 224 << 10;
+constexpr int kFewRows = 8, kFewColumns = 16;  // of the tokens' operand and of an accumulator: the least there is
+
+struct TokenRows {
+    const uint16_t* x;
+    int64_t ldx;
+    int wide;  // rows on 16 bytes
+    RowNorm norm;
+    int64_t d;
+    int n;
+    int32_t* word;  // or null
+};
+
+// The computing warps' barrier.
+__device__ __forceinline__ void meet() { asm volatile("bar.sync 1, 256;" ::: "memory"); }
+
+// Where the codes of token `row` from byte k on stand in the tokens' operand: blocks of 128 bytes of the sum, in each eight rows
+// in the 128-byte swizzle.
+__device__ __forceinline__ uint8_t* code_at(uint8_t* base, int row, int k) {
+    return base + (k >> 7) * kFewRows * 128 + row * 128 + (((k >> 4 & 7) ^ row) << 4) + (k & 15);
+}
+
+// load8 of rows that a kernel may have written while this one was on its way: not through the read-only path.
+__device__ __forceinline__ uint4 load8_written(const uint16_t* p, int64_t left, bool wide) {
+    if (wide && left >= 8) return __ldcg(reinterpret_cast<const uint4*>(p));
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t lo = 2 * i < left ? __ldcg(p + 2 * i) : 0u, hi = 2 * i + 1 < left ? __ldcg(p + 2 * i + 1) : 0u;
+        w[i] = lo | hi << 16;
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+struct TokenParts {  // in shared memory
+    uint32_t m[kFewTokens][8];
+    float s[kFewTokens][8];
+};
+
+// Codes of all tokens into the operand at `base`, their scales into `scale`, by 256 threads, all rows at once so that their loads
+// are on their way together.  Each thread takes the groups that quantize_row gives it, so a token gets the same bytes from
+// either.
+template <int DT, bool NORM>
+__device__ __forceinline__ void quantize_tokens(const TokenRows& A, uint8_t* base, float* scale, TokenParts& parts, int t) {
+    constexpr int R = kFewTokens, KEEP = 2;  // groups of a row that a thread keeps
+    const int n = A.n;
+    const int64_t d = A.d, groups = (d + 7) / 8;
+    struct Group {
+        uint4 w, x[R];
+    };
+    auto load = [&](int64_t g, Group& k) {
+        k.w = NORM && g < groups ? load8(A.norm.weight + 8 * g, d - 8 * g, A.norm.wide) : make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+            k.x[r] = r < n && g < groups ? load8_written(A.x + r * A.ldx + 8 * g, d - 8 * g, A.wide) : make_uint4(0u, 0u, 0u, 0u);
+    };
+    Group held[KEEP];
+#pragma unroll
+    for (int i = 0; i < KEEP; ++i) load(t + i * 256, held[i]);
+    // f(row, group, entries, v) for this thread's groups
+    auto every = [&](auto f) {
+        auto one = [&](int64_t g, const Group& k) {
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                if (r >= n || g >= groups) break;
+                float e[8], v[8];
+                widen8<DT>(k.x[r], e);
+                if (NORM) widen8<DT>(k.w, v);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[j] = NORM ? e[j] * v[j] : e[j];
+                f(r, g, e, v);
+            }
+        };
+#pragma unroll
+        for (int i = 0; i < KEEP; ++i) one(t + i * 256, held[i]);
+        for (int64_t g = t + KEEP * 256; g < groups; g += 256) {
+            Group k;
+            load(g, k);
+            one(g, k);
+        }
+    };
+    uint32_t m[R] = {};
+    float sum[R] = {}, f = 1.0f;
+    auto add_up = [&] {  // over the block: the same bits in all threads
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            m[r] = __reduce_max_sync(0xffffffffu, m[r]);
+#pragma unroll
+            for (int i = 16; i && NORM; i >>= 1) sum[r] += __shfl_xor_sync(0xffffffffu, sum[r], i);
+            if ((t & 31) == 0) parts.m[r][t >> 5] = m[r], parts.s[r][t >> 5] = sum[r];
+        }
+        meet();
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            sum[r] = 0.0f;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) m[r] = max(m[r], parts.m[r][i]), sum[r] += parts.s[r][i];
+        }
+    };
+    every([&](int r, int64_t, const float(&e)[8], const float(&v)[8]) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) m[r] = max(m[r], __float_as_uint(v[j]) & 0x7fffffffu);
+        if (NORM) sum[r] += sum_squares(e, f);
+    });
+    add_up();
+    float2 s[R];
+    float factor[R], squares[R];
+    bool passed = false;
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        s[r] = scale_of(__uint_as_float(m[r])), squares[r] = sum[r], factor[r] = 1.0f;
+        if (NORM && sum[r] > FLT_MAX && m[r] < 0x7f800000u) passed = true, factor[r] = 0x1p-80f;
+    }
+    if (passed) {  // see quantize_row; the same in all threads
+        f = 0x1p-80f;
+#pragma unroll
+        for (int r = 0; r < R; ++r) sum[r] = 0.0f;
+        every([&](int r, int64_t, const float(&e)[8], const float(&)[8]) { sum[r] += sum_squares(e, f); });
+        meet();  // the parts have been read
+        add_up();
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+            if (factor[r] != 1.0f) squares[r] = sum[r];
+    }
+    every([&](int r, int64_t g, const float(&)[8], const float(&v)[8]) { *reinterpret_cast<uint2*>(code_at(base, r, 8 * (int)g)) = round_codes(v, s[r].y); });
+    if (t == 0)
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            if (r >= n) break;
+            if (NORM && s[r].x > 0.0f) s[r].x *= factor[r] / sqrtf(squares[r] / (float)d + A.norm.eps * factor[r] * factor[r]);
+            scale[r] = s[r].x;
+            if (m[r] >= 0x7f800000u && A.word && blockIdx.x == 0) atomicOr(A.word, kWordNonfinite);
+        }
+}
+
+inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+// Equal tiles of channels for the blocks, in as few rounds as 128 channels allow.
+inline void plan_tiles(ProductArgs& p) {
+    const int64_t sms = sm_count(), rounds = ceil_div(p.d_out, 128 * sms);
+    p.bn = (int)std::min<int64_t>(128, ceil_div(ceil_div(p.d_out, rounds * sms), 8) * 8);
+    p.n_tiles = (int)ceil_div(p.d_out, p.bn);
+}
+// Bytes for stages of weights.  Behind them are the tokens' codes of `blocks` blocks of the sum; products read 128 rows of
+// weights and 16 of tokens, whatever there is.
+inline int few_ring(int blocks) { return kFewSmem - 1024 - std::max(kFewRows * 128 * blocks + 1024, 128 * 128); }
+// Stages of 16 to 32 KB: with less of a row at a time memory is slower (4096 x 11008 in boxes of 32 rows x 128 bytes: 23.5 us
+// one by one, 10.1 by fours, 8.8 by eights).
+inline void plan_stages(ProductArgs& p, int block_bytes, int ring) {
+    p.per_stage = std::max(1, (32 << 10) / block_bytes);
+    p.stages = std::min(ring / (p.per_stage * block_bytes), kFewMaxStages);
+}
+
+}  // namespace cmpq

@@ -1,11 +1,9 @@
 // Gated feed-forward block in 8 bits.
 #include <algorithm>
 
-#include "product_i8.cuh"
+#include "few_i8.cuh"
 
 namespace cmpq {
-
-constexpr int kFewTokens = 4;
 
 // The work space: h; the codes of the tokens, later of h; their scales.  For few tokens h, the down projection's sums and how
 // many parts of each tile's are there.
@@ -48,17 +46,10 @@ struct GatedSpace {
 // What blocks hand to one another goes through L2: stores, a fence, an atomic on the counter; an acquiring load of it, then
 // loads past L1.
 
-constexpr int kFewThreads = 320;  // a warp for the weights, one for the products, eight that compute
-constexpr int kFewMaxStages = 64;
-constexpr int kFewSmem = 224 << 10, kFewTokenBytes = 100 << 10;
-constexpr int kFewRows = 8, kFewColumns = 16;  // of the tokens' operand and of an accumulator: the least there is
 constexpr int kRowMax = 2, kMark = CMPQ_GATED_STATE_BYTES / 4 - 1;  // in the state: rows' maxima, the mark of a kernel that gave up
 
 struct FewArgs {
-    const uint16_t* x;
-    int64_t ldx;
-    int wide_x;
-    RowNorm norm;
+    TokenRows x;
     ProductArgs up, down;  // bn: channels of a tile; stages, per_stage; of up: y is h
     int d_in, d_ff;
     int ring;                             // bytes that the stages share
@@ -82,121 +73,12 @@ __device__ __forceinline__ bool wait_count(const int32_t* count, int target, vol
         }
     }
 }
-// The computing warps' barrier.
-__device__ __forceinline__ void meet() { asm volatile("bar.sync 1, 256;" ::: "memory"); }
 // The count before this block's addition, for thread 0 of them; what all of them wrote before is seen by whoever sees it.
 __device__ __forceinline__ int add_count(int32_t* count, int t) {
     meet();
     if (t != 0) return 0;
     __threadfence();
     return atomicAdd(count, 1);
-}
-
-// Where the codes of token `row` from byte k on stand in the tokens' operand: blocks of 128 bytes of the sum, in each eight rows
-// in the 128-byte swizzle.
-__device__ __forceinline__ uint8_t* code_at(uint8_t* base, int row, int k) {
-    return base + (k >> 7) * kFewRows * 128 + row * 128 + (((k >> 4 & 7) ^ row) << 4) + (k & 15);
-}
-
-struct TokenParts {  // in shared memory
-    uint32_t m[kFewTokens][8];
-    float s[kFewTokens][8];
-};
-
-// Codes of all tokens into the operand at `base`, their scales into `scale`, by 256 threads, all rows at once so that their loads
-// are on their way together.  Each thread takes the groups that quantize_row gives it, so a token gets the same bytes from
-// either.
-template <int DT, bool NORM>
-__device__ __forceinline__ void quantize_tokens(const FewArgs& A, uint8_t* base, float* scale, TokenParts& parts, int t) {
-    constexpr int R = kFewTokens, KEEP = 2;  // groups of a row that a thread keeps
-    const int n = A.up.n;
-    const int64_t d = A.d_in, groups = (d + 7) / 8;
-    struct Group {
-        uint4 w, x[R];
-    };
-    auto load = [&](int64_t g, Group& k) {
-        k.w = NORM && g < groups ? load8(A.norm.weight + 8 * g, d - 8 * g, A.norm.wide) : make_uint4(0u, 0u, 0u, 0u);
-#pragma unroll
-        for (int r = 0; r < R; ++r)
-            k.x[r] = r < n && g < groups ? load8(A.x + r * A.ldx + 8 * g, d - 8 * g, A.wide_x) : make_uint4(0u, 0u, 0u, 0u);
-    };
-    Group held[KEEP];
-#pragma unroll
-    for (int i = 0; i < KEEP; ++i) load(t + i * 256, held[i]);
-    // f(row, group, entries, v) for this thread's groups
-    auto every = [&](auto f) {
-        auto one = [&](int64_t g, const Group& k) {
-#pragma unroll
-            for (int r = 0; r < R; ++r) {
-                if (r >= n || g >= groups) break;
-                float e[8], v[8];
-                widen8<DT>(k.x[r], e);
-                if (NORM) widen8<DT>(k.w, v);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) v[j] = NORM ? e[j] * v[j] : e[j];
-                f(r, g, e, v);
-            }
-        };
-#pragma unroll
-        for (int i = 0; i < KEEP; ++i) one(t + i * 256, held[i]);
-        for (int64_t g = t + KEEP * 256; g < groups; g += 256) {
-            Group k;
-            load(g, k);
-            one(g, k);
-        }
-    };
-    uint32_t m[R] = {};
-    float sum[R] = {}, f = 1.0f;
-    auto add_up = [&] {  // over the block: the same bits in all threads
-#pragma unroll
-        for (int r = 0; r < R; ++r) {
-            m[r] = __reduce_max_sync(0xffffffffu, m[r]);
-#pragma unroll
-            for (int i = 16; i && NORM; i >>= 1) sum[r] += __shfl_xor_sync(0xffffffffu, sum[r], i);
-            if ((t & 31) == 0) parts.m[r][t >> 5] = m[r], parts.s[r][t >> 5] = sum[r];
-        }
-        meet();
-#pragma unroll
-        for (int r = 0; r < R; ++r) {
-            sum[r] = 0.0f;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) m[r] = max(m[r], parts.m[r][i]), sum[r] += parts.s[r][i];
-        }
-    };
-    every([&](int r, int64_t, const float(&e)[8], const float(&v)[8]) {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) m[r] = max(m[r], __float_as_uint(v[j]) & 0x7fffffffu);
-        if (NORM) sum[r] += sum_squares(e, f);
-    });
-    add_up();
-    float2 s[R];
-    float factor[R], squares[R];
-    bool passed = false;
-#pragma unroll
-    for (int r = 0; r < R; ++r) {
-        s[r] = scale_of(__uint_as_float(m[r])), squares[r] = sum[r], factor[r] = 1.0f;
-        if (NORM && sum[r] > FLT_MAX && m[r] < 0x7f800000u) passed = true, factor[r] = 0x1p-80f;
-    }
-    if (passed) {  // see quantize_row; the same in all threads
-        f = 0x1p-80f;
-#pragma unroll
-        for (int r = 0; r < R; ++r) sum[r] = 0.0f;
-        every([&](int r, int64_t, const float(&e)[8], const float(&)[8]) { sum[r] += sum_squares(e, f); });
-        meet();  // the parts have been read
-        add_up();
-#pragma unroll
-        for (int r = 0; r < R; ++r)
-            if (factor[r] != 1.0f) squares[r] = sum[r];
-    }
-    every([&](int r, int64_t g, const float(&)[8], const float(&v)[8]) { *reinterpret_cast<uint2*>(code_at(base, r, 8 * (int)g)) = round_codes(v, s[r].y); });
-    if (t == 0)
-#pragma unroll
-        for (int r = 0; r < R; ++r) {
-            if (r >= n) break;
-            if (NORM && s[r].x > 0.0f) s[r].x *= factor[r] / sqrtf(squares[r] / (float)d + A.norm.eps * factor[r] * factor[r]);
-            scale[r] = s[r].x;
-            if (m[r] >= 0x7f800000u && A.word && blockIdx.x == 0) atomicOr(A.word, kWordNonfinite);
-        }
 }
 
 template <int DT, bool NORM>
@@ -336,7 +218,7 @@ gated_few_kernel(const __grid_constant__ CUtensorMap gate_map, const __grid_cons
             __syncwarp();
             if (lane == 0) tc5::mbar_arrive(&tokens_there);
         };
-        quantize_tokens<DT, NORM>(A, tokens, scale, parts, t);
+        quantize_tokens<DT, NORM>(A.x, tokens, scale, parts, t);
         tokens_written();
         int32_t* tile_parts = A.sums + n * A.ld_sums;
         for (int64_t i = (int64_t)blockIdx.x * 256 + t; i < (n * A.ld_sums + A.down.n_tiles + 3) / 4; i += (int64_t)gridDim.x * 256)
@@ -487,8 +369,6 @@ gated_few_kernel(const __grid_constant__ CUtensorMap gate_map, const __grid_cons
     if (warp == 1) tc5::tmem_free<1>(tmem, 64);
 }
 
-static int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
-
 // Tiles, parts and stages; false where separate kernels are as fast, or the tokens' codes would take too much of the shared
 // memory.  In graphs, 1 token 4096 -> 11008 -> 4096 takes 30.2 us here and 35.0 in four kernels, 8 tokens 38.2 and 36.0; 1 token
 // 1536 -> 4096 -> 1536 (19 MB) 15.6 and 16.4, 1024 -> 2816 -> 1024 14.2 and 13.9.
@@ -497,12 +377,8 @@ static bool plan_few(FewArgs& a) {
     const int sms = sm_count();
     if ((2 * (int64_t)a.d_in + d.d_out) * a.d_ff < (16 << 20)) return false;
     u.kblocks = (int)ceil_div(a.d_in, 128), d.kblocks = (int)ceil_div(a.d_ff, 128);
-    constexpr int kMost = kFewTokenBytes / (kFewRows * 128);  // blocks of the sum whose tokens are held
-    if (u.kblocks > kMost) return false;
-    // equal tiles for the blocks, in as few rounds as 128 channels of each projection allow
-    const int64_t rounds = ceil_div(u.d_out, 128 * sms);
-    u.bn = (int)std::min<int64_t>(128, ceil_div(ceil_div(u.d_out, rounds * sms), 8) * 8);
-    u.n_tiles = (int)ceil_div(u.d_out, u.bn);
+    if (u.kblocks > kFewBlocks) return false;
+    plan_tiles(u);
     // channels and part of the sum of a unit, so that the block with the most of them is soonest done, in cycles: 23 bytes come
     // in one, a block of the sum takes 150 and a unit 1500 besides
     int64_t least = INT64_MAX;
@@ -510,7 +386,7 @@ static bool plan_few(FewArgs& a) {
         for (int parts = 1; parts <= std::min(d.kblocks, 32); ++parts) {
             const int64_t tiles = ceil_div(d.d_out, bn), blocks = ceil_div(d.kblocks, parts), each = ceil_div(tiles * ceil_div(d.kblocks, blocks), sms);
             const int64_t cost = each * (blocks * (bn * 128 / 23 + 150) + 1500);
-            if (blocks <= kMost && cost < least) {
+            if (blocks <= kFewBlocks && cost < least) {
                 least = cost, d.bn = bn, d.n_tiles = (int)tiles;
                 a.part_blocks = (int)blocks, a.parts = (int)ceil_div(d.kblocks, blocks), a.block_units = (int)each;
             }
@@ -518,13 +394,9 @@ static bool plan_few(FewArgs& a) {
     if (least == INT64_MAX) return false;
     a.ld_sums = (int64_t)d.n_tiles * d.bn;
     d.wide = aligned_to(d.y, 8) && d.ldy % 4 == 0;
-    // Stages of 16 to 32 KB: with less of a row at a time memory is slower.  Behind them the tokens' codes; products read 128 rows
-    // of weights and 16 of tokens, whatever there is.
-    const int behind = std::max(kFewRows * 128 * std::max(u.kblocks, a.part_blocks) + 1024, 128 * 128);
-    const int up_block = 2 * u.bn * 128, down_block = d.bn * 128;
-    a.ring = kFewSmem - 1024 - behind;
-    u.per_stage = std::max(1, (32 << 10) / up_block), d.per_stage = std::max(1, (32 << 10) / down_block);
-    u.stages = std::min(a.ring / (u.per_stage * up_block), kFewMaxStages), d.stages = std::min(a.ring / (d.per_stage * down_block), kFewMaxStages);
+    a.ring = few_ring(std::max(u.kblocks, a.part_blocks));
+    plan_stages(u, 2 * u.bn * 128, a.ring);
+    plan_stages(d, d.bn * 128, a.ring);
     return true;
 }
 
@@ -549,7 +421,7 @@ static cmpq_status launch_few(const FewArgs& a, const Weight8& gate, const Weigh
         return cudaLaunchKernelEx(&cfg, kernel, gate_map, up_map, down_map, a) == cudaSuccess ? launch_status() : CMPQ_ERR_CUDA;
     };
     static bool raised[2][64];
-    return a.norm.weight ? launch(gated_few_kernel<DT, true>, raised[0]) : launch(gated_few_kernel<DT, false>, raised[1]);
+    return a.x.norm.weight ? launch(gated_few_kernel<DT, true>, raised[0]) : launch(gated_few_kernel<DT, false>, raised[1]);
 }
 
 }  // namespace cmpq
@@ -580,8 +452,8 @@ extern "C" cmpq_status cmpq_gated_i8(const void* X, cmpq_dtype dt, int64_t n, in
     auto* kept = static_cast<int32_t*>(state);
     if (n <= kFewTokens) {
         FewArgs a = {};
-        a.x = static_cast<const uint16_t*>(X), a.ldx = ldx, a.wide_x = aligned_to(X, 16) && ldx % 8 == 0;
-        a.norm = {static_cast<const uint16_t*>(norm), aligned_to(norm, 16), eps};
+        a.x = {static_cast<const uint16_t*>(X), ldx, aligned_to(X, 16) && ldx % 8 == 0, {static_cast<const uint16_t*>(norm), aligned_to(norm, 16), eps},
+               d_in, (int)n, word};
         a.sums = g.sums;
         a.up.ws = gate->scale, a.up.us = up->scale;
         a.up.bias = static_cast<const uint16_t*>(gate->bias), a.up.ubias = static_cast<const uint16_t*>(up->bias);
@@ -594,6 +466,12 @@ extern "C" cmpq_status cmpq_gated_i8(const void* X, cmpq_dtype dt, int64_t n, in
         if (plan_few(a)) return dt == CMPQ_BF16 ? launch_few<CMPQ_BF16>(a, *gate, *up, *down, st) : launch_few<CMPQ_F16>(a, *gate, *up, *down, st);
     }
     int32_t* gave_up = word ? word : kept + kMark;
+    if (n <= kFewTokens && few_fits(d_in) && few_fits(d_ff)) {
+        const cmpq_status s = enqueue_few(X, dt, n, d_in, ldx, norm, eps, *gate, d_ff, up, {act, nullptr, 0}, g.h, g.ldh, word, gave_up, false, st);
+        return s != CMPQ_OK ? s
+                            : enqueue_few(g.h, dt, n, d_ff, g.ldh, nullptr, 0.0f, *down, d_out, nullptr, {CMPQ_ACT_NONE, residual, ldr}, y, ldy, word, gave_up,
+                                          true, st);
+    }
     cmpq_status s = enqueue_quantize(X, dt, n, d_in, ldx, norm, eps, g.codes, g.ldc_in, g.x_scale, word, nullptr, st);
     if (s != CMPQ_OK) return s;
     s = enqueue_product({g.codes, g.ldc_in, g.x_scale}, dt, n, d_in, *gate, d_ff, up, {act, nullptr, 0}, g.h, g.ldh, gave_up, true, st);

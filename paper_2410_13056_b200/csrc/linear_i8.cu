@@ -230,7 +230,7 @@ matmul_i8_tile_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_con
     if (warp == 1) tc5::tmem_free<1>(tmem, columns);
 }
 
-constexpr int kPairStages = 6, kPairStageBytes = 2 * 128 * 128;
+constexpr int kPairStages = 6, kPairStageBytes = 2 * 128 * 128;  // room for the widest tile
 constexpr size_t kPairSmem = kPairStages * kPairStageBytes + 1024;
 
 // Many tokens: pairs of CTAs stay on their SMs and walk over tiles of 256 tokens x 256 channels (cta_group::2).  A CTA
@@ -248,7 +248,7 @@ template <int DT, int KIND>
 __global__ void __launch_bounds__(kMmThreads, 1)
 matmul_i8_pair_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__ CUtensorMap umap, const __grid_constant__ CUtensorMap xmap,
                       const __grid_constant__ ProductArgs A) {
-    constexpr int kWide = KIND == kGated ? 128 : 256;  // channels of a tile
+    const int half = A.bn / 2, wide_tile = KIND == kGated ? half : A.bn;  // columns that a CTA loads; channels of a tile
     extern __shared__ uint8_t raw[];
     uint8_t* smem = raw + ((1024u - (tc5::smem_addr(raw) & 1023u)) & 1023u);
     __shared__ uint64_t full[kPairStages], empty[kPairStages], acc_full[2], acc_empty[2];
@@ -279,19 +279,20 @@ matmul_i8_pair_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_con
                 const int mt = tile % A.m_tiles, nt = tile / A.m_tiles;
                 for (int k = 0; k < A.kblocks; ++k) {
                     if (!(ok = tc5::mbar_wait<true>(empty + slot, phase, &failed))) break;
-                    if (rank == 0) tc5::mbar_expect_tx(full + slot, 2 * kPairStageBytes);
+                    if (rank == 0) tc5::mbar_expect_tx(full + slot, 2 * (128 + half) * 128);
                     uint8_t* at = smem + slot * kPairStageBytes;
                     tc5::tma_load_2d_pair(at, &xmap, full + slot, k * 128, mt * 256 + rank * 128);
                     if (KIND == kGated)
-                        tc5::tma_load_2d_pair(at + 128 * 128, rank ? &umap : &wmap, full + slot, k * 128, nt * 128);
+                        tc5::tma_load_2d_pair(at + 128 * 128, rank ? &umap : &wmap, full + slot, k * 128, nt * half);
                     else
-                        tc5::tma_load_2d_pair(at + 128 * 128, &wmap, full + slot, k * 128, nt * 256 + rank * 128);
+                        tc5::tma_load_2d_pair(at + 128 * 128, &wmap, full + slot, k * 128, nt * A.bn + rank * half);
                     if (++slot == kPairStages) slot = 0, phase ^= 1;
                 }
             }
         }
     } else if (warp == 1) {
         if (rank == 0 && tc5::elect_one()) {
+            const uint32_t idesc = tc5::idesc_i8(256, A.bn);
             int slot = 0, phase = 0, acc = 0, acc_phase = 1;
             bool ok = true;
             for (int tile = first; ok && tile < tiles; tile += step) {
@@ -304,7 +305,7 @@ matmul_i8_pair_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_con
                     const uint64_t a = tc5::desc_k_sw128(at), b = tc5::desc_k_sw128(at + 128 * 128);
 #pragma unroll
                     for (int j = 0; j < 4; ++j)
-                        tc5::mma_i8<2>(tmem + acc * 256, a + 2 * j, b + 2 * j, tc5::idesc_i8(256, 256), (k | j) != 0);
+                        tc5::mma_i8<2>(tmem + acc * 256, a + 2 * j, b + 2 * j, idesc, (k | j) != 0);
                     tc5::mma_commit_pair(empty + slot);
                     if (++slot == kPairStages) slot = 0, phase ^= 1;
                 }
@@ -321,16 +322,16 @@ matmul_i8_pair_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_con
             [&](int tile, int acc) {
                 const int t = tile % A.m_tiles * 256 + rank * 128 + quad * 32 + lane;
                 xs = t < A.n ? __ldcg(A.xs + t) : 0.0f;  // see the other kernel
-                const int o0 = tile / A.m_tiles * kWide;
-                reinterpret_cast<float2*>(scale_bias[acc])[i] = column_scale<DT, KIND>(A, o0, i, 256);
+                const int o0 = tile / A.m_tiles * wide_tile;
+                if (i < A.bn) reinterpret_cast<float2*>(scale_bias[acc])[i] = column_scale<DT, KIND>(A, o0, i, A.bn);
                 if (KIND == kFinish && A.residual && t < A.n)
-                    ask_for(A.residual + (int64_t)t * A.ldr + o0, min(upper * 128, A.d_out - o0), min(upper * 128 + 128, A.d_out - o0));
+                    ask_for(A.residual + (int64_t)t * A.ldr + o0, min(upper * half, A.d_out - o0), min(upper * half + half, A.d_out - o0));
                 asm volatile("bar.sync 1, 256;" ::: "memory");
             },
             [&](int acc, int parity) { return tc5::mbar_wait_warp<true>(acc_full + acc, parity, &failed); },
             [&](int tile, int acc) {
-                const int o0 = tile / A.m_tiles * kWide, row0 = tile % A.m_tiles * 256 + rank * 128 + quad * 32, t = row0 + lane;
-                const int left = min(kWide, A.d_out - o0), c0 = upper * (kWide / 2), c1 = c0 + kWide / 2;
+                const int o0 = tile / A.m_tiles * wide_tile, row0 = tile % A.m_tiles * 256 + rank * 128 + quad * 32, t = row0 + lane;
+                const int left = min(wide_tile, A.d_out - o0), c0 = upper * (wide_tile / 2), c1 = c0 + wide_tile / 2;
                 tc5::fence_after_sync();
                 if (row0 < A.n) {
                     const float2* sb = reinterpret_cast<float2*>(scale_bias[acc]);
@@ -338,7 +339,7 @@ matmul_i8_pair_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_con
                     uint16_t* y = A.y + (int64_t)t * A.ldy + o0;
                     if (KIND == kPlain) store_rows<DT>(rows, c0, c1, sb, A.bias != nullptr, xs, t < A.n, y, left, A.wide);
                     if (KIND == kFinish) store_finished<DT>(rows, c0, c1, sb, A, xs, t < A.n, y, A.residual + (int64_t)t * A.ldr + o0, left);
-                    if (KIND == kGated) store_gated<DT>(rows, c0, c1, 128, sb, A, xs, t < A.n, y, left);
+                    if (KIND == kGated) store_gated<DT>(rows, c0, c1, half, sb, A, xs, t < A.n, y, left);
                 }
                 tc5::fence_before_sync();
                 __syncwarp();
@@ -368,9 +369,9 @@ static int64_t tile_cycles(const ProductArgs& a, int bn) {
     const int64_t rounds = (blocks + sms - 1) / sms, pace = std::max(4 * std::max(32, bn / 2), (bn + std::min(a.n, 128)) * 2);
     return std::max<int64_t>(rounds * a.kblocks * pace, (int64_t)a.kblocks * 128 * a.cols / 3400) + rounds * (9000 + 8 * bn);
 }
-static int64_t pair_cycles(const ProductArgs& a) {
-    const int64_t tiles = (int64_t)((a.n + 255) / 256) * ((a.cols + 255) / 256), pairs = sm_count() / 2;
-    return (tiles + pairs - 1) / pairs * a.kblocks * 600 + 14000;
+static int64_t pair_cycles(const ProductArgs& a, int bn) {
+    const int64_t tiles = (int64_t)((a.n + 255) / 256) * ((a.cols + bn - 1) / bn), pairs = sm_count() / 2;
+    return (tiles + pairs - 1) / pairs * a.kblocks * (600 * (256 + bn) / 512) + 14000;  // the pace is that of the loads
 }
 
 template <int DT, int KIND>
@@ -382,14 +383,18 @@ static cmpq_status launch_kind(const TokenCodes& x, int64_t d_in, const Weight8&
     a.bn = 32;
     for (int bn = 48; bn <= 256; bn += 16)
         if (tile_cycles(a, bn) < tile_cycles(a, a.bn)) a.bn = bn;
-    const bool pair = a.n > 128 && pair_cycles(a) < tile_cycles(a, a.bn);
+    int wide = 256;  // narrower where that fills the last round better
+    for (int bn = 224; bn >= 128; bn -= 32)
+        if (pair_cycles(a, bn) < pair_cycles(a, wide)) wide = bn;
+    const bool pair = a.n > 128 && pair_cycles(a, wide) < tile_cycles(a, a.bn);
+    if (pair) a.bn = wide;
     a.rows = pair ? 128 : std::min(128, (a.n + 7) / 8 * 8);
     CUtensorMap wmap, umap, xmap;
-    const int box = pair ? 128 : KIND == kGated ? a.bn / 2 : a.bn, wide = pair ? (KIND == kGated ? 128 : 256) : box;
+    const int box = pair || KIND == kGated ? a.bn / 2 : a.bn, channels = KIND == kGated ? a.bn / 2 : a.bn;
     if (!make_byte_map(&wmap, w.codes, a.d_out, d_in, w.ld, box) || !make_byte_map(&xmap, x.codes, a.n, d_in, x.ld, a.rows)) return CMPQ_ERR_CUDA;
     umap = wmap;
     if (u && !make_byte_map(&umap, u->codes, a.d_out, d_in, u->ld, box)) return CMPQ_ERR_CUDA;
-    a.n_tiles = (a.d_out + wide - 1) / wide;
+    a.n_tiles = (a.d_out + channels - 1) / channels;
     static bool raised[2][64];
     if (pair) {
         a.m_tiles = (a.n + 255) / 256;
@@ -522,6 +527,13 @@ extern "C" cmpq_status cmpq_linear_i8_fused(const void* X, cmpq_dtype dt, int64_
     const int64_t ldc = (int64_t)round_up(d_in, 16);
     int32_t* mark = mark_of(ws, n, d_in, d_out);
     const auto st = static_cast<cudaStream_t>(stream);
+    // One launch for few tokens, whose blocks read all of X and write y without waiting for one another: apart, then.
+    const auto *x0 = static_cast<const uint16_t*>(X), *y0 = static_cast<const uint16_t*>(y);
+    if (n <= kFewTokens && few_fits(d_in) && (x0 + (n - 1) * ldx + d_in <= y0 || y0 + (n - 1) * ldy + d_out <= x0)) {
+        if (!nonfinite && cudaMemsetAsync(mark, 0, sizeof(*mark), st) != cudaSuccess) return CMPQ_ERR_CUDA;
+        return enqueue_few(X, dt, n, d_in, ldx, norm, eps, *weight, d_out, nullptr, {act, residual, ldr}, y, ldy, nonfinite, nonfinite ? nonfinite : mark,
+                           false, st);
+    }
     const cmpq_status s = enqueue_quantize(X, dt, n, d_in, ldx, norm, eps, codes, ldc, scale, nonfinite, nonfinite ? nullptr : mark, st);
     if (s != CMPQ_OK) return s;
     // the quantization lets the product start early; it was itself started after everything before it, the weights too

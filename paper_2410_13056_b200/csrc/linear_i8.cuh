@@ -34,6 +34,13 @@ cmpq_status enqueue_product(const TokenCodes& x, cmpq_dtype dt, int64_t n, int64
 cmpq_status enqueue_quantize(const void* X, cmpq_dtype dt, int64_t n, int64_t d, int64_t ldx, const void* norm, float eps, int8_t* codes, int64_t ldc,
                              float* scale, int32_t* word, int32_t* clear, cudaStream_t st);
 
+// Both in one launch, for up to kFewTokens tokens whose rows few_fits; word (may be null): where a NaN or an infinity is
+// reported.  behind: it may start while the kernel in front of it, which was launched without this, writes X.
+constexpr int kFewTokens = 4, kFewBlocks = 100;  // blocks of 128 entries whose codes a block of the kernel holds
+bool few_fits(int64_t d_in);
+cmpq_status enqueue_few(const void* X, cmpq_dtype dt, int64_t n, int64_t d_in, int64_t ldx, const void* norm, float eps, const Weight8& w, int64_t d_out,
+                        const Weight8* u, const Finish& f, void* y, int64_t ldy, int32_t* word, int32_t* gave_up, bool behind, cudaStream_t st);
+
 size_t linear_i8_codes_bytes(int64_t n, int64_t d_in);
 
 inline bool linear_sizes_ok(int64_t n, int64_t d_in, int64_t d_out) {

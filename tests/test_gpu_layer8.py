@@ -128,7 +128,7 @@ def test_norm_quantize_strides_and_extremes(dtype):
 
 # ---- linear layer ----------------------------------------------------------------------------------------------
 
-SIZES = [(1, 1, 1), (1, 512, 129), (2, 100, 33), (7, 1000, 64), (9, 130, 257), (31, 33, 31), (65, 300, 513), (128, 128, 256), (129, 1025, 257),
+SIZES = [(1, 1, 1), (1, 512, 129), (2, 100, 33), (4, 4097, 1000), (3, 12800, 300), (1, 12801, 96), (4, 64, 40000), (1, 4096, 19000), (7, 1000, 64), (9, 130, 257), (31, 33, 31), (65, 300, 513), (128, 128, 256), (129, 1025, 257),
          (300, 4097, 770), (513, 64, 129), (700, 640, 2049), (1900, 520, 4400)]
 
 
@@ -152,6 +152,22 @@ def test_linear_with_its_epilogue(n, d_in, d_out, dtype):
             into = r.clone()
             assert torch.equal(layer(x, out=into, activation=act, residual=into, norm=g, eps=EPS), y)   # in place
     layer.check()
+
+
+@pytest.mark.parametrize("n", [1, 4, 5, 200])
+def test_linear_in_place(n):
+    """out may be x, or overlap it."""
+    d, dtype = 4096, torch.bfloat16
+    layer, g, x = _weights(d, d, dtype, 1, True), _norm(d, dtype, 2), _tokens(n, d, dtype, 3)
+    want = layer(x, activation="silu", norm=g, residual=x)
+    for _ in range(20):
+        into = x.clone()
+        assert torch.equal(layer(into, out=into, activation="silu", norm=g, residual=into), want)
+    room = torch.zeros(n, 2 * d + 7, dtype=dtype, device="cuda")
+    for _ in range(20):
+        room[:, :d] = x
+        y = layer(room[:, :d], out=room[:, 7: d + 7], activation="silu", norm=g)
+    assert torch.equal(y, layer(x, activation="silu", norm=g))
 
 
 def test_activations_over_their_whole_range():
