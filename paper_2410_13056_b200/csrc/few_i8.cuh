@@ -50,7 +50,7 @@ struct TokenParts {  // in shared memory
 };
 
 // Codes of all tokens into the operand at `base`, their scales into `scale`, by 256 threads, all rows at once so that their loads
-// are on their way together.  Each thread takes the groups that quantize_row gives it, so a token gets the same bytes from
+// are on their way together.  Each thread takes the groups that norm_quantize_row gives it, so a token gets the same bytes from
 // either.
 template <int DT, bool NORM>
 __device__ __forceinline__ void quantize_tokens(const TokenRows& A, uint8_t* base, float* scale, TokenParts& parts, int t) {
@@ -111,7 +111,7 @@ __device__ __forceinline__ void quantize_tokens(const TokenRows& A, uint8_t* bas
     };
     every([&](int r, int64_t, const float(&e)[8], const float(&v)[8]) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) m[r] = max(m[r], __float_as_uint(v[j]) & 0x7fffffffu);
+        for (int j = 0; j < 8; ++j) m[r] = __float_as_uint(larger(__uint_as_float(m[r]), v[j]));
         if (NORM) sum[r] += sum_squares(e, f);
     });
     add_up();
@@ -123,7 +123,7 @@ __device__ __forceinline__ void quantize_tokens(const TokenRows& A, uint8_t* bas
         s[r] = scale_of(__uint_as_float(m[r])), squares[r] = sum[r], factor[r] = 1.0f;
         if (NORM && sum[r] > FLT_MAX && m[r] < 0x7f800000u) passed = true, factor[r] = 0x1p-80f;
     }
-    if (passed) {  // see quantize_row; the same in all threads
+    if (passed) {  // see norm_quantize_row; the same in all threads
         f = 0x1p-80f;
 #pragma unroll
         for (int r = 0; r < R; ++r) sum[r] = 0.0f;
@@ -144,8 +144,6 @@ __device__ __forceinline__ void quantize_tokens(const TokenRows& A, uint8_t* bas
             if (m[r] >= 0x7f800000u && A.word && blockIdx.x == 0) atomicOr(A.word, kWordNonfinite);
         }
 }
-
-inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 // Equal tiles of channels for the blocks, in as few rounds as 128 channels allow.
 inline void plan_tiles(ProductArgs& p) {

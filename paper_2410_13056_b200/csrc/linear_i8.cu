@@ -41,11 +41,12 @@ __device__ __forceinline__ uint2 group_codes(uint4 g, float inv) {
 // One block per token.  Magnitudes are compared two at a time in their own type and, between lanes, as bit patterns,
 // where a NaN is larger than infinity and infinity larger than every number: the maximum also tells whether the row is
 // finite.  A thread keeps KEEP groups of eight in registers, chosen by the row's length so that more blocks share an SM
-// where rows are short; rows of up to 16384 entries are read once, the rest of a longer one is read again.
+// where rows are short, and twice as many threads where they are long; rows of up to 32768 entries are read once, the rest of a
+// longer one is read again.
 // Measured in a stream of calls: 4096 x 8192 20 us (100 MB, 5.0 TB/s), 1000 x 11008 10.3 us; the first took 1.5 times as long
 // with conversions and 32-bit comparisons.
-template <int DT, int KEEP>
-__global__ void __launch_bounds__(kQtThreads)
+template <int DT, int KEEP, int THREADS = kQtThreads>
+__global__ void __launch_bounds__(THREADS)
 quantize_tokens_kernel(const uint16_t* __restrict__ X, int64_t d, int64_t ldx, int wide, int8_t* __restrict__ codes,
                        int64_t ldc, float* __restrict__ scale, int32_t* __restrict__ nonfinite, int32_t* __restrict__ clear) {
     tc5::dependents_may_start();
@@ -57,20 +58,20 @@ quantize_tokens_kernel(const uint16_t* __restrict__ X, int64_t d, int64_t ldx, i
     uint32_t m = 0;
 #pragma unroll
     for (int i = 0; i < KEEP; ++i) {
-        const int64_t g = t + (int64_t)i * kQtThreads;
+        const int64_t g = t + (int64_t)i * THREADS;
         keep[i] = make_uint4(0u, 0u, 0u, 0u);
         if (g < groups) keep[i] = load8(row + 8 * g, d - 8 * g, wide);
     }
 #pragma unroll
     for (int i = 0; i < KEEP; ++i) m = group_max<DT>(m, keep[i]);
-    for (int64_t g = t + (int64_t)KEEP * kQtThreads; g < groups; g += kQtThreads)
+    for (int64_t g = t + (int64_t)KEEP * THREADS; g < groups; g += THREADS)
         m = group_max<DT>(m, load8(row + 8 * g, d - 8 * g, wide));
-    __shared__ uint32_t part[kQtThreads / 32];
+    __shared__ uint32_t part[THREADS / 32];
     m = __reduce_max_sync(0xffffffffu, max(m & 0x7fffu, m >> 16 & 0x7fffu));  // of magnitudes, as bit patterns
     if ((t & 31) == 0) part[t >> 5] = m;
     __syncthreads();
 #pragma unroll
-    for (int i = 0; i < kQtThreads / 32; ++i) m = max(m, part[i]);
+    for (int i = 0; i < THREADS / 32; ++i) m = max(m, part[i]);
     const float amax = widen16<DT>((uint16_t)m);
     float s = amax * (1.0f / 127.0f), inv = 1.0f / s;
     if (amax < 0x1p-120f) s = inv = 0.0f;
@@ -81,10 +82,10 @@ quantize_tokens_kernel(const uint16_t* __restrict__ X, int64_t d, int64_t ldx, i
     }
 #pragma unroll
     for (int i = 0; i < KEEP; ++i) {
-        const int64_t g = t + (int64_t)i * kQtThreads;
+        const int64_t g = t + (int64_t)i * THREADS;
         if (g < groups) *reinterpret_cast<uint2*>(out + 8 * g) = group_codes<DT>(keep[i], inv);
     }
-    for (int64_t g = t + (int64_t)KEEP * kQtThreads; g < groups; g += kQtThreads)
+    for (int64_t g = t + (int64_t)KEEP * THREADS; g < groups; g += THREADS)
         *reinterpret_cast<uint2*>(out + 8 * g) = group_codes<DT>(load8(row + 8 * g, d - 8 * g, wide), inv);
 }
 
@@ -96,10 +97,7 @@ norm_quantize_kernel(const uint16_t* __restrict__ X, int64_t d, int64_t ldx, int
     tc5::dependents_may_start();
     __shared__ RowParts parts;
     if (threadIdx.x == 0 && clear && blockIdx.x == 0) *clear = 0;  // see the other kernel
-    const uint16_t* row = X + blockIdx.x * ldx;
-    RowHeld<KEEP, true> held;
-    held.load(row, d, wide, norm, threadIdx.x);
-    quantize_row<DT>(held, row, d, wide, norm, codes + blockIdx.x * ldc, scale + blockIdx.x, nonfinite, threadIdx.x, parts, [] { __syncthreads(); });
+    norm_quantize_row<DT, KEEP>(X + blockIdx.x * ldx, d, wide, norm, codes + blockIdx.x * ldc, scale + blockIdx.x, nonfinite, threadIdx.x, parts);
 }
 
 // ---- the product --------------------------------------------------------------------------------------------
@@ -448,7 +446,7 @@ static cmpq_status launch_quantize(const uint16_t* x, int64_t n, int64_t d, int6
     const int wide = aligned_to(x, 16) && ldx % 8 == 0;
     const int64_t keep = (d + 8 * kQtThreads - 1) / (8 * kQtThreads);
     const unsigned rows = (unsigned)n;
-    auto plain = [&](auto kernel) { return launch_cluster(kernel, rows, kQtThreads, 0, 1, false, st, x, d, ldx, wide, codes, ldc, scale, word, clear); };
+    auto plain = [&](auto kernel, int threads) { return launch_cluster(kernel, rows, threads, 0, 1, false, st, x, d, ldx, wide, codes, ldc, scale, word, clear); };
     auto normed = [&](auto kernel) {
         return launch_cluster(kernel, rows, kQtThreads, 0, 1, false, st, x, d, ldx, wide, RowNorm{norm, aligned_to(norm, 16), eps}, codes, ldc, scale, word, clear);
     };
@@ -456,9 +454,10 @@ static cmpq_status launch_quantize(const uint16_t* x, int64_t n, int64_t d, int6
         return keep <= 2   ? normed(norm_quantize_kernel<DT, 2>)
                : keep <= 4 ? normed(norm_quantize_kernel<DT, 4>)
                            : normed(norm_quantize_kernel<DT, 8>);
-    return keep <= 2   ? plain(quantize_tokens_kernel<DT, 2>)
-           : keep <= 4 ? plain(quantize_tokens_kernel<DT, 4>)
-                       : plain(quantize_tokens_kernel<DT, 8>);
+    return keep <= 2   ? plain(quantize_tokens_kernel<DT, 2>, kQtThreads)
+           : keep <= 4 ? plain(quantize_tokens_kernel<DT, 4>, kQtThreads)
+           : keep <= 8 ? plain(quantize_tokens_kernel<DT, 8>, kQtThreads)
+                       : plain(quantize_tokens_kernel<DT, 8, 2 * kQtThreads>, 2 * kQtThreads);
 }
 
 cmpq_status enqueue_quantize(const void* X, cmpq_dtype dt, int64_t n, int64_t d, int64_t ldx, const void* norm, float eps, int8_t* codes, int64_t ldc,

@@ -14,6 +14,8 @@ namespace cmpq {
 // first, activated, multiplies the second.
 enum { kPlain = 0, kFinish = 1, kGated = 2 };
 
+inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
 using Weight8 = cmpq_weight_i8;
 struct TokenCodes {
     const int8_t* codes;

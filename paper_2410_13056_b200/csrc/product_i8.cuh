@@ -28,36 +28,24 @@ __device__ __forceinline__ void all_max_sum(uint32_t& m, float& s, int t, RowPar
     for (int i = 0; i < kQtThreads / 32; ++i) m = max(m, parts.m[i]), s += parts.s[i];
 }
 
-// The squares of eight entries times f, added up as a tree: a row of 16384 entries goes through at most 8 + 3 + 5 + 8
-// additions one after the other.
+// The squares of eight entries times f: a row of 16384 entries goes through at most 8 + 5 + 5 + 8 roundings one after the other.
 __device__ __forceinline__ float sum_squares(const float (&x)[8], float f) {
-    float q[8];
+    float a = 0.0f, b = 0.0f;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) q[i] = x[i] * f * (x[i] * f);
-    return ((q[0] + q[1]) + (q[2] + q[3])) + ((q[4] + q[5]) + (q[6] + q[7]));
+    for (int i = 0; i < 4; ++i) a = __fmaf_rn(x[i] * f, x[i] * f, a), b = __fmaf_rn(x[i + 4] * f, x[i + 4] * f, b);
+    return a + b;
+}
+
+// The larger of m and |v|, a NaN if one of them is.
+__device__ __forceinline__ float larger(float m, float v) {
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(m) : "f"(m), "f"(fabsf(v)));
+    return m;
 }
 
 struct RowNorm {
     const uint16_t* weight;  // or null
     int wide;                // 16-byte aligned
     float eps;
-};
-
-// What a thread keeps of a row and of its norm's weight: KEEP groups of eight, asked for all at once.
-template <int KEEP, bool NORM>
-struct RowHeld {
-    uint4 x[KEEP], w[NORM ? KEEP : 1];
-
-    __device__ __forceinline__ void load(const uint16_t* row, int64_t d, bool wide, const RowNorm& norm, int t) {
-#pragma unroll
-        for (int i = 0; i < KEEP; ++i) {
-            const int64_t g = t + (int64_t)i * kQtThreads;
-            x[i] = make_uint4(0u, 0u, 0u, 0u);
-            if (NORM) w[i] = x[i];
-            if (8 * g < d) x[i] = load8(row + 8 * g, d - 8 * g, wide);
-            if (NORM && 8 * g < d) w[i] = load8(norm.weight + 8 * g, d - 8 * g, norm.wide);
-        }
-    }
 };
 
 // Codes of eight values: |v * inv| is at most 127 (1 + 2^-22), so adding 1.5 * 2^23 leaves the integer that rounding to even
@@ -78,53 +66,74 @@ __device__ __forceinline__ float2 scale_of(float amax) {
     return amax < 0x1p-120f ? make_float2(0.0f, 0.0f) : make_float2(s, 1.0f / s);
 }
 
-// Codes and scale of a row by 256 threads (t is a thread's number, sync() their barrier), behind a root-mean-square norm where
-// NORM.  A row's codes do not depend on its norm: code = rint(v 127 / max|v|) with v = x g, whatever v is divided by; the norm
-// enters the scale alone.  So nothing waits for the sum of squares, and the codes are as exact as without a norm.  v is one
-// fp32 product, so magnitudes are compared in fp32 here.  A sum that passes fp32 (entries above 2^54 or so) is taken again of
-// entries times 2^-80; entries that vanish there vanish beside it too.  What is not held is read again.
-template <int DT, int KEEP, bool NORM, class Sync>
-__device__ __forceinline__ void quantize_row(const RowHeld<KEEP, NORM>& held, const uint16_t* row, int64_t d, bool wide, const RowNorm& norm, int8_t* out,
-                                             float* scale, int32_t* nonfinite, int t, RowParts& parts, Sync sync) {
+// Codes and scale of a row behind a root-mean-square norm, by 256 threads (t is a thread's number).  A row's codes do not depend
+// on its norm: code = rint(v 127 / max|v|) with v = x g, whatever v is divided by; the norm enters the scale alone.  So nothing
+// waits for the sum of squares, and the codes are as exact as without a norm.  v is one fp32 product, so magnitudes are
+// compared in fp32.  A sum that passes fp32 (entries above 2^54 or so) is taken again of entries times 2^-80; entries that vanish
+// there vanish beside it too.  A thread keeps v of KEEP groups of eight; what is longer is read again.
+template <int DT, int KEEP>
+__device__ __forceinline__ void norm_quantize_row(const uint16_t* row, int64_t d, bool wide, const RowNorm& norm, int8_t* out, float* scale,
+                                                  int32_t* nonfinite, int t, RowParts& parts) {
     const int64_t groups = (d + 15) / 16 * 2;  // the codes' padding up to 16 is written too
-    auto load = [&](const uint16_t* p, int64_t g, bool on_16) { return load8(p + 8 * g, d - 8 * g, on_16); };
-    // f(group, its entries, v) for the thread's groups
-    auto every = [&](auto f) {
-        float x[8], v[8];
-        auto one = [&](int64_t g, uint4 rx, uint4 rw) {
-            widen8<DT>(rx, x);
-            if (NORM) widen8<DT>(rw, v);
+    const auto sync = [] { __syncthreads(); };
+    uint4 x[KEEP], w[KEEP];
+    float v[KEEP][8], e[8];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] = NORM ? x[j] * v[j] : x[j];
-            f(g, x, v);
-        };
+    for (int i = 0; i < KEEP; ++i) {
+        const int64_t g = t + (int64_t)i * kQtThreads;
+        x[i] = w[i] = make_uint4(0u, 0u, 0u, 0u);
+        if (8 * g < d) x[i] = load8(row + 8 * g, d - 8 * g, wide), w[i] = load8(norm.weight + 8 * g, d - 8 * g, norm.wide);
+    }
+    auto weighted = [&](int64_t g, float (&p)[8]) {
+        widen8<DT>(load8(row + 8 * g, d - 8 * g, wide), e);
+        widen8<DT>(load8(norm.weight + 8 * g, d - 8 * g, norm.wide), p);
 #pragma unroll
-        for (int i = 0; i < KEEP; ++i) {
-            const int64_t g = t + (int64_t)i * kQtThreads;
-            if (g < groups) one(g, held.x[i], held.w[NORM ? i : 0]);
-        }
-        for (int64_t g = t + (int64_t)KEEP * kQtThreads; g < groups; g += kQtThreads)
-            one(g, load(row, g, wide), NORM ? load(norm.weight, g, norm.wide) : make_uint4(0u, 0u, 0u, 0u));
+        for (int j = 0; j < 8; ++j) p[j] = e[j] * p[j];
     };
-    uint32_t m = 0;
-    float sum = 0.0f;
-    every([&](int64_t, const float(&x)[8], const float(&v)[8]) {
+    float most = 0.0f, sum = 0.0f;
+    auto look = [&](const float (&p)[8]) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) m = max(m, __float_as_uint(v[j]) & 0x7fffffffu);  // as bit patterns: NaN above infinity
-        if (NORM) sum += sum_squares(x, 1.0f);
-    });
+        for (int j = 0; j < 8; ++j) most = larger(most, p[j]);
+        sum += sum_squares(e, 1.0f);
+    };
+#pragma unroll
+    for (int i = 0; i < KEEP; ++i) {
+        widen8<DT>(x[i], e);
+        widen8<DT>(w[i], v[i]);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[i][j] = e[j] * v[i][j];
+        look(v[i]);
+    }
+    for (int64_t g = t + (int64_t)KEEP * kQtThreads; g < groups; g += kQtThreads) {
+        float p[8];
+        weighted(g, p);
+        look(p);
+    }
+    uint32_t m = __float_as_uint(most);  // compared as bit patterns from here on: NaN above infinity
     all_max_sum(m, sum, t, parts, sync);
     float2 s = scale_of(__uint_as_float(m));
-    every([&](int64_t g, const float(&)[8], const float(&v)[8]) { *reinterpret_cast<uint2*>(out + 8 * g) = round_codes(v, s.y); });
+#pragma unroll
+    for (int i = 0; i < KEEP; ++i) {
+        const int64_t g = t + (int64_t)i * kQtThreads;
+        if (g < groups) *reinterpret_cast<uint2*>(out + 8 * g) = round_codes(v[i], s.y);
+    }
+    for (int64_t g = t + (int64_t)KEEP * kQtThreads; g < groups; g += kQtThreads) {
+        float p[8];
+        weighted(g, p);
+        *reinterpret_cast<uint2*>(out + 8 * g) = round_codes(p, s.y);
+    }
     float f = 1.0f;
-    if (NORM && sum > FLT_MAX && m < 0x7f800000u) {  // the same in all threads; not a row with a NaN
+    if (sum > FLT_MAX && m < 0x7f800000u) {  // the same in all threads; not a row with a NaN
         f = 0x1p-80f, sum = 0.0f;
-        every([&](int64_t, const float(&x)[8], const float(&)[8]) { sum += sum_squares(x, f); });
+        for (int64_t g = t; 8 * g < d; g += kQtThreads) {
+            widen8<DT>(load8(row + 8 * g, d - 8 * g, wide), e);
+            sum += sum_squares(e, f);
+        }
         sync();  // the parts have been read
         all_max_sum(m, sum, t, parts, sync);
     }
     if (t == 0) {
-        if (NORM && s.x > 0.0f) s.x *= f / sqrtf(sum / (float)d + norm.eps * f * f);
+        if (s.x > 0.0f) s.x *= f / sqrtf(sum / (float)d + norm.eps * f * f);
         *scale = s.x;
         if (m >= 0x7f800000u && nonfinite) atomicOr(nonfinite, 1);
     }

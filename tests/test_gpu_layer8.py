@@ -126,6 +126,31 @@ def test_norm_quantize_strides_and_extremes(dtype):
     assert torch.equal(same[0], codes[:, :200]) and torch.equal(same[1], scale)
 
 
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("n,d", [(1024, 1), (1025, 4096), (1031, 511), (1500, 4104), (1100, 8192), (1027, 5003), (1025, 16384), (1030, 12801), (1024, 16400)])
+def test_many_rows_have_the_bytes_of_few(n, d, dtype):
+    x, g = _tokens(n, d, dtype, n), _norm(d, dtype, d)
+    x[7] = 0
+    if dtype == torch.bfloat16:
+        x[9] = (x[9].float() * 2.0 ** 100).to(dtype)
+        x[11] = (x[11].float() * 2.0 ** -60).to(dtype)
+    for view, w in ((x, g), (x[:, 1:], g[1:].clone())) if d > 1 else ((x, g),):
+        codes, scale = serving.quantize_tokens(view, w, EPS)
+        for lo in (0, n - 500):
+            c, s = serving.quantize_tokens(view[lo: lo + 500], w, EPS)
+            assert torch.equal(codes[lo: lo + 500], c) and torch.equal(scale[lo: lo + 500], s)
+    c, s, rel = ref.norm_quantize(_np(x[:20]), _np(g), EPS)
+    codes, scale = serving.quantize_tokens(x, g, EPS)
+    assert np.array_equal(codes[:20].cpu().numpy(), c) and np.all(np.abs(scale[:20].cpu().numpy() - s) <= rel * s)
+    word = torch.zeros(1, dtype=torch.int32, device="cuda")
+    x[n - 1, d - 1] = float("nan")
+    room = torch.full((n, (d + 15) // 16 * 16 + 16), 99, dtype=torch.int8, device="cuda")
+    B.cmpq_norm_quantize_tokens(x, g, EPS, room[:, :d], scale, word)
+    assert int(word) == 1 and torch.equal(room[: n - 1, :d], codes[: n - 1])
+    pad = (d + 15) // 16 * 16
+    assert torch.all(room[: n - 1, d: pad] == 0) and torch.all(room[:, pad:] == 99)
+
+
 # ---- linear layer ----------------------------------------------------------------------------------------------
 
 SIZES = [(1, 1, 1), (1, 512, 129), (2, 100, 33), (4, 4097, 1000), (3, 12800, 300), (1, 12801, 96), (4, 64, 40000), (1, 4096, 19000), (7, 1000, 64), (9, 130, 257), (31, 33, 31), (65, 300, 513), (128, 128, 256), (129, 1025, 257),
