@@ -65,6 +65,8 @@ int64_t rows(const Tensor& t, const char* name) {
     return n > 1 ? t.stride(0) : width;
 }
 
+bool capturing() { return c10::cuda::currentStreamCaptureStatusMayInitCtx() != c10::cuda::CaptureStatus::None; }
+
 // Work spaces.  Eager calls of a device and stream share one buffer (they run one after the other), whatever layer or cache
 // they are of.  A call that is being captured takes its own from the graph's memory, zeroed by a node of that graph, and
 // leaves nothing behind: a graph never depends on another one, on eager calls, or on the stream that it is replayed on.
@@ -73,7 +75,7 @@ struct Spaces {
     std::map<std::pair<int, void*>, Tensor> held;
 
     Tensor get(const at::Device& device, void* stream, size_t bytes) {
-        if (c10::cuda::currentStreamCaptureStatusMayInitCtx() != c10::cuda::CaptureStatus::None) return fresh(device, bytes);
+        if (capturing()) return fresh(device, bytes);
         Tensor& t = held[{device.index(), stream}];
         if (!t.defined() || (size_t)t.numel() < bytes) t = fresh(device, bytes);
         return t;
@@ -211,8 +213,7 @@ struct Gated {
     }
 
     Tensor state(void* stream) {
-        const bool captured = c10::cuda::currentStreamCaptureStatusMayInitCtx() != c10::cuda::CaptureStatus::None;
-        return captured && taken < kCaptured ? kept[taken++] : gated_states().get(word.device(), stream, CMPQ_GATED_STATE_BYTES);
+        return capturing() && taken < kCaptured ? kept[taken++] : gated_states().get(word.device(), stream, CMPQ_GATED_STATE_BYTES);
     }
 
     Tensor call(const Tensor& x, const OptTensor& into, const OptTensor& residual, const OptTensor& norm, double eps) {

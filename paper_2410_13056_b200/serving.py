@@ -79,6 +79,8 @@ class GatedMLP8:
         self.gate, self.up, self.down, self.activation = gate, up, down, activation
         self.d_in, self.d_ff, self.d_out = gate.d_in, gate.d_out, down.d_out
         self.word = self._impl.word
+        if not torch.cuda.is_current_stream_capturing():  # what the block keeps is there before its graphs run, on any stream
+            torch.cuda.current_stream(self.word.device).synchronize()
 
     def __call__(self, x, out=None, *, residual=None, norm=None, eps=1e-6):
         """x: fp16/bf16 [n][d_in].  Returns out [n][d_out] of x's dtype: block(x) + residual; residual, norm and eps as for

@@ -10,13 +10,17 @@
     python profile_cases.py stack --config c4_stack7b --budget 3.0
     python profile_cases.py layer --config c3_mlp7b --layer 0 --budget 3.0 --launches 5
     python profile_cases.py linear8 --tokens 37 --d-in 4096 --d-out 11008 --launches 20
+    python profile_cases.py linear8 --tokens 4000 --d-in 4096 --d-out 11008 --norm --act silu --launches 20
+    python profile_cases.py gated8 --tokens 1 --d-in 4096 --d-out 11008 --norm --launches 20
     python profile_cases.py attend8 --streams 24 --tokens 8191 --new 1 --heads 64 --kv-heads 8 --launches 3
     python profile_cases.py append8 --streams 5 --tokens 4096 --new 2048 --heads 64 --kv-heads 8 --launches 3
     python profile_cases.py serve --streams 8 --tokens 1000 --heads 32 --kv-heads 32 --launches 32
+    python profile_cases.py serve --streams 8 --tokens 1000 --heads 32 --kv-heads 32 --d-ff 11008 --launches 32
 
 `layer` runs the whole pass on one layer of a named workload and prints the time per C-ABI call.
 `serve` runs an attention block in 8 bits (projections, append with rotation, attention over the cache, output) on
-the prompts of some streams and then token by token; `linear8`, `append8` and `attend8` are its single calls.
+the prompts of some streams and then token by token, with --d-ff a whole decoder layer (norms, residual sums and the
+gated feed-forward block too); `linear8`, `gated8`, `append8` and `attend8` are its single calls.
 `stack` quantizes every layer of a multi-block workload (all 32 x 7 layers of the Llama-7B-shaped stack) and
 prints the total device time of the passes; under torchrun the layers are dealt round-robin to the ranks.
 
@@ -218,9 +222,27 @@ def run_linear8(a):
               for _ in range(max(1, min(16, int(3e8 // (a.d_in * a.d_out)))))]
     x = inputs.make_activations(a.tokens, a.d_in, inputs.BF16 if a.dtype == "bf16" else inputs.F16, 1, device="cuda")
     y = torch.empty(a.tokens, a.d_out, dtype=dt, device="cuda")
-    ms = _timed(lambda: [layer(x, out=y) for layer in layers], a.launches) / len(layers)
+    norm = torch.ones(a.d_in, dtype=dt, device="cuda") if a.norm else None
+    ms = _timed(lambda: [layer(x, out=y, activation=a.act, norm=norm) for layer in layers], a.launches) / len(layers)
     print("linear8: %d tokens, %d -> %d, %s: %.4f ms per layer (%.0f GB/s of weights, %.0f TOP/s)"
           % (a.tokens, a.d_in, a.d_out, a.dtype, ms, a.d_in * a.d_out / ms / 1e6, 2 * a.tokens * a.d_in * a.d_out / ms / 1e9))
+
+
+def run_gated8(a):
+    """The gated block d_in -> d_out -> d_in behind its norm, added to its input."""
+    from paper_2410_13056_b200 import serving
+
+    dt = torch.bfloat16 if a.dtype == "bf16" else torch.float16
+    weight = lambda o, i: serving.Int8Linear.from_weight((torch.randn(o, i, device="cuda") * 0.02).to(dt))
+    blocks = [serving.GatedMLP8(weight(a.d_out, a.d_in), weight(a.d_out, a.d_in), weight(a.d_in, a.d_out), activation=a.act or "silu")
+              for _ in range(max(1, min(8, int(3e8 // (3 * a.d_in * a.d_out)))))]
+    x = inputs.make_activations(a.tokens, a.d_in, inputs.BF16 if a.dtype == "bf16" else inputs.F16, 1, device="cuda")
+    y = torch.empty_like(x)
+    norm = torch.ones(a.d_in, dtype=dt, device="cuda") if a.norm else None
+    ms = _timed(lambda: [block(x, out=y, residual=x, norm=norm) for block in blocks], a.launches) / len(blocks)
+    work = 3 * a.d_in * a.d_out
+    print("gated8: %d tokens, %d -> %d -> %d, %s: %.4f ms per block (%.0f GB/s of weights, %.0f TOP/s)"
+          % (a.tokens, a.d_in, a.d_out, a.d_in, a.dtype, ms, work / ms / 1e6, 2 * a.tokens * work / ms / 1e9))
 
 
 def _served(a, length):
@@ -305,6 +327,16 @@ def run_serve(a):
     p = (q @ k.transpose(1, 2) / math.sqrt(d)).masked_fill(torch.ones(n, n, device="cuda", dtype=torch.bool).triu(1), -math.inf).softmax(-1)
     want = (p @ v).transpose(0, 1).flatten(1) @ wo.float().t()
     print("   first stream against fp32: relative error %.4f" % float((y[:n].float() - want).norm() / want.norm()))
+    if a.d_ff:  # from here on the whole layer
+        mlp = [(torch.randn(o, i, device="cuda", generator=g) * i ** -0.5).to(dt) for o, i in ((a.d_ff, d_model), (a.d_ff, d_model), (d_model, a.d_ff))]
+        norms = [(1.0 + 0.1 * torch.randn(d_model, device="cuda", generator=g)).to(dt) for _ in range(2)]
+        layer = serving.DecoderLayer8(layer, serving.GatedMLP8(*map(serving.Int8Linear.from_weight, mlp)), *norms)
+        ms = _timed(lambda: layer(x, *args, max_new=max(new), max_len=a.tokens), 3)
+        mid = layer.attention(x, *args, max_new=max(new), max_len=a.tokens, residual=x, norm=norms[0])[:n].float()
+        y = layer(x, *args, max_new=max(new), max_len=a.tokens)[:n].float()
+        v = mid / (mid.square().mean(1, keepdim=True) + layer.eps).sqrt() * norms[1].float()
+        want = (torch.nn.functional.silu(v @ mlp[0].float().t()) * (v @ mlp[1].float().t())) @ mlp[2].float().t()
+        print("   whole layer: %.3f ms; its feed-forward block against fp32: relative error %.4f" % (ms, float((y - mid - want).norm() / want.norm())))
     one = _i32(list(range(a.streams + 1)))
     token = torch.randn(a.streams, d_model, device="cuda", generator=g).to(dt)
     lens = args[1].clone()
@@ -316,13 +348,13 @@ def run_serve(a):
         token = layer(token, one, lens, table, max_new=1, max_len=a.tokens + a.launches)
     e1.record()
     layer.check()
-    print("   generation: %.4f ms a token and block for %d streams" % (e0.elapsed_time(e1) / a.launches, a.streams))
+    print("   generation: %.4f ms a token and %s for %d streams" % (e0.elapsed_time(e1) / a.launches, "layer" if a.d_ff else "block", a.streams))
 
 
 def main():
     ap = argparse.ArgumentParser()
     ap.add_argument("case", choices=["lloyd", "stats", "pack", "outliers", "protect", "layer", "matvec", "stack", "transpose", "sweep",
-                                     "linear8", "append8", "attend8", "serve"])
+                                     "linear8", "gated8", "append8", "attend8", "serve"])
     ap.add_argument("--config", default="c2_attn7b")
     ap.add_argument("--layer", type=int, default=0)
     ap.add_argument("--budget", type=float, default=3.0)
@@ -339,6 +371,9 @@ def main():
     ap.add_argument("--kv-heads", type=int, default=32)
     ap.add_argument("--head-dim", type=int, default=128)
     ap.add_argument("--page", type=int, default=64)
+    ap.add_argument("--d-ff", type=int, default=0, help="serve case: a whole decoder layer with a feed-forward block of this width")
+    ap.add_argument("--norm", action="store_true", help="linear8 and gated8: behind a root-mean-square norm")
+    ap.add_argument("--act", default=None, choices=["none", "relu", "silu", "gelu", "gelu_tanh"], help="linear8 and gated8: the activation")
     ap.add_argument("--fused", action="store_true",
                     help="layer case: outlier protection and final fit through cmpq_protect_and_quantize")
     ap.add_argument("--weighted", action="store_true",
@@ -349,8 +384,8 @@ def main():
     dt = inputs.BF16 if a.dtype == "bf16" else inputs.F16
     torch.cuda.set_device(int(os.environ.get("LOCAL_RANK", "0")))
     B.cmpq_set_lloyd_assignment(B.ASSIGN_ALL_PAIRS if a.assign == "all_pairs" else B.ASSIGN_ORDERED)
-    if a.case in ("linear8", "append8", "attend8", "serve"):
-        {"linear8": run_linear8, "serve": run_serve}.get(a.case, run_cache8)(a)
+    if a.case in ("linear8", "gated8", "append8", "attend8", "serve"):
+        {"linear8": run_linear8, "gated8": run_gated8, "serve": run_serve}.get(a.case, run_cache8)(a)
         return
     if a.case == "layer":
         run_layer(a)

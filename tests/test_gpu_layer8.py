@@ -330,6 +330,51 @@ def test_reports():
         assert e.value.status == 6
 
 
+@pytest.mark.parametrize("n", [1, 4])
+def test_reports_of_the_one_kernel(n):
+    d, ff = 1024, 6000
+    block, x = _block(n, d, ff, d, torch.float16, "silu", True), _tokens(n, d, torch.float16, 1)
+    y = block(x)
+    block.check()
+    for value, at in ((float("nan"), n - 1), (float("inf"), 0)):
+        bad = x.clone()
+        bad[at, 1000] = value
+        z = block(bad)
+        with pytest.raises(B.CmpqError) as e:
+            block.check()
+        keep = [i for i in range(n) if i != at]
+        assert e.value.status == 6 and torch.equal(z[keep], y[keep])
+    huge = x.clone()
+    huge[0] *= 1000                                       # its h passes fp16
+    z = block(huge)
+    with pytest.raises(B.CmpqError) as e:
+        block.check()
+    assert e.value.status == 6 and torch.equal(z[1:], y[1:])
+    assert torch.equal(block(x), y)
+    block.check()
+
+
+@pytest.mark.parametrize("d,ff", [(64, 200), (1024, 6000)])
+@pytest.mark.parametrize("n", [1, 3, 20, 300])
+def test_rows_of_zeros(n, d, ff):
+    """A token of zeros, and an h of zeros: what is left is the bias, activated where there is an activation, and the residual."""
+    dtype = torch.bfloat16
+    x = _tokens(n, d, dtype, 2)
+    x[0] = 0
+    block, g = _block(n, d, ff, d, dtype, "relu", False), _norm(d, dtype, 1)
+    y = block(x, residual=x, norm=g)
+    assert torch.all(y[0] == 0)
+    assert torch.all(block.gate(x, activation="gelu", norm=g)[0] == 0)
+    b = torch.linspace(-3, 3, ff).to(dtype).cuda()
+    layer = serving.Int8Linear(block.gate.w_codes, block.gate.w_scale, b)
+    assert torch.equal(layer(x, activation="relu", norm=g)[0], b.clamp(min=0))
+    dead = serving.Int8Linear(block.gate.w_codes, block.gate.w_scale * 0, torch.full((ff,), -1.0, dtype=dtype, device="cuda"))
+    down = serving.Int8Linear(block.down.w_codes, block.down.w_scale, b[:d].clone() if d <= ff else None)
+    y = serving.GatedMLP8(dead, block.up, down, "relu")(x, residual=x)
+    assert torch.equal(y, (x.float() + down.bias.float()).to(dtype))
+    block.check()
+
+
 def test_no_tokens_and_refusals():
     dtype = torch.float16
     block = _block(1, 64, 100, 48, dtype, "silu", True)
@@ -481,6 +526,29 @@ def test_decoder_layer_refuses_parts_that_do_not_fit():
 
 
 SERVED = (1, 4, 64, 400)
+
+
+def test_more_captured_calls_than_a_block_has_states_for():
+    d, ff, dtype = 1024, 6000, torch.float16
+    block, x, g = _block(1, d, ff, d, dtype, "silu", False), _tokens(2, d, dtype, 1), _norm(d, dtype, 2)
+    want = [x]
+    for _ in range(75):
+        want.append(block(want[-1], norm=g))
+    graphs, out, at = [], [], x
+    for part in range(3):                                 # each graph goes on from the one before it
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            for _ in range(25):
+                at = block(at, norm=g)
+        graphs.append(graph), out.append(at)
+    for _ in range(4):
+        for graph in graphs:
+            graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(out[i], want[25 * i + 25]) for i in range(3))
+        for t in out:
+            t.zero_()
+    block.check()
 
 
 @pytest.mark.parametrize("d,ff", [(256, 1000), (1024, 6000)])
