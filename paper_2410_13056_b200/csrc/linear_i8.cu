@@ -268,22 +268,30 @@ matmul_i8_pair_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_con
     tc5::cluster_sync();
     tc5::fence_after_sync();
     const uint32_t tmem = tmem_at;
-    tc5::wait_for_previous();
     if (warp == 0) {
         if (tc5::elect_one()) {
             int slot = 0, phase = 1;  // a new barrier counts as empty
             bool ok = true;
+            auto weights = [&](int nt, int k) {  // and both operands' bytes of both CTAs, whoever comes first
+                if (rank == 0) tc5::mbar_expect_tx(full + slot, 2 * (128 + half) * 128);
+                uint8_t* at = smem + slot * kPairStageBytes + 128 * 128;
+                if (KIND == kGated)
+                    tc5::tma_load_2d_pair(at, rank ? &umap : &wmap, full + slot, k * 128, nt * half);
+                else
+                    tc5::tma_load_2d_pair(at, &wmap, full + slot, k * 128, nt * A.bn + rank * half);
+            };
+            const int early = first < tiles ? min(kPairStages, A.kblocks) : 0;  // stages of weights that do not wait for the tokens
+            for (slot = 0; slot < early; ++slot) weights(first / A.m_tiles, slot);
+            slot = 0;
+            tc5::wait_for_previous();
             for (int tile = first; ok && tile < tiles; tile += step) {
                 const int mt = tile % A.m_tiles, nt = tile / A.m_tiles;
                 for (int k = 0; k < A.kblocks; ++k) {
-                    if (!(ok = tc5::mbar_wait<true>(empty + slot, phase, &failed))) break;
-                    if (rank == 0) tc5::mbar_expect_tx(full + slot, 2 * (128 + half) * 128);
-                    uint8_t* at = smem + slot * kPairStageBytes;
-                    tc5::tma_load_2d_pair(at, &xmap, full + slot, k * 128, mt * 256 + rank * 128);
-                    if (KIND == kGated)
-                        tc5::tma_load_2d_pair(at + 128 * 128, rank ? &umap : &wmap, full + slot, k * 128, nt * half);
-                    else
-                        tc5::tma_load_2d_pair(at + 128 * 128, &wmap, full + slot, k * 128, nt * A.bn + rank * half);
+                    if (tile != first || k >= early) {
+                        if (!(ok = tc5::mbar_wait(empty + slot, phase, &failed))) break;
+                        weights(nt, k);
+                    }
+                    tc5::tma_load_2d_pair(smem + slot * kPairStageBytes, &xmap, full + slot, k * 128, mt * 256 + rank * 128);
                     if (++slot == kPairStages) slot = 0, phase ^= 1;
                 }
             }
@@ -297,7 +305,7 @@ matmul_i8_pair_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_con
                 if (!tc5::mbar_wait<true>(acc_empty + acc, acc_phase, &failed)) break;
                 tc5::fence_after_sync();
                 for (int k = 0; k < A.kblocks; ++k) {
-                    if (!(ok = tc5::mbar_wait<true>(full + slot, phase, &failed))) break;
+                    if (!(ok = tc5::mbar_wait(full + slot, phase, &failed))) break;
                     tc5::fence_after_sync();
                     const uint32_t at = tc5::smem_addr(smem + slot * kPairStageBytes);
                     const uint64_t a = tc5::desc_k_sw128(at), b = tc5::desc_k_sw128(at + 128 * 128);
@@ -315,6 +323,7 @@ matmul_i8_pair_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_con
     } else {
         const int quad = warp & 3, upper = warp >= 6, i = threadIdx.x - 64;
         float xs = 0.0f;
+        tc5::wait_for_previous();
         walk_tiles(
             first, tiles, step,
             [&](int tile, int acc) {
@@ -326,7 +335,7 @@ matmul_i8_pair_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_con
                     ask_for(A.residual + (int64_t)t * A.ldr + o0, min(upper * half, A.d_out - o0), min(upper * half + half, A.d_out - o0));
                 asm volatile("bar.sync 1, 256;" ::: "memory");
             },
-            [&](int acc, int parity) { return tc5::mbar_wait_warp<true>(acc_full + acc, parity, &failed); },
+            [&](int acc, int parity) { return tc5::mbar_wait_warp(acc_full + acc, parity, &failed); },
             [&](int tile, int acc) {
                 const int o0 = tile / A.m_tiles * wide_tile, row0 = tile % A.m_tiles * 256 + rank * 128 + quad * 32, t = row0 + lane;
                 const int left = min(wide_tile, A.d_out - o0), c0 = upper * (wide_tile / 2), c1 = c0 + wide_tile / 2;
