@@ -5,22 +5,29 @@ namespace cmpq {
 
 struct FewProduct {
     TokenRows x;
-    ProductArgs p;  // bn: channels of a tile; stages, per_stage
-    int ring;
+    ProductArgs p;      // bn: channels of a tile; kblocks: of a slice; stages, per_stage
+    int slices, rows;   // of the sum; of the tokens' operand
+    int ring, reduce;   // where the tokens' codes and the slices' sums begin in shared memory
+    int behind;         // the kernel in front of this one writes the tokens
 };
 
 // A block takes tiles of up to 128 channels (of both projections where KIND is kGated), the accumulator's rows; the tokens are
 // its columns: an instruction reads 128 rows of its first operand whatever they hold (40 cycles for up to 32 columns), so it
-// should hold the weights.  Launched behind a kernel that writes its tokens, a block asks for its first weights before that
-// has ended.
-// Measured in graphs, weights from memory, against the quantization and the tile kernel, one token: 4096 -> 4096 8.0 us and 9.2,
-// 4096 -> 11008 10.9 and 12.3, 512 -> 512 4.3 and 4.4 (in eager calls 6.1 and 9.2: one launch).
+// should hold the weights.  Where the channels are spread over all SMs and a tile has 64 or 32 of them, its sum is cut into two
+// or four slices, each with rows and columns of its own: an instruction then takes as many blocks of the sum, what a slice's
+// rows make of another one's columns is left, and the slices are added up at the end (a token 4096 -> 4096 takes 32
+// instructions instead of 128, 2 us less).  Launched behind a kernel that writes its tokens, a block asks for its first
+// weights before that has ended.
+// Measured in graphs, weights from memory, against the quantization and the tile kernel, one token: 4096 -> 4096 6.9 us and 9.2,
+// 4096 -> 11008 11.2 and 12.2, 512 -> 512 4.5 and 4.4; in eager calls, where a launch more counts, 8.2 and 10.4, 12.4 and 14.4,
+// 6.2 and 9.1.  Of the 6.9 the weights' way takes 2.8; launch, the tokens' loads and sums and the products take turns.
 template <int DT, bool NORM, int KIND>
 __global__ void __launch_bounds__(kFewThreads, 1)
 few_product_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__ CUtensorMap umap, const __grid_constant__ FewProduct A) {
     extern __shared__ uint8_t raw[];
     uint8_t* smem = raw + ((1024u - (tc5::smem_addr(raw) & 1023u)) & 1023u);
     uint8_t* tokens = smem + A.ring;
+    int32_t* reduce = reinterpret_cast<int32_t*>(smem + A.reduce);
     __shared__ uint64_t full[kFewMaxStages], empty[kFewMaxStages], acc_full[2], acc_empty[2], tokens_there;
     __shared__ TokenParts parts;
     __shared__ float scale[kFewTokens];
@@ -28,8 +35,11 @@ few_product_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_consta
     __shared__ int failed;
     const ProductArgs& P = A.p;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, n = A.x.n, t = (int)threadIdx.x - 64;  // t: of the computing threads
-    const int tile_bytes = P.bn * 128, block_bytes = KIND == kGated ? 2 * tile_bytes : tile_bytes;    // of a block of the sum
-    if (threadIdx.x < kFewMaxStages) tc5::mbar_init(full + threadIdx.x, 1), tc5::mbar_init(empty + threadIdx.x, 1);
+    const int S = A.slices, high = 128 / S, box_bytes = P.bn * 128, slice_bytes = S == 1 ? box_bytes : high * 128;
+    const int half_bytes = S * slice_bytes, block_bytes = KIND == kGated ? 2 * half_bytes : half_bytes;  // of a projection, of a block of all slices
+    const int all = (P.n_tiles - 1 - blockIdx.x) / gridDim.x + 1;  // tiles
+    TokenGroup held[kFewHeld];
+    if (threadIdx.x < P.stages) tc5::mbar_init(full + threadIdx.x, 1), tc5::mbar_init(empty + threadIdx.x, 1);
     if (threadIdx.x == 0) {
         for (int i = 0; i < 2; ++i) tc5::mbar_init(acc_full + i, 1), tc5::mbar_init(acc_empty + i, 4);
         tc5::mbar_init(&tokens_there, 8);
@@ -37,25 +47,27 @@ few_product_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_consta
     }
     tc5::mbar_init_fence();
     if (warp == 1) tc5::tmem_alloc<1>(&tmem_at, 64);
+    if (warp >= 2 && !A.behind) load_tokens<NORM>(A.x, held, t);  // ahead of the weights
+    tc5::dependents_may_start();
     tc5::fence_before_sync();
     __syncthreads();
     tc5::fence_after_sync();
-    tc5::dependents_may_start();
     const uint32_t tmem = tmem_at;
     if (warp == 0) {
         if (tc5::elect_one()) {
             int slot = 0, phase = 1;  // a new barrier counts as empty
             bool ok = true;
-            for (int tile = blockIdx.x; ok && tile < P.n_tiles; tile += gridDim.x)
+            for (int i = 0, tile = blockIdx.x; ok && i < all; ++i, tile += gridDim.x)
                 for (int k = 0; k < P.kblocks; k += P.per_stage) {
                     if (!(ok = tc5::mbar_wait(empty + slot, phase, &failed))) break;
                     const int count = min(P.per_stage, P.kblocks - k);
                     uint8_t* at = smem + slot * P.per_stage * block_bytes;
-                    tc5::mbar_expect_tx(full + slot, count * block_bytes);
-                    for (int i = k; i < k + count; ++i, at += block_bytes) {
-                        tc5::tma_load_2d(at, &wmap, full + slot, i * 128, tile * P.bn);
-                        if (KIND == kGated) tc5::tma_load_2d(at + tile_bytes, &umap, full + slot, i * 128, tile * P.bn);
-                    }
+                    tc5::mbar_expect_tx(full + slot, count * S * (KIND == kGated ? 2 : 1) * box_bytes);
+                    for (int b = k; b < k + count; ++b, at += block_bytes)
+                        for (int q = 0; q < S; ++q) {
+                            tc5::tma_load_2d(at + q * slice_bytes, &wmap, full + slot, (q * P.kblocks + b) * 128, tile * P.bn);
+                            if (KIND == kGated) tc5::tma_load_2d(at + half_bytes + q * slice_bytes, &umap, full + slot, (q * P.kblocks + b) * 128, tile * P.bn);
+                        }
                     if (++slot == P.stages) slot = 0, phase ^= 1;
                 }
         }
@@ -64,7 +76,7 @@ few_product_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_consta
             const uint32_t idesc = tc5::idesc_i8(128, kFewColumns);
             int slot = 0, phase = 0, acc = 0, acc_phase = 1;
             bool ok = tc5::mbar_wait(&tokens_there, 0, &failed);
-            for (int tile = blockIdx.x; ok && tile < P.n_tiles; tile += gridDim.x) {
+            for (int i = 0; ok && i < all; ++i) {
                 if (!(ok = tc5::mbar_wait(acc_empty + acc, acc_phase, &failed))) break;
                 tc5::fence_after_sync();
                 const uint32_t into = tmem + acc * 2 * kFewColumns;
@@ -73,11 +85,11 @@ few_product_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_consta
                     if (!(ok = tc5::mbar_wait(full + slot, phase, &failed))) break;
                     tc5::fence_after_sync();
                     uint64_t w = tc5::desc_k_sw128(tc5::smem_addr(smem + slot * P.per_stage * block_bytes));  // counts 16 bytes
-                    for (int i = k; i < min(k + P.per_stage, P.kblocks); ++i, x += kFewRows * 8, w += block_bytes / 16)
+                    for (int b = k; b < min(k + P.per_stage, P.kblocks); ++b, x += A.rows * 8, w += block_bytes / 16)
 #pragma unroll
                         for (int j = 0; j < 4; ++j) {
-                            tc5::mma_i8<1>(into, w + 2 * j, x + 2 * j, idesc, (i | j) != 0);
-                            if (KIND == kGated) tc5::mma_i8<1>(into + kFewColumns, w + tile_bytes / 16 + 2 * j, x + 2 * j, idesc, (i | j) != 0);
+                            tc5::mma_i8<1>(into, w + 2 * j, x + 2 * j, idesc, (b | j) != 0);
+                            if (KIND == kGated) tc5::mma_i8<1>(into + kFewColumns, w + half_bytes / 16 + 2 * j, x + 2 * j, idesc, (b | j) != 0);
                         }
                     tc5::mma_commit(empty + slot);
                     if (++slot == P.stages) slot = 0, phase ^= 1;
@@ -88,17 +100,26 @@ few_product_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_consta
             }
         }
     } else {
-        tc5::wait_for_previous();
-        quantize_tokens<DT, NORM>(A.x, tokens, scale, parts, t);
+        if (A.behind) {
+            tc5::wait_for_previous();
+            load_tokens<NORM>(A.x, held, t);
+        }
+        // token r's codes of slice q are row 4 q + r of the operand
+        auto place = [&](int r, int k) {
+            const int block = k >> 7, q = (block >= P.kblocks) + (block >= 2 * P.kblocks) + (block >= 3 * P.kblocks), row = 4 * q + r;
+            return tokens + (block - q * P.kblocks) * A.rows * 128 + row * 128 + (((k >> 4 & 7) ^ (row & 7)) << 4) + (k & 15);
+        };
+        quantize_tokens<DT, NORM>(A.x, held, place, scale, parts, t);
         tc5::fence_async_smem();
         __syncwarp();
         if (lane == 0) tc5::mbar_arrive(&tokens_there);
         meet();  // the scales are there
-        const int c = (warp & 3) * 32 + lane;
+        // The accumulators' 128 rows are four warps'.  Row `row` holds slice q's sum of channel row - q high, tokens in columns 4 q
+        // .. 4 q + 3.  A thread finishes channel c of tokens first, first + S ..
+        const int row = (warp & 3) * 32 + lane, q = row / high, c = S == 1 ? row : t % high, first = S == 1 ? 0 : t / high;
         int acc = 0, parity = 0;
         bool ok = true;
-        // the accumulators' 128 rows are four warps'; kFewTokens of their columns count
-        for (int tile = blockIdx.x; ok && warp < 6 && tile < P.n_tiles; tile += gridDim.x) {
+        for (int i = 0, tile = blockIdx.x; warp < 6 && i < all; ++i, tile += gridDim.x) {
             const int o = tile * P.bn + c, at = min(o, P.d_out - 1);
             const bool real = c < P.bn && o < P.d_out;
             const float2 ws = column_scale<DT, kPlain>(P, at, 0, 1);
@@ -106,40 +127,61 @@ few_product_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_consta
             float res[kFewTokens];
 #pragma unroll
             for (int j = 0; j < kFewTokens; ++j) res[j] = KIND == kFinish && P.residual && real && j < n ? widen16<DT>(P.residual[j * P.ldr + o]) : 0.0f;
-            ok = tc5::mbar_wait_warp(acc_full + acc, parity, &failed);
+            ok = ok && tc5::mbar_wait_warp(acc_full + acc, parity, &failed);
             tc5::fence_after_sync();
+            uint32_t a[kFewTokens], b[kFewTokens];
             if (ok) {
-                uint32_t a[kFewTokens], b[kFewTokens];
-                const uint32_t from = tmem + ((uint32_t)(warp & 3) << 21) + acc * 2 * kFewColumns;
+                const uint32_t from = tmem + ((uint32_t)(warp & 3) << 21) + acc * 2 * kFewColumns + 4 * q;
                 tc5::tmem_ld4(from, a);
                 if (KIND == kGated) tc5::tmem_ld4(from + kFewColumns, b);
                 tc5::tmem_ld_wait();
-                auto store = [&](auto act) {
-#pragma unroll
-                    for (int j = 0; j < kFewTokens; ++j) {
-                        if (j >= n) break;
-                        float z = (float)(int)a[j] * scale[j] * ws.x;
-                        if (P.bias) z += ws.y;
-                        z = activate<decltype(act)::value>(z);
-                        if (KIND == kGated) {
-                            float u = (float)(int)b[j] * scale[j] * us;
-                            if (P.ubias) u += ub;
-                            z *= u;
-                        }
-                        if (KIND == kFinish && P.residual) z += res[j];
-                        if (real) P.y[j * P.ldy + o] = (uint16_t)round16x2<DT>(z, 0.0f);
-                    }
-                };
-                if (KIND == kPlain)
-                    store(ActIs<CMPQ_ACT_NONE>());
-                else
-                    with_act(P.act, store);
             }
             tc5::fence_before_sync();
             __syncwarp();
             if (lane == 0) tc5::mbar_arrive(acc_empty + acc);
             acc ^= 1;
             if (acc == 0) parity ^= 1;
+            if (S > 1) {  // [projection][slice][token][channel]
+                const auto four = [] { asm volatile("bar.sync 2, 128;" ::: "memory"); };
+#pragma unroll
+                for (int j = 0; j < kFewTokens; ++j) {
+                    reduce[q * 4 * high + j * high + row % high] = (int)a[j];
+                    if (KIND == kGated) reduce[512 + q * 4 * high + j * high + row % high] = (int)b[j];
+                }
+                four();
+#pragma unroll
+                for (int j = 0; j < kFewTokens; ++j) {
+                    int sum = 0, other = 0;
+                    for (int k = 0; k < S; ++k) {
+                        sum += reduce[k * 4 * high + j * high + c];
+                        if (KIND == kGated) other += reduce[512 + k * 4 * high + j * high + c];
+                    }
+                    a[j] = (uint32_t)sum, b[j] = (uint32_t)other;
+                }
+                four();  // they have been read
+            }
+            if (!ok) continue;
+            auto store = [&](auto act) {
+#pragma unroll
+                for (int j = 0; j < kFewTokens; ++j) {
+                    if (j >= n) break;
+                    if (S > 1 && j % S != first) continue;
+                    float z = (float)(int)a[j] * scale[j] * ws.x;
+                    if (P.bias) z += ws.y;
+                    z = activate<decltype(act)::value>(z);
+                    if (KIND == kGated) {
+                        float u = (float)(int)b[j] * scale[j] * us;
+                        if (P.ubias) u += ub;
+                        z *= u;
+                    }
+                    if (KIND == kFinish && P.residual) z += res[j];
+                    if (real) P.y[j * P.ldy + o] = (uint16_t)round16x2<DT>(z, 0.0f);
+                }
+            };
+            if (KIND == kPlain)
+                store(ActIs<CMPQ_ACT_NONE>());
+            else
+                with_act(P.act, store);
         }
     }
     __syncwarp();
@@ -170,8 +212,8 @@ static cmpq_status launch_few(FewProduct& a, const Weight8& w, const Weight8* u,
     return a.x.norm.weight ? launch(few_product_kernel<DT, true, KIND>, raised[0]) : launch(few_product_kernel<DT, false, KIND>, raised[1]);
 }
 
-// Rows of which a thread keeps its share: longer ones are read three times, and their products take longer than their weights
-// (one token 11008 -> 4096: 17.0 us here, 15.3 in two kernels; 8192 -> 8192 16.7 and 16.4).
+// Rows of which a thread keeps its share: longer ones are read three times by every block (4 tokens 11008 -> 4096: 16.2 us here,
+// 15.4 in two kernels; 8192 -> 8192 18.4 and 17.3; one token 14.5 and 15.4, 17.3 and 17.3).
 bool few_fits(int64_t d_in) { return d_in <= 4096; }
 
 cmpq_status enqueue_few(const void* X, cmpq_dtype dt, int64_t n, int64_t d_in, int64_t ldx, const void* norm, float eps, const Weight8& w, int64_t d_out,
@@ -187,8 +229,14 @@ cmpq_status enqueue_few(const void* X, cmpq_dtype dt, int64_t n, int64_t d_in, i
     p.n = (int)n, p.d_out = (int)d_out, p.kblocks = (int)ceil_div(d_in, 128);
     p.failed = gave_up;
     plan_tiles(p);
-    a.ring = few_ring(p.kblocks);
-    plan_stages(p, (u ? 2 : 1) * p.bn * 128, a.ring);
+    a.slices = p.kblocks <= 8 || p.bn > 64 ? 1 : p.bn > 32 ? 2 : 4;  // short sums are not worth the adding up
+    a.behind = behind;
+    a.rows = a.slices == 4 ? 16 : 8;
+    p.kblocks = (int)ceil_div(p.kblocks, a.slices);
+    const int token_bytes = p.kblocks * a.rows * 128, block = (u ? 2 : 1) * (a.slices == 1 ? p.bn * 128 : 128 * 128);
+    a.ring = few_ring(token_bytes + 4096);
+    a.reduce = a.ring + token_bytes + 1024;
+    plan_stages(p, block, a.ring);
     auto launch = [&](auto type) {
         constexpr int DT = decltype(type)::value;
         return u ? launch_few<DT, kGated>(a, w, u, behind, st)

@@ -49,29 +49,38 @@ struct TokenParts {  // in shared memory
     float s[kFewTokens][8];
 };
 
-// Codes of all tokens into the operand at `base`, their scales into `scale`, by 256 threads, all rows at once so that their loads
-// are on their way together.  Each thread takes the groups that norm_quantize_row gives it, so a token gets the same bytes from
-// either.
-template <int DT, bool NORM>
-__device__ __forceinline__ void quantize_tokens(const TokenRows& A, uint8_t* base, float* scale, TokenParts& parts, int t) {
-    constexpr int R = kFewTokens, KEEP = 2;  // groups of a row that a thread keeps
+// Eight entries of every token, and of the norm's weight.
+struct TokenGroup {
+    uint4 w, x[kFewTokens];
+
+    template <bool NORM>
+    __device__ __forceinline__ void load(const TokenRows& A, int64_t g) {
+        const uint4 none = make_uint4(0u, 0u, 0u, 0u);
+        const bool there = 8 * g < A.d;
+        w = NORM && there ? load8(A.norm.weight + 8 * g, A.d - 8 * g, A.norm.wide) : none;
+#pragma unroll
+        for (int r = 0; r < kFewTokens; ++r) x[r] = r < A.n && there ? load8_written(A.x + r * A.ldx + 8 * g, A.d - 8 * g, A.wide) : none;
+    }
+};
+constexpr int kFewHeld = 2;  // groups that a thread keeps, asked for before anything else
+
+template <bool NORM>
+__device__ __forceinline__ void load_tokens(const TokenRows& A, TokenGroup (&held)[kFewHeld], int t) {
+#pragma unroll
+    for (int i = 0; i < kFewHeld; ++i) held[i].load<NORM>(A, t + i * 256);
+}
+
+// Codes of all tokens, of entry k of token r to place(r, k), their scales into `scale`, by 256 threads, all rows at once so that
+// their loads are on their way together.  Each thread takes the groups that norm_quantize_row gives it, so a token gets the
+// same bytes from either.
+template <int DT, bool NORM, class Place>
+__device__ __forceinline__ void quantize_tokens(const TokenRows& A, const TokenGroup (&held)[kFewHeld], Place place, float* scale, TokenParts& parts, int t) {
+    constexpr int R = kFewTokens;
     const int n = A.n;
     const int64_t d = A.d, groups = (d + 7) / 8;
-    struct Group {
-        uint4 w, x[R];
-    };
-    auto load = [&](int64_t g, Group& k) {
-        k.w = NORM && g < groups ? load8(A.norm.weight + 8 * g, d - 8 * g, A.norm.wide) : make_uint4(0u, 0u, 0u, 0u);
-#pragma unroll
-        for (int r = 0; r < R; ++r)
-            k.x[r] = r < n && g < groups ? load8_written(A.x + r * A.ldx + 8 * g, d - 8 * g, A.wide) : make_uint4(0u, 0u, 0u, 0u);
-    };
-    Group held[KEEP];
-#pragma unroll
-    for (int i = 0; i < KEEP; ++i) load(t + i * 256, held[i]);
     // f(row, group, entries, v) for this thread's groups
     auto every = [&](auto f) {
-        auto one = [&](int64_t g, const Group& k) {
+        auto one = [&](int64_t g, const TokenGroup& k) {
 #pragma unroll
             for (int r = 0; r < R; ++r) {
                 if (r >= n || g >= groups) break;
@@ -84,10 +93,10 @@ __device__ __forceinline__ void quantize_tokens(const TokenRows& A, uint8_t* bas
             }
         };
 #pragma unroll
-        for (int i = 0; i < KEEP; ++i) one(t + i * 256, held[i]);
-        for (int64_t g = t + KEEP * 256; g < groups; g += 256) {
-            Group k;
-            load(g, k);
+        for (int i = 0; i < kFewHeld; ++i) one(t + i * 256, held[i]);
+        for (int64_t g = t + kFewHeld * 256; g < groups; g += 256) {
+            TokenGroup k;
+            k.load<NORM>(A, g);
             one(g, k);
         }
     };
@@ -134,7 +143,7 @@ __device__ __forceinline__ void quantize_tokens(const TokenRows& A, uint8_t* bas
         for (int r = 0; r < R; ++r)
             if (factor[r] != 1.0f) squares[r] = sum[r];
     }
-    every([&](int r, int64_t g, const float(&)[8], const float(&v)[8]) { *reinterpret_cast<uint2*>(code_at(base, r, 8 * (int)g)) = round_codes(v, s[r].y); });
+    every([&](int r, int64_t g, const float(&)[8], const float(&v)[8]) { *reinterpret_cast<uint2*>(place(r, 8 * (int)g)) = round_codes(v, s[r].y); });
     if (t == 0)
 #pragma unroll
         for (int r = 0; r < R; ++r) {
@@ -151,9 +160,9 @@ inline void plan_tiles(ProductArgs& p) {
     p.bn = (int)std::min<int64_t>(128, ceil_div(ceil_div(p.d_out, rounds * sms), 8) * 8);
     p.n_tiles = (int)ceil_div(p.d_out, p.bn);
 }
-// Bytes for stages of weights.  Behind them are the tokens' codes of `blocks` blocks of the sum; products read 128 rows of
-// weights and 16 of tokens, whatever there is.
-inline int few_ring(int blocks) { return kFewSmem - 1024 - std::max(kFewRows * 128 * blocks + 1024, 128 * 128); }
+// Bytes for stages of weights.  Behind them are the tokens' codes; products read 128 rows of weights and 16 of tokens, whatever
+// there is.
+inline int few_ring(int token_bytes) { return kFewSmem - 1024 - std::max(token_bytes + 1024, 128 * 128); }
 // Stages of 16 to 32 KB: with less of a row at a time memory is slower (4096 x 11008 in boxes of 32 rows x 128 bytes: 23.5 us
 // one by one, 10.1 by fours, 8.8 by eights).
 inline void plan_stages(ProductArgs& p, int block_bytes, int ring) {

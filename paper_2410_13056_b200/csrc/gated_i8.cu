@@ -95,6 +95,7 @@ gated_few_kernel(const __grid_constant__ CUtensorMap gate_map, const __grid_cons
     __shared__ int failed, go;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, n = A.up.n, t = (int)threadIdx.x - 64;  // t: of the computing threads
     const int tile_bytes = A.up.bn * 128, unit_bytes = A.down.bn * 128;  // of a block of the sum
+    TokenGroup held_tokens[kFewHeld];
     if (threadIdx.x < 2 * kFewMaxStages) tc5::mbar_init(&full[0][0] + threadIdx.x, 1), tc5::mbar_init(&empty[0][0] + threadIdx.x, 1);
     if (threadIdx.x == 0) {
         for (int i = 0; i < 2; ++i) tc5::mbar_init(acc_full + i, 1), tc5::mbar_init(acc_empty + i, 8);
@@ -104,6 +105,7 @@ gated_few_kernel(const __grid_constant__ CUtensorMap gate_map, const __grid_cons
     }
     tc5::mbar_init_fence();
     if (warp == 1) tc5::tmem_alloc<1>(&tmem_at, 64);
+    if (warp >= 2) load_tokens<NORM>(A.x, held_tokens, t);  // ahead of the weights
     tc5::fence_before_sync();
     __syncthreads();
     tc5::fence_after_sync();
@@ -218,7 +220,7 @@ gated_few_kernel(const __grid_constant__ CUtensorMap gate_map, const __grid_cons
             __syncwarp();
             if (lane == 0) tc5::mbar_arrive(&tokens_there);
         };
-        quantize_tokens<DT, NORM>(A.x, tokens, scale, parts, t);
+        quantize_tokens<DT, NORM>(A.x, held_tokens, [&](int r, int k) { return code_at(tokens, r, k); }, scale, parts, t);
         tokens_written();
         int32_t* tile_parts = A.sums + n * A.ld_sums;
         for (int64_t i = (int64_t)blockIdx.x * 256 + t; i < (n * A.ld_sums + A.down.n_tiles + 3) / 4; i += (int64_t)gridDim.x * 256)
@@ -383,8 +385,9 @@ static bool plan_few(FewArgs& a) {
     // in one, a block of the sum takes 150 and a unit 1500 besides
     int64_t least = INT64_MAX;
     for (int bn = 128; bn >= 8; bn -= 8)
-        for (int parts = 1; parts <= std::min(d.kblocks, 32); ++parts) {
-            const int64_t tiles = ceil_div(d.d_out, bn), blocks = ceil_div(d.kblocks, parts), each = ceil_div(tiles * ceil_div(d.kblocks, blocks), sms);
+        for (int full = 1; full <= 2; ++full) {  // units that fill the blocks once or twice
+            const int64_t tiles = ceil_div(d.d_out, bn), parts = std::min({std::max(full * sms / tiles, ceil_div(d.kblocks, kFewBlocks)), (int64_t)d.kblocks, (int64_t)32});
+            const int64_t blocks = ceil_div(d.kblocks, parts), each = ceil_div(tiles * ceil_div(d.kblocks, blocks), sms);
             const int64_t cost = each * (blocks * (bn * 128 / 23 + 150) + 1500);
             if (blocks <= kFewBlocks && cost < least) {
                 least = cost, d.bn = bn, d.n_tiles = (int)tiles;
@@ -394,7 +397,7 @@ static bool plan_few(FewArgs& a) {
     if (least == INT64_MAX) return false;
     a.ld_sums = (int64_t)d.n_tiles * d.bn;
     d.wide = aligned_to(d.y, 8) && d.ldy % 4 == 0;
-    a.ring = few_ring(std::max(u.kblocks, a.part_blocks));
+    a.ring = few_ring(kFewRows * 128 * std::max(u.kblocks, a.part_blocks));
     plan_stages(u, 2 * u.bn * 128, a.ring);
     plan_stages(d, d.bn * 128, a.ring);
     return true;
