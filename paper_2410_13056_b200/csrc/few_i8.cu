@@ -8,7 +8,6 @@ struct FewProduct {
     ProductArgs p;      // bn: channels of a tile; kblocks: of a slice; stages, per_stage
     int slices, rows;   // of the sum; of the tokens' operand
     int ring, reduce;   // where the tokens' codes and the slices' sums begin in shared memory
-    int behind;         // the kernel in front of this one writes the tokens
 };
 
 // A block takes tiles of up to 128 channels (of both projections where KIND is kGated), the accumulator's rows; the tokens are
@@ -18,9 +17,9 @@ struct FewProduct {
 // rows make of another one's columns is left, and the slices are added up at the end (a token 4096 -> 4096 takes 32
 // instructions instead of 128, 2 us less).  Launched behind a kernel that writes its tokens, a block asks for its first
 // weights before that has ended.
-// Measured in graphs, weights from memory, against the quantization and the tile kernel, one token: 4096 -> 4096 6.9 us and 9.2,
-// 4096 -> 11008 11.2 and 12.2, 512 -> 512 4.5 and 4.4; in eager calls, where a launch more counts, 8.2 and 10.4, 12.4 and 14.4,
-// 6.2 and 9.1.  Of the 6.9 the weights' way takes 2.8; launch, the tokens' loads and sums and the products take turns.
+// Measured in graphs, weights from memory, against the quantization and the tile kernel, one token: 4096 -> 4096 6.6 us and 9.2,
+// 4096 -> 11008 11.0 and 12.2, 512 -> 512 4.4 and 4.4; in eager calls, where a launch more counts, 8.2 and 10.4, 12.3 and 14.4,
+// 6.2 and 9.1.  Of the 6.6 the weights' way takes 2.6; launch, the tokens' loads and sums and the products take turns.
 template <int DT, bool NORM, int KIND>
 __global__ void __launch_bounds__(kFewThreads, 1)
 few_product_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__ CUtensorMap umap, const __grid_constant__ FewProduct A) {
@@ -38,7 +37,6 @@ few_product_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_consta
     const int S = A.slices, high = 128 / S, box_bytes = P.bn * 128, slice_bytes = S == 1 ? box_bytes : high * 128;
     const int half_bytes = S * slice_bytes, block_bytes = KIND == kGated ? 2 * half_bytes : half_bytes;  // of a projection, of a block of all slices
     const int all = (P.n_tiles - 1 - blockIdx.x) / gridDim.x + 1;  // tiles
-    TokenGroup held[kFewHeld];
     if (threadIdx.x < P.stages) tc5::mbar_init(full + threadIdx.x, 1), tc5::mbar_init(empty + threadIdx.x, 1);
     if (threadIdx.x == 0) {
         for (int i = 0; i < 2; ++i) tc5::mbar_init(acc_full + i, 1), tc5::mbar_init(acc_empty + i, 4);
@@ -47,7 +45,6 @@ few_product_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_consta
     }
     tc5::mbar_init_fence();
     if (warp == 1) tc5::tmem_alloc<1>(&tmem_at, 64);
-    if (warp >= 2 && !A.behind) load_tokens<NORM>(A.x, held, t);  // ahead of the weights
     tc5::dependents_may_start();
     tc5::fence_before_sync();
     __syncthreads();
@@ -100,16 +97,13 @@ few_product_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_consta
             }
         }
     } else {
-        if (A.behind) {
-            tc5::wait_for_previous();
-            load_tokens<NORM>(A.x, held, t);
-        }
+        tc5::wait_for_previous();
         // token r's codes of slice q are row 4 q + r of the operand
         auto place = [&](int r, int k) {
             const int block = k >> 7, q = (block >= P.kblocks) + (block >= 2 * P.kblocks) + (block >= 3 * P.kblocks), row = 4 * q + r;
             return tokens + (block - q * P.kblocks) * A.rows * 128 + row * 128 + (((k >> 4 & 7) ^ (row & 7)) << 4) + (k & 15);
         };
-        quantize_tokens<DT, NORM>(A.x, held, place, scale, parts, t);
+        quantize_tokens<DT, NORM>(A.x, place, scale, parts, t);
         tc5::fence_async_smem();
         __syncwarp();
         if (lane == 0) tc5::mbar_arrive(&tokens_there);
@@ -230,7 +224,6 @@ cmpq_status enqueue_few(const void* X, cmpq_dtype dt, int64_t n, int64_t d_in, i
     p.failed = gave_up;
     plan_tiles(p);
     a.slices = p.kblocks <= 8 || p.bn > 64 ? 1 : p.bn > 32 ? 2 : 4;  // short sums are not worth the adding up
-    a.behind = behind;
     a.rows = a.slices == 4 ? 16 : 8;
     p.kblocks = (int)ceil_div(p.kblocks, a.slices);
     const int token_bytes = p.kblocks * a.rows * 128, block = (u ? 2 : 1) * (a.slices == 1 ? p.bn * 128 : 128 * 128);

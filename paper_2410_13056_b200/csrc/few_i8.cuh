@@ -62,22 +62,19 @@ struct TokenGroup {
         for (int r = 0; r < kFewTokens; ++r) x[r] = r < A.n && there ? load8_written(A.x + r * A.ldx + 8 * g, A.d - 8 * g, A.wide) : none;
     }
 };
-constexpr int kFewHeld = 2;  // groups that a thread keeps, asked for before anything else
-
-template <bool NORM>
-__device__ __forceinline__ void load_tokens(const TokenRows& A, TokenGroup (&held)[kFewHeld], int t) {
-#pragma unroll
-    for (int i = 0; i < kFewHeld; ++i) held[i].load<NORM>(A, t + i * 256);
-}
+constexpr int kFewHeld = 2;  // groups that a thread keeps
 
 // Codes of all tokens, of entry k of token r to place(r, k), their scales into `scale`, by 256 threads, all rows at once so that
 // their loads are on their way together.  Each thread takes the groups that norm_quantize_row gives it, so a token gets the
 // same bytes from either.
 template <int DT, bool NORM, class Place>
-__device__ __forceinline__ void quantize_tokens(const TokenRows& A, const TokenGroup (&held)[kFewHeld], Place place, float* scale, TokenParts& parts, int t) {
+__device__ __forceinline__ void quantize_tokens(const TokenRows& A, Place place, float* scale, TokenParts& parts, int t) {
     constexpr int R = kFewTokens;
     const int n = A.n;
     const int64_t d = A.d, groups = (d + 7) / 8;
+    TokenGroup held[kFewHeld];
+#pragma unroll
+    for (int i = 0; i < kFewHeld; ++i) held[i].load<NORM>(A, t + i * 256);
     // f(row, group, entries, v) for this thread's groups
     auto every = [&](auto f) {
         auto one = [&](int64_t g, const TokenGroup& k) {

@@ -29,7 +29,7 @@ struct GatedSpace {
 
 // ---- few tokens: the whole block in one kernel ----------------------------------------------------------------
 //
-// While tokens are few the weights are the time, and between two kernels their stream stops: four launches take 36.5 us for a
+// While tokens are few the weights are the time, and between two kernels their stream stops: four launches take 35 us for a
 // token through 4096 -> 11008 -> 4096 whose weights come in 20.6.  Here one block to an SM walks through all of it (a
 // cooperative launch: its blocks wait for one another, once):
 //   every block quantizes all tokens into its shared memory
@@ -45,6 +45,12 @@ struct GatedSpace {
 //
 // What blocks hand to one another goes through L2: stores, a fence, an atomic on the counter; an acquiring load of it, then
 // loads past L1.
+//
+// Measured in graphs, weights from memory: one token 4096 -> 11008 -> 4096 30.5 us (4.4 TB/s), 4 tokens 31.0, one token 8192 ->
+// 28672 -> 8192 121 (5.8 TB/s).  A block's time for the first: its tokens quantized at 4 us, the last weights of both projections
+// at 16, h seen by all at 18.5, its part of h quantized at 20, the last products at 24, sums joined and written at 27.  Between
+// 16 and 20 the memory fills shared memory and rests a little; asking for more into L2 meanwhile gained nothing, since from
+// there to the SMs no more than 1.4 times the memory's rate was had.
 
 constexpr int kRowMax = 2, kMark = CMPQ_GATED_STATE_BYTES / 4 - 1;  // in the state: rows' maxima, the mark of a kernel that gave up
 
@@ -95,7 +101,6 @@ gated_few_kernel(const __grid_constant__ CUtensorMap gate_map, const __grid_cons
     __shared__ int failed, go;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, n = A.up.n, t = (int)threadIdx.x - 64;  // t: of the computing threads
     const int tile_bytes = A.up.bn * 128, unit_bytes = A.down.bn * 128;  // of a block of the sum
-    TokenGroup held_tokens[kFewHeld];
     if (threadIdx.x < 2 * kFewMaxStages) tc5::mbar_init(&full[0][0] + threadIdx.x, 1), tc5::mbar_init(&empty[0][0] + threadIdx.x, 1);
     if (threadIdx.x == 0) {
         for (int i = 0; i < 2; ++i) tc5::mbar_init(acc_full + i, 1), tc5::mbar_init(acc_empty + i, 8);
@@ -105,7 +110,6 @@ gated_few_kernel(const __grid_constant__ CUtensorMap gate_map, const __grid_cons
     }
     tc5::mbar_init_fence();
     if (warp == 1) tc5::tmem_alloc<1>(&tmem_at, 64);
-    if (warp >= 2) load_tokens<NORM>(A.x, held_tokens, t);  // ahead of the weights
     tc5::fence_before_sync();
     __syncthreads();
     tc5::fence_after_sync();
@@ -220,7 +224,7 @@ gated_few_kernel(const __grid_constant__ CUtensorMap gate_map, const __grid_cons
             __syncwarp();
             if (lane == 0) tc5::mbar_arrive(&tokens_there);
         };
-        quantize_tokens<DT, NORM>(A.x, held_tokens, [&](int r, int k) { return code_at(tokens, r, k); }, scale, parts, t);
+        quantize_tokens<DT, NORM>(A.x, [&](int r, int k) { return code_at(tokens, r, k); }, scale, parts, t);
         tokens_written();
         int32_t* tile_parts = A.sums + n * A.ld_sums;
         for (int64_t i = (int64_t)blockIdx.x * 256 + t; i < (n * A.ld_sums + A.down.n_tiles + 3) / 4; i += (int64_t)gridDim.x * 256)
@@ -372,8 +376,8 @@ gated_few_kernel(const __grid_constant__ CUtensorMap gate_map, const __grid_cons
 }
 
 // Tiles, parts and stages; false where separate kernels are as fast, or the tokens' codes would take too much of the shared
-// memory.  In graphs, 1 token 4096 -> 11008 -> 4096 takes 30.2 us here and 35.0 in four kernels, 8 tokens 38.2 and 36.0; 1 token
-// 1536 -> 4096 -> 1536 (19 MB) 15.6 and 16.4, 1024 -> 2816 -> 1024 14.2 and 13.9.
+// memory.  In graphs, 1 token 4096 -> 11008 -> 4096 takes 30.5 us here and 35.0 in four kernels, 8 tokens 38.2 and 36.0; 1 token
+// 1536 -> 4096 -> 1536 (19 MB) 14.9 and 16.4, 1024 -> 2816 -> 1024 14.2 and 13.9.
 static bool plan_few(FewArgs& a) {
     ProductArgs &u = a.up, &d = a.down;
     const int sms = sm_count();

@@ -43,8 +43,8 @@ __device__ __forceinline__ uint2 group_codes(uint4 g, float inv) {
 // finite.  A thread keeps KEEP groups of eight in registers, chosen by the row's length so that more blocks share an SM
 // where rows are short, and twice as many threads where they are long; rows of up to 32768 entries are read once, the rest of a
 // longer one is read again.
-// Measured in a stream of calls: 4096 x 8192 20 us (100 MB, 5.0 TB/s), 1000 x 11008 10.3 us; the first took 1.5 times as long
-// with conversions and 32-bit comparisons.
+// Measured in graphs: 4096 x 8192 17.8 us (100 MB, 5.6 TB/s), 4096 x 28672 58 (6.1 TB/s; 88 with 256 threads, which read the end
+// of the row twice); the first took 1.5 times as long with conversions and 32-bit comparisons.
 template <int DT, int KEEP, int THREADS = kQtThreads>
 __global__ void __launch_bounds__(THREADS)
 quantize_tokens_kernel(const uint16_t* __restrict__ X, int64_t d, int64_t ldx, int wide, int8_t* __restrict__ codes,
@@ -89,7 +89,8 @@ quantize_tokens_kernel(const uint16_t* __restrict__ X, int64_t d, int64_t ldx, i
         *reinterpret_cast<uint2*>(out + 8 * g) = group_codes<DT>(load8(row + 8 * g, d - 8 * g, wide), inv);
 }
 
-// The same behind a norm.
+// The same behind a norm.  Measured in graphs: 4096 x 8192 23 us (100 MB, 4.4 TB/s), 4096 x 4096 14 (3.6): the issue slots are two
+// thirds full, of which a third goes to what a row costs besides its entries.
 template <int DT, int KEEP>
 __global__ void __launch_bounds__(kQtThreads)
 norm_quantize_kernel(const uint16_t* __restrict__ X, int64_t d, int64_t ldx, int wide, RowNorm norm, int8_t* __restrict__ codes, int64_t ldc,
@@ -115,12 +116,13 @@ constexpr size_t kTileSmem = 208 << 10;
 // blocks fill the SMs; the weights pass through once and are the time while tokens are few.  Launched behind the
 // quantization of its tokens, a block asks for its first weights before that has ended.  A stage holds the
 // token rows that exist (to eight) and the channels'; the product reads on past those rows into whatever follows, which
-// only reaches accumulator rows that are not stored, and 16 KB behind the last stage are kept for it.  With that one
-// token's weights have some 30 stages on their way.
+// only reaches accumulator rows that are not stored, and 16 KB behind the last stage are kept for it.  A stage holds as
+// many 128-byte blocks of the sum as make 48 KB, 64 KB above 32 tokens: with less of a row at a time memory is slower
+// (100 tokens 11008 -> 4096: a block at a time 27.5 us, 64 KB 18.3; 8 tokens 28672 -> 8192 53 and 45).
 //
-// Measured with the quantization in a stream of calls, weights from memory: one token 4096 -> 4096 10.3 us, 8192 -> 28672 42 us
-// (5.6 TB/s, 0.86 of the copy rate); 37 tokens 4096 -> 11008 14.3 us (3.2 TB/s: launch, first loads and the last stage's way
-// out are half of it).  Splitting the sum over a cluster instead, weights as rows, took 1.5, 1.3 and 2.4 times as long.
+// Measured with the quantization in graphs, weights from memory: 8 tokens 4096 -> 4096 9.0 us, 8192 -> 28672 41.5 us (5.7 TB/s,
+// 0.86 of the copy rate); 53 tokens 4096 -> 11008 13.4 us (3.4 TB/s: launch, first loads and the last stage's way out are
+// half of it).  Splitting the sum over a cluster instead, weights as rows, took 1.5, 1.3 and 2.4 times as long.
 //
 // A gated tile's columns are bn / 2 channels of the gate and the same ones of the second projection, from maps of their own.
 template <int DT, int KIND>
@@ -231,17 +233,19 @@ matmul_i8_tile_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_con
 constexpr int kPairStages = 6, kPairStageBytes = 2 * 128 * 128;  // room for the widest tile
 constexpr size_t kPairSmem = kPairStages * kPairStageBytes + 1024;
 
-// Many tokens: pairs of CTAs stay on their SMs and walk over tiles of 256 tokens x 256 channels (cta_group::2).  A CTA
-// loads its 128 tokens and half of the channels, so each byte that an SM reads feeds 512 products; six stages of 32 KB.
+// Many tokens: pairs of CTAs stay on their SMs and walk over tiles of 256 tokens x bn channels (cta_group::2), 256 of them or
+// fewer, in steps of 32, where that fills the last round better.  A CTA loads its 128 tokens and half of the channels, so each
+// byte that an SM reads feeds 512 products; six stages of 32 KB, whose weights are asked for while the tokens are quantized.
 // Two accumulators of 256 columns alternate, the epilogue of one tile runs under the products of the next.  Token tiles
 // go fastest: the pairs at work share a few weight tiles and the token codes stay in L2.
 //
 // Measured: 4096 x 8192 x 28672 with the quantization 610 us in a few calls after a rest (3.15 POP/s, 0.96 of twice the library's
-// bf16 rate) and 680 to 694 in a long stream, where the power limit holds the clock; 2048 x 4096 x 11008 67 us, 72 with the
-// quantization, the tensor pipe at 81 % (172 pair tiles in 3 rounds of 74).
+// bf16 rate) and 670 in a long stream, where the power limit holds the clock; 2048 x 4096 x 11008 65 us, 71 with the
+// quantization, the tensor pipe at 81 %: the SMs ask L2 for some 12 TB/s then, which is what holds the pace.
 //
-// A gated tile is 256 tokens x 128 channels of both projections: the even CTA's half of the columns is the gate, the odd
-// one's the second projection, so a thread of the epilogue finds both of a channel in its accumulator row.
+// A gated tile is 256 tokens x bn / 2 channels of both projections: the even CTA's half of the columns is the gate, the odd
+// one's the second projection, so a thread of the epilogue finds both of a channel in its accumulator row; activations stay
+// under the next tile's products.  Of 2048 tokens 4096 -> 11008 it takes 115 us, the tensor pipe at 80 %.
 template <int DT, int KIND>
 __global__ void __launch_bounds__(kMmThreads, 1)
 matmul_i8_pair_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__ CUtensorMap umap, const __grid_constant__ CUtensorMap xmap,
@@ -370,7 +374,8 @@ matmul_i8_pair_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_con
 // Cycles that a way to cover the product takes, from sizes: rounds of blocks over the SMs, in each the blocks of the sum
 // at the pace of the products or of the loads (64 bytes a cycle and SM), and what a round or launch costs besides; not
 // less than the weights' way from memory (3400 bytes a cycle).  Fitted to sweeps of bn over 1 to 512 tokens and layers of
-// 4096 x 4096 to 8192 x 28672; e.g. 256 x 4096 x 11008: bn = 160 17.9 us, 80 22.7, pairs 21.6; 4096 x 8192 x 28672: pairs.
+// 4096 x 4096 to 8192 x 28672, where the choice is within 3 % of the best; e.g. 256 x 4096 x 11008: bn = 160 17.4 us, 176 17.7,
+// pairs of 160 17.2; 512 tokens: pairs of 160 24.3, 192 25.7, 256 29.9.
 static int64_t tile_cycles(const ProductArgs& a, int bn) {
     const int64_t blocks = (int64_t)((a.n + 127) / 128) * ((a.cols + bn - 1) / bn), sms = sm_count();
     const int64_t rounds = (blocks + sms - 1) / sms, pace = std::max(4 * std::max(32, bn / 2), (bn + std::min(a.n, 128)) * 2);
