@@ -46,9 +46,9 @@ struct GatedSpace {
 // What blocks hand to one another goes through L2: stores, a fence, an atomic on the counter; an acquiring load of it, then
 // loads past L1.
 //
-// Measured in graphs, weights from memory: one token 4096 -> 11008 -> 4096 30.5 us (4.4 TB/s), 4 tokens 31.0, one token 8192 ->
-// 28672 -> 8192 121 (5.8 TB/s).  A block's time for the first: its tokens quantized at 4 us, the last weights of both projections
-// at 16, h seen by all at 18.5, its part of h quantized at 20, the last products at 24, sums joined and written at 27.  Between
+// Measured in graphs, weights from memory: one token 4096 -> 11008 -> 4096 29.9 us (4.5 TB/s), 4 tokens 30.9, one token 8192 ->
+// 28672 -> 8192 121 (5.8 TB/s).  A block's time for the first: its tokens quantized at 3.4 us, the products of both projections
+// over at 16.4, h seen by all at 19.2, its part of h quantized at 20.6, the last products at 25.3, sums joined at 26.5.  Between
 // 16 and 20 the memory fills shared memory and rests a little; asking for more into L2 meanwhile gained nothing, since from
 // there to the SMs no more than 1.4 times the memory's rate was had.
 
@@ -376,7 +376,7 @@ gated_few_kernel(const __grid_constant__ CUtensorMap gate_map, const __grid_cons
 }
 
 // Tiles, parts and stages; false where separate kernels are as fast, or the tokens' codes would take too much of the shared
-// memory.  In graphs, 1 token 4096 -> 11008 -> 4096 takes 30.5 us here and 35.0 in four kernels, 8 tokens 38.2 and 36.0; 1 token
+// memory.  In graphs, 1 token 4096 -> 11008 -> 4096 takes 29.9 us here and 35.0 in four kernels, 8 tokens 38.2 and 36.0; 1 token
 // 1536 -> 4096 -> 1536 (19 MB) 14.9 and 16.4, 1024 -> 2816 -> 1024 14.2 and 13.9.
 static bool plan_few(FewArgs& a) {
     ProductArgs &u = a.up, &d = a.down;

@@ -240,12 +240,12 @@ constexpr size_t kPairSmem = kPairStages * kPairStageBytes + 1024;
 // go fastest: the pairs at work share a few weight tiles and the token codes stay in L2.
 //
 // Measured: 4096 x 8192 x 28672 with the quantization 610 us in a few calls after a rest (3.15 POP/s, 0.96 of twice the library's
-// bf16 rate) and 670 in a long stream, where the power limit holds the clock; 2048 x 4096 x 11008 65 us, 71 with the
-// quantization, the tensor pipe at 81 %: the SMs ask L2 for some 12 TB/s then, which is what holds the pace.
+// bf16 rate) and 670 in a long stream, where the power limit holds the clock; 2048 x 4096 x 11008 64 us, 71 with the
+// quantization, the tensor pipe at 71 %: the SMs ask L2 for some 12 TB/s then, which is what holds the pace.
 //
 // A gated tile is 256 tokens x bn / 2 channels of both projections: the even CTA's half of the columns is the gate, the odd
 // one's the second projection, so a thread of the epilogue finds both of a channel in its accumulator row; activations stay
-// under the next tile's products.  Of 2048 tokens 4096 -> 11008 it takes 115 us, the tensor pipe at 80 %.
+// under the next tile's products.  2048 tokens 4096 -> 11008 take 114 us, the tensor pipe at 82 %.
 template <int DT, int KIND>
 __global__ void __launch_bounds__(kMmThreads, 1)
 matmul_i8_pair_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__ CUtensorMap umap, const __grid_constant__ CUtensorMap xmap,
