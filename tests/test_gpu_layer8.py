@@ -214,6 +214,14 @@ def test_activations_over_their_whole_range():
                 got = layer(x, activation=act)
             _compare(got, y, tol)
         assert torch.equal(layer(x, activation="none"), layer(x))
+    # sums that pass float32
+    codes = torch.zeros(2, 16, dtype=torch.int8, device="cuda")
+    codes[0, 0], codes[1, 0] = -127, 127
+    layer = serving.Int8Linear(codes[:, :1], torch.full((2,), 3e38, device="cuda"))
+    assert torch.equal(layer(x), torch.tensor([[-np.inf, np.inf]], dtype=dtype, device="cuda"))
+    for act, low in (("relu", 0.0), ("gelu", 0.0), ("silu", np.nan), ("gelu_tanh", np.nan)):
+        y = layer(x, activation=act)[0].float().cpu().numpy()
+        assert y[1] == np.inf and (y[0] == low or np.isnan(y[0]) and np.isnan(low)), (act, y)
 
 
 # ---- gated block -----------------------------------------------------------------------------------------------
