@@ -13,7 +13,7 @@ struct FewProduct {
 // A block takes tiles of up to 128 channels (of both projections where KIND is kGated), the accumulator's rows; the tokens are
 // its columns: an instruction reads 128 rows of its first operand whatever they hold (40 cycles for up to 32 columns), so it
 // should hold the weights.  Where the channels are spread over all SMs and a tile has 64 or 32 of them, its sum is cut into two
-// or four slices, each with rows and columns of its own: an instruction then takes as many blocks of the sum, what a slice's
+// or four slices, every second or fourth block of it, each with rows and columns of its own: an instruction then takes as many blocks of the sum, what a slice's
 // rows make of another one's columns is left, and the slices are added up at the end (a token 4096 -> 4096 takes 32
 // instructions instead of 128, 2 us less).  Launched behind a kernel that writes its tokens, a block asks for its first
 // weights before that has ended.
@@ -62,8 +62,8 @@ few_product_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_consta
                     tc5::mbar_expect_tx(full + slot, count * S * (KIND == kGated ? 2 : 1) * box_bytes);
                     for (int b = k; b < k + count; ++b, at += block_bytes)
                         for (int q = 0; q < S; ++q) {
-                            tc5::tma_load_2d(at + q * slice_bytes, &wmap, full + slot, (q * P.kblocks + b) * 128, tile * P.bn);
-                            if (KIND == kGated) tc5::tma_load_2d(at + half_bytes + q * slice_bytes, &umap, full + slot, (q * P.kblocks + b) * 128, tile * P.bn);
+                            tc5::tma_load_2d(at + q * slice_bytes, &wmap, full + slot, (b * S + q) * 128, tile * P.bn);
+                            if (KIND == kGated) tc5::tma_load_2d(at + half_bytes + q * slice_bytes, &umap, full + slot, (b * S + q) * 128, tile * P.bn);
                         }
                     if (++slot == P.stages) slot = 0, phase ^= 1;
                 }
@@ -100,8 +100,8 @@ few_product_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_consta
         tc5::wait_for_previous();
         // token r's codes of slice q are row 4 q + r of the operand
         auto place = [&](int r, int k) {
-            const int block = k >> 7, q = (block >= P.kblocks) + (block >= 2 * P.kblocks) + (block >= 3 * P.kblocks), row = 4 * q + r;
-            return tokens + (block - q * P.kblocks) * A.rows * 128 + row * 128 + (((k >> 4 & 7) ^ (row & 7)) << 4) + (k & 15);
+            const int block = k >> 7, row = 4 * (block & (S - 1)) + r;
+            return tokens + (block >> (S >> 1)) * A.rows * 128 + row * 128 + (((k >> 4 & 7) ^ (row & 7)) << 4) + (k & 15);  // S is 1, 2 or 4
         };
         quantize_tokens<DT, NORM>(A.x, place, scale, parts, t);
         tc5::fence_async_smem();
@@ -206,8 +206,8 @@ static cmpq_status launch_few(FewProduct& a, const Weight8& w, const Weight8* u,
     return a.x.norm.weight ? launch(few_product_kernel<DT, true, KIND>, raised[0]) : launch(few_product_kernel<DT, false, KIND>, raised[1]);
 }
 
-// Rows of which a thread keeps its share: longer ones are read three times by every block (4 tokens 11008 -> 4096: 16.2 us here,
-// 15.4 in two kernels; 8192 -> 8192 18.4 and 17.3; one token 14.5 and 15.4, 17.3 and 17.3).
+// Rows of which a thread keeps its share: longer ones are read three times by every block (4 tokens 11008 -> 4096: 15.9 us here,
+// 12.8 in two kernels; 8192 -> 8192 19.7 and 18.0; one token 13.9 and 12.7, 16.6 and 18.2; one token 4096 -> 4096 6.6 and 8.3).
 bool few_fits(int64_t d_in) { return d_in <= 4096; }
 
 cmpq_status enqueue_few(const void* X, cmpq_dtype dt, int64_t n, int64_t d_in, int64_t ldx, const void* norm, float eps, const Weight8& w, int64_t d_out,

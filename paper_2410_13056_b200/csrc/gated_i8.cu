@@ -376,12 +376,13 @@ gated_few_kernel(const __grid_constant__ CUtensorMap gate_map, const __grid_cons
 }
 
 // Tiles, parts and stages; false where separate kernels are as fast, or the tokens' codes would take too much of the shared
-// memory.  In graphs, 1 token 4096 -> 11008 -> 4096 takes 29.9 us here and 35.0 in four kernels, 8 tokens 38.2 and 36.0; 1 token
-// 1536 -> 4096 -> 1536 (19 MB) 14.9 and 16.4, 1024 -> 2816 -> 1024 14.2 and 13.9.
+// memory.  In graphs, 1 token 4096 -> 11008 -> 4096 takes 29.7 us here and 32.4 in four kernels, 2048 -> 5632 -> 2048 16.5 and
+// 18.5, 1024 -> 2816 -> 1024 14.2 and 13.9.  Where the kernel that quantizes its own tokens does for both products, two of it
+// are faster (4096 -> 4096 -> 4096 20.2 here, 17.4 in two; 4 tokens 21.6 and 19.7).
 static bool plan_few(FewArgs& a) {
     ProductArgs &u = a.up, &d = a.down;
     const int sms = sm_count();
-    if ((2 * (int64_t)a.d_in + d.d_out) * a.d_ff < (16 << 20)) return false;
+    if ((few_fits(a.d_in) && few_fits(a.d_ff)) || (2 * (int64_t)a.d_in + d.d_out) * a.d_ff < (16 << 20)) return false;
     u.kblocks = (int)ceil_div(a.d_in, 128), d.kblocks = (int)ceil_div(a.d_ff, 128);
     if (u.kblocks > kFewBlocks) return false;
     plan_tiles(u);

@@ -120,13 +120,18 @@ constexpr size_t kTileSmem = 208 << 10;
 // many 128-byte blocks of the sum as make 48 KB, 64 KB above 32 tokens: with less of a row at a time memory is slower
 // (100 tokens 11008 -> 4096: a block at a time 27.5 us, 64 KB 18.3; 8 tokens 28672 -> 8192 53 and 45).
 //
-// Measured with the quantization in graphs, weights from memory: 8 tokens 4096 -> 4096 9.0 us, 8192 -> 28672 41.5 us (5.7 TB/s,
-// 0.86 of the copy rate); 53 tokens 4096 -> 11008 13.4 us (3.4 TB/s: launch, first loads and the last stage's way out are
+// Measured with the quantization in graphs, weights from memory: 8 tokens 4096 -> 4096 8.2 us, 8192 -> 28672 41.8 us (5.6 TB/s,
+// 0.85 of the copy rate); 53 tokens 4096 -> 11008 13.4 us (3.4 TB/s: launch, first loads and the last stage's way out are
 // half of it).  Splitting the sum over a cluster instead, weights as rows, took 1.5, 1.3 and 2.4 times as long.
 //
 // A gated tile's columns are bn / 2 channels of the gate and the same ones of the second projection, from maps of their own.
-template <int DT, int KIND>
-__global__ void __launch_bounds__(kMmThreads)
+//
+// SLICED: narrow tiles of few tokens leave most of an instruction's rows empty, and it takes 40 cycles all the same.  Every
+// second or fourth block of the sum gets rows and columns of its own then, an instruction takes as many blocks, and the slices
+// are added up at the end (see few_i8.cu): 8 tokens 11008 -> 4096 15.4 -> 12.9 us.  A kernel of its own, as its longer program
+// cost small layers 0.2 us.
+template <int DT, int KIND, bool SLICED>
+__global__ void __launch_bounds__(kMmThreads, 1)
 matmul_i8_tile_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__ CUtensorMap umap, const __grid_constant__ CUtensorMap xmap,
                       const __grid_constant__ ProductArgs A) {
     extern __shared__ uint8_t raw[];
@@ -137,7 +142,8 @@ matmul_i8_tile_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_con
     __shared__ int failed;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int nt = blockIdx.x / A.m_tiles, mt = blockIdx.x % A.m_tiles, bn = A.bn;
-    const int a_bytes = A.rows * 128, b_bytes = bn * 128, stage = A.per_stage * (a_bytes + b_bytes), columns = bn <= 32 ? 32 : bn <= 64 ? 64 : bn <= 128 ? 128 : 256;
+    const int S = SLICED ? A.slices : 1, N = S * bn, columns = N <= 32 ? 32 : N <= 64 ? 64 : N <= 128 ? 128 : 256;
+    const int row_box = A.rows * 128, box = bn * 128, a_bytes = S * row_box, b_bytes = S * box, stage = A.per_stage * (a_bytes + b_bytes);  // of a slice, of all
     if (threadIdx.x < A.stages) tc5::mbar_init(full + threadIdx.x, 1), tc5::mbar_init(empty + threadIdx.x, 1);
     if (threadIdx.x == 0) tc5::mbar_init(&done, 1), failed = 0;
     tc5::mbar_init_fence();
@@ -154,10 +160,10 @@ matmul_i8_tile_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_con
                 const int count = min(A.per_stage, A.kblocks - k);
                 tc5::mbar_expect_tx(full + slot, count * (a_bytes + b_bytes));  // the tokens' bytes too, whoever comes first
                 uint8_t* at = smem + slot * stage + A.per_stage * a_bytes;
-                for (int i = k; i < k + count; ++i, at += b_bytes) {
+                for (int i = k * S; i < (k + count) * S; ++i, at += box) {
                     if (KIND == kGated) {
                         tc5::tma_load_2d(at, &wmap, full + slot, i * 128, nt * (bn / 2));
-                        tc5::tma_load_2d(at + b_bytes / 2, &umap, full + slot, i * 128, nt * (bn / 2));
+                        tc5::tma_load_2d(at + box / 2, &umap, full + slot, i * 128, nt * (bn / 2));
                     } else {
                         tc5::tma_load_2d(at, &wmap, full + slot, i * 128, nt * bn);
                     }
@@ -167,7 +173,7 @@ matmul_i8_tile_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_con
         }
     } else if (warp == 1) {
         if (tc5::elect_one()) {
-            const uint32_t idesc = tc5::idesc_i8(128, bn);
+            const uint32_t idesc = tc5::idesc_i8(128, N);
             int slot = 0, phase = 0;
             for (int k = 0; k < A.kblocks; k += A.per_stage) {
                 if (!tc5::mbar_wait(full + slot, phase, &failed)) break;
@@ -193,8 +199,8 @@ matmul_i8_tile_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_con
                 int slot = 0, phase = 1;
                 for (int k = 0; k < A.kblocks; k += A.per_stage) {
                     if (!tc5::mbar_wait(empty + slot, phase, &failed)) break;
-                    for (int i = 0; i < min(A.per_stage, A.kblocks - k); ++i)
-                        tc5::tma_load_2d(smem + slot * stage + i * a_bytes, &xmap, full + slot, (k + i) * 128, mt * 128);
+                    for (int i = 0; i < min(A.per_stage, A.kblocks - k) * S; ++i)
+                        tc5::tma_load_2d(smem + slot * stage + i * row_box, &xmap, full + slot, (k * S + i) * 128, mt * 128);
                     if (++slot == A.stages) slot = 0, phase ^= 1;
                 }
             }
@@ -208,7 +214,36 @@ matmul_i8_tile_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_con
         asm volatile("bar.sync 1, 256;" ::: "memory");
         tc5::mbar_wait_warp(&done, 0, &failed);
         tc5::fence_after_sync();
-        if (mt * 128 + quad * 32 < A.n) {
+        if (SLICED) {
+            // Row q rows + t holds slice q's sums of token t, in columns q bn and on.  They are added up through shared memory, which
+            // no copy or product uses any more: [slice][token][column].
+            int32_t* sums = reinterpret_cast<int32_t*>(smem);
+            const int row = quad * 32 + lane, mine = row / A.rows;
+            for (int q = quad * 32 / A.rows; q < min(S, (quad * 32 + 31) / A.rows + 1); ++q)
+                for (int c = upper ? 16 : 0; c < bn; c += 32) {
+                    uint32_t r[16];
+                    tc5::tmem_ld16(tmem + ((uint32_t)quad << 21) + q * bn + c, r);
+                    tc5::tmem_ld_wait();
+                    if (mine == q)
+#pragma unroll
+                        for (int j = 0; j < 16; j += 4) *reinterpret_cast<int4*>(sums + row * bn + c + j) = make_int4(r[j], r[j + 1], r[j + 2], r[j + 3]);
+                }
+            asm volatile("bar.sync 1, 256;" ::: "memory");
+            for (int i = threadIdx.x - 64; i < A.n * (wide / 8); i += 256) {
+                const int token = i / (wide / 8), c = i % (wide / 8) * 8;
+                int z[8] = {}, u[8] = {};
+                for (int q = 0; q < S; ++q)
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        const int32_t* from = sums + (q * A.rows + token) * bn + c + j;
+                        z[j] += from[0];
+                        if (KIND == kGated) u[j] += from[bn / 2];
+                    }
+                if (c < left)
+                    store_eight<DT, KIND>(A, z, u, sb + c, sb + bn / 2 + c, __ldcg(A.xs + token), A.y + (int64_t)token * A.ldy + o0 + c,
+                                          A.residual + (int64_t)token * A.ldr + o0 + c, left - c);
+            }
+        } else if (mt * 128 + quad * 32 < A.n) {
             const uint32_t rows = tmem + ((uint32_t)quad << 21);
             uint16_t* y = A.y + (int64_t)t * A.ldy + o0;
             if (KIND == kPlain) store_rows<DT>(rows, c0, c1, sb, A.bias != nullptr, xs, real, y, left, A.wide);
@@ -407,7 +442,7 @@ static cmpq_status launch_kind(const TokenCodes& x, int64_t d_in, const Weight8&
     umap = wmap;
     if (u && !make_byte_map(&umap, u->codes, a.d_out, d_in, u->ld, box)) return CMPQ_ERR_CUDA;
     a.n_tiles = (a.d_out + channels - 1) / channels;
-    static bool raised[2][64];
+    static bool raised[3][64];
     if (pair) {
         a.m_tiles = (a.n + 255) / 256;
         if (!raise_smem_limit_once(matmul_i8_pair_kernel<DT, KIND>, kPairSmem, raised[0])) return CMPQ_ERR_CUDA;
@@ -418,13 +453,20 @@ static cmpq_status launch_kind(const TokenCodes& x, int64_t d_in, const Weight8&
     a.m_tiles = (a.n + 127) / 128;
     // one block to an SM: two that share it were slower at every size, their rounds and tails cost more than they hide
     const int64_t blocks = (int64_t)a.m_tiles * a.n_tiles;
-    const int block = (a.rows + a.bn) * 128;
+    // shorter sums are not worth the adding up, and wider tiles wait for memory: 32 tokens 2048 -> 2048 6.0 -> 6.6 us with four
+    // slices, 53 tokens 4096 -> 4096 9.2 -> 9.5 and 28672 -> 8192 45.8 -> 46.9 with two
+    a.slices = a.bn > 32 ? 1 : a.rows <= 32 && a.kblocks > 16 ? 4 : a.rows <= 64 && a.kblocks > 32 ? 2 : 1;
+    a.kblocks = (a.kblocks + a.slices - 1) / a.slices;
+    const int block = a.slices * (a.rows + a.bn) * 128;
     a.per_stage = std::max(1, std::min((a.n > 32 ? 64 << 10 : 48 << 10) / block, a.kblocks));
-    const size_t stage = a.per_stage * block, slack = (128 - a.rows) * 128 + 1024;
+    const size_t stage = a.per_stage * block, slack = (128 - a.slices * a.rows) * 128 + 1024;
     a.stages = std::min({(int)((kTileSmem - slack) / stage), kMmMaxStages, (a.kblocks + a.per_stage - 1) / a.per_stage});
-    if (!raise_smem_limit_once(matmul_i8_tile_kernel<DT, KIND>, kTileSmem, raised[1])) return CMPQ_ERR_CUDA;
     if (blocks > INT32_MAX) return CMPQ_ERR_UNSUPPORTED;
-    return launch_cluster(matmul_i8_tile_kernel<DT, KIND>, (unsigned)blocks, kMmThreads, a.stages * stage + slack, 1, behind, st, wmap, umap, xmap, a);
+    const auto launch = [&](auto kernel, bool (&done)[64]) {
+        if (!raise_smem_limit_once(kernel, kTileSmem, done)) return CMPQ_ERR_CUDA;
+        return launch_cluster(kernel, (unsigned)blocks, kMmThreads, a.stages * stage + slack, 1, behind, st, wmap, umap, xmap, a);
+    };
+    return a.slices > 1 ? launch(matmul_i8_tile_kernel<DT, KIND, true>, raised[1]) : launch(matmul_i8_tile_kernel<DT, KIND, false>, raised[2]);
 }
 
 template <int DT>

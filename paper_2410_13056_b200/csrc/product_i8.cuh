@@ -154,6 +154,7 @@ struct ProductArgs {
     int wide;               // y takes 16-byte stores
     int n_tiles, m_tiles;   // tiles of channels, of tokens
     int stages, per_stage, bn, rows;  // tile kernel: stages, blocks of the sum in each, columns of a tile, token rows that a box brings
+    int slices;                       // tile kernel: of the sum; kblocks and per_stage count blocks of all slices then
     int32_t* failed;
 };
 
@@ -258,6 +259,47 @@ __device__ __forceinline__ void store_gated(uint32_t tmem, int c0, int c1, int h
             }
         }
     });
+}
+
+// Eight columns of a token's row: z, or of a gated product both projections' (u), finished and written.
+template <int DT, int KIND>
+__device__ __forceinline__ void store_eight(const ProductArgs& A, const int (&z)[8], const int (&u)[8], const float2* scale_bias, const float2* up_scale_bias,
+                                            float xs, uint16_t* y, const uint16_t* residual, int left) {
+    float f[8];
+    if (KIND == kFinish && A.residual) widen8<DT>(load8(residual, left, A.wide_residual), f);
+    auto finish = [&](auto act) {
+        uint32_t w[4];
+#pragma unroll
+        for (int j = 0; j < 8; j += 2) {
+            float v[2];
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                const float2 sb = scale_bias[j + k];
+                v[k] = (float)z[j + k] * xs * sb.x;
+                if (A.bias) v[k] += sb.y;
+                v[k] = activate<decltype(act)::value>(v[k]);
+                if (KIND == kGated) {
+                    const float2 us = up_scale_bias[j + k];
+                    float o = (float)u[j + k] * xs * us.x;
+                    if (A.ubias) o += us.y;
+                    v[k] *= o;
+                }
+                if (KIND == kFinish && A.residual) v[k] += f[j + k];
+            }
+            w[j / 2] = round16x2<DT>(v[0], v[1]);
+        }
+        if ((KIND == kGated || A.wide) && left >= 8) {
+            *reinterpret_cast<uint4*>(y) = make_uint4(w[0], w[1], w[2], w[3]);
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                if (j < left) y[j] = (uint16_t)(w[j >> 1] >> (16 * (j & 1)));
+        }
+    };
+    if (KIND == kPlain)
+        finish(ActIs<CMPQ_ACT_NONE>());
+    else
+        with_act(A.act, finish);
 }
 
 // Scale and bias of column i of a tile whose channels begin at o0: of a gated tile the first half's, then the second's.

@@ -234,7 +234,7 @@ GATED = [(1, 1, 1, 1), (1, 16, 8, 16), (1, 512, 1408, 512), (2, 100, 37, 33), (3
 # one kernel does all of these: large layers, a few tokens; long and short sums, many tiles and parts for a block, sizes that
 # fill nothing
 FEW = [(1, 2050, 5461, 2049), (2, 4096, 2001, 4097), (3, 130, 80000, 65), (4, 12800, 700, 300), (1, 64, 131072, 64), (4, 8, 1000, 20000), (2, 16, 64, 262144),
-       (4, 1024, 6000, 1024), (3, 8192, 1000, 8192), (1, 1536, 4096, 1536), (4, 13000, 700, 300)]
+       (4, 1024, 6000, 1024), (3, 8192, 1000, 8192), (1, 1536, 4096, 1536), (4, 13000, 700, 300), (4, 4097, 1500, 4100), (1, 24, 5000, 50000), (2, 100, 9000, 30000)]
 
 
 def _block(n, d_in, d_ff, d_out, dtype, act, bias):
@@ -278,6 +278,19 @@ def test_a_token_has_the_same_bytes_in_every_batch(dtype, d, ff):
             part = slice(at, at + n)
             assert torch.equal(block(x[part], residual=x[part], norm=g), y[part]), n
             assert torch.equal(layer(h[part], activation="gelu", residual=x[part]), z[part]), n
+
+
+# a few tokens and long sums: tiles whose sums are cut into slices, with slices that end early or hold one block fewer
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("n,d_in,d_out", [(5, 2049, 500), (9, 4097, 1000), (16, 2500, 2049), (25, 2177, 130), (32, 11000, 515), (33, 4225, 770), (40, 4097, 97),
+                                          (57, 5000, 2051), (64, 8200, 1001)])
+def test_long_sums_of_a_few_tokens(n, d_in, d_out, dtype):
+    test_linear_with_its_epilogue(n, d_in, d_out, dtype)
+    test_gated_block(n, d_in, d_out, d_out, dtype)
+    for i, layer in enumerate((_weights(d_out, d_in, dtype, d_out, True), _weights(d_out, d_in, dtype, d_out, False, pad=16))):
+        x = _tokens(n, d_in, dtype, i)
+        y = layer(x)
+        _compare(y, *ref.finish(*ref.linear(*ref.norm_quantize(_np(x), None, EPS), *_parts(layer)), "none", None, dtype))
 
 
 @pytest.mark.parametrize("n", [1, 20, 300])
