@@ -1,5 +1,6 @@
 // 8-bit linear layers: quantization of tokens and the integer product with scales per token and channel.
 #include <algorithm>
+#include <atomic>
 
 #include "product_i8.cuh"
 #include "walk.cuh"
@@ -130,7 +131,12 @@ constexpr size_t kTileSmem = 208 << 10;
 // second or fourth block of the sum gets rows and columns of its own then, an instruction takes as many blocks, and the slices
 // are added up at the end (see few_i8.cu): 8 tokens 11008 -> 4096 15.4 -> 12.9 us.  A kernel of its own, as its longer program
 // cost small layers 0.2 us.
-template <int DT, int KIND, bool SLICED>
+//
+// SPLIT: the sum of a tile is cut over two or four CTAs of a cluster, which lets a few wide tiles with long sums use all SMs and
+// reads the tokens fewer times than as many narrow tiles.  Each CTA then takes a part of the tile's channels and adds up what the
+// others send it of those.  128 tokens 28672 -> 1024: 40 us whole, 18 over four; 11008 -> 4096 19.4 and 16.8 over two; 256 tokens 11008 -> 2048 19.0 and 15.7.
+enum { kWhole, kSliced, kSplit };
+template <int DT, int KIND, int SUM>
 __global__ void __launch_bounds__(kMmThreads, 1)
 matmul_i8_tile_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__ CUtensorMap umap, const __grid_constant__ CUtensorMap xmap,
                       const __grid_constant__ ProductArgs A) {
@@ -141,8 +147,9 @@ matmul_i8_tile_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_con
     __shared__ uint32_t tmem_at;
     __shared__ int failed;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int nt = blockIdx.x / A.m_tiles, mt = blockIdx.x % A.m_tiles, bn = A.bn;
-    const int S = SLICED ? A.slices : 1, N = S * bn, columns = N <= 32 ? 32 : N <= 64 ? 64 : N <= 128 ? 128 : 256;
+    const int parts = SUM == kSplit ? A.slices : 1, part = SUM == kSplit ? (int)tc5::cluster_rank() : 0, k0 = part * A.kblocks;
+    const int nt = blockIdx.x / parts / A.m_tiles, mt = blockIdx.x / parts % A.m_tiles, bn = A.bn;
+    const int S = SUM == kSliced ? A.slices : 1, N = S * bn, columns = N <= 32 ? 32 : N <= 64 ? 64 : N <= 128 ? 128 : 256;
     const int row_box = A.rows * 128, box = bn * 128, a_bytes = S * row_box, b_bytes = S * box, stage = A.per_stage * (a_bytes + b_bytes);  // of a slice, of all
     if (threadIdx.x < A.stages) tc5::mbar_init(full + threadIdx.x, 1), tc5::mbar_init(empty + threadIdx.x, 1);
     if (threadIdx.x == 0) tc5::mbar_init(&done, 1), failed = 0;
@@ -160,7 +167,7 @@ matmul_i8_tile_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_con
                 const int count = min(A.per_stage, A.kblocks - k);
                 tc5::mbar_expect_tx(full + slot, count * (a_bytes + b_bytes));  // the tokens' bytes too, whoever comes first
                 uint8_t* at = smem + slot * stage + A.per_stage * a_bytes;
-                for (int i = k * S; i < (k + count) * S; ++i, at += box) {
+                for (int i = k0 + k * S; i < k0 + (k + count) * S; ++i, at += box) {
                     if (KIND == kGated) {
                         tc5::tma_load_2d(at, &wmap, full + slot, i * 128, nt * (bn / 2));
                         tc5::tma_load_2d(at + box / 2, &umap, full + slot, i * 128, nt * (bn / 2));
@@ -188,6 +195,7 @@ matmul_i8_tile_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_con
             }
             tc5::mma_commit(&done);
         }
+        __syncwarp();
     } else {
         float2* sb = reinterpret_cast<float2*>(scale_bias);
         const int wide = KIND == kGated ? bn / 2 : bn;  // channels of the tile
@@ -200,21 +208,71 @@ matmul_i8_tile_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_con
                 for (int k = 0; k < A.kblocks; k += A.per_stage) {
                     if (!tc5::mbar_wait(empty + slot, phase, &failed)) break;
                     for (int i = 0; i < min(A.per_stage, A.kblocks - k) * S; ++i)
-                        tc5::tma_load_2d(smem + slot * stage + i * row_box, &xmap, full + slot, (k * S + i) * 128, mt * 128);
+                        tc5::tma_load_2d(smem + slot * stage + i * row_box, &xmap, full + slot, (k0 + k * S + i) * 128, mt * 128);
                     if (++slot == A.stages) slot = 0, phase ^= 1;
                 }
             }
             __syncwarp();
         }
-        const int step = KIND == kGated ? 8 : 16, quad = warp & 3, t = mt * 128 + quad * 32 + lane, half = (wide / step + 1) / 2 * step;
+        const int step = KIND == kGated ? 8 : 16, quad = warp & 3, t = mt * 128 + quad * 32 + lane, mine = wide / parts;
+        const int half = SUM == kSplit ? (mine / 8 + 1) / 2 * 8 : (mine / step + 1) / 2 * step;
         const bool real = t < A.n, upper = warp >= 6;
-        const int c0 = upper ? half : 0, c1 = upper ? wide : half;
+        const int c0 = part * mine + (upper ? half : 0), c1 = part * mine + (upper ? mine : half);
         if (KIND == kFinish && A.residual && real) ask_for(A.residual + (int64_t)t * A.ldr + o0, c0, min(c1, left));
         const float xs = real ? __ldcg(A.xs + t) : 0.0f;  // written while this kernel was on its way: not the read-only path
         asm volatile("bar.sync 1, 256;" ::: "memory");
         tc5::mbar_wait_warp(&done, 0, &failed);
         tc5::fence_after_sync();
-        if (SLICED) {
+        if (SUM == kSplit) {
+            // The CTA finishes `mine` of the tile's channels: the others' sums of those come through shared memory, which no copy
+            // or product uses any more, [CTA][token][column]; rows 16 bytes more apart, for the banks.
+            const int both = KIND == kGated ? 2 : 1, pitch = both * mine + 4, first = part * mine;
+            const uint32_t rows = tmem + ((uint32_t)quad << 21);
+            int32_t* sums = reinterpret_cast<int32_t*>(smem) + (quad * 32 + lane) * pitch;
+            const bool warp_real = mt * 128 + quad * 32 < A.n;
+            tc5::cluster_sync();  // everybody's products have ended
+            if (warp_real)
+                for (int p = 1; p < parts; ++p) {
+                    const int to = (part + p) & (parts - 1);
+                    for (int b = 0; b < both; ++b)
+                        for (int c = c0 - first; c < c1 - first; c += 8) {
+                            uint32_t r[8];
+                            tc5::tmem_ld8(rows + b * wide + to * mine + c, r);
+                            tc5::tmem_ld_wait();
+                            if (real) {
+                                int32_t* at = sums + (p - 1) * 128 * pitch + b * mine + c;
+                                tc5::store_remote(at, to, r[0], r[1], r[2], r[3]);
+                                tc5::store_remote(at + 4, to, r[4], r[5], r[6], r[7]);
+                            }
+                        }
+                }
+            __syncwarp();
+            tc5::cluster_sync();
+            if (warp_real)
+                for (int o = c0; o < c1; o += 8) {
+                    uint32_t r[8], s[8] = {};
+                    tc5::tmem_ld8(rows + o, r);
+                    if (KIND == kGated) tc5::tmem_ld8(rows + wide + o, s);
+                    tc5::tmem_ld_wait();
+                    int z[8], u[8];
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) z[j] = (int)r[j], u[j] = (int)s[j];
+                    for (int p = 0; p < parts - 1; ++p)
+#pragma unroll
+                        for (int j = 0; j < 8; j += 4) {
+                            const int32_t* at = sums + p * 128 * pitch + o - first + j;
+                            const int4 a = *reinterpret_cast<const int4*>(at);
+                            z[j] += a.x, z[j + 1] += a.y, z[j + 2] += a.z, z[j + 3] += a.w;
+                            if (KIND == kGated) {
+                                const int4 b = *reinterpret_cast<const int4*>(at + mine);
+                                u[j] += b.x, u[j + 1] += b.y, u[j + 2] += b.z, u[j + 3] += b.w;
+                            }
+                        }
+                    if (real && o < left)
+                        store_eight<DT, KIND>(A, z, u, sb + o, sb + wide + o, xs, A.y + (int64_t)t * A.ldy + o0 + o, A.residual + (int64_t)t * A.ldr + o0 + o,
+                                              left - o);
+                }
+        } else if (SUM == kSliced) {
             // Row q rows + t holds slice q's sums of token t, in columns q bn and on.  They are added up through shared memory, which
             // no copy or product uses any more: [slice][token][column].
             int32_t* sums = reinterpret_cast<int32_t*>(smem);
@@ -253,6 +311,7 @@ matmul_i8_tile_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_con
         tc5::fence_before_sync();
     }
     __syncwarp();
+    if (SUM == kSplit && warp < 2) tc5::cluster_sync(), tc5::cluster_sync();  // the epilogue's
     __syncthreads();
     if (failed) {  // the loads that were asked for have to land before the shared memory is given back
         if (threadIdx.x == 0) {
@@ -421,6 +480,48 @@ static int64_t pair_cycles(const ProductArgs& a, int bn) {
     return (tiles + pairs - 1) / pairs * a.kblocks * (600 * (256 + bn) / 512) + 14000;  // the pace is that of the loads
 }
 
+// Slices of a tile's sum, for products that no cluster shares.  Shorter sums are not worth the adding up, and wider tiles wait for
+// memory: 32 tokens 2048 -> 2048 6.0 -> 6.6 us with four slices, 53 tokens 4096 -> 4096 9.2 -> 9.5 and 28672 -> 8192 45.8 -> 46.9
+// with two.
+static int slices_of(const ProductArgs& a, int rows, int bn) {
+    return bn > 32 ? 1 : rows <= 32 && a.kblocks > 16 ? 4 : rows <= 64 && a.kblocks > 32 ? 2 : 1;
+}
+
+// Clusters of `parts` CTAs, each on an SM of its own, that run at once: fewer than the SMs would allow (33 of four on 148 SMs), as
+// a cluster keeps to one group of SMs.  Asked once per device; 0 where that fails.
+static int cluster_slots(int parts) {
+    static std::atomic<int> cached[2][64];  // 0 = not asked yet
+    static bool raised[64];
+    const auto kernel = matmul_i8_tile_kernel<CMPQ_BF16, kPlain, kSplit>;
+    int dev = 0, n = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess) return 0;
+    std::atomic<int>* slot = dev >= 0 && dev < 64 ? &cached[parts == 4][dev] : nullptr;
+    if (slot && (n = slot->load(std::memory_order_relaxed)) > 0) return n;
+    if (!raise_smem_limit_once(kernel, kTileSmem, raised)) return 0;
+    cudaLaunchAttribute attr;
+    attr.id = cudaLaunchAttributeClusterDimension;
+    attr.val.clusterDim.x = parts, attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(parts * sm_count()), cfg.blockDim = dim3(kMmThreads), cfg.dynamicSmemBytes = kTileSmem;
+    cfg.attrs = &attr, cfg.numAttrs = 1;
+    if (cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) != cudaSuccess) return 0;
+    if (slot) slot->store(n, std::memory_order_relaxed);
+    return n;
+}
+
+// The same with `parts` CTAs of a cluster to a tile, or one, to compare the two.  Here the loads' way from L2 and the weights' from
+// memory delay one another, and a cluster pays 3300 cycles for its two barriers and for sums that cross it.  Fitted to 600 calls
+// of 5 to 512 tokens, 2304 x 512 to 28672 x 12288: what it chooses is 1 % slower than the best of them in the mean (14 % at most)
+// and takes 0.90 of the time without clusters (0.45 to 1.05).
+static int64_t parts_cycles(const ProductArgs& a, int parts, int bn, int slots) {
+    const int64_t rounds = ceil_div(ceil_div(a.n, 128) * ceil_div(a.cols, bn), slots);
+    const int rows = std::min(128, (a.n + 7) / 8 * 8), slices = parts > 1 ? 1 : slices_of(a, rows, bn);
+    const int64_t loads = rounds * ((a.kblocks + parts - 1) / parts) * std::max(2 * std::max(64, bn) / slices, (bn + rows) * 2);
+    const int64_t memory = (int64_t)a.kblocks * 128 * a.cols / 3400;
+    return std::max(loads, memory) + std::min(loads, memory) * 2 / 5 + rounds * (10000 + 7 * bn) + (slices > 1 ? 2000 : 0) +
+           (parts > 1 ? 3300 + rows * (bn - bn / parts) * 2 / 5 : 0);
+}
+
 template <int DT, int KIND>
 static cmpq_status launch_kind(const TokenCodes& x, int64_t d_in, const Weight8& w, const Weight8* u, ProductArgs a, bool behind, cudaStream_t st) {
     a.kblocks = (int)((d_in + 127) / 128);
@@ -433,8 +534,20 @@ static cmpq_status launch_kind(const TokenCodes& x, int64_t d_in, const Weight8&
     int wide = 256;  // narrower where that fills the last round better
     for (int bn = 224; bn >= 128; bn -= 32)
         if (pair_cycles(a, bn) < pair_cycles(a, wide)) wide = bn;
-    const bool pair = a.n > 128 && pair_cycles(a, wide) < tile_cycles(a, a.bn);
+    bool pair = a.n > 128 && pair_cycles(a, wide) < tile_cycles(a, a.bn);
     if (pair) a.bn = wide;
+    // A few wide tiles with long sums: two or four CTAs to a tile.  A CTA finishes whole groups of eight channels.
+    int parts = 1;
+    if (a.kblocks > 16) {
+        int64_t least = pair ? (pair_cycles(a, wide) - 14000) * 14 / 10 + 14200 : parts_cycles(a, 1, a.bn, sm_count());  // pairs by the same fit
+        for (int c = 2; c <= 4; c *= 2) {
+            const int slots = cluster_slots(c);
+            for (int bn = 16 * c; slots > 0 && bn <= 256; bn += 16 * c) {
+                const int64_t cycles = parts_cycles(a, c, bn, slots);
+                if (cycles < least) least = cycles, a.bn = bn, parts = c, pair = false;
+            }
+        }
+    }
     a.rows = pair ? 128 : std::min(128, (a.n + 7) / 8 * 8);
     CUtensorMap wmap, umap, xmap;
     const int box = pair || KIND == kGated ? a.bn / 2 : a.bn, channels = KIND == kGated ? a.bn / 2 : a.bn;
@@ -442,7 +555,7 @@ static cmpq_status launch_kind(const TokenCodes& x, int64_t d_in, const Weight8&
     umap = wmap;
     if (u && !make_byte_map(&umap, u->codes, a.d_out, d_in, u->ld, box)) return CMPQ_ERR_CUDA;
     a.n_tiles = (a.d_out + channels - 1) / channels;
-    static bool raised[3][64];
+    static bool raised[4][64];
     if (pair) {
         a.m_tiles = (a.n + 255) / 256;
         if (!raise_smem_limit_once(matmul_i8_pair_kernel<DT, KIND>, kPairSmem, raised[0])) return CMPQ_ERR_CUDA;
@@ -453,20 +566,20 @@ static cmpq_status launch_kind(const TokenCodes& x, int64_t d_in, const Weight8&
     a.m_tiles = (a.n + 127) / 128;
     // one block to an SM: two that share it were slower at every size, their rounds and tails cost more than they hide
     const int64_t blocks = (int64_t)a.m_tiles * a.n_tiles;
-    // shorter sums are not worth the adding up, and wider tiles wait for memory: 32 tokens 2048 -> 2048 6.0 -> 6.6 us with four
-    // slices, 53 tokens 4096 -> 4096 9.2 -> 9.5 and 28672 -> 8192 45.8 -> 46.9 with two
-    a.slices = a.bn > 32 ? 1 : a.rows <= 32 && a.kblocks > 16 ? 4 : a.rows <= 64 && a.kblocks > 32 ? 2 : 1;
+    a.slices = parts > 1 ? parts : slices_of(a, a.rows, a.bn);
     a.kblocks = (a.kblocks + a.slices - 1) / a.slices;
-    const int block = a.slices * (a.rows + a.bn) * 128;
+    const int slices = parts > 1 ? 1 : a.slices, block = slices * (a.rows + a.bn) * 128;
     a.per_stage = std::max(1, std::min((a.n > 32 ? 64 << 10 : 48 << 10) / block, a.kblocks));
-    const size_t stage = a.per_stage * block, slack = (128 - a.slices * a.rows) * 128 + 1024;
+    const size_t stage = a.per_stage * block, slack = (128 - slices * a.rows) * 128 + 1024;
     a.stages = std::min({(int)((kTileSmem - slack) / stage), kMmMaxStages, (a.kblocks + a.per_stage - 1) / a.per_stage});
     if (blocks > INT32_MAX) return CMPQ_ERR_UNSUPPORTED;
+    const size_t exchange = (parts - 1) * 128 * (a.bn / parts + 4) * 4 + 1024;
     const auto launch = [&](auto kernel, bool (&done)[64]) {
         if (!raise_smem_limit_once(kernel, kTileSmem, done)) return CMPQ_ERR_CUDA;
-        return launch_cluster(kernel, (unsigned)blocks, kMmThreads, a.stages * stage + slack, 1, behind, st, wmap, umap, xmap, a);
+        return launch_cluster(kernel, (unsigned)blocks * parts, kMmThreads, std::max(a.stages * stage + slack, exchange), parts, behind, st, wmap, umap, xmap, a);
     };
-    return a.slices > 1 ? launch(matmul_i8_tile_kernel<DT, KIND, true>, raised[1]) : launch(matmul_i8_tile_kernel<DT, KIND, false>, raised[2]);
+    if (parts > 1) return launch(matmul_i8_tile_kernel<DT, KIND, kSplit>, raised[3]);
+    return a.slices > 1 ? launch(matmul_i8_tile_kernel<DT, KIND, kSliced>, raised[1]) : launch(matmul_i8_tile_kernel<DT, KIND, kWhole>, raised[2]);
 }
 
 template <int DT>

@@ -154,7 +154,7 @@ struct ProductArgs {
     int wide;               // y takes 16-byte stores
     int n_tiles, m_tiles;   // tiles of channels, of tokens
     int stages, per_stage, bn, rows;  // tile kernel: stages, blocks of the sum in each, columns of a tile, token rows that a box brings
-    int slices;                       // tile kernel: of the sum; kblocks and per_stage count blocks of all slices then
+    int slices;  // of a tile's sum, over an instruction or over the CTAs of a cluster
     int32_t* failed;
 };
 

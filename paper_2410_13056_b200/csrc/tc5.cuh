@@ -226,6 +226,14 @@ __device__ __forceinline__ uint32_t cluster_rank() {
 __device__ __forceinline__ void cluster_sync() {
     asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
+// 16 bytes into the shared memory of the cluster's CTA `rank`, at the place of `at` in this one's.
+__device__ __forceinline__ void store_remote(const void* at, uint32_t rank, uint32_t x, uint32_t y, uint32_t z, uint32_t w) {
+    asm volatile(
+        "{\n\t.reg .b32 a;\n\tmapa.shared::cluster.u32 a, %0, %1;\n\t"
+        "st.shared::cluster.v4.b32 [a], {%2, %3, %4, %5};\n\t}" ::"r"(smem_addr(at)),
+        "r"(rank), "r"(x), "r"(y), "r"(z), "r"(w)
+        : "memory");
+}
 __device__ __forceinline__ void dependents_may_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 __device__ __forceinline__ void wait_for_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 

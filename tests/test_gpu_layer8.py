@@ -293,6 +293,15 @@ def test_long_sums_of_a_few_tokens(n, d_in, d_out, dtype):
         _compare(y, *ref.finish(*ref.linear(*ref.norm_quantize(_np(x), None, EPS), *_parts(layer)), "none", None, dtype))
 
 
+# tiles whose sums two or four blocks share: parts that end early, one or more tiles of tokens, channels that fill no part, both
+# halves of a gated tile
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("n,d_in,d_out", [(5, 28672, 600), (20, 13000, 1100), (33, 5641, 1024), (64, 11000, 515), (100, 11008, 2050), (127, 8192, 1000), (128, 20480, 33),
+                                          (129, 11008, 450), (200, 28672, 1030), (300, 9000, 520), (512, 8193, 257)])
+def test_long_sums_over_a_cluster(n, d_in, d_out, dtype):
+    test_long_sums_of_a_few_tokens(n, d_in, d_out, dtype)
+
+
 @pytest.mark.parametrize("n", [1, 20, 300])
 def test_largest_sums_are_exact(n):
     """All codes at +-127 over long rows, in both of the block's products."""
