@@ -572,7 +572,7 @@ static cmpq_status launch_kind(const TokenCodes& x, int64_t d_in, const Weight8&
     a.per_stage = std::max(1, std::min((a.n > 32 ? 64 << 10 : 48 << 10) / block, a.kblocks));
     const size_t stage = a.per_stage * block, slack = (128 - slices * a.rows) * 128 + 1024;
     a.stages = std::min({(int)((kTileSmem - slack) / stage), kMmMaxStages, (a.kblocks + a.per_stage - 1) / a.per_stage});
-    if (blocks > INT32_MAX) return CMPQ_ERR_UNSUPPORTED;
+    if (blocks * parts > INT32_MAX) return CMPQ_ERR_UNSUPPORTED;
     const size_t exchange = (parts - 1) * 128 * (a.bn / parts + 4) * 4 + 1024;
     const auto launch = [&](auto kernel, bool (&done)[64]) {
         if (!raise_smem_limit_once(kernel, kTileSmem, done)) return CMPQ_ERR_CUDA;
