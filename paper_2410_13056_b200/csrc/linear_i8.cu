@@ -123,18 +123,19 @@ constexpr size_t kTileSmem = 208 << 10;
 //
 // Measured with the quantization in graphs, weights from memory: 8 tokens 4096 -> 4096 8.2 us, 8192 -> 28672 41.8 us (5.6 TB/s,
 // 0.85 of the copy rate); 53 tokens 4096 -> 11008 13.4 us (3.4 TB/s: launch, first loads and the last stage's way out are
-// half of it).  Splitting the sum over a cluster instead, weights as rows, took 1.5, 1.3 and 2.4 times as long.
+// half of it).  For these, weights as rows and the sum over a cluster took 1.5, 1.3 and 2.4 times as long.
 //
 // A gated tile's columns are bn / 2 channels of the gate and the same ones of the second projection, from maps of their own.
 //
-// SLICED: narrow tiles of few tokens leave most of an instruction's rows empty, and it takes 40 cycles all the same.  Every
+// kSliced: narrow tiles of few tokens leave most of an instruction's rows empty, and it takes 40 cycles all the same.  Every
 // second or fourth block of the sum gets rows and columns of its own then, an instruction takes as many blocks, and the slices
 // are added up at the end (see few_i8.cu): 8 tokens 11008 -> 4096 15.4 -> 12.9 us.  A kernel of its own, as its longer program
 // cost small layers 0.2 us.
 //
-// SPLIT: the sum of a tile is cut over two or four CTAs of a cluster, which lets a few wide tiles with long sums use all SMs and
+// kSplit: the sum of a tile is cut over two or four CTAs of a cluster, which lets a few wide tiles with long sums use all SMs and
 // reads the tokens fewer times than as many narrow tiles.  Each CTA then takes a part of the tile's channels and adds up what the
-// others send it of those.  128 tokens 28672 -> 1024: 40 us whole, 18 over four; 11008 -> 4096 19.4 and 16.8 over two; 256 tokens 11008 -> 2048 19.0 and 15.7.
+// others send it of those.  128 tokens 28672 -> 1024: 40 us whole, 18 over four; 11008 -> 4096 19.4 and 16.9 over
+// two; 256 tokens 11008 -> 2048 19.0 and 15.7.
 enum { kWhole, kSliced, kSplit };
 template <int DT, int KIND, int SUM>
 __global__ void __launch_bounds__(kMmThreads, 1)
