@@ -212,6 +212,7 @@ bool few_fits(int64_t d_in) { return d_in <= 4096; }
 
 cmpq_status enqueue_few(const void* X, cmpq_dtype dt, int64_t n, int64_t d_in, int64_t ldx, const void* norm, float eps, const Weight8& w, int64_t d_out,
                         const Weight8* u, const Finish& f, void* y, int64_t ldy, int32_t* word, int32_t* gave_up, bool behind, cudaStream_t st) {
+    if (sm_count() <= 0) return CMPQ_ERR_CUDA;  // no device to plan for
     FewProduct a = {};
     a.x = {static_cast<const uint16_t*>(X), ldx, aligned_to(X, 16) && ldx % 8 == 0, {static_cast<const uint16_t*>(norm), aligned_to(norm, 16), eps},
            d_in, (int)n, word};

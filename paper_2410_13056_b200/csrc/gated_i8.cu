@@ -458,6 +458,7 @@ extern "C" cmpq_status cmpq_gated_i8(const void* X, cmpq_dtype dt, int64_t n, in
     const GatedSpace g(ws, n, d_in, d_ff, d_out);
     const auto st = static_cast<cudaStream_t>(stream);
     auto* kept = static_cast<int32_t*>(state);
+    if (sm_count() <= 0) return CMPQ_ERR_CUDA;  // no device to plan for
     if (n <= kFewTokens) {
         FewArgs a = {};
         a.x = {static_cast<const uint16_t*>(X), ldx, aligned_to(X, 16) && ldx % 8 == 0, {static_cast<const uint16_t*>(norm), aligned_to(norm, 16), eps},

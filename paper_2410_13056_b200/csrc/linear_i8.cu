@@ -525,6 +525,7 @@ static int64_t parts_cycles(const ProductArgs& a, int parts, int bn, int slots) 
 
 template <int DT, int KIND>
 static cmpq_status launch_kind(const TokenCodes& x, int64_t d_in, const Weight8& w, const Weight8* u, ProductArgs a, bool behind, cudaStream_t st) {
+    if (sm_count() <= 0) return CMPQ_ERR_CUDA;  // no device to plan for
     a.kblocks = (int)((d_in + 127) / 128);
     a.wide = aligned_to(a.y, 16) && a.ldy % 8 == 0;
     a.wide_residual = aligned_to(a.residual, 16) && a.ldr % 8 == 0;

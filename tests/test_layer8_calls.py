@@ -1,0 +1,50 @@
+"""What calls of the 8-bit layers and of the gated block do where they cannot run, on the host: nothing here needs a GPU."""
+import os
+import subprocess
+import sys
+
+import pytest
+import torch
+
+from paper_2410_13056_b200 import binding as B
+from paper_2410_13056_b200 import build as cuda_build
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+CUDA = 4
+
+
+@pytest.fixture(scope="module")
+def L():
+    cuda_build.build()
+    return B.lib()
+
+
+# Calls whose arguments are all right, in a process of their own: one that ends by a signal ends alone.
+CALLS = r"""
+import ctypes
+from paper_2410_13056_b200 import binding as B
+L = B.lib()
+buf = (ctypes.c_char * (1 << 20))()
+p = (ctypes.addressof(buf) + 255) // 256 * 256
+y, room = p + (1 << 19), 1 << 40
+for name, n, d_in, d_ff, d_out in %r:
+    w = B.Weight8(p, (max(d_in, d_ff) + 15) // 16 * 16, p, None)
+    for word in (None, p):
+        if name == "linear":
+            s = L.cmpq_linear_i8_fused(p, 0, n, d_in, d_in, None, 0.0, w, d_out, 0, None, 0, y, d_out, word, p, room, None)
+        elif name == "matmul":
+            s = L.cmpq_matmul_i8(p, w.ld, p, p, w.ld, p, None, 0, n, d_in, d_out, y, d_out, p, room, None)
+        else:
+            s = L.cmpq_gated_i8(p, 0, n, d_in, d_in, None, 0.0, w, w, w, d_ff, d_out, 2, None, 0, y, d_out, word, p, p, room, None)
+        print(name, n, d_in, d_ff, d_out, word is not None, s, flush=True)
+"""
+
+
+def test_without_a_device_calls_answer_an_error(L):
+    if torch.cuda.is_available():
+        pytest.skip("the addresses are no GPU's")
+    calls = [("linear", 1, 20, 0, 5), ("linear", 4, 4096, 0, 500), ("linear", 9, 20, 0, 5), ("linear", 300, 9000, 0, 500), ("matmul", 2, 9000, 0, 500),
+             ("gated", 1, 20, 30, 5), ("gated", 2, 8192, 8192, 8192), ("gated", 9, 20, 30, 5)]
+    run = subprocess.run([sys.executable, "-c", CALLS % calls], cwd=ROOT, capture_output=True, text=True, timeout=200)
+    want = ["%s %d %d %d %d %s %d" % (*c, word, CUDA) for c in calls for word in (False, True)]
+    assert run.returncode == 0 and run.stdout.splitlines() == want, (run.returncode, run.stdout, run.stderr)
