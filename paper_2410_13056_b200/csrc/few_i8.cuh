@@ -32,18 +32,6 @@ __device__ __forceinline__ uint8_t* code_at(uint8_t* base, int row, int k) {
     return base + (k >> 7) * kFewRows * 128 + row * 128 + (((k >> 4 & 7) ^ row) << 4) + (k & 15);
 }
 
-// load8 of rows that a kernel may have written while this one was on its way: not through the read-only path.
-__device__ __forceinline__ uint4 load8_written(const uint16_t* p, int64_t left, bool wide) {
-    if (wide && left >= 8) return __ldcg(reinterpret_cast<const uint4*>(p));
-    uint32_t w[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const uint32_t lo = 2 * i < left ? __ldcg(p + 2 * i) : 0u, hi = 2 * i + 1 < left ? __ldcg(p + 2 * i + 1) : 0u;
-        w[i] = lo | hi << 16;
-    }
-    return make_uint4(w[0], w[1], w[2], w[3]);
-}
-
 struct TokenParts {  // in shared memory
     uint32_t m[kFewTokens][8];
     float s[kFewTokens][8];

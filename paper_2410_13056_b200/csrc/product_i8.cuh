@@ -10,6 +10,19 @@ namespace cmpq {
 
 constexpr int kQtThreads = 256;
 
+// load8 of rows that this kernel writes too (a residual may be the output), or that one before it may have written while this
+// one was on its way: not through the read-only path, which is for memory that nobody writes as long as a kernel runs.
+__device__ __forceinline__ uint4 load8_written(const uint16_t* p, int64_t left, bool wide) {
+    if (wide && left >= 8) return __ldcg(reinterpret_cast<const uint4*>(p));
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t lo = 2 * i < left ? __ldcg(p + 2 * i) : 0u, hi = 2 * i + 1 < left ? __ldcg(p + 2 * i + 1) : 0u;
+        w[i] = lo | hi << 16;
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
 struct RowParts {  // in shared memory
     uint32_t m[kQtThreads / 32];
     float s[kQtThreads / 32];
@@ -186,12 +199,12 @@ __device__ __forceinline__ void store_rows(uint32_t tmem, int c0, int c1, const 
     }
 }
 
-// Sixteen 16-bit entries of a row, of which `left` exist, as floats.
+// Sixteen 16-bit entries of a residual's row, of which `left` exist, as floats.
 template <int DT>
 __device__ __forceinline__ void load16(const uint16_t* p, int left, bool wide, float (&f)[16]) {
     float a[8], b[8];
-    widen8<DT>(load8(p, left, wide), a);
-    widen8<DT>(load8(p + 8, left - 8, wide), b);
+    widen8<DT>(load8_written(p, left, wide), a);
+    widen8<DT>(load8_written(p + 8, left - 8, wide), b);
 #pragma unroll
     for (int i = 0; i < 8; ++i) f[i] = a[i], f[i + 8] = b[i];
 }
@@ -266,7 +279,7 @@ template <int DT, int KIND>
 __device__ __forceinline__ void store_eight(const ProductArgs& A, const int (&z)[8], const int (&u)[8], const float2* scale_bias, const float2* up_scale_bias,
                                             float xs, uint16_t* y, const uint16_t* residual, int left) {
     float f[8];
-    if (KIND == kFinish && A.residual) widen8<DT>(load8(residual, left, A.wide_residual), f);
+    if (KIND == kFinish && A.residual) widen8<DT>(load8_written(residual, left, A.wide_residual), f);
     auto finish = [&](auto act) {
         uint32_t w[4];
 #pragma unroll

@@ -1,5 +1,6 @@
 """What calls of the 8-bit layers and of the gated block do where they cannot run, on the host: nothing here needs a GPU."""
 import os
+import re
 import subprocess
 import sys
 
@@ -48,3 +49,30 @@ def test_without_a_device_calls_answer_an_error(L):
     run = subprocess.run([sys.executable, "-c", CALLS % calls], cwd=ROOT, capture_output=True, text=True, timeout=200)
     want = ["%s %d %d %d %d %s %d" % (*c, word, CUDA) for c in calls for word in (False, True)]
     assert run.returncode == 0 and run.stdout.splitlines() == want, (run.returncode, run.stdout, run.stderr)
+
+
+def _body(source, head):
+    """The text of the function whose declaration contains `head`, braces matched."""
+    at = source.index(head)
+    at = source.index("{", at)
+    depth, end = 0, at
+    while True:
+        depth += {"{": 1, "}": -1}.get(source[end], 0)
+        end += 1
+        if depth == 0:
+            return source[at:end]
+
+
+def test_residuals_are_not_read_as_memory_that_nobody_writes():
+    """A residual may be the output, so the kernel that reads it writes it: neither load8, whose wide loads go through the
+    read-only path, nor __ldg may read one.  On the chip the difference cannot be seen as long as a thread reads its own entries."""
+    read_only = re.compile(r"\b(load8|__ldg)\(")
+    for name in sorted(os.listdir(cuda_build.CSRC)):
+        for line in open(os.path.join(cuda_build.CSRC, name)):
+            for call in read_only.finditer(line):
+                assert not re.match(r"[^;]*\bresidual\b", line[call.end():].split(")")[0]), (name, line)
+    product = open(os.path.join(cuda_build.CSRC, "product_i8.cuh")).read()
+    for head in ("void load16(", "void store_finished(", "void store_eight("):
+        body = _body(product, head)
+        assert not read_only.search(body), (head, body)
+    assert "load16<DT>(residual" in _body(product, "void store_finished(")
