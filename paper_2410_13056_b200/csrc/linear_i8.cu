@@ -1,7 +1,7 @@
 // 8-bit linear layers: quantization of tokens and the integer product with scales per token and channel.
 #include <algorithm>
-#include <atomic>
 
+#include "asked.h"
 #include "product_i8.cuh"
 #include "walk.cuh"
 
@@ -489,25 +489,25 @@ static int slices_of(const ProductArgs& a, int rows, int bn) {
 }
 
 // Clusters of `parts` CTAs, each on an SM of its own, that run at once: fewer than the SMs would allow (33 of four on 148 SMs), as
-// a cluster keeps to one group of SMs.  Asked once per device; 0 where that fails.
+// a cluster keeps to one group of SMs.  Asked once per device; 0, and no error left behind, where that fails.
 static int cluster_slots(int parts) {
-    static std::atomic<int> cached[2][64];  // 0 = not asked yet
+    static AskedOnce asked[2];
     static bool raised[64];
-    const auto kernel = matmul_i8_tile_kernel<CMPQ_BF16, kPlain, kSplit>;
-    int dev = 0, n = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess) return 0;
-    std::atomic<int>* slot = dev >= 0 && dev < 64 ? &cached[parts == 4][dev] : nullptr;
-    if (slot && (n = slot->load(std::memory_order_relaxed)) > 0) return n;
-    if (!raise_smem_limit_once(kernel, kTileSmem, raised)) return 0;
-    cudaLaunchAttribute attr;
-    attr.id = cudaLaunchAttributeClusterDimension;
-    attr.val.clusterDim.x = parts, attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(parts * sm_count()), cfg.blockDim = dim3(kMmThreads), cfg.dynamicSmemBytes = kTileSmem;
-    cfg.attrs = &attr, cfg.numAttrs = 1;
-    if (cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) != cudaSuccess) return 0;
-    if (slot) slot->store(n, std::memory_order_relaxed);
-    return n;
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess) return cudaGetLastError(), 0;
+    return asked[parts == 4].get(dev, [parts] {
+        const auto kernel = matmul_i8_tile_kernel<CMPQ_BF16, kPlain, kSplit>;
+        cudaLaunchAttribute attr;
+        attr.id = cudaLaunchAttributeClusterDimension;
+        attr.val.clusterDim.x = parts, attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = dim3(parts * sm_count()), cfg.blockDim = dim3(kMmThreads), cfg.dynamicSmemBytes = kTileSmem;
+        cfg.attrs = &attr, cfg.numAttrs = 1;
+        int n = 0;
+        if (raise_smem_limit_once(kernel, kTileSmem, raised) && cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) == cudaSuccess) return n;
+        cudaGetLastError();  // not the launch's that comes next, which does without clusters
+        return 0;
+    });
 }
 
 // The same with `parts` CTAs of a cluster to a tile, or one, to compare the two.  Here the loads' way from L2 and the weights' from

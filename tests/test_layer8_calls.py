@@ -76,3 +76,41 @@ def test_residuals_are_not_read_as_memory_that_nobody_writes():
         body = _body(product, head)
         assert not read_only.search(body), (head, body)
     assert "load16<DT>(residual" in _body(product, "void store_finished(")
+
+
+ASKED = r"""
+#include <cstdio>
+#include <initializer_list>
+#include "asked.h"
+
+int main() {
+    cmpq::AskedOnce fails, works;
+    int asked = 0, answers = 0;
+    for (int i = 0; i < 3; ++i)
+        for (int device : {0, 63}) answers += fails.get(device, [&] { return ++asked, 0; });
+    printf("%d %d ", answers, asked);  // no answer is kept as one
+    asked = answers = 0;
+    for (int i = 0; i < 3; ++i)
+        for (int device : {0, 5, 63}) answers += works.get(device, [&] { return ++asked, 7; });
+    printf("%d %d ", answers, asked);
+    asked = answers = 0;
+    for (int device : {-1, 64, 64}) answers += works.get(device, [&] { return ++asked, 9; });  // devices without a place
+    printf("%d %d\n", answers, asked);
+}
+"""
+
+
+def test_a_number_that_cannot_be_had_is_asked_for_once(tmp_path):
+    src, exe = tmp_path / "asked.cpp", str(tmp_path / "asked")
+    src.write_text(ASKED)
+    subprocess.run(["g++", "-std=c++17", "-O1", "-I", cuda_build.CSRC, str(src), "-o", exe], check=True)
+    assert subprocess.run([exe], capture_output=True, text=True, timeout=20).stdout.split() == ["0", "2", "63", "3", "27", "3"]
+
+
+def test_a_failed_query_leaves_no_error_behind():
+    """The launch behind it asks for the last error."""
+    source = open(os.path.join(cuda_build.CSRC, "linear_i8.cu")).read()
+    body = _body(source, "static int cluster_slots(")
+    failing = body[body.index("cudaOccupancyMaxActiveClusters"):]
+    assert re.match(r"[^;]*== cudaSuccess\) return n;\s*cudaGetLastError\(\);", failing), body
+    assert re.search(r"cudaGetDevice\(&dev\) != cudaSuccess\) return cudaGetLastError\(\), 0;", body)
