@@ -556,34 +556,97 @@ def cmpq_linear_i8(X, wc, w_scale, bias, y, ws, nonfinite=None):
         raise CmpqError(st, "cmpq_linear_i8")
 
 
+# The calls below are not made per token (serving.py makes theirs in C++), so what they are given is looked at before its address
+# is taken: kinds, sizes, and that all of it lies on X's device.
+
+def _vector(t, n, dtype, home, name):
+    """Address of `n` contiguous entries of `dtype` beside `home`; None stays."""
+    if t is None:
+        return None
+    if t.dtype != dtype or tuple(t.shape) != (n,) or not t.is_contiguous() or t.device != home.device:
+        raise ValueError("%s needs %d contiguous entries of %s on %s, got %s of shape %s on %s"
+                         % (name, n, dtype, home.device, t.dtype, tuple(t.shape), t.device))
+    return t.data_ptr()
+
+
+def _matrix(t, n, width, X, name):
+    """Address and leading dimension of [n][width] entries of X's dtype beside X; None stays."""
+    if t is None:
+        return None, 0
+    if t.dtype != X.dtype or tuple(t.shape) != (n, width) or t.device != X.device:
+        raise ValueError("%s needs shape [%d][%d] and X's dtype, beside it, got %s of shape %s on %s"
+                         % (name, n, width, t.dtype, tuple(t.shape), t.device))
+    return t.data_ptr(), _rows(t, width, name)
+
+
+def _space(t, X, name, least=0):
+    """Address and size in bytes of a buffer beside X."""
+    if not t.is_contiguous() or t.device != X.device or t.numel() * t.element_size() < least:
+        raise ValueError("%s needs %d contiguous bytes on %s, got %d on %s" % (name, least, X.device, t.numel() * t.element_size(), t.device))
+    return t.data_ptr(), t.numel() * t.element_size()
+
+
+def _word(t, X, name):
+    """Address of a call's word, an int32 beside X; None stays."""
+    if t is not None and (t.dtype != torch.int32 or t.numel() < 1 or t.device != X.device):
+        raise ValueError("%s needs an int32 on %s" % (name, X.device))
+    return _at(t)
+
+
 def weight8(codes, scale, bias=None):
-    """Weight8 structure of a layer's codes (int8 [d_out][d_in], rows on 16 bytes), scales (fp32 [d_out]) and bias."""
-    return Weight8(codes.data_ptr(), _code_rows(codes), scale.data_ptr(), None if bias is None else bias.data_ptr())
+    """Weight8 structure of a layer's codes (int8 [d_out][d_in], rows on 16 bytes), scales (fp32 [d_out]) and bias ([d_out] of the
+    activations' dtype), which it keeps."""
+    if codes.dtype != torch.int8 or codes.dim() != 2 or (codes.shape[1] > 1 and codes.stride(1) != 1):
+        raise ValueError("codes needs contiguous rows of int8 [d_out][d_in], got %s of shape %s" % (codes.dtype, tuple(codes.shape)))
+    d_out = codes.shape[0]
+    w = Weight8(codes.data_ptr(), _code_rows(codes), _vector(scale, d_out, torch.float32, codes, "scale"),
+                _vector(bias, d_out, torch.float16 if bias is None else bias.dtype, codes, "bias"))
+    w.tensors = codes, scale, bias
+    return w
+
+
+def _weight(w, d_out, d_in, X, name):
+    """A Weight8; one made by weight8() has to be [d_out][d_in], beside X, with a bias of its dtype."""
+    if hasattr(w, "tensors"):
+        codes, _, bias = w.tensors
+        if tuple(codes.shape) != (d_out, d_in) or codes.device != X.device or (bias is not None and bias.dtype != X.dtype):
+            raise ValueError("%s needs codes [%d][%d] beside X and a bias of its dtype, got codes %s on %s, bias %s"
+                             % (name, d_out, d_in, tuple(codes.shape), codes.device, None if bias is None else bias.dtype))
+    return w
+
+
+def _act(act):
+    if act not in ACTS:
+        raise ValueError("activation needs to be one of %s, got %r" % (", ".join(k for k in ACTS if k), act))
+    return ACTS[act]
+
+
+def _norm(norm, d, X):
+    return _vector(norm, d, X.dtype, X, "norm")
 
 
 def cmpq_norm_quantize_tokens(X, norm, eps, codes, scale, nonfinite=None):
     """cmpq_quantize_tokens behind a root-mean-square norm with weight `norm` ([d] of X's dtype, or None)."""
     n, d = X.shape
-    if norm is not None and (norm.dtype != X.dtype or tuple(norm.shape) != (d,) or not norm.is_contiguous() or norm.device != X.device):
-        raise ValueError("norm needs %d contiguous entries of X's dtype beside it" % d)
-    _check(lib().cmpq_norm_quantize_tokens(_at(X), _code(X), n, d, _rows(X, d, "X"), _at(norm), eps, _at(codes), _code_room(codes),
-                                           _at(scale), _at(nonfinite), _on(X)), "cmpq_norm_quantize_tokens")
+    norm = _norm(norm, d, X)
+    if codes.dtype != torch.int8 or tuple(codes.shape) != (n, d) or codes.device != X.device:
+        raise ValueError("codes needs int8 [%d][%d] beside X, got %s of shape %s on %s" % (n, d, codes.dtype, tuple(codes.shape), codes.device))
+    _check(lib().cmpq_norm_quantize_tokens(_at(X), _code(X), n, d, _rows(X, d, "X"), norm, eps, _at(codes), _code_room(codes),
+                                           _vector(scale, n, torch.float32, X, "scale"), _word(nonfinite, X, "nonfinite"), _on(X)),
+           "cmpq_norm_quantize_tokens")
 
 
 def _residual(residual, n, d_out, X):
-    if residual is None:
-        return None, 0
-    if residual.dtype != X.dtype or tuple(residual.shape) != (n, d_out):
-        raise ValueError("residual needs shape [%d][%d] and X's dtype" % (n, d_out))
-    return _at(residual), _rows(residual, d_out, "residual")
+    return _matrix(residual, n, d_out, X, "residual")
 
 
 def cmpq_linear_i8_fused(X, weight, d_out, y, ws, norm=None, eps=1e-6, act=None, residual=None, nonfinite=None):
     """y = act(the 8-bit linear layer `weight` (a Weight8) of norm(X)) + residual."""
     n, d_in = X.shape
-    _check(lib().cmpq_linear_i8_fused(_at(X), _code(X), n, d_in, _rows(X, d_in, "X"), _at(norm), eps, weight, d_out, ACTS[act],
-                                      *_residual(residual, n, d_out, X), _at(y), _rows(y, d_out, "y"), _at(nonfinite), _at(ws),
-                                      ws.numel(), _on(X)), "cmpq_linear_i8_fused")
+    _check(lib().cmpq_linear_i8_fused(_at(X), _code(X), n, d_in, _rows(X, d_in, "X"), _norm(norm, d_in, X), eps,
+                                      _weight(weight, d_out, d_in, X, "weight"), d_out, _act(act), *_residual(residual, n, d_out, X),
+                                      *_matrix(y, n, d_out, X, "y"), _word(nonfinite, X, "nonfinite"), *_space(ws, X, "ws"), _on(X)),
+           "cmpq_linear_i8_fused")
 
 
 def cmpq_gated_i8_ws_bytes(n, d_in, d_ff, d_out):
@@ -596,9 +659,10 @@ GATED_STATE_BYTES = 256
 def cmpq_gated_i8(X, gate, up, down, d_ff, d_out, y, state, ws, norm=None, eps=1e-6, act="silu", residual=None, word=None):
     """y = the gated block of norm(X), plus residual; gate, up, down: Weight8.  state: GATED_STATE_BYTES bytes that are 0."""
     n, d_in = X.shape
-    _check(lib().cmpq_gated_i8(_at(X), _code(X), n, d_in, _rows(X, d_in, "X"), _at(norm), eps, gate, up, down, d_ff, d_out, ACTS[act],
-                               *_residual(residual, n, d_out, X), _at(y), _rows(y, d_out, "y"), _at(word), _at(state), _at(ws), ws.numel(),
-                               _on(X)), "cmpq_gated_i8")
+    _check(lib().cmpq_gated_i8(_at(X), _code(X), n, d_in, _rows(X, d_in, "X"), _norm(norm, d_in, X), eps, _weight(gate, d_ff, d_in, X, "gate"),
+                               _weight(up, d_ff, d_in, X, "up"), _weight(down, d_out, d_ff, X, "down"), d_ff, d_out, _act(act),
+                               *_residual(residual, n, d_out, X), *_matrix(y, n, d_out, X, "y"), _word(word, X, "word"),
+                               _space(state, X, "state", GATED_STATE_BYTES)[0], *_space(ws, X, "ws"), _on(X)), "cmpq_gated_i8")
 
 
 def cmpq_check_cache(word):

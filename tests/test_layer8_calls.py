@@ -114,3 +114,99 @@ def test_a_failed_query_leaves_no_error_behind():
     failing = body[body.index("cudaOccupancyMaxActiveClusters"):]
     assert re.match(r"[^;]*== cudaSuccess\) return n;\s*cudaGetLastError\(\);", failing), body
     assert re.search(r"cudaGetDevice\(&dev\) != cudaSuccess\) return cudaGetLastError\(\), 0;", body)
+
+
+# ---- the wrappers of the C calls --------------------------------------------------------------------------------
+
+F16, BF16, F32, I8, U8, I32 = torch.float16, torch.bfloat16, torch.float32, torch.int8, torch.uint8, torch.int32
+N, D, FF, O = 3, 32, 48, 16
+ELSEWHERE = "meta"
+
+
+def _new(dtype, *shape, device="cpu"):
+    return torch.zeros(shape, dtype=dtype, device=device)
+
+
+def _halves(dtype, n):
+    """Every second of 2 n entries."""
+    return _new(dtype, 2 * n)[::2]
+
+
+def _matrices(n, d, dtype=F16):
+    return [_new(dtype, n - 1, d), _new(dtype, n + 1, d), _new(dtype, n, d - 1), _new(F32, n, d), _new(BF16, n, d), _new(dtype, n * d), _new(dtype, d, n).t(),
+            _new(dtype, n, d, device=ELSEWHERE)]
+
+
+def _vectors(n, dtype):
+    return [_new(dtype, n - 1), _new(dtype, n + 1), _halves(dtype, n), _new(dtype, n, 1), _new(torch.float64, n), _new(dtype, n, device=ELSEWHERE)]
+
+
+WORDS = [_new(torch.int64, 1), _new(I32, 0), _new(I32, 1, device=ELSEWHERE)]
+
+
+def _refused(call, good, bad):
+    """Every bad argument in the place of its good one; the good ones reach the library, which is not called here."""
+    for name, values in bad.items():
+        for value in values:
+            with pytest.raises((ValueError, TypeError)):
+                call(**{**good, name: value})
+
+
+@pytest.fixture
+def untouched(L, monkeypatch):
+    """The library, where every call of these says that it was made."""
+    made = []
+
+    class Library:
+        def __getattr__(self, name):
+            return lambda *a: made.append(name) or 0
+
+    monkeypatch.setattr(B, "lib", lambda: Library())
+    monkeypatch.setattr(B, "_on", lambda t: 0)
+    return made
+
+
+def test_norm_quantize_wrapper_refuses_what_does_not_fit(untouched):
+    good = dict(X=_new(F16, N, D), norm=_new(F16, D), eps=1e-6, codes=_new(I8, N, D), scale=_new(F32, N), nonfinite=_new(I32, 1))
+    codes = [_new(I8, N - 1, D), _new(I8, N + 1, D), _new(I8, N, D - 16), _new(I8, N, D + 16), _new(U8, N, D), _new(I8, N * D), _new(I8, N, D, device=ELSEWHERE)]
+    _refused(B.cmpq_norm_quantize_tokens, good, dict(norm=_vectors(D, F16) + [_new(BF16, D)], codes=codes, scale=_vectors(N, F32) + [_new(F16, N)], nonfinite=WORDS))
+    assert not untouched
+    B.cmpq_norm_quantize_tokens(**good)
+    assert untouched == ["cmpq_norm_quantize_tokens"]
+
+
+def _weights(d_out, d_in, bias=F16):
+    return B.weight8(_new(I8, d_out, d_in), _new(F32, d_out), None if bias is None else _new(bias, d_out))
+
+
+def test_linear_wrapper_refuses_what_does_not_fit(untouched):
+    good = dict(X=_new(F16, N, D), weight=_weights(O, D), d_out=O, y=_new(F16, N, O), ws=_new(U8, 4096), norm=_new(F16, D), eps=1e-6, act="silu",
+                residual=_new(F16, N, O), nonfinite=_new(I32, 1))
+    _refused(B.cmpq_linear_i8_fused, good, dict(weight=[_weights(O + 1, D), _weights(O - 1, D), _weights(O, D + 16), _weights(O, D, BF16)], d_out=[O + 1, O - 1],
+                                                y=_matrices(N, O), ws=[_new(U8, 4096)[::2], _new(U8, 4096, device=ELSEWHERE)], norm=_vectors(D, F16) + [_new(BF16, D)],
+                                                act=["tanh", "", 2], residual=_matrices(N, O), nonfinite=WORDS, X=[_new(F32, N, D), _new(F16, N, D + 1)]))
+    assert not untouched
+    for more in ({}, dict(norm=None, residual=None, nonfinite=None, act=None, weight=_weights(O, D, None)), dict(y=_new(F16, N, O + 8)[:, :O])):
+        B.cmpq_linear_i8_fused(**{**good, **more})
+    assert len(untouched) == 3
+
+
+def test_gated_wrapper_refuses_what_does_not_fit(untouched):
+    good = dict(X=_new(F16, N, D), gate=_weights(FF, D), up=_weights(FF, D), down=_weights(O, FF), d_ff=FF, d_out=O, y=_new(F16, N, O),
+                state=_new(U8, B.GATED_STATE_BYTES), ws=_new(U8, 4096), norm=_new(F16, D), eps=1e-6, act="gelu", residual=_new(F16, N, O), word=_new(I32, 1))
+    _refused(B.cmpq_gated_i8, good, dict(gate=[_weights(FF - 1, D), _weights(FF, D + 1)], up=[_weights(FF + 1, D)], down=[_weights(O, FF + 16), _weights(O + 1, FF), _weights(O, FF, BF16)],
+                                         d_ff=[FF - 1, FF + 1], d_out=[O + 1], y=_matrices(N, O), ws=[_new(U8, 4096, device=ELSEWHERE)], norm=_vectors(D, F16),
+                                         state=[_new(U8, B.GATED_STATE_BYTES - 1), _new(U8, 0), _new(U8, 256, device=ELSEWHERE), _new(I32, 128)[::2]],
+                                         act=["swish"], residual=_matrices(N, O), word=WORDS, X=[_new(F16, N, D + 1), _new(torch.int8, N, D)]))
+    assert not untouched
+    for more in ({}, dict(state=_new(I32, 64)), dict(norm=None, residual=None, word=None)):
+        B.cmpq_gated_i8(**{**good, **more})
+    assert len(untouched) == 3
+
+
+def test_weights_refuse_what_does_not_fit_and_keep_their_tensors():
+    good = dict(codes=_new(I8, O, D), scale=_new(F32, O), bias=_new(F16, O))
+    _refused(B.weight8, good, dict(codes=[_new(U8, O, D), _new(I8, D, O).t(), _new(I8, O * D), _new(I8, O + 1, D), _new(I8, O, D, device=ELSEWHERE)],
+                                   scale=_vectors(O, F32), bias=[_new(F16, O - 1), _halves(F16, O), _new(F16, O, device=ELSEWHERE)]))
+    w = B.weight8(*(t.clone() for t in good.values()))
+    assert (w.codes, w.ld, w.scale, w.bias) == (w.tensors[0].data_ptr(), D, w.tensors[1].data_ptr(), w.tensors[2].data_ptr())
