@@ -466,28 +466,6 @@ matmul_i8_pair_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_con
     if (warp == 1) tc5::tmem_free<2>(tmem, 512);
 }
 
-// Cycles that a way to cover the product takes, from sizes: rounds of blocks over the SMs, in each the blocks of the sum
-// at the pace of the products or of the loads (64 bytes a cycle and SM), and what a round or launch costs besides; not
-// less than the weights' way from memory (3400 bytes a cycle).  Fitted to sweeps of bn over 1 to 512 tokens and layers of
-// 4096 x 4096 to 8192 x 28672, where the choice is within 3 % of the best; e.g. 256 x 4096 x 11008: bn = 160 17.4 us, 176 17.7,
-// pairs of 160 17.2; 512 tokens: pairs of 160 24.3, 192 25.7, 256 29.9.
-static int64_t tile_cycles(const ProductArgs& a, int bn) {
-    const int64_t blocks = (int64_t)((a.n + 127) / 128) * ((a.cols + bn - 1) / bn), sms = sm_count();
-    const int64_t rounds = (blocks + sms - 1) / sms, pace = std::max(4 * std::max(32, bn / 2), (bn + std::min(a.n, 128)) * 2);
-    return std::max<int64_t>(rounds * a.kblocks * pace, (int64_t)a.kblocks * 128 * a.cols / 3400) + rounds * (9000 + 8 * bn);
-}
-static int64_t pair_cycles(const ProductArgs& a, int bn) {
-    const int64_t tiles = (int64_t)((a.n + 255) / 256) * ((a.cols + bn - 1) / bn), pairs = sm_count() / 2;
-    return (tiles + pairs - 1) / pairs * a.kblocks * (600 * (256 + bn) / 512) + 14000;  // the pace is that of the loads
-}
-
-// Slices of a tile's sum, for products that no cluster shares.  Shorter sums are not worth the adding up, and wider tiles wait for
-// memory: 32 tokens 2048 -> 2048 6.0 -> 6.6 us with four slices, 53 tokens 4096 -> 4096 9.2 -> 9.5 and 28672 -> 8192 45.8 -> 46.9
-// with two.
-static int slices_of(const ProductArgs& a, int rows, int bn) {
-    return bn > 32 ? 1 : rows <= 32 && a.kblocks > 16 ? 4 : rows <= 64 && a.kblocks > 32 ? 2 : 1;
-}
-
 // Clusters of `parts` CTAs, each on an SM of its own, that run at once: fewer than the SMs would allow (33 of four on 148 SMs), as
 // a cluster keeps to one group of SMs.  Asked once per device; 0, and no error left behind, where that fails.
 static int cluster_slots(int parts) {
@@ -510,47 +488,18 @@ static int cluster_slots(int parts) {
     });
 }
 
-// The same with `parts` CTAs of a cluster to a tile, or one, to compare the two.  Here the loads' way from L2 and the weights' from
-// memory delay one another, and a cluster pays 3300 cycles for its two barriers and for sums that cross it.  Fitted to 600 calls
-// of 5 to 512 tokens, 2304 x 512 to 28672 x 12288: what it chooses is 1 % slower than the best of them in the mean (14 % at most)
-// and takes 0.90 of the time without clusters (0.45 to 1.05).
-static int64_t parts_cycles(const ProductArgs& a, int parts, int bn, int slots) {
-    const int64_t rounds = ceil_div(ceil_div(a.n, 128) * ceil_div(a.cols, bn), slots);
-    const int rows = std::min(128, (a.n + 7) / 8 * 8), slices = parts > 1 ? 1 : slices_of(a, rows, bn);
-    const int64_t loads = rounds * ((a.kblocks + parts - 1) / parts) * std::max(2 * std::max(64, bn) / slices, (bn + rows) * 2);
-    const int64_t memory = (int64_t)a.kblocks * 128 * a.cols / 3400;
-    return std::max(loads, memory) + std::min(loads, memory) * 2 / 5 + rounds * (10000 + 7 * bn) + (slices > 1 ? 2000 : 0) +
-           (parts > 1 ? 3300 + rows * (bn - bn / parts) * 2 / 5 : 0);
-}
-
 template <int DT, int KIND>
 static cmpq_status launch_kind(const TokenCodes& x, int64_t d_in, const Weight8& w, const Weight8* u, ProductArgs a, bool behind, cudaStream_t st) {
-    if (sm_count() <= 0) return CMPQ_ERR_CUDA;  // no device to plan for
+    const int sms = sm_count();
+    if (sms <= 0) return CMPQ_ERR_CUDA;  // no device to plan for
     a.kblocks = (int)((d_in + 127) / 128);
     a.wide = aligned_to(a.y, 16) && a.ldy % 8 == 0;
     a.wide_residual = aligned_to(a.residual, 16) && a.ldr % 8 == 0;
     a.cols = (KIND == kGated ? 2 : 1) * (int64_t)a.d_out;
-    a.bn = 32;
-    for (int bn = 48; bn <= 256; bn += 16)
-        if (tile_cycles(a, bn) < tile_cycles(a, a.bn)) a.bn = bn;
-    int wide = 256;  // narrower where that fills the last round better
-    for (int bn = 224; bn >= 128; bn -= 32)
-        if (pair_cycles(a, bn) < pair_cycles(a, wide)) wide = bn;
-    bool pair = a.n > 128 && pair_cycles(a, wide) < tile_cycles(a, a.bn);
-    if (pair) a.bn = wide;
-    // A few wide tiles with long sums: two or four CTAs to a tile.  A CTA finishes whole groups of eight channels.
-    int parts = 1;
-    if (a.kblocks > 16) {
-        int64_t least = pair ? (pair_cycles(a, wide) - 14000) * 14 / 10 + 14200 : parts_cycles(a, 1, a.bn, sm_count());  // pairs by the same fit
-        for (int c = 2; c <= 4; c *= 2) {
-            const int slots = cluster_slots(c);
-            for (int bn = 16 * c; slots > 0 && bn <= 256; bn += 16 * c) {
-                const int64_t cycles = parts_cycles(a, c, bn, slots);
-                if (cycles < least) least = cycles, a.bn = bn, parts = c, pair = false;
-            }
-        }
-    }
-    a.rows = pair ? 128 : std::min(128, (a.n + 7) / 8 * 8);
+    const ProductPlan plan = plan_product({a.n, a.cols, a.kblocks, sms}, cluster_slots);
+    const bool pair = plan.pair;
+    const int parts = plan.parts;
+    a.bn = plan.bn, a.rows = plan.rows;
     CUtensorMap wmap, umap, xmap;
     const int box = pair || KIND == kGated ? a.bn / 2 : a.bn, channels = KIND == kGated ? a.bn / 2 : a.bn;
     if (!make_byte_map(&wmap, w.codes, a.d_out, d_in, w.ld, box) || !make_byte_map(&xmap, x.codes, a.n, d_in, x.ld, a.rows)) return CMPQ_ERR_CUDA;
@@ -562,18 +511,16 @@ static cmpq_status launch_kind(const TokenCodes& x, int64_t d_in, const Weight8&
         a.m_tiles = (a.n + 255) / 256;
         if (!raise_smem_limit_once(matmul_i8_pair_kernel<DT, KIND>, kPairSmem, raised[0])) return CMPQ_ERR_CUDA;
         const int64_t tiles = (int64_t)a.m_tiles * a.n_tiles;
-        return launch_cluster(matmul_i8_pair_kernel<DT, KIND>, 2 * (unsigned)std::min<int64_t>(tiles, sm_count() / 2), kMmThreads, kPairSmem, 2, behind,
+        return launch_cluster(matmul_i8_pair_kernel<DT, KIND>, 2 * (unsigned)std::min<int64_t>(tiles, sms / 2), kMmThreads, kPairSmem, 2, behind,
                               st, wmap, umap, xmap, a);
     }
     a.m_tiles = (a.n + 127) / 128;
     // one block to an SM: two that share it were slower at every size, their rounds and tails cost more than they hide
     const int64_t blocks = (int64_t)a.m_tiles * a.n_tiles;
-    a.slices = parts > 1 ? parts : slices_of(a, a.rows, a.bn);
+    a.slices = parts > 1 ? parts : plan.slices;
     a.kblocks = (a.kblocks + a.slices - 1) / a.slices;
-    const int slices = parts > 1 ? 1 : a.slices, block = slices * (a.rows + a.bn) * 128;
-    // wide tiles of clusters have more rows of weights on the way at once: 100 tokens 28672 -> 8192 47.9 -> 46.9 us with 48 KB, but
-    // 20480 -> 5120, in tiles of 96 channels, 26.8 -> 29.2
-    a.per_stage = std::max(1, std::min((a.n > 32 && (parts == 1 || a.bn < 128) ? 64 << 10 : 48 << 10) / block, a.kblocks));
+    a.per_stage = plan.per_stage;
+    const int slices = plan.slices, block = slices * (a.rows + a.bn) * 128;
     const size_t stage = a.per_stage * block, slack = (128 - slices * a.rows) * 128 + 1024;
     a.stages = std::min({(int)((kTileSmem - slack) / stage), kMmMaxStages, (a.kblocks + a.per_stage - 1) / a.per_stage});
     if (blocks * parts > INT32_MAX) return CMPQ_ERR_UNSUPPORTED;

@@ -6,6 +6,7 @@
 
 #include "cache.cuh"
 #include "epilogue.cuh"
+#include "plan_i8.h"
 #include "tc5.cuh"
 
 namespace cmpq {
@@ -13,8 +14,6 @@ namespace cmpq {
 // What a product does with its sums: scale and bias; activation and residual too; or two projections at once, of which the
 // first, activated, multiplies the second.
 enum { kPlain = 0, kFinish = 1, kGated = 2 };
-
-inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 using Weight8 = cmpq_weight_i8;
 struct TokenCodes {

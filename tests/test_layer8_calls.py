@@ -210,3 +210,73 @@ def test_weights_refuse_what_does_not_fit_and_keep_their_tensors():
                                    scale=_vectors(O, F32), bias=[_new(F16, O - 1), _halves(F16, O), _new(F16, O, device=ELSEWHERE)]))
     w = B.weight8(*(t.clone() for t in good.values()))
     assert (w.codes, w.ld, w.scale, w.bias) == (w.tensors[0].data_ptr(), D, w.tensors[1].data_ptr(), w.tensors[2].data_ptr())
+
+
+# ---- how products are covered -------------------------------------------------------------------------------------
+
+PLAN = r"""
+#include <cstdio>
+#include "plan_i8.h"
+
+int main() {
+    long long n, d_in, cols, sms, two, four;
+    while (scanf("%lld %lld %lld %lld %lld %lld", &n, &d_in, &cols, &sms, &two, &four) == 6) {
+        const auto a = cmpq::plan_product({n, cols, cmpq::ceil_div(d_in, 128), sms}, [&](int parts) { return (int)(parts == 2 ? two : four); });
+        printf("%d %d %d %d %d %d\n", a.pair, a.bn, a.rows, a.parts, a.slices, a.per_stage);
+    }
+}
+"""
+
+
+@pytest.fixture(scope="module")
+def plan(tmp_path_factory):
+    """plan([(tokens, entries of the sum, rows of weights, SMs, clusters of two, of four at once) ..]) -> [dict ..]"""
+    at = tmp_path_factory.mktemp("plan")
+    (at / "plan.cpp").write_text(PLAN)
+    subprocess.run(["g++", "-std=c++17", "-O2", "-I", cuda_build.CSRC, str(at / "plan.cpp"), "-o", str(at / "plan")], check=True)
+
+    def run(sizes):
+        out = subprocess.run([str(at / "plan")], input="".join("%d %d %d %d %d %d\n" % s for s in sizes), capture_output=True, text=True, timeout=300).stdout
+        plans = [dict(zip(("pair", "bn", "rows", "parts", "slices", "per_stage"), map(int, line.split()))) for line in out.splitlines()]
+        assert len(plans) == len(sizes)
+        return plans
+
+    return run
+
+
+B200 = (148, 74, 33)  # SMs; clusters of two and of four blocks that run at once
+SUMS = [64, 512, 1000, 2049, 4096, 5461, 8192, 11008, 13824, 14336, 18944, 28672, 131072]
+CHANNELS = [1, 33, 512, 1024, 2049, 3584, 4096, 5120, 8192, 11008, 22016, 28672, 57344]
+TOKENS = [1, 5, 8, 9, 31, 32, 33, 64, 65, 100, 128, 129, 192, 256, 257, 400, 512, 513, 576, 640, 768, 900, 1024, 1152, 1280, 1408, 1600, 1792, 2048, 2560, 3000, 3328, 4000, 4200,
+          4400, 10000, 1 << 20]
+
+
+def test_clusters_do_not_take_the_place_of_pairs_past_their_fit(plan):
+    sizes = [(n, d, o) for n in TOKENS for d in SUMS for o in CHANNELS]
+    with_clusters, without = plan([s + B200 for s in sizes]), plan([s + (148, 0, 0) for s in sizes])
+    taken = [s for s, a, b in zip(sizes, with_clusters, without) if a["parts"] > 1 and b["pair"]]
+    assert taken and max(n for n, *_ in taken) <= 512, [s for s in taken if s[0] > 512][:10]
+    assert all(a == b for s, a, b in zip(sizes, with_clusters, without) if a["parts"] == 1)
+    # what clusters are for: a few wide tiles with long sums
+    assert all(p["parts"] > 1 for p in plan([(128, 28672, 1024) + B200, (100, 11008, 4096) + B200, (256, 28672, 8192) + B200]))
+
+
+def test_plans_fit_the_kernels(plan):
+    """Shared memory, rows of an instruction, and whole groups of channels, over all sizes and on devices with few SMs."""
+    smem, most_stages = 208 << 10, 40
+    sizes = [(n, d, o) + device for device in (B200, (148, 0, 0), (20, 10, 4), (2, 1, 0)) for n in TOKENS for d in SUMS for o in CHANNELS]
+    for s, p in zip(sizes, plan(sizes)):
+        n, d, _ = s[:3]
+        rows, bn, parts, slices = p["rows"], p["bn"], p["parts"], p["slices"]
+        assert bn % 16 == 0 and 32 <= bn <= 256 and rows % 8 == 0 and 1 <= rows <= 128, (s, p)
+        if p["pair"]:
+            assert n > 128 and rows == 128 and parts == slices == 1 and bn >= 128 and bn % 32 == 0, (s, p)
+            continue
+        assert rows == min(128, -(-n // 8) * 8) and parts in (1, 2, 4) and slices in (1, 2, 4) and min(parts, slices) == 1, (s, p)
+        assert bn % (16 * parts) == 0 and slices * rows <= 128 and slices * bn <= 256 and (slices == 1 or n <= 64), (s, p)
+        block = slices * (rows + bn) * 128
+        slack = (128 - slices * rows) * 128 + 1024
+        assert 1 <= p["per_stage"] <= -(-(-(-d // 128)) // (parts * slices)), (s, p)
+        stages = min((smem - slack) // (p["per_stage"] * block), most_stages)
+        assert stages >= 1 and stages * p["per_stage"] * block + slack <= smem, (s, p)
+        assert (parts - 1) * 128 * (bn // parts + 4) * 4 + 1024 <= smem, (s, p)
