@@ -150,12 +150,14 @@ class AttentionLayer8:
 
     def __call__(self, x, tok_off, lens, table, max_new, max_len=None, window=0, *, residual=None, norm=None, eps=1e-6):
         """x: fp16/bf16 [n_tok][d_model], the new tokens of a batch (see PagedCache8).  Returns [n_tok][out.d_out]; norm and eps
-        as for the projection of x, residual as for the output's (see Int8Linear)."""
+        as for the projection of x, residual as for the output's (see Int8Linear).  Rows behind the last sequence have an attention
+        of 0; x has to be finite there too."""
         h, kv, d = self.n_heads, self.cache.n_kv, self.cache.head_dim
         y = self.qkv(x, norm=norm, eps=eps)
         q, k, v = (y[:, a * d: b * d].unflatten(1, (b - a, d)) for a, b in ((0, h), (h, h + kv), (h + kv, h + 2 * kv)))
         self.cache.append(k, v, tok_off, lens, table, q=q, cos=self.cos, sin=self.sin, interleaved=self.interleaved, q_out=q)
-        a = self.cache.attend(q, tok_off, lens, table, max_new, max_len, window=window)
+        # rows behind the last sequence are left alone by the attention, and the projection behind it takes all rows
+        a = self.cache.attend(q, tok_off, lens, table, max_new, max_len, window=window, out=y.new_zeros(y.shape[0], h, d))
         return self.out(a.flatten(1), residual=residual)
 
     def check(self):
@@ -177,7 +179,8 @@ class DecoderLayer8:
         self.attention_norm, self.mlp_norm, self.eps = attention_norm, mlp_norm, eps
 
     def __call__(self, x, tok_off, lens, table, max_new, max_len=None, window=0):
-        """x: fp16/bf16 [n_tok][d_model], the new tokens of a batch (see PagedCache8).  Returns the same shape."""
+        """x: fp16/bf16 [n_tok][d_model], the new tokens of a batch (see PagedCache8).  Returns the same shape; rows behind the last
+        sequence as in AttentionLayer8."""
         a = self.attention(x, tok_off, lens, table, max_new, max_len, window, residual=x, norm=self.attention_norm, eps=self.eps)
         return self.mlp(a, out=a, residual=a, norm=self.mlp_norm, eps=self.eps)
 
