@@ -485,8 +485,10 @@ cmpq_status cmpq_linear_i8_fused(const void* X, cmpq_dtype dt, int64_t n, int64_
  * state: CMPQ_GATED_STATE_BYTES bytes, 16-byte aligned, in which the blocks of a kernel meet.  They have to be 0 when the call's
  * kernels start, and are 0 again when they have ended: zero them once, when they are allocated, and after bit 3, which calls
  * with this state may report from then on.  Calls that may run at the same time, graphs' replays among them, need states and work
- * spaces of their own.  Up to four tokens of a large block go through one cooperative launch with a block on every SM.  ws: cmpq_gated_i8_ws_bytes(n, d_in, d_ff, d_out), 0 for arguments out of range. */
+ * spaces of their own.  Up to CMPQ_GATED_FEW_TOKENS tokens of a large block go through one cooperative launch with a block on every
+ * SM; calls of more tokens keep no more in the state than bit 3, and that only where word is NULL.  ws: cmpq_gated_i8_ws_bytes(n, d_in, d_ff, d_out), 0 for arguments out of range. */
 #define CMPQ_GATED_STATE_BYTES 256
+#define CMPQ_GATED_FEW_TOKENS 4
 size_t cmpq_gated_i8_ws_bytes(int64_t n, int64_t d_in, int64_t d_ff, int64_t d_out);
 cmpq_status cmpq_gated_i8(const void* X, cmpq_dtype dt, int64_t n, int64_t d_in, int64_t ldx, const void* norm, float eps,
                           const cmpq_weight_i8* gate, const cmpq_weight_i8* up, const cmpq_weight_i8* down, int64_t d_ff,

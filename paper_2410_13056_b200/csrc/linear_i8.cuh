@@ -37,7 +37,7 @@ cmpq_status enqueue_quantize(const void* X, cmpq_dtype dt, int64_t n, int64_t d,
 
 // Both in one launch, for up to kFewTokens tokens whose rows few_fits; word (may be null): where a NaN or an infinity is
 // reported.  behind: it may start while the kernel in front of it, which was launched without this, writes X.
-constexpr int kFewTokens = 4, kFewBlocks = 100;  // blocks of 128 entries whose codes a block of the kernel holds
+constexpr int kFewTokens = CMPQ_GATED_FEW_TOKENS, kFewBlocks = 100;  // blocks of 128 entries whose codes a block of the kernel holds
 bool few_fits(int64_t d_in);
 cmpq_status enqueue_few(const void* X, cmpq_dtype dt, int64_t n, int64_t d_in, int64_t ldx, const void* norm, float eps, const Weight8& w, int64_t d_out,
                         const Weight8* u, const Finish& f, void* y, int64_t ldy, int32_t* word, int32_t* gave_up, bool behind, cudaStream_t st);

@@ -197,10 +197,11 @@ struct Gated {
     Linear gate, up, down;
     cmpq_act act;
     Tensor word;
-    // States for captured calls, one each, 0 from here on: a node that zeroed it would cost every replay 2 us.  They live as
-    // long as the weights have to; calls beyond them take theirs from the graph, with such a node.
+    // States for captured calls of few tokens, one each, 0 from here on: a node that zeroed it would cost every replay 2 us.  They
+    // live as long as the weights have to; calls beyond them take theirs from the graph, with such a node.  One more is for
+    // calls of more tokens, which have a word and so leave their state alone.
     static constexpr int64_t kCaptured = 64;
-    Tensor kept;
+    Tensor kept, untouched;
     int64_t taken = 0;
 
     Gated(const Linear& g, const Linear& u, const Linear& d, const std::optional<std::string>& activation) : gate(g), up(u), down(d), act(act_of(activation)) {
@@ -209,10 +210,12 @@ struct Gated {
             refuse("gate [" + std::to_string(g.d_out) + "][" + std::to_string(g.d_in) + "], up [" + std::to_string(u.d_out) + "][" + std::to_string(u.d_in) +
                    "] and down [" + std::to_string(d.d_out) + "][" + std::to_string(d.d_in) + "] do not fit together");
         word = at::zeros({1}, at::TensorOptions().dtype(at::kInt).device(g.w.device()));
-        kept = at::zeros({kCaptured, CMPQ_GATED_STATE_BYTES}, at::TensorOptions().dtype(at::kByte).device(g.w.device()));
+        kept = at::zeros({kCaptured + 1, CMPQ_GATED_STATE_BYTES}, at::TensorOptions().dtype(at::kByte).device(g.w.device()));
+        untouched = kept[kCaptured];
     }
 
-    Tensor state(void* stream) {
+    Tensor state(int64_t n, void* stream) {
+        if (n > CMPQ_GATED_FEW_TOKENS) return untouched;
         return capturing() && taken < kCaptured ? kept[taken++] : gated_states().get(word.device(), stream, CMPQ_GATED_STATE_BYTES);
     }
 
@@ -224,7 +227,7 @@ struct Gated {
         if (a.n == 0) return y;
         void* stream = stream_of(x);
         const Tensor ws = gated_spaces().get(x.device(), stream, cmpq_gated_i8_ws_bytes(a.n, gate.d_in, gate.d_out, down.d_out));
-        const Tensor st = state(stream);
+        const Tensor st = state(a.n, stream);
         const cmpq_weight_i8 g = gate.weight(), u = up.weight(), d = down.weight();
         check(cmpq_gated_i8(x.data_ptr(), a.dt, a.n, gate.d_in, rows(x, "x"), a.norm, (float)eps, &g, &u, &d, gate.d_out, down.d_out, act, a.residual, a.ldr,
                             y.data_ptr(), rows(y, "out"), word.data_ptr<int32_t>(), st.data_ptr(), ws.data_ptr(), ws.numel(), stream),
@@ -379,7 +382,8 @@ PYBIND11_MODULE(_serving, m) {
         .def("__call__", &Gated::call, py::arg("x"), py::arg("out") = py::none(), py::arg("residual") = py::none(), py::arg("norm") = py::none(),
              py::arg("eps") = 1e-6)
         .def("check", &Gated::look)
-        .def_readonly("word", &Gated::word);
+        .def_readonly("word", &Gated::word)
+        .def_readonly("captured_states", &Gated::taken);
     py::class_<Cache>(m, "Cache")
         .def(py::init<const Tensor&, const Tensor&, const Tensor&, const Tensor&>())
         .def("append", &Cache::append, py::arg("k"), py::arg("v"), py::arg("tok_off"), py::arg("lens"), py::arg("table"), py::arg("q") = py::none(),

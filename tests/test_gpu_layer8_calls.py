@@ -130,3 +130,24 @@ def test_decoder_layer_in_graphs(dtype):
     layer.check(), eager.check()
     a, b = layer.attention.cache, eager.attention.cache
     assert torch.equal(a.k_codes, b.k_codes) and torch.equal(a.v_codes, b.v_codes)
+
+
+def test_captured_calls_take_a_state_only_where_blocks_meet_in_it():
+    """A program that captures a graph for every batch size has its states left for the calls that need them."""
+    d, ff, dtype = 1024, 6000, torch.bfloat16
+    block, x, g = base._block(1, d, ff, d, dtype, "silu", False), base._tokens(300, d, dtype, 1), base._norm(d, dtype, 2)
+    sizes = [5, 6, 8, 33, 64, 100, 128, 129, 200, 300] * 8 + [1, 2, 3, 4]
+    want = {n: block(x[:n], residual=x[:n], norm=g) for n in set(sizes)}
+    assert block._impl.captured_states == 0
+    graph, out = torch.cuda.CUDAGraph(), []
+    with torch.cuda.graph(graph):
+        for n in sizes:
+            out.append(block(x[:n], residual=x[:n], norm=g))
+    assert block._impl.captured_states == 4
+    for _ in range(3):
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(y, want[n]) for n, y in zip(sizes, out))
+        for y in out:
+            y.zero_()
+    block.check()
