@@ -136,8 +136,11 @@ constexpr size_t kTileSmem = 208 << 10;
 // reads the tokens fewer times than as many narrow tiles.  Each CTA then takes a part of the tile's channels and adds up what the
 // others send it of those.  128 tokens 28672 -> 1024: 40 us whole, 18 over four; 11008 -> 4096 19.4 and 16.9 over
 // two; 256 tokens 11008 -> 2048 19.0 and 15.7.
+//
+// ONE: a stage is one block of the sum.  The loops over the blocks are the time of an issuing thread, so they are written out without
+// those of a stage (4096 -> 4096, 320 tokens 12.6 us with both, 11.4 so).
 enum { kWhole, kSliced, kSplit };
-template <int DT, int KIND, int SUM>
+template <int DT, int KIND, int SUM, bool ONE>
 __global__ void __launch_bounds__(kMmThreads, 1)
 matmul_i8_tile_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__ CUtensorMap umap, const __grid_constant__ CUtensorMap xmap,
                       const __grid_constant__ ProductArgs A) {
@@ -151,7 +154,7 @@ matmul_i8_tile_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_con
     const int parts = SUM == kSplit ? A.slices : 1, part = SUM == kSplit ? (int)tc5::cluster_rank() : 0, k0 = part * A.kblocks;
     const int nt = blockIdx.x / parts / A.m_tiles, mt = blockIdx.x / parts % A.m_tiles, bn = A.bn;
     const int S = SUM == kSliced ? A.slices : 1, N = S * bn, columns = N <= 32 ? 32 : N <= 64 ? 64 : N <= 128 ? 128 : 256;
-    const int row_box = A.rows * 128, box = bn * 128, a_bytes = S * row_box, b_bytes = S * box, stage = A.per_stage * (a_bytes + b_bytes);  // of a slice, of all
+    const int row_box = A.rows * 128, box = bn * 128, a_bytes = S * row_box, b_bytes = S * box, stage = (ONE ? 1 : A.per_stage) * (a_bytes + b_bytes);  // of a slice, of all
     if (threadIdx.x < A.stages) tc5::mbar_init(full + threadIdx.x, 1), tc5::mbar_init(empty + threadIdx.x, 1);
     if (threadIdx.x == 0) tc5::mbar_init(&done, 1), failed = 0;
     tc5::mbar_init_fence();
@@ -163,7 +166,19 @@ matmul_i8_tile_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_con
     if (warp == 0) {
         if (tc5::elect_one()) {
             int slot = 0, phase = 1;  // a new barrier counts as empty
-            for (int k = 0; k < A.kblocks; k += A.per_stage) {
+            for (int i = 0; ONE && i < A.kblocks; ++i) {
+                if (!tc5::mbar_wait(empty + slot, phase, &failed)) break;
+                tc5::mbar_expect_tx(full + slot, stage);  // the tokens' bytes too, whoever comes first
+                uint8_t* at = smem + slot * stage + a_bytes;
+                if (KIND == kGated) {
+                    tc5::tma_load_2d(at, &wmap, full + slot, (k0 + i) * 128, nt * (bn / 2));
+                    tc5::tma_load_2d(at + box / 2, &umap, full + slot, (k0 + i) * 128, nt * (bn / 2));
+                } else {
+                    tc5::tma_load_2d(at, &wmap, full + slot, (k0 + i) * 128, nt * bn);
+                }
+                if (++slot == A.stages) slot = 0, phase ^= 1;
+            }
+            for (int k = 0; !ONE && k < A.kblocks; k += A.per_stage) {
                 if (!tc5::mbar_wait(empty + slot, phase, &failed)) break;
                 const int count = min(A.per_stage, A.kblocks - k);
                 tc5::mbar_expect_tx(full + slot, count * (a_bytes + b_bytes));  // the tokens' bytes too, whoever comes first
@@ -183,7 +198,17 @@ matmul_i8_tile_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_con
         if (tc5::elect_one()) {
             const uint32_t idesc = tc5::idesc_i8(128, N);
             int slot = 0, phase = 0;
-            for (int k = 0; k < A.kblocks; k += A.per_stage) {
+            for (int i = 0; ONE && i < A.kblocks; ++i) {
+                if (!tc5::mbar_wait(full + slot, phase, &failed)) break;
+                tc5::fence_after_sync();
+                const uint32_t at = tc5::smem_addr(smem + slot * stage);
+                const uint64_t a = tc5::desc_k_sw128(at), b = tc5::desc_k_sw128(at + a_bytes);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) tc5::mma_i8<1>(tmem, a + 2 * j, b + 2 * j, idesc, (i | j) != 0);
+                tc5::mma_commit(empty + slot);
+                if (++slot == A.stages) slot = 0, phase ^= 1;
+            }
+            for (int k = 0; !ONE && k < A.kblocks; k += A.per_stage) {
                 if (!tc5::mbar_wait(full + slot, phase, &failed)) break;
                 tc5::fence_after_sync();
                 const uint32_t at = tc5::smem_addr(smem + slot * stage);
@@ -206,7 +231,12 @@ matmul_i8_tile_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_con
         if (warp == 2) {  // the token codes: the first epilogue warp's work until then
             if (tc5::elect_one()) {
                 int slot = 0, phase = 1;
-                for (int k = 0; k < A.kblocks; k += A.per_stage) {
+                for (int i = 0; ONE && i < A.kblocks; ++i) {
+                    if (!tc5::mbar_wait(empty + slot, phase, &failed)) break;
+                    tc5::tma_load_2d(smem + slot * stage, &xmap, full + slot, (k0 + i) * 128, mt * 128);
+                    if (++slot == A.stages) slot = 0, phase ^= 1;
+                }
+                for (int k = 0; !ONE && k < A.kblocks; k += A.per_stage) {
                     if (!tc5::mbar_wait(empty + slot, phase, &failed)) break;
                     for (int i = 0; i < min(A.per_stage, A.kblocks - k) * S; ++i)
                         tc5::tma_load_2d(smem + slot * stage + i * row_box, &xmap, full + slot, (k0 + k * S + i) * 128, mt * 128);
@@ -474,7 +504,7 @@ static int cluster_slots(int parts) {
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess) return cudaGetLastError(), 0;
     return asked[parts == 4].get(dev, [parts] {
-        const auto kernel = matmul_i8_tile_kernel<CMPQ_BF16, kPlain, kSplit>;
+        const auto kernel = matmul_i8_tile_kernel<CMPQ_BF16, kPlain, kSplit, false>;
         cudaLaunchAttribute attr;
         attr.id = cudaLaunchAttributeClusterDimension;
         attr.val.clusterDim.x = parts, attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
@@ -506,7 +536,7 @@ static cmpq_status launch_kind(const TokenCodes& x, int64_t d_in, const Weight8&
     umap = wmap;
     if (u && !make_byte_map(&umap, u->codes, a.d_out, d_in, u->ld, box)) return CMPQ_ERR_CUDA;
     a.n_tiles = (a.d_out + channels - 1) / channels;
-    static bool raised[4][64];
+    static bool raised[6][64];
     if (pair) {
         a.m_tiles = (a.n + 255) / 256;
         if (!raise_smem_limit_once(matmul_i8_pair_kernel<DT, KIND>, kPairSmem, raised[0])) return CMPQ_ERR_CUDA;
@@ -529,8 +559,10 @@ static cmpq_status launch_kind(const TokenCodes& x, int64_t d_in, const Weight8&
         if (!raise_smem_limit_once(kernel, kTileSmem, done)) return CMPQ_ERR_CUDA;
         return launch_cluster(kernel, (unsigned)blocks * parts, kMmThreads, std::max(a.stages * stage + slack, exchange), parts, behind, st, wmap, umap, xmap, a);
     };
-    if (parts > 1) return launch(matmul_i8_tile_kernel<DT, KIND, kSplit>, raised[3]);
-    return a.slices > 1 ? launch(matmul_i8_tile_kernel<DT, KIND, kSliced>, raised[1]) : launch(matmul_i8_tile_kernel<DT, KIND, kWhole>, raised[2]);
+    const bool one = a.per_stage == 1;
+    if (parts > 1) return one ? launch(matmul_i8_tile_kernel<DT, KIND, kSplit, true>, raised[5]) : launch(matmul_i8_tile_kernel<DT, KIND, kSplit, false>, raised[3]);
+    if (a.slices > 1) return launch(matmul_i8_tile_kernel<DT, KIND, kSliced, false>, raised[1]);
+    return one ? launch(matmul_i8_tile_kernel<DT, KIND, kWhole, true>, raised[4]) : launch(matmul_i8_tile_kernel<DT, KIND, kWhole, false>, raised[2]);
 }
 
 template <int DT>

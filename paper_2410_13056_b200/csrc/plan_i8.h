@@ -58,6 +58,13 @@ inline int64_t parts_cycles(const ProductSize& p, int parts, int bn, int slots) 
            (parts > 1 ? 3300 + rows * (bn - bn / parts) * 2 / 5 : 0);
 }
 
+// Whether a stage of a tile holds one block of the sum.  Stages of several are for long sums in narrow tiles, whose weights memory
+// brings faster the more of a row is asked for at a time (5 tokens 13824 -> 5120, 48 channels to a tile: 22.8 us with one block, 18.8
+// with 64 KB; 28672 -> 8192, 64 channels 48.3 and 42.5); else the first products wait for more bytes than they need, and stages are few
+// (4096 -> 4096, 320 tokens, 96 channels 11.3 and 12.6; 8192 -> 8192, 80 tokens, 64 channels 16.7 and 18.5; 11008 -> 4096, 512 tokens,
+// 112 channels 25.6 and 28.7).  From 302 calls of 5 to 2048 tokens in tiles, 512 -> 1408 to 28672 -> 8192.
+inline bool stage_of_one(const ProductSize& p, int bn) { return (bn - 16) * (bn - 16) > 32 * p.kblocks; }
+
 // Tokens up to which clusters take the place of pairs.  Past the calls of the fit they do not pay: where the model would choose them for
 // 513 to 4400 tokens, 11008 -> 4096 to 28672 -> 8192, they took 0.98 to 1.39 times as long as pairs (1.19 in the mean of 50 calls), in
 // long streams 1.04 to 1.31 (1.17 of 68; 28672 -> 8192, 4200 tokens 923 us and 727; 11008 -> 4096, 1408 tokens 80 and 59).  A CTA of a split
@@ -80,6 +87,8 @@ inline ProductPlan plan_product(const ProductSize& p, Slots slots) {
     a.parts = 1;
     if (p.kblocks > 16 && (!a.pair || p.n <= kClusterTokens)) {
         int64_t least = a.pair ? (pair - 14000) * 14 / 10 + 14200 : parts_cycles(p, 1, a.bn, (int)p.sms);  // pairs by the same fit
+        // which had stages of several blocks everywhere: without this, clusters were up to 6 % slower (11008 -> 4096, 384 tokens)
+        if (!a.pair && slices_of(p, a.bn) == 1 && stage_of_one(p, a.bn)) least = least * 14 / 15;
         for (int c = 2; c <= 4; c *= 2) {
             const int at_once = slots(c);
             for (int bn = 16 * c; at_once > 0 && bn <= 256; bn += 16 * c)
@@ -92,6 +101,7 @@ inline ProductPlan plan_product(const ProductSize& p, Slots slots) {
     // 20480 -> 5120, in tiles of 96 channels, 26.8 -> 29.2
     const int block = a.slices * (a.rows + a.bn) * 128, stage = p.n > 32 && (a.parts == 1 || a.bn < 128) ? 64 << 10 : 48 << 10;
     a.per_stage = (int)std::max<int64_t>(1, std::min<int64_t>(stage / block, ceil_div(p.kblocks, a.parts * a.slices)));
+    if (a.parts == 1 && a.slices == 1 && stage_of_one(p, a.bn)) a.per_stage = 1;
     return a;
 }
 

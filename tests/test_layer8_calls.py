@@ -280,3 +280,17 @@ def test_plans_fit_the_kernels(plan):
         stages = min((smem - slack) // (p["per_stage"] * block), most_stages)
         assert stages >= 1 and stages * p["per_stage"] * block + slack <= smem, (s, p)
         assert (parts - 1) * 128 * (bn // parts + 4) * 4 + 1024 <= smem, (s, p)
+
+
+def test_stages_and_clusters_where_they_were_measured(plan):
+    """Tokens, entries of the sum, channels: stages of one block, of several, and clusters, each where the others took longer."""
+    one = [(320, 4096, 4096), (576, 4096, 4096), (128, 4096, 11008), (80, 8192, 8192), (192, 8192, 8192), (512, 11008, 4096), (640, 12288, 2304), (900, 2048, 2048),
+           (320, 11008, 4096), (384, 11008, 4096), (384, 13824, 5120), (1200, 8192, 1024), (129, 512, 1408)]
+    for s, p in zip(one, plan([s + B200 for s in one])):
+        assert p["parts"] == p["slices"] == p["per_stage"] == 1 and not p["pair"], (s, p)
+    several = [(5, 13824, 5120), (33, 13824, 5120), (16, 28672, 8192), (16, 2048, 2048), (80, 4096, 1024), (100, 4096, 4096), (512, 4096, 1024)]
+    for s, p in zip(several, plan([s + B200 for s in several])):
+        assert p["parts"] == p["slices"] == 1 and p["per_stage"] > 1 and not p["pair"], (s, p)
+    clusters = [(256, 11008, 4096), (128, 13824, 5120), (384, 28672, 4096), (400, 18944, 3584), (256, 5461, 2049), (640, 8192, 1024), (256, 28672, 8192)]
+    for s, p in zip(clusters, plan([s + B200 for s in clusters])):
+        assert p["parts"] > 1, (s, p)
