@@ -75,13 +75,15 @@ constexpr int kClusterTokens = 512;
 template <class Slots>
 inline ProductPlan plan_product(const ProductSize& p, Slots slots) {
     ProductPlan a = {};
-    int64_t tile = INT64_MAX, pair = INT64_MAX;
+    int64_t tile = INT64_MAX, pair = INT64_MAX, widest = INT64_MAX;
     int wide = 0;
     for (int bn = 32; bn <= 256; bn += 16)
         if (const int64_t cycles = tile_cycles(p, bn); cycles < tile) tile = cycles, a.bn = bn;
     for (int bn = 256; p.n > 128 && bn >= 128; bn -= 32)  // narrower where that fills the last round better
-        if (const int64_t cycles = pair_cycles(p, bn); cycles < pair) pair = cycles, wide = bn;
-    a.pair = pair < tile;
+        if (const int64_t cycles = pair_cycles(p, bn); cycles < pair) pair = cycles, wide = bn, widest = bn == 256 ? cycles : widest;
+    // The pace of narrow pairs is right beside wide ones, but a little too good beside tiles: where it promised less than 4 %, they took
+    // 0.99 to 1.09 times as long (12288 -> 2304, 900 tokens 29.5 us in tiles and 32.1, 8192 -> 1024, 2900 tokens 30.0 and 31.8).
+    a.pair = widest < tile || (p.n > 128 && pair + pair / 20 < tile);
     if (a.pair) a.bn = wide;
     // A few wide tiles with long sums: two or four CTAs to a tile.  A CTA finishes whole groups of eight channels.
     a.parts = 1;

@@ -294,3 +294,14 @@ def test_stages_and_clusters_where_they_were_measured(plan):
     clusters = [(256, 11008, 4096), (128, 13824, 5120), (384, 28672, 4096), (400, 18944, 3584), (256, 5461, 2049), (640, 8192, 1024), (256, 28672, 8192)]
     for s, p in zip(clusters, plan([s + B200 for s in clusters])):
         assert p["parts"] > 1, (s, p)
+
+
+def test_narrow_pairs_take_the_place_of_tiles_where_they_gain(plan):
+    """Tokens, entries of the sum, channels.  Measured in tiles and in narrow pairs: 29.5 and 32.1 us, 30.6 and 32.6, 27.7 and 29.2, 30.0 and
+    31.8, 21.0 and 22.1; then 68.7 and 67.0, 55.6 and 55.0, 138.6 and 134.9; and beside wide pairs, 52.4 and 51.3, 75.8 and 73.5."""
+    tiles = [(900, 12288, 2304), (1024, 12288, 2304), (2560, 8192, 1024), (2900, 8192, 1024), (3328, 4096, 1024)]
+    assert not any(p["pair"] for p in plan([s + (148, 0, 0) for s in tiles]))
+    narrow = [(1200, 14336, 4096), (1200, 11008, 4096), (1280, 28672, 4096), (900, 8192, 8192), (1408, 8192, 8192)]
+    assert all(p["pair"] and p["bn"] < 256 for p in plan([s + B200 for s in narrow]))
+    wide = [(4096, 8192, 28672), (2048, 4096, 11008), (4096, 4096, 4096)]
+    assert all(p["pair"] and p["bn"] == 256 for p in plan([s + B200 for s in wide]))
