@@ -305,3 +305,30 @@ def test_narrow_pairs_take_the_place_of_tiles_where_they_gain(plan):
     assert all(p["pair"] and p["bn"] < 256 for p in plan([s + B200 for s in narrow]))
     wide = [(4096, 8192, 28672), (2048, 4096, 11008), (4096, 4096, 4096)]
     assert all(p["pair"] and p["bn"] == 256 for p in plan([s + B200 for s in wide]))
+
+
+# ---- activations ----------------------------------------------------------------------------------------------------
+
+def test_the_stated_error_of_the_normal_distribution():
+    """The polynomial of by_normal with the coefficients as they stand in the source, against the function that it is fitted to."""
+    np, special = pytest.importorskip("numpy"), pytest.importorskip("scipy.special")
+    source = open(os.path.join(cuda_build.CSRC, "epilogue.cuh")).read()
+    comment, body = source[source.index("// z Phi(z)."):source.index("float by_normal(")], _body(source, "float by_normal(")
+    number = lambda text: float(np.float32(text))
+    root = number(re.search(r"__fmaf_rn\(([\d.]+)f, t, 1\.0f\)", body)[1])
+    coefficients = [number(re.search(r"float p = (-?[\d.]+)f", body)[1])] + [number(c) for c in re.findall(r"p = __fmaf_rn\(p, s, (-?[\d.]+)f\)", body)]
+    assert len(coefficients) == 9 and abs(root * 8 ** 0.5 - 1) < 2 ** -23
+    exact, rounded = (float(v) for v in re.search(r"off by ([\d.]+e-\d+) of its value, and with the roundings of float32 ([\d.]+e-\d+)", comment.replace("\n// ", " ")).groups())
+    t = np.linspace(0, 14, 400001, dtype=np.float32).astype(np.float64)
+    want = 0.5 * special.erfcx(t / np.sqrt(2))
+    s, p = 1 / (1 + root * t), np.zeros_like(t)
+    for c in coefficients:
+        p = p * s + c
+    worst = np.abs(s * p / want - 1).max()
+    assert 0.95 * exact < worst < exact
+    single = lambda v: v.astype(np.float32).astype(np.float64)
+    s, p = single(1 / single(root * t + 1)), np.zeros_like(t)
+    for c in coefficients:
+        p = single(p * s + c)
+    assert 0.9 * rounded < np.abs(single(p * s) / want - 1).max() < 1.1 * rounded
+    assert 1.1 * rounded < 5 * 2.0 ** -22 / 2              # less than half of what the header allows where t is small
