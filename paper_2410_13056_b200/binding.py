@@ -480,7 +480,9 @@ def _at(t):
 
 
 def _on(t):
-    """The current stream of t's device."""
+    """The current stream of t's device, which has to be a GPU: kernels take addresses as they are."""
+    if not t.is_cuda:
+        raise ValueError("needs tensors on the GPU, got one on %s" % t.device)
     return torch._C._cuda_getCurrentRawStream(t.get_device())
 
 

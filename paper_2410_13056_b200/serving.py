@@ -34,7 +34,8 @@ def quantize_tokens(x, norm=None, eps=1e-6):
     n, d = x.shape
     codes = torch.empty(n, (d + 15) // 16 * 16, dtype=torch.int8, device=x.device)[:, :d]
     scale = torch.empty(n, dtype=torch.float32, device=x.device)
-    B.cmpq_norm_quantize_tokens(x, norm, eps, codes, scale)
+    with torch.cuda.device_of(x):
+        B.cmpq_norm_quantize_tokens(x, norm, eps, codes, scale)
     return codes, scale
 
 

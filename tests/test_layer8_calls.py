@@ -212,6 +212,52 @@ def test_weights_refuse_what_does_not_fit_and_keep_their_tensors():
     assert (w.codes, w.ld, w.scale, w.bias) == (w.tensors[0].data_ptr(), D, w.tensors[1].data_ptr(), w.tensors[2].data_ptr())
 
 
+def test_tensors_of_the_host_are_refused(monkeypatch):
+    """Before an address of theirs gets to a kernel."""
+    from paper_2410_13056_b200 import serving
+
+    made = []
+
+    class Library:
+        def __getattr__(self, name):
+            return lambda *a: made.append(name) or 0
+
+    monkeypatch.setattr(B, "lib", lambda: Library())
+    with pytest.raises(ValueError, match="GPU"):
+        serving.quantize_tokens(_new(F16, N, D))
+    with pytest.raises(ValueError, match="GPU"):
+        serving.quantize_tokens(_new(F16, N, D), _new(F16, D))
+    with pytest.raises(ValueError, match="GPU"):
+        B.cmpq_linear_i8_fused(_new(F16, N, D), _weights(O, D), O, _new(F16, N, O), _new(U8, 4096))
+    with pytest.raises(ValueError, match="GPU"):
+        B.cmpq_gated_i8(_new(F16, N, D), _weights(FF, D), _weights(FF, D), _weights(O, FF), FF, O, _new(F16, N, O), _new(U8, 256), _new(U8, 4096))
+    with pytest.raises(ValueError, match="GPU"):
+        B.cmpq_quantize_tokens(_new(F16, N, D), _new(I8, N, D), _new(F32, N))
+    assert not made
+
+
+def test_tokens_are_quantized_on_their_own_device(untouched, monkeypatch):
+    from paper_2410_13056_b200 import serving
+
+    at = []
+
+    class DeviceOf:
+        def __init__(self, t):
+            self.t = t
+
+        def __enter__(self):
+            at.append(self.t)
+
+        def __exit__(self, *_):
+            assert untouched == ["cmpq_norm_quantize_tokens"]
+            at.append("left")
+
+    monkeypatch.setattr(torch.cuda, "device_of", DeviceOf)
+    x = _new(F16, N, D)
+    serving.quantize_tokens(x)
+    assert at[0] is x and at[1:] == ["left"]
+
+
 # ---- how products are covered -------------------------------------------------------------------------------------
 
 PLAN = r"""
