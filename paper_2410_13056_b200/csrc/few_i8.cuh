@@ -47,7 +47,7 @@ struct TokenGroup {
         const bool there = 8 * g < A.d;
         w = NORM && there ? load8(A.norm.weight + 8 * g, A.d - 8 * g, A.norm.wide) : none;
 #pragma unroll
-        for (int r = 0; r < kFewTokens; ++r) x[r] = r < A.n && there ? load8_written(A.x + r * A.ldx + 8 * g, A.d - 8 * g, A.wide) : none;
+        for (int r = 0; r < kFewTokens; ++r) x[r] = r < A.n && there ? load8_ordinary<true>(A.x + r * A.ldx + 8 * g, A.d - 8 * g, A.wide) : none;
     }
 };
 constexpr int kFewHeld = 2;  // groups that a thread keeps

@@ -10,14 +10,18 @@ namespace cmpq {
 
 constexpr int kQtThreads = 256;
 
-// load8 of rows that this kernel writes too (a residual may be the output), or that one before it may have written while this
-// one was on its way: not through the read-only path, which is for memory that nobody writes as long as a kernel runs.
-__device__ __forceinline__ uint4 load8_written(const uint16_t* p, int64_t left, bool wide) {
-    if (wide && left >= 8) return __ldcg(reinterpret_cast<const uint4*>(p));
+// load8 without the read-only path, which is for memory that nobody writes as long as a kernel runs.  WRITTEN: of rows that a kernel
+// may have written while this one was on its way, from L2.  Else of rows that this kernel writes too (a residual may be the
+// output), entries that nobody but the reading thread writes, and it only later: ordinary loads, whose second half of a sector
+// is in L1 (777 tokens 11008 -> 4096 45.1 us, 46.2 from L2).
+template <bool WRITTEN>
+__device__ __forceinline__ uint4 load8_ordinary(const uint16_t* p, int64_t left, bool wide) {
+    const auto load = [](const auto* at) { return WRITTEN ? __ldcg(at) : __ldca(at); };
+    if (wide && left >= 8) return load(reinterpret_cast<const uint4*>(p));
     uint32_t w[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const uint32_t lo = 2 * i < left ? __ldcg(p + 2 * i) : 0u, hi = 2 * i + 1 < left ? __ldcg(p + 2 * i + 1) : 0u;
+        const uint32_t lo = 2 * i < left ? load(p + 2 * i) : 0u, hi = 2 * i + 1 < left ? load(p + 2 * i + 1) : 0u;
         w[i] = lo | hi << 16;
     }
     return make_uint4(w[0], w[1], w[2], w[3]);
@@ -203,8 +207,8 @@ __device__ __forceinline__ void store_rows(uint32_t tmem, int c0, int c1, const 
 template <int DT>
 __device__ __forceinline__ void load16(const uint16_t* p, int left, bool wide, float (&f)[16]) {
     float a[8], b[8];
-    widen8<DT>(load8_written(p, left, wide), a);
-    widen8<DT>(load8_written(p + 8, left - 8, wide), b);
+    widen8<DT>(load8_ordinary<false>(p, left, wide), a);
+    widen8<DT>(load8_ordinary<false>(p + 8, left - 8, wide), b);
 #pragma unroll
     for (int i = 0; i < 8; ++i) f[i] = a[i], f[i + 8] = b[i];
 }
@@ -279,7 +283,7 @@ template <int DT, int KIND>
 __device__ __forceinline__ void store_eight(const ProductArgs& A, const int (&z)[8], const int (&u)[8], const float2* scale_bias, const float2* up_scale_bias,
                                             float xs, uint16_t* y, const uint16_t* residual, int left) {
     float f[8];
-    if (KIND == kFinish && A.residual) widen8<DT>(load8_written(residual, left, A.wide_residual), f);
+    if (KIND == kFinish && A.residual) widen8<DT>(load8_ordinary<false>(residual, left, A.wide_residual), f);
     auto finish = [&](auto act) {
         uint32_t w[4];
 #pragma unroll
