@@ -16,7 +16,7 @@ __device__ __forceinline__ float gate_by(float z, float w) { return __fdividef(z
 // erfcx(t / sqrt(2)) / (2 s) for t up to 14, by least squares with weights raised where it was worst: with the coefficients as
 // they stand here, off by 9.3e-8 of its value, and with the roundings of float32 3.1e-7.  Relative accuracy is kept where Phi is
 // small, for which a library call takes three times as long: a layer of 53 tokens 4096 -> 11008 took 15.1 us with it, 13.4 so, 12.0
-// with silu; 4000 tokens 201, 172 and 145.  An infinite z stays so, and t is held where its square is finite.
+// with silu; 4000 tokens 201, 172 and 145.  Infinity stays so, and t is held where its square is finite.
 __device__ __forceinline__ float by_normal(float z) {
     const float t = fminf(fabsf(z), 1e18f), s = __fdividef(1.0f, __fmaf_rn(0.353553385f, t, 1.0f));
     float p = -0.0295344833f;

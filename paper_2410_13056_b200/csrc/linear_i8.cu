@@ -117,12 +117,11 @@ constexpr size_t kTileSmem = 208 << 10;
 // blocks fill the SMs; the weights pass through once and are the time while tokens are few.  Launched behind the
 // quantization of its tokens, a block asks for its first weights before that has ended.  A stage holds the
 // token rows that exist (to eight) and the channels'; the product reads on past those rows into whatever follows, which
-// only reaches accumulator rows that are not stored, and 16 KB behind the last stage are kept for it.  A stage holds as
-// many 128-byte blocks of the sum as make 48 KB, 64 KB above 32 tokens: with less of a row at a time memory is slower
-// (100 tokens 11008 -> 4096: a block at a time 27.5 us, 64 KB 18.3; 8 tokens 28672 -> 8192 53 and 45).
+// only reaches accumulator rows that are not stored, and 16 KB behind the last stage are kept for it.  A stage holds one
+// 128-byte block of the sum, or 48 to 64 KB of them where weights come from memory in narrow tiles (stage_of_one: why, and figures).
 //
-// Measured with the quantization in graphs, weights from memory: 8 tokens 4096 -> 4096 8.2 us, 8192 -> 28672 41.8 us (5.6 TB/s,
-// 0.85 of the copy rate); 53 tokens 4096 -> 11008 13.4 us (3.4 TB/s: launch, first loads and the last stage's way out are
+// Measured with the quantization in graphs, weights from memory: 8 tokens 4096 -> 4096 8.4 us, 8192 -> 28672 42.3 us (5.6 TB/s,
+// 0.85 of the copy rate); 53 tokens 4096 -> 11008 11.9 us (3.8 TB/s: launch, first loads and the last stage's way out are
 // half of it).  For these, weights as rows and the sum over a cluster took 1.5, 1.3 and 2.4 times as long.
 //
 // A gated tile's columns are bn / 2 channels of the gate and the same ones of the second projection, from maps of their own.
@@ -134,8 +133,8 @@ constexpr size_t kTileSmem = 208 << 10;
 //
 // kSplit: the sum of a tile is cut over two or four CTAs of a cluster, which lets a few wide tiles with long sums use all SMs and
 // reads the tokens fewer times than as many narrow tiles.  Each CTA then takes a part of the tile's channels and adds up what the
-// others send it of those.  128 tokens 28672 -> 1024: 40 us whole, 18 over four; 11008 -> 4096 19.4 and 16.9 over
-// two; 256 tokens 11008 -> 2048 19.0 and 15.7.
+// others send it of those.  128 tokens 28672 -> 1024: 40 us whole, 18 over four; 11008 -> 4096 19.4 and 16.7 over
+// four; 256 tokens 11008 -> 2048 19.0 and 15.4.
 //
 // ONE: a stage is one block of the sum.  The loops over the blocks are the time of an issuing thread, so they are written out without
 // those of a stage (4096 -> 4096, 320 tokens 12.6 us with both, 11.4 so).
