@@ -563,6 +563,7 @@ cmpq_status cmpq_cache_read(const cmpq_cache* cache, const cmpq_batch* batch, cm
 /* cmpq_cache_attention: for query row t (position p, head h, its key-value head h / (n_heads / n_kv_heads))
  *   out[t][h] = sum_j softmax_j(scale * q[t][h] . k_j) v_j    over the visible tokens j of its sequence:
  * j <= p, and j > p - window when window > 0; with causal = 0 all lens[s] tokens (window must be 0 then).
+ * CMPQ_ZERO_BEHIND, added to causal: rows of out past tok_off[n_seq] are set to 0 instead of being left alone.
  * A row that sees no token (a position below 0, a sequence of length 0) is 0.  lse (optional, fp32
  * [n_tok][n_heads]) receives the natural logarithm of the softmax's sum, -infinity for such a row.
  * q [n_tok][ldq], out [n_tok][ldo] of `dt`, heads next to each other; queries finite.
@@ -577,6 +578,7 @@ cmpq_status cmpq_cache_read(const cmpq_cache* cache, const cmpq_batch* batch, cm
  * they have ended: zero them once, after allocating the buffer and after bit 3 of `word`, which every call on the buffer
  * reports from then on.  Calls that may run at the same time, graphs' replays among them, need buffers of their own. */
 #define CMPQ_ATTENTION_ZEROED 4096
+#define CMPQ_ZERO_BEHIND 0x100
 size_t cmpq_cache_attention_ws_bytes(int64_t n_seq, int64_t n_tok, int64_t max_new, int64_t max_len, int32_t n_heads,
                                      int32_t n_kv_heads, int32_t head_dim);
 cmpq_status cmpq_cache_attention(const cmpq_cache* cache, const cmpq_batch* batch, const void* q, int64_t ldq,

@@ -16,6 +16,7 @@ struct AttnArgs {
     int max_new, max_len, window;
     float scale;  // times log2(e): scores are kept in powers of two
     int n_heads, group, causal;
+    int zero_behind;  // rows of out behind the last sequence are set to 0
     int page_bits;  // log2 of a page's tokens
     int wide_q, wide_o;
     int32_t* word;
@@ -59,6 +60,18 @@ __device__ __forceinline__ uint32_t half_pair(uint32_t u, uint32_t pick) {
     const uint32_t h = __byte_perm(u, 0x64646464u, pick);
     const __half2 d = __hsub2(*reinterpret_cast<const __half2*>(&h), __halves2half2(__ushort_as_half(0x6480), __ushort_as_half(0x6480)));
     return *reinterpret_cast<const uint32_t*>(&d);
+}
+
+// Rows of out behind the last sequence, every `parts`-th of them, by `threads` threads; their stores need no waiting for.
+__device__ __forceinline__ void zero_behind(const AttnArgs& A, int64_t part, int64_t parts, int t, int threads) {
+    const int end = __ldg(A.b.tok_off + A.b.n_seq), width = A.n_heads * A.c.head_dim;
+    for (int64_t row = end + part; end >= 0 && row < A.b.n_tok; row += parts) {
+        uint16_t* o = A.out + row * A.ldo;
+        if (A.wide_o)
+            for (int i = 8 * t; i < width; i += 8 * threads) *reinterpret_cast<uint4*>(o + i) = make_uint4(0u, 0u, 0u, 0u);
+        else
+            for (int i = t; i < width; i += threads) o[i] = 0;
+    }
 }
 
 // An earlier call on this work space gave up: its counters cannot be relied on.

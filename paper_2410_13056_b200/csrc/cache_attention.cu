@@ -206,6 +206,7 @@ attention_rows_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_con
     }
 
     if (blockIdx.x == gridDim.x - 1 && tid == 127) report_stale(A);
+    if (A.zero_behind) zero_behind(A, blockIdx.x, gridDim.x, tid, 32 * C::kWarps);
 
     // The total, this warp's run, and the sequence it starts in: every warp for itself, 32 sequences at a time.
     int64_t total = 0, mine = 0, upto = 0;
@@ -686,17 +687,21 @@ extern "C" cmpq_status cmpq_cache_attention(const cmpq_cache* cache, const cmpq_
     if (!batch_ok(batch) || (dt != CMPQ_F16 && dt != CMPQ_BF16)) return CMPQ_ERR_INVALID_ARG;
     if (n_heads < 1 || n_heads > 4096 || n_heads % cache->n_kv_heads || max_new < 0 || max_new > INT32_MAX || max_len < 0 || max_len > INT32_MAX - 256)
         return CMPQ_ERR_INVALID_ARG;
+    const int zero = causal & CMPQ_ZERO_BEHIND;
+    causal &= ~CMPQ_ZERO_BEHIND;
     if (window < 0 || (window > 0 && !causal) || !(scale > 0.0f) || isinf(scale)) return CMPQ_ERR_INVALID_ARG;
     const int64_t row = (int64_t)n_heads * cache->head_dim;
     if (ldq < row || ldo < row) return CMPQ_ERR_INVALID_ARG;
-    if (batch->n_seq == 0 || batch->n_tok == 0) return CMPQ_OK;
+    if (batch->n_tok == 0 || (batch->n_seq == 0 && !zero)) return CMPQ_OK;
     if (!q || !out || !aligned_to(q, 2) || !aligned_to(out, 2) || !aligned_to(lse, 4)) return CMPQ_ERR_INVALID_ARG;
+    if (batch->n_seq == 0)
+        return cudaMemset2DAsync(out, ldo * 2, 0, row * 2, batch->n_tok, static_cast<cudaStream_t>(stream)) == cudaSuccess ? CMPQ_OK : CMPQ_ERR_CUDA;
     if (batch->n_tok * std::max(n_heads, cache->n_kv_heads) > INT32_MAX - 64) return CMPQ_ERR_UNSUPPORTED;
     if (!ws || !aligned_to(ws, 256) ||
         ws_bytes < cmpq_cache_attention_ws_bytes(batch->n_seq, batch->n_tok, max_new, max_len, n_heads, cache->n_kv_heads, cache->head_dim))
         return CMPQ_ERR_WORKSPACE;
     AttnArgs a{*cache, bounded(*batch), static_cast<const uint16_t*>(q), static_cast<uint16_t*>(out), lse, ldq, ldo, (int)max_new, (int)max_len,
-               (int)std::min<int64_t>(window, INT32_MAX), scale * kLog2e, n_heads, n_heads / cache->n_kv_heads, causal != 0,
+               (int)std::min<int64_t>(window, INT32_MAX), scale * kLog2e, n_heads, n_heads / cache->n_kv_heads, causal != 0, zero,
                31 - __builtin_clz(cache->page_tokens), aligned_to(q, 16) && ldq % 8 == 0, aligned_to(out, 16) && ldo % 8 == 0,
                word, static_cast<int*>(ws), reinterpret_cast<float*>(static_cast<char*>(ws) + CMPQ_ATTENTION_ZEROED), 0};
     auto st = static_cast<cudaStream_t>(stream);

@@ -134,6 +134,7 @@ attention_prefill_kernel(const __grid_constant__ AttnArgs A, const __grid_consta
     const int splits = plan.splits, unit = blockIdx.x / splits, z = blockIdx.x % splits;
     const int rb = plan.row_blocks - 1 - unit / plan.per_row_block, s = unit % plan.per_row_block / H, head = unit % H;
 
+    if (A.zero_behind && z == 0 && s == A.b.n_seq - 1) zero_behind(A, rb * H + head, (int64_t)plan.row_blocks * H, tid, kPfThreads);
     const int first = A.b.tok_off[s], n = A.b.tok_off[s + 1] - first, len = A.b.lens[s];
     if (len < 0 || len > A.max_len || n < 0 || n > A.max_new || first < 0 || (int64_t)first + n > A.b.n_tok) {
         if (tid == 0 && A.word) atomicOr(A.word, kWordTable);

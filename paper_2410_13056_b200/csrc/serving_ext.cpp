@@ -325,7 +325,7 @@ struct Cache {
 
     std::pair<Tensor, OptTensor> attend(const Tensor& q, const Tensor& off, const Tensor& lens, const Tensor& table, int64_t max_new,
                                         std::optional<int64_t> max_len, std::optional<double> scale, bool causal, int64_t window, const OptTensor& into,
-                                        bool want_lse) {
+                                        bool want_lse, bool zero_behind) {
         heads(q, "q", 0);
         const cmpq_dtype dt = code(q);
         const int64_t n = q.size(0), h = q.size(1);
@@ -342,7 +342,7 @@ struct Cache {
         const size_t bytes = cmpq_cache_attention_ws_bytes(b.n_seq, n, max_new, longest, (int32_t)h, c.n_kv_heads, c.head_dim);
         const Tensor ws = attention_spaces().get(q.device(), stream, bytes);
         check(cmpq_cache_attention(&c, &b, q.data_ptr(), rows(q, "q"), dt, (int32_t)h, max_new, longest,
-                                   scale ? (float)*scale : 1.0f / std::sqrt((float)c.head_dim), causal, window, out.data_ptr(), rows(out, "out"),
+                                   scale ? (float)*scale : 1.0f / std::sqrt((float)c.head_dim), causal | (zero_behind ? CMPQ_ZERO_BEHIND : 0), window, out.data_ptr(), rows(out, "out"),
                                    lse ? lse->data_ptr<float>() : nullptr, word.data_ptr<int32_t>(), ws.data_ptr(), ws.numel(), stream),
               "cmpq_cache_attention");
         return {out, lse};
@@ -389,7 +389,8 @@ PYBIND11_MODULE(_serving, m) {
         .def("append", &Cache::append, py::arg("k"), py::arg("v"), py::arg("tok_off"), py::arg("lens"), py::arg("table"), py::arg("q") = py::none(),
              py::arg("cos") = py::none(), py::arg("sin") = py::none(), py::arg("interleaved") = false, py::arg("q_out") = py::none())
         .def("read", &Cache::read)
-        .def("attend", &Cache::attend)
+        .def("attend", &Cache::attend, py::arg("q"), py::arg("tok_off"), py::arg("lens"), py::arg("table"), py::arg("max_new"), py::arg("max_len"), py::arg("scale"),
+             py::arg("causal"), py::arg("window"), py::arg("out"), py::arg("want_lse"), py::arg("zero_behind") = false)
         .def("check", &Cache::look)
         .def_readonly("k_codes", &Cache::k_codes)
         .def_readonly("k_scale", &Cache::k_scale)

@@ -125,10 +125,11 @@ class PagedCache8:
         return self._impl.read(tok_off, lens, table, n_tok, dtype is torch.bfloat16)
 
     def attend(self, q, tok_off, lens, table, max_new, max_len=None, scale=None, causal=True, window=0, out=None,
-               return_lse=False):
+               return_lse=False, zero_behind=False):
         """Attention of q [n_tok][heads][head_dim] over the cached tokens.  max_new, max_len: bounds of the new and of
-        the cached tokens of a sequence (max_len defaults to what the table can hold)."""
-        result = self._impl.attend(q, tok_off, lens, table, max_new, max_len, scale, causal, window, out, return_lse)
+        the cached tokens of a sequence (max_len defaults to what the table can hold).  Rows behind the last sequence are left
+        alone, or set to 0 with zero_behind."""
+        result = self._impl.attend(q, tok_off, lens, table, max_new, max_len, scale, causal, window, out, return_lse, zero_behind)
         return result if return_lse else result[0]
 
     def check(self):
@@ -157,8 +158,8 @@ class AttentionLayer8:
         y = self.qkv(x, norm=norm, eps=eps)
         q, k, v = (y[:, a * d: b * d].unflatten(1, (b - a, d)) for a, b in ((0, h), (h, h + kv), (h + kv, h + 2 * kv)))
         self.cache.append(k, v, tok_off, lens, table, q=q, cos=self.cos, sin=self.sin, interleaved=self.interleaved, q_out=q)
-        # rows behind the last sequence are left alone by the attention, and the projection behind it takes all rows
-        a = self.cache.attend(q, tok_off, lens, table, max_new, max_len, window=window, out=y.new_zeros(y.shape[0], h, d))
+        # the projection behind it takes all rows, those behind the last sequence too
+        a = self.cache.attend(q, tok_off, lens, table, max_new, max_len, window=window, zero_behind=True)
         return self.out(a.flatten(1), residual=residual)
 
     def check(self):

@@ -6,6 +6,7 @@ import torch
 
 import layer_ref as ref
 import test_gpu_layer8 as base
+from paper_2410_13056_b200 import binding as B
 from paper_2410_13056_b200 import serving
 from test_gpu_layer8 import DTYPES, EPS, H, KV, D, PAGE, WIDTH, i32
 
@@ -151,3 +152,59 @@ def test_captured_calls_take_a_state_only_where_blocks_meet_in_it():
         for y in out:
             y.zero_()
     block.check()
+
+
+# the kernel for few rows and the one for prompts, whose blocks share out the keys or not; outputs on 16 bytes and not
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("new,lens,heads,kv,d,page", [([1, 1, 1], [40, 300, 7], 8, 2, 64, 16), ([3, 0, 2], [90, 5, 64], 4, 4, 128, 64), ([0, 1], [9, 20], 6, 2, 256, 32),
+                                                      ([0, 0], [9, 0], 8, 2, 64, 16), ([200, 70], [500, 90], 8, 2, 64, 16), ([130, 0], [130, 40], 16, 1, 128, 64),
+                                                      ([0, 0, 300], [4, 4, 2000], 2, 2, 128, 128), ([300, 1], [300, 1], 64, 8, 64, 64)])
+def test_rows_behind_are_zeroed_where_that_is_asked_for(new, lens, heads, kv, d, page, dtype):
+    g = torch.Generator(device="cuda").manual_seed(3)
+    pages = -(-max(lens) // page)
+    c = serving.PagedCache8.empty(len(lens) * pages, kv, d, page)
+    for codes, scale in ((c.k_codes, c.k_scale), (c.v_codes, c.v_scale)):
+        codes.random_(-127, 128, generator=g), scale.uniform_(0.005, 0.02, generator=g)
+    table = torch.arange(len(lens) * pages, dtype=torch.int32, device="cuda").view(-1, pages)
+    n = sum(new)
+    off, lengths = i32(np.cumsum([0] + new)), i32(lens)
+    for rows in (n, n + 1, n + 37, n + 700):
+        q = torch.randn(rows, heads, d, device="cuda", generator=g).to(dtype)
+        for spare in (0, 3):                           # entries between the rows of the output
+            room = torch.full((rows + 1, heads * d + spare), 7.0, dtype=dtype, device="cuda")
+            out = room[:rows, : heads * d].unflatten(1, (heads, d))
+            for max_new in (max(1, *new), 700):        # the bound chooses the kernel
+                args = dict(max_new=max_new, max_len=max(lens), window=0)
+                want, lse = c.attend(q, off, lengths, table, out=out, return_lse=True, **args)
+                want = want[:n].clone()
+                assert torch.all(out[n:] == 7.0)       # left alone
+                got, again = c.attend(q, off, lengths, table, out=out, return_lse=True, zero_behind=True, **args)
+                assert torch.equal(got[:n], want) and torch.equal(again[:n], lse[:n]) and not got[n:].any()
+                assert torch.all(room[rows:] == 7.0) and torch.all(room[:, heads * d:] == 7.0)
+                room[:] = 7.0
+    c.check()
+
+
+def test_rows_behind_without_any_sequence():
+    c = serving.PagedCache8.empty(2, 2, 64, 16)
+    q, none = torch.ones(5, 4, 64, dtype=torch.float16, device="cuda"), i32([])
+    room = torch.full((6, 256 + 8), 7.0, dtype=torch.float16, device="cuda")
+    out = room[:5, :256].unflatten(1, (4, 64))
+    args = (i32([0]), none, torch.empty(0, 1, dtype=torch.int32, device="cuda"), 1, 16)
+    c.attend(q, *args, out=out)
+    assert torch.all(room == 7.0)
+    c.attend(q, *args, out=out, zero_behind=True)
+    assert not out.any() and torch.all(room[5:] == 7.0) and torch.all(room[:, 256:] == 7.0)
+    c.check()
+
+
+def test_offsets_that_do_not_fit_zero_nothing_out_of_range():
+    """What the host cannot see: the rows of a wrong batch are unspecified, nothing behind the array is written."""
+    c = serving.PagedCache8.empty(4, 2, 64, 16)
+    q = torch.ones(6, 4, 64, dtype=torch.float16, device="cuda")
+    room = torch.full((8, 256), 7.0, dtype=torch.float16, device="cuda")
+    for last in (7, 1 << 30, -1, -(1 << 31)):
+        c.attend(q, i32([0, last]), i32([3]), i32([[0, 1]]), 1, 16, out=room[:6].unflatten(1, (4, 64)), zero_behind=True)
+        with pytest.raises(B.CmpqError) as e:
+            c.check()
+        assert e.value.status == 1 and torch.all(room[6:] == 7.0)

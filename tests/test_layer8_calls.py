@@ -41,6 +41,27 @@ for name, n, d_in, d_ff, d_out in %r:
 """
 
 
+def test_attention_that_zeroes_rows_takes_its_arguments_as_it_did(L):
+    import ctypes
+
+    buf = (ctypes.c_char * 8192)()
+    p = (ctypes.addressof(buf) + 255) // 256 * 256
+    zero = 0x100
+    cache = B.Cache(k_codes=p, k_scale=p, v_codes=p, v_scale=p, n_pages=4, n_kv_heads=2, head_dim=64, page_tokens=16)
+
+    def attention(n_seq=2, n_tok=3, causal=1, window=0, out=p, q=p):
+        batch = B.Batch(tok_off=p, lens=p, table=p, ld_table=2, n_seq=n_seq, n_tok=n_tok)
+        return L.cmpq_cache_attention(cache, batch, q, 256, 0, 4, 2, 32, 0.1, causal, window, out, 256, None, None, None, 0, None)
+
+    invalid, workspace = 1, 3
+    for causal in (0, 1, zero, zero + 1):                  # all that comes next is the work space
+        assert attention(causal=causal) == workspace
+        assert attention(causal=causal, window=4) == (workspace if causal & 1 else invalid)
+        assert attention(causal=causal, out=None) == invalid
+        assert attention(causal=causal, n_tok=0, out=None) == 0
+        assert attention(causal=causal, n_seq=0, out=None) == (invalid if causal & zero else 0)
+
+
 def test_without_a_device_calls_answer_an_error(L):
     if torch.cuda.is_available():
         pytest.skip("the addresses are no GPU's")
