@@ -34,7 +34,7 @@ inline int64_t tile_cycles(const ProductSize& p, int bn) {
     return std::max(rounds * p.kblocks * pace, p.kblocks * 128 * p.cols / 3400) + rounds * (9000 + 8 * bn);
 }
 inline int64_t pair_cycles(const ProductSize& p, int bn) {
-    return ceil_div(ceil_div(p.n, 256) * ceil_div(p.cols, bn), p.sms / 2) * p.kblocks * (600 * (256 + bn) / 512) + 14000;  // the pace is that of the loads
+    return ceil_div(ceil_div(p.n, 256) * ceil_div(p.cols, bn), std::max<int64_t>(1, p.sms / 2)) * p.kblocks * (600 * (256 + bn) / 512) + 14000;  // the pace is that of the loads
 }
 
 // Slices of a tile's sum, for products that no cluster shares.  Shorter sums are not worth the adding up, and wider tiles wait for
@@ -48,7 +48,7 @@ inline int slices_of(const ProductSize& p, int bn) {
 // The same with `parts` CTAs of a cluster to a tile, or one, to compare the two.  Here the loads' way from L2 and the weights' from
 // memory delay one another, and a cluster pays 3300 cycles for its two barriers and for sums that cross it.  Fitted to 600 calls
 // of 5 to 512 tokens, 2304 x 512 to 28672 x 12288: what it chooses is 1 % slower than the best of them in the mean (14 % at most).
-// Over 169 calls that it gave to clusters, they took 0.79 of the time that tiles and pairs had taken (0.53 to 1.02).
+// Over 166 calls that it gave to clusters, they took 0.78 of the time that tiles and pairs had taken (0.54 to 1.02).
 inline int64_t parts_cycles(const ProductSize& p, int parts, int bn, int slots) {
     const int64_t rounds = ceil_div(ceil_div(p.n, 128) * ceil_div(p.cols, bn), slots);
     const int rows = tile_rows(p), slices = parts > 1 ? 1 : slices_of(p, bn);

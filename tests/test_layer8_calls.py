@@ -331,7 +331,7 @@ def test_clusters_do_not_take_the_place_of_pairs_past_their_fit(plan):
 def test_plans_fit_the_kernels(plan):
     """Shared memory, rows of an instruction, and whole groups of channels, over all sizes and on devices with few SMs."""
     smem, most_stages = 208 << 10, 40
-    sizes = [(n, d, o) + device for device in (B200, (148, 0, 0), (20, 10, 4), (2, 1, 0)) for n in TOKENS for d in SUMS for o in CHANNELS]
+    sizes = [(n, d, o) + device for device in (B200, (148, 0, 0), (20, 10, 4), (2, 1, 0), (1, 0, 0)) for n in TOKENS for d in SUMS for o in CHANNELS]
     for s, p in zip(sizes, plan(sizes)):
         n, d, _ = s[:3]
         rows, bn, parts, slices = p["rows"], p["bn"], p["parts"], p["slices"]
